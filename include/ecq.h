@@ -352,6 +352,58 @@ int ecq_step_static(uint64_t d, uint32_t bucket, uint32_t levels, float alpha, f
                     uint64_t seed, uint32_t W, uint32_t step, const float* const* grads,
                     float* err, float* out, void* cuda_stream);
 
+/* Element types of the operators below that take arrays of several. */
+#define ECQ_F32 0
+#define ECQ_BF16 1
+#define ECQ_F16 2
+
+/*
+ * Log probabilities of given tokens: where the gradient that the codec sends begins when the
+ * model is a language model (its loss), and what scoring and sampling with it need.  The codec's
+ * paper has no counterpart.  Per row of logits x [vocab], with z = x * inv_temperature:
+ *   lse       = ln sum_j exp z_j
+ *   logprob   = z_y - lse                       y the row's target
+ *   entropy   = - sum_j p_j ln p_j,  p_j = exp(z_j - lse)
+ *   top_*     the `top` largest z_j - lse and their indices, in descending order, equal
+ *             logits by index (the lower first)
+ * All arithmetic is fp32, whatever the logits' type; the sums' order is fixed by the shape.
+ *   logits    rows of `vocab` entries of type `dtype` (ECQ_F32, ECQ_BF16, ECQ_F16), row r at
+ *             entry r * row_stride (>= vocab); aligned to one element only
+ *   targets   [rows] or NULL (exactly when logprob is NULL).  A negative target is padding:
+ *             logprob 0.  A target >= vocab: logprob NaN.
+ *   inv_temperature   > 0, finite
+ *   top       0..min(vocab, ECQ_TOKEN_MAX_TOP); top_logprob and top_index are [rows * top],
+ *             NULL exactly when top is 0
+ *   logprob, entropy, lse   [rows] each or NULL, at least one output in all
+ * Logits of -inf are masked entries: probability 0, nothing to the entropy, no alternatives (a
+ * list that runs out of open entries ends in -inf with index -1).  Logits at the type's lowest
+ * finite value are ordinary entries.  A row with every entry at -inf has lse -inf, entropy 0 and
+ * a target's logprob -inf.  A row that holds a NaN or +inf gives NaN (indices -1).
+ * rows == 0 does nothing.  ECQ_ERR_ARG on a violation of the above, vocab > 2^30 or rows > 2^28.
+ * The current device's; one kernel launch; no workspace.
+ */
+#define ECQ_TOKEN_MAX_TOP 32
+int ecq_token_logprob(const void* logits, int dtype, uint64_t rows, uint32_t vocab, uint64_t row_stride,
+                      const int64_t* targets, float inv_temperature, uint32_t top, float* logprob,
+                      float* entropy, float* lse, float* top_logprob, int32_t* top_index,
+                      void* cuda_stream);
+
+/*
+ * Backward pass of ecq_token_logprob: the gradient of a loss with respect to the logits from its
+ * derivatives with respect to each row's logprob and entropy,
+ *   d_logits_j = inv_temperature * (d_logprob * ([j == y] - p_j) - d_entropy * p_j (ln p_j + entropy))
+ *   lse, entropy   as ecq_token_logprob wrote them (entropy may be NULL when d_entropy is)
+ *   d_logprob [rows], with targets, or both NULL; d_entropy [rows] or NULL; not both NULL.
+ *             Rows with a negative target have no part in d_logprob.
+ *   d_logits  the logits' type, row r at entry r * d_row_stride; may be the logits themselves
+ *             (same strides), must not overlap them otherwise
+ * Masked entries get 0, as do rows whose lse is -inf; rows whose lse is NaN get NaN.
+ */
+int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_t vocab, uint64_t row_stride,
+                           const int64_t* targets, float inv_temperature, const float* lse,
+                           const float* entropy, const float* d_logprob, const float* d_entropy,
+                           void* d_logits, uint64_t d_row_stride, void* cuda_stream);
+
 /*
  * Synchronise `cuda_stream`, then return and clear the context's sticky device
  * status: ECQ_OK, ECQ_ERR_NONFINITE, ECQ_ERR_TIMEOUT, or ECQ_ERR_CUDA if the

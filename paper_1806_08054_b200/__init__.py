@@ -14,4 +14,5 @@ from .binding import (  # noqa: F401
     ecq_step_host_workspace_bytes,
     ECQ_ERR_CAPACITY, ECQ_ERR_SYMBOL, ECQ_HUFFMAN_TABLE_BYTES, ecq_huffman_chunks, ecq_huffman_decode,
     ecq_huffman_encode, ecq_huffman_lengths, ecq_huffman_stream_bound, ecq_huffman_tables,
+    ECQ_BF16, ECQ_F16, ECQ_F32, ECQ_TOKEN_MAX_TOP, ecq_token_logprob, ecq_token_logprob_grad,
 )

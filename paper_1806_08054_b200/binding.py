@@ -95,6 +95,10 @@ def lib() -> ctypes.CDLL:
         L.ecq_huffman_encode.restype = i32
         L.ecq_huffman_decode.argtypes = [vp, vp, vp, u64, vp, vp, vp, vp]
         L.ecq_huffman_decode.restype = i32
+        L.ecq_token_logprob.argtypes = [vp, i32, u64, u32, u64, vp, f32, u32, vp, vp, vp, vp, vp, vp]
+        L.ecq_token_logprob.restype = i32
+        L.ecq_token_logprob_grad.argtypes = [vp, i32, u64, u32, u64, vp, f32, vp, vp, vp, vp, vp, u64, vp]
+        L.ecq_token_logprob_grad.restype = i32
         L.ecq_status.argtypes = [vp, vp]
         L.ecq_status.restype = i32
         L.ecq_launch_count.argtypes = []
@@ -393,3 +397,58 @@ def ecq_huffman_decode(ctx: int, tables: torch.Tensor, stream_words: torch.Tenso
                                   _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_huffman_decode")
+
+
+# ---- token log probabilities ----------------------------------------------------
+ECQ_F32, ECQ_BF16, ECQ_F16 = 0, 1, 2
+ECQ_TOKEN_MAX_TOP = 32
+_DTYPES = {torch.float32: ECQ_F32, torch.bfloat16: ECQ_BF16, torch.float16: ECQ_F16}
+
+
+def _rows(t: torch.Tensor, name: str):
+    """(address, dtype, rows, columns, row stride) of a [rows, columns] CUDA tensor."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor (there is no CPU path)" % name)
+    if t.dtype not in _DTYPES or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be float32, bfloat16 or float16 of two dimensions, the last one contiguous" % name)
+    return t.data_ptr(), _DTYPES[t.dtype], t.shape[0], t.shape[1], max(t.stride(0), t.shape[1]) if t.shape[0] < 2 else t.stride(0)
+
+
+def _vec(t, dtype, n: int, name: str):
+    if t is None:
+        return None
+    p = _dev(t, dtype, name)
+    if t.numel() != n:
+        raise ValueError("%s must have %d entries" % (name, n))
+    return p
+
+
+def ecq_token_logprob(logits: torch.Tensor, targets=None, logprob=None, entropy=None, lse=None, top_logprob=None,
+                      top_index=None, temperature: float = 1.0, stream=None) -> None:
+    """Log probability of each row's target, the row's entropy and logsumexp, and its best
+    alternatives ([rows, top] tensors), each where its output is given (see ecq.h)."""
+    p, dtype, rows, vocab, stride = _rows(logits, "logits")
+    top = 0 if top_index is None else (top_index.numel() // rows if rows else 0)
+    rc = lib().ecq_token_logprob(
+        p, dtype, rows, vocab, stride, _vec(targets, torch.int64, rows, "targets"), 1.0 / temperature, top,
+        _vec(logprob, torch.float32, rows, "logprob"), _vec(entropy, torch.float32, rows, "entropy"),
+        _vec(lse, torch.float32, rows, "lse"), _vec(top_logprob, torch.float32, rows * top, "top_logprob"),
+        _vec(top_index, torch.int32, rows * top, "top_index"), _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_token_logprob")
+
+
+def ecq_token_logprob_grad(logits: torch.Tensor, targets, lse: torch.Tensor, entropy, d_logprob, d_entropy,
+                           d_logits: torch.Tensor, temperature: float = 1.0, stream=None) -> None:
+    """Gradient with respect to the logits into ``d_logits`` (which may be ``logits``)."""
+    p, dtype, rows, vocab, stride = _rows(logits, "logits")
+    q, d_dtype, d_rows, d_vocab, d_stride = _rows(d_logits, "d_logits")
+    if (d_dtype, d_rows, d_vocab) != (dtype, rows, vocab):
+        raise ValueError("d_logits must have the shape and type of logits")
+    rc = lib().ecq_token_logprob_grad(
+        p, dtype, rows, vocab, stride, _vec(targets, torch.int64, rows, "targets"), 1.0 / temperature,
+        _vec(lse, torch.float32, rows, "lse"), _vec(entropy, torch.float32, rows, "entropy"),
+        _vec(d_logprob, torch.float32, rows, "d_logprob"), _vec(d_entropy, torch.float32, rows, "d_entropy"),
+        q, d_stride, _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_token_logprob_grad")

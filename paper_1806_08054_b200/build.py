@@ -7,14 +7,15 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libecq.so")
-SOURCES = ["ecq_api.cu"]
-HEADERS = ["ecq_common.cuh", "ecq_encode.cuh", "ecq_decode.cuh", "ecq_decode_ring.cuh", "ecq_stats.cuh", "ecq_entropy.cuh"]
+SOURCES = ["ecq_api.cu", "ecq_token.cu"]
+HEADERS = ["ecq_common.cuh", "ecq_encode.cuh", "ecq_decode.cuh", "ecq_decode_ring.cuh", "ecq_stats.cuh", "ecq_entropy.cuh",
+           "ecq_host.h", "ecq_elem.cuh", "ecq_token.cuh"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     # every fp32 operation of the codec is an explicit round-to-nearest intrinsic;
     # contraction is also switched off globally so nothing can be fused behind them
-    "-fmad=false", "-shared", "-Xcompiler", "-fPIC",
+    "-fmad=false", "-shared", "-Xcompiler", "-fPIC", "--threads", "0",
 ]
 
 

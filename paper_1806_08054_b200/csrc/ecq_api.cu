@@ -20,8 +20,11 @@
 #include "ecq_encode.cuh"
 #include "ecq_stats.cuh"
 #include "ecq_entropy.cuh"
+#include "ecq_host.h"
 
 using namespace ecq;
+
+std::atomic<uint64_t> ecq::g_launches{0};
 
 namespace {
 
@@ -45,8 +48,6 @@ cudaError_t launch_persistent(void (*kern)(KArgs...), uint32_t grid, uint32_t fu
     return cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
 }
 
-std::atomic<uint64_t> g_launches{0};
-
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                   const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -64,10 +65,6 @@ EncodeTiledFn tensor_map_encoder() {
     });
     return fn;
 }
-
-// Per-device set-up (kernel attributes, the built-in scratch's address) is kept in tables
-// indexed by the device ordinal; contexts on devices beyond them are refused.
-constexpr int kMaxDevices = 64;
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }

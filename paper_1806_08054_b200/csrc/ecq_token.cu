@@ -1,0 +1,117 @@
+// C ABI of the token log-probability operators: argument checks and launches.
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "../../include/ecq.h"
+#include "ecq_host.h"
+#include "ecq_token.cuh"
+
+using namespace ecq;
+
+namespace {
+
+template <typename T, bool ENT>
+int launch_forward(const TokenForward& P, uint64_t rows, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((uint32_t)(rows * P.cluster));
+    cfg.blockDim = dim3(kTokThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = P.cluster;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = P.cluster > 1 ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, token_logprob_kernel<T, ENT>, P) != cudaSuccess) {
+        cudaGetLastError();
+        return ECQ_ERR_CUDA;
+    }
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return ECQ_OK;
+}
+
+template <typename T>
+int launch_backward(const TokenBackward& P, cudaStream_t st) {
+    const uint64_t tasks = P.rows * P.chunks;
+    const uint32_t grid = tasks < 0x7FFFFFFFull ? (uint32_t)tasks : 0x7FFFFFFFu;
+    if (P.d_entropy) token_logprob_grad_kernel<T, true><<<grid, kTokGradThreads, 0, st>>>(P);
+    else token_logprob_grad_kernel<T, false><<<grid, kTokGradThreads, 0, st>>>(P);
+    if (cudaGetLastError() != cudaSuccess) return ECQ_ERR_CUDA;
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return ECQ_OK;
+}
+
+bool positive(float x) { return x > 0.f && x <= 3.402823466e38f; }
+
+bool bad_logits(const void* logits, int dtype, uint64_t rows, uint32_t vocab, uint64_t stride) {
+    const uint32_t es = dtype_bytes(dtype);
+    if (!es || !logits || !aligned_to(logits, es) || !vocab || vocab > 0x40000000u) return true;
+    return rows > 0x10000000ull || (rows > 1 && (stride < vocab || stride > 0x100000000ull));
+}
+
+}  // namespace
+
+extern "C" {
+
+int ecq_token_logprob(const void* logits, int dtype, uint64_t rows, uint32_t vocab, uint64_t row_stride,
+                      const int64_t* targets, float inv_temperature, uint32_t top, float* logprob,
+                      float* entropy, float* lse, float* top_logprob, int32_t* top_index,
+                      void* cuda_stream) {
+    if (rows == 0) return dtype_bytes(dtype) ? ECQ_OK : ECQ_ERR_ARG;
+    if (bad_logits(logits, dtype, rows, vocab, row_stride) || !positive(inv_temperature)) return ECQ_ERR_ARG;
+    if (top > ECQ_TOKEN_MAX_TOP || top > vocab) return ECQ_ERR_ARG;
+    if ((logprob != nullptr) != (targets != nullptr) || (top != 0) != (top_logprob != nullptr) ||
+        (top != 0) != (top_index != nullptr) || (!logprob && !entropy && !lse && !top))
+        return ECQ_ERR_ARG;
+    if (!aligned_to(targets, 8) || !aligned_to(logprob, 4) || !aligned_to(entropy, 4) || !aligned_to(lse, 4) ||
+        !aligned_to(top_logprob, 4) || !aligned_to(top_index, 4))
+        return ECQ_ERR_ARG;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return ECQ_ERR_CUDA;
+    TokenForward P = {logits, row_stride, targets, logprob, entropy, lse, top_logprob, top_index,
+                      vocab, top, 1, inv_temperature};
+    // A row is split over a cluster while there are fewer CTAs than SMs and each keeps a vector per thread.
+    const uint64_t row_bytes = (uint64_t)vocab * dtype_bytes(dtype);
+    while (P.cluster < (uint32_t)kTokMaxCluster && rows * P.cluster < (uint64_t)sms &&
+           row_bytes >= (uint64_t)P.cluster * 2 * kTokThreads * 16)
+        P.cluster *= 2;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    switch (dtype) {
+        case ECQ_F32: return entropy ? launch_forward<float, true>(P, rows, st) : launch_forward<float, false>(P, rows, st);
+        case ECQ_BF16:
+            return entropy ? launch_forward<__nv_bfloat16, true>(P, rows, st) : launch_forward<__nv_bfloat16, false>(P, rows, st);
+        default: return entropy ? launch_forward<__half, true>(P, rows, st) : launch_forward<__half, false>(P, rows, st);
+    }
+}
+
+int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_t vocab, uint64_t row_stride,
+                           const int64_t* targets, float inv_temperature, const float* lse,
+                           const float* entropy, const float* d_logprob, const float* d_entropy,
+                           void* d_logits, uint64_t d_row_stride, void* cuda_stream) {
+    if (rows == 0) return dtype_bytes(dtype) ? ECQ_OK : ECQ_ERR_ARG;
+    if (bad_logits(logits, dtype, rows, vocab, row_stride) || bad_logits(d_logits, dtype, rows, vocab, d_row_stride) ||
+        !positive(inv_temperature))
+        return ECQ_ERR_ARG;
+    if (!lse || (d_logprob != nullptr) != (targets != nullptr) || (d_entropy && !entropy) || (!d_logprob && !d_entropy))
+        return ECQ_ERR_ARG;
+    if (!aligned_to(targets, 8) || !aligned_to(lse, 4) || !aligned_to(entropy, 4) || !aligned_to(d_logprob, 4) ||
+        !aligned_to(d_entropy, 4))
+        return ECQ_ERR_ARG;
+    if (logits == d_logits && row_stride != d_row_stride && rows > 1) return ECQ_ERR_ARG;
+    TokenBackward P = {logits, d_logits, rows, row_stride, d_row_stride, targets, lse, entropy, d_logprob,
+                       d_entropy, vocab, 1, inv_temperature};
+    const uint32_t per = kTokGradThreads * kTokGradUnroll * (16u / dtype_bytes(dtype));
+    P.chunks = (vocab + per - 1) / per;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    switch (dtype) {
+        case ECQ_F32: return launch_backward<float>(P, st);
+        case ECQ_BF16: return launch_backward<__nv_bfloat16>(P, st);
+        default: return launch_backward<__half>(P, st);
+    }
+}
+
+}  // extern "C"

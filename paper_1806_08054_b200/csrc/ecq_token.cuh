@@ -1,0 +1,536 @@
+// Log probabilities of given tokens from a language model's logits, with the entropy of each row
+// and its best alternatives, and the backward pass to the logits.
+#pragma once
+
+#include <cfloat>
+#include <cstdint>
+
+#include "ecq_common.cuh"
+#include "ecq_elem.cuh"
+
+namespace ecq {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// ---- forward ---------------------------------------------------------------------------------
+//
+// With z_j = tau x_j (tau = 1 / temperature), m = max_j x_j, and in powers of two
+// d_j = (x_j - m) tau log2(e), a row needs
+//     s = sum_j 2^d_j,  t = sum_j 2^d_j d_j
+//     lse = tau m + ln s,  log p_y = tau (x_y - m) - ln s,  H = ln 2 (log2 s - t / s).
+// x_j - m is taken before the product with tau: near the maximum the difference is exact, and
+// entries masked with the type's lowest value cannot overflow to a 0/0.
+//
+// One pass over the logits: every thread carries (m, s, t) of the entries it has seen and rescales
+// s and t when a batch of its entries raises m; the threads' triples are merged by shuffles,
+// through shared memory, and across the CTAs of a cluster when a row is split over one.
+//
+// The best `top` entries need no second pass over the row: threads are taken in kTokGroups groups,
+// and the top-th largest of the groups' maxima is a bound that at least `top` entries reach, all of
+// them in the groups whose maximum reaches it.  Only those groups' entries (about top / kTokGroups
+// of the row) are read again, out of L2, and the few that reach the bound are ranked by counting.
+// Entries are ordered by value, equal ones by index (the lower first); a 64-bit key holds both.
+
+constexpr int kTokThreads = 256;
+constexpr int kTokGroups = 128;
+constexpr int kTokUnroll = 4;            // 16-byte vectors in flight per thread
+constexpr int kTokMaxTop = 32;
+constexpr int kTokMaxCluster = 8;
+constexpr int kTokCandidates = 1024;
+
+struct TokenForward {
+    const void* logits;
+    uint64_t row_stride;
+    const int64_t* targets;
+    float* logprob;
+    float* entropy;
+    float* lse;
+    float* top_logprob;
+    int32_t* top_index;
+    uint32_t vocab;
+    uint32_t top;
+    uint32_t cluster;                    // CTAs per row
+    float tau;
+};
+
+struct TokenSums { float m, s, t; };
+
+// Sums relative to a larger maximum.  The exponent is held at -1e4 (2^-1e4 is 0) so that the
+// initial m, the lowest finite value, and s = t = 0 give 0 and not 0 * inf.
+__device__ __forceinline__ void token_rescale(TokenSums& a, float m, float k) {
+    const float d = fmaxf(__fmul_rn(__fsub_rn(a.m, m), k), -1e4f);
+    const float f = ex2(d);
+    a.t = __fmul_rn(__fmaf_rn(a.s, d, a.t), f);
+    a.s = __fmul_rn(a.s, f);
+    a.m = m;
+}
+
+__device__ __forceinline__ void token_merge(TokenSums& a, TokenSums b, float k) {
+    const float m = fmaxf(a.m, b.m);
+    token_rescale(a, m, k);
+    token_rescale(b, m, k);
+    a.s = __fadd_rn(a.s, b.s);
+    a.t = __fadd_rn(a.t, b.t);
+}
+
+template <int N, bool ENT>
+__device__ __forceinline__ void token_add(TokenSums& a, const float* x, float k) {
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+    if (m > a.m) token_rescale(a, m, k);
+    float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float d = __fmul_rn(__fsub_rn(x[i], a.m), k);
+        const float e = ex2(d);
+        float& s = i & 1 ? s1 : s0;
+        float& t = i & 1 ? t1 : t0;
+        s = __fadd_rn(s, e);
+        // a masked entry has d = -inf and e = 0; it adds nothing to t
+        if (ENT) t = __fmaf_rn(e, fmaxf(d, -1e4f), t);
+    }
+    a.s = __fadd_rn(a.s, __fadd_rn(s0, s1));
+    if (ENT) a.t = __fadd_rn(a.t, __fadd_rn(t0, t1));
+}
+
+// Larger keys are better: value first, then the lower index.  0 is below every entry's key.
+__device__ __forceinline__ uint64_t token_key(float x, uint32_t index) {
+    const uint32_t b = __float_as_uint(__fadd_rn(x, 0.f));                 // -0 and 0 are equal
+    const uint32_t o = b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+    return ((uint64_t)o << 32) | (uint32_t)~index;
+}
+__device__ __forceinline__ float token_key_value(uint64_t key) {
+    const uint32_t o = (uint32_t)(key >> 32);
+    return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ uint32_t token_key_index(uint64_t key) { return ~(uint32_t)key; }
+
+// The part of a row that one CTA has: vectors [v0, v1) of the row's 16-byte aligned body, and
+// the single entries before or behind the body where this CTA is the first or the last.
+template <typename T>
+struct TokenSpan {
+    const T* row;
+    uint32_t head, nv, vocab;            // entries before the body, vectors of the body
+    uint32_t v0, v1;
+    bool first, last;
+
+    __device__ __forceinline__ uint32_t edge_index(uint32_t i, bool& have) const {
+        // i-th of the up to 2 * (16 / sizeof(T) - 1) single entries
+        constexpr uint32_t E = Elem<T>::kPer16;
+        if (i < E) { have = first && i < head; return i; }
+        const uint32_t j = head + nv * E + (i - E);
+        have = last && j < vocab;
+        return j;
+    }
+    __device__ __forceinline__ uint4 vec(uint32_t v) const {
+        return __ldg(reinterpret_cast<const uint4*>(row + head) + v);
+    }
+    __device__ __forceinline__ uint32_t vec_index(uint32_t v) const { return head + v * Elem<T>::kPer16; }
+};
+
+struct TokenShared {
+    uint64_t cand[kTokCandidates];
+    uint64_t lists[kTokMaxCluster][kTokMaxTop];      // rank 0: every CTA's best entries
+    TokenSums sums[kTokMaxCluster];                  // rank 0: every CTA's sums
+    TokenSums warp_sums[kTokThreads / 32];
+    float group_max[kTokGroups];
+    uint32_t flagged[kTokGroups];
+    uint32_t n_flagged, n_cand, warp_count[kTokThreads / 32];
+    uint64_t best;
+    float bound;
+};
+
+__device__ __forceinline__ void token_append(TokenShared& sm, uint64_t key) {
+    const uint32_t at = atomicAdd(&sm.n_cand, 1u);
+    if (at < (uint32_t)kTokCandidates) sm.cand[at] = key;
+}
+
+// Candidates of a CTA whose entries that reach the bound do not fit the list: a row of equal
+// entries, or one whose few open entries stand before a mask of the lowest finite value.  Entries
+// above the bound are collected first; if they fit, entries equal to it are taken in index order
+// until there are enough.  Otherwise (all of them in few groups) the best are taken one by one.
+template <typename T>
+__device__ __noinline__ void token_collect_slow(TokenShared& sm, const TokenSpan<T>& sp, uint32_t top) {
+    constexpr uint32_t E = Elem<T>::kPer16;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const float bound = sm.bound;
+    float x[E];
+    __syncthreads();
+    if (tid == 0) sm.n_cand = 0;
+    __syncthreads();
+    for (uint32_t v = sp.v0 + tid; v < sp.v1; v += kTokThreads) {
+        Elem<T>::widen(sp.vec(v), x);
+        for (uint32_t i = 0; i < E; ++i)
+            if (x[i] > bound) token_append(sm, token_key(x[i], sp.vec_index(v) + i));
+    }
+    if (tid < 2 * E) {
+        bool have;
+        const uint32_t j = sp.edge_index(tid, have);
+        if (have) { const float y = Elem<T>::load(sp.row + j); if (y > bound) token_append(sm, token_key(y, j)); }
+    }
+    __syncthreads();
+    uint32_t n = sm.n_cand;
+    if (n <= (uint32_t)kTokCandidates - kTokMaxTop) {
+        // ties in index order: head, body in chunks of one vector per thread, tail
+        for (int part = 0; part < 3 && n < top; ++part) {
+            const uint32_t begin = part == 1 ? sp.v0 : 0, end = part == 1 ? sp.v1 : 1;
+            for (uint32_t base = begin; base < end && n < top; base += kTokThreads) {
+                uint32_t mask = 0, index0 = 0;
+                if (part == 1) {
+                    if (base + tid < end) {
+                        index0 = sp.vec_index(base + tid);
+                        Elem<T>::widen(sp.vec(base + tid), x);
+                        for (uint32_t i = 0; i < E; ++i) mask |= (x[i] == bound ? 1u : 0u) << i;
+                    }
+                } else if (tid < E) {
+                    bool have;
+                    index0 = sp.edge_index(part == 0 ? tid : E + tid, have);
+                    mask = have && Elem<T>::load(sp.row + index0) == bound ? 1u : 0u;
+                }
+                const uint32_t mine = __popc(mask);
+                uint32_t before = mine;                              // inclusive prefix over the warp
+                for (int o = 1; o < 32; o <<= 1) {
+                    const uint32_t u = __shfl_up_sync(~0u, before, o);
+                    if (lane >= (uint32_t)o) before += u;
+                }
+                if (lane == 31) sm.warp_count[warp] = before;
+                __syncthreads();
+                uint32_t at = n + before - mine, all = 0;
+                for (uint32_t w = 0; w < kTokThreads / 32; ++w) {
+                    if (w < warp) at += sm.warp_count[w];
+                    all += sm.warp_count[w];
+                }
+                for (uint32_t i = 0; i < E; ++i)
+                    if ((mask >> i) & 1u) {
+                        if (at < top) sm.cand[at] = token_key(bound, index0 + i);
+                        ++at;
+                    }
+                n += all;
+                __syncthreads();
+            }
+        }
+        if (tid == 0) sm.n_cand = n < top ? n : (sm.n_cand > top ? sm.n_cand : top);
+        __syncthreads();
+        return;
+    }
+    uint64_t limit = ~0ull;
+    uint32_t found = 0;
+    for (; found < top; ++found) {
+        uint64_t best = 0;
+        for (uint32_t v = sp.v0 + tid; v < sp.v1; v += kTokThreads) {
+            Elem<T>::widen(sp.vec(v), x);
+            for (uint32_t i = 0; i < E; ++i) {
+                const uint64_t key = x[i] >= -FLT_MAX ? token_key(x[i], sp.vec_index(v) + i) : 0;
+                if (key < limit && key > best) best = key;
+            }
+        }
+        if (tid < 2 * E) {
+            bool have;
+            const uint32_t j = sp.edge_index(tid, have);
+            const float y = have ? Elem<T>::load(sp.row + j) : 0.f;
+            const uint64_t key = have && y >= -FLT_MAX ? token_key(y, j) : 0;
+            if (key < limit && key > best) best = key;
+        }
+        if (tid == 0) sm.best = 0;
+        __syncthreads();
+        if (best) atomicMax((unsigned long long*)&sm.best, (unsigned long long)best);
+        __syncthreads();
+        limit = sm.best;
+        if (limit == 0) break;
+        if (tid == 0) sm.cand[found] = limit;
+        __syncthreads();
+    }
+    __syncthreads();
+    if (tid == 0) sm.n_cand = found;
+    __syncthreads();
+}
+
+// The CTA's best `top` entries into sm.cand (any order, sm.n_cand of them, more than needed).
+template <typename T>
+__device__ __forceinline__ void token_collect(TokenShared& sm, const TokenSpan<T>& sp, float m, uint32_t top) {
+    constexpr uint32_t E = Elem<T>::kPer16;
+    constexpr uint32_t L = kTokThreads / kTokGroups;                  // threads per group
+    const uint32_t tid = threadIdx.x;
+#pragma unroll
+    for (uint32_t o = 1; o < L; o <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    if (tid % L == 0) sm.group_max[tid / L] = m;
+    if (tid == 0) { sm.n_cand = 0; sm.n_flagged = 0; }
+    __syncthreads();
+    if (tid < (uint32_t)kTokGroups) {
+        const float mine = sm.group_max[tid];
+        uint32_t rank = 0;
+        for (uint32_t g = 0; g < (uint32_t)kTokGroups; ++g) {
+            const float o = sm.group_max[g];
+            rank += (o > mine || (o == mine && g < tid)) ? 1u : 0u;
+        }
+        if (rank == top - 1) sm.bound = mine;
+    }
+    __syncthreads();
+    const float bound = sm.bound;
+    if (tid < (uint32_t)kTokGroups && sm.group_max[tid] >= bound) sm.flagged[atomicAdd(&sm.n_flagged, 1u)] = tid;
+    __syncthreads();
+    const uint32_t steps = (sp.v1 - sp.v0 + kTokThreads - 1) / kTokThreads;
+    const uint32_t per_group = steps * L;
+    const uint32_t work = sm.n_flagged * per_group;
+    for (uint32_t i = tid; i < work; i += kTokThreads) {
+        const uint32_t f = i / per_group, r = i - f * per_group;
+        const uint32_t v = sp.v0 + (r / L) * kTokThreads + sm.flagged[f] * L + r % L;
+        if (v >= sp.v1) continue;
+        float x[E];
+        Elem<T>::widen(sp.vec(v), x);
+#pragma unroll
+        for (uint32_t j = 0; j < E; ++j)
+            if (x[j] >= bound) token_append(sm, token_key(x[j], sp.vec_index(v) + j));
+    }
+    if (tid < 2 * E) {
+        bool have;
+        const uint32_t j = sp.edge_index(tid, have);
+        if (have) { const float y = Elem<T>::load(sp.row + j); if (y >= bound) token_append(sm, token_key(y, j)); }
+    }
+    __syncthreads();
+    if (sm.n_cand > (uint32_t)kTokCandidates) token_collect_slow<T>(sm, sp, top);
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void cluster_store(uint32_t addr, uint64_t v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_store(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+
+template <typename T, bool ENT>
+__global__ void __launch_bounds__(kTokThreads, 4) token_logprob_kernel(TokenForward P) {
+    constexpr uint32_t E = Elem<T>::kPer16;
+    __shared__ TokenShared sm;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t C = P.cluster, rank = blockIdx.x % C;
+    const uint64_t row = blockIdx.x / C;
+    if (C > 1) cluster_arrive();                                      // every CTA of the row has started
+
+    TokenSpan<T> sp;
+    sp.row = reinterpret_cast<const T*>(P.logits) + row * P.row_stride;
+    const uint32_t odd = (uint32_t)((16u - (reinterpret_cast<uintptr_t>(sp.row) & 15u)) & 15u) / (uint32_t)sizeof(T);
+    sp.vocab = P.vocab;
+    sp.head = odd < P.vocab ? odd : P.vocab;
+    sp.nv = (P.vocab - sp.head) / E;
+    const uint32_t per = (sp.nv + C - 1) / C;
+    sp.v0 = rank * per < sp.nv ? rank * per : sp.nv;
+    sp.v1 = sp.v0 + per < sp.nv ? sp.v0 + per : sp.nv;
+    sp.first = rank == 0;
+    sp.last = rank == C - 1;
+
+    const float k = __fmul_rn(P.tau, kLog2e);
+    TokenSums a = {-FLT_MAX, 0.f, 0.f};
+    uint32_t v = sp.v0 + tid;
+    for (; v + (kTokUnroll - 1) * kTokThreads < sp.v1; v += kTokUnroll * kTokThreads) {
+        uint4 raw[kTokUnroll];
+#pragma unroll
+        for (int u = 0; u < kTokUnroll; ++u) raw[u] = sp.vec(v + u * kTokThreads);
+        float x[kTokUnroll * E];
+#pragma unroll
+        for (int u = 0; u < kTokUnroll; ++u) Elem<T>::widen(raw[u], x + u * E);
+        token_add<kTokUnroll * E, ENT>(a, x, k);
+    }
+    for (; v < sp.v1; v += kTokThreads) {
+        float x[E];
+        Elem<T>::widen(sp.vec(v), x);
+        token_add<E, ENT>(a, x, k);
+    }
+    if (tid < 2 * E) {
+        bool have;
+        const uint32_t j = sp.edge_index(tid, have);
+        if (have) { const float x[1] = {Elem<T>::load(sp.row + j)}; token_add<1, ENT>(a, x, k); }
+    }
+
+    const float own_max = a.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        token_merge(a, {__shfl_xor_sync(~0u, a.m, o), __shfl_xor_sync(~0u, a.s, o), __shfl_xor_sync(~0u, a.t, o)}, k);
+    if (lane == 0) sm.warp_sums[warp] = a;
+    if (P.top) token_collect<T>(sm, sp, own_max, P.top);              // its barriers order warp_sums too
+    else __syncthreads();
+    if (C > 1) cluster_wait();
+
+    if (tid == 0) {
+        a = sm.warp_sums[0];
+        for (int w = 1; w < kTokThreads / 32; ++w) token_merge(a, sm.warp_sums[w], k);
+        const uint32_t to = cluster_addr(&sm.sums[rank], 0);
+        cluster_store(to, a.m); cluster_store(to + 4, a.s); cluster_store(to + 8, a.t);
+    }
+    if (P.top) {
+        const uint32_t n = sm.n_cand;
+        for (uint32_t i = n + tid; i < P.top; i += kTokThreads)
+            cluster_store(cluster_addr(&sm.lists[rank][i], 0), (uint64_t)0);
+        for (uint32_t i = tid; i < n; i += kTokThreads) {
+            const uint64_t key = sm.cand[i];
+            uint32_t better = 0;
+            for (uint32_t j = 0; j < n; ++j) better += sm.cand[j] > key ? 1u : 0u;
+            if (better < P.top) cluster_store(cluster_addr(&sm.lists[rank][better], 0), key);
+        }
+    }
+    if (C > 1) {
+        cluster_arrive();
+        cluster_wait();
+        if (rank != 0) return;
+    } else {
+        __syncthreads();
+    }
+
+    a = sm.sums[0];
+    for (uint32_t c = 1; c < C; ++c) token_merge(a, sm.sums[c], k);
+    const bool empty = a.s == 0.f;                                    // nothing left by the mask
+    const float ln_s = logf(a.s);                                     // -inf where empty, NaN where the row holds one
+    if (tid == 0) {
+        if (P.lse) P.lse[row] = empty ? -INFINITY : __fmaf_rn(a.m, P.tau, ln_s);
+        if (ENT) P.entropy[row] = empty ? 0.f : __fsub_rn(ln_s, __fmul_rn(kLn2, __fdiv_rn(a.t, a.s)));
+        if (P.logprob) {
+            const int64_t y = P.targets[row];
+            float lp = 0.f;
+            if (y >= (int64_t)P.vocab) lp = NAN;
+            else if (y >= 0)
+                lp = empty ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(Elem<T>::load(sp.row + y), a.m), P.tau), ln_s);
+            P.logprob[row] = lp;
+        }
+    }
+    if (P.top) {
+        const uint64_t* all = &sm.lists[0][0];
+        const bool valid = a.s > 0.f;                                 // false for NaN as well
+        const uint32_t n = C * P.top;
+        if (tid < P.top && !valid) {
+            P.top_logprob[row * P.top + tid] = empty ? -INFINITY : NAN;
+            P.top_index[row * P.top + tid] = -1;
+        }
+        if (valid && tid < n) {
+            const uint64_t key = all[(tid / P.top) * kTokMaxTop + tid % P.top];
+            uint32_t better = 0;
+            for (uint32_t c = 0; c < C; ++c)
+                for (uint32_t j = 0; j < P.top; ++j) {
+                    const uint64_t o = sm.lists[c][j];
+                    // absent entries (key 0) are ordered by their place
+                    better += o > key || (o == key && c * P.top + j < tid) ? 1u : 0u;
+                }
+            if (better < P.top) {
+                const float lp = __fsub_rn(__fmul_rn(__fsub_rn(token_key_value(key), a.m), P.tau), ln_s);
+                P.top_logprob[row * P.top + better] = key ? lp : -INFINITY;
+                P.top_index[row * P.top + better] = key ? (int32_t)token_key_index(key) : -1;
+            }
+        }
+    }
+}
+
+// ---- backward --------------------------------------------------------------------------------
+//
+// For a loss L with g = dL/d log p_y and e = dL/dH of a row, log p_j = tau x_j - lse,
+//     dL/dx_j = tau (g [j = y] - p_j (g + e (log p_j + H))).
+// One read of the logits, one write of their gradient; lse and H come from the forward pass.
+
+constexpr int kTokGradThreads = 256;
+constexpr int kTokGradUnroll = 4;
+
+struct TokenBackward {
+    const void* logits;
+    void* d_logits;
+    uint64_t rows, row_stride, d_row_stride;
+    const int64_t* targets;
+    const float* lse;
+    const float* entropy;
+    const float* d_logprob;
+    const float* d_entropy;
+    uint32_t vocab, chunks;              // CTAs' worth of vectors per row
+    float tau;
+};
+
+struct TokenRow { float lse, w, u, hit; uint32_t target; bool empty; };
+
+template <typename T, bool ENT, int N>
+__device__ __forceinline__ void token_grad(const TokenRow& r, const TokenBackward& P, uint32_t index, float* x) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float lp = __fmaf_rn(x[i], P.tau, -r.lse);
+        const float p = ex2(__fmul_rn(lp, kLog2e));
+        if (ENT) {
+            lp = fmaxf(lp, -1e30f);                                   // a masked entry: 0, not 0 * inf
+            x[i] = __fmul_rn(p, __fmaf_rn(r.u, lp, r.w));
+        } else {
+            x[i] = __fmul_rn(p, r.w);
+        }
+        if (r.empty) x[i] = 0.f;
+        if (index + i == r.target) x[i] = __fadd_rn(x[i], r.hit);
+    }
+}
+
+template <typename T, bool ENT>
+__global__ void __launch_bounds__(kTokGradThreads) token_logprob_grad_kernel(TokenBackward P) {
+    constexpr uint32_t E = Elem<T>::kPer16;
+    constexpr uint32_t kChunk = kTokGradThreads * kTokGradUnroll;
+    const uint32_t tid = threadIdx.x;
+    const uint64_t tasks = P.rows * P.chunks;
+    for (uint64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+        const uint64_t row = task / P.chunks;
+        const uint32_t chunk = (uint32_t)(task - row * P.chunks);
+        const T* in = reinterpret_cast<const T*>(P.logits) + row * P.row_stride;
+        T* out = reinterpret_cast<T*>(P.d_logits) + row * P.d_row_stride;
+        const uint32_t odd = (uint32_t)((16u - (reinterpret_cast<uintptr_t>(in) & 15u)) & 15u) / (uint32_t)sizeof(T);
+        const uint32_t head = odd < P.vocab ? odd : P.vocab;
+        const uint32_t nv = (P.vocab - head) / E;
+        const bool same = ((reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
+        const uint4* vin = reinterpret_cast<const uint4*>(in + head);
+        uint4 raw[kTokGradUnroll];
+        const uint32_t v0 = chunk * kChunk + tid;
+#pragma unroll
+        for (int u = 0; u < kTokGradUnroll; ++u)
+            if (v0 + u * kTokGradThreads < nv) raw[u] = vin[v0 + u * kTokGradThreads];
+
+        TokenRow r;
+        r.lse = P.lse[row];
+        r.empty = r.lse == -INFINITY;
+        const int64_t y = P.targets ? P.targets[row] : -1;
+        const float g = P.d_logprob && y >= 0 ? P.d_logprob[row] : 0.f;
+        r.target = y >= 0 && y < (int64_t)P.vocab && !r.empty ? (uint32_t)y : 0xFFFFFFFFu;
+        r.hit = __fmul_rn(P.tau, g);
+        if (ENT) {
+            const float e = P.d_entropy[row];
+            r.u = -__fmul_rn(P.tau, e);
+            r.w = -__fmul_rn(P.tau, __fmaf_rn(e, P.entropy[row], g));
+        } else {
+            r.u = 0.f;
+            r.w = -r.hit;
+        }
+        if (r.lse != r.lse) r.w = r.lse;                              // a row with a NaN gives NaN
+
+#pragma unroll
+        for (int u = 0; u < kTokGradUnroll; ++u) {
+            const uint32_t v = v0 + u * kTokGradThreads;
+            if (v >= nv) break;
+            const uint32_t index = head + v * E;
+            float x[E];
+            Elem<T>::widen(raw[u], x);
+            token_grad<T, ENT, (int)E>(r, P, index, x);
+            if (same) {
+                reinterpret_cast<uint4*>(out + head)[v] = Elem<T>::narrow(x);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < E; ++i) Elem<T>::store(out + index + i, x[i]);
+            }
+        }
+        if (chunk == P.chunks - 1 && tid < 2 * E) {
+            const uint32_t j = tid < E ? tid : head + nv * E + (tid - E);
+            if (tid < E ? tid < head : j < P.vocab) {
+                float x[1] = {Elem<T>::load(in + j)};
+                token_grad<T, ENT, 1>(r, P, j, x);
+                Elem<T>::store(out + j, x[0]);
+            }
+        }
+    }
+}
+
+}  // namespace ecq
