@@ -405,6 +405,86 @@ int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_
                            void* d_logits, uint64_t d_row_stride, void* cuda_stream);
 
 /*
+ * Orthogonalised matrix updates: what follows the exchange when the model's matrices are stepped
+ * by an orthogonalised momentum (as the Muon optimiser does) instead of the averaged gradient
+ * itself.  Like the codec it works on flat vectors, in which a plan says where the matrices lie.
+ * The codec's paper has no counterpart.  For each matrix, with m = min(rows, cols):
+ *   momentum <- mu * momentum + grad
+ *   U = nesterov ? grad + mu * momentum : momentum
+ *   X = U / |U|_F                                      (|.|_F the root of the sum of squares)
+ *   `steps` times:  X <- a X + (b G + c G^2) X,  G = X X^T   (X^T X from the right if rows > cols)
+ *   update = scale * X
+ *   params <- (1 - lr * decay) * params - lr * update
+ * The default a, b, c = 3.4445, -4.7750, 2.0315 in every step (5 of them are usual) bring the
+ * singular values of X to about 1 without converging to it.
+ *
+ * A zero matrix has a zero update.  A matrix whose U holds a NaN or Inf (or whose sum does) has a
+ * zero update, its momentum and params are left as they are, and ECQ_ERR_NONFINITE becomes
+ * pending (ecq_muon_status); the others are not affected.
+ *
+ * Entries of the flat vectors that belong to no matrix are neither read nor written.  Matrices of
+ * one plan must not overlap.
+ *
+ * ecq_muon_create
+ *   count        1..ECQ_MUON_MAX_COUNT matrices; the arrays are HOST, read before the call returns
+ *   offsets      first entry of each matrix in the flat vectors (no alignment needed)
+ *   rows, cols   1..ECQ_MUON_MAX_SIDE, the smaller of the two at most ECQ_MUON_MAX_RANK
+ *   strides      entries from one row to the next (>= cols), or NULL: cols
+ *   scales       factor of each matrix's update, or NULL: 1
+ *   steps        1..ECQ_MUON_MAX_STEPS
+ *   coefficients a, b, c of each step, or NULL for the defaults.  ECQ_ERR_ARG if some singular
+ *                value in (0, 1] would leave the range that the kernels' fp16 copies hold
+ *                (iterates up to 8, |b| s^2 + |c| s^4 up to 128).
+ *   precision    ECQ_MUON_HALF: operands of the products rounded to 11 bits, X kept with 22; the
+ *                result is within about 1e-3 of exact (relative, 2-norm).
+ *                ECQ_MUON_SPLIT: all operands with 22 bits, three times the products; the error of
+ *                fp32 arithmetic.
+ *                ECQ_MUON_AUTO: HALF where a call's outputs are bf16 alone, else SPLIT.
+ *   The plan holds its tables on the current device; ECQ_ERR_ALLOC / ECQ_ERR_CUDA if that fails.
+ * ecq_muon_destroy  NULL is allowed.  Do not destroy a plan with work in flight.
+ * ecq_muon_set_tiles  tile of the product kernel: 256 x 256 by pairs of CTAs, 128 x 128 or
+ *                128 x 64 by one; AUTO: the largest of which there are enough for every SM.  The
+ *                result may differ in the last bits of the sums.
+ * ecq_muon_set_wait_limit  as ecq_set_wait_limit: polls before an in-kernel wait gives up and
+ *                ECQ_ERR_TIMEOUT becomes pending.
+ * ecq_muon_bind  gives the plan its scratch memory: at least ecq_muon_workspace_bytes() bytes,
+ *                256-byte aligned, owned by the caller and left alone until the plan is bound
+ *                anew or destroyed.  Waits for `cuda_stream`.  A plan's calls share it: they must be
+ *                ordered, on one stream or by events.
+ * ecq_muon_orthogonalize  update = X alone (scale not applied) of the matrices in `in`, for flat
+ *                vectors of ECQ_F32, ECQ_BF16 or ECQ_F16; in == out is allowed for equal types.
+ * ecq_muon_step  params or update may be NULL, not both.  update is a flat vector of
+ *                `update_dtype`.  0 <= mu <= 1; lr, decay >= 0.  The vectors must not overlap.
+ * All vectors are 16-byte aligned, ECQ_ERR_ARG otherwise or before the plan is bound.
+ * ecq_muon_status  as ecq_status.
+ */
+typedef struct ecq_muon ecq_muon;
+#define ECQ_MUON_MAX_COUNT 65536
+#define ECQ_MUON_MAX_SIDE (1u << 22)
+#define ECQ_MUON_MAX_RANK 32768
+#define ECQ_MUON_MAX_STEPS 64
+#define ECQ_MUON_AUTO 0
+#define ECQ_MUON_HALF 1
+#define ECQ_MUON_SPLIT 2
+#define ECQ_MUON_TILES_AUTO 0
+#define ECQ_MUON_TILES_256X256 1
+#define ECQ_MUON_TILES_128X128 2
+#define ECQ_MUON_TILES_128X64 3
+int ecq_muon_create(ecq_muon** out, uint32_t count, const uint64_t* offsets, const uint32_t* rows,
+                    const uint32_t* cols, const uint64_t* strides, const float* scales, uint32_t steps,
+                    const float* coefficients, int precision);
+void ecq_muon_destroy(ecq_muon* plan);
+int ecq_muon_set_tiles(ecq_muon* plan, int tiles);
+int ecq_muon_set_wait_limit(ecq_muon* plan, uint32_t polls);
+uint64_t ecq_muon_workspace_bytes(const ecq_muon* plan);
+int ecq_muon_bind(ecq_muon* plan, void* workspace, uint64_t bytes, void* cuda_stream);
+int ecq_muon_orthogonalize(ecq_muon* plan, const void* in, int in_dtype, void* out, int out_dtype,
+                           void* cuda_stream);
+int ecq_muon_step(ecq_muon* plan, const float* grad, float* momentum, float mu, int nesterov, float lr,
+                  float decay, float* params, void* update, int update_dtype, void* cuda_stream);
+int ecq_muon_status(ecq_muon* plan, void* cuda_stream);
+
+/*
  * Synchronise `cuda_stream`, then return and clear the context's sticky device
  * status: ECQ_OK, ECQ_ERR_NONFINITE, ECQ_ERR_TIMEOUT, or ECQ_ERR_CUDA if the
  * stream itself reports an error.

@@ -15,4 +15,7 @@ from .binding import (  # noqa: F401
     ECQ_ERR_CAPACITY, ECQ_ERR_SYMBOL, ECQ_HUFFMAN_TABLE_BYTES, ecq_huffman_chunks, ecq_huffman_decode,
     ecq_huffman_encode, ecq_huffman_lengths, ecq_huffman_stream_bound, ecq_huffman_tables,
     ECQ_BF16, ECQ_F16, ECQ_F32, ECQ_TOKEN_MAX_TOP, ecq_token_logprob, ecq_token_logprob_grad,
+    ECQ_MUON_AUTO, ECQ_MUON_HALF, ECQ_MUON_SPLIT, ECQ_MUON_TILES_AUTO, ECQ_MUON_TILES_128X128, ECQ_MUON_TILES_128X64,
+    ECQ_MUON_TILES_256X256, ecq_muon_bind, ecq_muon_create, ecq_muon_destroy, ecq_muon_orthogonalize, ecq_muon_set_tiles,
+    ecq_muon_set_wait_limit, ecq_muon_status, ecq_muon_step, ecq_muon_workspace_bytes,
 )

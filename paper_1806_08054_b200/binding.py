@@ -99,6 +99,24 @@ def lib() -> ctypes.CDLL:
         L.ecq_token_logprob.restype = i32
         L.ecq_token_logprob_grad.argtypes = [vp, i32, u64, u32, u64, vp, f32, vp, vp, vp, vp, vp, u64, vp]
         L.ecq_token_logprob_grad.restype = i32
+        L.ecq_muon_create.argtypes = [ctypes.POINTER(vp), u32, vp, vp, vp, vp, vp, u32, vp, i32]
+        L.ecq_muon_create.restype = i32
+        L.ecq_muon_destroy.argtypes = [vp]
+        L.ecq_muon_destroy.restype = None
+        L.ecq_muon_set_tiles.argtypes = [vp, i32]
+        L.ecq_muon_set_tiles.restype = i32
+        L.ecq_muon_set_wait_limit.argtypes = [vp, u32]
+        L.ecq_muon_set_wait_limit.restype = i32
+        L.ecq_muon_workspace_bytes.argtypes = [vp]
+        L.ecq_muon_workspace_bytes.restype = u64
+        L.ecq_muon_bind.argtypes = [vp, vp, u64, vp]
+        L.ecq_muon_bind.restype = i32
+        L.ecq_muon_orthogonalize.argtypes = [vp, vp, i32, vp, i32, vp]
+        L.ecq_muon_orthogonalize.restype = i32
+        L.ecq_muon_step.argtypes = [vp, vp, vp, f32, i32, f32, f32, vp, vp, i32, vp]
+        L.ecq_muon_step.restype = i32
+        L.ecq_muon_status.argtypes = [vp, vp]
+        L.ecq_muon_status.restype = i32
         L.ecq_status.argtypes = [vp, vp]
         L.ecq_status.restype = i32
         L.ecq_launch_count.argtypes = []
@@ -452,3 +470,106 @@ def ecq_token_logprob_grad(logits: torch.Tensor, targets, lse: torch.Tensor, ent
         q, d_stride, _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_token_logprob_grad")
+
+
+# ---- orthogonalised matrix updates ------------------------------------------------
+ECQ_MUON_AUTO, ECQ_MUON_HALF, ECQ_MUON_SPLIT = 0, 1, 2
+ECQ_MUON_TILES_AUTO, ECQ_MUON_TILES_256X256, ECQ_MUON_TILES_128X128, ECQ_MUON_TILES_128X64 = 0, 1, 2, 3
+_muon_entries = {}      # plan -> entries a flat vector needs
+_muon_keep = {}         # plan -> its workspace
+
+
+def ecq_muon_create(offsets: Sequence[int], rows: Sequence[int], cols: Sequence[int], strides=None, scales=None,
+                    steps: int = 5, coefficients=None, precision: int = ECQ_MUON_AUTO) -> int:
+    """Plan of the matrices of a flat vector (see ecq.h); ``coefficients`` is a sequence of ``steps``
+    triples.  Bind a workspace to it with :func:`ecq_muon_bind` before use."""
+    n = len(offsets)
+    if not (len(rows) == len(cols) == n) or (strides is not None and len(strides) != n) or \
+            (scales is not None and len(scales) != n):
+        raise ValueError("offsets, rows, cols, strides and scales must have one entry per matrix")
+    if min([*offsets, *rows, *cols, *(strides or [0])], default=0) < 0:
+        raise ValueError("offsets, rows, cols and strides must not be negative")
+    flat = None
+    if coefficients is not None:
+        flat = [float(x) for triple in coefficients for x in triple]
+        if len(flat) != 3 * steps:
+            raise ValueError("coefficients must be three numbers per step")
+        flat = (ctypes.c_float * len(flat))(*flat)
+    h = ctypes.c_void_p()
+    rc = lib().ecq_muon_create(
+        ctypes.byref(h), n, (ctypes.c_uint64 * n)(*offsets), (ctypes.c_uint32 * n)(*rows), (ctypes.c_uint32 * n)(*cols),
+        None if strides is None else (ctypes.c_uint64 * n)(*strides),
+        None if scales is None else (ctypes.c_float * n)(*scales), steps, flat, precision)
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_muon_create")
+    ld = cols if strides is None else strides
+    _muon_entries[h.value] = max(o + (r - 1) * s + c for o, r, c, s in zip(offsets, rows, cols, ld))
+    return h.value
+
+
+def ecq_muon_destroy(plan: int) -> None:
+    _muon_entries.pop(plan, None)
+    _muon_keep.pop(plan, None)
+    lib().ecq_muon_destroy(plan)
+
+
+def ecq_muon_set_tiles(plan: int, tiles: int) -> None:
+    rc = lib().ecq_muon_set_tiles(plan, tiles)
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_muon_set_tiles")
+
+
+def ecq_muon_set_wait_limit(plan: int, polls: int) -> None:
+    rc = lib().ecq_muon_set_wait_limit(plan, polls)
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_muon_set_wait_limit")
+
+
+def ecq_muon_workspace_bytes(plan: int) -> int:
+    return int(lib().ecq_muon_workspace_bytes(plan))
+
+
+def ecq_muon_bind(plan: int, workspace: torch.Tensor, stream=None) -> None:
+    """Give the plan its scratch memory (any CUDA tensor of enough bytes, kept alive by the plan)."""
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    rc = lib().ecq_muon_bind(plan, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_muon_bind")
+    _muon_keep[plan] = workspace
+
+
+def _flat(plan: int, t: torch.Tensor, name: str, dtype=None) -> int:
+    if t.dtype not in _DTYPES:
+        raise ValueError("%s must be float32, bfloat16 or float16" % name)
+    p = _dev(t, dtype or t.dtype, name)
+    if t.numel() < _muon_entries[plan]:
+        raise ValueError("%s must have at least %d entries" % (name, _muon_entries[plan]))
+    return p
+
+
+def ecq_muon_orthogonalize(plan: int, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+    """Orthogonalise the plan's matrices of the flat vector ``src`` into ``dst``."""
+    rc = lib().ecq_muon_orthogonalize(plan, _flat(plan, src, "src"), _DTYPES[src.dtype], _flat(plan, dst, "dst"),
+                                      _DTYPES[dst.dtype], _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_muon_orthogonalize")
+
+
+def ecq_muon_step(plan: int, grad: torch.Tensor, momentum: torch.Tensor, params=None, update=None, *, mu: float = 0.95,
+                  nesterov: bool = True, lr: float = 0.0, decay: float = 0.0, stream=None) -> None:
+    """One optimiser step of the plan's matrices: ``momentum`` is updated in place, ``params`` are
+    stepped where they are given, and the update itself is written where ``update`` is."""
+    f32 = torch.float32
+    rc = lib().ecq_muon_step(
+        plan, _flat(plan, grad, "grad", f32), _flat(plan, momentum, "momentum", f32), mu, int(nesterov), lr, decay,
+        None if params is None else _flat(plan, params, "params", f32),
+        None if update is None else _flat(plan, update, "update"), 0 if update is None else _DTYPES[update.dtype],
+        _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_muon_step")
+
+
+def ecq_muon_status(plan: int, stream=None) -> int:
+    """Synchronise the stream and return (and clear) the plan's sticky device status."""
+    return int(lib().ecq_muon_status(plan, _stream(stream)))

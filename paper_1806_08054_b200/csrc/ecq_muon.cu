@@ -1,0 +1,443 @@
+// C ABI of the Newton-Schulz orthogonaliser: plan, tables, launches.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <mutex>
+#include <new>
+#include <vector>
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "../../include/ecq.h"
+#include "ecq_host.h"
+#include "ecq_muon.cuh"
+
+using namespace ecq;
+
+namespace {
+
+struct Step { float a, b, c, shift; };
+
+// Tile shapes of the product kernel: CTAs per tile and columns (rows are 128 a CTA).
+struct Shape { uint32_t cg, tn; };
+constexpr Shape kShapes[] = {{2, 256}, {1, 128}, {1, 64}};
+constexpr int kShapeCount = 3;
+
+uint64_t round64(uint64_t x) { return (x + 63) / 64 * 64; }
+
+}  // namespace
+
+struct ecq_muon {
+    int device, sms;
+    int precision;
+    int tiles;                           // ECQ_MUON_TILES_*
+    uint32_t wait_limit;
+    std::vector<Step> steps;
+    std::vector<MuonMat> mats;
+    uint64_t x_entries, g_entries;       // fp16 entries of one copy of X, of one of G or B
+    // device tables, one allocation
+    unsigned char* block;
+    MuonMat* d_mats;
+    MuonSpan* d_spans;
+    MuonTile *d_prep, *d_sym[kShapeCount], *d_full[kShapeCount];
+    double* d_partial;
+    uint32_t *d_sound, *d_status, *h_status;
+    unsigned char* d_maps;
+    uint32_t n_spans, n_prep, n_sym[kShapeCount], n_full[kShapeCount];
+    unsigned char* workspace;            // the caller's, NULL until bound
+};
+
+namespace {
+
+bool tensor_map(CUtensorMap* tm, const __half* base, uint64_t inner, uint64_t rows, uint64_t ld) {
+    typedef CUresult (*Fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                           const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                           CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static Fn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<Fn>(p);
+    });
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * 2};
+    const cuuint32_t box[2] = {64, 64}, unit[2] = {1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(base), dims, strides, box, unit,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+MuonWork work_of(const ecq_muon* p) {
+    MuonWork w;
+    __half* at = reinterpret_cast<__half*>(p->workspace);
+    for (int c = 0; c < 2; ++c) {
+        w.xh[c] = at; at += p->x_entries;
+        w.xl[c] = at; at += p->x_entries;
+    }
+    w.gh = at; at += p->g_entries;
+    w.gl = at; at += p->g_entries;
+    w.bh = at; at += p->g_entries;
+    w.bl = at;
+    return w;
+}
+
+uint64_t workspace_bytes(const ecq_muon* p) { return 8 * (p->x_entries + p->g_entries); }
+
+// Singular values start in (0, 1]; the scaled fp16 copies hold iterates up to 8 and polynomials
+// b s^2 + c s^4 up to 128.
+bool steps_in_range(const std::vector<Step>& steps) {
+    for (int i = 0; i <= 4096; ++i) {
+        double s = i / 4096.0;
+        for (const Step& k : steps) {
+            const double g = s * s;
+            if (!(std::fabs(k.b * g) + std::fabs(k.c * g * g) <= 128.0)) return false;
+            s = std::fabs(s * (k.a + k.b * g + k.c * g * g));
+            if (!(s <= 8.0)) return false;
+        }
+    }
+    return true;
+}
+
+void build_tiles(const ecq_muon* p, const Shape& shape, std::vector<MuonTile>& sym, std::vector<MuonTile>& full) {
+    const uint32_t tm = shape.cg * 128;
+    for (uint32_t i = 0; i < p->mats.size(); ++i) {
+        const MuonMat& mat = p->mats[i];
+        const uint32_t rb = (mat.m + tm - 1) / tm;
+        for (uint32_t r = 0; r < rb; ++r) {
+            // tiles of a symmetric product that touch the lower triangle
+            for (uint32_t c = 0; c * shape.tn < mat.m && c * shape.tn < (r + 1) * tm; ++c)
+                sym.push_back({i, (uint16_t)r, (uint16_t)c});
+            for (uint32_t c = 0; c * shape.tn < mat.n; ++c) full.push_back({i, (uint16_t)r, (uint16_t)c});
+        }
+    }
+}
+
+template <int CG, int TN, typename TO>
+int launch_product(const ecq_muon* p, const MuonPhase& ph, cudaStream_t st) {
+    using S = MuonShape<CG, TN>;
+    static std::once_flag once[kMaxDevices];
+    static int clusters[kMaxDevices];
+    auto kern = muon_product_kernel<CG, TN, TO>;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.blockDim = dim3(kMuonThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.attrs = at;
+    cfg.numAttrs = CG > 1 ? 1 : 0;
+    std::call_once(once[p->device], [&] {
+        int n = 0;
+        cfg.gridDim = dim3(p->sms / CG * CG);
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) return;
+        if (CG == 1) n = p->sms;
+        else if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) return;
+        clusters[p->device] = std::min(n, p->sms / CG);
+    });
+    if (clusters[p->device] <= 0) return ECQ_ERR_CUDA;
+    cfg.gridDim = dim3(std::min<uint32_t>(ph.n_tiles, clusters[p->device]) * CG);
+    cfg.stream = st;
+    if (cudaLaunchKernelEx(&cfg, kern, ph) != cudaSuccess) {
+        cudaGetLastError();
+        return ECQ_ERR_CUDA;
+    }
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return ECQ_OK;
+}
+
+template <typename TO>
+int launch_shape(const ecq_muon* p, int shape, const MuonPhase& ph, cudaStream_t st) {
+    switch (shape) {
+        case 0: return launch_product<2, 256, TO>(p, ph, st);
+        case 1: return launch_product<1, 128, TO>(p, ph, st);
+        default: return launch_product<1, 64, TO>(p, ph, st);
+    }
+}
+
+int choose_shape(const ecq_muon* p) {
+    if (p->tiles != ECQ_MUON_TILES_AUTO) return p->tiles - 1;
+    for (int s = 0; s < kShapeCount - 1; ++s)
+        if (p->n_full[s] * kShapes[s].cg >= (uint32_t)p->sms) return s;
+    return kShapeCount - 1;
+}
+
+int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int out_dtype, cudaStream_t st) {
+    const MuonWork ws = work_of(p);
+    const int terms = p->precision == ECQ_MUON_HALF ? 1
+                      : p->precision == ECQ_MUON_SPLIT ? 3
+                      : (out.params || out_dtype != ECQ_BF16) ? 3 : 1;
+    if (in.momentum) {
+        muon_norm_kernel<float, true><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
+        muon_prepare_kernel<float, true><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_status);
+    } else if (in_dtype == ECQ_F32) {
+        muon_norm_kernel<float, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
+        muon_prepare_kernel<float, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_status);
+    } else if (in_dtype == ECQ_BF16) {
+        muon_norm_kernel<__nv_bfloat16, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
+        muon_prepare_kernel<__nv_bfloat16, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_status);
+    } else {
+        muon_norm_kernel<__half, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
+        muon_prepare_kernel<__half, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_status);
+    }
+    if (cudaGetLastError() != cudaSuccess) return ECQ_ERR_CUDA;
+    g_launches.fetch_add(2, std::memory_order_relaxed);
+
+    const int shape = choose_shape(p);
+    MuonPhase ph = {};
+    ph.mats = p->d_mats;
+    ph.maps = p->d_maps;
+    ph.sound = p->d_sound;
+    ph.status = p->d_status;
+    ph.ws = ws;
+    ph.out = out;
+    ph.terms = terms;
+    ph.wait_limit = p->wait_limit;
+    const float sx = kMuonScaleX, sg = kMuonScaleG;
+    for (size_t k = 0; k < p->steps.size(); ++k) {
+        const Step& s = p->steps[k];
+        const float t = s.shift;
+        ph.src = (int)(k & 1);
+        ph.last = 0;
+        ph.kind = kMuonGram;
+        ph.tiles = p->d_sym[shape]; ph.n_tiles = p->n_sym[shape];
+        ph.lin = 0.f; ph.acc = sg / (sx * sx); ph.shift = sg * t;
+        int rc = launch_shape<float>(p, shape, ph, st);
+        if (rc != ECQ_OK) return rc;
+        ph.kind = kMuonPoly;
+        ph.lin = s.b + 2 * s.c * t; ph.acc = s.c / sg; ph.shift = 0.f;
+        rc = launch_shape<float>(p, shape, ph, st);
+        if (rc != ECQ_OK) return rc;
+        ph.kind = kMuonApply;
+        ph.tiles = p->d_full[shape]; ph.n_tiles = p->n_full[shape];
+        ph.last = k + 1 == p->steps.size();
+        ph.lin = s.a + s.b * t + s.c * t * t; ph.acc = 1.f / sg;
+        if (ph.last) { ph.lin /= sx; ph.acc /= sx; }
+        rc = !ph.last || out_dtype == ECQ_F32 || !out.update ? launch_shape<float>(p, shape, ph, st)
+             : out_dtype == ECQ_BF16 ? launch_shape<__nv_bfloat16>(p, shape, ph, st)
+                                     : launch_shape<__half>(p, shape, ph, st);
+        if (rc != ECQ_OK) return rc;
+    }
+    return ECQ_OK;
+}
+
+bool finite(float x) { return x - x == 0.f; }
+
+int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t* rows, const uint32_t* cols,
+           const uint64_t* strides, const float* scales, uint32_t steps, const float* coefficients) {
+    for (uint32_t k = 0; k < steps; ++k) {
+        Step s = {3.4445f, -4.7750f, 2.0315f, 0.f};
+        if (coefficients) s = {coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2], 0.f};
+        if (!finite(s.a) || !finite(s.b) || !finite(s.c)) return ECQ_ERR_ARG;
+        if (k + 2 >= steps && steps > 2) s.shift = 1.f;
+        p->steps.push_back(s);
+    }
+    if (!steps_in_range(p->steps)) return ECQ_ERR_ARG;
+    std::vector<MuonSpan> spans;
+    std::vector<MuonTile> prep, sym[kShapeCount], full[kShapeCount];
+    for (uint32_t i = 0; i < count; ++i) {
+        MuonMat mat = {};
+        mat.offset = offsets[i];
+        mat.rows = rows[i]; mat.cols = cols[i];
+        mat.stride = strides ? strides[i] : cols[i];
+        if (!mat.rows || !mat.cols || mat.rows > ECQ_MUON_MAX_SIDE || mat.cols > ECQ_MUON_MAX_SIDE ||
+            std::min(mat.rows, mat.cols) > ECQ_MUON_MAX_RANK || mat.stride < mat.cols || mat.stride > (1ull << 40) ||
+            mat.offset > (1ull << 48))
+            return ECQ_ERR_ARG;
+        mat.tall = mat.rows > mat.cols;
+        mat.m = std::min(mat.rows, mat.cols); mat.n = std::max(mat.rows, mat.cols);
+        mat.ld_x = (uint32_t)round64(mat.n); mat.ld_g = (uint32_t)round64(mat.m);
+        mat.scale = scales ? scales[i] : 1.f;
+        if (!finite(mat.scale)) return ECQ_ERR_ARG;
+        mat.x_at = p->x_entries; mat.g_at = p->g_entries;
+        p->x_entries += (uint64_t)mat.m * mat.ld_x;
+        p->g_entries += (uint64_t)mat.m * mat.ld_g;
+        // spans of about kMuonSpan entries: flat where the rows lie end to end, else whole rows or parts of them
+        mat.part0 = (uint32_t)spans.size();
+        if (mat.stride == mat.cols) {
+            const uint64_t all = (uint64_t)mat.rows * mat.cols;
+            for (uint64_t at = 0; at < all; at += kMuonSpan)
+                spans.push_back({mat.offset + at, 0, i, 1, (uint32_t)std::min<uint64_t>(kMuonSpan, all - at)});
+        } else {
+            const uint32_t per = std::max<uint32_t>(1, kMuonSpan / mat.cols);
+            for (uint32_t r = 0; r < mat.rows; r += per)
+                for (uint32_t c = 0; c < mat.cols; c += kMuonSpan)
+                    spans.push_back({mat.offset + (uint64_t)r * mat.stride + c, mat.stride, i, std::min(per, mat.rows - r),
+                                     std::min(kMuonSpan, mat.cols - c)});
+        }
+        mat.parts = (uint32_t)spans.size() - mat.part0;
+        for (uint32_t r = 0; r * 64 < mat.rows; ++r)
+            for (uint32_t c = 0; c * 64 < mat.cols; ++c) prep.push_back({i, (uint16_t)r, (uint16_t)c});
+        p->mats.push_back(mat);
+    }
+    for (int s = 0; s < kShapeCount; ++s) build_tiles(p, kShapes[s], sym[s], full[s]);
+    if (spans.size() > 0x7FFFFFFFull || prep.size() > 0x7FFFFFFFull) return ECQ_ERR_ARG;
+
+    uint64_t bytes = 0;
+    auto place = [&](uint64_t n) { const uint64_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
+    const uint64_t o_mats = place(count * sizeof(MuonMat)), o_spans = place(spans.size() * sizeof(MuonSpan));
+    const uint64_t o_prep = place(prep.size() * sizeof(MuonTile));
+    uint64_t o_sym[kShapeCount], o_full[kShapeCount];
+    for (int s = 0; s < kShapeCount; ++s) {
+        o_sym[s] = place(sym[s].size() * sizeof(MuonTile));
+        o_full[s] = place(full[s].size() * sizeof(MuonTile));
+    }
+    const uint64_t o_partial = place(spans.size() * 8), o_sound = place(count * 4ull), o_status = place(4);
+    const uint64_t o_maps = place((uint64_t)count * kMapsPerMat * 128);
+    std::vector<unsigned char> host(bytes, 0);
+    memcpy(host.data() + o_mats, p->mats.data(), count * sizeof(MuonMat));
+    memcpy(host.data() + o_spans, spans.data(), spans.size() * sizeof(MuonSpan));
+    memcpy(host.data() + o_prep, prep.data(), prep.size() * sizeof(MuonTile));
+    for (int s = 0; s < kShapeCount; ++s) {
+        memcpy(host.data() + o_sym[s], sym[s].data(), sym[s].size() * sizeof(MuonTile));
+        memcpy(host.data() + o_full[s], full[s].data(), full[s].size() * sizeof(MuonTile));
+    }
+    if (cudaGetDevice(&p->device) != cudaSuccess || p->device < 0 || p->device >= kMaxDevices ||
+        cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess)
+        return ECQ_ERR_CUDA;
+    if (cudaMalloc(&p->block, bytes) != cudaSuccess || cudaHostAlloc(&p->h_status, 4, cudaHostAllocDefault) != cudaSuccess) {
+        cudaGetLastError();
+        return ECQ_ERR_ALLOC;
+    }
+    if (cudaMemcpy(p->block, host.data(), bytes, cudaMemcpyHostToDevice) != cudaSuccess) return ECQ_ERR_CUDA;
+    p->d_mats = reinterpret_cast<MuonMat*>(p->block + o_mats);
+    p->d_spans = reinterpret_cast<MuonSpan*>(p->block + o_spans);
+    p->d_prep = reinterpret_cast<MuonTile*>(p->block + o_prep);
+    for (int s = 0; s < kShapeCount; ++s) {
+        p->d_sym[s] = reinterpret_cast<MuonTile*>(p->block + o_sym[s]);
+        p->d_full[s] = reinterpret_cast<MuonTile*>(p->block + o_full[s]);
+        p->n_sym[s] = (uint32_t)sym[s].size();
+        p->n_full[s] = (uint32_t)full[s].size();
+    }
+    p->d_partial = reinterpret_cast<double*>(p->block + o_partial);
+    p->d_sound = reinterpret_cast<uint32_t*>(p->block + o_sound);
+    p->d_status = reinterpret_cast<uint32_t*>(p->block + o_status);
+    p->d_maps = p->block + o_maps;
+    p->n_spans = (uint32_t)spans.size();
+    p->n_prep = (uint32_t)prep.size();
+    return ECQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ecq_muon_create(ecq_muon** out, uint32_t count, const uint64_t* offsets, const uint32_t* rows,
+                    const uint32_t* cols, const uint64_t* strides, const float* scales, uint32_t steps,
+                    const float* coefficients, int precision) {
+    if (!out) return ECQ_ERR_ARG;
+    *out = nullptr;
+    if (!count || count > ECQ_MUON_MAX_COUNT || !offsets || !rows || !cols || !steps || steps > ECQ_MUON_MAX_STEPS ||
+        precision < ECQ_MUON_AUTO || precision > ECQ_MUON_SPLIT)
+        return ECQ_ERR_ARG;
+    ecq_muon* p = new (std::nothrow) ecq_muon();
+    if (!p) return ECQ_ERR_ALLOC;
+    p->precision = precision;
+    p->wait_limit = ECQ_WAIT_LIMIT_DEFAULT;
+    int rc;
+    try {
+        rc = create(p, count, offsets, rows, cols, strides, scales, steps, coefficients);
+    } catch (const std::bad_alloc&) {
+        rc = ECQ_ERR_ALLOC;
+    }
+    if (rc != ECQ_OK) { ecq_muon_destroy(p); return rc; }
+    *out = p;
+    return ECQ_OK;
+}
+
+void ecq_muon_destroy(ecq_muon* p) {
+    if (!p) return;
+    if (p->block) cudaFree(p->block);
+    if (p->h_status) cudaFreeHost(p->h_status);
+    delete p;
+}
+
+int ecq_muon_set_tiles(ecq_muon* p, int tiles) {
+    if (!p || tiles < ECQ_MUON_TILES_AUTO || tiles > ECQ_MUON_TILES_128X64) return ECQ_ERR_ARG;
+    p->tiles = tiles;
+    return ECQ_OK;
+}
+
+int ecq_muon_set_wait_limit(ecq_muon* p, uint32_t polls) {
+    if (!p) return ECQ_ERR_ARG;
+    p->wait_limit = polls;
+    return ECQ_OK;
+}
+
+uint64_t ecq_muon_workspace_bytes(const ecq_muon* p) { return p ? workspace_bytes(p) : 0; }
+
+int ecq_muon_bind(ecq_muon* p, void* workspace, uint64_t bytes, void* cuda_stream) {
+    if (!p || !workspace || !aligned_to(workspace, 256) || bytes < workspace_bytes(p)) return ECQ_ERR_ARG;
+    if (cudaSetDevice(p->device) != cudaSuccess) return ECQ_ERR_CUDA;
+    p->workspace = static_cast<unsigned char*>(workspace);
+    const MuonWork w = work_of(p);
+    try {
+        std::vector<CUtensorMap> maps(p->mats.size() * kMapsPerMat);
+        for (size_t i = 0; i < p->mats.size(); ++i) {
+            const MuonMat& mat = p->mats[i];
+            const __half* x[4] = {w.xh[0], w.xl[0], w.xh[1], w.xl[1]};
+            const __half* g[4] = {w.gh, w.gl, w.bh, w.bl};
+            for (int k = 0; k < 4; ++k)
+                if (!tensor_map(&maps[i * kMapsPerMat + k], x[k] + mat.x_at, mat.n, mat.m, mat.ld_x) ||
+                    !tensor_map(&maps[i * kMapsPerMat + 4 + k], g[k] + mat.g_at, mat.m, mat.m, mat.ld_g)) {
+                    p->workspace = nullptr;
+                    return ECQ_ERR_CUDA;
+                }
+        }
+        cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+        if (cudaMemcpyAsync(p->d_maps, maps.data(), maps.size() * sizeof(CUtensorMap), cudaMemcpyHostToDevice, st) !=
+                cudaSuccess ||
+            cudaStreamSynchronize(st) != cudaSuccess) {
+            p->workspace = nullptr;
+            return ECQ_ERR_CUDA;
+        }
+    } catch (const std::bad_alloc&) {
+        p->workspace = nullptr;
+        return ECQ_ERR_ALLOC;
+    }
+    return ECQ_OK;
+}
+
+int ecq_muon_orthogonalize(ecq_muon* p, const void* in, int in_dtype, void* out, int out_dtype, void* cuda_stream) {
+    if (!p || !p->workspace || !in || !out || !dtype_bytes(in_dtype) || !dtype_bytes(out_dtype) || !aligned_to(in, 16) ||
+        !aligned_to(out, 16) || (in == out && in_dtype != out_dtype))
+        return ECQ_ERR_ARG;
+    const MuonIn i = {in, nullptr, 0.f, 0};
+    const MuonOut o = {nullptr, out, 1.f, 0.f, 0};
+    return iterate(p, i, in_dtype, o, out_dtype, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int ecq_muon_step(ecq_muon* p, const float* grad, float* momentum, float mu, int nesterov, float lr, float decay,
+                  float* params, void* update, int update_dtype, void* cuda_stream) {
+    if (!p || !p->workspace || !grad || !momentum || (!params && !update) || !aligned_to(grad, 16) ||
+        !aligned_to(momentum, 16) || !aligned_to(params, 16) || !aligned_to(update, 16) ||
+        (update && !dtype_bytes(update_dtype)))
+        return ECQ_ERR_ARG;
+    if (grad == momentum || (params && (params == grad || params == momentum || params == update)) ||
+        update == static_cast<const void*>(grad) || update == momentum)
+        return ECQ_ERR_ARG;
+    if (!(mu >= 0.f && mu <= 1.f) || !(lr >= 0.f) || !(decay >= 0.f) || !finite(lr) || !finite(decay) ||
+        !finite(lr * decay) || (nesterov != 0 && nesterov != 1))
+        return ECQ_ERR_ARG;
+    const MuonIn i = {grad, momentum, mu, nesterov};
+    const MuonOut o = {params, update, 1.f - lr * decay, lr, 1};
+    return iterate(p, i, ECQ_F32, o, update ? update_dtype : ECQ_F32, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int ecq_muon_status(ecq_muon* p, void* cuda_stream) {
+    if (!p) return ECQ_ERR_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (cudaMemcpyAsync(p->h_status, p->d_status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaMemsetAsync(p->d_status, 0, 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+        return ECQ_ERR_CUDA;
+    const uint32_t s = *p->h_status;
+    return s & kStatusTimeout ? ECQ_ERR_TIMEOUT : s & kStatusNonFinite ? ECQ_ERR_NONFINITE : ECQ_OK;
+}
+
+}  // extern "C"
