@@ -22,8 +22,8 @@ struct Step { float a, b, c, shift; };
 
 // Tile shapes of the product kernel: CTAs per tile and columns (rows are 128 a CTA).
 struct Shape { uint32_t cg, tn; };
-constexpr Shape kShapes[] = {{2, 256}, {1, 128}, {1, 64}};
-constexpr int kShapeCount = 3;
+constexpr Shape kShapes[] = {{2, 256}, {2, 128}, {1, 128}, {1, 64}};
+constexpr int kShapeCount = 4;
 
 uint64_t round64(uint64_t x) { return (x + 63) / 64 * 64; }
 
@@ -43,6 +43,8 @@ struct ecq_muon {
     MuonSpan* d_spans;
     MuonTile *d_prep, *d_sym[kShapeCount], *d_full[kShapeCount];
     double* d_partial;
+    MuonStep* d_steps;
+    unsigned long long *d_done, *d_next;
     uint32_t *d_sound, *d_status, *h_status;
     unsigned char* d_maps;
     uint32_t n_spans, n_prep, n_sym[kShapeCount], n_full[kShapeCount];
@@ -51,7 +53,9 @@ struct ecq_muon {
 
 namespace {
 
-bool tensor_map(CUtensorMap* tm, const __half* base, uint64_t inner, uint64_t rows, uint64_t ld) {
+// Map of a matrix of `rows` rows of `inner` fp16, read or written in boxes of box_rows x box_inner.
+bool tensor_map(CUtensorMap* tm, const __half* base, uint64_t inner, uint64_t rows, uint64_t ld, uint32_t box_inner,
+                uint32_t box_rows) {
     typedef CUresult (*Fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -66,9 +70,10 @@ bool tensor_map(CUtensorMap* tm, const __half* base, uint64_t inner, uint64_t ro
     });
     if (!fn) return false;
     const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * 2};
-    const cuuint32_t box[2] = {64, 64}, unit[2] = {1, 1};
+    const cuuint32_t box[2] = {box_inner, box_rows}, unit[2] = {1, 1};
     return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(base), dims, strides, box, unit,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, box_inner == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -117,19 +122,19 @@ void build_tiles(const ecq_muon* p, const Shape& shape, std::vector<MuonTile>& s
     }
 }
 
-template <int CG, int TN, typename TO>
-int launch_product(const ecq_muon* p, const MuonPhase& ph, cudaStream_t st) {
-    using S = MuonShape<CG, TN>;
+template <int CG, int TN, bool SPLIT>
+int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st) {
+    using S = MuonShape<CG, TN, SPLIT>;
     static std::once_flag once[kMaxDevices];
     static int clusters[kMaxDevices];
-    auto kern = muon_product_kernel<CG, TN, TO>;
+    auto kern = muon_iterate_kernel<CG, TN, SPLIT>;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = CG;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
-    cfg.blockDim = dim3(kMuonThreads);
+    cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.attrs = at;
     cfg.numAttrs = CG > 1 ? 1 : 0;
@@ -142,9 +147,12 @@ int launch_product(const ecq_muon* p, const MuonPhase& ph, cudaStream_t st) {
         clusters[p->device] = std::min(n, p->sms / CG);
     });
     if (clusters[p->device] <= 0) return ECQ_ERR_CUDA;
-    cfg.gridDim = dim3(std::min<uint32_t>(ph.n_tiles, clusters[p->device]) * CG);
+    it.shape = (uint32_t)shape;
+    it.sym = p->d_sym[shape]; it.n_sym = p->n_sym[shape];
+    it.full = p->d_full[shape]; it.n_full = p->n_full[shape];
+    cfg.gridDim = dim3(std::min<uint32_t>(it.n_full, clusters[p->device]) * CG);
     cfg.stream = st;
-    if (cudaLaunchKernelEx(&cfg, kern, ph) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, kern, it) != cudaSuccess) {
         cudaGetLastError();
         return ECQ_ERR_CUDA;
     }
@@ -152,20 +160,12 @@ int launch_product(const ecq_muon* p, const MuonPhase& ph, cudaStream_t st) {
     return ECQ_OK;
 }
 
-template <typename TO>
-int launch_shape(const ecq_muon* p, int shape, const MuonPhase& ph, cudaStream_t st) {
-    switch (shape) {
-        case 0: return launch_product<2, 256, TO>(p, ph, st);
-        case 1: return launch_product<1, 128, TO>(p, ph, st);
-        default: return launch_product<1, 64, TO>(p, ph, st);
-    }
-}
-
-int choose_shape(const ecq_muon* p) {
-    if (p->tiles != ECQ_MUON_TILES_AUTO) return p->tiles - 1;
-    for (int s = 0; s < kShapeCount - 1; ++s)
-        if (p->n_full[s] * kShapes[s].cg >= (uint32_t)p->sms) return s;
-    return kShapeCount - 1;
+// Tiles of a call: the plan's choice, or the largest of which there are enough for every SM.
+int choose_tiles(const ecq_muon* p, bool split) {
+    if (p->tiles != ECQ_MUON_TILES_AUTO) return p->tiles;
+    if (p->n_full[split ? 1 : 0] * 2 >= (uint32_t)p->sms) return ECQ_MUON_TILES_256X256;
+    if (p->n_full[2] >= (uint32_t)p->sms) return ECQ_MUON_TILES_128X128;
+    return ECQ_MUON_TILES_128X64;
 }
 
 int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int out_dtype, cudaStream_t st) {
@@ -175,56 +175,39 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
                       : (out.params || out_dtype != ECQ_BF16) ? 3 : 1;
     if (in.momentum) {
         muon_norm_kernel<float, true><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<float, true><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_status);
+        muon_prepare_kernel<float, true><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
     } else if (in_dtype == ECQ_F32) {
         muon_norm_kernel<float, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<float, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_status);
+        muon_prepare_kernel<float, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
     } else if (in_dtype == ECQ_BF16) {
         muon_norm_kernel<__nv_bfloat16, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<__nv_bfloat16, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_status);
+        muon_prepare_kernel<__nv_bfloat16, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
     } else {
         muon_norm_kernel<__half, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<__half, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_status);
+        muon_prepare_kernel<__half, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
     }
     if (cudaGetLastError() != cudaSuccess) return ECQ_ERR_CUDA;
     g_launches.fetch_add(2, std::memory_order_relaxed);
 
-    const int shape = choose_shape(p);
-    MuonPhase ph = {};
-    ph.mats = p->d_mats;
-    ph.maps = p->d_maps;
-    ph.sound = p->d_sound;
-    ph.status = p->d_status;
-    ph.ws = ws;
-    ph.out = out;
-    ph.terms = terms;
-    ph.wait_limit = p->wait_limit;
-    const float sx = kMuonScaleX, sg = kMuonScaleG;
-    for (size_t k = 0; k < p->steps.size(); ++k) {
-        const Step& s = p->steps[k];
-        const float t = s.shift;
-        ph.src = (int)(k & 1);
-        ph.last = 0;
-        ph.kind = kMuonGram;
-        ph.tiles = p->d_sym[shape]; ph.n_tiles = p->n_sym[shape];
-        ph.lin = 0.f; ph.acc = sg / (sx * sx); ph.shift = sg * t;
-        int rc = launch_shape<float>(p, shape, ph, st);
-        if (rc != ECQ_OK) return rc;
-        ph.kind = kMuonPoly;
-        ph.lin = s.b + 2 * s.c * t; ph.acc = s.c / sg; ph.shift = 0.f;
-        rc = launch_shape<float>(p, shape, ph, st);
-        if (rc != ECQ_OK) return rc;
-        ph.kind = kMuonApply;
-        ph.tiles = p->d_full[shape]; ph.n_tiles = p->n_full[shape];
-        ph.last = k + 1 == p->steps.size();
-        ph.lin = s.a + s.b * t + s.c * t * t; ph.acc = 1.f / sg;
-        if (ph.last) { ph.lin /= sx; ph.acc /= sx; }
-        rc = !ph.last || out_dtype == ECQ_F32 || !out.update ? launch_shape<float>(p, shape, ph, st)
-             : out_dtype == ECQ_BF16 ? launch_shape<__nv_bfloat16>(p, shape, ph, st)
-                                     : launch_shape<__half>(p, shape, ph, st);
-        if (rc != ECQ_OK) return rc;
-    }
-    return ECQ_OK;
+    MuonIterate m = {};
+    m.mats = p->d_mats;
+    m.maps = p->d_maps;
+    m.steps = p->d_steps;
+    m.n_steps = (uint32_t)p->steps.size();
+    m.sound = p->d_sound;
+    m.done = p->d_done;
+    m.next = p->d_next;
+    m.status = p->d_status;
+    m.out = out;
+    m.out_dtype = out_dtype;
+    m.wait_limit = p->wait_limit;
+    const int tiles = choose_tiles(p, terms == 3);
+    if (terms == 3)
+        return tiles == ECQ_MUON_TILES_256X256 ? launch_iterate<2, 128, true>(p, m, 1, st)
+                                               : launch_iterate<1, 64, true>(p, m, 3, st);
+    return tiles == ECQ_MUON_TILES_256X256   ? launch_iterate<2, 256, false>(p, m, 0, st)
+           : tiles == ECQ_MUON_TILES_128X128 ? launch_iterate<1, 128, false>(p, m, 2, st)
+                                             : launch_iterate<1, 64, false>(p, m, 3, st);
 }
 
 bool finite(float x) { return x - x == 0.f; }
@@ -276,7 +259,20 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
             for (uint32_t c = 0; c * 64 < mat.cols; ++c) prep.push_back({i, (uint16_t)r, (uint16_t)c});
         p->mats.push_back(mat);
     }
-    for (int s = 0; s < kShapeCount; ++s) build_tiles(p, kShapes[s], sym[s], full[s]);
+    for (int s = 0; s < kShapeCount; ++s) {
+        build_tiles(p, kShapes[s], sym[s], full[s]);
+        for (const MuonTile& t : sym[s]) ++p->mats[t.mat].tiles_sym[s];
+        for (const MuonTile& t : full[s]) ++p->mats[t.mat].tiles_full[s];
+        if ((2 * sym[s].size() + full[s].size()) * steps > 0x7FFFFFFFull) return ECQ_ERR_ARG;
+    }
+    const float sx = kMuonScaleX, sg = kMuonScaleG;
+    std::vector<MuonStep> table;
+    for (uint32_t k = 0; k < steps; ++k) {
+        // b G + c G^2 with G = D + t I; the products carry the scales of their operands
+        const Step& s = p->steps[k];
+        const float t = s.shift, out = k + 1 == steps ? 1.f / sx : 1.f;
+        table.push_back({s.b + 2 * s.c * t, s.c / sg, (s.a + s.b * t + s.c * t * t) * out, out / sg, sg * t});
+    }
     if (spans.size() > 0x7FFFFFFFull || prep.size() > 0x7FFFFFFFull) return ECQ_ERR_ARG;
 
     uint64_t bytes = 0;
@@ -289,10 +285,12 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
         o_full[s] = place(full[s].size() * sizeof(MuonTile));
     }
     const uint64_t o_partial = place(spans.size() * 8), o_sound = place(count * 4ull), o_status = place(4);
+    const uint64_t o_steps = place(steps * sizeof(MuonStep)), o_done = place(count * 8ull), o_next = place(8);
     const uint64_t o_maps = place((uint64_t)count * kMapsPerMat * 128);
     std::vector<unsigned char> host(bytes, 0);
     memcpy(host.data() + o_mats, p->mats.data(), count * sizeof(MuonMat));
     memcpy(host.data() + o_spans, spans.data(), spans.size() * sizeof(MuonSpan));
+    memcpy(host.data() + o_steps, table.data(), steps * sizeof(MuonStep));
     memcpy(host.data() + o_prep, prep.data(), prep.size() * sizeof(MuonTile));
     for (int s = 0; s < kShapeCount; ++s) {
         memcpy(host.data() + o_sym[s], sym[s].data(), sym[s].size() * sizeof(MuonTile));
@@ -318,6 +316,9 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     p->d_partial = reinterpret_cast<double*>(p->block + o_partial);
     p->d_sound = reinterpret_cast<uint32_t*>(p->block + o_sound);
     p->d_status = reinterpret_cast<uint32_t*>(p->block + o_status);
+    p->d_steps = reinterpret_cast<MuonStep*>(p->block + o_steps);
+    p->d_done = reinterpret_cast<unsigned long long*>(p->block + o_done);
+    p->d_next = reinterpret_cast<unsigned long long*>(p->block + o_next);
     p->d_maps = p->block + o_maps;
     p->n_spans = (uint32_t)spans.size();
     p->n_prep = (uint32_t)prep.size();
@@ -383,12 +384,19 @@ int ecq_muon_bind(ecq_muon* p, void* workspace, uint64_t bytes, void* cuda_strea
             const MuonMat& mat = p->mats[i];
             const __half* x[4] = {w.xh[0], w.xl[0], w.xh[1], w.xl[1]};
             const __half* g[4] = {w.gh, w.gl, w.bh, w.bl};
-            for (int k = 0; k < 4; ++k)
-                if (!tensor_map(&maps[i * kMapsPerMat + k], x[k] + mat.x_at, mat.n, mat.m, mat.ld_x) ||
-                    !tensor_map(&maps[i * kMapsPerMat + 4 + k], g[k] + mat.g_at, mat.m, mat.m, mat.ld_g)) {
-                    p->workspace = nullptr;
-                    return ECQ_ERR_CUDA;
-                }
+            CUtensorMap* to = &maps[i * kMapsPerMat];
+            bool ok = true;
+            for (int k = 0; k < 4 && ok; ++k) {
+                ok = tensor_map(to + kMapOperand + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 64, 64) &&
+                     tensor_map(to + kMapOperand + 4 + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 64, 64) &&
+                     tensor_map(to + kMapBlock + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 64, 32) &&
+                     tensor_map(to + kMapBlock + 4 + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 64, 32) &&
+                     tensor_map(to + kMapMirror + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 32, 64);
+            }
+            if (!ok) {
+                p->workspace = nullptr;
+                return ECQ_ERR_CUDA;
+            }
         }
         cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
         if (cudaMemcpyAsync(p->d_maps, maps.data(), maps.size() * sizeof(CUtensorMap), cudaMemcpyHostToDevice, st) !=
