@@ -21,9 +21,9 @@ namespace {
 struct Step { float a, b, c, shift; };
 
 // Tile shapes of the product kernel: CTAs per tile and columns (rows are 128 a CTA).
-struct Shape { uint32_t cg, tn; };
-constexpr Shape kShapes[] = {{2, 256}, {2, 128}, {1, 128}, {1, 64}};
-constexpr int kShapeCount = 4;
+struct Shape { uint32_t cg, tn; bool split; };
+constexpr Shape kShapes[] = {{2, 256, false}, {1, 128, false}, {1, 64, false}, {2, 128, true}, {1, 64, true}};
+constexpr int kShapeCount = 5;
 
 uint64_t round64(uint64_t x) { return (x + 63) / 64 * 64; }
 
@@ -37,25 +37,30 @@ struct ecq_muon {
     std::vector<Step> steps;
     std::vector<MuonMat> mats;
     uint64_t x_entries, g_entries;       // fp16 entries of one copy of X, of one of G or B
+    uint64_t xm_entries, gm_entries;     // entries of X and of G in block order
     // device tables, one allocation
     unsigned char* block;
     MuonMat* d_mats;
     MuonSpan* d_spans;
-    MuonTile *d_prep, *d_sym[kShapeCount], *d_full[kShapeCount];
+    MuonTile* d_prep;
+    MuonTask* d_tasks[kShapeCount];
     double* d_partial;
     MuonStep* d_steps;
     unsigned long long *d_done, *d_next;
     uint32_t *d_sound, *d_status, *h_status;
     unsigned char* d_maps;
-    uint32_t n_spans, n_prep, n_sym[kShapeCount], n_full[kShapeCount];
+    uint32_t n_spans, n_prep, n_tasks[kShapeCount];
+    uint64_t n_full[kShapeCount];        // tiles of one product with X, over all matrices
     unsigned char* workspace;            // the caller's, NULL until bound
 };
 
 namespace {
 
-// Map of a matrix of `rows` rows of `inner` fp16, read or written in boxes of box_rows x box_inner.
-bool tensor_map(CUtensorMap* tm, const __half* base, uint64_t inner, uint64_t rows, uint64_t ld, uint32_t box_inner,
-                uint32_t box_rows) {
+// Map of a matrix of `rows` rows of `inner` fp16, loaded in boxes of 64 entries of box_rows rows.
+// With `columns` it is taken as columns / 64 matrices of 64 columns each instead, next to each other,
+// `boxes` of which a box spans.
+bool tensor_map(CUtensorMap* tm, const __half* base, uint64_t inner, uint64_t rows, uint64_t ld, uint32_t box_rows,
+                uint64_t columns = 0, uint32_t boxes = 0) {
     typedef CUresult (*Fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -69,11 +74,10 @@ bool tensor_map(CUtensorMap* tm, const __half* base, uint64_t inner, uint64_t ro
             fn = reinterpret_cast<Fn>(p);
     });
     if (!fn) return false;
-    const cuuint64_t dims[2] = {inner, rows}, strides[1] = {ld * 2};
-    const cuuint32_t box[2] = {box_inner, box_rows}, unit[2] = {1, 1};
-    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(base), dims, strides, box, unit,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, box_inner == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    const cuuint64_t dims[3] = {columns ? 64 : inner, rows, columns / 64}, strides[2] = {ld * 2, 128};
+    const cuuint32_t box[3] = {64, box_rows, boxes}, unit[3] = {1, 1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, columns ? 3 : 2, const_cast<__half*>(base), dims, strides, box, unit,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -87,11 +91,15 @@ MuonWork work_of(const ecq_muon* p) {
     w.gh = at; at += p->g_entries;
     w.gl = at; at += p->g_entries;
     w.bh = at; at += p->g_entries;
-    w.bl = at;
+    w.bl = at; at += p->g_entries;
+    w.xm = reinterpret_cast<float*>(at);
+    w.gm = w.xm + p->xm_entries;
     return w;
 }
 
-uint64_t workspace_bytes(const ecq_muon* p) { return 8 * (p->x_entries + p->g_entries); }
+uint64_t workspace_bytes(const ecq_muon* p) {
+    return 8 * (p->x_entries + p->g_entries) + 4 * (p->xm_entries + p->gm_entries);
+}
 
 // Singular values start in (0, 1]; the scaled fp16 copies hold iterates up to 8 and polynomials
 // b s^2 + c s^4 up to 128.
@@ -108,19 +116,85 @@ bool steps_in_range(const std::vector<Step>& steps) {
     return true;
 }
 
-void build_tiles(const ecq_muon* p, const Shape& shape, std::vector<MuonTile>& sym, std::vector<MuonTile>& full) {
-    const uint32_t tm = shape.cg * 128;
-    for (uint32_t i = 0; i < p->mats.size(); ++i) {
-        const MuonMat& mat = p->mats[i];
-        const uint32_t rb = (mat.m + tm - 1) / tm;
-        for (uint32_t r = 0; r < rb; ++r) {
-            // tiles of a symmetric product that touch the lower triangle
-            for (uint32_t c = 0; c * shape.tn < mat.m && c * shape.tn < (r + 1) * tm; ++c)
-                sym.push_back({i, (uint16_t)r, (uint16_t)c});
-            for (uint32_t c = 0; c * shape.tn < mat.n; ++c) full.push_back({i, (uint16_t)r, (uint16_t)c});
+// Entries of the matrices that are worked on together.  Three such groups are under way at a time,
+// each with 8 bytes an entry of X, of which about half is alive: they about fill the L2 cache.
+constexpr uint64_t kGroupEntries = 12ull << 20;
+constexpr uint64_t kLanes = 3;
+
+// Tiles of all steps in the order in which they are handed out.  Matrices are taken in groups, and
+// kLanes groups at a time go through their products one by one in turn, a third of a step apart:
+// between a group's product and the next one, which waits for all of it, there is the other
+// groups' work.
+struct TaskList {
+    const std::vector<MuonMat>& mats;
+    Shape shape;
+    uint32_t steps;
+    bool split;
+    std::vector<MuonTask> tasks;
+    std::vector<uint64_t> sym, full;     // tiles per product, by matrix
+
+    TaskList(const std::vector<MuonMat>& all, Shape s, uint32_t n_steps, bool all_low)
+        : mats(all), shape(s), steps(n_steps), split(all_low), sym(all.size()), full(all.size()) {
+        for (size_t i = 0; i < mats.size(); ++i) {
+            const uint32_t tm = shape.cg * 128, rb = (mats[i].m + tm - 1) / tm;
+            for (uint32_t r = 0; r < rb; ++r) sym[i] += sym_columns(mats[i], r);
+            full[i] = (uint64_t)rb * ((mats[i].n + shape.tn - 1) / shape.tn);
         }
     }
-}
+    // tiles of row block r that touch the lower triangle
+    uint32_t sym_columns(const MuonMat& mat, uint32_t r) const {
+        return (std::min(mat.m, (r + 1) * shape.cg * 128) + shape.tn - 1) / shape.tn;
+    }
+    void add(uint32_t i, uint32_t step, int kind) {
+        const MuonMat& mat = mats[i];
+        const uint32_t tm = shape.cg * 128, rb = (mat.m + tm - 1) / tm;
+        const uint64_t need = step * (2 * sym[i] + full[i]) + kind * sym[i];
+        uint16_t flags = (uint16_t)kind;
+        if (kind == kMuonApply) {
+            // fp32 while small singular values are still to be amplified: an error made in the
+            // last two steps is not
+            if (split || step + 2 < steps) flags |= kMuonReadWide;
+            if (split || step + 3 < steps) flags |= kMuonWriteWide;
+            if (step + 1 == steps) flags |= kMuonLast;
+        } else if (split) {
+            // without SPLIT the polynomial takes G as its operands have it: their rounding errors
+            // cancel in part
+            flags |= kind == kMuonGram ? kMuonWriteWide : kMuonReadWide;
+        }
+        for (uint32_t r = 0; r < rb; ++r) {
+            const uint32_t cb = kind == kMuonApply ? (mat.n + shape.tn - 1) / shape.tn : sym_columns(mat, r);
+            for (uint32_t c = 0; c < cb; ++c) {
+                uint16_t f = flags;
+                if (kind != kMuonApply && c * shape.tn / tm < r) f |= kMuonMirror;
+                tasks.push_back({i, (uint16_t)r, (uint16_t)c, (uint16_t)step, f, (uint32_t)need});
+            }
+        }
+    }
+    void build() {
+        std::vector<std::pair<uint32_t, uint32_t>> groups;
+        uint64_t all = 0, held = 0;
+        for (const MuonMat& mat : mats) all += (uint64_t)mat.m * mat.ld_x;
+        const uint64_t most = std::min<uint64_t>(kGroupEntries, (all + kLanes - 1) / kLanes);
+        uint32_t from = 0;
+        for (uint32_t i = 0; i < mats.size(); ++i) {
+            held += (uint64_t)mats[i].m * mats[i].ld_x;
+            if (held >= most || i + 1 == mats.size()) {
+                groups.push_back({from, i + 1});
+                from = i + 1;
+                held = 0;
+            }
+        }
+        // lane l takes the groups l, l + kLanes, ...; in every turn each lane has one product, and lane
+        // l starts l turns later
+        const uint64_t turns = (groups.size() + kLanes - 1) / kLanes * 3 * steps + kLanes;
+        for (uint64_t turn = 0; turn < turns; ++turn)
+            for (uint64_t lane = 0; lane < kLanes && lane <= turn; ++lane) {
+                const uint64_t at = turn - lane, g = at / (3 * steps) * kLanes + lane, in = at % (3 * steps);
+                if (g >= groups.size()) continue;
+                for (uint32_t i = groups[g].first; i < groups[g].second; ++i) add(i, (uint32_t)(in / 3), (int)(in % 3));
+            }
+    }
+};
 
 template <int CG, int TN, bool SPLIT>
 int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st) {
@@ -147,10 +221,8 @@ int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st
         clusters[p->device] = std::min(n, p->sms / CG);
     });
     if (clusters[p->device] <= 0) return ECQ_ERR_CUDA;
-    it.shape = (uint32_t)shape;
-    it.sym = p->d_sym[shape]; it.n_sym = p->n_sym[shape];
-    it.full = p->d_full[shape]; it.n_full = p->n_full[shape];
-    cfg.gridDim = dim3(std::min<uint32_t>(it.n_full, clusters[p->device]) * CG);
+    it.tasks = p->d_tasks[shape]; it.n_tasks = p->n_tasks[shape];
+    cfg.gridDim = dim3((uint32_t)std::min<uint64_t>(p->n_full[shape], clusters[p->device]) * CG);
     cfg.stream = st;
     if (cudaLaunchKernelEx(&cfg, kern, it) != cudaSuccess) {
         cudaGetLastError();
@@ -163,8 +235,8 @@ int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st
 // Tiles of a call: the plan's choice, or the largest of which there are enough for every SM.
 int choose_tiles(const ecq_muon* p, bool split) {
     if (p->tiles != ECQ_MUON_TILES_AUTO) return p->tiles;
-    if (p->n_full[split ? 1 : 0] * 2 >= (uint32_t)p->sms) return ECQ_MUON_TILES_256X256;
-    if (p->n_full[2] >= (uint32_t)p->sms) return ECQ_MUON_TILES_128X128;
+    if (p->n_full[split ? 3 : 0] * 2 >= (uint64_t)p->sms) return ECQ_MUON_TILES_256X256;
+    if (!split && p->n_full[1] >= (uint64_t)p->sms) return ECQ_MUON_TILES_128X128;
     return ECQ_MUON_TILES_128X64;
 }
 
@@ -175,16 +247,16 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
                       : (out.params || out_dtype != ECQ_BF16) ? 3 : 1;
     if (in.momentum) {
         muon_norm_kernel<float, true><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<float, true><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
+        muon_prepare_kernel<float, true><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, terms == 3, p->d_sound, p->d_done, p->d_next, p->d_status);
     } else if (in_dtype == ECQ_F32) {
         muon_norm_kernel<float, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<float, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
+        muon_prepare_kernel<float, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, terms == 3, p->d_sound, p->d_done, p->d_next, p->d_status);
     } else if (in_dtype == ECQ_BF16) {
         muon_norm_kernel<__nv_bfloat16, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<__nv_bfloat16, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
+        muon_prepare_kernel<__nv_bfloat16, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, terms == 3, p->d_sound, p->d_done, p->d_next, p->d_status);
     } else {
         muon_norm_kernel<__half, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<__half, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
+        muon_prepare_kernel<__half, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, terms == 3, p->d_sound, p->d_done, p->d_next, p->d_status);
     }
     if (cudaGetLastError() != cudaSuccess) return ECQ_ERR_CUDA;
     g_launches.fetch_add(2, std::memory_order_relaxed);
@@ -193,8 +265,8 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
     m.mats = p->d_mats;
     m.maps = p->d_maps;
     m.steps = p->d_steps;
-    m.n_steps = (uint32_t)p->steps.size();
     m.sound = p->d_sound;
+    m.ws = ws;
     m.done = p->d_done;
     m.next = p->d_next;
     m.status = p->d_status;
@@ -203,11 +275,11 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
     m.wait_limit = p->wait_limit;
     const int tiles = choose_tiles(p, terms == 3);
     if (terms == 3)
-        return tiles == ECQ_MUON_TILES_256X256 ? launch_iterate<2, 128, true>(p, m, 1, st)
-                                               : launch_iterate<1, 64, true>(p, m, 3, st);
+        return tiles == ECQ_MUON_TILES_256X256 ? launch_iterate<2, 128, true>(p, m, 3, st)
+                                               : launch_iterate<1, 64, true>(p, m, 4, st);
     return tiles == ECQ_MUON_TILES_256X256   ? launch_iterate<2, 256, false>(p, m, 0, st)
-           : tiles == ECQ_MUON_TILES_128X128 ? launch_iterate<1, 128, false>(p, m, 2, st)
-                                             : launch_iterate<1, 64, false>(p, m, 3, st);
+           : tiles == ECQ_MUON_TILES_128X128 ? launch_iterate<1, 128, false>(p, m, 1, st)
+                                             : launch_iterate<1, 64, false>(p, m, 2, st);
 }
 
 bool finite(float x) { return x - x == 0.f; }
@@ -223,7 +295,8 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     }
     if (!steps_in_range(p->steps)) return ECQ_ERR_ARG;
     std::vector<MuonSpan> spans;
-    std::vector<MuonTile> prep, sym[kShapeCount], full[kShapeCount];
+    std::vector<MuonTile> prep;
+    std::vector<MuonTask> tasks[kShapeCount];
     for (uint32_t i = 0; i < count; ++i) {
         MuonMat mat = {};
         mat.offset = offsets[i];
@@ -241,6 +314,9 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
         mat.x_at = p->x_entries; mat.g_at = p->g_entries;
         p->x_entries += (uint64_t)mat.m * mat.ld_x;
         p->g_entries += (uint64_t)mat.m * mat.ld_g;
+        mat.xm_at = p->xm_entries; mat.gm_at = p->gm_entries;
+        p->xm_entries += (uint64_t)((mat.m + 31) / 32 * 32) * mat.ld_x;
+        p->gm_entries += (uint64_t)((mat.m + 31) / 32 * 32) * mat.ld_g;
         // spans of about kMuonSpan entries: flat where the rows lie end to end, else whole rows or parts of them
         mat.part0 = (uint32_t)spans.size();
         if (mat.stride == mat.cols) {
@@ -260,10 +336,16 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
         p->mats.push_back(mat);
     }
     for (int s = 0; s < kShapeCount; ++s) {
-        build_tiles(p, kShapes[s], sym[s], full[s]);
-        for (const MuonTile& t : sym[s]) ++p->mats[t.mat].tiles_sym[s];
-        for (const MuonTile& t : full[s]) ++p->mats[t.mat].tiles_full[s];
-        if ((2 * sym[s].size() + full[s].size()) * steps > 0x7FFFFFFFull) return ECQ_ERR_ARG;
+        TaskList list(p->mats, kShapes[s], steps, kShapes[s].split);
+        uint64_t all = 0;
+        for (uint32_t i = 0; i < count; ++i) {
+            p->n_full[s] += list.full[i];
+            all += steps * (2 * list.sym[i] + list.full[i]);
+        }
+        if (all > 0x10000000ull) return ECQ_ERR_ARG;
+        list.build();
+        tasks[s].swap(list.tasks);
+        p->n_tasks[s] = (uint32_t)tasks[s].size();
     }
     const float sx = kMuonScaleX, sg = kMuonScaleG;
     std::vector<MuonStep> table;
@@ -279,11 +361,8 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     auto place = [&](uint64_t n) { const uint64_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
     const uint64_t o_mats = place(count * sizeof(MuonMat)), o_spans = place(spans.size() * sizeof(MuonSpan));
     const uint64_t o_prep = place(prep.size() * sizeof(MuonTile));
-    uint64_t o_sym[kShapeCount], o_full[kShapeCount];
-    for (int s = 0; s < kShapeCount; ++s) {
-        o_sym[s] = place(sym[s].size() * sizeof(MuonTile));
-        o_full[s] = place(full[s].size() * sizeof(MuonTile));
-    }
+    uint64_t o_tasks[kShapeCount];
+    for (int s = 0; s < kShapeCount; ++s) o_tasks[s] = place(tasks[s].size() * sizeof(MuonTask));
     const uint64_t o_partial = place(spans.size() * 8), o_sound = place(count * 4ull), o_status = place(4);
     const uint64_t o_steps = place(steps * sizeof(MuonStep)), o_done = place(count * 8ull), o_next = place(8);
     const uint64_t o_maps = place((uint64_t)count * kMapsPerMat * 128);
@@ -292,10 +371,8 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     memcpy(host.data() + o_spans, spans.data(), spans.size() * sizeof(MuonSpan));
     memcpy(host.data() + o_steps, table.data(), steps * sizeof(MuonStep));
     memcpy(host.data() + o_prep, prep.data(), prep.size() * sizeof(MuonTile));
-    for (int s = 0; s < kShapeCount; ++s) {
-        memcpy(host.data() + o_sym[s], sym[s].data(), sym[s].size() * sizeof(MuonTile));
-        memcpy(host.data() + o_full[s], full[s].data(), full[s].size() * sizeof(MuonTile));
-    }
+    for (int s = 0; s < kShapeCount; ++s)
+        memcpy(host.data() + o_tasks[s], tasks[s].data(), tasks[s].size() * sizeof(MuonTask));
     if (cudaGetDevice(&p->device) != cudaSuccess || p->device < 0 || p->device >= kMaxDevices ||
         cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess)
         return ECQ_ERR_CUDA;
@@ -307,12 +384,7 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     p->d_mats = reinterpret_cast<MuonMat*>(p->block + o_mats);
     p->d_spans = reinterpret_cast<MuonSpan*>(p->block + o_spans);
     p->d_prep = reinterpret_cast<MuonTile*>(p->block + o_prep);
-    for (int s = 0; s < kShapeCount; ++s) {
-        p->d_sym[s] = reinterpret_cast<MuonTile*>(p->block + o_sym[s]);
-        p->d_full[s] = reinterpret_cast<MuonTile*>(p->block + o_full[s]);
-        p->n_sym[s] = (uint32_t)sym[s].size();
-        p->n_full[s] = (uint32_t)full[s].size();
-    }
+    for (int s = 0; s < kShapeCount; ++s) p->d_tasks[s] = reinterpret_cast<MuonTask*>(p->block + o_tasks[s]);
     p->d_partial = reinterpret_cast<double*>(p->block + o_partial);
     p->d_sound = reinterpret_cast<uint32_t*>(p->block + o_sound);
     p->d_status = reinterpret_cast<uint32_t*>(p->block + o_status);
@@ -387,11 +459,14 @@ int ecq_muon_bind(ecq_muon* p, void* workspace, uint64_t bytes, void* cuda_strea
             CUtensorMap* to = &maps[i * kMapsPerMat];
             bool ok = true;
             for (int k = 0; k < 4 && ok; ++k) {
-                ok = tensor_map(to + kMapOperand + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 64, 64) &&
-                     tensor_map(to + kMapOperand + 4 + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 64, 64) &&
-                     tensor_map(to + kMapBlock + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 64, 32) &&
-                     tensor_map(to + kMapBlock + 4 + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 64, 32) &&
-                     tensor_map(to + kMapMirror + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 32, 64);
+                ok = tensor_map(to + kMapX128 + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 128) &&
+                     tensor_map(to + kMapX64 + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 64) &&
+                     tensor_map(to + kMapXN128 + k, x[k] + mat.x_at, 64, mat.m, mat.ld_x, 64, mat.ld_x, 2) &&
+                     tensor_map(to + kMapXN64 + k, x[k] + mat.x_at, 64, mat.m, mat.ld_x, 64, mat.ld_x, 1);
+                if (k < 2)
+                    ok = ok && tensor_map(to + kMapG128 + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 128) &&
+                         tensor_map(to + kMapG64 + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 64) &&
+                         tensor_map(to + kMapB128 + k, g[2 + k] + mat.g_at, mat.m, mat.m, mat.ld_g, 128);
             }
             if (!ok) {
                 p->workspace = nullptr;

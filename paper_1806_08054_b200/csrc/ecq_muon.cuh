@@ -15,16 +15,17 @@ namespace ecq {
 // computed and written twice; the third is full.
 //
 // Numbers.  The products run on the tensor cores with fp16 operands and fp32 accumulators.  What
-// keeps the result accurate is that X itself is never rounded to 11 bits: it is kept as a pair
-// hi + lo of fp16 (22 bits), and the linear term a X takes both.  A rounding error of X in the
+// keeps the result accurate is that X itself is not rounded to 11 bits: it is kept in fp32 beside
+// the fp16 operand, and the linear term a X takes that.  A rounding error of X in the
 // directions of small singular values would be multiplied by a (3.44) in every step.  Against 64
 // bits, relative error of the result for spectra from flat to 1/i^1.5: bf16 throughout 1e-2 to
-// 9e-2, fp16 throughout 1e-3 to 1e-2, with the pair 3e-4 to 1.7e-3.
+// 9e-2, fp16 throughout 1e-3 to 1e-2, with X in fp32 3e-4 to 1.7e-3.  The last two steps have
+// nothing left to amplify, and X is kept in fp16 alone there (no difference measured).
 // In the last two steps, where most singular values are near 1, G is replaced by D = G - I
 // (exactly the same polynomial: b G + c G^2 = (b + c) I + (b + 2c) D + c D^2), so that the
 // rounding of G's diagonal does not cancel against a X: 5e-4 to 1.1e-3.
-// With three products per product (hi hi + hi lo + lo hi) all operands have 22 bits and the
-// result's error is that of fp32 arithmetic.
+// With SPLIT, operands are pairs hi + lo of fp16 (22 bits), of which three products are taken
+// (hi hi, hi lo, lo hi), and the result's error is that of fp32 arithmetic.
 //
 // X, G and the polynomial are stored scaled by powers of two, so that fp16's narrow range holds
 // entries as small as 1 / (m n)^0.5 and their low halves.
@@ -34,11 +35,11 @@ constexpr float kMuonScaleG = 256.f;
 
 struct MuonMat {
     uint64_t offset, stride;             // in the caller's flat vectors, entries
-    uint64_t x_at, g_at;                 // in the workspace, entries of fp16 (each of hi and lo)
+    uint64_t x_at, g_at;                 // in the workspace's fp16 arrays, entries
+    uint64_t xm_at, gm_at;               // in its arrays in block order, entries
     uint32_t rows, cols, m, n;
     uint32_t ld_x, ld_g;                 // padded to 64 entries
     uint32_t part0, parts;               // its partial sums of squares
-    uint32_t tiles_sym[4], tiles_full[4];  // tiles of its products, by tile shape
     uint32_t tall;
     float scale;
 };
@@ -61,8 +62,15 @@ struct MuonOut {
 struct MuonSpan { uint64_t start, stride; uint32_t mat, rows, len; };   // rows of len entries
 struct MuonTile { uint32_t mat; uint16_t i, j; };
 
+// Operands are row-major fp16.  What the epilogues add to a product (X to the third, G to the
+// second) never feeds a tensor core, and is kept in block order: blocks of 32 x 32 entries, row by
+// row, in each of which 16-byte pieces of the 32 rows follow each other, first all rows' first
+// pieces.  A thread that has a row of an accumulator then reads and writes its pieces directly, 512
+// contiguous bytes a warp, and nothing of it passes through shared memory, whose bandwidth the
+// operands use up.
 struct MuonWork {
     __half *xh[2], *xl[2], *gh, *gl, *bh, *bl;
+    float *xm, *gm;
 };
 
 __device__ __forceinline__ float muon_direction(const MuonIn& in, float g, float m_new) {
@@ -133,7 +141,7 @@ __device__ __forceinline__ void muon_split(float v, __half& hi, __half& lo) {
 // NaN or Inf: then X_0 = 0 and its momentum (and later its weights) stay as they are.
 template <typename T, bool MOM>
 __global__ void __launch_bounds__(kMuonPrepThreads) muon_prepare_kernel(
-    const MuonMat* mats, const MuonTile* tiles, const double* partial, MuonIn in, MuonWork ws, uint32_t* sound,
+    const MuonMat* mats, const MuonTile* tiles, const double* partial, MuonIn in, MuonWork ws, int low, uint32_t* sound,
     unsigned long long* done, unsigned long long* next, uint32_t* status) {
     const MuonTile tile = tiles[blockIdx.x];
     const MuonMat mat = mats[tile.mat];
@@ -234,7 +242,9 @@ __global__ void __launch_bounds__(kMuonPrepThreads) muon_prepare_kernel(
         for (int i = 0; i < 4; ++i) muon_split(x[k][i], hi[i], lo[i]);
         const uint64_t to = mat.x_at + (uint64_t)xr * mat.ld_x + xc;  // xc + 4 <= ld_x: a tile is 64 wide
         *reinterpret_cast<uint2*>(ws.xh[0] + to) = *reinterpret_cast<uint2*>(hi);
-        *reinterpret_cast<uint2*>(ws.xl[0] + to) = *reinterpret_cast<uint2*>(lo);
+        if (low) *reinterpret_cast<uint2*>(ws.xl[0] + to) = *reinterpret_cast<uint2*>(lo);
+        const uint64_t blk = mat.xm_at + ((uint64_t)(xr >> 5) * (mat.ld_x >> 5) + (xc >> 5)) * 1024;
+        *reinterpret_cast<uint4*>(ws.xm + blk + ((xc & 31) >> 2) * 128 + (xr & 31) * 4) = Elem<float>::narrow(x[k]);
     }
 }
 
@@ -324,8 +334,8 @@ __device__ __forceinline__ void leader_arrive(uint32_t leader_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
 }
 
-// A 64 x 64 box of fp16 into this CTA's shared memory; in a pair the bytes are counted on the
-// first CTA's barrier.
+// A box of fp16 into this CTA's shared memory; in a pair the bytes are counted on the first
+// CTA's barrier.
 template <int CG>
 __device__ __forceinline__ void muon_load(uint32_t dst, const void* map, uint32_t x, uint32_t y, uint32_t bar) {
     if (CG == 1)
@@ -337,33 +347,56 @@ __device__ __forceinline__ void muon_load(uint32_t dst, const void* map, uint32_
                      " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
                      : "memory");
 }
+template <int CG>
+__device__ __forceinline__ void muon_load3(uint32_t dst, const void* map, uint32_t x, uint32_t y, uint32_t z, uint32_t bar) {
+    if (CG == 1)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+                     " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
+                     " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                     : "memory");
+}
 
 enum { kMuonGram = 0, kMuonPoly = 1, kMuonApply = 2 };
-// Tensor maps of a matrix.  Loads of operands take 64 x 64 boxes, the epilogue reads and writes
-// blocks of 32 rows and 64 columns, and the mirrored halves of symmetric products are written in
-// blocks of 64 rows and 32 columns.  Each group: X (hi, lo of two copies), G (hi, lo), B (hi, lo).
-enum { kMapX = 0, kMapG = 4, kMapB = 6, kMapOperand = 0, kMapBlock = 8, kMapMirror = 16, kMapsPerMat = 20 };
+// Tensor maps of a matrix, hi and lo next to each other: left operands in boxes of 128 rows, right
+// ones in boxes of 128 or 64, 64 entries along K each; X as the right operand whose rows run along
+// K, in boxes of 64 rows by one or two times 64 columns.  X has two copies.
+enum {
+    kMapX128 = 0, kMapX64 = 4, kMapXN128 = 8, kMapXN64 = 12, kMapG128 = 16, kMapG64 = 18, kMapB128 = 20, kMapsPerMat = 22
+};
 
+// out = lin * in + acc * product - shift on the diagonal
 struct MuonStep { float poly_lin, poly_acc, apply_lin, apply_acc, shift; };
+
+// One tile of the whole computation; the list of them is in the order in which they are handed out.
+enum { kMuonKind = 3, kMuonReadWide = 4, kMuonWriteWide = 8, kMuonLast = 16, kMuonMirror = 32 };
+struct MuonTask {
+    uint32_t mat;
+    uint16_t i, j;
+    uint16_t step, flags;                // kind, and whether block-order X or G is fp32 (else fp16)
+    uint32_t need;                       // tiles of the matrix that have to be finished before
+};
 
 struct MuonIterate {
     const MuonMat* mats;
     const unsigned char* maps;           // kMapsPerMat tensor maps of 128 bytes per matrix
-    const MuonTile *sym, *full;          // tiles of a symmetric product, of the product with X
+    const MuonTask* tasks;
     const MuonStep* steps;
     const uint32_t* sound;
+    MuonWork ws;
     unsigned long long* done;            // per matrix: parts of tiles finished since the call began
     unsigned long long* next;            // the next tile that nobody has taken
     uint32_t* status;
     MuonOut out;
     int out_dtype;
-    uint32_t n_sym, n_full, n_steps;
-    uint32_t shape;                      // index of MuonMat::tiles_sym, tiles_full
+    uint32_t n_tasks;
     uint32_t wait_limit;
 };
 
 constexpr uint32_t kMuonBox = 8192;                                   // 64 x 64 fp16
-constexpr uint32_t kMuonBlock = 4096;                                 // 32 x 64 fp16
+constexpr uint32_t kMuonBlock = 2048;                                 // 32 x 32 fp16
 constexpr uint32_t kMuonQueue = 2;
 constexpr uint32_t kMuonChunk = 4;                                    // 64-wide steps along K per partial sum (SPLIT)
 
@@ -377,15 +410,15 @@ struct MuonShape {
     static constexpr uint32_t kStageBytes = kHalves * (kBytesA + kBytesB);
     static constexpr uint32_t kEpiWarps = TN >= 128 ? 8 : 4;
     static constexpr uint32_t kCols = TN / (kEpiWarps / 4);           // columns of an epilogue warp
-    static constexpr uint32_t kThreads = (kEpiWarps + 3) * 32;        // + loads, products, tile queue
+    static constexpr uint32_t kThreads = (kEpiWarps + 3) * 32;        // + loads, products, signals
     static constexpr uint32_t kEpiBytes = kEpiWarps * 2 * kMuonBlock;
     static constexpr uint32_t kStagesFit = (230u * 1024u - 2048u - kEpiBytes) / kStageBytes;
     static constexpr uint32_t kStages = kStagesFit < 6 ? kStagesFit : 6;
     static constexpr uint32_t kSmem = kStages * kStageBytes + kEpiBytes + 1024;   // + alignment
     static constexpr uint32_t kAccCols = SPLIT ? 2 * TN : TN;         // hi hi, and the two small products
     static constexpr uint32_t kTmemCols = 2 * kAccCols;
-    // arrivals per tile on MuonIterate::done, and on a queue slot
-    static constexpr uint32_t kParts = CG * kEpiWarps, kReaders = CG * (kEpiWarps + 1) + 1;
+    // counts per tile on MuonIterate::done, arrivals on a queue slot
+    static constexpr uint32_t kParts = CG, kReaders = CG * (kEpiWarps + 2) + 1;
 };
 
 // Waits that give up: the limit is per wait, and one that ran out ends all others soon.
@@ -427,47 +460,9 @@ __device__ __forceinline__ bool muon_wait_done(const unsigned long long* done, u
     return false;
 }
 
-// One tile of the whole computation, in the order in which they are handed out: for each step G
-// of all matrices, then the polynomials, then the products with X.
-struct MuonTask {
-    MuonTile tile;
-    uint32_t step;
-    int kind;
-    unsigned long long need;             // parts of the matrix's earlier tiles that it waits for
-    bool end;
-};
-
-template <typename S>
-__device__ __forceinline__ MuonTask muon_task(const MuonIterate& P, uint32_t t) {
-    MuonTask k;
-    const uint32_t per = 2 * P.n_sym + P.n_full;
-    k.step = t / per;
-    k.end = k.step >= P.n_steps;
-    if (k.end) return k;
-    const uint32_t r = t - k.step * per;
-    k.kind = r < P.n_sym ? kMuonGram : r < 2 * P.n_sym ? kMuonPoly : kMuonApply;
-    k.tile = k.kind == kMuonApply ? P.full[r - 2 * P.n_sym] : P.sym[k.kind == kMuonGram ? r : r - P.n_sym];
-    const MuonMat& mat = P.mats[k.tile.mat];
-    const unsigned long long sym = mat.tiles_sym[P.shape], full = mat.tiles_full[P.shape];
-    k.need = S::kParts * (k.step * (2 * sym + full) + k.kind * sym);
-    return k;
-}
-
-__device__ __forceinline__ void muon_write_last(const MuonIterate& P, const MuonMat& mat, uint64_t at, float o, bool sound) {
-    if (P.out.update) {
-        const float u = P.out.scaled ? __fmul_rn(mat.scale, o) : o;
-        if (P.out_dtype == 0) reinterpret_cast<float*>(P.out.update)[at] = u;
-        else if (P.out_dtype == 1) reinterpret_cast<__nv_bfloat16*>(P.out.update)[at] = __float2bfloat16_rn(u);
-        else reinterpret_cast<__half*>(P.out.update)[at] = __float2half_rn(u);
-    }
-    if (P.out.params && sound) {
-        const float p = P.out.params[at];
-        P.out.params[at] = __fmaf_rn(-__fmul_rn(P.out.rate, mat.scale), o, __fmul_rn(P.out.keep, p));
-    }
-}
-
-// Place of the 16 bytes with columns 8 c .. 8 c + 7 of row r in a block of 128-byte swizzled rows.
-__device__ __forceinline__ uint32_t muon_swizzle(uint32_t r, uint32_t c) { return r * 128u + ((c ^ (r & 7u)) << 4); }
+// Place of the 16 bytes with columns 8 c .. 8 c + 7 of row r in a block of 64-byte rows: neither
+// eight lanes with a row each nor eight with two whole rows meet in a bank.
+__device__ __forceinline__ uint32_t muon_swizzle(uint32_t r, uint32_t c) { return r * 64u + ((c ^ ((r >> 1) & 3u)) << 4); }
 
 __device__ __forceinline__ uint4 lds16(uint32_t addr) {
     uint4 v;
@@ -478,6 +473,19 @@ __device__ __forceinline__ void sts16(uint32_t addr, uint4 v) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+__device__ __forceinline__ void prefetch_map(const void* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// One lane of a converged warp, in a form from which the compiler can tell that it is one: TMA and
+// tcgen05 instructions take their operands from uniform registers, and behind a plain comparison of
+// the lane's number each of them costs about 0.1 us to issue.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 // Every step of every matrix in one launch.  Tiles are taken from a counter in a fixed order; each
 // waits until the tiles that its operands come from are finished.  Those are earlier in the order,
 // so they have been taken by CTAs that are running: some tile can always go on, whatever number
@@ -486,22 +494,23 @@ template <int CG, int TN, bool SPLIT>
 __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_iterate_kernel(const MuonIterate P) {
     using S = MuonShape<CG, TN, SPLIT>;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 4 + 2 * kMuonQueue + S::kEpiWarps];
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 6 + 2 * kMuonQueue];
     __shared__ uint32_t tmem_slot, queue[kMuonQueue];
     __shared__ volatile uint32_t stop;
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages;
     const uint32_t acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 16;
-    const uint32_t q_full = acc_empty + 16, q_empty = q_full + 8 * kMuonQueue, loaded = q_empty + 8 * kMuonQueue;
+    const uint32_t q_full = acc_empty + 16, q_empty = q_full + 8 * kMuonQueue, stored = q_empty + 8 * kMuonQueue;
     const uint32_t rank = CG == 1 ? 0 : cta_rank();
     const uint32_t limit = P.wait_limit;
 
     if (tid == 0) {
         for (uint32_t s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
-        for (uint32_t b = 0; b < 2; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, S::kParts); }
+        for (uint32_t b = 0; b < 2; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, CG * S::kEpiWarps); }
         for (uint32_t q = 0; q < kMuonQueue; ++q) { mbar_init(q_full + 8 * q, 1); mbar_init(q_empty + 8 * q, S::kReaders); }
-        for (uint32_t w = 0; w < S::kEpiWarps; ++w) mbar_init(loaded + 8 * w, 1);
+        mbar_init(stored, S::kEpiWarps);
+        mbar_init(stored + 8, S::kEpiWarps);
         stop = 0;
         fence_mbar_init();
     }
@@ -512,7 +521,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
     tcgen05_after_sync();
     const uint32_t tmem = tmem_slot;
 
-    // n-th tile of this CTA (or pair); false when there is none or a wait ran out
+    // n-th tile of this CTA (or pair); false when a wait ran out
     auto take = [&](uint32_t n, uint32_t& t) {
         const uint32_t q = n % kMuonQueue;
         if (!(CG == 1 ? muon_wait(q_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)
@@ -526,43 +535,73 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
         if (CG == 1) mbar_arrive(bar);
         else leader_arrive(leader_addr(bar));
     };
+    // the first CTA's load thread: hands tile t to all roles of both
+    auto give = [&](uint32_t n, uint32_t t) {
+        const uint32_t q = n % kMuonQueue;
+        if (!muon_wait(q_empty + 8 * q, ((n / kMuonQueue) & 1) ^ 1, limit, &stop)) return false;
+        *reinterpret_cast<volatile uint32_t*>(&queue[q]) = t;
+        mbar_arrive(q_full + 8 * q);
+        if (CG == 2) {
+            uint32_t v, bar;
+            asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(v) : "r"(smem_u32(&queue[q])));
+            asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(bar) : "r"(q_full + 8 * q));
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(v), "r"(t) : "memory");
+            leader_arrive(bar);
+        }
+        return true;
+    };
 
     if (warp == S::kEpiWarps) {
         // ---- loads -------------------------------------------------------------------------------
-        if (lane == 0) {
-            uint32_t it = 0, t;
+        if (elect_one()) {
+            uint32_t it = 0, t = 0;
             bool ok = true;
-            for (uint32_t n = 0; ok && take(n, t); ++n) {
+            const uint32_t total = P.n_tasks;
+            // a tile is claimed when the loads of the one before it are issued: one that waits for
+            // its operands then holds up no tile that another CTA could have had
+            unsigned long long claim = rank == 0 ? atomicAdd(P.next, 1ull) : 0;
+            for (uint32_t n = 0; ok; ++n) {
+                if (rank == 0) {
+                    t = (uint32_t)min(claim, (unsigned long long)total);
+                    if (!give(n, t)) break;
+                } else if (!take(n, t)) {
+                    break;
+                }
                 taken(n);
-                const MuonTask task = muon_task<S>(P, t);
-                if (task.end) break;
-                const unsigned char* map = P.maps + (uint64_t)task.tile.mat * kMapsPerMat * 128;
-                const MuonMat& mat = P.mats[task.tile.mat];
-                const uint32_t kb = ((task.kind == kMuonGram ? mat.n : mat.m) + 63) / 64;
-                const uint32_t row = task.tile.i * (CG * 128u) + rank * 128u;
-                const uint32_t col = task.tile.j * (uint32_t)TN + rank * (TN / CG);
-                const int x = kMapX + 2 * (task.step & 1);
-                const unsigned char* ma = map + (task.kind == kMuonGram ? x : task.kind == kMuonPoly ? kMapG : kMapB) * 128;
-                const unsigned char* mb = map + (task.kind == kMuonPoly ? kMapG : x) * 128;
-                if (!muon_wait_done(P.done + task.tile.mat, task.need, limit, &stop, 0)) break;
+                if (t >= total) break;
+                const MuonTask task = P.tasks[t];
+                const int kind = task.flags & kMuonKind;
+                const unsigned char* map = P.maps + (uint64_t)task.mat * kMapsPerMat * 128;
+                const MuonMat& mat = P.mats[task.mat];
+                const uint32_t kb = ((kind == kMuonGram ? mat.n : mat.m) + 63) / 64;
+                const uint32_t row = task.i * (CG * 128u) + rank * 128u;
+                const uint32_t col = task.j * (uint32_t)TN + rank * (TN / CG);
+                const int x = 2 * (task.step & 1);
+                const bool along_n = kind == kMuonApply;
+                const bool wide = S::kBoxesB == 2;
+                const unsigned char* ma = map + (kind == kMuonGram ? kMapX128 + x : along_n ? kMapB128 : kMapG128) * 128;
+                const unsigned char* mb = map + (kind == kMuonGram ? (wide ? kMapX128 : kMapX64) + x
+                                                 : along_n ? (wide ? kMapXN128 : kMapXN64) + x
+                                                           : wide ? kMapG128 : kMapG64) * 128;
+#pragma unroll
+                for (uint32_t h = 0; h < S::kHalves; ++h) {
+                    prefetch_map(ma + 128 * h);
+                    prefetch_map(mb + 128 * h);
+                }
+                if (!muon_wait_done(P.done + task.mat, (unsigned long long)S::kParts * task.need, limit, &stop, 0)) break;
                 for (uint32_t k = 0; k < kb; ++k, ++it) {
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
                     if (!muon_wait(empty + 8 * s, ph ^ 1, limit, &stop)) { ok = false; break; }
                     if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * S::kStageBytes);
                     const uint32_t bar = CG == 1 ? full + 8 * s : leader_addr(full + 8 * s);
-                    uint32_t dst = ring + s * S::kStageBytes;
+                    const uint32_t da = ring + s * S::kStageBytes, db = da + S::kHalves * S::kBytesA;
 #pragma unroll
-                    for (uint32_t h = 0; h < S::kHalves; ++h)
-#pragma unroll
-                        for (uint32_t b = 0; b < S::kBoxesA; ++b, dst += kMuonBox)
-                            muon_load<CG>(dst, ma + 128 * h, k * 64, row + b * 64, bar);
-#pragma unroll
-                    for (uint32_t h = 0; h < S::kHalves; ++h)
-#pragma unroll
-                        for (uint32_t b = 0; b < S::kBoxesB; ++b, dst += kMuonBox) {
-                            if (task.kind == kMuonApply) muon_load<CG>(dst, mb + 128 * h, col + b * 64, k * 64, bar);
-                            else muon_load<CG>(dst, mb + 128 * h, k * 64, col + b * 64, bar);
-                        }
+                    for (uint32_t h = 0; h < S::kHalves; ++h) {
+                        muon_load<CG>(da + h * S::kBytesA, ma + 128 * h, k * 64, row, bar);
+                        if (along_n) muon_load3<CG>(db + h * S::kBytesB, mb + 128 * h, 0, k * 64, col / 64, bar);
+                        else muon_load<CG>(db + h * S::kBytesB, mb + 128 * h, k * 64, col, bar);
+                    }
+                    if (rank == 0 && k + 1 == kb) claim = atomicAdd(P.next, 1ull);
                 }
             }
             // nothing of this CTA's is in flight when it leaves: every stage's last load was consumed
@@ -575,16 +614,17 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
         }
     } else if (warp == S::kEpiWarps + 1) {
         // ---- products ----------------------------------------------------------------------------
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             uint32_t it = 0, acc = 0, t;
             bool ok = true;
             for (uint32_t n = 0; ok && take(n, t); ++n) {
                 taken(n);
-                const MuonTask task = muon_task<S>(P, t);
-                if (task.end) break;
-                const MuonMat& mat = P.mats[task.tile.mat];
-                const uint32_t kb = ((task.kind == kMuonGram ? mat.n : mat.m) + 63) / 64;
-                const bool along_n = task.kind == kMuonApply;          // right operand's rows run along K
+                if (t >= P.n_tasks) break;
+                const MuonTask task = P.tasks[t];
+                const int kind = task.flags & kMuonKind;
+                const MuonMat& mat = P.mats[task.mat];
+                const uint32_t kb = ((kind == kMuonGram ? mat.n : mat.m) + 63) / 64;
+                const bool along_n = kind == kMuonApply;               // right operand's rows run along K
                 // fp32 accumulators, fp16 operands
                 const uint32_t idesc = (1u << 4) | ((uint32_t)(TN / 8) << 17) | ((uint32_t)(CG * 128 / 16) << 24) |
                                        (along_n ? 1u << 16 : 0u);
@@ -622,93 +662,107 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
             }
         }
     } else if (warp == S::kEpiWarps + 2) {
-        // ---- tile queue --------------------------------------------------------------------------
-        if (lane == 0 && rank == 0) {
-            const uint32_t total = (2 * P.n_sym + P.n_full) * P.n_steps;
-            uint32_t t = (uint32_t)min(atomicAdd(P.next, 1ull), (unsigned long long)total);
-            for (uint32_t n = 0;; ++n) {
-                const uint32_t q = n % kMuonQueue;
-                if (!muon_wait(q_empty + 8 * q, ((n / kMuonQueue) & 1) ^ 1, limit, &stop)) break;
-                *reinterpret_cast<volatile uint32_t*>(&queue[q]) = t;
-                mbar_arrive(q_full + 8 * q);
-                if (CG == 2) {
-                    uint32_t v, b;
-                    asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(v) : "r"(smem_u32(&queue[q])));
-                    asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(b) : "r"(q_full + 8 * q));
-                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(v), "r"(t) : "memory");
-                    leader_arrive(b);
-                }
-                if (t >= total) break;
-                t = (uint32_t)min(atomicAdd(P.next, 1ull), (unsigned long long)total);
+        // ---- signals -----------------------------------------------------------------------------
+        // Making a tile's results visible to the other SMs takes 1 to 2.5 us; the warps that wrote
+        // them have the next tile to do meanwhile.
+        if (lane == 0) {
+            uint32_t t;
+            for (uint32_t n = 0; take(n, t); ++n) {
+                taken(n);
+                if (t >= P.n_tasks) break;
+                const uint32_t mat = P.tasks[t].mat;
+                if (!muon_wait(stored + 8 * (n & 1), (n >> 1) & 1, limit, &stop)) break;
+                asm volatile("fence.proxy.async;" ::: "memory");       // what was stored is read next by TMA
+                __threadfence();
+                asm volatile("red.release.gpu.global.add.u64 [%0], %1;" ::"l"(P.done + mat), "l"(1ull) : "memory");
             }
         }
     } else {
         // ---- results -----------------------------------------------------------------------------
-        // Every warp has 32 rows and kCols columns of a tile.  What its results are added to comes
-        // in blocks of 32 x 64 by TMA, is replaced by the result in place, and leaves by TMA.
+        // Every warp has 32 rows and kCols columns of a tile, taken in blocks of 32 x 32.  What a
+        // block's results are added to is read ahead into registers.  Results that are operands
+        // later are turned in shared memory: a thread has a row of the accumulator, but in global
+        // memory four lanes with 16 bytes each share a row's block.
         const uint32_t quad = warp & 3, c0 = (warp >> 2) * S::kCols;
         const uint32_t block = ring + S::kStages * S::kStageBytes + warp * 2 * kMuonBlock;
         const uint32_t lane_addr = tmem + ((quad * 32u) << 16);
-        uint32_t acc = 0, loads = 0, t;
+        constexpr uint32_t kBlocks = S::kCols / 32;
+        // where a copy's lane has its 16 bytes: row cr and every eighth one below, columns 8 cc ..
+        const uint32_t cr = lane >> 2, cc = lane & 3;
+        const uint32_t copy_to = block + muon_swizzle(cr, cc);         // + 512 for each eight rows
+        const uint32_t own = block + lane * 64, flip = (lane >> 1) & 3;   // this lane's row: piece c at own + ((c ^ flip) << 4)
+        uint32_t acc = 0, t;
         bool ok = true;
         for (uint32_t n = 0; ok && __all_sync(~0u, take(n, t)); ++n) {
             __syncwarp();
             if (lane == 0) taken(n);
-            const MuonTask task = muon_task<S>(P, t);
-            if (task.end) break;
-            const MuonMat mat = P.mats[task.tile.mat];
-            const MuonStep step = P.steps[task.step];
-            const unsigned char* map = P.maps + (uint64_t)task.tile.mat * kMapsPerMat * 128;
-            const bool apply = task.kind == kMuonApply, gram = task.kind == kMuonGram;
-            const bool last = apply && task.step + 1 == P.n_steps;
-            const int src = task.step & 1;
-            const uint32_t row0 = task.tile.i * (CG * 128u) + rank * 128u + quad * 32u;
-            const uint32_t col0 = task.tile.j * (uint32_t)TN + c0;
+            if (t >= P.n_tasks) break;
+            const MuonTask task = P.tasks[t];
+            const int kind = task.flags & kMuonKind;
+            const MuonMat& mat = P.mats[task.mat];
+            const bool apply = kind == kMuonApply, gram = kind == kMuonGram;
+            const bool last = (task.flags & kMuonLast) != 0, mirror = (task.flags & kMuonMirror) != 0;
+            const bool read_wide = (task.flags & kMuonReadWide) != 0, write_wide = (task.flags & kMuonWriteWide) != 0;
+            const uint32_t src = task.step & 1;
+            const uint32_t m = mat.m, width = apply ? mat.n : m, ld = apply ? mat.ld_x : mat.ld_g;
+            const uint32_t row0 = task.i * (CG * 128u) + rank * 128u + quad * 32u;
+            const uint32_t col0 = task.j * (uint32_t)TN + c0;
             const uint32_t r = row0 + lane;
-            const uint32_t width = apply ? mat.n : mat.m;
-            const bool rows_in = row0 < mat.m;
-            const bool low = SPLIT || apply;                           // hi and lo, or hi alone
-            const bool mirror = !apply && task.tile.j * (uint32_t)TN / (CG * 128u) < task.tile.i;
-            const bool sound = last ? P.sound[task.tile.mat] != 0 : true;
-            const unsigned char* in_map = map + (kMapBlock + (apply ? kMapX + 2 * src : kMapG)) * 128;
-            const unsigned char* out_map = map + (kMapBlock + (gram ? kMapG : apply ? kMapX + 2 * (src ^ 1) : kMapB)) * 128;
-            const unsigned char* mir_map = map + (kMapMirror + (gram ? 0 : 2)) * 128;
+            const MuonStep& step = P.steps[task.step];
             const float lin = apply ? step.apply_lin : step.poly_lin;
             const float mul = gram ? kMuonScaleG / (kMuonScaleX * kMuonScaleX) : apply ? step.apply_acc : step.poly_acc;
+            const uint64_t at = (apply ? mat.x_at : mat.g_at) + (uint64_t)(row0 + cr) * ld + col0 + 8 * cc;
+            __half* out_hi = (gram ? P.ws.gh : apply ? P.ws.xh[src ^ 1] : P.ws.bh) + at;
+            __half* out_lo = (gram ? P.ws.gl : apply ? P.ws.xl[src ^ 1] : P.ws.bl) + at;
+            const uint64_t down = 8ull * ld;
+            const int rows_left = (int)(m - row0 - cr);                // > 8 i: row 8 i of the copy is inside
+            // this warp's first block in block order; 4 KB of fp32 each (of fp16, the first half)
+            uint4* order = reinterpret_cast<uint4*>((apply ? P.ws.xm + mat.xm_at : P.ws.gm + mat.gm_at) +
+                                                    ((uint64_t)(row0 >> 5) * (ld >> 5) + (col0 >> 5)) * 1024) + lane;
+            // blocks inside the matrix; 0 for a warp whose rows are all below it
+            const uint32_t blocks = row0 >= m || col0 >= width ? 0 : min(kBlocks, (width - col0 + 31) / 32);
 
-            auto fetch = [&](uint32_t col) {                           // lane 0
-                mbar_arrive_expect_tx(loaded + 8 * warp, (low ? 2 : 1) * kMuonBlock);
-                tma_load_2d(block, in_map, (int)col, (int)row0, loaded + 8 * warp);
-                if (low) tma_load_2d(block + kMuonBlock, in_map + 128, (int)col, (int)row0, loaded + 8 * warp);
-            };
-            const bool any = rows_in && col0 < width;
-            if (!gram && any) {
-                int go = 1;
-                if (lane == 0) {
-                    go = muon_wait_done(P.done + task.tile.mat, task.need, limit, &stop, 100);
-                    if (go) fetch(col0);
+            uint4 in[8];
+            auto fetch = [&](uint32_t b) {
+                if (gram || b >= blocks) return;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) in[i] = __ldcg(order + 256 * b + 32 * i);
+                if (read_wide) {
+#pragma unroll
+                    for (uint32_t i = 4; i < 8; ++i) in[i] = __ldcg(order + 256 * b + 32 * i);
                 }
+            };
+            // a block in shared memory to rows of global memory
+            auto flush = [&](uint32_t from, __half* to) {
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    if (rows_left > (int)(8 * i)) *reinterpret_cast<uint4*>(to + i * down) = lds16(from + 512 * i);
+            };
+            if (!gram && blocks) {
+                int go = 1;
+                if (lane == 0)
+                    go = muon_wait_done(P.done + task.mat, (unsigned long long)S::kParts * task.need, limit, &stop, 100);
                 if (!__shfl_sync(~0u, go, 0)) break;
             }
+            fetch(0);
 
             float sum[SPLIT ? S::kCols : 1];
             if (SPLIT) {
 #pragma unroll
-                for (uint32_t i = 0; i < S::kCols; ++i) sum[i] = 0.f;
-                const uint32_t kb = ((gram ? mat.n : mat.m) + 63) / 64;
+                for (uint32_t i = 0; i < S::kCols; ++i) sum[SPLIT ? i : 0] = 0.f;
+                const uint32_t kb = ((gram ? mat.n : m) + 63) / 64;
                 for (uint32_t chunk = 0; chunk < (kb + kMuonChunk - 1) / kMuonChunk; ++chunk, ++acc) {
                     ok = __all_sync(~0u, muon_wait(acc_full + 8 * (acc & 1), (acc >> 1) & 1, limit, &stop));
                     if (!ok) break;
                     tcgen05_after_sync();
 #pragma unroll
-                    for (uint32_t h = 0; h < S::kCols / 32; ++h) {
+                    for (uint32_t h = 0; h < kBlocks; ++h) {
                         float v[32], w[32];
                         tmem_load32(lane_addr + (acc & 1) * S::kAccCols + c0 + 32 * h, v);
                         tmem_load32(lane_addr + (acc & 1) * S::kAccCols + TN + c0 + 32 * h, w);
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            sum[(SPLIT ? 32 * h : 0) + (SPLIT ? i : 0)] =
-                                __fadd_rn(sum[(SPLIT ? 32 * h : 0) + (SPLIT ? i : 0)], __fadd_rn(v[i], w[i]));
+                            sum[SPLIT ? 32 * h + i : 0] = __fadd_rn(sum[SPLIT ? 32 * h + i : 0], __fadd_rn(v[i], w[i]));
                     }
                     tcgen05_before_sync();
                     __syncwarp();
@@ -724,113 +778,212 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
             if (!ok) break;
 
 #pragma unroll
-            for (uint32_t b = 0; b < S::kCols / 64; ++b) {
-                const uint32_t col = col0 + 64 * b;
-                if (!rows_in || col >= width) continue;                // the whole warp
-                if (b > 0) {                                           // the buffer's last block has left
-                    if (lane == 0) {
-                        bulk_wait_read0();
-                        if (!gram) fetch(col);
-                    }
-                    __syncwarp();
-                }
-                float y[64];
+            for (uint32_t b = 0; b < kBlocks; ++b) {
+                if (b >= blocks) break;                                // the whole warp
+                const uint32_t col = col0 + 32 * b;
+                float y[32];
                 if (SPLIT) {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) y[i] = sum[SPLIT ? 64 * b + i : 0];
+                    for (int i = 0; i < 32; ++i) y[i] = sum[SPLIT ? 32 * b + i : 0];
                 } else {
-                    tmem_load32(lane_addr + (acc & 1) * S::kAccCols + c0 + 64 * b, y);
-                    tmem_load32(lane_addr + (acc & 1) * S::kAccCols + c0 + 64 * b + 32, y + 32);
+                    tmem_load32(lane_addr + (acc & 1) * S::kAccCols + c0 + 32 * b, y);
                 }
-#pragma unroll
-                for (int i = 0; i < 64; ++i) y[i] = __fmul_rn(mul, y[i]);
+                // pairs of columns in one operation each
+                const uint64_t mul2v = pack2(mul, mul), lin2v = pack2(lin, lin);
                 if (gram) {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i)
-                        if (r == col + i) y[i] = __fsub_rn(y[i], step.shift);
-                } else {
-                    ok = __all_sync(~0u, muon_wait(loaded + 8 * warp, loads & 1, limit, &stop));
-                    ++loads;
-                    if (!ok) break;
+                    for (int i = 0; i < 16; ++i) unpack2(mul2(pack2(y[2 * i], y[2 * i + 1]), mul2v), y[2 * i], y[2 * i + 1]);
+                    if (col < row0 + 32 && row0 < col + 32) {          // the block meets the diagonal
 #pragma unroll
-                    for (uint32_t c = 0; c < 8; ++c) {
-                        float x[8], l[8];
-                        Elem<__half>::widen(lds16(block + muon_swizzle(lane, c)), x);
-                        if (low) {
-                            Elem<__half>::widen(lds16(block + kMuonBlock + muon_swizzle(lane, c)), l);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) x[i] = __fadd_rn(x[i], l[i]);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) y[8 * c + i] = __fmaf_rn(lin, x[i], y[8 * c + i]);
+                        for (int i = 0; i < 32; ++i)
+                            if (r == col + i) y[i] = __fsub_rn(y[i], step.shift);
                     }
+                } else {
+                    auto add = [&](int i, float u, float v) {          // to columns 2 i and 2 i + 1
+                        unpack2(fma2(lin2v, pack2(u, v), mul2(pack2(y[2 * i], y[2 * i + 1]), mul2v)), y[2 * i], y[2 * i + 1]);
+                    };
+                    if (read_wide) {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            add(2 * c, __uint_as_float(in[c].x), __uint_as_float(in[c].y));
+                            add(2 * c + 1, __uint_as_float(in[c].z), __uint_as_float(in[c].w));
+                        }
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            float x[8];
+                            Elem<__half>::widen(in[c], x);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) add(4 * c + i, x[2 * i], x[2 * i + 1]);
+                        }
+                    }
+                    fetch(b + 1);
                 }
                 if (!last) {
+                    uint32_t hi[16];
 #pragma unroll
-                    for (uint32_t c = 0; c < 8; ++c) {
-                        __half hi[8], lo[8];
+                    for (int i = 0; i < 16; ++i) hi[i] = Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) muon_split(y[8 * c + i], hi[i], lo[i]);
-                        sts16(block + muon_swizzle(lane, c), *reinterpret_cast<uint4*>(hi));
-                        if (low) sts16(block + kMuonBlock + muon_swizzle(lane, c), *reinterpret_cast<uint4*>(lo));
-                    }
-                    // mirrored: 64 rows of 32 entries, into the half that HALF leaves free
-                    auto turn = [&](uint32_t to, bool high) {
+                    for (uint32_t c = 0; c < 4; ++c)
+                        sts16(own + ((c ^ flip) << 4), make_uint4(hi[4 * c], hi[4 * c + 1], hi[4 * c + 2], hi[4 * c + 3]));
+                    if (gram || apply) {
+                        if (write_wide) {
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) {
-                            __half hi, lo;
-                            muon_split(y[i], hi, lo);
-                            asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + i * 64 + 2 * lane),
-                                         "h"(__half_as_ushort(high ? hi : lo)) : "memory");
-                        }
-                    };
-                    if (!SPLIT && mirror) turn(block + kMuonBlock, true);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        tma_store_2d(out_map, (int)col, (int)row0, block);
-                        if (low) tma_store_2d(out_map + 128, (int)col, (int)row0, block + kMuonBlock);
-                        if (!SPLIT && mirror) tma_store_2d(mir_map, (int)row0, (int)col, block + kMuonBlock);
-                        bulk_commit();
-                    }
-                    if (SPLIT && mirror) {
-                        if (lane == 0) bulk_wait_read0();
-                        __syncwarp();
-                        turn(block, true);
-                        turn(block + kMuonBlock, false);
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) {
-                            tma_store_2d(mir_map, (int)row0, (int)col, block);
-                            tma_store_2d(mir_map + 128, (int)row0, (int)col, block + kMuonBlock);
-                            bulk_commit();
+                            for (uint32_t i = 0; i < 8; ++i) __stcg(order + 256 * b + 32 * i, Elem<float>::narrow(y + 4 * i));
+                        } else {
+#pragma unroll
+                            for (uint32_t i = 0; i < 4; ++i)
+                                __stcg(order + 256 * b + 32 * i, make_uint4(hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]));
                         }
                     }
-                } else if (mat.tall) {                                 // the caller's rows run along the lanes
+                    if (SPLIT) {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i)
-                        if (r < mat.m && col + i < width)
-                            muon_write_last(P, mat, mat.offset + (uint64_t)(col + i) * mat.stride + r, y[i], sound);
-                } else {                                               // turned in the buffer, rotated by the row
+                        for (int i = 0; i < 16; ++i) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[i]));
+                            unpack2(sub2(pack2(y[2 * i], y[2 * i + 1]), pack2(f.x, f.y)), y[2 * i], y[2 * i + 1]);
+                        }
+#pragma unroll
+                        for (uint32_t c = 0; c < 4; ++c)
+                            sts16(own + kMuonBlock + ((c ^ flip) << 4), Elem<__half>::narrow(y + 8 * c));
+                    }
                     __syncwarp();
+                    flush(copy_to, out_hi + 32 * b);
+                    if (SPLIT) flush(copy_to + kMuonBlock, out_lo + 32 * b);
+                    if (mirror) {
+                        // the transposed block: row c of it has the 32 lanes' entries of column c
+                        auto turn = [&](const uint32_t* w, __half* base) {
+                            __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 64; ++i)
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(block + lane * 256 + ((i + lane) & 63) * 4), "f"(y[i])
-                                     : "memory");
+                            for (uint32_t i = 0; i < 32; ++i)
+                                asm volatile("st.shared.b16 [%0], %1;"
+                                             ::"r"(block + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + 2 * (lane & 7)),
+                                             "h"((uint16_t)(w[i >> 1] >> (16 * (i & 1)))) : "memory");
+                            __syncwarp();
+                            __half* to = base + mat.g_at + (uint64_t)(col + cr) * ld + row0 + 8 * cc;
+#pragma unroll
+                            for (uint32_t i = 0; i < 4; ++i)
+                                if (col + cr + 8 * i < m) *reinterpret_cast<uint4*>(to + i * down) = lds16(copy_to + 512 * i);
+                        };
+                        turn(hi, gram ? P.ws.gh : P.ws.bh);
+                        if (SPLIT) {
+                            uint32_t lo[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) lo[i] = Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
+                            turn(lo, gram ? P.ws.gl : P.ws.bl);
+                        }
+                    }
+                } else {
+                    // to the caller's vectors: rows of the block along its own or, where X is the
+                    // transpose, along its columns
+                    const bool tall = mat.tall;
+                    const uint32_t or0 = tall ? col : row0, oc0 = tall ? row0 : col;
+                    const uint32_t rows = mat.rows, cols = mat.cols;
+                    const uint64_t offset = mat.offset, stride = mat.stride;
+                    const bool sound = P.sound[task.mat] != 0;
                     __syncwarp();
-                    for (uint32_t i = 0; i < 32 && row0 + i < mat.m; ++i)
+                    if (!P.out.params && P.out_dtype != 0) {
+                        const float scale = P.out.scaled ? mat.scale : 1.f;
+                        const bool bf = P.out_dtype == 1;
+                        uint16_t* out = reinterpret_cast<uint16_t*>(P.out.update) + offset + (uint64_t)(or0 + cr) * stride + oc0 + 8 * cc;
+                        const bool whole = ((offset | stride) & 7) == 0;
 #pragma unroll
-                        for (uint32_t g = 0; g < 64; g += 32)
-                            if (col + g + lane < width) {
-                                float o;
-                                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(o) : "r"(block + i * 256 + ((g + lane + i) & 63) * 4));
-                                muon_write_last(P, mat, mat.offset + (uint64_t)(row0 + i) * mat.stride + col + g + lane, o, sound);
+                        for (uint32_t c = 0; c < 4; ++c) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float u = __fmul_rn(scale, y[8 * c + 2 * i]), v = __fmul_rn(scale, y[8 * c + 2 * i + 1]);
+                                w[i] = bf ? Elem<__nv_bfloat16>::pair(u, v) : Elem<__half>::pair(u, v);
                             }
-                    fence_proxy_async_smem();                          // the next block comes by TMA
-                    __syncwarp();
+                            if (!tall) {
+                                sts16(own + ((c ^ flip) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i)
+                                    asm volatile("st.shared.b16 [%0], %1;"
+                                                 ::"r"(block + muon_swizzle(8 * c + i, lane >> 3) + 2 * (lane & 7)),
+                                                 "h"((uint16_t)(w[i >> 1] >> (16 * (i & 1)))) : "memory");
+                            }
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i) {
+                            const uint32_t oc = oc0 + 8 * cc;
+                            if (or0 + cr + 8 * i >= rows || oc >= cols) continue;
+                            const uint4 v = lds16(copy_to + 512 * i);
+                            uint16_t* to = out + 8 * i * stride;
+                            if (whole && oc + 8 <= cols) {
+                                *reinterpret_cast<uint4*>(to) = v;
+                            } else {
+                                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                                for (int k = 0; k < 8; ++k)
+                                    if (oc + k < cols) to[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+                            }
+                        }
+                    } else {
+                        // 32 x 32 floats, 16-byte pieces of a row exchanged by its number
+                        const bool whole = ((offset | stride) & 3) == 0;
+#pragma unroll
+                        for (uint32_t c = 0; c < 8; ++c) {
+                            if (!tall) {
+                                sts16(block + lane * 128 + ((c ^ (lane & 7)) << 4), Elem<float>::narrow(y + 4 * c));
+                            } else {
+#pragma unroll
+                                for (uint32_t i = 4 * c; i < 4 * c + 4; ++i)
+                                    asm volatile("st.shared.f32 [%0], %1;"
+                                                 ::"r"(block + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + 4 * (lane & 3)), "f"(y[i])
+                                                 : "memory");
+                            }
+                        }
+                        __syncwarp();
+                        const uint32_t fr = lane >> 3, fc = lane & 7;
+#pragma unroll
+                        for (uint32_t i = 0; i < 8; ++i) {
+                            const uint32_t rr = i * 4 + fr, oc = oc0 + 4 * fc;
+                            if (or0 + rr >= rows || oc >= cols) continue;
+                            float o[4], u[4];
+                            Elem<float>::widen(lds16(block + rr * 128 + ((fc ^ (rr & 7)) << 4)), o);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) u[k] = P.out.scaled ? __fmul_rn(mat.scale, o[k]) : o[k];
+                            const uint64_t at = offset + (uint64_t)(or0 + rr) * stride + oc;
+                            const uint32_t count = min(4u, cols - oc);
+                            if (P.out.update) {
+                                if (P.out_dtype == 0) {
+                                    float* to = reinterpret_cast<float*>(P.out.update) + at;
+                                    if (whole && count == 4) *reinterpret_cast<uint4*>(to) = Elem<float>::narrow(u);
+                                    else
+#pragma unroll
+                                        for (uint32_t k = 0; k < 4; ++k)
+                                            if (k < count) to[k] = u[k];
+                                } else {
+                                    uint16_t* to = reinterpret_cast<uint16_t*>(P.out.update) + at;
+#pragma unroll
+                                    for (uint32_t k = 0; k < 4; ++k)
+                                        if (k < count)
+                                            to[k] = P.out_dtype == 1 ? __bfloat16_as_ushort(__float2bfloat16_rn(u[k]))
+                                                                     : __half_as_ushort(__float2half_rn(u[k]));
+                                }
+                            }
+                            if (P.out.params && sound) {
+                                float* to = P.out.params + at;
+                                const float rate = -__fmul_rn(P.out.rate, mat.scale);
+                                if (whole && count == 4) {
+                                    float p[4];
+                                    Elem<float>::widen(*reinterpret_cast<const uint4*>(to), p);
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) p[k] = __fmaf_rn(rate, o[k], __fmul_rn(P.out.keep, p[k]));
+                                    *reinterpret_cast<uint4*>(to) = Elem<float>::narrow(p);
+                                } else {
+#pragma unroll
+                                    for (uint32_t k = 0; k < 4; ++k)
+                                        if (k < count) to[k] = __fmaf_rn(rate, o[k], __fmul_rn(P.out.keep, to[k]));
+                                }
+                            }
+                        }
+                    }
                 }
+                __syncwarp();                                          // the buffer is free again
             }
-            if (!ok) break;
             if (!SPLIT) {
                 tcgen05_before_sync();
                 __syncwarp();
@@ -840,16 +993,9 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 }
                 ++acc;
             }
-            if (lane == 0) {
-                bulk_wait_all();                                       // written, not only read
-                asm volatile("red.release.gpu.global.add.u64 [%0], %1;" ::"l"(P.done + task.tile.mat), "l"(1ull) : "memory");
-            }
             __syncwarp();
-        }
-        if (lane == 0) {
-            bulk_wait_all();
-            if (stop)                                                  // a block may still be on its way
-                for (uint32_t i = 0; i < 1u << 12 && !mbar_try_wait(loaded + 8 * warp, loads & 1); ++i) {}
+            // the signal warp does the rest; the barrier's last use, two tiles ago, is over first
+            if (lane == 0 && muon_wait(stored + 8 * (n & 1), ((n >> 1) & 1) ^ 1, limit, &stop)) mbar_arrive(stored + 8 * (n & 1));
         }
     }
     __syncwarp();
