@@ -36,8 +36,8 @@ struct ecq_muon {
     uint32_t wait_limit;
     std::vector<Step> steps;
     std::vector<MuonMat> mats;
-    uint64_t x_entries, g_entries;       // fp16 entries of one copy of X, of one of G or B
-    uint64_t xm_entries, gm_entries;     // entries of X and of G in block order
+    uint64_t x_entries, g_entries;       // fp16 entries of one copy of X, of one m x m buffer
+    uint64_t xm_entries, gm_entries;     // entries of the same in block order
     // device tables, one allocation
     unsigned char* block;
     MuonMat* d_mats;
@@ -45,11 +45,11 @@ struct ecq_muon {
     MuonTile* d_prep;
     MuonTask* d_tasks[kShapeCount];
     double* d_partial;
-    MuonStep* d_steps;
+    MuonProduct* d_products;
     unsigned long long *d_done, *d_next;
     uint32_t *d_sound, *d_status, *h_status;
     unsigned char* d_maps;
-    uint32_t n_spans, n_prep, n_tasks[kShapeCount];
+    uint32_t n_spans, n_prep, n_tasks[kShapeCount], products_at[kShapeCount];
     uint64_t n_full[kShapeCount];        // tiles of one product with X, over all matrices
     unsigned char* workspace;            // the caller's, NULL until bound
 };
@@ -88,17 +88,18 @@ MuonWork work_of(const ecq_muon* p) {
         w.xh[c] = at; at += p->x_entries;
         w.xl[c] = at; at += p->x_entries;
     }
-    w.gh = at; at += p->g_entries;
-    w.gl = at; at += p->g_entries;
-    w.bh = at; at += p->g_entries;
-    w.bl = at; at += p->g_entries;
-    w.xm = reinterpret_cast<float*>(at);
-    w.gm = w.xm + p->xm_entries;
+    for (int k = 0; k < kMuonSquare; ++k) {
+        w.mh[k] = at; at += p->g_entries;
+        w.ml[k] = at; at += p->g_entries;
+    }
+    float* order = reinterpret_cast<float*>(at);
+    w.xm = order; order += p->xm_entries;
+    for (int k = 0; k < kMuonSquare; ++k) { w.mm[k] = order; order += p->gm_entries; }
     return w;
 }
 
 uint64_t workspace_bytes(const ecq_muon* p) {
-    return 8 * (p->x_entries + p->g_entries) + 4 * (p->xm_entries + p->gm_entries);
+    return 8 * p->x_entries + 4 * p->xm_entries + kMuonSquare * (4 * p->g_entries + 4 * p->gm_entries);
 }
 
 // Singular values start in (0, 1]; the scaled fp16 copies hold iterates up to 8 and polynomials
@@ -116,58 +117,147 @@ bool steps_in_range(const std::vector<Step>& steps) {
     return true;
 }
 
+// First steps of an iteration that may be merged: at most three, not among the last two, and only
+// while the polynomials stay in the range of their fp16 copies (R up to 200; G, B, S as in single
+// steps).
+uint32_t mergeable(const std::vector<Step>& steps) {
+    uint32_t k = steps.size() > 2 ? std::min<uint32_t>(3, (uint32_t)steps.size() - 2) : 1;
+    for (; k > 1; --k) {
+        bool ok = true;
+        for (int i = 0; i <= 4096 && ok; ++i) {
+            double g = (i / 4096.0) * (i / 4096.0), alpha = 1.0, whole = 1.0;
+            for (uint32_t j = 0; j < k && ok; ++j) {
+                const double p = steps[j].a + steps[j].b * g + steps[j].c * g * g;
+                alpha *= steps[j].a;
+                whole *= p;
+                ok = std::fabs(whole - alpha) <= 200.0 && std::fabs(p * g) <= 128.0;
+                g *= p * p;
+            }
+        }
+        if (ok) return k;
+    }
+    return 1;
+}
+
+// Products of one matrix in their order.  m x m buffers: 0 G, 1 and 2 B, 3 S, 4 R; the last R of
+// merged steps goes to S's place.
+std::vector<MuonProduct> program(const std::vector<Step>& steps, uint32_t merge, bool split) {
+    constexpr uint8_t none = 255;
+    const float sx = kMuonScaleX, sg = kMuonScaleG;
+    const uint8_t wide = kMuonReadWide | kMuonWriteWide;
+    const uint32_t n = (uint32_t)steps.size();
+    std::vector<MuonProduct> out;
+    auto put = [&](int kind, int left, int right, int to, int in, int in2, float lin, float lin2, float acc, float shift,
+                   int flags) {
+        out.push_back({lin, lin2, acc, shift, (uint8_t)kind, (uint8_t)left, (uint8_t)right, (uint8_t)to, (uint8_t)in,
+                       (uint8_t)in2, (uint8_t)flags, (uint8_t)0});
+        out.back().after = (uint8_t)(out.size() - 1);
+    };
+    uint32_t copy = 0;
+    for (uint32_t k = 0; k < n;) {
+        // X is kept in fp32 while small singular values are still to be amplified: an error made in
+        // the last two steps is not
+        const uint32_t end = k == 0 ? merge : k + 1;
+        const int x_in = split || k + 2 < n ? kMuonReadWide : 0;
+        const int x_out = split || end + 2 < n ? kMuonWriteWide : kMuonWriteNarrow;
+        const float unscale = end == n ? 1.f / sx : 1.f;
+        const int x_flags = x_in | (end == n ? kMuonLast : x_out);
+        if (end == k + 1) {
+            // b G + c G^2 with G = D + t I.  Without SPLIT it takes D as the operands have it: their
+            // rounding errors cancel in part
+            const Step& s = steps[k];
+            const float t = s.shift;
+            put(kMuonGram, copy, copy, 0, none, none, 0.f, 0.f, sg / (sx * sx), sg * t, split ? kMuonWriteWide : kMuonWriteNarrow);
+            put(kMuonSym, 0, 0, 1, 0, none, s.b + 2 * s.c * t, 0.f, s.c / sg, 0.f, split ? kMuonReadWide : 0);
+            put(kMuonApply, 1, copy, copy ^ 1, 0, none, (s.a + s.b * t + s.c * t * t) * unscale, 0.f, unscale / sg, 0.f, x_flags);
+        } else {
+            float alpha = steps[0].a;
+            int r = 1, b = 1;                                          // the first R is the first B
+            put(kMuonGram, copy, copy, 0, none, none, 0.f, 0.f, sg / (sx * sx), 0.f, kMuonWriteWide);
+            put(kMuonSym, 0, 0, 1, 0, none, steps[0].b, 0.f, steps[0].c / sg, 0.f, wide);
+            for (uint32_t j = 1; j < end; ++j) {
+                const Step &before = steps[j - 1], &s = steps[j];
+                // R of the step before last is formed beside S: it needs no more than B
+                put(kMuonSym, b, 0, 3, 0, none, before.a, 0.f, 1.f / sg, 0.f, wide);
+                if (j == 2) {
+                    put(kMuonSym, 2, 1, 4, 1, 2, steps[1].a, alpha, 1.f / sg, 0.f, wide);
+                    out.back().after -= 1;
+                    alpha *= steps[1].a;
+                    r = 4;
+                }
+                put(kMuonSym, b, 3, 0, 3, none, before.a, 0.f, 1.f / sg, 0.f, wide);
+                b = j == 1 ? 2 : 1;
+                put(kMuonSym, 0, 0, b, 0, none, s.b, 0.f, s.c / sg, 0.f, wide);
+            }
+            const Step& s = steps[end - 1];
+            put(kMuonSym, b, r, 3, r, b, s.a, alpha, 1.f / sg, 0.f, wide);
+            alpha *= s.a;
+            put(kMuonApply, 3, copy, copy ^ 1, 0, none, alpha * unscale, 0.f, unscale / sg, 0.f, x_flags);
+        }
+        copy ^= 1;
+        k = end;
+    }
+    return out;
+}
+
 // Entries of the matrices that are worked on together.  Three such groups are under way at a time,
 // each with 8 bytes an entry of X, of which about half is alive: they about fill the L2 cache.
 constexpr uint64_t kGroupEntries = 12ull << 20;
 constexpr uint64_t kLanes = 3;
 
-// Tiles of all steps in the order in which they are handed out.  Matrices are taken in groups, and
-// kLanes groups at a time go through their products one by one in turn, a third of a step apart:
-// between a group's product and the next one, which waits for all of it, there is the other
-// groups' work.
+// Tiles of all products in the order in which they are handed out.  Matrices are taken in groups, and
+// kLanes groups at a time go through their products one by one in turn: between a group's product
+// and the next one, which waits for all of it, there is the other groups' work.
 struct TaskList {
     const std::vector<MuonMat>& mats;
     Shape shape;
-    uint32_t steps;
-    bool split;
+    std::vector<MuonProduct> products;   // the single-step program, then the merged one
+    uint32_t count[2];                   // products of either
     std::vector<MuonTask> tasks;
     std::vector<uint64_t> sym, full;     // tiles per product, by matrix
 
-    TaskList(const std::vector<MuonMat>& all, Shape s, uint32_t n_steps, bool all_low)
-        : mats(all), shape(s), steps(n_steps), split(all_low), sym(all.size()), full(all.size()) {
+    TaskList(const std::vector<MuonMat>& all, Shape s, const std::vector<Step>& steps)
+        : mats(all), shape(s), sym(all.size()), full(all.size()) {
+        products = program(steps, 1, s.split);
+        const std::vector<MuonProduct> merged = program(steps, mergeable(steps), s.split);
+        count[0] = (uint32_t)products.size();
+        count[1] = (uint32_t)merged.size();
+        products.insert(products.end(), merged.begin(), merged.end());
         for (size_t i = 0; i < mats.size(); ++i) {
             const uint32_t tm = shape.cg * 128, rb = (mats[i].m + tm - 1) / tm;
             for (uint32_t r = 0; r < rb; ++r) sym[i] += sym_columns(mats[i], r);
             full[i] = (uint64_t)rb * ((mats[i].n + shape.tn - 1) / shape.tn);
         }
     }
+    // Merging three steps saves two products X X^T and two with X, 6 m^2 n, and costs 6 m^3; with
+    // tiles that reach over the diagonal, 6.5 against 7.5.  Singular values near 1 lose a factor
+    // alpha (41) in alpha X + R X: small matrices, whose singular values are all large in X_0,
+    // take single steps (error of 96 x 160: 7e-4, merged 1.4e-3).
+    bool merged(uint32_t i) const { return 5ull * mats[i].n >= 6ull * mats[i].m && mats[i].m >= 256; }
+    uint64_t tiles(uint32_t i, const MuonProduct& p) const { return p.kind == kMuonApply ? full[i] : sym[i]; }
+    uint64_t all_tiles(uint32_t i) const {
+        uint64_t n = 0;
+        const uint32_t from = merged(i) ? count[0] : 0;
+        for (uint32_t k = 0; k < count[merged(i)]; ++k) n += tiles(i, products[from + k]);
+        return n;
+    }
     // tiles of row block r that touch the lower triangle
     uint32_t sym_columns(const MuonMat& mat, uint32_t r) const {
         return (std::min(mat.m, (r + 1) * shape.cg * 128) + shape.tn - 1) / shape.tn;
     }
-    void add(uint32_t i, uint32_t step, int kind) {
+    void add(uint32_t i, uint32_t at) {
         const MuonMat& mat = mats[i];
+        const uint32_t from = merged(i) ? count[0] : 0;
+        if (at >= count[merged(i)]) return;
+        const MuonProduct& p = products[from + at];
         const uint32_t tm = shape.cg * 128, rb = (mat.m + tm - 1) / tm;
-        const uint64_t need = step * (2 * sym[i] + full[i]) + kind * sym[i];
-        uint16_t flags = (uint16_t)kind;
-        if (kind == kMuonApply) {
-            // fp32 while small singular values are still to be amplified: an error made in the
-            // last two steps is not
-            if (split || step + 2 < steps) flags |= kMuonReadWide;
-            if (split || step + 3 < steps) flags |= kMuonWriteWide;
-            if (step + 1 == steps) flags |= kMuonLast;
-        } else if (split) {
-            // without SPLIT the polynomial takes G as its operands have it: their rounding errors
-            // cancel in part
-            flags |= kind == kMuonGram ? kMuonWriteWide : kMuonReadWide;
-        }
+        uint64_t need = 0;
+        for (uint32_t k = 0; k < p.after; ++k) need += tiles(i, products[from + k]);
         for (uint32_t r = 0; r < rb; ++r) {
-            const uint32_t cb = kind == kMuonApply ? (mat.n + shape.tn - 1) / shape.tn : sym_columns(mat, r);
-            for (uint32_t c = 0; c < cb; ++c) {
-                uint16_t f = flags;
-                if (kind != kMuonApply && c * shape.tn / tm < r) f |= kMuonMirror;
-                tasks.push_back({i, (uint16_t)r, (uint16_t)c, (uint16_t)step, f, (uint32_t)need});
-            }
+            const uint32_t cb = p.kind == kMuonApply ? (mat.n + shape.tn - 1) / shape.tn : sym_columns(mat, r);
+            for (uint32_t c = 0; c < cb; ++c)
+                tasks.push_back({i, (uint16_t)r, (uint16_t)c, (uint16_t)(from + at),
+                                 (uint16_t)(p.kind != kMuonApply && c * shape.tn / tm < r), (uint32_t)need});
         }
     }
     void build() {
@@ -186,12 +276,13 @@ struct TaskList {
         }
         // lane l takes the groups l, l + kLanes, ...; in every turn each lane has one product, and lane
         // l starts l turns later
-        const uint64_t turns = (groups.size() + kLanes - 1) / kLanes * 3 * steps + kLanes;
+        const uint64_t length = std::max(count[0], count[1]);
+        const uint64_t turns = (groups.size() + kLanes - 1) / kLanes * length + kLanes;
         for (uint64_t turn = 0; turn < turns; ++turn)
             for (uint64_t lane = 0; lane < kLanes && lane <= turn; ++lane) {
-                const uint64_t at = turn - lane, g = at / (3 * steps) * kLanes + lane, in = at % (3 * steps);
+                const uint64_t at = turn - lane, g = at / length * kLanes + lane;
                 if (g >= groups.size()) continue;
-                for (uint32_t i = groups[g].first; i < groups[g].second; ++i) add(i, (uint32_t)(in / 3), (int)(in % 3));
+                for (uint32_t i = groups[g].first; i < groups[g].second; ++i) add(i, (uint32_t)(at % length));
             }
     }
 };
@@ -222,6 +313,7 @@ int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st
     });
     if (clusters[p->device] <= 0) return ECQ_ERR_CUDA;
     it.tasks = p->d_tasks[shape]; it.n_tasks = p->n_tasks[shape];
+    it.products = p->d_products + p->products_at[shape];
     cfg.gridDim = dim3((uint32_t)std::min<uint64_t>(p->n_full[shape], clusters[p->device]) * CG);
     cfg.stream = st;
     if (cudaLaunchKernelEx(&cfg, kern, it) != cudaSuccess) {
@@ -264,7 +356,6 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
     MuonIterate m = {};
     m.mats = p->d_mats;
     m.maps = p->d_maps;
-    m.steps = p->d_steps;
     m.sound = p->d_sound;
     m.ws = ws;
     m.done = p->d_done;
@@ -335,25 +426,20 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
             for (uint32_t c = 0; c * 64 < mat.cols; ++c) prep.push_back({i, (uint16_t)r, (uint16_t)c});
         p->mats.push_back(mat);
     }
+    std::vector<MuonProduct> table;
     for (int s = 0; s < kShapeCount; ++s) {
-        TaskList list(p->mats, kShapes[s], steps, kShapes[s].split);
+        TaskList list(p->mats, kShapes[s], p->steps);
         uint64_t all = 0;
         for (uint32_t i = 0; i < count; ++i) {
             p->n_full[s] += list.full[i];
-            all += steps * (2 * list.sym[i] + list.full[i]);
+            all += list.all_tiles(i);
         }
         if (all > 0x10000000ull) return ECQ_ERR_ARG;
         list.build();
         tasks[s].swap(list.tasks);
         p->n_tasks[s] = (uint32_t)tasks[s].size();
-    }
-    const float sx = kMuonScaleX, sg = kMuonScaleG;
-    std::vector<MuonStep> table;
-    for (uint32_t k = 0; k < steps; ++k) {
-        // b G + c G^2 with G = D + t I; the products carry the scales of their operands
-        const Step& s = p->steps[k];
-        const float t = s.shift, out = k + 1 == steps ? 1.f / sx : 1.f;
-        table.push_back({s.b + 2 * s.c * t, s.c / sg, (s.a + s.b * t + s.c * t * t) * out, out / sg, sg * t});
+        p->products_at[s] = (uint32_t)table.size();
+        table.insert(table.end(), list.products.begin(), list.products.end());
     }
     if (spans.size() > 0x7FFFFFFFull || prep.size() > 0x7FFFFFFFull) return ECQ_ERR_ARG;
 
@@ -364,12 +450,12 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     uint64_t o_tasks[kShapeCount];
     for (int s = 0; s < kShapeCount; ++s) o_tasks[s] = place(tasks[s].size() * sizeof(MuonTask));
     const uint64_t o_partial = place(spans.size() * 8), o_sound = place(count * 4ull), o_status = place(4);
-    const uint64_t o_steps = place(steps * sizeof(MuonStep)), o_done = place(count * 8ull), o_next = place(8);
+    const uint64_t o_products = place(table.size() * sizeof(MuonProduct)), o_done = place(count * 8ull), o_next = place(8);
     const uint64_t o_maps = place((uint64_t)count * kMapsPerMat * 128);
     std::vector<unsigned char> host(bytes, 0);
     memcpy(host.data() + o_mats, p->mats.data(), count * sizeof(MuonMat));
     memcpy(host.data() + o_spans, spans.data(), spans.size() * sizeof(MuonSpan));
-    memcpy(host.data() + o_steps, table.data(), steps * sizeof(MuonStep));
+    memcpy(host.data() + o_products, table.data(), table.size() * sizeof(MuonProduct));
     memcpy(host.data() + o_prep, prep.data(), prep.size() * sizeof(MuonTile));
     for (int s = 0; s < kShapeCount; ++s)
         memcpy(host.data() + o_tasks[s], tasks[s].data(), tasks[s].size() * sizeof(MuonTask));
@@ -388,7 +474,7 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     p->d_partial = reinterpret_cast<double*>(p->block + o_partial);
     p->d_sound = reinterpret_cast<uint32_t*>(p->block + o_sound);
     p->d_status = reinterpret_cast<uint32_t*>(p->block + o_status);
-    p->d_steps = reinterpret_cast<MuonStep*>(p->block + o_steps);
+    p->d_products = reinterpret_cast<MuonProduct*>(p->block + o_products);
     p->d_done = reinterpret_cast<unsigned long long*>(p->block + o_done);
     p->d_next = reinterpret_cast<unsigned long long*>(p->block + o_next);
     p->d_maps = p->block + o_maps;
@@ -455,18 +541,17 @@ int ecq_muon_bind(ecq_muon* p, void* workspace, uint64_t bytes, void* cuda_strea
         for (size_t i = 0; i < p->mats.size(); ++i) {
             const MuonMat& mat = p->mats[i];
             const __half* x[4] = {w.xh[0], w.xl[0], w.xh[1], w.xl[1]};
-            const __half* g[4] = {w.gh, w.gl, w.bh, w.bl};
             CUtensorMap* to = &maps[i * kMapsPerMat];
             bool ok = true;
-            for (int k = 0; k < 4 && ok; ++k) {
+            for (int k = 0; k < 4 && ok; ++k)
                 ok = tensor_map(to + kMapX128 + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 128) &&
                      tensor_map(to + kMapX64 + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 64) &&
                      tensor_map(to + kMapXN128 + k, x[k] + mat.x_at, 64, mat.m, mat.ld_x, 64, mat.ld_x, 2) &&
                      tensor_map(to + kMapXN64 + k, x[k] + mat.x_at, 64, mat.m, mat.ld_x, 64, mat.ld_x, 1);
-                if (k < 2)
-                    ok = ok && tensor_map(to + kMapG128 + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 128) &&
-                         tensor_map(to + kMapG64 + k, g[k] + mat.g_at, mat.m, mat.m, mat.ld_g, 64) &&
-                         tensor_map(to + kMapB128 + k, g[2 + k] + mat.g_at, mat.m, mat.m, mat.ld_g, 128);
+            for (int k = 0; k < 2 * kMuonSquare && ok; ++k) {
+                const __half* sq = (k & 1 ? w.ml[k / 2] : w.mh[k / 2]) + mat.g_at;
+                ok = tensor_map(to + kMapM128 + k, sq, mat.m, mat.m, mat.ld_g, 128) &&
+                     tensor_map(to + kMapM64 + k, sq, mat.m, mat.m, mat.ld_g, 64);
             }
             if (!ok) {
                 p->workspace = nullptr;

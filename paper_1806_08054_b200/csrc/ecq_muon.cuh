@@ -14,6 +14,16 @@ namespace ecq {
 // Three products a step: G and G^2 are symmetric, so only tiles that touch the lower triangle are
 // computed and written twice; the third is full.
 //
+// Merged steps.  For wide matrices the first steps need not touch X one by one: with B = b G + c G^2,
+//     X' = (alpha I + R) X,  G' = (a I + B) G (a I + B)
+// every matrix being a polynomial in the first G, all of them commute and all products are
+// symmetric.  A further step costs, instead of G and a product with X (3 m^2 n), the products
+//     S = a G + B G,  G' = a S + B S,  R' = a R + alpha B + B R,  alpha' = a alpha
+// (3 m^3) and none of X's memory traffic.  Rounding errors of G' grow by a^2 a step relative to
+// small eigenvalues, so this is done for the first three steps at most, in which singular values
+// are brought up to order 1, with what is added to each product in fp32: no difference in the
+// result's error was measured against single steps.  (All five merged: up to 0.5.)
+//
 // Numbers.  The products run on the tensor cores with fp16 operands and fp32 accumulators.  What
 // keeps the result accurate is that X itself is not rounded to 11 bits: it is kept in fp32 beside
 // the fp16 operand, and the linear term a X takes that.  A rounding error of X in the
@@ -62,15 +72,16 @@ struct MuonOut {
 struct MuonSpan { uint64_t start, stride; uint32_t mat, rows, len; };   // rows of len entries
 struct MuonTile { uint32_t mat; uint16_t i, j; };
 
-// Operands are row-major fp16.  What the epilogues add to a product (X to the third, G to the
-// second) never feeds a tensor core, and is kept in block order: blocks of 32 x 32 entries, row by
+// Operands are row-major fp16.  What the epilogues add to a product (X, G and so on) never feeds a
+// tensor core, and is kept in block order: blocks of 32 x 32 entries, row by
 // row, in each of which 16-byte pieces of the 32 rows follow each other, first all rows' first
 // pieces.  A thread that has a row of an accumulator then reads and writes its pieces directly, 512
 // contiguous bytes a warp, and nothing of it passes through shared memory, whose bandwidth the
 // operands use up.
+constexpr int kMuonSquare = 5;           // m x m buffers: G, B, another B, S, R
 struct MuonWork {
-    __half *xh[2], *xl[2], *gh, *gl, *bh, *bl;
-    float *xm, *gm;
+    __half *xh[2], *xl[2], *mh[kMuonSquare], *ml[kMuonSquare];
+    float *xm, *mm[kMuonSquare];
 };
 
 __device__ __forceinline__ float muon_direction(const MuonIn& in, float g, float m_new) {
@@ -359,23 +370,28 @@ __device__ __forceinline__ void muon_load3(uint32_t dst, const void* map, uint32
                      : "memory");
 }
 
-enum { kMuonGram = 0, kMuonPoly = 1, kMuonApply = 2 };
+enum { kMuonGram = 0, kMuonSym = 1, kMuonApply = 2 };                // X X^T, m x m, m x m times X
 // Tensor maps of a matrix, hi and lo next to each other: left operands in boxes of 128 rows, right
 // ones in boxes of 128 or 64, 64 entries along K each; X as the right operand whose rows run along
 // K, in boxes of 64 rows by one or two times 64 columns.  X has two copies.
-enum {
-    kMapX128 = 0, kMapX64 = 4, kMapXN128 = 8, kMapXN64 = 12, kMapG128 = 16, kMapG64 = 18, kMapB128 = 20, kMapsPerMat = 22
+enum { kMapX128 = 0, kMapX64 = 4, kMapXN128 = 8, kMapXN64 = 12, kMapM128 = 16, kMapM64 = 26, kMapsPerMat = 36 };
+
+// One product of the iteration: out = lin * in + lin2 * in2 + acc * left right, less `shift` on the
+// diagonal.  Buffers are copies of X or m x m ones by the kind.  In block order, in and in2 are
+// fp32 with kMuonReadWide, else fp16; out is written there, too, as fp32 or fp16 or not at all.
+enum { kMuonReadWide = 1, kMuonWriteWide = 2, kMuonWriteNarrow = 4, kMuonLast = 8 };
+struct MuonProduct {
+    float lin, lin2, acc, shift;
+    uint8_t kind, left, right, out;
+    uint8_t in, in2, flags;              // 255: none
+    uint8_t after;                       // products before it that have to be finished
 };
 
-// out = lin * in + acc * product - shift on the diagonal
-struct MuonStep { float poly_lin, poly_acc, apply_lin, apply_acc, shift; };
-
 // One tile of the whole computation; the list of them is in the order in which they are handed out.
-enum { kMuonKind = 3, kMuonReadWide = 4, kMuonWriteWide = 8, kMuonLast = 16, kMuonMirror = 32 };
 struct MuonTask {
     uint32_t mat;
     uint16_t i, j;
-    uint16_t step, flags;                // kind, and whether block-order X or G is fp32 (else fp16)
+    uint16_t product, mirror;
     uint32_t need;                       // tiles of the matrix that have to be finished before
 };
 
@@ -383,7 +399,7 @@ struct MuonIterate {
     const MuonMat* mats;
     const unsigned char* maps;           // kMapsPerMat tensor maps of 128 bytes per matrix
     const MuonTask* tasks;
-    const MuonStep* steps;
+    const MuonProduct* products;
     const uint32_t* sound;
     MuonWork ws;
     unsigned long long* done;            // per matrix: parts of tiles finished since the call began
@@ -570,19 +586,18 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 taken(n);
                 if (t >= total) break;
                 const MuonTask task = P.tasks[t];
-                const int kind = task.flags & kMuonKind;
+                const MuonProduct& pr = P.products[task.product];
+                const int kind = pr.kind;
                 const unsigned char* map = P.maps + (uint64_t)task.mat * kMapsPerMat * 128;
                 const MuonMat& mat = P.mats[task.mat];
                 const uint32_t kb = ((kind == kMuonGram ? mat.n : mat.m) + 63) / 64;
                 const uint32_t row = task.i * (CG * 128u) + rank * 128u;
                 const uint32_t col = task.j * (uint32_t)TN + rank * (TN / CG);
-                const int x = 2 * (task.step & 1);
-                const bool along_n = kind == kMuonApply;
-                const bool wide = S::kBoxesB == 2;
-                const unsigned char* ma = map + (kind == kMuonGram ? kMapX128 + x : along_n ? kMapB128 : kMapG128) * 128;
-                const unsigned char* mb = map + (kind == kMuonGram ? (wide ? kMapX128 : kMapX64) + x
-                                                 : along_n ? (wide ? kMapXN128 : kMapXN64) + x
-                                                           : wide ? kMapG128 : kMapG64) * 128;
+                const bool along_n = kind == kMuonApply, wide = S::kBoxesB == 2;
+                const unsigned char* ma = map + ((kind == kMuonGram ? kMapX128 : kMapM128) + 2 * pr.left) * 128;
+                const unsigned char* mb = map + ((kind == kMuonGram ? (wide ? kMapX128 : kMapX64)
+                                                  : along_n ? (wide ? kMapXN128 : kMapXN64)
+                                                            : (wide ? kMapM128 : kMapM64)) + 2 * pr.right) * 128;
 #pragma unroll
                 for (uint32_t h = 0; h < S::kHalves; ++h) {
                     prefetch_map(ma + 128 * h);
@@ -621,7 +636,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 taken(n);
                 if (t >= P.n_tasks) break;
                 const MuonTask task = P.tasks[t];
-                const int kind = task.flags & kMuonKind;
+                const int kind = P.products[task.product].kind;
                 const MuonMat& mat = P.mats[task.mat];
                 const uint32_t kb = ((kind == kMuonGram ? mat.n : mat.m) + 63) / 64;
                 const bool along_n = kind == kMuonApply;               // right operand's rows run along K
@@ -698,27 +713,26 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
             if (lane == 0) taken(n);
             if (t >= P.n_tasks) break;
             const MuonTask task = P.tasks[t];
-            const int kind = task.flags & kMuonKind;
+            const MuonProduct& pr = P.products[task.product];
             const MuonMat& mat = P.mats[task.mat];
-            const bool apply = kind == kMuonApply, gram = kind == kMuonGram;
-            const bool last = (task.flags & kMuonLast) != 0, mirror = (task.flags & kMuonMirror) != 0;
-            const bool read_wide = (task.flags & kMuonReadWide) != 0, write_wide = (task.flags & kMuonWriteWide) != 0;
-            const uint32_t src = task.step & 1;
+            const bool apply = pr.kind == kMuonApply, gram = pr.kind == kMuonGram;
+            const uint32_t flags = pr.flags;
+            const bool last = (flags & kMuonLast) != 0, mirror = task.mirror != 0, read_wide = (flags & kMuonReadWide) != 0;
             const uint32_t m = mat.m, width = apply ? mat.n : m, ld = apply ? mat.ld_x : mat.ld_g;
             const uint32_t row0 = task.i * (CG * 128u) + rank * 128u + quad * 32u;
             const uint32_t col0 = task.j * (uint32_t)TN + c0;
             const uint32_t r = row0 + lane;
-            const MuonStep& step = P.steps[task.step];
-            const float lin = apply ? step.apply_lin : step.poly_lin;
-            const float mul = gram ? kMuonScaleG / (kMuonScaleX * kMuonScaleX) : apply ? step.apply_acc : step.poly_acc;
+            const float lin = pr.lin, mul = pr.acc, shift = pr.shift;
             const uint64_t at = (apply ? mat.x_at : mat.g_at) + (uint64_t)(row0 + cr) * ld + col0 + 8 * cc;
-            __half* out_hi = (gram ? P.ws.gh : apply ? P.ws.xh[src ^ 1] : P.ws.bh) + at;
-            __half* out_lo = (gram ? P.ws.gl : apply ? P.ws.xl[src ^ 1] : P.ws.bl) + at;
+            __half* out_hi = (apply ? P.ws.xh[pr.out] : P.ws.mh[pr.out]) + at;
+            __half* out_lo = (apply ? P.ws.xl[pr.out] : P.ws.ml[pr.out]) + at;
             const uint64_t down = 8ull * ld;
             const int rows_left = (int)(m - row0 - cr);                // > 8 i: row 8 i of the copy is inside
             // this warp's first block in block order; 4 KB of fp32 each (of fp16, the first half)
-            uint4* order = reinterpret_cast<uint4*>((apply ? P.ws.xm + mat.xm_at : P.ws.gm + mat.gm_at) +
-                                                    ((uint64_t)(row0 >> 5) * (ld >> 5) + (col0 >> 5)) * 1024) + lane;
+            const uint64_t order_at = (apply ? mat.xm_at : mat.gm_at) +
+                                      ((uint64_t)(row0 >> 5) * (ld >> 5) + (col0 >> 5)) * 1024 + 4 * lane;
+            const float* order_in = (apply ? P.ws.xm : P.ws.mm[gram ? 0 : pr.in]) + order_at;
+            float* order_out = (apply ? P.ws.xm : P.ws.mm[pr.out]) + order_at;
             // blocks inside the matrix; 0 for a warp whose rows are all below it
             const uint32_t blocks = row0 >= m || col0 >= width ? 0 : min(kBlocks, (width - col0 + 31) / 32);
 
@@ -726,10 +740,10 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
             auto fetch = [&](uint32_t b) {
                 if (gram || b >= blocks) return;
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) in[i] = __ldcg(order + 256 * b + 32 * i);
+                for (uint32_t i = 0; i < 4; ++i) in[i] = __ldcg(reinterpret_cast<const uint4*>(order_in) + 256 * b + 32 * i);
                 if (read_wide) {
 #pragma unroll
-                    for (uint32_t i = 4; i < 8; ++i) in[i] = __ldcg(order + 256 * b + 32 * i);
+                    for (uint32_t i = 4; i < 8; ++i) in[i] = __ldcg(reinterpret_cast<const uint4*>(order_in) + 256 * b + 32 * i);
                 }
             };
             // a block in shared memory to rows of global memory
@@ -796,7 +810,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                     if (col < row0 + 32 && row0 < col + 32) {          // the block meets the diagonal
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (r == col + i) y[i] = __fsub_rn(y[i], step.shift);
+                            if (r == col + i) y[i] = __fsub_rn(y[i], shift);
                     }
                 } else {
                     auto add = [&](int i, float u, float v) {          // to columns 2 i and 2 i + 1
@@ -817,6 +831,19 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                             for (int i = 0; i < 4; ++i) add(4 * c + i, x[2 * i], x[2 * i + 1]);
                         }
                     }
+                    if (pr.in2 != 255) {                               // fp32 always
+                        const float* second = P.ws.mm[pr.in2] + order_at;
+                        const uint64_t lin2b = pack2(pr.lin2, pr.lin2);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) in[c] = __ldcg(reinterpret_cast<const uint4*>(second) + 256 * b + 32 * c);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            unpack2(fma2(lin2b, pack2(__uint_as_float(in[c].x), __uint_as_float(in[c].y)), pack2(y[4 * c], y[4 * c + 1])),
+                                    y[4 * c], y[4 * c + 1]);
+                            unpack2(fma2(lin2b, pack2(__uint_as_float(in[c].z), __uint_as_float(in[c].w)), pack2(y[4 * c + 2], y[4 * c + 3])),
+                                    y[4 * c + 2], y[4 * c + 3]);
+                        }
+                    }
                     fetch(b + 1);
                 }
                 if (!last) {
@@ -826,15 +853,14 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
 #pragma unroll
                     for (uint32_t c = 0; c < 4; ++c)
                         sts16(own + ((c ^ flip) << 4), make_uint4(hi[4 * c], hi[4 * c + 1], hi[4 * c + 2], hi[4 * c + 3]));
-                    if (gram || apply) {
-                        if (write_wide) {
+                    uint4* order = reinterpret_cast<uint4*>(order_out) + 256 * b;
+                    if (flags & kMuonWriteWide) {
 #pragma unroll
-                            for (uint32_t i = 0; i < 8; ++i) __stcg(order + 256 * b + 32 * i, Elem<float>::narrow(y + 4 * i));
-                        } else {
+                        for (uint32_t i = 0; i < 8; ++i) __stcg(order + 32 * i, Elem<float>::narrow(y + 4 * i));
+                    } else if (flags & kMuonWriteNarrow) {
 #pragma unroll
-                            for (uint32_t i = 0; i < 4; ++i)
-                                __stcg(order + 256 * b + 32 * i, make_uint4(hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]));
-                        }
+                        for (uint32_t i = 0; i < 4; ++i)
+                            __stcg(order + 32 * i, make_uint4(hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]));
                     }
                     if (SPLIT) {
 #pragma unroll
@@ -864,12 +890,12 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                             for (uint32_t i = 0; i < 4; ++i)
                                 if (col + cr + 8 * i < m) *reinterpret_cast<uint4*>(to + i * down) = lds16(copy_to + 512 * i);
                         };
-                        turn(hi, gram ? P.ws.gh : P.ws.bh);
+                        turn(hi, P.ws.mh[pr.out]);
                         if (SPLIT) {
                             uint32_t lo[16];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) lo[i] = Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
-                            turn(lo, gram ? P.ws.gl : P.ws.bl);
+                            turn(lo, P.ws.ml[pr.out]);
                         }
                     }
                 } else {
