@@ -324,6 +324,16 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float* v) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
 __device__ __forceinline__ void tcgen05_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tcgen05_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
@@ -489,6 +499,96 @@ __device__ __forceinline__ void sts16(uint32_t addr, uint4 v) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// A block of 32 x 32 finished entries, row or0 and column oc0 of the caller's matrix, from shared
+// memory (rows of 64 or 128 bytes) to the update and the weights.
+__device__ __forceinline__ void muon_out_narrow(const MuonIterate& P, const MuonMat& mat, uint32_t block, uint32_t or0, uint32_t oc0) {
+    const uint32_t lane = threadIdx.x & 31, cr = lane >> 2, cc = lane & 3, oc = oc0 + 8 * cc;
+    if (oc >= mat.cols) return;
+    uint16_t* to = reinterpret_cast<uint16_t*>(P.out.update) + mat.offset + (uint64_t)(or0 + cr) * mat.stride + oc;
+    const uint64_t down = 8 * mat.stride;
+    if (((mat.offset | mat.stride) & 7) == 0 && oc + 8 <= mat.cols) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i, to += down)
+            if (or0 + cr + 8 * i < mat.rows) *reinterpret_cast<uint4*>(to) = lds16(block + muon_swizzle(cr, cc) + 512 * i);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i, to += down) {
+            if (or0 + cr + 8 * i >= mat.rows) break;
+            const uint4 v = lds16(block + muon_swizzle(cr, cc) + 512 * i);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (oc + k < mat.cols) to[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+        }
+    }
+}
+
+// Weights are read before any is written: a block waits for memory once.
+__device__ __forceinline__ void muon_out_wide(const MuonIterate& P, const MuonMat& mat, uint32_t block, uint32_t or0, uint32_t oc0,
+                                           bool sound) {
+    const uint32_t lane = threadIdx.x & 31;
+    const float rate = -__fmul_rn(P.out.rate, mat.scale), up = P.out.scaled ? mat.scale : 1.f, keep = P.out.keep;
+    float* params = sound ? P.out.params : nullptr;
+    void* update = P.out.update;
+    if (((mat.offset | mat.stride) & 3) == 0 && oc0 + 32 <= mat.cols && P.out_dtype == 0) {
+        const uint32_t fr = lane >> 3, fc = lane & 7;                  // eight lanes with 16 bytes each to a row
+        const uint64_t to = mat.offset + (uint64_t)(or0 + fr) * mat.stride + oc0 + 4 * fc, down = 4 * mat.stride;
+        uint4 p[8];
+        if (params) {
+            const float* from = params + to;
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i, from += down)
+                if (or0 + fr + 4 * i < mat.rows) p[i] = *reinterpret_cast<const uint4*>(from);
+        }
+        float* out = reinterpret_cast<float*>(update) + to;
+        float* par = params + to;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i, out += down, par += down) {
+            const uint32_t rr = i * 4 + fr;
+            if (or0 + rr >= mat.rows) break;
+            float o[4], w[4];
+            Elem<float>::widen(lds16(block + rr * 128 + ((fc ^ (rr & 7)) << 4)), o);
+            if (params) {
+                Elem<float>::widen(p[i], w);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = __fmaf_rn(rate, o[k], __fmul_rn(keep, w[k]));
+                *reinterpret_cast<uint4*>(par) = Elem<float>::narrow(w);
+            }
+            if (update) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = __fmul_rn(up, o[k]);
+                *reinterpret_cast<uint4*>(out) = Elem<float>::narrow(w);
+            }
+        }
+        return;
+    }
+    if (oc0 + lane >= mat.cols) return;                                // any alignment: the lanes along a row
+    uint64_t to = mat.offset + (uint64_t)or0 * mat.stride + oc0 + lane;
+    for (uint32_t half = 0; half < 32; half += 16) {
+        float p[16];
+        if (params) {
+            const float* from = params + to;
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i, from += mat.stride)
+                if (or0 + half + i < mat.rows) p[i] = *from;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i, to += mat.stride) {
+            const uint32_t rr = half + i;
+            if (or0 + rr >= mat.rows) return;
+            float o;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(o) : "r"(block + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + 4 * (lane & 3)));
+            if (params) params[to] = __fmaf_rn(rate, o, __fmul_rn(keep, p[i]));
+            if (update) {
+                const float u = __fmul_rn(up, o);
+                if (P.out_dtype == 0) reinterpret_cast<float*>(update)[to] = u;
+                else if (P.out_dtype == 1) reinterpret_cast<__nv_bfloat16*>(update)[to] = __float2bfloat16_rn(u);
+                else reinterpret_cast<__half*>(update)[to] = __float2half_rn(u);
+            }
+        }
+    }
+}
+
 __device__ __forceinline__ void prefetch_map(const void* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -507,7 +607,7 @@ __device__ __forceinline__ bool elect_one() {
 // so they have been taken by CTAs that are running: some tile can always go on, whatever number
 // of CTAs the GPU has room for.
 template <int CG, int TN, bool SPLIT>
-__global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_iterate_kernel(const MuonIterate P) {
+__global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_iterate_kernel(const __grid_constant__ MuonIterate P) {
     using S = MuonShape<CG, TN, SPLIT>;
     extern __shared__ unsigned char raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 6 + 2 * kMuonQueue];
@@ -594,6 +694,8 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 const uint32_t row = task.i * (CG * 128u) + rank * 128u;
                 const uint32_t col = task.j * (uint32_t)TN + rank * (TN / CG);
                 const bool along_n = kind == kMuonApply, wide = S::kBoxesB == 2;
+                // a tile on the diagonal of M M^T has one operand on both sides
+                const bool once = S::kBoxesB == 2 && !along_n && pr.left == pr.right && task.i == task.j;
                 const unsigned char* ma = map + ((kind == kMuonGram ? kMapX128 : kMapM128) + 2 * pr.left) * 128;
                 const unsigned char* mb = map + ((kind == kMuonGram ? (wide ? kMapX128 : kMapX64)
                                                   : along_n ? (wide ? kMapXN128 : kMapXN64)
@@ -607,12 +709,13 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 for (uint32_t k = 0; k < kb; ++k, ++it) {
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
                     if (!muon_wait(empty + 8 * s, ph ^ 1, limit, &stop)) { ok = false; break; }
-                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * S::kStageBytes);
+                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * (once ? S::kHalves * S::kBytesA : S::kStageBytes));
                     const uint32_t bar = CG == 1 ? full + 8 * s : leader_addr(full + 8 * s);
                     const uint32_t da = ring + s * S::kStageBytes, db = da + S::kHalves * S::kBytesA;
 #pragma unroll
                     for (uint32_t h = 0; h < S::kHalves; ++h) {
                         muon_load<CG>(da + h * S::kBytesA, ma + 128 * h, k * 64, row, bar);
+                        if (once) continue;
                         if (along_n) muon_load3<CG>(db + h * S::kBytesB, mb + 128 * h, 0, k * 64, col / 64, bar);
                         else muon_load<CG>(db + h * S::kBytesB, mb + 128 * h, k * 64, col, bar);
                     }
@@ -636,13 +739,16 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 taken(n);
                 if (t >= P.n_tasks) break;
                 const MuonTask task = P.tasks[t];
-                const int kind = P.products[task.product].kind;
+                const MuonProduct& pr = P.products[task.product];
+                const int kind = pr.kind;
                 const MuonMat& mat = P.mats[task.mat];
                 const uint32_t kb = ((kind == kMuonGram ? mat.n : mat.m) + 63) / 64;
                 const bool along_n = kind == kMuonApply;               // right operand's rows run along K
                 // fp32 accumulators, fp16 operands
                 const uint32_t idesc = (1u << 4) | ((uint32_t)(TN / 8) << 17) | ((uint32_t)(CG * 128 / 16) << 24) |
                                        (along_n ? 1u << 16 : 0u);
+                const bool once = S::kBoxesB == 2 && !along_n && pr.left == pr.right && task.i == task.j;
+                const uint32_t b_at = once ? 0 : S::kHalves * S::kBytesA;
                 const uint32_t b_lead = along_n ? kMuonBox : 16;
                 const uint32_t b_k16 = along_n ? 2048u : 32u;          // bytes to the next 16 along K
                 uint32_t in_chunk = 0, d = 0;
@@ -654,7 +760,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
                     if (!muon_wait(full + 8 * s, ph, limit, &stop)) { ok = false; break; }
                     tcgen05_after_sync();
-                    const uint32_t a0 = ring + s * S::kStageBytes, b0 = a0 + S::kHalves * S::kBytesA;
+                    const uint32_t a0 = ring + s * S::kStageBytes, b0 = a0 + b_at;
                     const uint64_t da = umma_desc(a0, 16, 1024), db = umma_desc(b0, b_lead, 1024);
                     const uint64_t dal = umma_desc(a0 + S::kBytesA, 16, 1024), dbl = umma_desc(b0 + S::kBytesB, b_lead, 1024);
 #pragma unroll
@@ -758,7 +864,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                     go = muon_wait_done(P.done + task.mat, (unsigned long long)S::kParts * task.need, limit, &stop, 100);
                 if (!__shfl_sync(~0u, go, 0)) break;
             }
-            fetch(0);
+            if (!SPLIT) fetch(0);
 
             float sum[SPLIT ? S::kCols : 1];
             if (SPLIT) {
@@ -770,13 +876,13 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                     if (!ok) break;
                     tcgen05_after_sync();
 #pragma unroll
-                    for (uint32_t h = 0; h < kBlocks; ++h) {
-                        float v[32], w[32];
-                        tmem_load32(lane_addr + (acc & 1) * S::kAccCols + c0 + 32 * h, v);
-                        tmem_load32(lane_addr + (acc & 1) * S::kAccCols + TN + c0 + 32 * h, w);
+                    for (uint32_t h = 0; h < S::kCols / 16; ++h) {
+                        float v[16], w[16];
+                        tmem_load16(lane_addr + (acc & 1) * S::kAccCols + c0 + 16 * h, v);
+                        tmem_load16(lane_addr + (acc & 1) * S::kAccCols + TN + c0 + 16 * h, w);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            sum[SPLIT ? 32 * h + i : 0] = __fadd_rn(sum[SPLIT ? 32 * h + i : 0], __fadd_rn(v[i], w[i]));
+                        for (int i = 0; i < 16; ++i)
+                            sum[SPLIT ? 16 * h + i : 0] = __fadd_rn(sum[SPLIT ? 16 * h + i : 0], __fadd_rn(v[i], w[i]));
                     }
                     tcgen05_before_sync();
                     __syncwarp();
@@ -790,12 +896,11 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 tcgen05_after_sync();
             }
             if (!ok) break;
+            if (SPLIT) fetch(0);                                       // not before: the sums take the registers
 
-#pragma unroll
-            for (uint32_t b = 0; b < kBlocks; ++b) {
-                if (b >= blocks) break;                                // the whole warp
+            // a finished block, 32 columns of this lane's row
+            auto result = [&](uint32_t b, float* y) {
                 const uint32_t col = col0 + 32 * b;
-                float y[32];
                 if (SPLIT) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) y[i] = sum[SPLIT ? 32 * b + i : 0];
@@ -846,169 +951,126 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                     }
                     fetch(b + 1);
                 }
-                if (!last) {
-                    uint32_t hi[16];
+            };
+            auto keep_block = [&](uint32_t b) {
+                const uint32_t col = col0 + 32 * b;
+                float y[32];
+                result(b, y);
+                uint32_t hi[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) hi[i] = Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
+                for (int i = 0; i < 16; ++i) hi[i] = Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
+#pragma unroll
+                for (uint32_t c = 0; c < 4; ++c)
+                    sts16(own + ((c ^ flip) << 4), make_uint4(hi[4 * c], hi[4 * c + 1], hi[4 * c + 2], hi[4 * c + 3]));
+                uint4* order = reinterpret_cast<uint4*>(order_out) + 256 * b;
+                if (flags & kMuonWriteWide) {
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) __stcg(order + 32 * i, Elem<float>::narrow(y + 4 * i));
+                } else if (flags & kMuonWriteNarrow) {
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
+                        __stcg(order + 32 * i, make_uint4(hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]));
+                }
+                if (SPLIT) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[i]));
+                        unpack2(sub2(pack2(y[2 * i], y[2 * i + 1]), pack2(f.x, f.y)), y[2 * i], y[2 * i + 1]);
+                    }
 #pragma unroll
                     for (uint32_t c = 0; c < 4; ++c)
-                        sts16(own + ((c ^ flip) << 4), make_uint4(hi[4 * c], hi[4 * c + 1], hi[4 * c + 2], hi[4 * c + 3]));
-                    uint4* order = reinterpret_cast<uint4*>(order_out) + 256 * b;
-                    if (flags & kMuonWriteWide) {
+                        sts16(own + kMuonBlock + ((c ^ flip) << 4), Elem<__half>::narrow(y + 8 * c));
+                }
+                __syncwarp();
+                flush(copy_to, out_hi + 32 * b);
+                if (SPLIT) flush(copy_to + kMuonBlock, out_lo + 32 * b);
+                if (mirror) {
+                    // the transposed block: row c of it has the 32 lanes' entries of column c
+                    auto turn = [&](const uint32_t* w, __half* base) {
+                        __syncwarp();
 #pragma unroll
-                        for (uint32_t i = 0; i < 8; ++i) __stcg(order + 32 * i, Elem<float>::narrow(y + 4 * i));
-                    } else if (flags & kMuonWriteNarrow) {
+                        for (uint32_t i = 0; i < 32; ++i)
+                            asm volatile("st.shared.b16 [%0], %1;"
+                                         ::"r"(block + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + 2 * (lane & 7)),
+                                         "h"((uint16_t)(w[i >> 1] >> (16 * (i & 1)))) : "memory");
+                        __syncwarp();
+                        __half* to = base + mat.g_at + (uint64_t)(col + cr) * ld + row0 + 8 * cc;
 #pragma unroll
                         for (uint32_t i = 0; i < 4; ++i)
-                            __stcg(order + 32 * i, make_uint4(hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]));
-                    }
+                            if (col + cr + 8 * i < m) *reinterpret_cast<uint4*>(to + i * down) = lds16(copy_to + 512 * i);
+                    };
+                    turn(hi, P.ws.mh[pr.out]);
                     if (SPLIT) {
+                        uint32_t lo[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[i]));
-                            unpack2(sub2(pack2(y[2 * i], y[2 * i + 1]), pack2(f.x, f.y)), y[2 * i], y[2 * i + 1]);
-                        }
-#pragma unroll
-                        for (uint32_t c = 0; c < 4; ++c)
-                            sts16(own + kMuonBlock + ((c ^ flip) << 4), Elem<__half>::narrow(y + 8 * c));
+                        for (int i = 0; i < 16; ++i) lo[i] = Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
+                        turn(lo, P.ws.ml[pr.out]);
                     }
-                    __syncwarp();
-                    flush(copy_to, out_hi + 32 * b);
-                    if (SPLIT) flush(copy_to + kMuonBlock, out_lo + 32 * b);
-                    if (mirror) {
-                        // the transposed block: row c of it has the 32 lanes' entries of column c
-                        auto turn = [&](const uint32_t* w, __half* base) {
-                            __syncwarp();
+                }
+                __syncwarp();                                      // the buffer is free again
+            };
+            auto out_block = [&](uint32_t b) {
+                const uint32_t col = col0 + 32 * b;
+                float y[32];
+                result(b, y);
+                // to the caller's vectors: the block turned in shared memory to the caller's rows
+                // (where X is the transpose, its columns)
+                const bool narrow = !P.out.params && P.out_dtype != 0;
+                __syncwarp();
+                if (narrow) {
+                    const float scale = P.out.scaled ? mat.scale : 1.f;
 #pragma unroll
-                            for (uint32_t i = 0; i < 32; ++i)
+                    for (uint32_t c = 0; c < 4; ++c) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float u = __fmul_rn(scale, y[8 * c + 2 * i]), v = __fmul_rn(scale, y[8 * c + 2 * i + 1]);
+                            w[i] = P.out_dtype == 1 ? Elem<__nv_bfloat16>::pair(u, v) : Elem<__half>::pair(u, v);
+                        }
+                        if (!mat.tall) {
+                            sts16(own + ((c ^ flip) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
                                 asm volatile("st.shared.b16 [%0], %1;"
-                                             ::"r"(block + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + 2 * (lane & 7)),
+                                             ::"r"(block + muon_swizzle(8 * c + i, lane >> 3) + 2 * (lane & 7)),
                                              "h"((uint16_t)(w[i >> 1] >> (16 * (i & 1)))) : "memory");
-                            __syncwarp();
-                            __half* to = base + mat.g_at + (uint64_t)(col + cr) * ld + row0 + 8 * cc;
-#pragma unroll
-                            for (uint32_t i = 0; i < 4; ++i)
-                                if (col + cr + 8 * i < m) *reinterpret_cast<uint4*>(to + i * down) = lds16(copy_to + 512 * i);
-                        };
-                        turn(hi, P.ws.mh[pr.out]);
-                        if (SPLIT) {
-                            uint32_t lo[16];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) lo[i] = Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
-                            turn(lo, P.ws.ml[pr.out]);
                         }
                     }
-                } else {
-                    // to the caller's vectors: rows of the block along its own or, where X is the
-                    // transpose, along its columns
-                    const bool tall = mat.tall;
-                    const uint32_t or0 = tall ? col : row0, oc0 = tall ? row0 : col;
-                    const uint32_t rows = mat.rows, cols = mat.cols;
-                    const uint64_t offset = mat.offset, stride = mat.stride;
-                    const bool sound = P.sound[task.mat] != 0;
-                    __syncwarp();
-                    if (!P.out.params && P.out_dtype != 0) {
-                        const float scale = P.out.scaled ? mat.scale : 1.f;
-                        const bool bf = P.out_dtype == 1;
-                        uint16_t* out = reinterpret_cast<uint16_t*>(P.out.update) + offset + (uint64_t)(or0 + cr) * stride + oc0 + 8 * cc;
-                        const bool whole = ((offset | stride) & 7) == 0;
+                } else {                                           // 16-byte pieces of a row exchanged by its number
 #pragma unroll
-                        for (uint32_t c = 0; c < 4; ++c) {
-                            uint32_t w[4];
+                    for (uint32_t c = 0; c < 8; ++c) {
+                        if (!mat.tall) {
+                            sts16(block + lane * 128 + ((c ^ (lane & 7)) << 4), Elem<float>::narrow(y + 4 * c));
+                        } else {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float u = __fmul_rn(scale, y[8 * c + 2 * i]), v = __fmul_rn(scale, y[8 * c + 2 * i + 1]);
-                                w[i] = bf ? Elem<__nv_bfloat16>::pair(u, v) : Elem<__half>::pair(u, v);
-                            }
-                            if (!tall) {
-                                sts16(own + ((c ^ flip) << 4), make_uint4(w[0], w[1], w[2], w[3]));
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 8; ++i)
-                                    asm volatile("st.shared.b16 [%0], %1;"
-                                                 ::"r"(block + muon_swizzle(8 * c + i, lane >> 3) + 2 * (lane & 7)),
-                                                 "h"((uint16_t)(w[i >> 1] >> (16 * (i & 1)))) : "memory");
-                            }
-                        }
-                        __syncwarp();
-#pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i) {
-                            const uint32_t oc = oc0 + 8 * cc;
-                            if (or0 + cr + 8 * i >= rows || oc >= cols) continue;
-                            const uint4 v = lds16(copy_to + 512 * i);
-                            uint16_t* to = out + 8 * i * stride;
-                            if (whole && oc + 8 <= cols) {
-                                *reinterpret_cast<uint4*>(to) = v;
-                            } else {
-                                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                                for (int k = 0; k < 8; ++k)
-                                    if (oc + k < cols) to[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
-                            }
-                        }
-                    } else {
-                        // 32 x 32 floats, 16-byte pieces of a row exchanged by its number
-                        const bool whole = ((offset | stride) & 3) == 0;
-#pragma unroll
-                        for (uint32_t c = 0; c < 8; ++c) {
-                            if (!tall) {
-                                sts16(block + lane * 128 + ((c ^ (lane & 7)) << 4), Elem<float>::narrow(y + 4 * c));
-                            } else {
-#pragma unroll
-                                for (uint32_t i = 4 * c; i < 4 * c + 4; ++i)
-                                    asm volatile("st.shared.f32 [%0], %1;"
-                                                 ::"r"(block + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + 4 * (lane & 3)), "f"(y[i])
-                                                 : "memory");
-                            }
-                        }
-                        __syncwarp();
-                        const uint32_t fr = lane >> 3, fc = lane & 7;
-#pragma unroll
-                        for (uint32_t i = 0; i < 8; ++i) {
-                            const uint32_t rr = i * 4 + fr, oc = oc0 + 4 * fc;
-                            if (or0 + rr >= rows || oc >= cols) continue;
-                            float o[4], u[4];
-                            Elem<float>::widen(lds16(block + rr * 128 + ((fc ^ (rr & 7)) << 4)), o);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) u[k] = P.out.scaled ? __fmul_rn(mat.scale, o[k]) : o[k];
-                            const uint64_t at = offset + (uint64_t)(or0 + rr) * stride + oc;
-                            const uint32_t count = min(4u, cols - oc);
-                            if (P.out.update) {
-                                if (P.out_dtype == 0) {
-                                    float* to = reinterpret_cast<float*>(P.out.update) + at;
-                                    if (whole && count == 4) *reinterpret_cast<uint4*>(to) = Elem<float>::narrow(u);
-                                    else
-#pragma unroll
-                                        for (uint32_t k = 0; k < 4; ++k)
-                                            if (k < count) to[k] = u[k];
-                                } else {
-                                    uint16_t* to = reinterpret_cast<uint16_t*>(P.out.update) + at;
-#pragma unroll
-                                    for (uint32_t k = 0; k < 4; ++k)
-                                        if (k < count)
-                                            to[k] = P.out_dtype == 1 ? __bfloat16_as_ushort(__float2bfloat16_rn(u[k]))
-                                                                     : __half_as_ushort(__float2half_rn(u[k]));
-                                }
-                            }
-                            if (P.out.params && sound) {
-                                float* to = P.out.params + at;
-                                const float rate = -__fmul_rn(P.out.rate, mat.scale);
-                                if (whole && count == 4) {
-                                    float p[4];
-                                    Elem<float>::widen(*reinterpret_cast<const uint4*>(to), p);
-#pragma unroll
-                                    for (int k = 0; k < 4; ++k) p[k] = __fmaf_rn(rate, o[k], __fmul_rn(P.out.keep, p[k]));
-                                    *reinterpret_cast<uint4*>(to) = Elem<float>::narrow(p);
-                                } else {
-#pragma unroll
-                                    for (uint32_t k = 0; k < 4; ++k)
-                                        if (k < count) to[k] = __fmaf_rn(rate, o[k], __fmul_rn(P.out.keep, to[k]));
-                                }
-                            }
+                            for (uint32_t i = 4 * c; i < 4 * c + 4; ++i)
+                                asm volatile("st.shared.f32 [%0], %1;"
+                                             ::"r"(block + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + 4 * (lane & 3)), "f"(y[i])
+                                             : "memory");
                         }
                     }
                 }
-                __syncwarp();                                          // the buffer is free again
+                __syncwarp();
+                const uint32_t or0 = mat.tall ? col : row0, oc0 = mat.tall ? row0 : col;
+                if (narrow) muon_out_narrow(P, mat, block, or0, oc0);
+                else muon_out_wide(P, mat, block, or0, oc0, P.sound[task.mat] != 0);
+                __syncwarp();
+            };
+            // sums in registers need fixed places; elsewhere a loop is kept, as unrolled code spills
+            if constexpr (SPLIT) {
+#pragma unroll
+                for (uint32_t b = 0; b < kBlocks; ++b)
+                    if (b < blocks) {                                  // the whole warp
+                        if (!last) keep_block(b);
+                        else out_block(b);
+                    }
+            } else if (!last) {
+#pragma unroll 1
+                for (uint32_t b = 0; b < blocks; ++b) keep_block(b);
+            } else {
+#pragma unroll 1
+                for (uint32_t b = 0; b < blocks; ++b) out_block(b);
             }
             if (!SPLIT) {
                 tcgen05_before_sync();
