@@ -21,9 +21,9 @@ namespace {
 struct Step { float a, b, c, shift; };
 
 // Tile shapes of the product kernel: CTAs per tile and columns (rows are 128 a CTA).
-struct Shape { uint32_t cg, tn; bool split; };
-constexpr Shape kShapes[] = {{2, 256, false}, {1, 128, false}, {1, 64, false}, {2, 128, true}, {1, 64, true}};
-constexpr int kShapeCount = 5;
+struct Shape { uint32_t cg, tn; };
+constexpr Shape kShapes[] = {{2, 256}, {2, 128}, {1, 128}, {1, 64}};
+constexpr int kShapeCount = 4;
 
 uint64_t round64(uint64_t x) { return (x + 63) / 64 * 64; }
 
@@ -36,8 +36,7 @@ struct ecq_muon {
     uint32_t wait_limit;
     std::vector<Step> steps;
     std::vector<MuonMat> mats;
-    uint64_t x_entries, g_entries;       // fp16 entries of one copy of X, of one m x m buffer
-    uint64_t xm_entries, gm_entries;     // entries of the same in block order
+    uint64_t x_tiles, m_tiles;           // tiles of one X buffer, of one m x m buffer
     // device tables, one allocation
     unsigned char* block;
     MuonMat* d_mats;
@@ -48,7 +47,7 @@ struct ecq_muon {
     MuonProduct* d_products;
     unsigned long long *d_done, *d_next;
     uint32_t *d_sound, *d_status, *h_status;
-    unsigned char* d_maps;
+    CUtensorMap rows128, rows64;         // of the bound workspace
     uint32_t n_spans, n_prep, n_tasks[kShapeCount], products_at[kShapeCount];
     uint64_t n_full[kShapeCount];        // tiles of one product with X, over all matrices
     unsigned char* workspace;            // the caller's, NULL until bound
@@ -56,11 +55,9 @@ struct ecq_muon {
 
 namespace {
 
-// Map of a matrix of `rows` rows of `inner` fp16, loaded in boxes of 64 entries of box_rows rows.
-// With `columns` it is taken as columns / 64 matrices of 64 columns each instead, next to each other,
-// `boxes` of which a box spans.
-bool tensor_map(CUtensorMap* tm, const __half* base, uint64_t inner, uint64_t rows, uint64_t ld, uint32_t box_rows,
-                uint64_t columns = 0, uint32_t boxes = 0) {
+// Map of `tiles` tiles as pieces of 16 times eight rows of 16 bytes, loaded in boxes of eight pieces
+// of `units` times eight rows.
+bool tensor_map(CUtensorMap* tm, void* base, uint64_t tiles, uint32_t units) {
     typedef CUresult (*Fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -74,32 +71,23 @@ bool tensor_map(CUtensorMap* tm, const __half* base, uint64_t inner, uint64_t ro
             fn = reinterpret_cast<Fn>(p);
     });
     if (!fn) return false;
-    const cuuint64_t dims[3] = {columns ? 64 : inner, rows, columns / 64}, strides[2] = {ld * 2, 128};
-    const cuuint32_t box[3] = {64, box_rows, boxes}, unit[3] = {1, 1, 1};
-    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, columns ? 3 : 2, const_cast<__half*>(base), dims, strides, box, unit,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint64_t dims[3] = {64, 16, 8 * tiles}, strides[2] = {128, kMuonPiece};
+    const cuuint32_t box[3] = {64, units, 8}, unit[3] = {1, 1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, base, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+uint64_t workspace_tiles(const ecq_muon* p) { return 4 * p->x_tiles + 2 * kMuonSquare * p->m_tiles; }
 
 MuonWork work_of(const ecq_muon* p) {
     MuonWork w;
-    __half* at = reinterpret_cast<__half*>(p->workspace);
-    for (int c = 0; c < 2; ++c) {
-        w.xh[c] = at; at += p->x_entries;
-        w.xl[c] = at; at += p->x_entries;
-    }
-    for (int k = 0; k < kMuonSquare; ++k) {
-        w.mh[k] = at; at += p->g_entries;
-        w.ml[k] = at; at += p->g_entries;
-    }
-    float* order = reinterpret_cast<float*>(at);
-    w.xm = order; order += p->xm_entries;
-    for (int k = 0; k < kMuonSquare; ++k) { w.mm[k] = order; order += p->gm_entries; }
+    uint32_t at = 0;
+    w.base = p->workspace;
+    for (auto& copy : w.x)
+        for (uint32_t& half : copy) { half = at; at += (uint32_t)p->x_tiles; }
+    for (auto& square : w.m)
+        for (uint32_t& half : square) { half = at; at += (uint32_t)p->m_tiles; }
     return w;
-}
-
-uint64_t workspace_bytes(const ecq_muon* p) {
-    return 8 * p->x_entries + 4 * p->xm_entries + kMuonSquare * (4 * p->g_entries + 4 * p->gm_entries);
 }
 
 // Singular values start in (0, 1]; the scaled fp16 copies hold iterates up to 8 and polynomials
@@ -141,10 +129,10 @@ uint32_t mergeable(const std::vector<Step>& steps) {
 
 // Products of one matrix in their order.  m x m buffers: 0 G, 1 and 2 B, 3 S, 4 R; the last R of
 // merged steps goes to S's place.
-std::vector<MuonProduct> program(const std::vector<Step>& steps, uint32_t merge, bool split) {
+std::vector<MuonProduct> program(const std::vector<Step>& steps, uint32_t merge) {
     constexpr uint8_t none = 255;
     const float sx = kMuonScaleX, sg = kMuonScaleG;
-    const uint8_t wide = kMuonReadWide | kMuonWriteWide;
+    const int in_low = kMuonReadLow, out_low = kMuonWriteLow, both = in_low | out_low;
     const uint32_t n = (uint32_t)steps.size();
     std::vector<MuonProduct> out;
     auto put = [&](int kind, int left, int right, int to, int in, int in2, float lin, float lin2, float acc, float shift,
@@ -155,42 +143,40 @@ std::vector<MuonProduct> program(const std::vector<Step>& steps, uint32_t merge,
     };
     uint32_t copy = 0;
     for (uint32_t k = 0; k < n;) {
-        // X is kept in fp32 while small singular values are still to be amplified: an error made in
+        // X has a low half while small singular values are still to be amplified: an error made in
         // the last two steps is not
         const uint32_t end = k == 0 ? merge : k + 1;
-        const int x_in = split || k + 2 < n ? kMuonReadWide : 0;
-        const int x_out = split || end + 2 < n ? kMuonWriteWide : kMuonWriteNarrow;
         const float unscale = end == n ? 1.f / sx : 1.f;
-        const int x_flags = x_in | (end == n ? kMuonLast : x_out);
+        const int x_flags = (k + 2 < n ? in_low : 0) | (end == n ? kMuonLast : end + 2 < n ? out_low : 0);
         if (end == k + 1) {
-            // b G + c G^2 with G = D + t I.  Without SPLIT it takes D as the operands have it: their
-            // rounding errors cancel in part
+            // b G + c G^2 with G = D + t I, of D as the operands have it: their rounding errors
+            // cancel in part
             const Step& s = steps[k];
             const float t = s.shift;
-            put(kMuonGram, copy, copy, 0, none, none, 0.f, 0.f, sg / (sx * sx), sg * t, split ? kMuonWriteWide : kMuonWriteNarrow);
-            put(kMuonSym, 0, 0, 1, 0, none, s.b + 2 * s.c * t, 0.f, s.c / sg, 0.f, split ? kMuonReadWide : 0);
+            put(kMuonGram, copy, copy, 0, none, none, 0.f, 0.f, sg / (sx * sx), sg * t, 0);
+            put(kMuonSym, 0, 0, 1, 0, none, s.b + 2 * s.c * t, 0.f, s.c / sg, 0.f, 0);
             put(kMuonApply, 1, copy, copy ^ 1, 0, none, (s.a + s.b * t + s.c * t * t) * unscale, 0.f, unscale / sg, 0.f, x_flags);
         } else {
             float alpha = steps[0].a;
             int r = 1, b = 1;                                          // the first R is the first B
-            put(kMuonGram, copy, copy, 0, none, none, 0.f, 0.f, sg / (sx * sx), 0.f, kMuonWriteWide);
-            put(kMuonSym, 0, 0, 1, 0, none, steps[0].b, 0.f, steps[0].c / sg, 0.f, wide);
+            put(kMuonGram, copy, copy, 0, none, none, 0.f, 0.f, sg / (sx * sx), 0.f, out_low);
+            put(kMuonSym, 0, 0, 1, 0, none, steps[0].b, 0.f, steps[0].c / sg, 0.f, in_low);
             for (uint32_t j = 1; j < end; ++j) {
                 const Step &before = steps[j - 1], &s = steps[j];
-                // R of the step before last is formed beside S: it needs no more than B
-                put(kMuonSym, b, 0, 3, 0, none, before.a, 0.f, 1.f / sg, 0.f, wide);
+                put(kMuonSym, b, 0, 3, 0, none, before.a, 0.f, 1.f / sg, 0.f, both);
                 if (j == 2) {
-                    put(kMuonSym, 2, 1, 4, 1, 2, steps[1].a, alpha, 1.f / sg, 0.f, wide);
+                    // R of the step before last is formed beside S: it needs no more than B
+                    put(kMuonSym, 2, 1, 4, 1, 2, steps[1].a, alpha, 1.f / sg, 0.f, 0);
                     out.back().after -= 1;
                     alpha *= steps[1].a;
                     r = 4;
                 }
-                put(kMuonSym, b, 3, 0, 3, none, before.a, 0.f, 1.f / sg, 0.f, wide);
+                put(kMuonSym, b, 3, 0, 3, none, before.a, 0.f, 1.f / sg, 0.f, both);
                 b = j == 1 ? 2 : 1;
-                put(kMuonSym, 0, 0, b, 0, none, s.b, 0.f, s.c / sg, 0.f, wide);
+                put(kMuonSym, 0, 0, b, 0, none, s.b, 0.f, s.c / sg, 0.f, in_low);
             }
             const Step& s = steps[end - 1];
-            put(kMuonSym, b, r, 3, r, b, s.a, alpha, 1.f / sg, 0.f, wide);
+            put(kMuonSym, b, r, 3, r, b, s.a, alpha, 1.f / sg, 0.f, 0);
             alpha *= s.a;
             put(kMuonApply, 3, copy, copy ^ 1, 0, none, alpha * unscale, 0.f, unscale / sg, 0.f, x_flags);
         }
@@ -218,8 +204,8 @@ struct TaskList {
 
     TaskList(const std::vector<MuonMat>& all, Shape s, const std::vector<Step>& steps)
         : mats(all), shape(s), sym(all.size()), full(all.size()) {
-        products = program(steps, 1, s.split);
-        const std::vector<MuonProduct> merged = program(steps, mergeable(steps), s.split);
+        products = program(steps, 1);
+        const std::vector<MuonProduct> merged = program(steps, mergeable(steps));
         count[0] = (uint32_t)products.size();
         count[1] = (uint32_t)merged.size();
         products.insert(products.end(), merged.begin(), merged.end());
@@ -263,11 +249,11 @@ struct TaskList {
     void build() {
         std::vector<std::pair<uint32_t, uint32_t>> groups;
         uint64_t all = 0, held = 0;
-        for (const MuonMat& mat : mats) all += (uint64_t)mat.m * mat.ld_x;
+        for (const MuonMat& mat : mats) all += (uint64_t)mat.m * mat.n;
         const uint64_t most = std::min<uint64_t>(kGroupEntries, (all + kLanes - 1) / kLanes);
         uint32_t from = 0;
         for (uint32_t i = 0; i < mats.size(); ++i) {
-            held += (uint64_t)mats[i].m * mats[i].ld_x;
+            held += (uint64_t)mats[i].m * mats[i].n;
             if (held >= most || i + 1 == mats.size()) {
                 groups.push_back({from, i + 1});
                 from = i + 1;
@@ -327,8 +313,8 @@ int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st
 // Tiles of a call: the plan's choice, or the largest of which there are enough for every SM.
 int choose_tiles(const ecq_muon* p, bool split) {
     if (p->tiles != ECQ_MUON_TILES_AUTO) return p->tiles;
-    if (p->n_full[split ? 3 : 0] * 2 >= (uint64_t)p->sms) return ECQ_MUON_TILES_256X256;
-    if (!split && p->n_full[1] >= (uint64_t)p->sms) return ECQ_MUON_TILES_128X128;
+    if (p->n_full[split ? 1 : 0] * 2 >= (uint64_t)p->sms) return ECQ_MUON_TILES_256X256;
+    if (!split && p->n_full[2] >= (uint64_t)p->sms) return ECQ_MUON_TILES_128X128;
     return ECQ_MUON_TILES_128X64;
 }
 
@@ -339,23 +325,24 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
                       : (out.params || out_dtype != ECQ_BF16) ? 3 : 1;
     if (in.momentum) {
         muon_norm_kernel<float, true><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<float, true><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, terms == 3, p->d_sound, p->d_done, p->d_next, p->d_status);
+        muon_prepare_kernel<float, true><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
     } else if (in_dtype == ECQ_F32) {
         muon_norm_kernel<float, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<float, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, terms == 3, p->d_sound, p->d_done, p->d_next, p->d_status);
+        muon_prepare_kernel<float, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
     } else if (in_dtype == ECQ_BF16) {
         muon_norm_kernel<__nv_bfloat16, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<__nv_bfloat16, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, terms == 3, p->d_sound, p->d_done, p->d_next, p->d_status);
+        muon_prepare_kernel<__nv_bfloat16, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
     } else {
         muon_norm_kernel<__half, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<__half, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, terms == 3, p->d_sound, p->d_done, p->d_next, p->d_status);
+        muon_prepare_kernel<__half, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
     }
     if (cudaGetLastError() != cudaSuccess) return ECQ_ERR_CUDA;
     g_launches.fetch_add(2, std::memory_order_relaxed);
 
     MuonIterate m = {};
     m.mats = p->d_mats;
-    m.maps = p->d_maps;
+    m.rows128 = p->rows128;
+    m.rows64 = p->rows64;
     m.sound = p->d_sound;
     m.ws = ws;
     m.done = p->d_done;
@@ -366,11 +353,11 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
     m.wait_limit = p->wait_limit;
     const int tiles = choose_tiles(p, terms == 3);
     if (terms == 3)
-        return tiles == ECQ_MUON_TILES_256X256 ? launch_iterate<2, 128, true>(p, m, 3, st)
-                                               : launch_iterate<1, 64, true>(p, m, 4, st);
+        return tiles == ECQ_MUON_TILES_256X256 ? launch_iterate<2, 128, true>(p, m, 1, st)
+                                               : launch_iterate<1, 64, true>(p, m, 3, st);
     return tiles == ECQ_MUON_TILES_256X256   ? launch_iterate<2, 256, false>(p, m, 0, st)
-           : tiles == ECQ_MUON_TILES_128X128 ? launch_iterate<1, 128, false>(p, m, 1, st)
-                                             : launch_iterate<1, 64, false>(p, m, 2, st);
+           : tiles == ECQ_MUON_TILES_128X128 ? launch_iterate<1, 128, false>(p, m, 2, st)
+                                             : launch_iterate<1, 64, false>(p, m, 3, st);
 }
 
 bool finite(float x) { return x - x == 0.f; }
@@ -399,15 +386,14 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
             return ECQ_ERR_ARG;
         mat.tall = mat.rows > mat.cols;
         mat.m = std::min(mat.rows, mat.cols); mat.n = std::max(mat.rows, mat.cols);
-        mat.ld_x = (uint32_t)round64(mat.n); mat.ld_g = (uint32_t)round64(mat.m);
+        mat.pad = (uint32_t)round64(mat.m);
+        mat.down = (mat.m + 127) / 128;
         mat.scale = scales ? scales[i] : 1.f;
         if (!finite(mat.scale)) return ECQ_ERR_ARG;
-        mat.x_at = p->x_entries; mat.g_at = p->g_entries;
-        p->x_entries += (uint64_t)mat.m * mat.ld_x;
-        p->g_entries += (uint64_t)mat.m * mat.ld_g;
-        mat.xm_at = p->xm_entries; mat.gm_at = p->gm_entries;
-        p->xm_entries += (uint64_t)((mat.m + 31) / 32 * 32) * mat.ld_x;
-        p->gm_entries += (uint64_t)((mat.m + 31) / 32 * 32) * mat.ld_g;
+        mat.x_tile = (uint32_t)p->x_tiles; mat.m_tile = (uint32_t)p->m_tiles;
+        p->x_tiles += round64(mat.n) / 64 * mat.down;
+        p->m_tiles += (uint64_t)mat.pad / 64 * mat.down;
+        if (workspace_tiles(p) > 0x0FFFFFFFull) return ECQ_ERR_ARG;    // pieces are TMA coordinates
         // spans of about kMuonSpan entries: flat where the rows lie end to end, else whole rows or parts of them
         mat.part0 = (uint32_t)spans.size();
         if (mat.stride == mat.cols) {
@@ -451,7 +437,6 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     for (int s = 0; s < kShapeCount; ++s) o_tasks[s] = place(tasks[s].size() * sizeof(MuonTask));
     const uint64_t o_partial = place(spans.size() * 8), o_sound = place(count * 4ull), o_status = place(4);
     const uint64_t o_products = place(table.size() * sizeof(MuonProduct)), o_done = place(count * 8ull), o_next = place(8);
-    const uint64_t o_maps = place((uint64_t)count * kMapsPerMat * 128);
     std::vector<unsigned char> host(bytes, 0);
     memcpy(host.data() + o_mats, p->mats.data(), count * sizeof(MuonMat));
     memcpy(host.data() + o_spans, spans.data(), spans.size() * sizeof(MuonSpan));
@@ -477,7 +462,6 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     p->d_products = reinterpret_cast<MuonProduct*>(p->block + o_products);
     p->d_done = reinterpret_cast<unsigned long long*>(p->block + o_done);
     p->d_next = reinterpret_cast<unsigned long long*>(p->block + o_next);
-    p->d_maps = p->block + o_maps;
     p->n_spans = (uint32_t)spans.size();
     p->n_prep = (uint32_t)prep.size();
     return ECQ_OK;
@@ -529,45 +513,15 @@ int ecq_muon_set_wait_limit(ecq_muon* p, uint32_t polls) {
     return ECQ_OK;
 }
 
-uint64_t ecq_muon_workspace_bytes(const ecq_muon* p) { return p ? workspace_bytes(p) : 0; }
+uint64_t ecq_muon_workspace_bytes(const ecq_muon* p) { return p ? kMuonTileBytes * workspace_tiles(p) : 0; }
 
 int ecq_muon_bind(ecq_muon* p, void* workspace, uint64_t bytes, void* cuda_stream) {
-    if (!p || !workspace || !aligned_to(workspace, 256) || bytes < workspace_bytes(p)) return ECQ_ERR_ARG;
+    if (!p || !workspace || !aligned_to(workspace, 256) || bytes < kMuonTileBytes * workspace_tiles(p)) return ECQ_ERR_ARG;
     if (cudaSetDevice(p->device) != cudaSuccess) return ECQ_ERR_CUDA;
     p->workspace = static_cast<unsigned char*>(workspace);
-    const MuonWork w = work_of(p);
-    try {
-        std::vector<CUtensorMap> maps(p->mats.size() * kMapsPerMat);
-        for (size_t i = 0; i < p->mats.size(); ++i) {
-            const MuonMat& mat = p->mats[i];
-            const __half* x[4] = {w.xh[0], w.xl[0], w.xh[1], w.xl[1]};
-            CUtensorMap* to = &maps[i * kMapsPerMat];
-            bool ok = true;
-            for (int k = 0; k < 4 && ok; ++k)
-                ok = tensor_map(to + kMapX128 + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 128) &&
-                     tensor_map(to + kMapX64 + k, x[k] + mat.x_at, mat.n, mat.m, mat.ld_x, 64) &&
-                     tensor_map(to + kMapXN128 + k, x[k] + mat.x_at, 64, mat.m, mat.ld_x, 64, mat.ld_x, 2) &&
-                     tensor_map(to + kMapXN64 + k, x[k] + mat.x_at, 64, mat.m, mat.ld_x, 64, mat.ld_x, 1);
-            for (int k = 0; k < 2 * kMuonSquare && ok; ++k) {
-                const __half* sq = (k & 1 ? w.ml[k / 2] : w.mh[k / 2]) + mat.g_at;
-                ok = tensor_map(to + kMapM128 + k, sq, mat.m, mat.m, mat.ld_g, 128) &&
-                     tensor_map(to + kMapM64 + k, sq, mat.m, mat.m, mat.ld_g, 64);
-            }
-            if (!ok) {
-                p->workspace = nullptr;
-                return ECQ_ERR_CUDA;
-            }
-        }
-        cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-        if (cudaMemcpyAsync(p->d_maps, maps.data(), maps.size() * sizeof(CUtensorMap), cudaMemcpyHostToDevice, st) !=
-                cudaSuccess ||
-            cudaStreamSynchronize(st) != cudaSuccess) {
-            p->workspace = nullptr;
-            return ECQ_ERR_CUDA;
-        }
-    } catch (const std::bad_alloc&) {
+    if (!tensor_map(&p->rows128, workspace, workspace_tiles(p), 16) || !tensor_map(&p->rows64, workspace, workspace_tiles(p), 8)) {
         p->workspace = nullptr;
-        return ECQ_ERR_ALLOC;
+        return ECQ_ERR_CUDA;
     }
     return ECQ_OK;
 }

@@ -4,6 +4,8 @@
 
 #include <cstdint>
 
+#include <cuda.h>
+
 #include "ecq_common.cuh"
 #include "ecq_elem.cuh"
 
@@ -21,16 +23,16 @@ namespace ecq {
 //     S = a G + B G,  G' = a S + B S,  R' = a R + alpha B + B R,  alpha' = a alpha
 // (3 m^3) and none of X's memory traffic.  Rounding errors of G' grow by a^2 a step relative to
 // small eigenvalues, so this is done for the first three steps at most, in which singular values
-// are brought up to order 1, with what is added to each product in fp32: no difference in the
-// result's error was measured against single steps.  (All five merged: up to 0.5.)
+// are brought up to order 1, with G and S as pairs: no difference in the result's error was
+// measured against single steps.  (All five merged: up to 0.5.)
 //
 // Numbers.  The products run on the tensor cores with fp16 operands and fp32 accumulators.  What
-// keeps the result accurate is that X itself is not rounded to 11 bits: it is kept in fp32 beside
-// the fp16 operand, and the linear term a X takes that.  A rounding error of X in the
+// keeps the result accurate is that X itself is not rounded to 11 bits: it is a pair hi + lo of fp16
+// (22 bits) of which the products take hi, and the linear term a X both.  A rounding error of X in the
 // directions of small singular values would be multiplied by a (3.44) in every step.  Against 64
 // bits, relative error of the result for spectra from flat to 1/i^1.5: bf16 throughout 1e-2 to
-// 9e-2, fp16 throughout 1e-3 to 1e-2, with X in fp32 3e-4 to 1.7e-3.  The last two steps have
-// nothing left to amplify, and X is kept in fp16 alone there (no difference measured).
+// 9e-2, fp16 throughout 1e-3 to 1e-2, with the pair 3e-4 to 1.7e-3.  The last two steps have
+// nothing left to amplify, and X has no low half there (no difference measured).
 // In the last two steps, where most singular values are near 1, G is replaced by D = G - I
 // (exactly the same polynomial: b G + c G^2 = (b + c) I + (b + 2c) D + c D^2), so that the
 // rounding of G's diagonal does not cancel against a X: 5e-4 to 1.1e-3.
@@ -45,10 +47,9 @@ constexpr float kMuonScaleG = 256.f;
 
 struct MuonMat {
     uint64_t offset, stride;             // in the caller's flat vectors, entries
-    uint64_t x_at, g_at;                 // in the workspace's fp16 arrays, entries
-    uint64_t xm_at, gm_at;               // in its arrays in block order, entries
     uint32_t rows, cols, m, n;
-    uint32_t ld_x, ld_g;                 // padded to 64 entries
+    uint32_t x_tile, m_tile;             // first tile in each X and m x m buffer of the workspace
+    uint32_t pad, down;                  // m rounded up to 64; tiles below each other, of 128 rows
     uint32_t part0, parts;               // its partial sums of squares
     uint32_t tall;
     float scale;
@@ -72,17 +73,24 @@ struct MuonOut {
 struct MuonSpan { uint64_t start, stride; uint32_t mat, rows, len; };   // rows of len entries
 struct MuonTile { uint32_t mat; uint16_t i, j; };
 
-// Operands are row-major fp16.  What the epilogues add to a product (X, G and so on) never feeds a
-// tensor core, and is kept in block order: blocks of 32 x 32 entries, row by
-// row, in each of which 16-byte pieces of the 32 rows follow each other, first all rows' first
-// pieces.  A thread that has a row of an accumulator then reads and writes its pieces directly, 512
-// contiguous bytes a warp, and nothing of it passes through shared memory, whose bandwidth the
-// operands use up.
+// The workspace is an array of tiles of 128 rows and 64 columns of fp16, 16 KB each, those of a
+// matrix's first 64 columns below each other first.  In a tile 16-byte pieces of 128 rows follow
+// each other, then the next pieces: the image that a tensor-core operand without swizzle has in
+// shared memory, with K along a row or along the rows alike.  Loads are plain boxes, and the 32
+// threads that have a row of an accumulator each read and write 512 contiguous bytes at a time:
+// results do not pass through shared memory, whose bandwidth the operands use up, and an SM's
+// stores, which leave it at 32 bytes a clock, are whole lines.  (Row-major operands, turned in shared
+// memory, with fp32 copies beside them for what is added: 2 bytes an entry more to store; rows of
+// 128 swizzled bytes, a row per thread: 32 lines an instruction, and slower still.)  Up to the next
+// multiple of 64, entries beyond a matrix's rows and columns are zeros.
 constexpr int kMuonSquare = 5;           // m x m buffers: G, B, another B, S, R
 struct MuonWork {
-    __half *xh[2], *xl[2], *mh[kMuonSquare], *ml[kMuonSquare];
-    float *xm, *mm[kMuonSquare];
+    unsigned char* base;
+    uint32_t x[2][2], m[kMuonSquare][2]; // first tile of each buffer; copies of X; hi, lo
 };
+constexpr uint32_t kMuonTileBytes = 16384, kMuonPiece = 2048;
+
+__device__ __forceinline__ unsigned char* muon_tile(const MuonWork& ws, uint32_t tile) { return ws.base + (uint64_t)tile * kMuonTileBytes; }
 
 __device__ __forceinline__ float muon_direction(const MuonIn& in, float g, float m_new) {
     return in.nesterov ? __fmaf_rn(in.mu, m_new, g) : m_new;
@@ -152,7 +160,7 @@ __device__ __forceinline__ void muon_split(float v, __half& hi, __half& lo) {
 // NaN or Inf: then X_0 = 0 and its momentum (and later its weights) stay as they are.
 template <typename T, bool MOM>
 __global__ void __launch_bounds__(kMuonPrepThreads) muon_prepare_kernel(
-    const MuonMat* mats, const MuonTile* tiles, const double* partial, MuonIn in, MuonWork ws, int low, uint32_t* sound,
+    const MuonMat* mats, const MuonTile* tiles, const double* partial, MuonIn in, MuonWork ws, uint32_t* sound,
     unsigned long long* done, unsigned long long* next, uint32_t* status) {
     const MuonTile tile = tiles[blockIdx.x];
     const MuonMat mat = mats[tile.mat];
@@ -247,26 +255,23 @@ __global__ void __launch_bounds__(kMuonPrepThreads) muon_prepare_kernel(
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const uint32_t xr = xr0 + ty + 16 * k;
-        if (xr >= mat.m) continue;
         __half hi[4], lo[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) muon_split(x[k][i], hi[i], lo[i]);
-        const uint64_t to = mat.x_at + (uint64_t)xr * mat.ld_x + xc;  // xc + 4 <= ld_x: a tile is 64 wide
-        *reinterpret_cast<uint2*>(ws.xh[0] + to) = *reinterpret_cast<uint2*>(hi);
-        if (low) *reinterpret_cast<uint2*>(ws.xl[0] + to) = *reinterpret_cast<uint2*>(lo);
-        const uint64_t blk = mat.xm_at + ((uint64_t)(xr >> 5) * (mat.ld_x >> 5) + (xc >> 5)) * 1024;
-        *reinterpret_cast<uint4*>(ws.xm + blk + ((xc & 31) >> 2) * 128 + (xr & 31) * 4) = Elem<float>::narrow(x[k]);
+        const uint32_t tile = mat.x_tile + (xc >> 6) * mat.down + (xr >> 7);
+        const uint32_t at = (tx >> 1) * kMuonPiece + (xr & 127) * 16 + (tx & 1) * 8;
+        *reinterpret_cast<uint2*>(muon_tile(ws, ws.x[0][0] + tile) + at) = *reinterpret_cast<uint2*>(hi);
+        *reinterpret_cast<uint2*>(muon_tile(ws, ws.x[0][1] + tile) + at) = *reinterpret_cast<uint2*>(lo);
     }
 }
 
 // ---- tensor-core products --------------------------------------------------------------------
 
-// Shared-memory matrix descriptor of a tile in 128-byte swizzled rows: `lead` and `step` are the
-// byte distances between 64-wide column blocks (where the tile's rows are along K) and between
-// groups of eight 128-byte rows.
+// Shared-memory descriptor of an operand without swizzle: units of eight rows of 16 bytes, 128 bytes
+// each.  `lead` is the byte distance from a unit to the next one along K, `step` to the next one
+// along M or N.
 __device__ __forceinline__ uint64_t umma_desc(uint32_t addr, uint32_t lead, uint32_t step) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(step >> 4) << 32) |
-           (1ull << 46) | (2ull << 61);
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(step >> 4) << 32) | (1ull << 46);
 }
 
 template <int CG>
@@ -355,41 +360,26 @@ __device__ __forceinline__ void leader_arrive(uint32_t leader_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
 }
 
-// A box of fp16 into this CTA's shared memory; in a pair the bytes are counted on the first
+// Eight pieces of a tile's 128 or 64 rows (from the unit-th eight on) into this CTA's shared memory; in a pair the bytes are counted on the first
 // CTA's barrier.
 template <int CG>
-__device__ __forceinline__ void muon_load(uint32_t dst, const void* map, uint32_t x, uint32_t y, uint32_t bar) {
-    if (CG == 1)
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-                     " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
-                     : "memory");
-    else
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
-                     " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
-                     : "memory");
-}
-template <int CG>
-__device__ __forceinline__ void muon_load3(uint32_t dst, const void* map, uint32_t x, uint32_t y, uint32_t z, uint32_t bar) {
+__device__ __forceinline__ void muon_load(uint32_t dst, const void* map, uint32_t unit, uint32_t piece, uint32_t bar) {
     if (CG == 1)
         asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-                     " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                     " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(0), "r"(unit), "r"(piece), "r"(bar)
                      : "memory");
     else
         asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
-                     " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                     " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(0), "r"(unit), "r"(piece), "r"(bar)
                      : "memory");
 }
 
 enum { kMuonGram = 0, kMuonSym = 1, kMuonApply = 2 };                // X X^T, m x m, m x m times X
-// Tensor maps of a matrix, hi and lo next to each other: left operands in boxes of 128 rows, right
-// ones in boxes of 128 or 64, 64 entries along K each; X as the right operand whose rows run along
-// K, in boxes of 64 rows by one or two times 64 columns.  X has two copies.
-enum { kMapX128 = 0, kMapX64 = 4, kMapXN128 = 8, kMapXN64 = 12, kMapM128 = 16, kMapM64 = 26, kMapsPerMat = 36 };
 
 // One product of the iteration: out = lin * in + lin2 * in2 + acc * left right, less `shift` on the
-// diagonal.  Buffers are copies of X or m x m ones by the kind.  In block order, in and in2 are
-// fp32 with kMuonReadWide, else fp16; out is written there, too, as fp32 or fp16 or not at all.
-enum { kMuonReadWide = 1, kMuonWriteWide = 2, kMuonWriteNarrow = 4, kMuonLast = 8 };
+// diagonal.  Buffers are copies of X or m x m ones by the kind.  Low halves of in are read and of out
+// written with the flags (with SPLIT always, and then of in2, too).
+enum { kMuonReadLow = 1, kMuonWriteLow = 2, kMuonLast = 4 };
 struct MuonProduct {
     float lin, lin2, acc, shift;
     uint8_t kind, left, right, out;
@@ -406,8 +396,8 @@ struct MuonTask {
 };
 
 struct MuonIterate {
+    CUtensorMap rows128, rows64;         // the workspace, in boxes of 128 or 64 rows of a tile
     const MuonMat* mats;
-    const unsigned char* maps;           // kMapsPerMat tensor maps of 128 bytes per matrix
     const MuonTask* tasks;
     const MuonProduct* products;
     const uint32_t* sound;
@@ -499,6 +489,17 @@ __device__ __forceinline__ void sts16(uint32_t addr, uint4 v) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// A row's 32 columns of a block: four pieces.  (Reads of what other SMs have written come behind an
+// acquire.)
+__device__ __forceinline__ void muon_get(const unsigned char* p, uint4 (&v)[4]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = __ldcg(reinterpret_cast<const uint4*>(p + c * kMuonPiece));
+}
+__device__ __forceinline__ void muon_put(unsigned char* p, const uint4 (&v)[4]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) __stcg(reinterpret_cast<uint4*>(p + c * kMuonPiece), v[c]);
+}
+
 // A block of 32 x 32 finished entries, row or0 and column oc0 of the caller's matrix, from shared
 // memory (rows of 64 or 128 bytes) to the update and the weights.
 __device__ __forceinline__ void muon_out_narrow(const MuonIterate& P, const MuonMat& mat, uint32_t block, uint32_t or0, uint32_t oc0) {
@@ -587,10 +588,6 @@ __device__ __forceinline__ void muon_out_wide(const MuonIterate& P, const MuonMa
             }
         }
     }
-}
-
-__device__ __forceinline__ void prefetch_map(const void* map) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
 // One lane of a converged warp, in a form from which the compiler can tell that it is one: TMA and
@@ -688,22 +685,19 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 const MuonTask task = P.tasks[t];
                 const MuonProduct& pr = P.products[task.product];
                 const int kind = pr.kind;
-                const unsigned char* map = P.maps + (uint64_t)task.mat * kMapsPerMat * 128;
                 const MuonMat& mat = P.mats[task.mat];
-                const uint32_t kb = ((kind == kMuonGram ? mat.n : mat.m) + 63) / 64;
+                const uint32_t kb = ((kind == kMuonGram ? mat.n : mat.m) + 63) / 64, down = mat.down;
                 const uint32_t row = task.i * (CG * 128u) + rank * 128u;
                 const uint32_t col = task.j * (uint32_t)TN + rank * (TN / CG);
-                const bool along_n = kind == kMuonApply, wide = S::kBoxesB == 2;
+                const bool along_n = kind == kMuonApply;
                 // a tile on the diagonal of M M^T has one operand on both sides
                 const bool once = S::kBoxesB == 2 && !along_n && pr.left == pr.right && task.i == task.j;
-                const unsigned char* ma = map + ((kind == kMuonGram ? kMapX128 : kMapM128) + 2 * pr.left) * 128;
-                const unsigned char* mb = map + ((kind == kMuonGram ? (wide ? kMapX128 : kMapX64)
-                                                  : along_n ? (wide ? kMapXN128 : kMapXN64)
-                                                            : (wide ? kMapM128 : kMapM64)) + 2 * pr.right) * 128;
+                uint32_t left[2], right[2];                            // tiles
 #pragma unroll
                 for (uint32_t h = 0; h < S::kHalves; ++h) {
-                    prefetch_map(ma + 128 * h);
-                    prefetch_map(mb + 128 * h);
+                    left[h] = (kind == kMuonGram ? P.ws.x[pr.left][h] + mat.x_tile : P.ws.m[pr.left][h] + mat.m_tile) + row / 128;
+                    right[h] = (kind == kMuonSym ? P.ws.m[pr.right][h] + mat.m_tile : P.ws.x[pr.right][h] + mat.x_tile) +
+                               (along_n ? col / 64 * down : col / 128);
                 }
                 if (!muon_wait_done(P.done + task.mat, (unsigned long long)S::kParts * task.need, limit, &stop, 0)) break;
                 for (uint32_t k = 0; k < kb; ++k, ++it) {
@@ -714,10 +708,18 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                     const uint32_t da = ring + s * S::kStageBytes, db = da + S::kHalves * S::kBytesA;
 #pragma unroll
                     for (uint32_t h = 0; h < S::kHalves; ++h) {
-                        muon_load<CG>(da + h * S::kBytesA, ma + 128 * h, k * 64, row, bar);
+                        muon_load<CG>(da + h * S::kBytesA, &P.rows128, 0, 8 * (left[h] + k * down), bar);
                         if (once) continue;
-                        if (along_n) muon_load3<CG>(db + h * S::kBytesB, mb + 128 * h, 0, k * 64, col / 64, bar);
-                        else muon_load<CG>(db + h * S::kBytesB, mb + 128 * h, k * 64, col, bar);
+                        if (along_n) {                                 // 64 columns a box, their rows along K
+#pragma unroll
+                            for (uint32_t b = 0; b < S::kBoxesB; ++b)
+                                muon_load<CG>(db + h * S::kBytesB + b * kMuonBox, &P.rows64, (k & 1) * 8,
+                                              8 * (right[h] + b * down + k / 2), bar);
+                        } else if (S::kBoxesB == 2) {
+                            muon_load<CG>(db + h * S::kBytesB, &P.rows128, 0, 8 * (right[h] + k * down), bar);
+                        } else {
+                            muon_load<CG>(db + h * S::kBytesB, &P.rows64, (col & 64) / 8, 8 * (right[h] + k * down), bar);
+                        }
                     }
                     if (rank == 0 && k + 1 == kb) claim = atomicAdd(P.next, 1ull);
                 }
@@ -749,8 +751,10 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                                        (along_n ? 1u << 16 : 0u);
                 const bool once = S::kBoxesB == 2 && !along_n && pr.left == pr.right && task.i == task.j;
                 const uint32_t b_at = once ? 0 : S::kHalves * S::kBytesA;
-                const uint32_t b_lead = along_n ? kMuonBox : 16;
-                const uint32_t b_k16 = along_n ? 2048u : 32u;          // bytes to the next 16 along K
+                // bytes from a unit to the next along K and along M or N, and from 16 along K to the next
+                constexpr uint32_t a_lead = kMuonPiece, b_rows = S::kBoxesB * 1024;
+                const uint32_t b_lead = along_n ? 128 : b_rows, b_step = along_n ? 1024 : 128;
+                const uint32_t b_k16 = along_n ? 256 : 2 * b_rows;
                 uint32_t in_chunk = 0, d = 0;
                 for (uint32_t k = 0; k < kb; ++k, ++it) {
                     if (in_chunk == 0) {
@@ -761,12 +765,12 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                     if (!muon_wait(full + 8 * s, ph, limit, &stop)) { ok = false; break; }
                     tcgen05_after_sync();
                     const uint32_t a0 = ring + s * S::kStageBytes, b0 = a0 + b_at;
-                    const uint64_t da = umma_desc(a0, 16, 1024), db = umma_desc(b0, b_lead, 1024);
-                    const uint64_t dal = umma_desc(a0 + S::kBytesA, 16, 1024), dbl = umma_desc(b0 + S::kBytesB, b_lead, 1024);
+                    const uint64_t da = umma_desc(a0, a_lead, 128), db = umma_desc(b0, b_lead, b_step);
+                    const uint64_t dal = umma_desc(a0 + S::kBytesA, a_lead, 128), dbl = umma_desc(b0 + S::kBytesB, b_lead, b_step);
 #pragma unroll
                     for (uint32_t q = 0; q < 4; ++q) {
                         const bool add = in_chunk > 0 || q > 0;
-                        const uint64_t qa = (32 * q) >> 4, qb = (uint64_t)((b_k16 * q) >> 4);
+                        const uint64_t qa = (2 * a_lead * q) >> 4, qb = (b_k16 * q) >> 4;
                         umma_f16<CG>(d, da + qa, db + qb, idesc, add);
                         if (SPLIT) {
                             umma_f16<CG>(d + TN, da + qa, dbl + qb, idesc, add);
@@ -801,17 +805,12 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
     } else {
         // ---- results -----------------------------------------------------------------------------
         // Every warp has 32 rows and kCols columns of a tile, taken in blocks of 32 x 32.  What a
-        // block's results are added to is read ahead into registers.  Results that are operands
-        // later are turned in shared memory: a thread has a row of the accumulator, but in global
-        // memory four lanes with 16 bytes each share a row's block.
+        // block's results are added to is read ahead into registers.
         const uint32_t quad = warp & 3, c0 = (warp >> 2) * S::kCols;
         const uint32_t block = ring + S::kStages * S::kStageBytes + warp * 2 * kMuonBlock;
         const uint32_t lane_addr = tmem + ((quad * 32u) << 16);
         constexpr uint32_t kBlocks = S::kCols / 32;
-        // where a copy's lane has its 16 bytes: row cr and every eighth one below, columns 8 cc ..
-        const uint32_t cr = lane >> 2, cc = lane & 3;
-        const uint32_t copy_to = block + muon_swizzle(cr, cc);         // + 512 for each eight rows
-        const uint32_t own = block + lane * 64, flip = (lane >> 1) & 3;   // this lane's row: piece c at own + ((c ^ flip) << 4)
+        const uint32_t own = block + lane * 64, flip = (lane >> 1) & 3;   // this lane's row in shared memory: piece c at own + ((c ^ flip) << 4)
         uint32_t acc = 0, t;
         bool ok = true;
         for (uint32_t n = 0; ok && __all_sync(~0u, take(n, t)); ++n) {
@@ -823,40 +822,30 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
             const MuonMat& mat = P.mats[task.mat];
             const bool apply = pr.kind == kMuonApply, gram = pr.kind == kMuonGram;
             const uint32_t flags = pr.flags;
-            const bool last = (flags & kMuonLast) != 0, mirror = task.mirror != 0, read_wide = (flags & kMuonReadWide) != 0;
-            const uint32_t m = mat.m, width = apply ? mat.n : m, ld = apply ? mat.ld_x : mat.ld_g;
+            const bool last = (flags & kMuonLast) != 0, mirror = task.mirror != 0;
+            const bool read_low = SPLIT || (flags & kMuonReadLow), write_low = SPLIT || (flags & kMuonWriteLow);
+            const uint32_t m = mat.m, pad = mat.pad, width = ((apply ? mat.n : m) + 63) / 64 * 64;
             const uint32_t row0 = task.i * (CG * 128u) + rank * 128u + quad * 32u;
             const uint32_t col0 = task.j * (uint32_t)TN + c0;
             const uint32_t r = row0 + lane;
             const float lin = pr.lin, mul = pr.acc, shift = pr.shift;
-            const uint64_t at = (apply ? mat.x_at : mat.g_at) + (uint64_t)(row0 + cr) * ld + col0 + 8 * cc;
-            __half* out_hi = (apply ? P.ws.xh[pr.out] : P.ws.mh[pr.out]) + at;
-            __half* out_lo = (apply ? P.ws.xl[pr.out] : P.ws.ml[pr.out]) + at;
-            const uint64_t down = 8ull * ld;
-            const int rows_left = (int)(m - row0 - cr);                // > 8 i: row 8 i of the copy is inside
-            // this warp's first block in block order; 4 KB of fp32 each (of fp16, the first half)
-            const uint64_t order_at = (apply ? mat.xm_at : mat.gm_at) +
-                                      ((uint64_t)(row0 >> 5) * (ld >> 5) + (col0 >> 5)) * 1024 + 4 * lane;
-            const float* order_in = (apply ? P.ws.xm : P.ws.mm[gram ? 0 : pr.in]) + order_at;
-            float* order_out = (apply ? P.ws.xm : P.ws.mm[pr.out]) + order_at;
+            // this lane's first piece of the warp's first block, in any buffer
+            const uint32_t tile = (apply ? mat.x_tile : mat.m_tile) + (col0 >> 6) * mat.down + (row0 >> 7);
+            const uint32_t piece = (col0 & 32) * (kMuonPiece / 8) + (r & 127) * 16;
+            const uint64_t right = (uint64_t)mat.down * kMuonTileBytes;   // to the next 64 columns
+            auto place = [&](uint32_t buffer, uint32_t b) {
+                return muon_tile(P.ws, buffer + tile) + piece + (b >> 1) * right + (b & 1) * (4 * kMuonPiece);
+            };
+            const uint32_t (*const buffers)[2] = apply ? P.ws.x : P.ws.m;
+            const uint32_t in_at = gram ? 0 : apply ? pr.right : pr.in;
             // blocks inside the matrix; 0 for a warp whose rows are all below it
-            const uint32_t blocks = row0 >= m || col0 >= width ? 0 : min(kBlocks, (width - col0 + 31) / 32);
+            const uint32_t blocks = row0 >= pad || col0 >= width ? 0 : min(kBlocks, (width - col0) / 32);
 
-            uint4 in[8];
+            uint4 in[4], low[4];
             auto fetch = [&](uint32_t b) {
                 if (gram || b >= blocks) return;
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) in[i] = __ldcg(reinterpret_cast<const uint4*>(order_in) + 256 * b + 32 * i);
-                if (read_wide) {
-#pragma unroll
-                    for (uint32_t i = 4; i < 8; ++i) in[i] = __ldcg(reinterpret_cast<const uint4*>(order_in) + 256 * b + 32 * i);
-                }
-            };
-            // a block in shared memory to rows of global memory
-            auto flush = [&](uint32_t from, __half* to) {
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i)
-                    if (rows_left > (int)(8 * i)) *reinterpret_cast<uint4*>(to + i * down) = lds16(from + 512 * i);
+                muon_get(place(buffers[in_at][0], b), in);
+                if (read_low) muon_get(place(buffers[in_at][1], b), low);
             };
             if (!gram && blocks) {
                 int go = 1;
@@ -908,46 +897,39 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                     tmem_load32(lane_addr + (acc & 1) * S::kAccCols + c0 + 32 * b, y);
                 }
                 // pairs of columns in one operation each
-                const uint64_t mul2v = pack2(mul, mul), lin2v = pack2(lin, lin);
+                const uint64_t mul2v = pack2(mul, mul);
                 if (gram) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) unpack2(mul2(pack2(y[2 * i], y[2 * i + 1]), mul2v), y[2 * i], y[2 * i + 1]);
                     if (col < row0 + 32 && row0 < col + 32) {          // the block meets the diagonal
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (r == col + i) y[i] = __fsub_rn(y[i], shift);
+                            if (r == col + i && r < m) y[i] = __fsub_rn(y[i], shift);
                     }
                 } else {
-                    auto add = [&](int i, float u, float v) {          // to columns 2 i and 2 i + 1
-                        unpack2(fma2(lin2v, pack2(u, v), mul2(pack2(y[2 * i], y[2 * i + 1]), mul2v)), y[2 * i], y[2 * i + 1]);
-                    };
-                    if (read_wide) {
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            add(2 * c, __uint_as_float(in[c].x), __uint_as_float(in[c].y));
-                            add(2 * c + 1, __uint_as_float(in[c].z), __uint_as_float(in[c].w));
-                        }
-                    } else {
+                    // y = mul * y + by * v, or y + by * v
+                    auto add = [&](const uint4 (&v)[4], float by, bool first) {
+                        const uint64_t by2 = pack2(by, by);
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             float x[8];
-                            Elem<__half>::widen(in[c], x);
+                            Elem<__half>::widen(v[c], x);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) add(4 * c + i, x[2 * i], x[2 * i + 1]);
+                            for (int i = 0; i < 4; ++i) {
+                                float &u = y[8 * c + 2 * i], &w = y[8 * c + 2 * i + 1];
+                                uint64_t before = pack2(u, w);
+                                if (first) before = mul2(before, mul2v);
+                                unpack2(fma2(by2, pack2(x[2 * i], x[2 * i + 1]), before), u, w);
+                            }
                         }
-                    }
-                    if (pr.in2 != 255) {                               // fp32 always
-                        const float* second = P.ws.mm[pr.in2] + order_at;
-                        const uint64_t lin2b = pack2(pr.lin2, pr.lin2);
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) in[c] = __ldcg(reinterpret_cast<const uint4*>(second) + 256 * b + 32 * c);
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            unpack2(fma2(lin2b, pack2(__uint_as_float(in[c].x), __uint_as_float(in[c].y)), pack2(y[4 * c], y[4 * c + 1])),
-                                    y[4 * c], y[4 * c + 1]);
-                            unpack2(fma2(lin2b, pack2(__uint_as_float(in[c].z), __uint_as_float(in[c].w)), pack2(y[4 * c + 2], y[4 * c + 3])),
-                                    y[4 * c + 2], y[4 * c + 3]);
-                        }
+                    };
+                    add(in, lin, true);
+                    if (read_low) add(low, lin, false);
+                    if (pr.in2 != 255) {
+                        muon_get(place(P.ws.m[pr.in2][0], b), in);
+                        if (SPLIT) muon_get(place(P.ws.m[pr.in2][1], b), low);
+                        add(in, pr.lin2, false);
+                        if (SPLIT) add(low, pr.lin2, false);
                     }
                     fetch(b + 1);
                 }
@@ -956,58 +938,44 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 const uint32_t col = col0 + 32 * b;
                 float y[32];
                 result(b, y);
-                uint32_t hi[16];
+                // the transposed block: row c of it has the 32 lanes' entries of column c
+                auto turn = [&](const uint4 (&v)[4], uint32_t buffer) {
+                    __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) hi[i] = Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
+                    for (uint32_t c = 0; c < 4; ++c) {
+                        const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
 #pragma unroll
-                for (uint32_t c = 0; c < 4; ++c)
-                    sts16(own + ((c ^ flip) << 4), make_uint4(hi[4 * c], hi[4 * c + 1], hi[4 * c + 2], hi[4 * c + 3]));
-                uint4* order = reinterpret_cast<uint4*>(order_out) + 256 * b;
-                if (flags & kMuonWriteWide) {
-#pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) __stcg(order + 32 * i, Elem<float>::narrow(y + 4 * i));
-                } else if (flags & kMuonWriteNarrow) {
-#pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i)
-                        __stcg(order + 32 * i, make_uint4(hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]));
-                }
-                if (SPLIT) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[i]));
-                        unpack2(sub2(pack2(y[2 * i], y[2 * i + 1]), pack2(f.x, f.y)), y[2 * i], y[2 * i + 1]);
-                    }
-#pragma unroll
-                    for (uint32_t c = 0; c < 4; ++c)
-                        sts16(own + kMuonBlock + ((c ^ flip) << 4), Elem<__half>::narrow(y + 8 * c));
-                }
-                __syncwarp();
-                flush(copy_to, out_hi + 32 * b);
-                if (SPLIT) flush(copy_to + kMuonBlock, out_lo + 32 * b);
-                if (mirror) {
-                    // the transposed block: row c of it has the 32 lanes' entries of column c
-                    auto turn = [&](const uint32_t* w, __half* base) {
-                        __syncwarp();
-#pragma unroll
-                        for (uint32_t i = 0; i < 32; ++i)
+                        for (uint32_t i = 0; i < 8; ++i)
                             asm volatile("st.shared.b16 [%0], %1;"
-                                         ::"r"(block + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + 2 * (lane & 7)),
+                                         ::"r"(block + (8 * c + i) * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + 2 * (lane & 7)),
                                          "h"((uint16_t)(w[i >> 1] >> (16 * (i & 1)))) : "memory");
-                        __syncwarp();
-                        __half* to = base + mat.g_at + (uint64_t)(col + cr) * ld + row0 + 8 * cc;
-#pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i)
-                            if (col + cr + 8 * i < m) *reinterpret_cast<uint4*>(to + i * down) = lds16(copy_to + 512 * i);
-                    };
-                    turn(hi, P.ws.mh[pr.out]);
-                    if (SPLIT) {
-                        uint32_t lo[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) lo[i] = Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
-                        turn(lo, P.ws.ml[pr.out]);
                     }
+                    __syncwarp();
+                    uint4 t[4];
+#pragma unroll
+                    for (uint32_t c = 0; c < 4; ++c) t[c] = lds16(own + ((c ^ flip) << 4));
+                    if (col + lane < pad)
+                        muon_put(muon_tile(P.ws, buffer + mat.m_tile + (row0 >> 6) * mat.down + (col >> 7)) +
+                                     (row0 & 32) * (kMuonPiece / 8) + ((col & 127) + lane) * 16, t);
+                };
+                uint4 v[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] = Elem<__half>::narrow(y + 8 * c);
+                if (r < pad) muon_put(place(buffers[pr.out][0], b), v);
+                if (mirror) turn(v, P.ws.m[pr.out][0]);
+                if (write_low) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float f[8];
+                        Elem<__half>::widen(v[c], f);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            unpack2(sub2(pack2(y[8 * c + 2 * i], y[8 * c + 2 * i + 1]), pack2(f[2 * i], f[2 * i + 1])), f[2 * i], f[2 * i + 1]);
+                        v[c] = Elem<__half>::narrow(f);
+                    }
+                    if (r < pad) muon_put(place(buffers[pr.out][1], b), v);
+                    if (mirror) turn(v, P.ws.m[pr.out][1]);
                 }
-                __syncwarp();                                      // the buffer is free again
             };
             auto out_block = [&](uint32_t b) {
                 const uint32_t col = col0 + 32 * b;
