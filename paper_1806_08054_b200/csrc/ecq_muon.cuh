@@ -426,7 +426,7 @@ struct MuonShape {
     static constexpr uint32_t kStageBytes = kHalves * (kBytesA + kBytesB);
     static constexpr uint32_t kEpiWarps = TN >= 128 ? 8 : 4;
     static constexpr uint32_t kCols = TN / (kEpiWarps / 4);           // columns of an epilogue warp
-    static constexpr uint32_t kThreads = (kEpiWarps + 3) * 32;        // + loads, products, signals
+    static constexpr uint32_t kThreads = (kEpiWarps + 4) * 32;        // + two for loads, products, signals
     static constexpr uint32_t kEpiBytes = kEpiWarps * 2 * kMuonBlock;
     static constexpr uint32_t kStagesFit = (230u * 1024u - 2048u - kEpiBytes) / kStageBytes;
     static constexpr uint32_t kStages = kStagesFit < 6 ? kStagesFit : 6;
@@ -434,7 +434,7 @@ struct MuonShape {
     static constexpr uint32_t kAccCols = SPLIT ? 2 * TN : TN;         // hi hi, and the two small products
     static constexpr uint32_t kTmemCols = 2 * kAccCols;
     // counts per tile on MuonIterate::done, arrivals on a queue slot
-    static constexpr uint32_t kParts = CG, kReaders = CG * (kEpiWarps + 2) + 1;
+    static constexpr uint32_t kParts = CG, kReaders = CG * (kEpiWarps + 3) + 1;
 };
 
 // Waits that give up: the limit is per wait, and one that ran out ends all others soon.
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
     const uint32_t limit = P.wait_limit;
 
     if (tid == 0) {
-        for (uint32_t s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        for (uint32_t s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 2); mbar_init(empty + 8 * s, 1); }
         for (uint32_t b = 0; b < 2; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, CG * S::kEpiWarps); }
         for (uint32_t q = 0; q < kMuonQueue; ++q) { mbar_init(q_full + 8 * q, 1); mbar_init(q_empty + 8 * q, S::kReaders); }
         mbar_init(stored, S::kEpiWarps);
@@ -664,17 +664,22 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
         return true;
     };
 
-    if (warp == S::kEpiWarps) {
+    if (warp == S::kEpiWarps || warp == S::kEpiWarps + 3) {
         // ---- loads -------------------------------------------------------------------------------
+        // One warp for the left operands, one for the right: a thread issues a TMA load in about 200
+        // clocks, and 32 KB in two boxes by one take 756 clocks, by two 580 (in three 789 and 616).
+        // Each load thread of each CTA has part in every stage: one that had none could fall two
+        // rounds of the ring behind, where the barriers' parities are the same again.
         if (elect_one()) {
+            const bool first = warp == S::kEpiWarps, giver = first && rank == 0;
             uint32_t it = 0, t = 0;
             bool ok = true;
             const uint32_t total = P.n_tasks;
             // a tile is claimed when the loads of the one before it are issued: one that waits for
             // its operands then holds up no tile that another CTA could have had
-            unsigned long long claim = rank == 0 ? atomicAdd(P.next, 1ull) : 0;
+            unsigned long long claim = giver ? atomicAdd(P.next, 1ull) : 0;
             for (uint32_t n = 0; ok; ++n) {
-                if (rank == 0) {
+                if (giver) {
                     t = (uint32_t)min(claim, (unsigned long long)total);
                     if (!give(n, t)) break;
                 } else if (!take(n, t)) {
@@ -690,38 +695,43 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 const uint32_t row = task.i * (CG * 128u) + rank * 128u;
                 const uint32_t col = task.j * (uint32_t)TN + rank * (TN / CG);
                 const bool along_n = kind == kMuonApply;
-                // a tile on the diagonal of M M^T has one operand on both sides
-                const bool once = S::kBoxesB == 2 && !along_n && pr.left == pr.right && task.i == task.j;
-                uint32_t left[2], right[2];                            // tiles
+                uint32_t from[2];                                      // tiles
 #pragma unroll
                 for (uint32_t h = 0; h < S::kHalves; ++h) {
-                    left[h] = (kind == kMuonGram ? P.ws.x[pr.left][h] + mat.x_tile : P.ws.m[pr.left][h] + mat.m_tile) + row / 128;
-                    right[h] = (kind == kMuonSym ? P.ws.m[pr.right][h] + mat.m_tile : P.ws.x[pr.right][h] + mat.x_tile) +
-                               (along_n ? col / 64 * down : col / 128);
+                    if (first)
+                        from[h] = (kind == kMuonGram ? P.ws.x[pr.left][h] + mat.x_tile : P.ws.m[pr.left][h] + mat.m_tile) + row / 128;
+                    else
+                        from[h] = (kind == kMuonSym ? P.ws.m[pr.right][h] + mat.m_tile : P.ws.x[pr.right][h] + mat.x_tile) +
+                                  (along_n ? col / 64 * down : col / 128);
                 }
                 if (!muon_wait_done(P.done + task.mat, (unsigned long long)S::kParts * task.need, limit, &stop, 0)) break;
                 for (uint32_t k = 0; k < kb; ++k, ++it) {
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
                     if (!muon_wait(empty + 8 * s, ph ^ 1, limit, &stop)) { ok = false; break; }
-                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * (once ? S::kHalves * S::kBytesA : S::kStageBytes));
                     const uint32_t bar = CG == 1 ? full + 8 * s : leader_addr(full + 8 * s);
                     const uint32_t da = ring + s * S::kStageBytes, db = da + S::kHalves * S::kBytesA;
+                    if (first) {
+                        if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * S::kHalves * S::kBytesA);
 #pragma unroll
-                    for (uint32_t h = 0; h < S::kHalves; ++h) {
-                        muon_load<CG>(da + h * S::kBytesA, &P.rows128, 0, 8 * (left[h] + k * down), bar);
-                        if (once) continue;
-                        if (along_n) {                                 // 64 columns a box, their rows along K
+                        for (uint32_t h = 0; h < S::kHalves; ++h)
+                            muon_load<CG>(da + h * S::kBytesA, &P.rows128, 0, 8 * (from[h] + k * down), bar);
+                        if (giver && k + 1 == kb) claim = atomicAdd(P.next, 1ull);
+                    } else {
+                        if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * S::kHalves * S::kBytesB);
 #pragma unroll
-                            for (uint32_t b = 0; b < S::kBoxesB; ++b)
-                                muon_load<CG>(db + h * S::kBytesB + b * kMuonBox, &P.rows64, (k & 1) * 8,
-                                              8 * (right[h] + b * down + k / 2), bar);
-                        } else if (S::kBoxesB == 2) {
-                            muon_load<CG>(db + h * S::kBytesB, &P.rows128, 0, 8 * (right[h] + k * down), bar);
-                        } else {
-                            muon_load<CG>(db + h * S::kBytesB, &P.rows64, (col & 64) / 8, 8 * (right[h] + k * down), bar);
+                        for (uint32_t h = 0; h < S::kHalves; ++h) {
+                            if (along_n) {                             // 64 columns a box, their rows along K
+#pragma unroll
+                                for (uint32_t b = 0; b < S::kBoxesB; ++b)
+                                    muon_load<CG>(db + h * S::kBytesB + b * kMuonBox, &P.rows64, (k & 1) * 8,
+                                                  8 * (from[h] + b * down + k / 2), bar);
+                            } else if (S::kBoxesB == 2) {
+                                muon_load<CG>(db + h * S::kBytesB, &P.rows128, 0, 8 * (from[h] + k * down), bar);
+                            } else {
+                                muon_load<CG>(db + h * S::kBytesB, &P.rows64, (col & 64) / 8, 8 * (from[h] + k * down), bar);
+                            }
                         }
                     }
-                    if (rank == 0 && k + 1 == kb) claim = atomicAdd(P.next, 1ull);
                 }
             }
             // nothing of this CTA's is in flight when it leaves: every stage's last load was consumed
@@ -749,8 +759,6 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 // fp32 accumulators, fp16 operands
                 const uint32_t idesc = (1u << 4) | ((uint32_t)(TN / 8) << 17) | ((uint32_t)(CG * 128 / 16) << 24) |
                                        (along_n ? 1u << 16 : 0u);
-                const bool once = S::kBoxesB == 2 && !along_n && pr.left == pr.right && task.i == task.j;
-                const uint32_t b_at = once ? 0 : S::kHalves * S::kBytesA;
                 // bytes from a unit to the next along K and along M or N, and from 16 along K to the next
                 constexpr uint32_t a_lead = kMuonPiece, b_rows = S::kBoxesB * 1024;
                 const uint32_t b_lead = along_n ? 128 : b_rows, b_step = along_n ? 1024 : 128;
@@ -764,7 +772,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
                     if (!muon_wait(full + 8 * s, ph, limit, &stop)) { ok = false; break; }
                     tcgen05_after_sync();
-                    const uint32_t a0 = ring + s * S::kStageBytes, b0 = a0 + b_at;
+                    const uint32_t a0 = ring + s * S::kStageBytes, b0 = a0 + S::kHalves * S::kBytesA;
                     const uint64_t da = umma_desc(a0, a_lead, 128), db = umma_desc(b0, b_lead, b_step);
                     const uint64_t dal = umma_desc(a0 + S::kBytesA, a_lead, 128), dbl = umma_desc(b0 + S::kBytesB, b_lead, b_step);
 #pragma unroll
