@@ -131,8 +131,15 @@ def strerror(status: int) -> str:
     return lib().ecq_strerror(status).decode()
 
 
+# The current stream's address without building a Stream object (about 2 us a call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream) -> int:
     if stream is None:
+        if _raw_stream is not None and _device is not None:
+            return _raw_stream(_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
@@ -427,18 +434,20 @@ def _rows(t: torch.Tensor, name: str):
     """(address, dtype, rows, columns, row stride) of a [rows, columns] CUDA tensor."""
     if not t.is_cuda:
         raise ValueError("%s must be a CUDA tensor (there is no CPU path)" % name)
-    if t.dtype not in _DTYPES or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    dtype, shape, stride = _DTYPES.get(t.dtype), t.shape, t.stride()
+    if dtype is None or len(shape) != 2 or (shape[1] > 1 and stride[1] != 1):
         raise ValueError("%s must be float32, bfloat16 or float16 of two dimensions, the last one contiguous" % name)
-    return t.data_ptr(), _DTYPES[t.dtype], t.shape[0], t.shape[1], max(t.stride(0), t.shape[1]) if t.shape[0] < 2 else t.stride(0)
+    rows, cols = shape
+    return t.data_ptr(), dtype, rows, cols, stride[0] if rows > 1 else max(stride[0], cols)
 
 
 def _vec(t, dtype, n: int, name: str):
     if t is None:
         return None
-    p = _dev(t, dtype, name)
-    if t.numel() != n:
-        raise ValueError("%s must have %d entries" % (name, n))
-    return p
+    if t.dtype is dtype and t.is_cuda and t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
+    _dev(t, dtype, name)
+    raise ValueError("%s must have %d entries" % (name, n))
 
 
 def ecq_token_logprob(logits: torch.Tensor, targets=None, logprob=None, entropy=None, lse=None, top_logprob=None,
@@ -447,7 +456,7 @@ def ecq_token_logprob(logits: torch.Tensor, targets=None, logprob=None, entropy=
     alternatives ([rows, top] tensors), each where its output is given (see ecq.h)."""
     p, dtype, rows, vocab, stride = _rows(logits, "logits")
     top = 0 if top_index is None else (top_index.numel() // rows if rows else 0)
-    rc = lib().ecq_token_logprob(
+    rc = (_lib or lib()).ecq_token_logprob(
         p, dtype, rows, vocab, stride, _vec(targets, torch.int64, rows, "targets"), 1.0 / temperature, top,
         _vec(logprob, torch.float32, rows, "logprob"), _vec(entropy, torch.float32, rows, "entropy"),
         _vec(lse, torch.float32, rows, "lse"), _vec(top_logprob, torch.float32, rows * top, "top_logprob"),
@@ -463,7 +472,7 @@ def ecq_token_logprob_grad(logits: torch.Tensor, targets, lse: torch.Tensor, ent
     q, d_dtype, d_rows, d_vocab, d_stride = _rows(d_logits, "d_logits")
     if (d_dtype, d_rows, d_vocab) != (dtype, rows, vocab):
         raise ValueError("d_logits must have the shape and type of logits")
-    rc = lib().ecq_token_logprob_grad(
+    rc = (_lib or lib()).ecq_token_logprob_grad(
         p, dtype, rows, vocab, stride, _vec(targets, torch.int64, rows, "targets"), 1.0 / temperature,
         _vec(lse, torch.float32, rows, "lse"), _vec(entropy, torch.float32, rows, "entropy"),
         _vec(d_logprob, torch.float32, rows, "d_logprob"), _vec(d_entropy, torch.float32, rows, "d_entropy"),
@@ -540,17 +549,19 @@ def ecq_muon_bind(plan: int, workspace: torch.Tensor, stream=None) -> None:
 
 
 def _flat(plan: int, t: torch.Tensor, name: str, dtype=None) -> int:
-    if t.dtype not in _DTYPES:
+    have = t.dtype
+    if have in _DTYPES and (dtype is None or have is dtype) and t.is_cuda and t.is_contiguous() and \
+            t.numel() >= _muon_entries[plan]:
+        return t.data_ptr()
+    if have not in _DTYPES:
         raise ValueError("%s must be float32, bfloat16 or float16" % name)
-    p = _dev(t, dtype or t.dtype, name)
-    if t.numel() < _muon_entries[plan]:
-        raise ValueError("%s must have at least %d entries" % (name, _muon_entries[plan]))
-    return p
+    _dev(t, dtype or have, name)
+    raise ValueError("%s must have at least %d entries" % (name, _muon_entries[plan]))
 
 
 def ecq_muon_orthogonalize(plan: int, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
     """Orthogonalise the plan's matrices of the flat vector ``src`` into ``dst``."""
-    rc = lib().ecq_muon_orthogonalize(plan, _flat(plan, src, "src"), _DTYPES[src.dtype], _flat(plan, dst, "dst"),
+    rc = (_lib or lib()).ecq_muon_orthogonalize(plan, _flat(plan, src, "src"), _DTYPES[src.dtype], _flat(plan, dst, "dst"),
                                       _DTYPES[dst.dtype], _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_muon_orthogonalize")
@@ -561,7 +572,7 @@ def ecq_muon_step(plan: int, grad: torch.Tensor, momentum: torch.Tensor, params=
     """One optimiser step of the plan's matrices: ``momentum`` is updated in place, ``params`` are
     stepped where they are given, and the update itself is written where ``update`` is."""
     f32 = torch.float32
-    rc = lib().ecq_muon_step(
+    rc = (_lib or lib()).ecq_muon_step(
         plan, _flat(plan, grad, "grad", f32), _flat(plan, momentum, "momentum", f32), mu, int(nesterov), lr, decay,
         None if params is None else _flat(plan, params, "params", f32),
         None if update is None else _flat(plan, update, "update"), 0 if update is None else _DTYPES[update.dtype],

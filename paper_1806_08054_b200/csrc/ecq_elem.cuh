@@ -13,6 +13,7 @@ template <typename T> struct Elem;
 
 template <> struct Elem<float> {
     static constexpr int kPer16 = 4;
+    static constexpr uint32_t kMinusInf = 0xFF800000u;               // a 32-bit word of them
     static __device__ __forceinline__ void widen(const uint4& v, float* x) {
         x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y);
         x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
@@ -26,6 +27,7 @@ template <> struct Elem<float> {
 
 template <> struct Elem<__nv_bfloat16> {
     static constexpr int kPer16 = 8;
+    static constexpr uint32_t kMinusInf = 0xFF80FF80u;
     static __device__ __forceinline__ void widen(const uint4& v, float* x) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -47,6 +49,7 @@ template <> struct Elem<__nv_bfloat16> {
 
 template <> struct Elem<__half> {
     static constexpr int kPer16 = 8;
+    static constexpr uint32_t kMinusInf = 0xFC00FC00u;
     static __device__ __forceinline__ void widen(const uint4& v, float* x) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll

@@ -11,25 +11,37 @@ using namespace ecq;
 
 namespace {
 
-template <typename T, bool ENT>
+template <typename T, bool ENT, int HOLD, int NT>
 int launch_forward(const TokenForward& P, uint64_t rows, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((uint32_t)(rows * P.cluster));
-    cfg.blockDim = dim3(kTokThreads);
+    cfg.gridDim = dim3((uint32_t)(rows << P.cluster_log2));
+    cfg.blockDim = dim3(NT);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = P.cluster;
+    at[0].val.clusterDim.x = 1u << P.cluster_log2;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = P.cluster > 1 ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, token_logprob_kernel<T, ENT>, P) != cudaSuccess) {
+    cfg.numAttrs = P.cluster_log2 ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, token_logprob_kernel<T, ENT, HOLD, NT>, P) != cudaSuccess) {
         cudaGetLastError();
         return ECQ_ERR_CUDA;
     }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return ECQ_OK;
+}
+
+template <typename T>
+int launch_forward(const TokenForward& P, uint64_t rows, cudaStream_t st) {
+    // vectors of a CTA's part of a row; one more where the row does not start on a vector
+    const uint32_t per_cta = (P.vocab / (16 / (uint32_t)sizeof(T)) >> P.cluster_log2) + 1;
+    if (!P.cluster_log2)
+        return P.entropy ? launch_forward<T, true, 0, kTokStream>(P, rows, st) : launch_forward<T, false, 0, kTokStream>(P, rows, st);
+    if (per_cta <= (uint32_t)(kTokHold * kTokThreads))
+        return P.entropy ? launch_forward<T, true, kTokHold, kTokThreads>(P, rows, st)
+                         : launch_forward<T, false, kTokHold, kTokThreads>(P, rows, st);
+    return P.entropy ? launch_forward<T, true, 0, kTokThreads>(P, rows, st) : launch_forward<T, false, 0, kTokThreads>(P, rows, st);
 }
 
 template <typename T>
@@ -73,18 +85,17 @@ int ecq_token_logprob(const void* logits, int dtype, uint64_t rows, uint32_t voc
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return ECQ_ERR_CUDA;
     TokenForward P = {logits, row_stride, targets, logprob, entropy, lse, top_logprob, top_index,
-                      vocab, top, 1, inv_temperature};
+                      vocab, top, 0, inv_temperature};
     // A row is split over a cluster while there are fewer CTAs than SMs and each keeps a vector per thread.
     const uint64_t row_bytes = (uint64_t)vocab * dtype_bytes(dtype);
-    while (P.cluster < (uint32_t)kTokMaxCluster && rows * P.cluster < (uint64_t)sms &&
-           row_bytes >= (uint64_t)P.cluster * 2 * kTokThreads * 16)
-        P.cluster *= 2;
+    while ((1u << P.cluster_log2) < (uint32_t)kTokMaxCluster && rows << P.cluster_log2 < (uint64_t)sms &&
+           row_bytes >= (uint64_t)(2u << P.cluster_log2) * kTokThreads * 16)
+        ++P.cluster_log2;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     switch (dtype) {
-        case ECQ_F32: return entropy ? launch_forward<float, true>(P, rows, st) : launch_forward<float, false>(P, rows, st);
-        case ECQ_BF16:
-            return entropy ? launch_forward<__nv_bfloat16, true>(P, rows, st) : launch_forward<__nv_bfloat16, false>(P, rows, st);
-        default: return entropy ? launch_forward<__half, true>(P, rows, st) : launch_forward<__half, false>(P, rows, st);
+        case ECQ_F32: return launch_forward<float>(P, rows, st);
+        case ECQ_BF16: return launch_forward<__nv_bfloat16>(P, rows, st);
+        default: return launch_forward<__half>(P, rows, st);
     }
 }
 

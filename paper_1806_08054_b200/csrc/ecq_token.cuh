@@ -32,9 +32,12 @@ constexpr float kLn2 = 0.6931471805599453f;
 // of the row) are read again, out of L2, and the few that reach the bound are ranked by counting.
 // Entries are ordered by value, equal ones by index (the lower first); a 64-bit key holds both.
 
-constexpr int kTokThreads = 256;
+constexpr int kTokThreads = 256;         // of a CTA that has a part of a row
+constexpr int kTokStream = 128;          // of a CTA that has rows to itself, eight of them an SM: while some
+                                         // rank their best entries the others keep the memory busy
 constexpr int kTokGroups = 128;
 constexpr int kTokUnroll = 4;            // 16-byte vectors in flight per thread
+constexpr int kTokHold = 8;              // vectors per thread that a CTA keeps in registers
 constexpr int kTokMaxTop = 32;
 constexpr int kTokMaxCluster = 8;
 constexpr int kTokCandidates = 1024;
@@ -50,7 +53,7 @@ struct TokenForward {
     int32_t* top_index;
     uint32_t vocab;
     uint32_t top;
-    uint32_t cluster;                    // CTAs per row
+    uint32_t cluster_log2;               // CTAs per row, a power of two
     float tau;
 };
 
@@ -132,12 +135,13 @@ struct TokenSpan {
 
 struct TokenShared {
     uint64_t cand[kTokCandidates];
-    uint64_t lists[kTokMaxCluster][kTokMaxTop];      // rank 0: every CTA's best entries
+    uint64_t lists[kTokMaxCluster * kTokMaxTop];     // rank 0: every CTA's best entries, `top` of each
+    uint64_t counts[kTokMaxCluster];                 // and how many they are
     TokenSums sums[kTokMaxCluster];                  // rank 0: every CTA's sums
-    TokenSums warp_sums[kTokThreads / 32];
-    float group_max[kTokGroups];
-    uint32_t flagged[kTokGroups];
-    uint32_t n_flagged, n_cand, warp_count[kTokThreads / 32];
+    TokenSums warp_sums[8];
+    __align__(16) float group_max[kTokGroups];
+    uint32_t flagged[kTokMaxTop + kTokGroups];
+    uint32_t n_tied, n_cand, warp_count[8];
     uint64_t best;
     float bound;
 };
@@ -151,7 +155,7 @@ __device__ __forceinline__ void token_append(TokenShared& sm, uint64_t key) {
 // entries, or one whose few open entries stand before a mask of the lowest finite value.  Entries
 // above the bound are collected first; if they fit, entries equal to it are taken in index order
 // until there are enough.  Otherwise (all of them in few groups) the best are taken one by one.
-template <typename T>
+template <typename T, int NT>
 __device__ __noinline__ void token_collect_slow(TokenShared& sm, const TokenSpan<T>& sp, uint32_t top) {
     constexpr uint32_t E = Elem<T>::kPer16;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -160,7 +164,7 @@ __device__ __noinline__ void token_collect_slow(TokenShared& sm, const TokenSpan
     __syncthreads();
     if (tid == 0) sm.n_cand = 0;
     __syncthreads();
-    for (uint32_t v = sp.v0 + tid; v < sp.v1; v += kTokThreads) {
+    for (uint32_t v = sp.v0 + tid; v < sp.v1; v += NT) {
         Elem<T>::widen(sp.vec(v), x);
         for (uint32_t i = 0; i < E; ++i)
             if (x[i] > bound) token_append(sm, token_key(x[i], sp.vec_index(v) + i));
@@ -176,7 +180,7 @@ __device__ __noinline__ void token_collect_slow(TokenShared& sm, const TokenSpan
         // ties in index order: head, body in chunks of one vector per thread, tail
         for (int part = 0; part < 3 && n < top; ++part) {
             const uint32_t begin = part == 1 ? sp.v0 : 0, end = part == 1 ? sp.v1 : 1;
-            for (uint32_t base = begin; base < end && n < top; base += kTokThreads) {
+            for (uint32_t base = begin; base < end && n < top; base += NT) {
                 uint32_t mask = 0, index0 = 0;
                 if (part == 1) {
                     if (base + tid < end) {
@@ -198,7 +202,7 @@ __device__ __noinline__ void token_collect_slow(TokenShared& sm, const TokenSpan
                 if (lane == 31) sm.warp_count[warp] = before;
                 __syncthreads();
                 uint32_t at = n + before - mine, all = 0;
-                for (uint32_t w = 0; w < kTokThreads / 32; ++w) {
+                for (uint32_t w = 0; w < NT / 32; ++w) {
                     if (w < warp) at += sm.warp_count[w];
                     all += sm.warp_count[w];
                 }
@@ -219,7 +223,7 @@ __device__ __noinline__ void token_collect_slow(TokenShared& sm, const TokenSpan
     uint32_t found = 0;
     for (; found < top; ++found) {
         uint64_t best = 0;
-        for (uint32_t v = sp.v0 + tid; v < sp.v1; v += kTokThreads) {
+        for (uint32_t v = sp.v0 + tid; v < sp.v1; v += NT) {
             Elem<T>::widen(sp.vec(v), x);
             for (uint32_t i = 0; i < E; ++i) {
                 const uint64_t key = x[i] >= -FLT_MAX ? token_key(x[i], sp.vec_index(v) + i) : 0;
@@ -247,42 +251,89 @@ __device__ __noinline__ void token_collect_slow(TokenShared& sm, const TokenSpan
     __syncthreads();
 }
 
-// The CTA's best `top` entries into sm.cand (any order, sm.n_cand of them, more than needed).
-template <typename T>
-__device__ __forceinline__ void token_collect(TokenShared& sm, const TokenSpan<T>& sp, float m, uint32_t top) {
+// The CTA's best `top` entries into sm.cand (any order, sm.n_cand of them, more than needed).  With
+// HOLD the threads still have the CTA's vectors.
+template <typename T, int HOLD, int NT>
+__device__ __forceinline__ void token_collect(TokenShared& sm, const TokenSpan<T>& sp, float m, uint32_t top,
+                                              const uint4 (&raw)[HOLD ? HOLD : 1]) {
     constexpr uint32_t E = Elem<T>::kPer16;
-    constexpr uint32_t L = kTokThreads / kTokGroups;                  // threads per group
+    constexpr uint32_t L = NT / kTokGroups;                  // threads per group
     const uint32_t tid = threadIdx.x;
 #pragma unroll
     for (uint32_t o = 1; o < L; o <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
     if (tid % L == 0) sm.group_max[tid / L] = m;
-    if (tid == 0) { sm.n_cand = 0; sm.n_flagged = 0; }
+    if (tid == 0) { sm.n_cand = 0; sm.n_tied = 0; }
     __syncthreads();
-    if (tid < (uint32_t)kTokGroups) {
-        const float mine = sm.group_max[tid];
+    {                                                                 // L = 2 threads count for a group
+        const uint32_t g0 = tid / L;
+        const float mine = sm.group_max[g0];
         uint32_t rank = 0;
-        for (uint32_t g = 0; g < (uint32_t)kTokGroups; ++g) {
-            const float o = sm.group_max[g];
-            rank += (o > mine || (o == mine && g < tid)) ? 1u : 0u;
+#pragma unroll 8
+        for (uint32_t g = (tid % L) * 4; g < (uint32_t)kTokGroups; g += 4 * L) {
+            const float4 o = *reinterpret_cast<const float4*>(&sm.group_max[g]);
+            rank += (o.x > mine || (o.x == mine && g < g0)) ? 1u : 0u;
+            rank += (o.y > mine || (o.y == mine && g + 1 < g0)) ? 1u : 0u;
+            rank += (o.z > mine || (o.z == mine && g + 2 < g0)) ? 1u : 0u;
+            rank += (o.w > mine || (o.w == mine && g + 3 < g0)) ? 1u : 0u;
         }
-        if (rank == top - 1) sm.bound = mine;
-    }
-    __syncthreads();
-    const float bound = sm.bound;
-    if (tid < (uint32_t)kTokGroups && sm.group_max[tid] >= bound) sm.flagged[atomicAdd(&sm.n_flagged, 1u)] = tid;
-    __syncthreads();
-    const uint32_t steps = (sp.v1 - sp.v0 + kTokThreads - 1) / kTokThreads;
-    const uint32_t per_group = steps * L;
-    const uint32_t work = sm.n_flagged * per_group;
-    for (uint32_t i = tid; i < work; i += kTokThreads) {
-        const uint32_t f = i / per_group, r = i - f * per_group;
-        const uint32_t v = sp.v0 + (r / L) * kTokThreads + sm.flagged[f] * L + r % L;
-        if (v >= sp.v1) continue;
-        float x[E];
-        Elem<T>::widen(sp.vec(v), x);
 #pragma unroll
-        for (uint32_t j = 0; j < E; ++j)
-            if (x[j] >= bound) token_append(sm, token_key(x[j], sp.vec_index(v) + j));
+        for (uint32_t o = 1; o < L; o <<= 1) rank += __shfl_xor_sync(~0u, rank, o);
+        if (rank == top - 1 && tid % L == 0) sm.bound = mine;
+        // with entries streaming past, the groups that may reach the bound are those ranked before it
+        if (!HOLD && rank < top && tid % L == 0) sm.flagged[rank] = g0;
+        __syncthreads();
+        if constexpr (HOLD == 0) {
+            if (rank >= top && tid % L == 0 && mine == sm.bound) sm.flagged[top + atomicAdd(&sm.n_tied, 1u)] = g0;
+            __syncthreads();
+        }
+    }
+    const float bound = sm.bound;
+    if constexpr (HOLD > 0) {
+        if (m >= bound) {
+#pragma unroll
+            for (uint32_t u = 0; u < (uint32_t)HOLD; ++u) {
+                float x[E];
+                Elem<T>::widen(raw[u], x);
+                float best = x[0];
+#pragma unroll
+                for (uint32_t j = 1; j < E; ++j) best = fmaxf(best, x[j]);
+                const uint32_t v = sp.v0 + tid + u * NT;
+                if (best >= bound && v < sp.v1) {
+#pragma unroll
+                    for (uint32_t j = 0; j < E; ++j)
+                        if (x[j] >= bound) token_append(sm, token_key(x[j], sp.vec_index(v) + j));
+                }
+            }
+        }
+    } else {
+        // Groups whose maximum equals the bound but that rank behind it count, too: an entry of
+        // theirs that equals it may come before others by index.
+        const uint32_t steps = (sp.v1 - sp.v0 + NT - 1) / NT, per_group = steps * L;
+        const uint32_t work = (top + sm.n_tied) * per_group;
+        for (uint32_t i0 = tid; i0 < work; i0 += NT * kTokUnroll) {
+            uint4 some[kTokUnroll];
+            uint32_t at[kTokUnroll];
+#pragma unroll
+            for (int u = 0; u < kTokUnroll; ++u) {
+                constexpr uint32_t none = Elem<T>::kMinusInf;
+                const uint32_t i = i0 + u * NT, f = i / per_group, r = i - f * per_group;
+                at[u] = i < work ? sp.v0 + (r / L) * NT + sm.flagged[f] * L + r % L : sp.v1;
+                some[u] = at[u] < sp.v1 ? sp.vec(at[u]) : make_uint4(none, none, none, none);
+            }
+#pragma unroll
+            for (int u = 0; u < kTokUnroll; ++u) {
+                float x[E];
+                Elem<T>::widen(some[u], x);
+                float best = x[0];
+#pragma unroll
+                for (uint32_t j = 1; j < E; ++j) best = fmaxf(best, x[j]);
+                if (best >= bound) {
+#pragma unroll
+                    for (uint32_t j = 0; j < E; ++j)
+                        if (x[j] >= bound) token_append(sm, token_key(x[j], sp.vec_index(at[u]) + j));
+                }
+            }
+        }
     }
     if (tid < 2 * E) {
         bool have;
@@ -290,7 +341,7 @@ __device__ __forceinline__ void token_collect(TokenShared& sm, const TokenSpan<T
         if (have) { const float y = Elem<T>::load(sp.row + j); if (y >= bound) token_append(sm, token_key(y, j)); }
     }
     __syncthreads();
-    if (sm.n_cand > (uint32_t)kTokCandidates) token_collect_slow<T>(sm, sp, top);
+    if (sm.n_cand > (uint32_t)kTokCandidates) token_collect_slow<T, NT>(sm, sp, top);
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
@@ -307,13 +358,16 @@ __device__ __forceinline__ void cluster_store(uint32_t addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
-template <typename T, bool ENT>
-__global__ void __launch_bounds__(kTokThreads, 4) token_logprob_kernel(TokenForward P) {
+// HOLD vectors a thread are read once and kept (few rows, each split over a cluster: the chain from
+// the first load to the result counts), or, with 0, the row streams past (many rows: occupancy
+// counts).
+template <typename T, bool ENT, int HOLD, int NT>
+__global__ void __launch_bounds__(NT, HOLD ? 2 : 1024 / NT) token_logprob_kernel(TokenForward P) {
     constexpr uint32_t E = Elem<T>::kPer16;
     __shared__ TokenShared sm;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t C = P.cluster, rank = blockIdx.x % C;
-    const uint64_t row = blockIdx.x / C;
+    const uint32_t C = 1u << P.cluster_log2, rank = blockIdx.x & (C - 1);
+    const uint64_t row = blockIdx.x >> P.cluster_log2;
     if (C > 1) cluster_arrive();                                      // every CTA of the row has started
 
     TokenSpan<T> sp;
@@ -322,28 +376,52 @@ __global__ void __launch_bounds__(kTokThreads, 4) token_logprob_kernel(TokenForw
     sp.vocab = P.vocab;
     sp.head = odd < P.vocab ? odd : P.vocab;
     sp.nv = (P.vocab - sp.head) / E;
-    const uint32_t per = (sp.nv + C - 1) / C;
+    const uint32_t per = (sp.nv + C - 1) >> P.cluster_log2;
     sp.v0 = rank * per < sp.nv ? rank * per : sp.nv;
     sp.v1 = sp.v0 + per < sp.nv ? sp.v0 + per : sp.nv;
     sp.first = rank == 0;
     sp.last = rank == C - 1;
 
+    // the target's logit, asked for before it is needed
+    int64_t target = -1;
+    float target_x = 0.f;
+    if (P.logprob && rank == 0 && tid == 0) {
+        target = P.targets[row];
+        if (target >= 0 && target < (int64_t)P.vocab) target_x = Elem<T>::load(sp.row + target);
+    }
     const float k = __fmul_rn(P.tau, kLog2e);
     TokenSums a = {-FLT_MAX, 0.f, 0.f};
-    uint32_t v = sp.v0 + tid;
-    for (; v + (kTokUnroll - 1) * kTokThreads < sp.v1; v += kTokUnroll * kTokThreads) {
-        uint4 raw[kTokUnroll];
+    // batches of vectors; what is missing at the end is as if masked
+    uint4 held[HOLD ? HOLD : 1];
+    auto fetch = [&](uint32_t v) {
+        constexpr uint32_t none = Elem<T>::kMinusInf;
+        return v < sp.v1 ? sp.vec(v) : make_uint4(none, none, none, none);
+    };
+    if constexpr (HOLD > 0) {
 #pragma unroll
-        for (int u = 0; u < kTokUnroll; ++u) raw[u] = sp.vec(v + u * kTokThreads);
-        float x[kTokUnroll * E];
+        for (int u = 0; u < HOLD; ++u) held[u] = fetch(sp.v0 + tid + u * NT);
 #pragma unroll
-        for (int u = 0; u < kTokUnroll; ++u) Elem<T>::widen(raw[u], x + u * E);
-        token_add<kTokUnroll * E, ENT>(a, x, k);
-    }
-    for (; v < sp.v1; v += kTokThreads) {
-        float x[E];
-        Elem<T>::widen(sp.vec(v), x);
-        token_add<E, ENT>(a, x, k);
+        for (int u = 0; u < HOLD; u += 2) {
+            float x[2 * E];
+            Elem<T>::widen(held[u], x);
+            Elem<T>::widen(held[u + 1], x + E);
+            token_add<2 * E, ENT>(a, x, k);
+        }
+    } else {
+        for (uint32_t v = sp.v0 + tid; v < sp.v1 + tid; v += kTokUnroll * NT) {
+            uint4 raw[kTokUnroll];
+            if (v - tid + kTokUnroll * NT <= sp.v1) {
+#pragma unroll
+                for (int u = 0; u < kTokUnroll; ++u) raw[u] = sp.vec(v + u * NT);
+            } else {
+#pragma unroll
+                for (int u = 0; u < kTokUnroll; ++u) raw[u] = fetch(v + u * NT);
+            }
+            float x[kTokUnroll * E];
+#pragma unroll
+            for (int u = 0; u < kTokUnroll; ++u) Elem<T>::widen(raw[u], x + u * E);
+            token_add<kTokUnroll * E, ENT>(a, x, k);
+        }
     }
     if (tid < 2 * E) {
         bool have;
@@ -356,25 +434,30 @@ __global__ void __launch_bounds__(kTokThreads, 4) token_logprob_kernel(TokenForw
     for (int o = 16; o > 0; o >>= 1)
         token_merge(a, {__shfl_xor_sync(~0u, a.m, o), __shfl_xor_sync(~0u, a.s, o), __shfl_xor_sync(~0u, a.t, o)}, k);
     if (lane == 0) sm.warp_sums[warp] = a;
-    if (P.top) token_collect<T>(sm, sp, own_max, P.top);              // its barriers order warp_sums too
+    if (P.top) token_collect<T, HOLD, NT>(sm, sp, own_max, P.top, held);              // its barriers order warp_sums too
     else __syncthreads();
     if (C > 1) cluster_wait();
 
+    if (warp == 0) {
+        a = sm.warp_sums[lane & (NT / 32 - 1)];
+#pragma unroll
+        for (int o = NT / 64; o > 0; o >>= 1)
+            token_merge(a, {__shfl_xor_sync(~0u, a.m, o), __shfl_xor_sync(~0u, a.s, o), __shfl_xor_sync(~0u, a.t, o)}, k);
+    }
     if (tid == 0) {
-        a = sm.warp_sums[0];
-        for (int w = 1; w < kTokThreads / 32; ++w) token_merge(a, sm.warp_sums[w], k);
         const uint32_t to = cluster_addr(&sm.sums[rank], 0);
         cluster_store(to, a.m); cluster_store(to + 4, a.s); cluster_store(to + 8, a.t);
     }
     if (P.top) {
         const uint32_t n = sm.n_cand;
-        for (uint32_t i = n + tid; i < P.top; i += kTokThreads)
-            cluster_store(cluster_addr(&sm.lists[rank][i], 0), (uint64_t)0);
-        for (uint32_t i = tid; i < n; i += kTokThreads) {
+        for (uint32_t i = n + tid; i < P.top; i += NT)
+            cluster_store(cluster_addr(&sm.lists[rank * P.top + i], 0), (uint64_t)0);
+        if (tid == 0) cluster_store(cluster_addr(&sm.counts[rank], 0), (uint64_t)(n < P.top ? n : P.top));
+        for (uint32_t i = tid; i < n; i += NT) {
             const uint64_t key = sm.cand[i];
             uint32_t better = 0;
             for (uint32_t j = 0; j < n; ++j) better += sm.cand[j] > key ? 1u : 0u;
-            if (better < P.top) cluster_store(cluster_addr(&sm.lists[rank][better], 0), key);
+            if (better < P.top) cluster_store(cluster_addr(&sm.lists[rank * P.top + better], 0), key);
         }
     }
     if (C > 1) {
@@ -393,35 +476,51 @@ __global__ void __launch_bounds__(kTokThreads, 4) token_logprob_kernel(TokenForw
         if (P.lse) P.lse[row] = empty ? -INFINITY : __fmaf_rn(a.m, P.tau, ln_s);
         if (ENT) P.entropy[row] = empty ? 0.f : __fsub_rn(ln_s, __fmul_rn(kLn2, __fdiv_rn(a.t, a.s)));
         if (P.logprob) {
-            const int64_t y = P.targets[row];
             float lp = 0.f;
-            if (y >= (int64_t)P.vocab) lp = NAN;
-            else if (y >= 0)
-                lp = empty ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(Elem<T>::load(sp.row + y), a.m), P.tau), ln_s);
+            if (target >= (int64_t)P.vocab) lp = NAN;
+            else if (target >= 0)
+                lp = empty ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(target_x, a.m), P.tau), ln_s);
             P.logprob[row] = lp;
         }
     }
     if (P.top) {
-        const uint64_t* all = &sm.lists[0][0];
         const bool valid = a.s > 0.f;                                 // false for NaN as well
-        const uint32_t n = C * P.top;
         if (tid < P.top && !valid) {
             P.top_logprob[row * P.top + tid] = empty ? -INFINITY : NAN;
             P.top_index[row * P.top + tid] = -1;
         }
-        if (valid && tid < n) {
-            const uint64_t key = all[(tid / P.top) * kTokMaxTop + tid % P.top];
+        if (valid && C == 1 && tid < P.top) {
+            const uint64_t key = sm.lists[tid];
+            P.top_logprob[row * P.top + tid] =
+                key ? __fsub_rn(__fmul_rn(__fsub_rn(token_key_value(key), a.m), P.tau), ln_s) : -INFINITY;
+            P.top_index[row * P.top + tid] = key ? (int32_t)token_key_index(key) : -1;
+        } else if (valid && tid < C * P.top) {
+            // every CTA's list is in order: an entry's place is the number of better ones in each
+            const uint64_t key = sm.lists[tid];
+            uint32_t lo[kTokMaxCluster];
+#pragma unroll
+            for (int c = 0; c < kTokMaxCluster; ++c) lo[c] = 0;
+#pragma unroll
+            for (uint32_t step = kTokMaxTop; step > 0; step >>= 1) {
+                if (step > P.top) continue;
+#pragma unroll
+                for (uint32_t c = 0; c < (uint32_t)kTokMaxCluster; ++c)
+                    if (c < C && lo[c] + step <= P.top && sm.lists[c * P.top + lo[c] + step - 1] > key) lo[c] += step;
+            }
             uint32_t better = 0;
-            for (uint32_t c = 0; c < C; ++c)
-                for (uint32_t j = 0; j < P.top; ++j) {
-                    const uint64_t o = sm.lists[c][j];
-                    // absent entries (key 0) are ordered by their place
-                    better += o > key || (o == key && c * P.top + j < tid) ? 1u : 0u;
-                }
-            if (better < P.top) {
-                const float lp = __fsub_rn(__fmul_rn(__fsub_rn(token_key_value(key), a.m), P.tau), ln_s);
-                P.top_logprob[row * P.top + better] = key ? lp : -INFINITY;
-                P.top_index[row * P.top + better] = key ? (int32_t)token_key_index(key) : -1;
+#pragma unroll
+            for (int c = 0; c < kTokMaxCluster; ++c) better += lo[c];
+            if (key && better < P.top) {
+                P.top_logprob[row * P.top + better] = __fsub_rn(__fmul_rn(__fsub_rn(token_key_value(key), a.m), P.tau), ln_s);
+                P.top_index[row * P.top + better] = (int32_t)token_key_index(key);
+            }
+        }
+        if (valid && C > 1 && tid < P.top) {                          // where the open entries run out
+            uint64_t open = 0;
+            for (uint32_t c = 0; c < C; ++c) open += sm.counts[c];
+            if (tid >= open) {
+                P.top_logprob[row * P.top + tid] = -INFINITY;
+                P.top_index[row * P.top + tid] = -1;
             }
         }
     }

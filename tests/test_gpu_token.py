@@ -210,7 +210,7 @@ def test_all_large_entries_with_one_thread():
     x[:, vec % 256 < 4] += 50.0
     y = torch.zeros(200, dtype=torch.int64, device="cuda")
     out = forward(x, y, 1.0, 32)
-    v, i = torch.topk(x, 32, dim=1)
+    v, i = best(x, 32)                                      # torch.topk orders equal values as it likes
     assert torch.equal(out["top_index"].long(), i)
 
 
