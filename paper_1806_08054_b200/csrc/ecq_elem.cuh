@@ -21,6 +21,9 @@ template <> struct Elem<float> {
     static __device__ __forceinline__ uint4 narrow(const float* x) {
         return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
+    static __device__ __forceinline__ float largest(const uint4& v) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
     static __device__ __forceinline__ float load(const float* p) { return *p; }
     static __device__ __forceinline__ void store(float* p, float x) { *p = x; }
 };
@@ -43,6 +46,11 @@ template <> struct Elem<__nv_bfloat16> {
     static __device__ __forceinline__ uint4 narrow(const float* x) {
         return make_uint4(pair(x[0], x[1]), pair(x[2], x[3]), pair(x[4], x[5]), pair(x[6], x[7]));
     }
+    static __device__ __forceinline__ float largest(const uint4& v) {    // of two at a time; NaNs lose
+        const __nv_bfloat162* w = reinterpret_cast<const __nv_bfloat162*>(&v);
+        const __nv_bfloat162 m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+        return fmaxf(__bfloat162float(__low2bfloat16(m)), __bfloat162float(__high2bfloat16(m)));
+    }
     static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 };
@@ -64,6 +72,11 @@ template <> struct Elem<__half> {
     }
     static __device__ __forceinline__ uint4 narrow(const float* x) {
         return make_uint4(pair(x[0], x[1]), pair(x[2], x[3]), pair(x[4], x[5]), pair(x[6], x[7]));
+    }
+    static __device__ __forceinline__ float largest(const uint4& v) {    // of two at a time; NaNs lose
+        const __half2* w = reinterpret_cast<const __half2*>(&v);
+        const __half2 m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+        return fmaxf(__half2float(__low2half(m)), __half2float(__high2half(m)));
     }
     static __device__ __forceinline__ float load(const __half* p) { return __half2float(*p); }
     static __device__ __forceinline__ void store(__half* p, float x) { *p = __float2half_rn(x); }

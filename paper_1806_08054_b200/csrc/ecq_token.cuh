@@ -77,25 +77,46 @@ __device__ __forceinline__ void token_merge(TokenSums& a, TokenSums b, float k) 
     a.t = __fadd_rn(a.t, b.t);
 }
 
-template <int N, bool ENT>
-__device__ __forceinline__ void token_add(TokenSums& a, const float* x, float k) {
-    float m = x[0];
+// One entry.
+template <bool ENT>
+__device__ __forceinline__ void token_add(TokenSums& a, float x, float k) {
+    if (x > a.m) token_rescale(a, x, k);
+    const float d = __fmul_rn(__fsub_rn(x, a.m), k), e = ex2(d);
+    a.s = __fadd_rn(a.s, e);
+    // a masked entry has d = -inf and e = 0; it adds nothing to t
+    if (ENT) a.t = __fmaf_rn(e, fmaxf(d, -1e4f), a.t);
+}
+
+// N vectors, two entries an instruction where there is one.
+template <typename T, bool ENT, int N>
+__device__ __forceinline__ void token_add(TokenSums& a, const uint4* raw, float k) {
+    constexpr int E = Elem<T>::kPer16;
+    float m = Elem<T>::largest(raw[0]);
 #pragma unroll
-    for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+    for (int u = 1; u < N; ++u) m = fmaxf(m, Elem<T>::largest(raw[u]));
     if (m > a.m) token_rescale(a, m, k);
-    float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+    const uint64_t m2 = pack2(a.m, a.m), k2 = pack2(k, k);
+    uint64_t s2 = 0, t2 = 0;                                          // two zeros
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float d = __fmul_rn(__fsub_rn(x[i], a.m), k);
-        const float e = ex2(d);
-        float& s = i & 1 ? s1 : s0;
-        float& t = i & 1 ? t1 : t0;
-        s = __fadd_rn(s, e);
-        // a masked entry has d = -inf and e = 0; it adds nothing to t
-        if (ENT) t = __fmaf_rn(e, fmaxf(d, -1e4f), t);
+    for (int u = 0; u < N; ++u) {
+        float x[E];
+        Elem<T>::widen(raw[u], x);
+#pragma unroll
+        for (int i = 0; i < E; i += 2) {
+            float d0, d1;
+            unpack2(mul2(sub2(pack2(x[i], x[i + 1]), m2), k2), d0, d1);
+            const uint64_t e2 = pack2(ex2(d0), ex2(d1));
+            s2 = add2(s2, e2);
+            if (ENT) t2 = fma2(e2, pack2(fmaxf(d0, -1e4f), fmaxf(d1, -1e4f)), t2);
+        }
     }
-    a.s = __fadd_rn(a.s, __fadd_rn(s0, s1));
-    if (ENT) a.t = __fadd_rn(a.t, __fadd_rn(t0, t1));
+    float u, v;
+    unpack2(s2, u, v);
+    a.s = __fadd_rn(a.s, __fadd_rn(u, v));
+    if (ENT) {
+        unpack2(t2, u, v);
+        a.t = __fadd_rn(a.t, __fadd_rn(u, v));
+    }
 }
 
 // Larger keys are better: value first, then the lower index.  0 is below every entry's key.
@@ -294,11 +315,8 @@ __device__ __forceinline__ void token_collect(TokenShared& sm, const TokenSpan<T
             for (uint32_t u = 0; u < (uint32_t)HOLD; ++u) {
                 float x[E];
                 Elem<T>::widen(raw[u], x);
-                float best = x[0];
-#pragma unroll
-                for (uint32_t j = 1; j < E; ++j) best = fmaxf(best, x[j]);
                 const uint32_t v = sp.v0 + tid + u * NT;
-                if (best >= bound && v < sp.v1) {
+                if (Elem<T>::largest(raw[u]) >= bound && v < sp.v1) {
 #pragma unroll
                     for (uint32_t j = 0; j < E; ++j)
                         if (x[j] >= bound) token_append(sm, token_key(x[j], sp.vec_index(v) + j));
@@ -324,10 +342,7 @@ __device__ __forceinline__ void token_collect(TokenShared& sm, const TokenSpan<T
             for (int u = 0; u < kTokUnroll; ++u) {
                 float x[E];
                 Elem<T>::widen(some[u], x);
-                float best = x[0];
-#pragma unroll
-                for (uint32_t j = 1; j < E; ++j) best = fmaxf(best, x[j]);
-                if (best >= bound) {
+                if (Elem<T>::largest(some[u]) >= bound) {
 #pragma unroll
                     for (uint32_t j = 0; j < E; ++j)
                         if (x[j] >= bound) token_append(sm, token_key(x[j], sp.vec_index(at[u]) + j));
@@ -401,12 +416,7 @@ __global__ void __launch_bounds__(NT, HOLD ? 2 : 1024 / NT) token_logprob_kernel
 #pragma unroll
         for (int u = 0; u < HOLD; ++u) held[u] = fetch(sp.v0 + tid + u * NT);
 #pragma unroll
-        for (int u = 0; u < HOLD; u += 2) {
-            float x[2 * E];
-            Elem<T>::widen(held[u], x);
-            Elem<T>::widen(held[u + 1], x + E);
-            token_add<2 * E, ENT>(a, x, k);
-        }
+        for (int u = 0; u < HOLD; u += 2) token_add<T, ENT, 2>(a, held + u, k);
     } else {
         for (uint32_t v = sp.v0 + tid; v < sp.v1 + tid; v += kTokUnroll * NT) {
             uint4 raw[kTokUnroll];
@@ -417,16 +427,13 @@ __global__ void __launch_bounds__(NT, HOLD ? 2 : 1024 / NT) token_logprob_kernel
 #pragma unroll
                 for (int u = 0; u < kTokUnroll; ++u) raw[u] = fetch(v + u * NT);
             }
-            float x[kTokUnroll * E];
-#pragma unroll
-            for (int u = 0; u < kTokUnroll; ++u) Elem<T>::widen(raw[u], x + u * E);
-            token_add<kTokUnroll * E, ENT>(a, x, k);
+            token_add<T, ENT, kTokUnroll>(a, raw, k);
         }
     }
     if (tid < 2 * E) {
         bool have;
         const uint32_t j = sp.edge_index(tid, have);
-        if (have) { const float x[1] = {Elem<T>::load(sp.row + j)}; token_add<1, ENT>(a, x, k); }
+        if (have) token_add<ENT>(a, Elem<T>::load(sp.row + j), k);
     }
 
     const float own_max = a.m;
