@@ -45,8 +45,8 @@ struct ecq_muon {
     MuonTask* d_tasks[kShapeCount];
     double* d_partial;
     MuonProduct* d_products;
-    unsigned long long *d_done, *d_next;
-    uint32_t *d_sound, *d_status, *h_status;
+    unsigned long long *d_done, *d_next, *d_factor;
+    uint32_t *d_added, *d_prep_next, *d_sound, *d_status, *h_status;
     CUtensorMap rows128, rows64;         // of the bound workspace
     uint32_t n_spans, n_prep, n_tasks[kShapeCount], products_at[kShapeCount];
     uint64_t n_full[kShapeCount];        // tiles of one product with X, over all matrices
@@ -280,15 +280,17 @@ int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st
     static int clusters[kMaxDevices];
     auto kern = muon_iterate_kernel<CG, TN, SPLIT>;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CG;
-    at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CG;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.attrs = at;
-    cfg.numAttrs = CG > 1 ? 1 : 0;
+    cfg.numAttrs = CG > 1 ? 2 : 1;
     std::call_once(once[p->device], [&] {
         int n = 0;
         cfg.gridDim = dim3(p->sms / CG * CG);
@@ -310,6 +312,31 @@ int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st
     return ECQ_OK;
 }
 
+// The launches may be scheduled while what is ahead of them in the stream drains; they touch no
+// global memory before it has completed.
+template <typename T, bool MOM>
+int launch_prepare(const ecq_muon* p, MuonPrepare pre, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.blockDim = dim3(kMuonPrepThreads);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const bool both = p->n_spans + p->n_prep <= 5u * (uint32_t)p->sms;
+    for (pre.what = both ? 2 : 0; pre.what < 3; ++pre.what) {
+        cfg.gridDim = dim3(both ? p->n_spans + p->n_prep : pre.what ? p->n_prep : p->n_spans);
+        if (cudaLaunchKernelEx(&cfg, muon_prepare_kernel<T, MOM>, pre) != cudaSuccess) {
+            cudaGetLastError();
+            return ECQ_ERR_CUDA;
+        }
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+        if (pre.what == 1) break;
+    }
+    return ECQ_OK;
+}
+
 // Tiles of a call: the plan's choice, or the largest of which there are enough for every SM.
 int choose_tiles(const ecq_muon* p, bool split) {
     if (p->tiles != ECQ_MUON_TILES_AUTO) return p->tiles;
@@ -323,21 +350,13 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
     const int terms = p->precision == ECQ_MUON_HALF ? 1
                       : p->precision == ECQ_MUON_SPLIT ? 3
                       : (out.params || out_dtype != ECQ_BF16) ? 3 : 1;
-    if (in.momentum) {
-        muon_norm_kernel<float, true><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<float, true><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
-    } else if (in_dtype == ECQ_F32) {
-        muon_norm_kernel<float, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<float, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
-    } else if (in_dtype == ECQ_BF16) {
-        muon_norm_kernel<__nv_bfloat16, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<__nv_bfloat16, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
-    } else {
-        muon_norm_kernel<__half, false><<<p->n_spans, kMuonSpanThreads, 0, st>>>(p->d_spans, in, p->d_partial);
-        muon_prepare_kernel<__half, false><<<p->n_prep, kMuonPrepThreads, 0, st>>>(p->d_mats, p->d_prep, p->d_partial, in, ws, p->d_sound, p->d_done, p->d_next, p->d_status);
-    }
-    if (cudaGetLastError() != cudaSuccess) return ECQ_ERR_CUDA;
-    g_launches.fetch_add(2, std::memory_order_relaxed);
+    const MuonPrepare pre = {p->d_spans, p->d_prep, p->d_mats, in, ws, p->d_partial, p->d_added, p->d_factor, p->d_prep_next,
+                             p->d_sound, p->d_done, p->d_next, p->d_status, p->n_spans, p->wait_limit, 0};
+    const int rc = in.momentum              ? launch_prepare<float, true>(p, pre, st)
+                   : in_dtype == ECQ_F32    ? launch_prepare<float, false>(p, pre, st)
+                   : in_dtype == ECQ_BF16   ? launch_prepare<__nv_bfloat16, false>(p, pre, st)
+                                            : launch_prepare<__half, false>(p, pre, st);
+    if (rc != ECQ_OK) return rc;
 
     MuonIterate m = {};
     m.mats = p->d_mats;
@@ -347,6 +366,10 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
     m.ws = ws;
     m.done = p->d_done;
     m.next = p->d_next;
+    m.added = p->d_added;
+    m.factor = p->d_factor;
+    m.prepare_next = p->d_prep_next;
+    m.n_mats = (uint32_t)p->mats.size();
     m.status = p->d_status;
     m.out = out;
     m.out_dtype = out_dtype;
@@ -427,7 +450,7 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
         p->products_at[s] = (uint32_t)table.size();
         table.insert(table.end(), list.products.begin(), list.products.end());
     }
-    if (spans.size() > 0x7FFFFFFFull || prep.size() > 0x7FFFFFFFull) return ECQ_ERR_ARG;
+    if (spans.size() + prep.size() > 0x7FFFFFFFull) return ECQ_ERR_ARG;
 
     uint64_t bytes = 0;
     auto place = [&](uint64_t n) { const uint64_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
@@ -437,6 +460,7 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     for (int s = 0; s < kShapeCount; ++s) o_tasks[s] = place(tasks[s].size() * sizeof(MuonTask));
     const uint64_t o_partial = place(spans.size() * 8), o_sound = place(count * 4ull), o_status = place(4);
     const uint64_t o_products = place(table.size() * sizeof(MuonProduct)), o_done = place(count * 8ull), o_next = place(8);
+    const uint64_t o_added = place(count * 4ull), o_prep_next = place(4), o_factor = place(count * 8ull);
     std::vector<unsigned char> host(bytes, 0);
     memcpy(host.data() + o_mats, p->mats.data(), count * sizeof(MuonMat));
     memcpy(host.data() + o_spans, spans.data(), spans.size() * sizeof(MuonSpan));
@@ -455,6 +479,9 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     p->d_mats = reinterpret_cast<MuonMat*>(p->block + o_mats);
     p->d_spans = reinterpret_cast<MuonSpan*>(p->block + o_spans);
     p->d_prep = reinterpret_cast<MuonTile*>(p->block + o_prep);
+    p->d_added = reinterpret_cast<uint32_t*>(p->block + o_added);
+    p->d_factor = reinterpret_cast<unsigned long long*>(p->block + o_factor);
+    p->d_prep_next = reinterpret_cast<uint32_t*>(p->block + o_prep_next);
     for (int s = 0; s < kShapeCount; ++s) p->d_tasks[s] = reinterpret_cast<MuonTask*>(p->block + o_tasks[s]);
     p->d_partial = reinterpret_cast<double*>(p->block + o_partial);
     p->d_sound = reinterpret_cast<uint32_t*>(p->block + o_sound);
