@@ -50,6 +50,7 @@ struct ecq_muon {
     CUtensorMap rows128, rows64;         // of the bound workspace
     uint32_t n_spans, n_prep, n_tasks[kShapeCount], products_at[kShapeCount];
     uint64_t n_full[kShapeCount];        // tiles of one product with X, over all matrices
+    uint64_t padded[2];                  // entries of all X with rows in whole 128s, in whole 256s
     unsigned char* workspace;            // the caller's, NULL until bound
 };
 
@@ -337,10 +338,14 @@ int launch_prepare(const ecq_muon* p, MuonPrepare pre, cudaStream_t st) {
     return ECQ_OK;
 }
 
-// Tiles of a call: the plan's choice, or the largest of which there are enough for every SM.
+// Tiles of a call: the plan's choice, or the largest of which there are enough for every SM.  Pairs
+// take 256 rows at a time, which has to fill: 48 matrices of 128 x 512 take 160 us with pairs and
+// 109 without, three of 1537 x 611 (a fifth of the rows empty) 307 and 290 (22-bit operands), but
+// resnet50's matrices (a tenth) 1022 and 1160.  Too few tiles for the SMs: one 1024 x 1024 takes 218,
+// 161 and 141 us with 256 x 256, 128 x 128 and 128 x 64, three of them 254, 192 and 215.
 int choose_tiles(const ecq_muon* p, bool split) {
     if (p->tiles != ECQ_MUON_TILES_AUTO) return p->tiles;
-    if (p->n_full[split ? 1 : 0] * 2 >= (uint64_t)p->sms) return ECQ_MUON_TILES_256X256;
+    if (p->n_full[split ? 1 : 0] * 2 >= (uint64_t)p->sms && 100 * p->padded[1] <= 115 * p->padded[0]) return ECQ_MUON_TILES_256X256;
     if (!split && p->n_full[2] >= (uint64_t)p->sms) return ECQ_MUON_TILES_128X128;
     return ECQ_MUON_TILES_128X64;
 }
@@ -415,6 +420,8 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
         if (!finite(mat.scale)) return ECQ_ERR_ARG;
         mat.x_tile = (uint32_t)p->x_tiles; mat.m_tile = (uint32_t)p->m_tiles;
         p->x_tiles += round64(mat.n) / 64 * mat.down;
+        p->padded[0] += (uint64_t)(mat.m + 127) / 128 * 128 * mat.n;
+        p->padded[1] += (uint64_t)(mat.m + 255) / 256 * 256 * mat.n;
         p->m_tiles += (uint64_t)mat.pad / 64 * mat.down;
         if (workspace_tiles(p) > 0x0FFFFFFFull) return ECQ_ERR_ARG;    // pieces are TMA coordinates
         // spans of about kMuonSpan entries: flat where the rows lie end to end, else whole rows or parts of them

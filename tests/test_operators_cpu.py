@@ -41,3 +41,49 @@ def test_logprob_grad_refuses(bad):
 def test_no_rows_is_nothing_to_do():
     assert logprob(rows=0) == ecq.ECQ_OK and grad(rows=0) == ecq.ECQ_OK
     assert logprob(rows=0, dtype=9) == ecq.ECQ_ERR_ARG
+
+
+def create(offsets=(0,), rows=(8,), cols=(6,), strides=None, scales=None, steps=5, coefficients=None, precision=0, out=True,
+           count=None):
+    n = len(offsets)
+    u64, u32, f32 = ctypes.c_uint64 * n, ctypes.c_uint32 * n, ctypes.c_float * n
+    h = ctypes.c_void_p()
+    rc = binding.lib().ecq_muon_create(
+        ctypes.byref(h) if out else None, n if count is None else count, u64(*offsets), u32(*rows), u32(*cols),
+        None if strides is None else u64(*strides), None if scales is None else f32(*scales), steps,
+        None if coefficients is None else (ctypes.c_float * len(coefficients))(*coefficients), precision)
+    assert h.value is None
+    return rc
+
+
+@pytest.mark.parametrize("bad", [
+    dict(out=False), dict(count=0), dict(count=65537), dict(rows=(0,)), dict(cols=(0,)), dict(rows=((1 << 22) + 1,)),
+    dict(rows=(32769,), cols=(32769,)), dict(strides=(5,)), dict(offsets=((1 << 48) + 1,)), dict(scales=(float("nan"),)),
+    dict(steps=0), dict(steps=65), dict(precision=-1), dict(precision=3), dict(coefficients=[float("inf")] * 15),
+    dict(coefficients=[30.0, 0.0, 0.0] * 5), dict(coefficients=[1.0, 200.0, -200.0] * 5)])
+def test_muon_create_refuses(bad):
+    assert create(**bad) == ecq.ECQ_ERR_ARG
+
+
+def test_muon_calls_refuse_no_plan():
+    L = binding.lib()
+    assert L.ecq_muon_orthogonalize(None, P, 0, P, 0, None) == ecq.ECQ_ERR_ARG
+    assert L.ecq_muon_step(None, P, P, 0.9, 1, 0.1, 0.0, P, None, 0, None) == ecq.ECQ_ERR_ARG
+    assert L.ecq_muon_bind(None, P, 0, None) == ecq.ECQ_ERR_ARG
+    assert L.ecq_muon_set_tiles(None, 0) == ecq.ECQ_ERR_ARG
+    assert L.ecq_muon_set_wait_limit(None, 1) == ecq.ECQ_ERR_ARG
+    assert L.ecq_muon_status(None, None) == ecq.ECQ_ERR_ARG
+    assert L.ecq_muon_workspace_bytes(None) == 0
+    L.ecq_muon_destroy(None)
+
+
+def test_binding_refuses_before_the_library():
+    import torch
+    for bad in (dict(rows=[8, 8]), dict(strides=[6, 6]), dict(scales=[]), dict(coefficients=[(1.0, 1.0, 1.0)] * 4),
+                dict(offsets=[-1])):
+        args = dict(offsets=[0], rows=[8], cols=[6])
+        args.update(bad)
+        with pytest.raises(ValueError):
+            ecq.ecq_muon_create(**args)
+    with pytest.raises(ValueError):
+        ecq.ecq_token_logprob(torch.zeros(2, 8), torch.zeros(2, dtype=torch.int64), torch.zeros(2))
