@@ -435,27 +435,32 @@ int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_
  *   coefficients a, b, c of each step, or NULL for the defaults.  ECQ_ERR_ARG if some singular
  *                value in (0, 1] would leave the range that the kernels' fp16 copies hold
  *                (iterates up to 8, |b| s^2 + |c| s^4 up to 128).
- *   precision    ECQ_MUON_HALF: operands of the products rounded to 11 bits, X kept with 22; the
- *                result is within about 1e-3 of exact (relative, 2-norm).
+ *   precision    ECQ_MUON_HALF: operands of the products rounded to 11 bits, X kept with 22; with
+ *                the default coefficients the result is within about 1e-3 of exact (relative, the
+ *                root of the sum of squares), 1e-2 where a few singular values carry all of U.
+ *                bf16, for comparison, rounds by up to 4e-3.
  *                ECQ_MUON_SPLIT: all operands with 22 bits, three times the products; the error of
- *                fp32 arithmetic.
+ *                fp32 arithmetic (a few 1e-6).
  *                ECQ_MUON_AUTO: HALF where a call's outputs are bf16 alone, else SPLIT.
  *   The plan holds its tables on the current device; ECQ_ERR_ALLOC / ECQ_ERR_CUDA if that fails.
  * ecq_muon_destroy  NULL is allowed.  Do not destroy a plan with work in flight.
- * ecq_muon_set_tiles  tile of the product kernel: 256 x 256 by pairs of CTAs, 128 x 128 or
- *                128 x 64 by one; AUTO: the largest of which there are enough for every SM.  The
- *                result may differ in the last bits of the sums.
+ * ecq_muon_set_tiles  tile of the product kernel: 256 x 256 by pairs of CTAs (256 x 128 with
+ *                ECQ_MUON_SPLIT), 128 x 128 (128 x 64 with it) or 128 x 64 by one; AUTO: the largest
+ *                of which there are enough for every SM and that the matrices fill.  The result may
+ *                differ in the last bits of the sums.  ECQ_ERR_ALLOC / ECQ_ERR_CUDA if the lists of
+ *                tiles cannot be laid down; the choice is then as it was.
  * ecq_muon_set_wait_limit  as ecq_set_wait_limit: polls before an in-kernel wait gives up and
  *                ECQ_ERR_TIMEOUT becomes pending.
  * ecq_muon_bind  gives the plan its scratch memory: at least ecq_muon_workspace_bytes() bytes,
  *                256-byte aligned, owned by the caller and left alone until the plan is bound
- *                anew or destroyed.  Waits for `cuda_stream`.  A plan's calls share it: they must be
- *                ordered, on one stream or by events.
+ *                anew or destroyed.  A plan's calls share it: they must be ordered, on one stream or by
+ *                events, and none may be in flight when the plan is bound anew.
  * ecq_muon_orthogonalize  update = X alone (scale not applied) of the matrices in `in`, for flat
  *                vectors of ECQ_F32, ECQ_BF16 or ECQ_F16; in == out is allowed for equal types.
  * ecq_muon_step  params or update may be NULL, not both.  update is a flat vector of
  *                `update_dtype`.  0 <= mu <= 1; lr, decay >= 0.  The vectors must not overlap.
- * All vectors are 16-byte aligned, ECQ_ERR_ARG otherwise or before the plan is bound.
+ * All vectors are 16-byte aligned, ECQ_ERR_ARG otherwise or before the plan is bound.  Two
+ * launches where the matrices are few and small, else three.
  * ecq_muon_status  as ecq_status.
  */
 typedef struct ecq_muon ecq_muon;

@@ -42,13 +42,12 @@ struct ecq_muon {
     MuonMat* d_mats;
     MuonSpan* d_spans;
     MuonTile* d_prep;
-    MuonTask* d_tasks[kShapeCount];
+    unsigned char* d_tasks[kShapeCount]; // products and tiles by tile shape, each an allocation, NULL until needed
     double* d_partial;
-    MuonProduct* d_products;
     unsigned long long *d_done, *d_next, *d_factor;
     uint32_t *d_added, *d_prep_next, *d_sound, *d_status, *h_status;
     CUtensorMap rows128, rows64;         // of the bound workspace
-    uint32_t n_spans, n_prep, n_tasks[kShapeCount], products_at[kShapeCount];
+    uint32_t n_spans, n_prep, n_tasks[kShapeCount], tasks_at[kShapeCount];
     uint64_t n_full[kShapeCount];        // tiles of one product with X, over all matrices
     uint64_t padded[2];                  // entries of all X with rows in whole 128s, in whole 256s
     unsigned char* workspace;            // the caller's, NULL until bound
@@ -301,8 +300,10 @@ int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st
         clusters[p->device] = std::min(n, p->sms / CG);
     });
     if (clusters[p->device] <= 0) return ECQ_ERR_CUDA;
-    it.tasks = p->d_tasks[shape]; it.n_tasks = p->n_tasks[shape];
-    it.products = p->d_products + p->products_at[shape];
+    if (!p->d_tasks[shape]) return ECQ_ERR_ARG;
+    it.products = reinterpret_cast<const MuonProduct*>(p->d_tasks[shape]);
+    it.tasks = reinterpret_cast<const MuonTask*>(p->d_tasks[shape] + p->tasks_at[shape]);
+    it.n_tasks = p->n_tasks[shape];
     cfg.gridDim = dim3((uint32_t)std::min<uint64_t>(p->n_full[shape], clusters[p->device]) * CG);
     cfg.stream = st;
     if (cudaLaunchKernelEx(&cfg, kern, it) != cudaSuccess) {
@@ -350,6 +351,12 @@ int choose_tiles(const ecq_muon* p, bool split) {
     return ECQ_MUON_TILES_128X64;
 }
 
+// Index in kShapes of a tile choice.
+int shape_of(int tiles, bool split) {
+    if (split) return tiles == ECQ_MUON_TILES_256X256 ? 1 : 3;
+    return tiles == ECQ_MUON_TILES_256X256 ? 0 : tiles == ECQ_MUON_TILES_128X128 ? 2 : 3;
+}
+
 int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int out_dtype, cudaStream_t st) {
     const MuonWork ws = work_of(p);
     const int terms = p->precision == ECQ_MUON_HALF ? 1
@@ -379,16 +386,44 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
     m.out = out;
     m.out_dtype = out_dtype;
     m.wait_limit = p->wait_limit;
-    const int tiles = choose_tiles(p, terms == 3);
-    if (terms == 3)
-        return tiles == ECQ_MUON_TILES_256X256 ? launch_iterate<2, 128, true>(p, m, 1, st)
-                                               : launch_iterate<1, 64, true>(p, m, 3, st);
-    return tiles == ECQ_MUON_TILES_256X256   ? launch_iterate<2, 256, false>(p, m, 0, st)
-           : tiles == ECQ_MUON_TILES_128X128 ? launch_iterate<1, 128, false>(p, m, 2, st)
-                                             : launch_iterate<1, 64, false>(p, m, 3, st);
+    const int shape = shape_of(choose_tiles(p, terms == 3), terms == 3);
+    if (terms == 3) return shape == 1 ? launch_iterate<2, 128, true>(p, m, shape, st) : launch_iterate<1, 64, true>(p, m, shape, st);
+    return shape == 0   ? launch_iterate<2, 256, false>(p, m, shape, st)
+           : shape == 2 ? launch_iterate<1, 128, false>(p, m, shape, st)
+                        : launch_iterate<1, 64, false>(p, m, shape, st);
 }
 
 bool finite(float x) { return x - x == 0.f; }
+
+// The tile lists that the plan's precision and tile choice need and that it does not have yet.
+int build_tasks(ecq_muon* p) {
+    for (int split = 0; split < 2; ++split) {
+        if (p->precision == (split ? ECQ_MUON_HALF : ECQ_MUON_SPLIT)) continue;
+        const int shape = shape_of(choose_tiles(p, split), split);
+        if (p->d_tasks[shape]) continue;
+        TaskList list(p->mats, kShapes[shape], p->steps);
+        uint64_t all = 0;
+        for (uint32_t i = 0; i < p->mats.size(); ++i) all += list.all_tiles(i);
+        if (all > 0x10000000ull) return ECQ_ERR_ARG;
+        list.tasks.reserve(all);
+        list.build();
+        const uint64_t products = (list.products.size() * sizeof(MuonProduct) + 255) / 256 * 256;
+        unsigned char* to = nullptr;
+        if (cudaMalloc(&to, products + list.tasks.size() * sizeof(MuonTask)) != cudaSuccess) {
+            cudaGetLastError();
+            return ECQ_ERR_ALLOC;
+        }
+        if (cudaMemcpy(to, list.products.data(), list.products.size() * sizeof(MuonProduct), cudaMemcpyHostToDevice) != cudaSuccess ||
+            cudaMemcpy(to + products, list.tasks.data(), list.tasks.size() * sizeof(MuonTask), cudaMemcpyHostToDevice) != cudaSuccess) {
+            cudaFree(to);
+            return ECQ_ERR_CUDA;
+        }
+        p->d_tasks[shape] = to;
+        p->tasks_at[shape] = (uint32_t)products;
+        p->n_tasks[shape] = (uint32_t)list.tasks.size();
+    }
+    return ECQ_OK;
+}
 
 int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t* rows, const uint32_t* cols,
            const uint64_t* strides, const float* scales, uint32_t steps, const float* coefficients) {
@@ -402,7 +437,6 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     if (!steps_in_range(p->steps)) return ECQ_ERR_ARG;
     std::vector<MuonSpan> spans;
     std::vector<MuonTile> prep;
-    std::vector<MuonTask> tasks[kShapeCount];
     for (uint32_t i = 0; i < count; ++i) {
         MuonMat mat = {};
         mat.offset = offsets[i];
@@ -442,39 +476,23 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
             for (uint32_t c = 0; c * 64 < mat.cols; ++c) prep.push_back({i, (uint16_t)r, (uint16_t)c});
         p->mats.push_back(mat);
     }
-    std::vector<MuonProduct> table;
-    for (int s = 0; s < kShapeCount; ++s) {
-        TaskList list(p->mats, kShapes[s], p->steps);
-        uint64_t all = 0;
-        for (uint32_t i = 0; i < count; ++i) {
-            p->n_full[s] += list.full[i];
-            all += list.all_tiles(i);
-        }
-        if (all > 0x10000000ull) return ECQ_ERR_ARG;
-        list.build();
-        tasks[s].swap(list.tasks);
-        p->n_tasks[s] = (uint32_t)tasks[s].size();
-        p->products_at[s] = (uint32_t)table.size();
-        table.insert(table.end(), list.products.begin(), list.products.end());
-    }
+    for (int s = 0; s < kShapeCount; ++s)
+        for (const MuonMat& mat : p->mats)
+            p->n_full[s] += (uint64_t)((mat.m + kShapes[s].cg * 128 - 1) / (kShapes[s].cg * 128)) *
+                            ((mat.n + kShapes[s].tn - 1) / kShapes[s].tn);
     if (spans.size() + prep.size() > 0x7FFFFFFFull) return ECQ_ERR_ARG;
 
     uint64_t bytes = 0;
     auto place = [&](uint64_t n) { const uint64_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
     const uint64_t o_mats = place(count * sizeof(MuonMat)), o_spans = place(spans.size() * sizeof(MuonSpan));
     const uint64_t o_prep = place(prep.size() * sizeof(MuonTile));
-    uint64_t o_tasks[kShapeCount];
-    for (int s = 0; s < kShapeCount; ++s) o_tasks[s] = place(tasks[s].size() * sizeof(MuonTask));
     const uint64_t o_partial = place(spans.size() * 8), o_sound = place(count * 4ull), o_status = place(4);
-    const uint64_t o_products = place(table.size() * sizeof(MuonProduct)), o_done = place(count * 8ull), o_next = place(8);
+    const uint64_t o_done = place(count * 8ull), o_next = place(8);
     const uint64_t o_added = place(count * 4ull), o_prep_next = place(4), o_factor = place(count * 8ull);
     std::vector<unsigned char> host(bytes, 0);
     memcpy(host.data() + o_mats, p->mats.data(), count * sizeof(MuonMat));
     memcpy(host.data() + o_spans, spans.data(), spans.size() * sizeof(MuonSpan));
-    memcpy(host.data() + o_products, table.data(), table.size() * sizeof(MuonProduct));
     memcpy(host.data() + o_prep, prep.data(), prep.size() * sizeof(MuonTile));
-    for (int s = 0; s < kShapeCount; ++s)
-        memcpy(host.data() + o_tasks[s], tasks[s].data(), tasks[s].size() * sizeof(MuonTask));
     if (cudaGetDevice(&p->device) != cudaSuccess || p->device < 0 || p->device >= kMaxDevices ||
         cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess)
         return ECQ_ERR_CUDA;
@@ -489,16 +507,14 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     p->d_added = reinterpret_cast<uint32_t*>(p->block + o_added);
     p->d_factor = reinterpret_cast<unsigned long long*>(p->block + o_factor);
     p->d_prep_next = reinterpret_cast<uint32_t*>(p->block + o_prep_next);
-    for (int s = 0; s < kShapeCount; ++s) p->d_tasks[s] = reinterpret_cast<MuonTask*>(p->block + o_tasks[s]);
     p->d_partial = reinterpret_cast<double*>(p->block + o_partial);
     p->d_sound = reinterpret_cast<uint32_t*>(p->block + o_sound);
     p->d_status = reinterpret_cast<uint32_t*>(p->block + o_status);
-    p->d_products = reinterpret_cast<MuonProduct*>(p->block + o_products);
     p->d_done = reinterpret_cast<unsigned long long*>(p->block + o_done);
     p->d_next = reinterpret_cast<unsigned long long*>(p->block + o_next);
     p->n_spans = (uint32_t)spans.size();
     p->n_prep = (uint32_t)prep.size();
-    return ECQ_OK;
+    return build_tasks(p);
 }
 
 }  // namespace
@@ -531,14 +547,27 @@ int ecq_muon_create(ecq_muon** out, uint32_t count, const uint64_t* offsets, con
 void ecq_muon_destroy(ecq_muon* p) {
     if (!p) return;
     if (p->block) cudaFree(p->block);
+    for (unsigned char* tasks : p->d_tasks)
+        if (tasks) cudaFree(tasks);
     if (p->h_status) cudaFreeHost(p->h_status);
     delete p;
 }
 
 int ecq_muon_set_tiles(ecq_muon* p, int tiles) {
     if (!p || tiles < ECQ_MUON_TILES_AUTO || tiles > ECQ_MUON_TILES_128X64) return ECQ_ERR_ARG;
+    const int before = p->tiles;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(p->device) != cudaSuccess) return ECQ_ERR_CUDA;
+    int rc;
     p->tiles = tiles;
-    return ECQ_OK;
+    try {
+        rc = build_tasks(p);
+    } catch (const std::bad_alloc&) {
+        rc = ECQ_ERR_ALLOC;
+    }
+    if (rc != ECQ_OK) p->tiles = before;
+    cudaSetDevice(dev);
+    return rc;
 }
 
 int ecq_muon_set_wait_limit(ecq_muon* p, uint32_t polls) {
