@@ -11,7 +11,7 @@ using namespace ecq;
 
 namespace {
 
-template <typename T, bool ENT, int HOLD, int NT>
+template <typename T, bool ENT, int NT>
 int launch_forward(const TokenForward& P, uint64_t rows, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((uint32_t)(rows << P.cluster_log2));
@@ -24,7 +24,7 @@ int launch_forward(const TokenForward& P, uint64_t rows, cudaStream_t st) {
     at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = P.cluster_log2 ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, token_logprob_kernel<T, ENT, HOLD, NT>, P) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, token_logprob_kernel<T, ENT, NT>, P) != cudaSuccess) {
         cudaGetLastError();
         return ECQ_ERR_CUDA;
     }
@@ -33,15 +33,9 @@ int launch_forward(const TokenForward& P, uint64_t rows, cudaStream_t st) {
 }
 
 template <typename T>
-int launch_forward(const TokenForward& P, uint64_t rows, cudaStream_t st) {
-    // vectors of a CTA's part of a row; one more where the row does not start on a vector
-    const uint32_t per_cta = (P.vocab / (16 / (uint32_t)sizeof(T)) >> P.cluster_log2) + 1;
-    if (!P.cluster_log2)
-        return P.entropy ? launch_forward<T, true, 0, kTokStream>(P, rows, st) : launch_forward<T, false, 0, kTokStream>(P, rows, st);
-    if (per_cta <= (uint32_t)(kTokHold * kTokThreads))
-        return P.entropy ? launch_forward<T, true, kTokHold, kTokThreads>(P, rows, st)
-                         : launch_forward<T, false, kTokHold, kTokThreads>(P, rows, st);
-    return P.entropy ? launch_forward<T, true, 0, kTokThreads>(P, rows, st) : launch_forward<T, false, 0, kTokThreads>(P, rows, st);
+int launch_forward(const TokenForward& P, uint64_t rows, bool stream, cudaStream_t st) {
+    if (stream) return P.entropy ? launch_forward<T, true, kTokStream>(P, rows, st) : launch_forward<T, false, kTokStream>(P, rows, st);
+    return P.entropy ? launch_forward<T, true, kTokThreads>(P, rows, st) : launch_forward<T, false, kTokThreads>(P, rows, st);
 }
 
 template <typename T>
@@ -86,16 +80,25 @@ int ecq_token_logprob(const void* logits, int dtype, uint64_t rows, uint32_t voc
         return ECQ_ERR_CUDA;
     TokenForward P = {logits, row_stride, targets, logprob, entropy, lse, top_logprob, top_index,
                       vocab, top, 0, inv_temperature};
-    // A row is split over a cluster while there are fewer CTAs than SMs and each keeps a vector per thread.
-    const uint64_t row_bytes = (uint64_t)vocab * dtype_bytes(dtype);
-    while ((1u << P.cluster_log2) < (uint32_t)kTokMaxCluster && rows << P.cluster_log2 < (uint64_t)sms &&
-           row_bytes >= (uint64_t)(2u << P.cluster_log2) * kTokThreads * 16)
-        ++P.cluster_log2;
+    // Vectors of 16 bytes that a thread has of a row.  A row of 12 or more is split over a cluster of
+    // CTAs, as long as 3 are left for each thread and there is no more than a CTA an SM, or, with 24
+    // left, three.  In us, on 1, 2, 4 and 8 CTAs, with top 5 (one row: 20) and entropy:
+    //     bf16   1 x 16384    6.0   6.5   6.6   7.1       200 x 50257   11.6  12.7  18.3  26.1
+    //            1 x 50257   10.1   8.7   7.4   7.2       60 x 128001   14.5  10.9  10.4  12.6
+    //           24 x 50257    8.9   8.2   7.3   8.0      200 x 128001   24.2  20.1  26.0  32.8
+    //           60 x 50257    9.0   8.4   8.9  10.9      400 x 128001   30.7  37.3  42.1  60.0
+    const uint32_t held = vocab / (16 / (uint32_t)dtype_bytes(dtype)) / kTokThreads;
+    if (held >= 12)
+        for (uint32_t c = 1; (1u << c) <= (uint32_t)kTokMaxCluster && held >> c >= 3; ++c)
+            if (rows << c <= (uint64_t)(held >> c >= 24 ? 3 : 1) * (uint64_t)sms) P.cluster_log2 = c;
+    // Half the threads a CTA where the rows are more than fit the GPU at once (2047 x 50257, top 8: 59.2
+    // against 62.6 us; 400 x 50257: 20.5 against 17.2) or short (400 x 4096: 6.8 against 7.7).
+    const bool stream = !P.cluster_log2 && (rows > (uint64_t)(1024 / kTokThreads) * (uint64_t)sms || held < 4);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     switch (dtype) {
-        case ECQ_F32: return launch_forward<float>(P, rows, st);
-        case ECQ_BF16: return launch_forward<__nv_bfloat16>(P, rows, st);
-        default: return launch_forward<__half>(P, rows, st);
+        case ECQ_F32: return launch_forward<float>(P, rows, stream, st);
+        case ECQ_BF16: return launch_forward<__nv_bfloat16>(P, rows, stream, st);
+        default: return launch_forward<__half>(P, rows, stream, st);
     }
 }
 

@@ -32,12 +32,11 @@ constexpr float kLn2 = 0.6931471805599453f;
 // of the row) are read again, out of L2, and the few that reach the bound are ranked by counting.
 // Entries are ordered by value, equal ones by index (the lower first); a 64-bit key holds both.
 
-constexpr int kTokThreads = 256;         // of a CTA that has a part of a row
-constexpr int kTokStream = 128;          // of a CTA that has rows to itself, eight of them an SM: while some
-                                         // rank their best entries the others keep the memory busy
+constexpr int kTokThreads = 256;         // of a CTA where rows are few, four of them an SM
+constexpr int kTokStream = 128;          // where they are many, eight an SM: while some rank their best
+                                         // entries the others keep the memory busy
 constexpr int kTokGroups = 128;
 constexpr int kTokUnroll = 4;            // 16-byte vectors in flight per thread
-constexpr int kTokHold = 8;              // vectors per thread that a CTA keeps in registers
 constexpr int kTokMaxTop = 32;
 constexpr int kTokMaxCluster = 8;
 constexpr int kTokCandidates = 1024;
@@ -272,11 +271,9 @@ __device__ __noinline__ void token_collect_slow(TokenShared& sm, const TokenSpan
     __syncthreads();
 }
 
-// The CTA's best `top` entries into sm.cand (any order, sm.n_cand of them, more than needed).  With
-// HOLD the threads still have the CTA's vectors.
-template <typename T, int HOLD, int NT>
-__device__ __forceinline__ void token_collect(TokenShared& sm, const TokenSpan<T>& sp, float m, uint32_t top,
-                                              const uint4 (&raw)[HOLD ? HOLD : 1]) {
+// The CTA's best `top` entries into sm.cand (any order, sm.n_cand of them, more than needed).
+template <typename T, int NT>
+__device__ __forceinline__ void token_collect(TokenShared& sm, const TokenSpan<T>& sp, float m, uint32_t top) {
     constexpr uint32_t E = Elem<T>::kPer16;
     constexpr uint32_t L = NT / kTokGroups;                  // threads per group
     const uint32_t tid = threadIdx.x;
@@ -300,30 +297,14 @@ __device__ __forceinline__ void token_collect(TokenShared& sm, const TokenSpan<T
 #pragma unroll
         for (uint32_t o = 1; o < L; o <<= 1) rank += __shfl_xor_sync(~0u, rank, o);
         if (rank == top - 1 && tid % L == 0) sm.bound = mine;
-        // with entries streaming past, the groups that may reach the bound are those ranked before it
-        if (!HOLD && rank < top && tid % L == 0) sm.flagged[rank] = g0;
+        // the groups that may reach the bound are those ranked before it
+        if (rank < top && tid % L == 0) sm.flagged[rank] = g0;
         __syncthreads();
-        if constexpr (HOLD == 0) {
-            if (rank >= top && tid % L == 0 && mine == sm.bound) sm.flagged[top + atomicAdd(&sm.n_tied, 1u)] = g0;
-            __syncthreads();
-        }
+        if (rank >= top && tid % L == 0 && mine == sm.bound) sm.flagged[top + atomicAdd(&sm.n_tied, 1u)] = g0;
+        __syncthreads();
     }
     const float bound = sm.bound;
-    if constexpr (HOLD > 0) {
-        if (m >= bound) {
-#pragma unroll
-            for (uint32_t u = 0; u < (uint32_t)HOLD; ++u) {
-                float x[E];
-                Elem<T>::widen(raw[u], x);
-                const uint32_t v = sp.v0 + tid + u * NT;
-                if (Elem<T>::largest(raw[u]) >= bound && v < sp.v1) {
-#pragma unroll
-                    for (uint32_t j = 0; j < E; ++j)
-                        if (x[j] >= bound) token_append(sm, token_key(x[j], sp.vec_index(v) + j));
-                }
-            }
-        }
-    } else {
+    {
         // Groups whose maximum equals the bound but that rank behind it count, too: an entry of
         // theirs that equals it may come before others by index.
         const uint32_t steps = (sp.v1 - sp.v0 + NT - 1) / NT, per_group = steps * L;
@@ -373,11 +354,8 @@ __device__ __forceinline__ void cluster_store(uint32_t addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
-// HOLD vectors a thread are read once and kept (few rows, each split over a cluster: the chain from
-// the first load to the result counts), or, with 0, the row streams past (many rows: occupancy
-// counts).
-template <typename T, bool ENT, int HOLD, int NT>
-__global__ void __launch_bounds__(NT, HOLD ? 2 : 1024 / NT) token_logprob_kernel(TokenForward P) {
+template <typename T, bool ENT, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) token_logprob_kernel(TokenForward P) {
     constexpr uint32_t E = Elem<T>::kPer16;
     __shared__ TokenShared sm;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -407,28 +385,20 @@ __global__ void __launch_bounds__(NT, HOLD ? 2 : 1024 / NT) token_logprob_kernel
     const float k = __fmul_rn(P.tau, kLog2e);
     TokenSums a = {-FLT_MAX, 0.f, 0.f};
     // batches of vectors; what is missing at the end is as if masked
-    uint4 held[HOLD ? HOLD : 1];
     auto fetch = [&](uint32_t v) {
         constexpr uint32_t none = Elem<T>::kMinusInf;
         return v < sp.v1 ? sp.vec(v) : make_uint4(none, none, none, none);
     };
-    if constexpr (HOLD > 0) {
+    for (uint32_t v = sp.v0 + tid; v < sp.v1 + tid; v += kTokUnroll * NT) {
+        uint4 raw[kTokUnroll];
+        if (v - tid + kTokUnroll * NT <= sp.v1) {
 #pragma unroll
-        for (int u = 0; u < HOLD; ++u) held[u] = fetch(sp.v0 + tid + u * NT);
+            for (int u = 0; u < kTokUnroll; ++u) raw[u] = sp.vec(v + u * NT);
+        } else {
 #pragma unroll
-        for (int u = 0; u < HOLD; u += 2) token_add<T, ENT, 2>(a, held + u, k);
-    } else {
-        for (uint32_t v = sp.v0 + tid; v < sp.v1 + tid; v += kTokUnroll * NT) {
-            uint4 raw[kTokUnroll];
-            if (v - tid + kTokUnroll * NT <= sp.v1) {
-#pragma unroll
-                for (int u = 0; u < kTokUnroll; ++u) raw[u] = sp.vec(v + u * NT);
-            } else {
-#pragma unroll
-                for (int u = 0; u < kTokUnroll; ++u) raw[u] = fetch(v + u * NT);
-            }
-            token_add<T, ENT, kTokUnroll>(a, raw, k);
+            for (int u = 0; u < kTokUnroll; ++u) raw[u] = fetch(v + u * NT);
         }
+        token_add<T, ENT, kTokUnroll>(a, raw, k);
     }
     if (tid < 2 * E) {
         bool have;
@@ -441,7 +411,7 @@ __global__ void __launch_bounds__(NT, HOLD ? 2 : 1024 / NT) token_logprob_kernel
     for (int o = 16; o > 0; o >>= 1)
         token_merge(a, {__shfl_xor_sync(~0u, a.m, o), __shfl_xor_sync(~0u, a.s, o), __shfl_xor_sync(~0u, a.t, o)}, k);
     if (lane == 0) sm.warp_sums[warp] = a;
-    if (P.top) token_collect<T, HOLD, NT>(sm, sp, own_max, P.top, held);              // its barriers order warp_sums too
+    if (P.top) token_collect<T, NT>(sm, sp, own_max, P.top);              // its barriers order warp_sums too
     else __syncthreads();
     if (C > 1) cluster_wait();
 
