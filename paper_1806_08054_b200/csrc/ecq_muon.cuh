@@ -475,7 +475,7 @@ struct MuonShape {
     static constexpr uint32_t kBoxesA = 2, kBoxesB = TN / CG / 64;
     static constexpr uint32_t kBytesA = kBoxesA * kMuonBox, kBytesB = kBoxesB * kMuonBox;
     static constexpr uint32_t kStageBytes = kHalves * (kBytesA + kBytesB);
-    static constexpr uint32_t kEpiWarps = TN >= 128 ? 8 : 4;
+    static constexpr uint32_t kEpiWarps = 8;
     static constexpr uint32_t kCols = TN / (kEpiWarps / 4);           // columns of an epilogue warp
     static constexpr uint32_t kThreads = (kEpiWarps + 4) * 32;        // + two for loads, products, signals
     static constexpr uint32_t kEpiBytes = kEpiWarps * 2 * kMuonBlock;
