@@ -445,7 +445,8 @@ int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_
  *   The plan holds its tables on the current device; ECQ_ERR_ALLOC / ECQ_ERR_CUDA if that fails.
  * ecq_muon_destroy  NULL is allowed.  Do not destroy a plan with work in flight.
  * ecq_muon_set_tiles  tile of the product kernel: 256 x 256 by pairs of CTAs (256 x 128 with
- *                ECQ_MUON_SPLIT), 128 x 128 (128 x 64 with it) or 128 x 64 by one; AUTO: the largest
+ *                ECQ_MUON_SPLIT), 128 x 128 (128 x 64 with it) or 128 x 64 by one (by two that share
+ *                the sums where tiles are few and long); AUTO: the largest
  *                of which there are enough for every SM and that the matrices fill.  The result may
  *                differ in the last bits of the sums.  ECQ_ERR_ALLOC / ECQ_ERR_CUDA if the lists of
  *                tiles cannot be laid down; the choice is then as it was.

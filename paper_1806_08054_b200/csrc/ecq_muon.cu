@@ -49,6 +49,8 @@ struct ecq_muon {
     CUtensorMap rows128, rows64;         // of the bound workspace
     uint32_t n_spans, n_prep, n_tasks[kShapeCount], tasks_at[kShapeCount];
     uint64_t n_full[kShapeCount];        // tiles of one product with X, over all matrices
+    uint64_t n_sym;                      // tiles of 128 x 64 of one symmetric product
+    uint64_t k_steps, chain;             // steps of 64 along K of every product, and products, over all matrices
     uint64_t padded[2];                  // entries of all X with rows in whole 128s, in whole 256s
     unsigned char* workspace;            // the caller's, NULL until bound
 };
@@ -246,6 +248,16 @@ struct TaskList {
                                  (uint16_t)(p.kind != kMuonApply && c * shape.tn / tm < r), (uint32_t)need});
         }
     }
+    void measure(uint64_t& n_sym, uint64_t& k_steps, uint64_t& chain) const {
+        n_sym = k_steps = chain = 0;
+        for (uint32_t i = 0; i < mats.size(); ++i) {
+            const uint32_t from = merged(i) ? count[0] : 0;
+            n_sym += sym[i];
+            chain += count[merged(i)];
+            for (uint32_t k = 0; k < count[merged(i)]; ++k)
+                k_steps += ((products[from + k].kind == kMuonGram ? mats[i].n : mats[i].m) + 63) / 64;
+        }
+    }
     void build() {
         std::vector<std::pair<uint32_t, uint32_t>> groups;
         uint64_t all = 0, held = 0;
@@ -273,38 +285,39 @@ struct TaskList {
     }
 };
 
-template <int CG, int TN, bool SPLIT>
+template <int CG, int TN, bool SPLIT, bool KS = false>
 int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st) {
-    using S = MuonShape<CG, TN, SPLIT>;
+    constexpr int kCluster = KS ? 2 : CG;
+    using S = MuonShape<CG, TN, SPLIT, KS>;
     static std::once_flag once[kMaxDevices];
     static int clusters[kMaxDevices];
-    auto kern = muon_iterate_kernel<CG, TN, SPLIT>;
+    auto kern = muon_iterate_kernel<CG, TN, SPLIT, KS>;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = CG;
+    at[1].val.clusterDim.x = kCluster;
     at[1].val.clusterDim.y = 1;
     at[1].val.clusterDim.z = 1;
     cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.attrs = at;
-    cfg.numAttrs = CG > 1 ? 2 : 1;
+    cfg.numAttrs = kCluster > 1 ? 2 : 1;
     std::call_once(once[p->device], [&] {
         int n = 0;
-        cfg.gridDim = dim3(p->sms / CG * CG);
+        cfg.gridDim = dim3(p->sms / kCluster * kCluster);
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) return;
-        if (CG == 1) n = p->sms;
+        if (kCluster == 1) n = p->sms;
         else if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) return;
-        clusters[p->device] = std::min(n, p->sms / CG);
+        clusters[p->device] = std::min(n, p->sms / kCluster);
     });
     if (clusters[p->device] <= 0) return ECQ_ERR_CUDA;
     if (!p->d_tasks[shape]) return ECQ_ERR_ARG;
     it.products = reinterpret_cast<const MuonProduct*>(p->d_tasks[shape]);
     it.tasks = reinterpret_cast<const MuonTask*>(p->d_tasks[shape] + p->tasks_at[shape]);
     it.n_tasks = p->n_tasks[shape];
-    cfg.gridDim = dim3((uint32_t)std::min<uint64_t>(p->n_full[shape], clusters[p->device]) * CG);
+    cfg.gridDim = dim3((uint32_t)std::min<uint64_t>(p->n_full[shape], clusters[p->device]) * kCluster);
     cfg.stream = st;
     if (cudaLaunchKernelEx(&cfg, kern, it) != cudaSuccess) {
         cudaGetLastError();
@@ -351,6 +364,18 @@ int choose_tiles(const ecq_muon* p, bool split) {
     return ECQ_MUON_TILES_128X64;
 }
 
+// Whether two CTAs share the K of a tile of 128 x 64: where the symmetric products have no more tiles
+// than there are pairs, and the products are long enough, counted in steps of 64 along K.  In us, one
+// CTA a tile and two (22-bit operands: three times the work a step):
+//     22 bits  96 x 160  (2.3 steps) 90 97     1024 x 1024 (16) 228 193   1000 x 2048 (20) 301 250
+//              2497 x 85 (15) 186 136          1537 x 611 (13) 217 181, three of them (90 tiles) 264 284
+//     11 bits  64 x 1024 (6) 82 94   512 x 2048 (12) 144 147   128 x 4096 (23) 150 120
+//              1024 x 1024 (16, but 128 tiles in every third product) 148 155
+bool share_along_k(const ecq_muon* p, bool split) {
+    return p->n_sym * 2 <= (uint64_t)p->sms && (split || p->n_full[3] * 2 <= (uint64_t)p->sms) &&
+           p->k_steps >= (split ? 5u : 16u) * p->chain;
+}
+
 // Index in kShapes of a tile choice.
 int shape_of(int tiles, bool split) {
     if (split) return tiles == ECQ_MUON_TILES_256X256 ? 1 : 3;
@@ -387,10 +412,14 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
     m.out_dtype = out_dtype;
     m.wait_limit = p->wait_limit;
     const int shape = shape_of(choose_tiles(p, terms == 3), terms == 3);
-    if (terms == 3) return shape == 1 ? launch_iterate<2, 128, true>(p, m, shape, st) : launch_iterate<1, 64, true>(p, m, shape, st);
-    return shape == 0   ? launch_iterate<2, 256, false>(p, m, shape, st)
-           : shape == 2 ? launch_iterate<1, 128, false>(p, m, shape, st)
-                        : launch_iterate<1, 64, false>(p, m, shape, st);
+    const bool joint = shape == 3 && share_along_k(p, terms == 3);
+    if (terms == 3) {
+        if (shape == 1) return launch_iterate<2, 128, true>(p, m, shape, st);
+        return joint ? launch_iterate<1, 64, true, true>(p, m, shape, st) : launch_iterate<1, 64, true>(p, m, shape, st);
+    }
+    if (shape == 0) return launch_iterate<2, 256, false>(p, m, shape, st);
+    if (shape == 2) return launch_iterate<1, 128, false>(p, m, shape, st);
+    return joint ? launch_iterate<1, 64, false, true>(p, m, shape, st) : launch_iterate<1, 64, false>(p, m, shape, st);
 }
 
 bool finite(float x) { return x - x == 0.f; }
@@ -407,6 +436,7 @@ int build_tasks(ecq_muon* p) {
         if (all > 0x10000000ull) return ECQ_ERR_ARG;
         list.tasks.reserve(all);
         list.build();
+        if (shape == 3) list.measure(p->n_sym, p->k_steps, p->chain);
         const uint64_t products = (list.products.size() * sizeof(MuonProduct) + 255) / 256 * 256;
         unsigned char* to = nullptr;
         if (cudaMalloc(&to, products + list.tasks.size() * sizeof(MuonTask)) != cudaSuccess) {

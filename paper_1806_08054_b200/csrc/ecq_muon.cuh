@@ -399,11 +399,20 @@ __device__ __forceinline__ uint32_t cta_rank() {
 __device__ __forceinline__ void pair_sync() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
-// The same shared-memory location in the pair's first CTA.
+// The same shared-memory location in another CTA of the cluster; in its first.
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t cta) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(cta));
+    return a;
+}
 __device__ __forceinline__ uint32_t leader_addr(uint32_t addr) {
     uint32_t a;
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(addr));
     return a;
+}
+// The same behind reads of this CTA's shared memory alone, whose values are there.
+__device__ __forceinline__ void leader_arrive_read(uint32_t leader_bar) {
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
 }
 __device__ __forceinline__ void leader_arrive(uint32_t leader_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
@@ -465,11 +474,18 @@ struct MuonIterate {
 constexpr uint32_t kMuonBox = 8192;                                   // 64 x 64 fp16
 constexpr uint32_t kMuonBlock = 2048;                                 // 32 x 32 fp16
 constexpr uint32_t kMuonQueue = 2;
+constexpr uint32_t kMuonShare = 128 * 32 * 4;                         // partial sums from one CTA to another
 constexpr uint32_t kMuonChunk = 4;                                    // 64-wide steps along K per partial sum (SPLIT)
 
 // CG CTAs work on one tile of CG * 128 rows and TN columns; each stages its 128 rows of the left
 // operand and TN / CG rows of the right one, 64 along K at a time, both halves of each with SPLIT.
-template <int CG, int TN, bool SPLIT>
+//
+// With KS two CTAs have half of a tile's K each, for matrices with few tiles and long products: an SM
+// takes 48 bytes a clock from L2, 2.1 us for 8 steps of 24 KB.  Each finishes 32 columns of the tile,
+// with the other's partial sums added that come through its shared memory; that takes about 0.9 us a
+// product.  (Four CTAs a tile were never faster: 2497 x 85 with 22 bits took 186 us with one, 147 with
+// two and 154 with four, 1000 x 2048 301, 264 and 460.)
+template <int CG, int TN, bool SPLIT, bool KS = false>
 struct MuonShape {
     static constexpr uint32_t kHalves = SPLIT ? 2 : 1;
     static constexpr uint32_t kBoxesA = 2, kBoxesB = TN / CG / 64;
@@ -478,14 +494,17 @@ struct MuonShape {
     static constexpr uint32_t kEpiWarps = 8;
     static constexpr uint32_t kCols = TN / (kEpiWarps / 4);           // columns of an epilogue warp
     static constexpr uint32_t kThreads = (kEpiWarps + 4) * 32;        // + two for loads, products, signals
-    static constexpr uint32_t kEpiBytes = kEpiWarps * 2 * kMuonBlock;
-    static constexpr uint32_t kStagesFit = (230u * 1024u - 2048u - kEpiBytes) / kStageBytes;
+    static constexpr uint32_t kFinish = KS ? 4 : kEpiWarps;           // of them, warps that finish results
+    static constexpr uint32_t kEpiBytes = kFinish * 2 * kMuonBlock;
+    static constexpr uint32_t kShareBytes = KS ? kMuonShare : 0;
+    static constexpr uint32_t kStagesFit = (230u * 1024u - 2048u - kEpiBytes - kShareBytes) / kStageBytes;
     static constexpr uint32_t kStages = kStagesFit < 6 ? kStagesFit : 6;
-    static constexpr uint32_t kSmem = kStages * kStageBytes + kEpiBytes + 1024;   // + alignment
+    static constexpr uint32_t kSmem = kStages * kStageBytes + kEpiBytes + kShareBytes + 1024;   // + alignment
     static constexpr uint32_t kAccCols = SPLIT ? 2 * TN : TN;         // hi hi, and the two small products
     static constexpr uint32_t kTmemCols = 2 * kAccCols;
-    // counts per tile on MuonIterate::done, arrivals on a queue slot
-    static constexpr uint32_t kParts = CG, kReaders = CG * (kEpiWarps + 3) + 1;
+    // counts per tile on MuonIterate::done
+    static constexpr uint32_t kParts = KS ? 2 : CG;
+    static_assert(!KS || (CG == 1 && TN == 64), "");
 };
 
 // Waits that give up: the limit is per wait, and one that ran out ends all others soon.
@@ -654,11 +673,20 @@ __device__ __forceinline__ bool elect_one() {
 // waits until the tiles that its operands come from are finished.  Those are earlier in the order,
 // so they have been taken by CTAs that are running: some tile can always go on, whatever number
 // of CTAs the GPU has room for.
-template <int CG, int TN, bool SPLIT>
-__global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_iterate_kernel(const __grid_constant__ MuonIterate P) {
-    using S = MuonShape<CG, TN, SPLIT>;
+//
+// What bounds it.  Large matrices (24 layers of 1024 x 1024 to 1024 x 4096, 6.4 to 6.7 ms, 2.36 at the
+// tensor cores' rate): operands and results through L2, 9.6 TB/s, with the tensor pipe busy 39 %
+// of the time, and the power cap.  Few tiles (1024 x 1024, 132 us): 15 products one after the other,
+// 8.5 us each: 0.7 for the first load, 4.2 for 16 steps of 24 KB at the 48 bytes a clock that an SM takes
+// from L2 (the products alone: 1.6), 1.5 for the results, 1 to make them visible, 0.5 to see that.
+// Smallest (96 x 160, 60 us): the same with 0.5 for the products.
+template <int CG, int TN, bool SPLIT, bool KS>
+__global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muon_iterate_kernel(const __grid_constant__ MuonIterate P) {
+    using S = MuonShape<CG, TN, SPLIT, KS>;
+    constexpr bool kJoint = CG == 2 || KS;                            // two CTAs work together
+    constexpr uint32_t ctas = kJoint ? 2 : 1;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 6 + 2 * kMuonQueue];
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 6 + 2 * kMuonQueue + (KS ? 8 : 0)];
     __shared__ uint32_t tmem_slot, queue[kMuonQueue];
     __shared__ volatile uint32_t stop;
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
@@ -666,22 +694,29 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages;
     const uint32_t acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 16;
     const uint32_t q_full = acc_empty + 16, q_empty = q_full + 8 * kMuonQueue, stored = q_empty + 8 * kMuonQueue;
-    const uint32_t rank = CG == 1 ? 0 : cta_rank();
+    // the other's partial sums, by warp: come, and read
+    const uint32_t share_full = stored + 16, share_empty = share_full + 32;
+    const uint32_t cta = kJoint ? cta_rank() : 0, rank = KS ? 0 : cta;   // rank: which rows of the tile
     const uint32_t limit = P.wait_limit;
+    // this CTA's steps along K
+    auto steps_from = [&](uint32_t kb) { return KS ? min(cta * ((kb + ctas - 1) / ctas), kb) : 0; };
+    auto steps_to = [&](uint32_t kb) { return KS ? min((cta + 1) * ((kb + ctas - 1) / ctas), kb) : kb; };
 
     if (tid == 0) {
         for (uint32_t s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 2); mbar_init(empty + 8 * s, 1); }
         for (uint32_t b = 0; b < 2; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, CG * S::kEpiWarps); }
-        for (uint32_t q = 0; q < kMuonQueue; ++q) { mbar_init(q_full + 8 * q, 1); mbar_init(q_empty + 8 * q, S::kReaders); }
-        mbar_init(stored, S::kEpiWarps);
-        mbar_init(stored + 8, S::kEpiWarps);
+        for (uint32_t q = 0; q < kMuonQueue; ++q) { mbar_init(q_full + 8 * q, 1); mbar_init(q_empty + 8 * q, ctas * (S::kEpiWarps + 3) + (KS ? ctas : 1)); }
+        mbar_init(stored, S::kFinish);
+        mbar_init(stored + 8, S::kFinish);
+        if (KS)
+            for (uint32_t i = 0; i < 8; ++i) mbar_init(share_full + 8 * i, 1);
         stop = 0;
         fence_mbar_init();
     }
     if (warp == S::kEpiWarps + 1) tmem_alloc<CG>(smem_u32(&tmem_slot), S::kTmemCols);
     tcgen05_before_sync();
     __syncthreads();
-    if (CG == 2) pair_sync();
+    if (kJoint) pair_sync();
     tcgen05_after_sync();
     const uint32_t tmem = tmem_slot;
     griddep_wait();
@@ -693,29 +728,30 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
     // n-th tile of this CTA (or pair); false when a wait ran out
     auto take = [&](uint32_t n, uint32_t& t) {
         const uint32_t q = n % kMuonQueue;
-        if (!(CG == 1 ? muon_wait(q_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)
+        if (!(!kJoint ? muon_wait(q_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)
                       : muon_wait_pair(q_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)))
             return false;
         t = *reinterpret_cast<volatile uint32_t*>(&queue[q]);
         return true;
     };
-    auto taken = [&](uint32_t n) {
+    // A release to the other CTA would wait for the results on their way to memory; nothing is handed
+    // over here but the slot, which has been read: the arrival's address depends on what was in it
+    // (numbers are below 2^31).  (Relaxed and without that, the read was moved behind the arrival.)
+    auto taken = [&](uint32_t n, uint32_t t) {
         const uint32_t bar = q_empty + 8 * (n % kMuonQueue);
-        if (CG == 1) mbar_arrive(bar);
-        else leader_arrive(leader_addr(bar));
+        if (!kJoint) mbar_arrive(bar);
+        else leader_arrive_read(leader_addr(bar + (t >> 31)));
     };
-    // the first CTA's load thread: hands tile t to all roles of both
+    // the first CTA's load thread: hands tile t to all roles of the cluster
     auto give = [&](uint32_t n, uint32_t t) {
         const uint32_t q = n % kMuonQueue;
         if (!muon_wait(q_empty + 8 * q, ((n / kMuonQueue) & 1) ^ 1, limit, &stop)) return false;
         *reinterpret_cast<volatile uint32_t*>(&queue[q]) = t;
         mbar_arrive(q_full + 8 * q);
-        if (CG == 2) {
-            uint32_t v, bar;
-            asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(v) : "r"(smem_u32(&queue[q])));
-            asm("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(bar) : "r"(q_full + 8 * q));
+        if (kJoint) {
+            const uint32_t v = peer_addr(smem_u32(&queue[q]), 1);
             asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(v), "r"(t) : "memory");
-            leader_arrive(bar);
+            leader_arrive(peer_addr(q_full + 8 * q, 1));
         }
         return true;
     };
@@ -727,7 +763,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
         // Each load thread of each CTA has part in every stage: one that had none could fall two
         // rounds of the ring behind, where the barriers' parities are the same again.
         if (elect_one()) {
-            const bool first = warp == S::kEpiWarps, giver = first && rank == 0;
+            const bool first = warp == S::kEpiWarps, giver = first && cta == 0;
             uint32_t it = 0, t = 0;
             bool ok = true;
             const uint32_t total = P.n_tasks;
@@ -741,7 +777,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 } else if (!take(n, t)) {
                     break;
                 }
-                taken(n);
+                taken(n, t);
                 if (t >= total) break;
                 const MuonTask task = P.tasks[t];
                 const MuonProduct& pr = P.products[task.product];
@@ -761,7 +797,8 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                                   (along_n ? col / 64 * down : col / 128);
                 }
                 if (!muon_wait_done(P.done + task.mat, (unsigned long long)S::kParts * task.need, limit, &stop, 0)) break;
-                for (uint32_t k = 0; k < kb; ++k, ++it) {
+                const uint32_t k1 = steps_to(kb);
+                for (uint32_t k = steps_from(kb); k < k1; ++k, ++it) {
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
                     if (!muon_wait(empty + 8 * s, ph ^ 1, limit, &stop)) { ok = false; break; }
                     const uint32_t bar = CG == 1 ? full + 8 * s : leader_addr(full + 8 * s);
@@ -771,7 +808,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
 #pragma unroll
                         for (uint32_t h = 0; h < S::kHalves; ++h)
                             muon_load<CG>(da + h * S::kBytesA, &P.rows128, 0, 8 * (from[h] + k * down), bar);
-                        if (giver && k + 1 == kb) claim = atomicAdd(P.next, 1ull);
+                        if (giver && k + 1 == k1) claim = atomicAdd(P.next, 1ull);
                     } else {
                         if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * S::kHalves * S::kBytesB);
 #pragma unroll
@@ -804,7 +841,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
             uint32_t it = 0, acc = 0, t;
             bool ok = true;
             for (uint32_t n = 0; ok && take(n, t); ++n) {
-                taken(n);
+                taken(n, t);
                 if (t >= P.n_tasks) break;
                 const MuonTask task = P.tasks[t];
                 const MuonProduct& pr = P.products[task.product];
@@ -820,7 +857,8 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 const uint32_t b_lead = along_n ? 128 : b_rows, b_step = along_n ? 1024 : 128;
                 const uint32_t b_k16 = along_n ? 256 : 2 * b_rows;
                 uint32_t in_chunk = 0, d = 0;
-                for (uint32_t k = 0; k < kb; ++k, ++it) {
+                const uint32_t k0 = steps_from(kb), k1 = steps_to(kb);
+                for (uint32_t k = k0; k < k1; ++k, ++it) {
                     if (in_chunk == 0) {
                         if (!muon_wait(acc_empty + 8 * (acc & 1), ((acc >> 1) & 1) ^ 1, limit, &stop)) { ok = false; break; }
                         d = tmem + (acc & 1) * S::kAccCols;
@@ -842,7 +880,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                         }
                     }
                     umma_commit<CG>(empty + 8 * s);
-                    if (++in_chunk == (SPLIT ? kMuonChunk : kb) || k + 1 == kb) {
+                    if (++in_chunk == (SPLIT ? kMuonChunk : k1 - k0) || k + 1 == k1) {
                         umma_commit<CG>(acc_full + 8 * (acc & 1));
                         in_chunk = 0;
                         ++acc;
@@ -858,7 +896,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
         if (lane == 0) {
             uint32_t t;
             for (uint32_t n = 0; take(n, t); ++n) {
-                taken(n);
+                taken(n, t);
                 if (t >= P.n_tasks) break;
                 const uint32_t mat = P.tasks[t].mat;
                 if (!muon_wait(stored + 8 * (n & 1), (n >> 1) & 1, limit, &stop)) break;
@@ -869,8 +907,11 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
         // ---- results -----------------------------------------------------------------------------
         // Every warp has 32 rows and kCols columns of a tile, taken in blocks of 32 x 32.  What a
         // block's results are added to is read ahead into registers.
-        const uint32_t quad = warp & 3, c0 = (warp >> 2) * S::kCols;
-        const uint32_t block = ring + S::kStages * S::kStageBytes + warp * 2 * kMuonBlock;
+        const uint32_t quad = warp & 3, half = KS ? (warp >> 2) ^ cta : warp >> 2, c0 = half * S::kCols;
+        const bool finish = !KS || warp < 4;
+        const uint32_t block = ring + S::kStages * S::kStageBytes + (finish ? warp : 0) * 2 * kMuonBlock;
+        // the other CTA's sums for this warp's rows: 16 bytes of 32 rows, then the next
+        const uint32_t share = ring + S::kStages * S::kStageBytes + S::kEpiBytes + quad * (kMuonShare / 4) + lane * 16;
         const uint32_t lane_addr = tmem + ((quad * 32u) << 16);
         constexpr uint32_t kBlocks = S::kCols / 32;
         const uint32_t own = block + lane * 64, flip = (lane >> 1) & 3;   // this lane's row in shared memory: piece c at own + ((c ^ flip) << 4)
@@ -878,7 +919,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
         bool ok = true;
         for (uint32_t n = 0; ok && __all_sync(~0u, take(n, t)); ++n) {
             __syncwarp();
-            if (lane == 0) taken(n);
+            if (lane == 0) taken(n, t);
             if (t >= P.n_tasks) break;
             const MuonTask task = P.tasks[t];
             const MuonProduct& pr = P.products[task.product];
@@ -910,20 +951,24 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 muon_get(place(buffers[in_at][0], b), in);
                 if (read_low) muon_get(place(buffers[in_at][1], b), low);
             };
-            if (!gram && blocks) {
+            if (!gram && blocks && finish) {
                 int go = 1;
                 if (lane == 0)
                     go = muon_wait_done(P.done + task.mat, (unsigned long long)S::kParts * task.need, limit, &stop, 100);
                 if (!__shfl_sync(~0u, go, 0)) break;
             }
-            if (!SPLIT) fetch(0);
+            if ((!SPLIT || S::kCols == 32) && finish) fetch(0);
+            uint32_t steps = 1;                                        // along K; without SPLIT, whether there is one
+            if (KS || SPLIT) {
+                const uint32_t kb = ((gram ? mat.n : m) + 63) / 64;
+                steps = steps_to(kb) - steps_from(kb);
+            }
 
             float sum[SPLIT ? S::kCols : 1];
             if (SPLIT) {
 #pragma unroll
                 for (uint32_t i = 0; i < S::kCols; ++i) sum[SPLIT ? i : 0] = 0.f;
-                const uint32_t kb = ((gram ? mat.n : m) + 63) / 64;
-                for (uint32_t chunk = 0; chunk < (kb + kMuonChunk - 1) / kMuonChunk; ++chunk, ++acc) {
+                for (uint32_t chunk = 0; chunk < (steps + kMuonChunk - 1) / kMuonChunk; ++chunk, ++acc) {
                     ok = __all_sync(~0u, muon_wait(acc_full + 8 * (acc & 1), (acc >> 1) & 1, limit, &stop));
                     if (!ok) break;
                     tcgen05_after_sync();
@@ -943,12 +988,54 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                         else leader_arrive(leader_addr(acc_empty + 8 * (acc & 1)));
                     }
                 }
-            } else {
+            } else if (steps) {
                 ok = __all_sync(~0u, muon_wait(acc_full + 8 * (acc & 1), (acc >> 1) & 1, limit, &stop));
                 tcgen05_after_sync();
             }
             if (!ok) break;
-            if (SPLIT) fetch(0);                                       // not before: the sums take the registers
+            if (SPLIT && S::kCols != 32) fetch(0);                     // not before: the sums take the registers
+            // this warp's block of the accumulators is read
+            auto release = [&] {
+                tcgen05_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 1) mbar_arrive(acc_empty + 8 * (acc & 1));
+                    else leader_arrive(leader_addr(acc_empty + 8 * (acc & 1)));
+                }
+                ++acc;
+            };
+            if (!finish) {
+                // to the CTA that finishes these columns; it has read the last tile's before
+                float y[32];
+                if (SPLIT) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) y[i] = sum[SPLIT ? i : 0];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) y[i] = 0.f;
+                    if (steps) {
+                        tmem_load32(lane_addr + (acc & 1) * S::kAccCols + c0, y);
+                        release();
+                    }
+                }
+                ok = __all_sync(~0u, muon_wait_pair(share_empty + 8 * quad, (n & 1) ^ 1, limit, &stop));
+                if (!ok) break;
+                const uint32_t to = peer_addr(share, half);
+                const uint32_t bar = peer_addr(share_full + 8 * quad, half);
+                if (lane == 0)
+                    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(kMuonShare / 4) : "memory");
+#pragma unroll
+                for (uint32_t c = 0; c < 8; ++c)
+                    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1,%2,%3,%4}, [%5];"
+                                 ::"r"(to + c * 512), "f"(y[4 * c]), "f"(y[4 * c + 1]), "f"(y[4 * c + 2]), "f"(y[4 * c + 3]), "r"(bar) : "memory");
+                continue;
+            }
+
+            if (KS) {
+                ok = __all_sync(~0u, muon_wait_pair(share_full + 8 * quad, n & 1, limit, &stop));
+                if (!ok) break;
+            }
+
 
             // a finished block, 32 columns of this lane's row
             auto result = [&](uint32_t b, float* y) {
@@ -956,8 +1043,21 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
                 if (SPLIT) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) y[i] = sum[SPLIT ? 32 * b + i : 0];
-                } else {
+                } else if (!KS || steps) {
                     tmem_load32(lane_addr + (acc & 1) * S::kAccCols + c0 + 32 * b, y);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) y[i] = 0.f;
+                }
+                if (KS) {
+#pragma unroll
+                    for (uint32_t c = 0; c < 8; ++c) {
+                        const uint4 w = lds16(share + c * 512);
+                        y[4 * c] = __fadd_rn(y[4 * c], __uint_as_float(w.x));
+                        y[4 * c + 1] = __fadd_rn(y[4 * c + 1], __uint_as_float(w.y));
+                        y[4 * c + 2] = __fadd_rn(y[4 * c + 2], __uint_as_float(w.z));
+                        y[4 * c + 3] = __fadd_rn(y[4 * c + 3], __uint_as_float(w.w));
+                    }
                 }
                 // pairs of columns in one operation each
                 const uint64_t mul2v = pack2(mul, mul);
@@ -1103,24 +1203,19 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT>::kThreads, 1) muon_it
 #pragma unroll 1
                 for (uint32_t b = 0; b < blocks; ++b) out_block(b);
             }
-            if (!SPLIT) {
-                tcgen05_before_sync();
-                __syncwarp();
-                if (lane == 0) {
-                    if (CG == 1) mbar_arrive(acc_empty + 8 * (acc & 1));
-                    else leader_arrive(leader_addr(acc_empty + 8 * (acc & 1)));
-                }
-                ++acc;
-            }
+            if (!SPLIT && steps) release();
             __syncwarp();
             // the signal warp does the rest; the barrier's last use, two tiles ago, is over first
             if (lane == 0 && muon_wait(stored + 8 * (n & 1), ((n >> 1) & 1) ^ 1, limit, &stop)) mbar_arrive(stored + 8 * (n & 1));
+            // and the other may send the next tile's sums: last, as this release waits for the results
+            // on their way to memory (before them: 1.2 us more a product)
+            if (KS && lane == 0) leader_arrive(peer_addr(share_empty + 8 * quad, cta ^ 1));
         }
     }
     __syncwarp();
     tcgen05_before_sync();
     __syncthreads();
-    if (CG == 2) pair_sync();
+    if (kJoint) pair_sync();
     tcgen05_after_sync();
     if (tid == 0 && stop) atomicOr(P.status, kStatusTimeout);
     if (warp == S::kEpiWarps + 1) tmem_free<CG>(tmem, S::kTmemCols);

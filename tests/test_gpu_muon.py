@@ -107,6 +107,21 @@ def test_sizes(rows, cols, tiles):
         plan.close()
 
 
+@pytest.mark.parametrize("shapes", [[(2497, 85)], [(40, 9001)], [(9001, 40)], [(128, 4096)], [(1000, 1333)], [(64, 7000)],
+                                    [(70, 5000), (5000, 130), (1, 9000), (129, 4100)]], ids=str)
+def test_few_tiles_and_long_products(shapes):
+    """Where two CTAs share the sums of a tile; for the smallest of them one of the two has nothing to add."""
+    for precision, dst, tol in ((ecq.ECQ_MUON_HALF, "bf16", HALF), (ecq.ECQ_MUON_SPLIT, "f32", SPLIT)):
+        plan = Plan(shapes, gap=3, precision=precision)
+        src = data(plan, 11)
+        first = check_orth(plan, src, dst, tol)
+        for _ in range(20):
+            again = torch.full_like(first, 5.0)
+            ecq.ecq_muon_orthogonalize(plan.h, src, again)
+            assert torch.equal(first, again)
+        plan.close()
+
+
 @pytest.mark.parametrize("tiles", list(TILES))
 def test_many_matrices_odd_offsets_and_strides(tiles):
     shapes = [(96, 160), (31, 700), (260, 130), (1, 50), (64, 64), (513, 300), (17, 17), (300, 513)]
