@@ -311,7 +311,9 @@ __global__ void __launch_bounds__(kMuonPrepThreads, 5) muon_prepare_kernel(const
         n = slot;
     }
     if (P.what == 0 || (P.what == 2 && n < P.n_spans)) muon_add_squares<T, MOM>(P, n, part);
-    else muon_make_x<T, MOM>(P, P.what == 2 ? n - P.n_spans : n, stage, factor);
+    // last tiles first: their entries are still in the L2 cache, and the products begin with the first
+    // (two lm layers, 201 MB: 613 -> 606 us)
+    else muon_make_x<T, MOM>(P, P.what == 2 ? n - P.n_spans : gridDim.x - 1 - n, stage, factor);
 }
 
 // ---- tensor-core products --------------------------------------------------------------------
