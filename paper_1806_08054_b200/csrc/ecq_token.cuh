@@ -534,7 +534,7 @@ __device__ __forceinline__ void token_grad(const TokenRow& r, const TokenBackwar
         float lp = __fmaf_rn(x[i], P.tau, -r.lse);
         const float p = ex2(__fmul_rn(lp, kLog2e));
         if (ENT) {
-            lp = fmaxf(lp, -1e30f);                                   // a masked entry: 0, not 0 * inf
+            lp = fmaxf(lp, -1e4f);                                    // where p is 0: 0, not 0 * inf, also for a large u
             x[i] = __fmul_rn(p, __fmaf_rn(r.u, lp, r.w));
         } else {
             x[i] = __fmul_rn(p, r.w);

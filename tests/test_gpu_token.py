@@ -325,6 +325,21 @@ def test_row_offsets_beyond_32_bits():
     assert torch.equal(d, want)
 
 
+@pytest.mark.parametrize("dtype", list(DT))
+def test_masked_entries_beside_a_large_entropy_derivative(dtype):
+    """Their gradient is 0, whatever the derivative: no 0 * inf."""
+    _, x, y = make(4, 3001, dtype, 3003)
+    x[:, 5:2000] = -math.inf
+    x[:, 2000] = torch.finfo(DT[dtype]).min
+    y[:] = 1
+    out = forward(x, y, 1.0, 0)
+    e = torch.tensor([1e8, -1e10, 1e20, -1e30], device="cuda")
+    d = torch.full_like(x, 5.0)
+    ecq.ecq_token_logprob_grad(x, y, out["lse"], out["entropy"], torch.ones(4, device="cuda"), e, d)
+    assert torch.all(d[:, 5:2001] == 0)
+    assert not torch.any(torch.isnan(d))
+
+
 def test_refusals():
     _, x, y = make(2, 64, "f32")
     lp = torch.zeros(2, device="cuda")
