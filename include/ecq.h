@@ -392,12 +392,14 @@ int ecq_token_logprob(const void* logits, int dtype, uint64_t rows, uint32_t voc
  * Backward pass of ecq_token_logprob: the gradient of a loss with respect to the logits from its
  * derivatives with respect to each row's logprob and entropy,
  *   d_logits_j = inv_temperature * (d_logprob * ([j == y] - p_j) - d_entropy * p_j (ln p_j + entropy))
- *   lse, entropy   as ecq_token_logprob wrote them (entropy may be NULL when d_entropy is)
+ *   lse, entropy   as ecq_token_logprob wrote them (entropy may be NULL when d_entropy is).  Where
+ *             |lse| is 128 or more (16-bit logits: 1024), or infinite, its rounding would show in the
+ *             probabilities, and the row's sum is taken anew from the logits.
  *   d_logprob [rows], with targets, or both NULL; d_entropy [rows] or NULL; not both NULL.
  *             Rows with a negative target have no part in d_logprob.
  *   d_logits  the logits' type, row r at entry r * d_row_stride; may be the logits themselves
  *             (same strides), must not overlap them otherwise
- * Masked entries get 0, as do rows whose lse is -inf; rows whose lse is NaN get NaN.
+ * Masked entries get 0, as do rows without open entries; rows whose lse is NaN get NaN.
  */
 int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_t vocab, uint64_t row_stride,
                            const int64_t* targets, float inv_temperature, const float* lse,

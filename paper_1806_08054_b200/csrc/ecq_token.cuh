@@ -508,9 +508,19 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprob_kernel(TokenForwa
 // For a loss L with g = dL/d log p_y and e = dL/dH of a row, log p_j = tau x_j - lse,
 //     dL/dx_j = tau (g [j = y] - p_j (g + e (log p_j + H))).
 // One read of the logits, one write of their gradient; lse and H come from the forward pass.
+//
+// lse is tau max x + ln s rounded to 32 bits: 2^-24 |lse| of it is lost, and p is off by that part of
+// itself.  A row of the lowest finite value, or one far from zero, loses all of ln s, and a row with
+// tau max x out of range has an lse of -inf or inf.  Where the loss could pass a sixteenth of what the
+// logits' type rounds to (for fp32: what the sums of the forward pass are off by), one CTA takes
+// the whole row, adds s up again and takes log p_j = tau (x_j - m) - ln s.  All rows of that kind: 8192 x
+// 50257 bf16 451 us against 266, 24 x 128001 42 against 8.  One CTA, because the row may be
+// overwritten in place; by few registers (no unrolling), as its call counts for the whole kernel (with 64
+// instead of 40 the ordinary rows take 301 us).
 
 constexpr int kTokGradThreads = 256;
 constexpr int kTokGradUnroll = 4;
+template <typename T> constexpr float kTokLargeLse = sizeof(T) == 4 ? 128.f : 1024.f;
 
 struct TokenBackward {
     const void* logits;
@@ -525,13 +535,14 @@ struct TokenBackward {
     float tau;
 };
 
-struct TokenRow { float lse, w, u, hit; uint32_t target; bool empty; };
+struct TokenRow { float m, lse, w, u, hit; uint32_t target; bool empty; };   // of x - m
 
-template <typename T, bool ENT, int N>
+// MAX: m is not 0.
+template <typename T, bool ENT, bool MAX, int N>
 __device__ __forceinline__ void token_grad(const TokenRow& r, const TokenBackward& P, uint32_t index, float* x) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        float lp = __fmaf_rn(x[i], P.tau, -r.lse);
+        float lp = __fmaf_rn(MAX ? __fsub_rn(x[i], r.m) : x[i], P.tau, -r.lse);
         const float p = ex2(__fmul_rn(lp, kLog2e));
         if (ENT) {
             lp = fmaxf(lp, -1e4f);                                    // where p is 0: 0, not 0 * inf, also for a large u
@@ -544,12 +555,91 @@ __device__ __forceinline__ void token_grad(const TokenRow& r, const TokenBackwar
     }
 }
 
+// What is known of a row whose lse is given relative to m.
+template <bool ENT>
+__device__ __forceinline__ TokenRow token_row(const TokenBackward& P, uint64_t row, float m, float lse) {
+    TokenRow r;
+    r.m = m;
+    r.lse = lse;
+    r.empty = lse == -INFINITY;
+    const int64_t y = P.targets ? P.targets[row] : -1;
+    const float g = P.d_logprob && y >= 0 ? P.d_logprob[row] : 0.f;
+    r.target = y >= 0 && y < (int64_t)P.vocab && !r.empty ? (uint32_t)y : 0xFFFFFFFFu;
+    r.hit = __fmul_rn(P.tau, g);
+    if (ENT) {
+        const float e = P.d_entropy[row];
+        r.u = -__fmul_rn(P.tau, e);
+        r.w = -__fmul_rn(P.tau, __fmaf_rn(e, P.entropy[row], g));
+    } else {
+        r.u = 0.f;
+        r.w = -r.hit;
+    }
+    if (lse != lse) r.w = lse;                                        // a row with a NaN gives NaN
+    return r;
+}
+
+// A whole row, with its sum taken anew.
 template <typename T, bool ENT>
-__global__ void __launch_bounds__(kTokGradThreads) token_logprob_grad_kernel(TokenBackward P) {
+__device__ __noinline__ void token_grad_large(const TokenBackward& P, uint64_t row) {
+    constexpr uint32_t E = Elem<T>::kPer16;
+    __shared__ TokenSums sums[kTokGradThreads / 32];
+    const uint32_t tid = threadIdx.x;
+    const T* in = reinterpret_cast<const T*>(P.logits) + row * P.row_stride;
+    T* out = reinterpret_cast<T*>(P.d_logits) + row * P.d_row_stride;
+    const uint32_t odd = (uint32_t)((16u - (reinterpret_cast<uintptr_t>(in) & 15u)) & 15u) / (uint32_t)sizeof(T);
+    const uint32_t head = odd < P.vocab ? odd : P.vocab;
+    const uint32_t nv = (P.vocab - head) / E;
+    const uint4* vin = reinterpret_cast<const uint4*>(in + head);
+    const float k = __fmul_rn(P.tau, kLog2e);
+    const uint32_t edge = tid < E ? tid : head + nv * E + (tid - E);  // this thread's single entry, if it has one
+    const bool has_edge = tid < 2 * E && (tid < E ? tid < head : edge < P.vocab);
+
+    TokenSums a = {-FLT_MAX, 0.f, 0.f};
+#pragma unroll 1
+    for (uint32_t v = tid; v < nv; v += kTokGradThreads) {
+        const uint4 raw = vin[v];
+        token_add<T, false, 1>(a, &raw, k);
+    }
+    if (has_edge) token_add<false>(a, Elem<T>::load(in + edge), k);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        token_merge(a, {__shfl_xor_sync(~0u, a.m, o), __shfl_xor_sync(~0u, a.s, o), 0.f}, k);
+    __syncthreads();                                                  // the row before has read its sums
+    if ((tid & 31) == 0) sums[tid >> 5] = a;
+    __syncthreads();
+    a = sums[0];
+#pragma unroll
+    for (int w = 1; w < kTokGradThreads / 32; ++w) token_merge(a, sums[w], k);
+
+    const TokenRow r = token_row<ENT>(P, row, a.m, logf(a.s));        // -inf for an empty row
+#pragma unroll 1
+    for (uint32_t v = tid; v < nv; v += kTokGradThreads) {
+        const uint32_t index = head + v * E;
+        float x[E];
+        Elem<T>::widen(vin[v], x);
+        token_grad<T, ENT, true, (int)E>(r, P, index, x);
+        if (((reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0) {
+            reinterpret_cast<uint4*>(out + head)[v] = Elem<T>::narrow(x);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < E; ++i) Elem<T>::store(out + index + i, x[i]);
+        }
+    }
+    if (has_edge) {
+        float x[1] = {Elem<T>::load(in + edge)};
+        token_grad<T, ENT, true, 1>(r, P, edge, x);
+        Elem<T>::store(out + edge, x[0]);
+    }
+}
+
+template <typename T, bool ENT>
+// (With fp32 the compiler would take 56 registers: 270 us for 4096 x 50257 against 242.)
+__global__ void __launch_bounds__(kTokGradThreads, sizeof(T) == 4 ? 6 : 0) token_logprob_grad_kernel(const __grid_constant__ TokenBackward P) {
     constexpr uint32_t E = Elem<T>::kPer16;
     constexpr uint32_t kChunk = kTokGradThreads * kTokGradUnroll;
     const uint32_t tid = threadIdx.x;
     const uint64_t tasks = P.rows * P.chunks;
+    bool large = false;                                               // a row is left for later
     for (uint64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
         const uint64_t row = task / P.chunks;
         const uint32_t chunk = (uint32_t)(task - row * P.chunks);
@@ -566,22 +656,11 @@ __global__ void __launch_bounds__(kTokGradThreads) token_logprob_grad_kernel(Tok
         for (int u = 0; u < kTokGradUnroll; ++u)
             if (v0 + u * kTokGradThreads < nv) raw[u] = vin[v0 + u * kTokGradThreads];
 
-        TokenRow r;
-        r.lse = P.lse[row];
-        r.empty = r.lse == -INFINITY;
-        const int64_t y = P.targets ? P.targets[row] : -1;
-        const float g = P.d_logprob && y >= 0 ? P.d_logprob[row] : 0.f;
-        r.target = y >= 0 && y < (int64_t)P.vocab && !r.empty ? (uint32_t)y : 0xFFFFFFFFu;
-        r.hit = __fmul_rn(P.tau, g);
-        if (ENT) {
-            const float e = P.d_entropy[row];
-            r.u = -__fmul_rn(P.tau, e);
-            r.w = -__fmul_rn(P.tau, __fmaf_rn(e, P.entropy[row], g));
-        } else {
-            r.u = 0.f;
-            r.w = -r.hit;
+        const TokenRow r = token_row<ENT>(P, row, 0.f, P.lse[row]);
+        if (fabsf(r.lse) >= kTokLargeLse<T>) {                        // not for NaN
+            large |= chunk == 0;
+            continue;
         }
-        if (r.lse != r.lse) r.w = r.lse;                              // a row with a NaN gives NaN
 
 #pragma unroll
         for (int u = 0; u < kTokGradUnroll; ++u) {
@@ -590,7 +669,7 @@ __global__ void __launch_bounds__(kTokGradThreads) token_logprob_grad_kernel(Tok
             const uint32_t index = head + v * E;
             float x[E];
             Elem<T>::widen(raw[u], x);
-            token_grad<T, ENT, (int)E>(r, P, index, x);
+            token_grad<T, ENT, false, (int)E>(r, P, index, x);
             if (same) {
                 reinterpret_cast<uint4*>(out + head)[v] = Elem<T>::narrow(x);
             } else {
@@ -602,11 +681,16 @@ __global__ void __launch_bounds__(kTokGradThreads) token_logprob_grad_kernel(Tok
             const uint32_t j = tid < E ? tid : head + nv * E + (tid - E);
             if (tid < E ? tid < head : j < P.vocab) {
                 float x[1] = {Elem<T>::load(in + j)};
-                token_grad<T, ENT, 1>(r, P, j, x);
+                token_grad<T, ENT, false, 1>(r, P, j, x);
                 Elem<T>::store(out + j, x[0]);
             }
         }
     }
+    // behind the loop, where nothing is held in registers across the call
+    if (large)
+        for (uint64_t task = blockIdx.x; task < tasks; task += gridDim.x)
+            if (task % P.chunks == 0 && fabsf(P.lse[task / P.chunks]) >= kTokLargeLse<T>)
+                token_grad_large<T, ENT>(P, task / P.chunks);
 }
 
 }  // namespace ecq

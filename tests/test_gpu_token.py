@@ -258,6 +258,73 @@ def test_backward(rows, vocab, dtype):
         assert torch.equal(check_grad(x, y, temperature, ent, in_place=True), d)
 
 
+def uncentred(rows, vocab, dtype, stride, seed, offset):
+    """Rows whose lse alone does not tell the probabilities: every entry (or all but a few) at the
+    type's lowest value, entries far from zero, entries at the highest value; and rows without open entries."""
+    buf, x, y = make(rows, vocab, dtype, stride, seed=seed, offset=offset)
+    info = torch.finfo(DT[dtype])
+    far = 30000.0 if dtype == "f16" else 1e5                # entries a rounding of the type apart
+    x[0] = info.min
+    x[1] = info.min; x[1, vocab // 2:] = -math.inf
+    x[2] += far
+    x[3] -= far
+    x[4] = info.max; x[4, ::3] = info.min
+    x[5] = -math.inf
+    x[6] = 8 * x[6] + 500.0
+    y[:7] = torch.tensor([0, 1, 2, vocab - 1, 1, 3, -1], device="cuda")[:7] % vocab
+    y[6] = -1
+    return buf, x, y
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("vocab,offset", [(8, 0), (301, 1), (1000, 0), (9001, 3), (50257, 1), (131075, 0)])
+def test_backward_of_uncentred_rows(vocab, offset, dtype):
+    """Against the definition in 64 bits.  p has the error of the sums (1e-5) and three roundings of
+    tau (x - m), which is at most 104 where p is not 0: 2e-5 + 8 * 2^-24 * 104 of p, and the entropy's."""
+    for temperature, ent in ((1.0, True), (0.5, True), (2.0, False)):
+        tau = 1.0 / temperature
+        _, x, y = uncentred(9, vocab, dtype, vocab + 1, 5, offset)
+        out = forward(x, y, temperature, 0)
+        g = torch.randn(9, device="cuda")
+        e = torch.randn(9, device="cuda") if ent else None
+        z = x.double() * tau
+        z[5] = 0                                            # the empty row, set right below
+        z -= z.max(1, keepdim=True).values                  # not less lse: 64 bits lose ln V beside 3e38, too
+        logp = z - z.exp().sum(1, keepdim=True).log()
+        p = logp.exp()
+        plogp = torch.where(p > 0, p * logp, 0.0)
+        H = -plogp.sum(1)
+        hot = torch.zeros_like(z).scatter_(1, y.clamp(min=0)[:, None], (y >= 0).double()[:, None])
+        gd = torch.where(y >= 0, g.double(), 0.0)[:, None]
+        ref, size = gd * (hot - p), gd.abs() * (hot + p)
+        if ent:
+            ref = ref - e.double()[:, None] * (plogp + p * H[:, None])
+            size = size + e.double().abs()[:, None] * (plogp.abs() + p * (1 + H[:, None]))
+        ref, size = ref * tau, size * tau
+        ref[5] = 0; size[5] = 0
+        store = {torch.float32: 0.0, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -10}[x.dtype]
+        allow = (2e-5 + 8 * EPS * 104) * size + store * ref.abs() + 2.0 ** -24
+        d = torch.full_like(x, 3.0)
+        ecq.ecq_token_logprob_grad(x, y, out["lse"], out["entropy"] if ent else None, g, e, d, temperature=temperature)
+        assert torch.all((d.double() - ref).abs() <= allow)
+        other = make(9, vocab, dtype, vocab + 2, offset=2)[1]                  # another alignment
+        ecq.ecq_token_logprob_grad(x, y, out["lse"], out["entropy"] if ent else None, g, e, other, temperature=temperature)
+        assert torch.equal(other, d)
+        ecq.ecq_token_logprob_grad(x, y, out["lse"], out["entropy"] if ent else None, g, e, x, temperature=temperature)
+        assert torch.equal(x, d)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_backward_of_rows_around_the_limits_of_lse(dtype):
+    """|lse| on either side of 128 and of 1024, and rows beyond them among many others."""
+    _, x, y = make(400, 8191, dtype, 8200)
+    x[:200] += torch.linspace(100, 140, 200, device="cuda")[:, None]
+    x[200:] -= torch.linspace(1000, 1060, 200, device="cuda")[:, None]
+    x[::7] = make(400, 8191, dtype, seed=9)[1][::7]
+    check_grad(x, y, 1.0, True)
+    check_grad(x, y, 1.0, False, in_place=True)
+
+
 def test_backward_against_differences():
     """(L(x + h v) - L(x - h v)) / 2h of L = sum g log p + e H.  With h = 1e-2 the third-order term is
     about h^2 of the result and the rounding of L about 1e-6 |L| / h: 1e-3 of |v| together."""
