@@ -399,7 +399,8 @@ int ecq_token_logprob(const void* logits, int dtype, uint64_t rows, uint32_t voc
  *             Rows with a negative target have no part in d_logprob.
  *   d_logits  the logits' type, row r at entry r * d_row_stride; may be the logits themselves
  *             (same strides), must not overlap them otherwise
- * Masked entries get 0, as do rows without open entries; rows whose lse is NaN get NaN.
+ * Masked entries get 0, as do rows without open entries; rows whose lse is NaN, or whose target is
+ * vocab or more, get NaN.
  */
 int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_t vocab, uint64_t row_stride,
                            const int64_t* targets, float inv_temperature, const float* lse,

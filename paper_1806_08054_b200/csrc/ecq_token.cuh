@@ -559,10 +559,11 @@ __device__ __forceinline__ void token_grad(const TokenRow& r, const TokenBackwar
 template <bool ENT>
 __device__ __forceinline__ TokenRow token_row(const TokenBackward& P, uint64_t row, float m, float lse) {
     TokenRow r;
+    const int64_t y = P.targets ? P.targets[row] : -1;
+    if (y >= (int64_t)P.vocab) lse = NAN;                             // as its log probability
     r.m = m;
     r.lse = lse;
     r.empty = lse == -INFINITY;
-    const int64_t y = P.targets ? P.targets[row] : -1;
     const float g = P.d_logprob && y >= 0 ? P.d_logprob[row] : 0.f;
     r.target = y >= 0 && y < (int64_t)P.vocab && !r.empty ? (uint32_t)y : 0xFFFFFFFFu;
     r.hit = __fmul_rn(P.tau, g);

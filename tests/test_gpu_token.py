@@ -186,6 +186,22 @@ def test_target_outside_the_vocabulary():
 
 
 @pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("ent", [False, True])
+def test_backward_of_a_target_outside_the_vocabulary(dtype, ent):
+    """NaN, as its log probability: not a gradient without the target's entry."""
+    _, x, y = make(6, 2001, dtype, 2002)
+    x[2] += 5000.0
+    x[3] = -math.inf
+    x[4, 7:] = -math.inf
+    y[:] = torch.tensor([2001, -1, 1 << 40, 2001, 5000, 2000], device="cuda")
+    out = forward(x, y, 1.0, 0)
+    assert torch.equal(torch.isnan(out["logprob"]).cpu(), torch.tensor([True, False, True, True, True, False]))
+    d, g = torch.full_like(x, 5.0), torch.ones(6, device="cuda")
+    ecq.ecq_token_logprob_grad(x, y, out["lse"], out["entropy"] if ent else None, g, g if ent else None, d)
+    assert torch.all(torch.isnan(d[[0, 2, 3, 4]])) and torch.all(torch.isfinite(d[[1, 5]]))
+
+
+@pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("rows,vocab", [(2, 600), (1, 50257), (200, 9001), (2, 131075)])
 def test_ties_go_to_the_lowest_index(rows, vocab, dtype):
     """Equal rows, few distinct values, signed zeros, a long run of large entries in one place."""
