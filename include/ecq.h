@@ -371,7 +371,7 @@ int ecq_step_static(uint64_t d, uint32_t bucket, uint32_t levels, float alpha, f
  *             entry r * row_stride (>= vocab); aligned to one element only
  *   targets   [rows] or NULL (exactly when logprob is NULL).  A negative target is padding:
  *             logprob 0.  A target >= vocab: logprob NaN.
- *   inv_temperature   > 0, finite
+ *   inv_temperature   > 0, at most 2.3e38 (its product with log2(e) is finite)
  *   top       0..min(vocab, ECQ_TOKEN_MAX_TOP); top_logprob and top_index are [rows * top],
  *             NULL exactly when top is 0
  *   logprob, entropy, lse   [rows] each or NULL, at least one output in all

@@ -1,4 +1,5 @@
 // C ABI of the token log-probability operators: argument checks and launches.
+#include <cfloat>
 #include <cstdint>
 
 #include <cuda_runtime.h>
@@ -49,7 +50,8 @@ int launch_backward(const TokenBackward& P, cudaStream_t st) {
     return ECQ_OK;
 }
 
-bool positive(float x) { return x > 0.f && x <= 3.402823466e38f; }
+// The kernels take it times log2(e).
+bool positive(float x) { return x > 0.f && x * kLog2e <= FLT_MAX; }
 
 bool bad_logits(const void* logits, int dtype, uint64_t rows, uint32_t vocab, uint64_t stride) {
     const uint32_t es = dtype_bytes(dtype);

@@ -38,6 +38,11 @@ def test_logprob_grad_refuses(bad):
     assert grad(**bad) == ecq.ECQ_ERR_ARG
 
 
+@pytest.mark.parametrize("tau", [2.4e38, 3.4e38])
+def test_a_temperature_beyond_the_range_of_its_powers_of_two_is_refused(tau):
+    assert logprob(tau=tau) == ecq.ECQ_ERR_ARG and grad(tau=tau) == ecq.ECQ_ERR_ARG
+
+
 def test_no_rows_is_nothing_to_do():
     assert logprob(rows=0) == ecq.ECQ_OK and grad(rows=0) == ecq.ECQ_OK
     assert logprob(rows=0, dtype=9) == ecq.ECQ_ERR_ARG
