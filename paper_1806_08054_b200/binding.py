@@ -438,6 +438,8 @@ def _rows(t: torch.Tensor, name: str):
     if dtype is None or len(shape) != 2 or (shape[1] > 1 and stride[1] != 1):
         raise ValueError("%s must be float32, bfloat16 or float16 of two dimensions, the last one contiguous" % name)
     rows, cols = shape
+    if cols > 0xFFFFFFFF:                                   # ctypes would pass its low 32 bits
+        raise ValueError("%s must have less than 2^32 columns" % name)
     return t.data_ptr(), dtype, rows, cols, stride[0] if rows > 1 else max(stride[0], cols)
 
 
@@ -498,6 +500,9 @@ def ecq_muon_create(offsets: Sequence[int], rows: Sequence[int], cols: Sequence[
         raise ValueError("offsets, rows, cols, strides and scales must have one entry per matrix")
     if min([*offsets, *rows, *cols, *(strides or [0])], default=0) < 0:
         raise ValueError("offsets, rows, cols and strides must not be negative")
+    # ctypes would pass the low bits
+    if max([*rows, *cols, steps], default=0) >> 32 or max([*offsets, *(strides or [0])], default=0) >> 64:
+        raise ValueError("rows, cols and steps must be below 2^32, offsets and strides below 2^64")
     flat = None
     if coefficients is not None:
         flat = [float(x) for triple in coefficients for x in triple]

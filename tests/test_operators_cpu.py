@@ -92,3 +92,25 @@ def test_binding_refuses_before_the_library():
             ecq.ecq_muon_create(**args)
     with pytest.raises(ValueError):
         ecq.ecq_token_logprob(torch.zeros(2, 8), torch.zeros(2, dtype=torch.int64), torch.zeros(2))
+
+
+def test_binding_refuses_sizes_whose_low_bits_would_pass():
+    """ctypes passes a number modulo 2^32 or 2^64: 2^32 + 8 rows would be taken for 8."""
+    import torch
+    from unittest import mock
+    for bad in (dict(rows=[(1 << 32) + 8]), dict(cols=[(1 << 32) + 6]), dict(offsets=[1 << 64]), dict(strides=[(1 << 64) + 6]),
+                dict(steps=(1 << 32) + 5)):
+        args = dict(offsets=[0], rows=[8], cols=[6])
+        args.update(bad)
+        with mock.patch.object(binding.lib(), "ecq_muon_create", side_effect=AssertionError("reached the library")):
+            with pytest.raises(ValueError):
+                ecq.ecq_muon_create(**args)
+    wide = torch.zeros(1, dtype=torch.bfloat16).expand(1, (1 << 32) + 8)
+
+    class OnGpu:                                            # a CUDA tensor of that shape, as the binding sees it
+        is_cuda, dtype, shape = True, wide.dtype, wide.shape
+        stride = staticmethod(lambda: ((1 << 32) + 8, 1))
+        data_ptr = staticmethod(lambda: P)
+
+    with pytest.raises(ValueError):
+        binding._rows(OnGpu, "logits")
