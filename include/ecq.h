@@ -464,7 +464,8 @@ int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_
  * ecq_muon_step  params or update may be NULL, not both.  update is a flat vector of
  *                `update_dtype`.  0 <= mu <= 1; lr, decay >= 0.  The vectors must not overlap.
  * All vectors are 16-byte aligned, ECQ_ERR_ARG otherwise or before the plan is bound.  Two
- * launches where the matrices are few and small, else three.
+ * launches where the matrices are few and small, else three.  ECQ_ERR_CUDA if one of them fails: the
+ * momentum may be updated then, params are not; later calls are not affected.
  * ecq_muon_status  as ecq_status.
  */
 typedef struct ecq_muon ecq_muon;

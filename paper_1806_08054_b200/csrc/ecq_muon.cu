@@ -1,5 +1,6 @@
 // C ABI of the Newton-Schulz orthogonaliser: plan, tables, launches.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -53,6 +54,8 @@ struct ecq_muon {
     uint64_t k_steps, chain;             // steps of 64 along K of every product, and products, over all matrices
     uint64_t padded[2];                  // entries of all X with rows in whole 128s, in whole 256s
     unsigned char* workspace;            // the caller's, NULL until bound
+    uint64_t reset_bytes;                // from d_added on: what a call's first launches count in
+    bool unfinished;                     // the last call could not launch all of its kernels
 };
 
 namespace {
@@ -285,15 +288,11 @@ struct TaskList {
     }
 };
 
-template <int CG, int TN, bool SPLIT, bool KS = false>
-int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st) {
-    constexpr int kCluster = KS ? 2 : CG;
+template <int CG, int TN, bool SPLIT, bool KS>
+cudaLaunchConfig_t iterate_config(cudaLaunchAttribute (&at)[2]) {
+    constexpr uint32_t kCluster = KS ? 2 : CG;
     using S = MuonShape<CG, TN, SPLIT, KS>;
-    static std::once_flag once[kMaxDevices];
-    static int clusters[kMaxDevices];
-    auto kern = muon_iterate_kernel<CG, TN, SPLIT, KS>;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
@@ -304,28 +303,52 @@ int launch_iterate(const ecq_muon* p, MuonIterate it, int shape, cudaStream_t st
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.attrs = at;
     cfg.numAttrs = kCluster > 1 ? 2 : 1;
-    std::call_once(once[p->device], [&] {
-        int n = 0;
-        cfg.gridDim = dim3(p->sms / kCluster * kCluster);
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) return;
-        if (kCluster == 1) n = p->sms;
-        else if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) return;
-        clusters[p->device] = std::min(n, p->sms / kCluster);
-    });
-    if (clusters[p->device] <= 0) return ECQ_ERR_CUDA;
-    if (!p->d_tasks[shape]) return ECQ_ERR_ARG;
-    it.products = reinterpret_cast<const MuonProduct*>(p->d_tasks[shape]);
-    it.tasks = reinterpret_cast<const MuonTask*>(p->d_tasks[shape] + p->tasks_at[shape]);
-    it.n_tasks = p->n_tasks[shape];
-    cfg.gridDim = dim3((uint32_t)std::min<uint64_t>(p->n_full[shape], clusters[p->device]) * kCluster);
+    return cfg;
+}
+
+// Clusters of the kernel that the plan's device holds at a time, with the kernel's attributes set; 0
+// where one of the queries fails, which the next call asks again.
+template <int CG, int TN, bool SPLIT, bool KS>
+uint32_t iterate_clusters(const ecq_muon* p) {
+    constexpr int kCluster = KS ? 2 : CG;
+    static std::atomic<uint32_t> known[kMaxDevices];
+    uint32_t have = known[p->device].load(std::memory_order_acquire);
+    if (have) return have;
+    auto kern = muon_iterate_kernel<CG, TN, SPLIT, KS>;
+    cudaLaunchAttribute at[2] = {};
+    cudaLaunchConfig_t cfg = iterate_config<CG, TN, SPLIT, KS>(at);
+    cfg.gridDim = dim3(p->sms / kCluster * kCluster);
+    int n = p->sms;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess ||
+        (kCluster > 1 && cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess)) {
+        cudaGetLastError();
+        return 0;
+    }
+    have = (uint32_t)std::max(0, std::min(n, p->sms / kCluster));
+    known[p->device].store(have, std::memory_order_release);
+    return have;
+}
+
+template <int CG, int TN, bool SPLIT, bool KS>
+int launch_iterate(const ecq_muon* p, const MuonIterate& it, uint64_t clusters, cudaStream_t st) {
+    cudaLaunchAttribute at[2] = {};
+    cudaLaunchConfig_t cfg = iterate_config<CG, TN, SPLIT, KS>(at);
+    cfg.gridDim = dim3((uint32_t)clusters * (KS ? 2 : CG));
     cfg.stream = st;
-    if (cudaLaunchKernelEx(&cfg, kern, it) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, muon_iterate_kernel<CG, TN, SPLIT, KS>, it) != cudaSuccess) {
         cudaGetLastError();
         return ECQ_ERR_CUDA;
     }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return ECQ_OK;
 }
+
+struct IterateKernel {
+    uint32_t (*clusters)(const ecq_muon*);
+    int (*launch)(const ecq_muon*, const MuonIterate&, uint64_t, cudaStream_t);
+};
+template <int CG, int TN, bool SPLIT, bool KS = false>
+IterateKernel iterate_kernel() { return {iterate_clusters<CG, TN, SPLIT, KS>, launch_iterate<CG, TN, SPLIT, KS>}; }
 
 // The launches may be scheduled while what is ahead of them in the stream drains; they touch no
 // global memory before it has completed.
@@ -382,21 +405,48 @@ int shape_of(int tiles, bool split) {
     return tiles == ECQ_MUON_TILES_256X256 ? 0 : tiles == ECQ_MUON_TILES_128X128 ? 2 : 3;
 }
 
+IterateKernel choose_kernel(const ecq_muon* p, int shape, bool split) {
+    const bool joint = shape == 3 && share_along_k(p, split);
+    if (split) {
+        if (shape == 1) return iterate_kernel<2, 128, true>();
+        return joint ? iterate_kernel<1, 64, true, true>() : iterate_kernel<1, 64, true>();
+    }
+    if (shape == 0) return iterate_kernel<2, 256, false>();
+    if (shape == 2) return iterate_kernel<1, 128, false>();
+    return joint ? iterate_kernel<1, 64, false, true>() : iterate_kernel<1, 64, false>();
+}
+
 int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int out_dtype, cudaStream_t st) {
     const MuonWork ws = work_of(p);
-    const int terms = p->precision == ECQ_MUON_HALF ? 1
-                      : p->precision == ECQ_MUON_SPLIT ? 3
-                      : (out.params || out_dtype != ECQ_BF16) ? 3 : 1;
+    const bool split = p->precision == ECQ_MUON_SPLIT ||
+                       (p->precision == ECQ_MUON_AUTO && (out.params || out_dtype != ECQ_BF16));
+    const int shape = shape_of(choose_tiles(p, split), split);
+    // what can fail does so before the momentum is touched
+    const IterateKernel kernel = choose_kernel(p, shape, split);
+    const uint32_t clusters = kernel.clusters(p);
+    if (!clusters) return ECQ_ERR_CUDA;
+    if (!p->d_tasks[shape]) return ECQ_ERR_ARG;
+
+    // The first launches count in these, the last one sets them to zero again.  Where a call could not
+    // launch all of its kernels, the next one does.
+    if (p->unfinished && cudaMemsetAsync(p->d_added, 0, p->reset_bytes, st) != cudaSuccess) {
+        cudaGetLastError();
+        return ECQ_ERR_CUDA;
+    }
+    p->unfinished = true;
     const MuonPrepare pre = {p->d_spans, p->d_prep, p->d_mats, in, ws, p->d_partial, p->d_added, p->d_factor, p->d_prep_next,
                              p->d_sound, p->d_done, p->d_next, p->d_status, p->n_spans, p->wait_limit, 0};
-    const int rc = in.momentum              ? launch_prepare<float, true>(p, pre, st)
-                   : in_dtype == ECQ_F32    ? launch_prepare<float, false>(p, pre, st)
-                   : in_dtype == ECQ_BF16   ? launch_prepare<__nv_bfloat16, false>(p, pre, st)
-                                            : launch_prepare<__half, false>(p, pre, st);
+    int rc = in.momentum              ? launch_prepare<float, true>(p, pre, st)
+             : in_dtype == ECQ_F32    ? launch_prepare<float, false>(p, pre, st)
+             : in_dtype == ECQ_BF16   ? launch_prepare<__nv_bfloat16, false>(p, pre, st)
+                                      : launch_prepare<__half, false>(p, pre, st);
     if (rc != ECQ_OK) return rc;
 
     MuonIterate m = {};
     m.mats = p->d_mats;
+    m.products = reinterpret_cast<const MuonProduct*>(p->d_tasks[shape]);
+    m.tasks = reinterpret_cast<const MuonTask*>(p->d_tasks[shape] + p->tasks_at[shape]);
+    m.n_tasks = p->n_tasks[shape];
     m.rows128 = p->rows128;
     m.rows64 = p->rows64;
     m.sound = p->d_sound;
@@ -411,15 +461,9 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
     m.out = out;
     m.out_dtype = out_dtype;
     m.wait_limit = p->wait_limit;
-    const int shape = shape_of(choose_tiles(p, terms == 3), terms == 3);
-    const bool joint = shape == 3 && share_along_k(p, terms == 3);
-    if (terms == 3) {
-        if (shape == 1) return launch_iterate<2, 128, true>(p, m, shape, st);
-        return joint ? launch_iterate<1, 64, true, true>(p, m, shape, st) : launch_iterate<1, 64, true>(p, m, shape, st);
-    }
-    if (shape == 0) return launch_iterate<2, 256, false>(p, m, shape, st);
-    if (shape == 2) return launch_iterate<1, 128, false>(p, m, shape, st);
-    return joint ? launch_iterate<1, 64, false, true>(p, m, shape, st) : launch_iterate<1, 64, false>(p, m, shape, st);
+    rc = kernel.launch(p, m, std::min<uint64_t>(p->n_full[shape], clusters), st);
+    if (rc == ECQ_OK) p->unfinished = false;
+    return rc;
 }
 
 bool finite(float x) { return x - x == 0.f; }
@@ -542,6 +586,7 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
     p->d_status = reinterpret_cast<uint32_t*>(p->block + o_status);
     p->d_done = reinterpret_cast<unsigned long long*>(p->block + o_done);
     p->d_next = reinterpret_cast<unsigned long long*>(p->block + o_next);
+    p->reset_bytes = bytes - o_added;
     p->n_spans = (uint32_t)spans.size();
     p->n_prep = (uint32_t)prep.size();
     return build_tasks(p);
