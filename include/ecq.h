@@ -446,6 +446,8 @@ int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_
  *                fp32 arithmetic (a few 1e-6).
  *                ECQ_MUON_AUTO: HALF where a call's outputs are bf16 alone, else SPLIT.
  *   The plan holds its tables on the current device; ECQ_ERR_ALLOC / ECQ_ERR_CUDA if that fails.
+ *   That device has to be the current one in ecq_muon_orthogonalize, ecq_muon_step and
+ *   ecq_muon_status, ECQ_ERR_ARG otherwise.
  * ecq_muon_destroy  NULL is allowed.  Do not destroy a plan with work in flight.
  * ecq_muon_set_tiles  tile of the product kernel: 256 x 256 by pairs of CTAs (256 x 128 with
  *                ECQ_MUON_SPLIT), 128 x 128 (128 x 64 with it) or 128 x 64 by one (by two that share

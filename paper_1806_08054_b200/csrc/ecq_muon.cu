@@ -468,6 +468,12 @@ int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int
 
 bool finite(float x) { return x - x == 0.f; }
 
+// Whether the plan's device is the current one: its addresses and the stream are that one's.
+bool on_device(const ecq_muon* p) {
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == p->device;
+}
+
 // The tile lists that the plan's precision and tile choice need and that it does not have yet.
 int build_tasks(ecq_muon* p) {
     for (int split = 0; split < 2; ++split) {
@@ -655,18 +661,18 @@ uint64_t ecq_muon_workspace_bytes(const ecq_muon* p) { return p ? kMuonTileBytes
 
 int ecq_muon_bind(ecq_muon* p, void* workspace, uint64_t bytes, void* cuda_stream) {
     if (!p || !workspace || !aligned_to(workspace, 256) || bytes < kMuonTileBytes * workspace_tiles(p)) return ECQ_ERR_ARG;
-    if (cudaSetDevice(p->device) != cudaSuccess) return ECQ_ERR_CUDA;
-    p->workspace = static_cast<unsigned char*>(workspace);
-    if (!tensor_map(&p->rows128, workspace, workspace_tiles(p), 16) || !tensor_map(&p->rows64, workspace, workspace_tiles(p), 8)) {
-        p->workspace = nullptr;
-        return ECQ_ERR_CUDA;
-    }
-    return ECQ_OK;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(p->device) != cudaSuccess) return ECQ_ERR_CUDA;
+    const bool mapped = tensor_map(&p->rows128, workspace, workspace_tiles(p), 16) &&
+                        tensor_map(&p->rows64, workspace, workspace_tiles(p), 8);
+    p->workspace = mapped ? static_cast<unsigned char*>(workspace) : nullptr;
+    cudaSetDevice(dev);
+    return mapped ? ECQ_OK : ECQ_ERR_CUDA;
 }
 
 int ecq_muon_orthogonalize(ecq_muon* p, const void* in, int in_dtype, void* out, int out_dtype, void* cuda_stream) {
     if (!p || !p->workspace || !in || !out || !dtype_bytes(in_dtype) || !dtype_bytes(out_dtype) || !aligned_to(in, 16) ||
-        !aligned_to(out, 16) || (in == out && in_dtype != out_dtype))
+        !aligned_to(out, 16) || (in == out && in_dtype != out_dtype) || !on_device(p))
         return ECQ_ERR_ARG;
     const MuonIn i = {in, nullptr, 0.f, 0};
     const MuonOut o = {nullptr, out, 1.f, 0.f, 0};
@@ -683,7 +689,7 @@ int ecq_muon_step(ecq_muon* p, const float* grad, float* momentum, float mu, int
         update == static_cast<const void*>(grad) || update == momentum)
         return ECQ_ERR_ARG;
     if (!(mu >= 0.f && mu <= 1.f) || !(lr >= 0.f) || !(decay >= 0.f) || !finite(lr) || !finite(decay) ||
-        !finite(lr * decay) || (nesterov != 0 && nesterov != 1))
+        !finite(lr * decay) || (nesterov != 0 && nesterov != 1) || !on_device(p))
         return ECQ_ERR_ARG;
     const MuonIn i = {grad, momentum, mu, nesterov};
     const MuonOut o = {params, update, 1.f - lr * decay, lr, 1};
@@ -691,7 +697,7 @@ int ecq_muon_step(ecq_muon* p, const float* grad, float* momentum, float mu, int
 }
 
 int ecq_muon_status(ecq_muon* p, void* cuda_stream) {
-    if (!p) return ECQ_ERR_ARG;
+    if (!p || !on_device(p)) return ECQ_ERR_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (cudaMemcpyAsync(p->h_status, p->d_status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
         cudaMemsetAsync(p->d_status, 0, 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)

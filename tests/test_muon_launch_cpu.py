@@ -124,3 +124,20 @@ def test_a_reset_that_fails_is_tried_again(lib):
     assert p.step() == ECQ_ERR_CUDA and p.events() == []
     assert p.step() == ecq.ECQ_OK and p.events()[:2] == ["memset", "prepare"]
     p.close()
+
+
+def test_a_plan_stays_on_its_device(lib):
+    """Binding and tile choices leave the caller's device as it is; with another one than the plan's
+    current, calls are refused."""
+    lib.cudaSetDevice(3)
+    p = Plan(lib, *SMALL, bind=False)
+    lib.cudaSetDevice(1)
+    assert p.bind() == ecq.ECQ_OK and lib.fake_device() == 1
+    assert lib.ecq_muon_set_tiles(p.h, ecq.ECQ_MUON_TILES_128X128) == ecq.ECQ_OK and lib.fake_device() == 1
+    assert p.step() == ecq.ECQ_ERR_ARG
+    assert lib.ecq_muon_orthogonalize(p.h, P, 0, 2 * P, 0, None) == ecq.ECQ_ERR_ARG
+    assert lib.ecq_muon_status(p.h, None) == ecq.ECQ_ERR_ARG
+    assert p.events() == []
+    lib.cudaSetDevice(3)
+    assert p.step() == ecq.ECQ_OK and lib.ecq_muon_status(p.h, None) == ecq.ECQ_OK
+    p.close()
