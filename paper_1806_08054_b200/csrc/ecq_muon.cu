@@ -110,6 +110,30 @@ bool steps_in_range(const std::vector<Step>& steps) {
     return true;
 }
 
+// The last two steps work with D = G - I where that keeps what is stored small: its polynomial
+// (b + 2c) D + c D^2 is b G + c G^2 less (b + c) I, which is near zero for singular values near 1, and
+// -(b + c) I for those near 0.  Iterates that stay far below 1 get the larger numbers from it: rounding
+// errors that then cancel against a X, or numbers out of fp16's range.  So it is done where the
+// polynomial reaches no more than twice what b G + c G^2 does (0.98 times with the default
+// coefficients; 1 for coefficients that converge to 1), and 128.
+void choose_shifts(std::vector<Step>& steps) {
+    if (steps.size() <= 2) return;
+    for (size_t k = steps.size() - 2; k < steps.size(); ++k) {
+        double plain = 0.0, shifted = 0.0;
+        for (int i = 0; i <= 4096; ++i) {
+            double s = i / 4096.0;
+            for (size_t j = 0; j < k; ++j) {
+                const double g = s * s;
+                s = std::fabs(s * (steps[j].a + steps[j].b * g + steps[j].c * g * g));
+            }
+            const double b = steps[k].b, c = steps[k].c, g = s * s, d = g - 1.0;
+            plain = std::max(plain, std::fabs(b * g + c * g * g));
+            shifted = std::max(shifted, std::fabs((b + 2 * c) * d + c * d * d));
+        }
+        steps[k].shift = shifted <= 2 * plain && shifted <= 128.0 ? 1.f : 0.f;
+    }
+}
+
 // First steps of an iteration that may be merged: at most three, not among the last two, and only
 // while the polynomials stay in the range of their fp16 copies (R up to 200; G, B, S as in single
 // steps).
@@ -511,10 +535,10 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
         Step s = {3.4445f, -4.7750f, 2.0315f, 0.f};
         if (coefficients) s = {coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2], 0.f};
         if (!finite(s.a) || !finite(s.b) || !finite(s.c)) return ECQ_ERR_ARG;
-        if (k + 2 >= steps && steps > 2) s.shift = 1.f;
         p->steps.push_back(s);
     }
     if (!steps_in_range(p->steps)) return ECQ_ERR_ARG;
+    choose_shifts(p->steps);
     std::vector<MuonSpan> spans;
     std::vector<MuonTile> prep;
     for (uint32_t i = 0; i < count; ++i) {

@@ -35,7 +35,8 @@ namespace ecq {
 // nothing left to amplify, and X has no low half there (no difference measured).
 // In the last two steps, where most singular values are near 1, G is replaced by D = G - I
 // (exactly the same polynomial: b G + c G^2 = (b + c) I + (b + 2c) D + c D^2), so that the
-// rounding of G's diagonal does not cancel against a X: 5e-4 to 1.1e-3.
+// rounding of G's diagonal does not cancel against a X: 5e-4 to 1.1e-3.  (Not with coefficients whose
+// iterates stay far below 1, for which it would.)
 // With SPLIT, operands are pairs hi + lo of fp16 (22 bits), of which three products are taken
 // (hi hi, hi lo, lo hi), and the result's error is that of fp32 arithmetic.
 //

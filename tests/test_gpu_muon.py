@@ -183,6 +183,19 @@ def test_steps_and_coefficients():
         plan.close()
 
 
+@pytest.mark.parametrize("coefficients", [[(0.1, 0.0, 0.0), (1.0, 0.0, 0.0), (10.0, 5000.0, 0.0)],
+                                          [(0.1, 0.0, 0.0), (2.0, 0.0, 0.0), (3.0, 400.0, -300.0), (0.5, -0.02, 0.001)],
+                                          [(0.05, 0.0, 0.0), (1.0, 0.0, 0.0), (10.0, 100.0, 0.0)],
+                                          [(0.2, 0.0, 0.0), (1.0, 0.0, 0.0), (1.0, 60.0, 60.0)]], ids=str)
+def test_coefficients_whose_iterates_stay_small(coefficients):
+    """The last steps' polynomial is large only for singular values that do not occur: it is neither to
+    leave the range of the 16-bit copies nor to take their rounding to the result."""
+    for precision, tol in ((ecq.ECQ_MUON_HALF, HALF), (ecq.ECQ_MUON_SPLIT, SPLIT)):
+        plan = Plan([(90, 140), (300, 700)], steps=len(coefficients), coefficients=coefficients, precision=precision)
+        check_orth(plan, data(plan, 6), "f32", tol)
+        plan.close()
+
+
 def test_zero_matrix_and_nan_matrix():
     plan = Plan([(40, 50), (64, 64), (50, 40), (30, 30)], gap=3)
     grad, mom, par = data(plan, 1), data(plan, 2), data(plan, 3)
