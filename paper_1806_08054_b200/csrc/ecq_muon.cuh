@@ -958,7 +958,9 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                 int go = 1;
                 if (lane == 0)
                     go = muon_wait_done(P.done + task.mat, (unsigned long long)S::kParts * task.need, limit, &stop, 100);
-                if (!__shfl_sync(~0u, go, 0)) break;
+                go = __shfl_sync(~0u, go, 0);
+                __syncwarp();                                          // the shuffle alone orders no memory for the other lanes
+                if (!go) break;
             }
             if ((!SPLIT || S::kCols == 32) && finish) fetch(0);
             uint32_t steps = 1;                                        // along K; without SPLIT, whether there is one
