@@ -413,10 +413,6 @@ __device__ __forceinline__ uint32_t leader_addr(uint32_t addr) {
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(addr));
     return a;
 }
-// The same behind reads of this CTA's shared memory alone, whose values are there.
-__device__ __forceinline__ void leader_arrive_read(uint32_t leader_bar) {
-    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
-}
 __device__ __forceinline__ void leader_arrive(uint32_t leader_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
 }
@@ -689,14 +685,15 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
     constexpr bool kJoint = CG == 2 || KS;                            // two CTAs work together
     constexpr uint32_t ctas = kJoint ? 2 : 1;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 6 + 2 * kMuonQueue + (KS ? 8 : 0)];
-    __shared__ uint32_t tmem_slot, queue[kMuonQueue];
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 6 + 4 * kMuonQueue + (KS ? 8 : 0)];
+    __shared__ uint32_t tmem_slot, queue[kMuonQueue], passed[kMuonQueue];
     __shared__ volatile uint32_t stop;
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages;
     const uint32_t acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 16;
-    const uint32_t q_full = acc_empty + 16, q_empty = q_full + 8 * kMuonQueue, stored = q_empty + 8 * kMuonQueue;
+    const uint32_t q_full = acc_empty + 16, q_empty = q_full + 8 * kMuonQueue;
+    const uint32_t pass_full = q_empty + 8 * kMuonQueue, pass_empty = pass_full + 8 * kMuonQueue, stored = pass_empty + 8 * kMuonQueue;
     // the other's partial sums, by warp: come, and read
     const uint32_t share_full = stored + 16, share_empty = share_full + 32;
     const uint32_t cta = kJoint ? cta_rank() : 0, rank = KS ? 0 : cta;   // rank: which rows of the tile
@@ -708,7 +705,12 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
     if (tid == 0) {
         for (uint32_t s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 2); mbar_init(empty + 8 * s, 1); }
         for (uint32_t b = 0; b < 2; ++b) { mbar_init(acc_full + 8 * b, 1); mbar_init(acc_empty + 8 * b, CG * S::kEpiWarps); }
-        for (uint32_t q = 0; q < kMuonQueue; ++q) { mbar_init(q_full + 8 * q, 1); mbar_init(q_empty + 8 * q, ctas * (S::kEpiWarps + 3) + (KS ? ctas : 1)); }
+        for (uint32_t q = 0; q < kMuonQueue; ++q) {
+            mbar_init(q_full + 8 * q, 1);
+            mbar_init(q_empty + 8 * q, S::kEpiWarps + 2 + (rank == 0 ? 1 : 0));   // results, right operands, signals, products
+            mbar_init(pass_full + 8 * q, 1);
+            mbar_init(pass_empty + 8 * q, 1);
+        }
         mbar_init(stored, S::kFinish);
         mbar_init(stored + 8, S::kFinish);
         if (KS)
@@ -728,34 +730,39 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
         if (tid == 0) *P.prepare_next = 0;
     }
 
+    // Numbers of tiles go from the thread that loads left operands to the other roles of its CTA through
+    // `queue`; those of a second CTA are passed to that thread of it first.  So what crosses CTAs is
+    // released by threads that have written no results: a release to the other CTA would wait for
+    // those on their way to memory (all roles arriving at the first CTA: two lm layers 550 -> 561 us, 48 of 512 x
+    // 512 324 -> 340; this way 553 and 318).
+    //
     // n-th tile of this CTA (or pair); false when a wait ran out
     auto take = [&](uint32_t n, uint32_t& t) {
         const uint32_t q = n % kMuonQueue;
-        if (!(!kJoint ? muon_wait(q_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)
-                      : muon_wait_pair(q_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)))
-            return false;
+        if (!muon_wait(q_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)) return false;
         t = *reinterpret_cast<volatile uint32_t*>(&queue[q]);
         return true;
     };
-    // A release to the other CTA would wait for the results on their way to memory; nothing is handed
-    // over here but the slot, which has been read: the arrival's address depends on what was in it
-    // (numbers are below 2^31).  (Relaxed and without that, the read was moved behind the arrival.)
-    auto taken = [&](uint32_t n, uint32_t t) {
-        const uint32_t bar = q_empty + 8 * (n % kMuonQueue);
-        if (!kJoint) mbar_arrive(bar);
-        else leader_arrive_read(leader_addr(bar + (t >> 31)));
-    };
-    // the first CTA's load thread: hands tile t to all roles of the cluster
+    auto taken = [&](uint32_t n) { mbar_arrive(q_empty + 8 * (n % kMuonQueue)); };
     auto give = [&](uint32_t n, uint32_t t) {
         const uint32_t q = n % kMuonQueue;
         if (!muon_wait(q_empty + 8 * q, ((n / kMuonQueue) & 1) ^ 1, limit, &stop)) return false;
         *reinterpret_cast<volatile uint32_t*>(&queue[q]) = t;
         mbar_arrive(q_full + 8 * q);
-        if (kJoint) {
-            const uint32_t v = peer_addr(smem_u32(&queue[q]), 1);
-            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(v), "r"(t) : "memory");
-            leader_arrive(peer_addr(q_full + 8 * q, 1));
-        }
+        return true;
+    };
+    auto pass = [&](uint32_t n, uint32_t t) {                          // by the first CTA
+        const uint32_t q = n % kMuonQueue;
+        if (!muon_wait_pair(pass_empty + 8 * q, ((n / kMuonQueue) & 1) ^ 1, limit, &stop)) return false;
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_addr(smem_u32(&passed[q]), 1)), "r"(t) : "memory");
+        leader_arrive(peer_addr(pass_full + 8 * q, 1));
+        return true;
+    };
+    auto receive = [&](uint32_t n, uint32_t& t) {                      // by the second
+        const uint32_t q = n % kMuonQueue;
+        if (!muon_wait_pair(pass_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)) return false;
+        t = *reinterpret_cast<volatile uint32_t*>(&passed[q]);
+        leader_arrive(leader_addr(pass_empty + 8 * q));
         return true;
     };
 
@@ -776,11 +783,13 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
             for (uint32_t n = 0; ok; ++n) {
                 if (giver) {
                     t = (uint32_t)min(claim, (unsigned long long)total);
-                    if (!give(n, t)) break;
-                } else if (!take(n, t)) {
-                    break;
+                    if ((kJoint && !pass(n, t)) || !give(n, t)) break;
+                } else if (first) {
+                    if (!receive(n, t) || !give(n, t)) break;
+                } else {
+                    if (!take(n, t)) break;
+                    taken(n);
                 }
-                taken(n, t);
                 if (t >= total) break;
                 const MuonTask task = P.tasks[t];
                 const MuonProduct& pr = P.products[task.product];
@@ -844,7 +853,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
             uint32_t it = 0, acc = 0, t;
             bool ok = true;
             for (uint32_t n = 0; ok && take(n, t); ++n) {
-                taken(n, t);
+                taken(n);
                 if (t >= P.n_tasks) break;
                 const MuonTask task = P.tasks[t];
                 const MuonProduct& pr = P.products[task.product];
@@ -863,7 +872,9 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                 const uint32_t k0 = steps_from(kb), k1 = steps_to(kb);
                 for (uint32_t k = k0; k < k1; ++k, ++it) {
                     if (in_chunk == 0) {
-                        if (!muon_wait(acc_empty + 8 * (acc & 1), ((acc >> 1) & 1) ^ 1, limit, &stop)) { ok = false; break; }
+                        ok = CG == 1 ? muon_wait(acc_empty + 8 * (acc & 1), ((acc >> 1) & 1) ^ 1, limit, &stop)
+                                     : muon_wait_pair(acc_empty + 8 * (acc & 1), ((acc >> 1) & 1) ^ 1, limit, &stop);
+                        if (!ok) break;
                         d = tmem + (acc & 1) * S::kAccCols;
                     }
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
@@ -899,7 +910,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
         if (lane == 0) {
             uint32_t t;
             for (uint32_t n = 0; take(n, t); ++n) {
-                taken(n, t);
+                taken(n);
                 if (t >= P.n_tasks) break;
                 const uint32_t mat = P.tasks[t].mat;
                 if (!muon_wait(stored + 8 * (n & 1), (n >> 1) & 1, limit, &stop)) break;
@@ -922,7 +933,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
         bool ok = true;
         for (uint32_t n = 0; ok && __all_sync(~0u, take(n, t)); ++n) {
             __syncwarp();
-            if (lane == 0) taken(n, t);
+            if (lane == 0) taken(n);
             if (t >= P.n_tasks) break;
             const MuonTask task = P.tasks[t];
             const MuonProduct& pr = P.products[task.product];

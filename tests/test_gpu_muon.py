@@ -281,6 +281,25 @@ def test_repeatable_back_to_back_and_on_another_stream(tiles):
     plan.close()
 
 
+@pytest.mark.parametrize("tiles,precision", [(0, 1), (0, 2), (1, 1), (1, 2), (3, 1), (3, 2)])
+def test_many_tiles_of_many_sizes_over_and_over(tiles, precision):
+    """Numbers of tiles that two CTAs hand each other, with tiles that take from one step along K to dozens:
+    200 calls with the same bits."""
+    shapes = [(64, 147), (64, 64), (64, 576), (256, 64), (128, 1152), (512, 128), (256, 2304), (1024, 256), (85, 2497), (3, 4000),
+              (700, 700)]
+    plan = Plan(shapes, gap=1, tiles=tiles, precision=precision)
+    src = data(plan, 4)
+    first = torch.full_like(src, 5.0)
+    ecq.ecq_muon_orthogonalize(plan.h, src, first)
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(200):
+        again = torch.full_like(src, 5.0)
+        ecq.ecq_muon_orthogonalize(plan.h, src, again)
+        wrong += (again != first).sum()
+    assert wrong.item() == 0
+    plan.close()
+
+
 @pytest.mark.parametrize("tiles", list(TILES))
 def test_a_wait_that_runs_out_is_reported(tiles):
     plan = Plan([(300, 400)], tiles=TILES[tiles])
