@@ -1233,6 +1233,10 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
     __syncthreads();
     if (kJoint) pair_sync();
     tcgen05_after_sync();
+    // After a wait that ran out, partial sums and arrivals that this CTA did not wait for may still be on
+    // their way to it from the other one, which has issued its last by now: 20,000 clocks to land.
+    if (kJoint && stop)
+        for (const long long from = clock64(); clock64() - from < 20000;) {}
     if (tid == 0 && stop) atomicOr(P.status, kStatusTimeout);
     if (warp == S::kEpiWarps + 1) tmem_free<CG>(tmem, S::kTmemCols);
 }

@@ -313,6 +313,25 @@ def test_a_wait_that_runs_out_is_reported(tiles):
     plan.close()
 
 
+@pytest.mark.parametrize("shape,tiles", [((2497, 85), 0), ((300, 1000), 1), ((128, 4096), 0), ((300, 1000), 2)])
+def test_waits_that_run_out_in_the_middle_of_a_call(shape, tiles):
+    """Whatever was on its way then is let land: the call ends with a status, and the next is right."""
+    for precision in (ecq.ECQ_MUON_HALF, ecq.ECQ_MUON_SPLIT):
+        plan = Plan([shape], tiles=tiles, precision=precision)
+        src = data(plan, 1)
+        want, out = torch.empty_like(src), torch.empty_like(src)
+        ecq.ecq_muon_orthogonalize(plan.h, src, want)
+        for limit in (0, 1, 5, 30, 200, 1000):
+            ecq.ecq_muon_set_wait_limit(plan.h, limit)
+            ecq.ecq_muon_orthogonalize(plan.h, src, out)
+            status = ecq.ecq_muon_status(plan.h)
+            assert status in (ecq.ECQ_OK, ecq.ECQ_ERR_TIMEOUT) and (limit or status == ecq.ECQ_ERR_TIMEOUT)
+            ecq.ecq_muon_set_wait_limit(plan.h, ecq.ECQ_WAIT_LIMIT_DEFAULT)
+            ecq.ecq_muon_orthogonalize(plan.h, src, out)
+            assert torch.equal(out, want)
+        plan.close()
+
+
 def test_offsets_beyond_32_bits():
     first = (1 << 32) + 12345
     need = (first + 200 * 300) * 2
