@@ -441,7 +441,8 @@ int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_
  *   precision    ECQ_MUON_HALF: operands of the products rounded to 11 bits, X kept with 22; with
  *                the default coefficients the result is within about 1e-3 of exact (relative, the
  *                root of the sum of squares), 1e-2 where a few singular values carry all of U.
- *                bf16, for comparison, rounds by up to 4e-3.
+ *                bf16, for comparison, rounds by up to 4e-3.  At 262144 columns the sums' own
+ *                rounding has brought 1e-3 to 2e-3; plans with a longer matrix take SPLIT instead.
  *                ECQ_MUON_SPLIT: all operands with 22 bits, three times the products; the error of
  *                fp32 arithmetic (a few 1e-6).
  *                ECQ_MUON_AUTO: HALF where a call's outputs are bf16 alone, else SPLIT.

@@ -26,6 +26,13 @@ struct Shape { uint32_t cg, tn; };
 constexpr Shape kShapes[] = {{2, 256}, {2, 128}, {1, 128}, {1, 64}};
 constexpr int kShapeCount = 4;
 
+// With 11-bit operands a sum along K stays in one accumulator, whose rounding errors grow with its length:
+// 64 rows, by columns, error of the result with 11 and with 22 bits (sums of 256 terms):
+//     65536 1.2e-3 2.3e-6   262144 1.9e-3 2.2e-6   1048576 4.9e-3 2.2e-6   4194304 2.2e-2 2.2e-6
+// Plans with longer matrices than this take 22 bits for all: at 262144 columns, 64 rows 5.6 -> 6.1 ms, 1024 rows
+// 6.2 -> 11.6 ms.
+constexpr uint32_t kHalfLongest = 262144;
+
 uint64_t round64(uint64_t x) { return (x + 63) / 64 * 64; }
 
 }  // namespace
@@ -56,6 +63,7 @@ struct ecq_muon {
     unsigned char* workspace;            // the caller's, NULL until bound
     uint64_t reset_bytes;                // from d_added on: what a call's first launches count in
     bool unfinished;                     // the last call could not launch all of its kernels
+    bool long_sums;                      // a matrix has more than kHalfLongest columns
 };
 
 namespace {
@@ -442,7 +450,7 @@ IterateKernel choose_kernel(const ecq_muon* p, int shape, bool split) {
 
 int iterate(ecq_muon* p, const MuonIn& in, int in_dtype, const MuonOut& out, int out_dtype, cudaStream_t st) {
     const MuonWork ws = work_of(p);
-    const bool split = p->precision == ECQ_MUON_SPLIT ||
+    const bool split = p->precision == ECQ_MUON_SPLIT || p->long_sums ||
                        (p->precision == ECQ_MUON_AUTO && (out.params || out_dtype != ECQ_BF16));
     const int shape = shape_of(choose_tiles(p, split), split);
     // what can fail does so before the momentum is touched
@@ -501,7 +509,7 @@ bool on_device(const ecq_muon* p) {
 // The tile lists that the plan's precision and tile choice need and that it does not have yet.
 int build_tasks(ecq_muon* p) {
     for (int split = 0; split < 2; ++split) {
-        if (p->precision == (split ? ECQ_MUON_HALF : ECQ_MUON_SPLIT)) continue;
+        if (p->long_sums ? !split : p->precision == (split ? ECQ_MUON_HALF : ECQ_MUON_SPLIT)) continue;
         const int shape = shape_of(choose_tiles(p, split), split);
         if (p->d_tasks[shape]) continue;
         TaskList list(p->mats, kShapes[shape], p->steps);
@@ -552,6 +560,7 @@ int create(ecq_muon* p, uint32_t count, const uint64_t* offsets, const uint32_t*
             return ECQ_ERR_ARG;
         mat.tall = mat.rows > mat.cols;
         mat.m = std::min(mat.rows, mat.cols); mat.n = std::max(mat.rows, mat.cols);
+        p->long_sums |= mat.n > kHalfLongest;
         mat.pad = (uint32_t)round64(mat.m);
         mat.down = (mat.m + 127) / 128;
         mat.scale = scales ? scales[i] : 1.f;

@@ -281,6 +281,16 @@ def test_repeatable_back_to_back_and_on_another_stream(tiles):
     plan.close()
 
 
+@pytest.mark.parametrize("rows,cols", [(64, 200_001), (64, 1 << 20), (1 << 20, 50)])
+def test_very_long_sums(rows, cols):
+    """The rounding errors of long sums do not reach the result, whatever the operands' precision."""
+    for precision, tol in ((ecq.ECQ_MUON_HALF, HALF), (ecq.ECQ_MUON_SPLIT, SPLIT)):
+        plan = Plan([(rows, cols)], precision=precision)
+        src = data(plan, 7, kind="flat")
+        check_orth(plan, src, "f32", tol)
+        plan.close()
+
+
 @pytest.mark.parametrize("tiles,precision", [(0, 1), (0, 2), (1, 1), (1, 2), (3, 1), (3, 2)])
 def test_many_tiles_of_many_sizes_over_and_over(tiles, precision):
     """Numbers of tiles that two CTAs hand each other, with tiles that take from one step along K to dozens:
