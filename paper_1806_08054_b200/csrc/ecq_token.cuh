@@ -514,11 +514,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprob_kernel(TokenForwa
 // tau max x out of range has an lse of -inf or inf.  Where the loss could pass a sixteenth of what the
 // logits' type rounds to (for fp32: what the sums of the forward pass are off by), one CTA takes
 // the whole row, adds s up again and takes log p_j = tau (x_j - m) - ln s.  All rows of that kind: 8192 x
-// 50257 bf16 451 us against 266, 24 x 128001 42 against 8.  One CTA, because the row may be
+// 50257 bf16 445 us against 264, 24 x 128001 41 against 8.  One CTA, because the row may be
 // overwritten in place; by few registers (no unrolling), as its call counts for the whole kernel (with 64
 // instead of 40 the ordinary rows take 301 us).
 
 constexpr int kTokGradThreads = 256;
+constexpr uint32_t kTokNoTarget = 0xFFFFFFFFu;
 constexpr int kTokGradUnroll = 4;
 template <typename T> constexpr float kTokLargeLse = sizeof(T) == 4 ? 128.f : 1024.f;
 
@@ -537,9 +538,9 @@ struct TokenBackward {
 
 struct TokenRow { float m, lse, w, u, hit; uint32_t target; bool empty; };   // of x - m
 
-// MAX: m is not 0.
+// MAX: m is not 0.  The target's entry is set by token_grad_target.
 template <typename T, bool ENT, bool MAX, int N>
-__device__ __forceinline__ void token_grad(const TokenRow& r, const TokenBackward& P, uint32_t index, float* x) {
+__device__ __forceinline__ void token_grad(const TokenRow& r, const TokenBackward& P, float* x) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         float lp = __fmaf_rn(MAX ? __fsub_rn(x[i], r.m) : x[i], P.tau, -r.lse);
@@ -551,7 +552,6 @@ __device__ __forceinline__ void token_grad(const TokenRow& r, const TokenBackwar
             x[i] = __fmul_rn(p, r.w);
         }
         if (r.empty) x[i] = 0.f;
-        if (index + i == r.target) x[i] = __fadd_rn(x[i], r.hit);
     }
 }
 
@@ -565,7 +565,7 @@ __device__ __forceinline__ TokenRow token_row(const TokenBackward& P, uint64_t r
     r.lse = lse;
     r.empty = lse == -INFINITY;
     const float g = P.d_logprob && y >= 0 ? P.d_logprob[row] : 0.f;
-    r.target = y >= 0 && y < (int64_t)P.vocab && !r.empty ? (uint32_t)y : 0xFFFFFFFFu;
+    r.target = y >= 0 && y < (int64_t)P.vocab && !r.empty ? (uint32_t)y : kTokNoTarget;
     r.hit = __fmul_rn(P.tau, g);
     if (ENT) {
         const float e = P.d_entropy[row];
@@ -577,6 +577,22 @@ __device__ __forceinline__ TokenRow token_row(const TokenBackward& P, uint64_t r
     }
     if (lse != lse) r.w = lse;                                        // a row with a NaN gives NaN
     return r;
+}
+
+// The target's entry from its logit: tau (g (1 - p) - e p (log p + H)).  A token that the model is sure of
+// has p near 1, and all of its row's gradient is of the size of 1 - p: that is not to be a
+// difference of rounded numbers (ex2's error alone is 2^-22).  Not inlined, for its registers.
+template <typename T, bool ENT>
+__device__ __noinline__ void token_grad_target(const TokenBackward& P, uint64_t row, float m, float lse, float x) {
+    const uint64_t y = (uint64_t)P.targets[row];
+    const float lp = __fmaf_rn(__fsub_rn(x, m), P.tau, -lse);
+    const float g = P.d_logprob ? P.d_logprob[row] : 0.f;
+    float d = -__fmul_rn(__fmul_rn(P.tau, g), expm1f(lp));
+    if (ENT) {                                                        // the same as any entry's without g
+        const float e = P.d_entropy[row], w = -__fmul_rn(P.tau, __fmul_rn(e, P.entropy[row]));
+        d = __fadd_rn(d, __fmul_rn(ex2(__fmul_rn(lp, kLog2e)), __fmaf_rn(-__fmul_rn(P.tau, e), fmaxf(lp, -1e4f), w)));
+    }
+    Elem<T>::store(reinterpret_cast<T*>(P.d_logits) + row * P.d_row_stride + y, d);
 }
 
 // A whole row, with its sum taken anew.
@@ -613,29 +629,35 @@ __device__ __noinline__ void token_grad_large(const TokenBackward& P, uint64_t r
     for (int w = 1; w < kTokGradThreads / 32; ++w) token_merge(a, sums[w], k);
 
     const TokenRow r = token_row<ENT>(P, row, a.m, logf(a.s));        // -inf for an empty row
+    // the thread that has the target's vector or edge, which it alone overwrites
+    const uint32_t hit_v = (r.target - head) / E;
+    const bool owner = r.target != kTokNoTarget &&
+                       (r.target >= head && hit_v < nv ? hit_v % kTokGradThreads == tid : has_edge && edge == r.target);
+    const float hit_x = owner ? Elem<T>::load(in + r.target) : 0.f;
 #pragma unroll 1
     for (uint32_t v = tid; v < nv; v += kTokGradThreads) {
-        const uint32_t index = head + v * E;
         float x[E];
         Elem<T>::widen(vin[v], x);
-        token_grad<T, ENT, true, (int)E>(r, P, index, x);
+        token_grad<T, ENT, true, (int)E>(r, P, x);
         if (((reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0) {
             reinterpret_cast<uint4*>(out + head)[v] = Elem<T>::narrow(x);
         } else {
 #pragma unroll
-            for (uint32_t i = 0; i < E; ++i) Elem<T>::store(out + index + i, x[i]);
+            for (uint32_t i = 0; i < E; ++i) Elem<T>::store(out + head + v * E + i, x[i]);
         }
     }
     if (has_edge) {
         float x[1] = {Elem<T>::load(in + edge)};
-        token_grad<T, ENT, true, 1>(r, P, edge, x);
+        token_grad<T, ENT, true, 1>(r, P, x);
         Elem<T>::store(out + edge, x[0]);
     }
+    if (owner) token_grad_target<T, ENT>(P, row, r.m, r.lse, hit_x);
 }
 
 template <typename T, bool ENT>
-// (With fp32 the compiler would take 56 registers: 270 us for 4096 x 50257 against 242.)
-__global__ void __launch_bounds__(kTokGradThreads, sizeof(T) == 4 ? 6 : 0) token_logprob_grad_kernel(const __grid_constant__ TokenBackward P) {
+// (Left to itself the compiler takes 48 registers or more: 8192 x 50257 bf16 274 us against 264, 4096 x
+// 50257 fp32 270 against 242.)
+__global__ void __launch_bounds__(kTokGradThreads, 6) token_logprob_grad_kernel(const __grid_constant__ TokenBackward P) {
     constexpr uint32_t E = Elem<T>::kPer16;
     constexpr uint32_t kChunk = kTokGradThreads * kTokGradUnroll;
     const uint32_t tid = threadIdx.x;
@@ -662,30 +684,35 @@ __global__ void __launch_bounds__(kTokGradThreads, sizeof(T) == 4 ? 6 : 0) token
             large |= chunk == 0;
             continue;
         }
+        const uint32_t edge = tid < E ? tid : head + nv * E + (tid - E);
+        const bool has_edge = chunk == P.chunks - 1 && tid < 2 * E && (tid < E ? tid < head : edge < P.vocab);
+        // the thread that has the target's vector or edge, which it alone overwrites
+        const uint32_t hit_v = (r.target - head) / E;
+        const bool owner = r.target != kTokNoTarget &&
+                           (r.target >= head && hit_v < nv ? hit_v / kChunk == chunk && hit_v % kTokGradThreads == tid
+                                                           : has_edge && edge == r.target);
+        const float hit_x = owner ? Elem<T>::load(in + r.target) : 0.f;
 
 #pragma unroll
         for (int u = 0; u < kTokGradUnroll; ++u) {
             const uint32_t v = v0 + u * kTokGradThreads;
             if (v >= nv) break;
-            const uint32_t index = head + v * E;
             float x[E];
             Elem<T>::widen(raw[u], x);
-            token_grad<T, ENT, false, (int)E>(r, P, index, x);
+            token_grad<T, ENT, false, (int)E>(r, P, x);
             if (same) {
                 reinterpret_cast<uint4*>(out + head)[v] = Elem<T>::narrow(x);
             } else {
 #pragma unroll
-                for (uint32_t i = 0; i < E; ++i) Elem<T>::store(out + index + i, x[i]);
+                for (uint32_t i = 0; i < E; ++i) Elem<T>::store(out + head + v * E + i, x[i]);
             }
         }
-        if (chunk == P.chunks - 1 && tid < 2 * E) {
-            const uint32_t j = tid < E ? tid : head + nv * E + (tid - E);
-            if (tid < E ? tid < head : j < P.vocab) {
-                float x[1] = {Elem<T>::load(in + j)};
-                token_grad<T, ENT, false, 1>(r, P, j, x);
-                Elem<T>::store(out + j, x[0]);
-            }
+        if (has_edge) {
+            float x[1] = {Elem<T>::load(in + edge)};
+            token_grad<T, ENT, false, 1>(r, P, x);
+            Elem<T>::store(out + edge, x[0]);
         }
+        if (owner) token_grad_target<T, ENT>(P, row, 0.f, r.lse, hit_x);
     }
     // behind the loop, where nothing is held in registers across the call
     if (large)

@@ -274,6 +274,36 @@ def test_backward(rows, vocab, dtype):
         assert torch.equal(check_grad(x, y, temperature, ent, in_place=True), d)
 
 
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("vocab,offset", [(5, 0), (1003, 1), (1003, 6), (30001, 3)])
+def test_backward_at_a_token_that_is_nearly_certain(vocab, offset, dtype):
+    """g (1 - p) at the target, for p from 0.9 to within 1e-6 of 1, from a logit at which log p takes one
+    rounding: 16 * 2^-24 of itself.  lse is the definition's in 64 bits, near 0, rounded once: 2^-24 of
+    itself, and so of 1 - p."""
+    rows = 64
+    _, x, y = make(rows, vocab, dtype, vocab + 1, offset=offset)
+    x.copy_(-3.0 - math.log(vocab) - torch.arange(rows, device="cuda")[:, None] / 6 + 0.2 * x)
+    x.scatter_(1, y[:, None], 0.0)
+    z = x.double()
+    rest = z.exp().scatter(1, y[:, None], 0.0).sum(1)       # lse = ln(1 + rest), 1 - p = rest / (1 + rest)
+    lse = torch.log1p(rest).float()
+    g = torch.randn(rows, device="cuda")
+    p = z.exp() / (1 + rest)[:, None]
+    logp = z - torch.log1p(rest)[:, None]
+    H = -(p * logp).sum(1).float()
+    d = torch.empty_like(x)
+    ecq.ecq_token_logprob_grad(x, y, lse, None, g, None, d)
+    want = g.double() * rest / (1 + rest)
+    store = {torch.float32: 0.0, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}[x.dtype]
+    got = d.double().gather(1, y[:, None])[:, 0]
+    assert torch.all((got - want).abs() <= (16 * EPS + store) * want.abs() + 2.0 ** -25)
+    # beside a derivative of the entropy that is as small as a regulariser's
+    ecq.ecq_token_logprob_grad(x, y, lse, H, g, torch.full_like(g, 1e-3), d)
+    extra = 1e-3 * (p.gather(1, y[:, None]) * (logp.gather(1, y[:, None]) + H.double()[:, None]))[:, 0]
+    got = d.double().gather(1, y[:, None])[:, 0]
+    assert torch.all((got - (want - extra)).abs() <= (16 * EPS + store) * (want.abs() + extra.abs()) + 32 * EPS * 1e-3 * H + 2.0 ** -25)
+
+
 def uncentred(rows, vocab, dtype, stride, seed, offset):
     """Rows whose lse alone does not tell the probabilities: every entry (or all but a few) at the
     type's lowest value, entries far from zero, entries at the highest value; and rows without open entries."""
