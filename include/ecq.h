@@ -379,7 +379,8 @@ int ecq_step_static(uint64_t d, uint32_t bucket, uint32_t levels, float alpha, f
  * list that runs out of open entries ends in -inf with index -1).  Logits at the type's lowest
  * finite value are ordinary entries.  A row with every entry at -inf has lse -inf, entropy 0 and
  * a target's logprob -inf.  A row that holds a NaN or +inf gives NaN (indices -1).
- * rows == 0 does nothing.  ECQ_ERR_ARG on a violation of the above, vocab > 2^30 or rows > 2^28.
+ * rows == 0 does nothing.  ECQ_ERR_ARG on a violation of the above, vocab > 2^30, rows > 2^28 or
+ * row_stride > 2^32.
  * The current device's; one kernel launch; no workspace.
  */
 #define ECQ_TOKEN_MAX_TOP 32
@@ -430,9 +431,10 @@ int ecq_token_logprob_grad(const void* logits, int dtype, uint64_t rows, uint32_
  *
  * ecq_muon_create
  *   count        1..ECQ_MUON_MAX_COUNT matrices; the arrays are HOST, read before the call returns
- *   offsets      first entry of each matrix in the flat vectors (no alignment needed)
- *   rows, cols   1..ECQ_MUON_MAX_SIDE, the smaller of the two at most ECQ_MUON_MAX_RANK
- *   strides      entries from one row to the next (>= cols), or NULL: cols
+ *   offsets      first entry of each matrix in the flat vectors (no alignment needed; at most 2^48)
+ *   rows, cols   1..ECQ_MUON_MAX_SIDE, the smaller of the two at most ECQ_MUON_MAX_RANK; the workspace
+ *                of all of them at most 4 TB and their tiles in all products at most 2^28
+ *   strides      entries from one row to the next (>= cols, at most 2^40), or NULL: cols
  *   scales       factor of each matrix's update, or NULL: 1
  *   steps        1..ECQ_MUON_MAX_STEPS
  *   coefficients a, b, c of each step, or NULL for the defaults.  ECQ_ERR_ARG if some singular

@@ -224,7 +224,11 @@ std::vector<MuonProduct> program(const std::vector<Step>& steps, uint32_t merge)
 }
 
 // Entries of the matrices that are worked on together.  Three such groups are under way at a time,
-// each with 8 bytes an entry of X, of which about half is alive: they about fill the L2 cache.
+// each with 8 bytes an entry of X, of which about half is alive: they about fill the L2 cache.  Smaller
+// groups leave SMs without a tile, larger ones make no difference.  In ms with groups of 3, 6, 12, 24 and
+// 48 M entries, layers of (w, 4w), (4w, w) and four (w, w) to a bf16 update:
+//     w 640, 20 layers   2.38 2.02 2.05 2.06 2.07     w 1024, 12   4.60 3.62 3.20 3.20 3.21
+//     w 1280, 8          4.80 4.10 3.80 3.75 3.85     w 2048, 4    6.4  6.2  6.3  6.2  6.1
 constexpr uint64_t kGroupEntries = 12ull << 20;
 constexpr uint64_t kLanes = 3;
 
@@ -408,10 +412,15 @@ int launch_prepare(const ecq_muon* p, MuonPrepare pre, cudaStream_t st) {
 }
 
 // Tiles of a call: the plan's choice, or the largest of which there are enough for every SM.  Pairs
-// take 256 rows at a time, which has to fill: 48 matrices of 128 x 512 take 160 us with pairs and
-// 109 without, three of 1537 x 611 (a fifth of the rows empty) 307 and 290 (22-bit operands), but
-// resnet50's matrices (a tenth) 1022 and 1160.  Too few tiles for the SMs: one 1024 x 1024 takes 218,
-// 161 and 141 us with 256 x 256, 128 x 128 and 128 x 64, three of them 254, 192 and 215.
+// take 256 rows at a time, which has to fill.  In us with 256 x 256, 128 x 128 and 128 x 64, 11 bits, and
+// with 256 x 128 and 128 x 64, 22 bits, by the rows that pairs compute for one of 128-row tiles:
+//     2.00  48 of 128 x 512    160 116 102 | 195 131     1.14  6 of 896 x 1792    351 296 396 | 554 589
+//     1.33  60 of 384 x 384    357 255 368 | 540 439     1.11  4 of 1152 x 2304   401 361 527 | 665 771
+//     1.20  3 of 1537 x 611    288 214 188 | 311 266     1.09  4 of 1408 x 1408   372 380 603 | 730 929
+//     1.20  30 of 640 x 640    419 366 603 | 816 798     1.00  2048 x 2048        327 306 478 | 505 787
+// With 22 bits the crossing is the rule's; with 11 bits it lies lower, at 1.10 (the rule costs the 1.14 and
+// 1.11 lines 50 and 40 us).  Too few tiles for the SMs: one 1024 x 1024 takes 222, 165 and 148 us, 263 and
+// 194 with 22 bits; three of them 256, 196 and 216, and 308 and 335.
 int choose_tiles(const ecq_muon* p, bool split) {
     if (p->tiles != ECQ_MUON_TILES_AUTO) return p->tiles;
     if (p->n_full[split ? 1 : 0] * 2 >= (uint64_t)p->sms && 100 * p->padded[1] <= 115 * p->padded[0]) return ECQ_MUON_TILES_256X256;

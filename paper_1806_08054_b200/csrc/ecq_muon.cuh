@@ -673,12 +673,12 @@ __device__ __forceinline__ bool elect_one() {
 // so they have been taken by CTAs that are running: some tile can always go on, whatever number
 // of CTAs the GPU has room for.
 //
-// What bounds it.  Large matrices (24 layers of 1024 x 1024 to 1024 x 4096, 6.4 to 6.7 ms, 2.36 at the
-// tensor cores' rate): operands and results through L2, 9.6 TB/s, with the tensor pipe busy 39 %
-// of the time, and the power cap.  Few tiles (1024 x 1024, 132 us): 15 products one after the other,
-// 8.5 us each: 0.7 for the first load, 4.2 for 16 steps of 24 KB at the 48 bytes a clock that an SM takes
-// from L2 (the products alone: 1.6), 1.5 for the results, 1 to make them visible, 0.5 to see that.
-// Smallest (96 x 160, 60 us): the same with 0.5 for the products.
+// What bounds it.  Large matrices (two layers of 1024 x 1024 to 1024 x 4096, 460 us of the call's 548): operands
+// and results through L2, 9.8 TB/s, with the tensor pipe busy 40 % of the time; 24 such layers (5.9 ms
+// undisturbed, 6.5 among others, 2.36 at the tensor cores' rate) meet the power cap besides.  Few tiles (1024 x
+// 1024, 137 us): 15 products one after the other, 9 us each: 0.7 for the first load, 4.2 for 16 steps of
+// 24 KB at the 48 bytes a clock that an SM takes from L2 (the products alone: 1.6), 1.5 for the results, 1 to
+// make them visible, 0.5 to see that.  Smallest (96 x 160, 63 us): the same with 0.5 for the products.
 template <int CG, int TN, bool SPLIT, bool KS>
 __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muon_iterate_kernel(const __grid_constant__ MuonIterate P) {
     using S = MuonShape<CG, TN, SPLIT, KS>;
