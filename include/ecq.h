@@ -500,6 +500,113 @@ int ecq_muon_step(ecq_muon* plan, const float* grad, float* momentum, float mu, 
 int ecq_muon_status(ecq_muon* plan, void* cuda_stream);
 
 /*
+ * Matrices in 8 bits: what a language model's layer keeps and multiplies between the two ends that the
+ * calls above serve, with the idea that the codec has for gradients (few bits, and a scale for each
+ * piece).  The codec's paper has no counterpart.
+ *
+ * A matrix in 8 bits holds x_ij as q_ij 2^e: q in e4m3 (largest value L = 448, 3 bits of mantissa) or e5m2
+ * (57344, 2 bits), and one 2^e for each 128 consecutive columns of a row, the smallest power of two
+ * with max|x| <= L 2^e, not below 2^-127.  q = x 2^-e rounded to nearest, ties to even.  A block with a NaN or
+ * Inf is NaN throughout; the others are not affected.  Blocks of zeros are exact.
+ *   data     1 byte an entry; 16-byte aligned, rows `stride` bytes apart (a multiple of 16, >= cols)
+ *   scales   ecq_act8_scale_bytes(rows, cols) bytes, 16-byte aligned: e + 127, 255 for a NaN block, in groups of
+ *            128 rows and four blocks as the tensor cores take them: row r's block b at
+ *              ((r / 128) * ceil(cols / 512) + b / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4
+ *            Bytes between those of real blocks are neither written nor used.
+ * The scales being powers of two, restored values are exact in bf16 (between 2^-126 and its largest) and storing a matrix in 8 bits again,
+ * along its other axis, changes only entries that are 2^-14 (e5m2: 2^-30) of their new block's largest or less.
+ *
+ * A matrix of a call, in any type: its first entry, entries from row to row, and the scales (NULL where the
+ * type has none).  Plain matrices (ECQ_F32, ECQ_BF16, ECQ_F16) are aligned to one entry only, any
+ * stride >= cols; 16-byte aligned ones are faster.  The plain matrices of one call have one type (the
+ * addend and the result of ecq_act8_product excepted), the 8-bit ones any of the two each.  The structs are read before the
+ * call returns.  "or NULL": not given, or a result that is not wanted; at least one result has to be.
+ *
+ * rows (m) == 0 does nothing (a weight's gradient is zero).  ECQ_ERR_ARG for rows or columns beyond 2^28, strides beyond 2^36, more than
+ * 2^31 - 1 tiles of 128 x 128, no columns, or a violation of what is said above and below.  Results must not overlap each
+ * other, or inputs; a plain result may be a plain input of the same place and strides.  Entries
+ * behind a row's last column are left as they are.  All on the current device; each call is one kernel
+ * launch, ecq_act8_norm_grad with a weight's gradient two; no allocation; any of them may be captured into a CUDA graph.
+ *
+ * ecq_act8_store   x (any type) in 8 bits as q and, transposed, as q_t [cols, rows], whose blocks are 128 rows
+ *                  of x; either may be NULL.
+ * ecq_act8_load    the values that q stands for, rounded to x's type.
+ */
+#define ECQ_E4M3 3
+#define ECQ_E5M2 4
+typedef struct {
+    void* data;
+    uint64_t stride;
+    void* scales;
+    int32_t dtype;
+} ecq_act8_matrix;
+uint64_t ecq_act8_scale_bytes(uint64_t rows, uint64_t cols);
+int ecq_act8_store(uint64_t rows, uint64_t cols, const ecq_act8_matrix* x, const ecq_act8_matrix* q,
+                   const ecq_act8_matrix* q_t, void* cuda_stream);
+int ecq_act8_load(uint64_t rows, uint64_t cols, const ecq_act8_matrix* q, const ecq_act8_matrix* x,
+                  void* cuda_stream);
+
+/*
+ * Gated activation h = g sigmoid(g) u of gate and up (both of one type, plain or 8 bits):
+ *   out       h, plain, or NULL; out8, out8_t: h in 8 bits, and transposed, or NULL
+ *   gate8, up8   gate and up in 8 bits, for the backward pass, or NULL
+ * and its gradient, from gate and up as they were given or as they were kept:
+ *   d_gate = d_out u sigmoid(g) (1 + g (1 - sigmoid(g)))      d_up = d_out g sigmoid(g)
+ * each plain, in 8 bits or in 8 bits transposed, or several of these.  Arithmetic is fp32; entries of gate at -inf give NaN.
+ */
+int ecq_act8_gate(uint64_t rows, uint64_t cols, const ecq_act8_matrix* gate, const ecq_act8_matrix* up,
+                  const ecq_act8_matrix* out, const ecq_act8_matrix* out8, const ecq_act8_matrix* out8_t,
+                  const ecq_act8_matrix* gate8, const ecq_act8_matrix* up8, void* cuda_stream);
+int ecq_act8_gate_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* gate, const ecq_act8_matrix* up,
+                       const ecq_act8_matrix* d_out, const ecq_act8_matrix* d_gate, const ecq_act8_matrix* d_up,
+                       const ecq_act8_matrix* d_gate8, const ecq_act8_matrix* d_gate8_t,
+                       const ecq_act8_matrix* d_up8, const ecq_act8_matrix* d_up8_t, void* cuda_stream);
+
+/*
+ * Root-mean-square norm with the residual's addition, of each row:
+ *   s = x + residual                                  (residual may be NULL)
+ *   rstd = 1 / sqrt(mean_j s_j^2 + eps)               eps >= 0
+ *   y_j = s_j rstd w_j                                weight [cols] of weight_dtype, or NULL: 1
+ * in fp32 throughout (s is not rounded before it is normed; squares are added in fp32, so rows whose
+ * sum of squares is beyond its range give zeros, as s rstd does there).
+ *   sum, out     s and y, plain, or NULL; sum8, out8: in 8 bits, or NULL; rstd [rows] or NULL
+ *   cols         at most ECQ_ACT8_NORM_MAX_COLS
+ * A row of zeros with eps == 0 gives NaN.
+ *
+ * Its gradient, from sum (plain, or in 8 bits as sum8 kept it) and rstd, with n = s rstd and g = d_out w:
+ *   d_x = rstd (g - n mean_j(g_j n_j)) + d_sum        (d_sum, the gradient that reaches s by itself, or NULL)
+ *   d_weight [cols] = sum over the rows of d_out n    or NULL
+ * d_x is the gradient of x and of the residual alike, or NULL.  The rows' sums are added in an order that the sizes (and
+ * the GPU's number of SMs) fix: results repeat.
+ *   workspace    of ecq_act8_norm_grad_workspace_bytes (of the current device), 16-byte aligned; only with d_weight, else NULL.  Nothing in it
+ *                outlives the call; calls that may overlap need one each.
+ */
+#define ECQ_ACT8_NORM_MAX_COLS 16384
+int ecq_act8_norm(uint64_t rows, uint64_t cols, const ecq_act8_matrix* x, const ecq_act8_matrix* residual,
+                  const void* weight, int weight_dtype, float eps, const ecq_act8_matrix* sum,
+                  const ecq_act8_matrix* out, const ecq_act8_matrix* out8, const ecq_act8_matrix* sum8,
+                  float* rstd, void* cuda_stream);
+uint64_t ecq_act8_norm_grad_workspace_bytes(uint64_t rows, uint64_t cols);
+int ecq_act8_norm_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* sum, const void* weight,
+                       int weight_dtype, const float* rstd, const ecq_act8_matrix* d_out,
+                       const ecq_act8_matrix* d_sum, const ecq_act8_matrix* d_x, float* d_weight,
+                       void* workspace, uint64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Product of matrices in 8 bits, d = a b^T + c: a [m, k], b [n, k] with blocks along k (a weight or an activation
+ * stored transposed serves the products of the backward pass), c [m, n] plain or NULL, d [m, n] plain, or in 8
+ * bits where c is NULL.  Sums over k are in fp32, in an order that the sizes (and the GPU's number of SMs) fix; d is rounded once.  c may
+ * be d, in place: adding a weight's gradient to what is there.
+ *   status   device word or NULL: bit 1 (value 2) is set when an in-kernel wait ran out (ECQ_ERR_TIMEOUT's
+ *            meaning); entries of d that it concerned are NaN.  Never cleared by the library.
+ * ecq_act8_set_wait_limit  as ecq_set_wait_limit, for this process's products.
+ */
+int ecq_act8_product(uint64_t m, uint64_t n, uint64_t k, const ecq_act8_matrix* a, const ecq_act8_matrix* b,
+                     const ecq_act8_matrix* c, const ecq_act8_matrix* d, uint32_t* status,
+                     void* cuda_stream);
+int ecq_act8_set_wait_limit(uint32_t polls);
+
+/*
  * Synchronise `cuda_stream`, then return and clear the context's sticky device
  * status: ECQ_OK, ECQ_ERR_NONFINITE, ECQ_ERR_TIMEOUT, or ECQ_ERR_CUDA if the
  * stream itself reports an error.

@@ -18,4 +18,7 @@ from .binding import (  # noqa: F401
     ECQ_MUON_AUTO, ECQ_MUON_HALF, ECQ_MUON_SPLIT, ECQ_MUON_TILES_AUTO, ECQ_MUON_TILES_128X128, ECQ_MUON_TILES_128X64,
     ECQ_MUON_TILES_256X256, ecq_muon_bind, ecq_muon_create, ecq_muon_destroy, ecq_muon_orthogonalize, ecq_muon_set_tiles,
     ecq_muon_set_wait_limit, ecq_muon_status, ecq_muon_step, ecq_muon_workspace_bytes,
+    ECQ_ACT8_NORM_MAX_COLS, ECQ_E4M3, ECQ_E5M2, ecq_act8_gate, ecq_act8_gate_grad, ecq_act8_load, ecq_act8_norm,
+    ecq_act8_norm_grad, ecq_act8_norm_grad_workspace_bytes, ecq_act8_product, ecq_act8_scale_bytes,
+    ecq_act8_set_wait_limit, ecq_act8_store,
 )

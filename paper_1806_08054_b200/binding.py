@@ -36,6 +36,11 @@ class EcqError(RuntimeError):
         super().__init__("%s: %s (status %d)" % (where, strerror(status), status))
 
 
+class Act8Matrix(ctypes.Structure):
+    """A matrix of an ecq_act8_* call: ``ecq_act8_matrix`` of ecq.h."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_uint64), ("scales", ctypes.c_void_p), ("dtype", ctypes.c_int32)]
+
+
 def lib() -> ctypes.CDLL:
     """Load the compiled library; raise if it has not been built."""
     global _lib
@@ -117,6 +122,27 @@ def lib() -> ctypes.CDLL:
         L.ecq_muon_step.restype = i32
         L.ecq_muon_status.argtypes = [vp, vp]
         L.ecq_muon_status.restype = i32
+        mat = ctypes.POINTER(Act8Matrix)
+        L.ecq_act8_scale_bytes.argtypes = [u64, u64]
+        L.ecq_act8_scale_bytes.restype = u64
+        L.ecq_act8_store.argtypes = [u64, u64, mat, mat, mat, vp]
+        L.ecq_act8_store.restype = i32
+        L.ecq_act8_load.argtypes = [u64, u64, mat, mat, vp]
+        L.ecq_act8_load.restype = i32
+        L.ecq_act8_gate.argtypes = [u64, u64] + [mat] * 7 + [vp]
+        L.ecq_act8_gate.restype = i32
+        L.ecq_act8_gate_grad.argtypes = [u64, u64] + [mat] * 9 + [vp]
+        L.ecq_act8_gate_grad.restype = i32
+        L.ecq_act8_norm.argtypes = [u64, u64, mat, mat, vp, i32, f32, mat, mat, mat, mat, vp, vp]
+        L.ecq_act8_norm.restype = i32
+        L.ecq_act8_norm_grad_workspace_bytes.argtypes = [u64, u64]
+        L.ecq_act8_norm_grad_workspace_bytes.restype = u64
+        L.ecq_act8_norm_grad.argtypes = [u64, u64, mat, vp, i32, vp, mat, mat, mat, vp, vp, u64, vp]
+        L.ecq_act8_norm_grad.restype = i32
+        L.ecq_act8_product.argtypes = [u64, u64, u64, mat, mat, mat, mat, vp, vp]
+        L.ecq_act8_product.restype = i32
+        L.ecq_act8_set_wait_limit.argtypes = [u32]
+        L.ecq_act8_set_wait_limit.restype = i32
         L.ecq_status.argtypes = [vp, vp]
         L.ecq_status.restype = i32
         L.ecq_launch_count.argtypes = []
@@ -589,3 +615,168 @@ def ecq_muon_step(plan: int, grad: torch.Tensor, momentum: torch.Tensor, params=
 def ecq_muon_status(plan: int, stream=None) -> int:
     """Synchronise the stream and return (and clear) the plan's sticky device status."""
     return int(lib().ecq_muon_status(plan, _stream(stream)))
+
+
+# ---- matrices in 8 bits -----------------------------------------------------------
+ECQ_E4M3, ECQ_E5M2 = 3, 4
+ECQ_ACT8_NORM_MAX_COLS = 16384
+_DTYPES8 = {torch.float8_e4m3fn: ECQ_E4M3, torch.float8_e5m2: ECQ_E5M2}
+
+
+def ecq_act8_scale_bytes(rows: int, cols: int) -> int:
+    """Bytes of the scales of a [rows, cols] matrix in 8 bits (0: beyond what the calls take)."""
+    if not (0 <= rows < 1 << 64 and 0 <= cols < 1 << 64):
+        raise ValueError("rows and cols must not be negative, and below 2^64")
+    return int(lib().ecq_act8_scale_bytes(rows, cols))
+
+
+def _matrix(m, name: str, shape=None):
+    """A plain tensor [rows, cols], or the pair (q, scales) of a matrix in 8 bits, as the library takes it."""
+    if m is None:
+        return None
+    scales = None
+    if type(m) is tuple or type(m) is list:
+        m, scales = m
+    have, stride = m.shape, m.stride()
+    if len(have) != 2 or not m.is_cuda:
+        raise ValueError("%s must be a CUDA tensor of two dimensions, or a pair (q, scales) (there is no CPU path)" % name)
+    if shape is not None and have != shape:
+        raise ValueError("%s must be %d x %d" % (name, *shape))
+    if have[1] > 1 and stride[1] != 1 or (have[0] > 1 and stride[0] < have[1]):
+        raise ValueError("%s must have contiguous rows that do not overlap" % name)
+    where = m.get_device()
+    if scales is None:
+        dtype = _DTYPES.get(m.dtype)
+        if dtype is None:
+            raise ValueError("%s must be float32, bfloat16 or float16, or a pair (q, scales)" % name)
+        at = None
+    else:
+        dtype = _DTYPES8.get(m.dtype)
+        if dtype is None or scales.dtype is not torch.uint8 or not scales.is_contiguous() or scales.get_device() != where or \
+                scales.numel() < -(-have[0] // 128) * -(-have[1] // 512) * 512:
+            raise ValueError("%s must be (float8_e4m3fn or float8_e5m2, uint8 scales of ecq_act8_scale_bytes on the same device)" % name)
+        at = scales.data_ptr()
+    if where != _current_device():
+        raise ValueError("%s must be on the current device" % name)
+    return Act8Matrix(m.data_ptr(), stride[0] if have[0] > 1 or scales is not None else max(stride[0], have[1]), at, dtype)
+
+
+def _current_device() -> int:
+    return _device() if _device is not None else torch.cuda.current_device()
+
+
+def _like(t):
+    return (t[0] if type(t) is tuple or type(t) is list else t).shape
+
+
+def _vector(t, dtype, n: int, name: str):
+    if t is not None and t.is_cuda and t.get_device() != _current_device():
+        raise ValueError("%s must be on the current device" % name)
+    return _vec(t, dtype, n, name)
+
+
+def _weight(w, n: int):
+    if w is None:
+        return None, 0
+    if w.dtype not in _DTYPES:
+        raise ValueError("weight must be float32, bfloat16 or float16")
+    return _vector(w, w.dtype, n, "weight"), _DTYPES[w.dtype]
+
+
+def ecq_act8_store(x, out=None, out_t=None, stream=None) -> None:
+    """``x`` (a tensor, or a pair) in 8 bits: ``out`` and, transposed, ``out_t`` are pairs (q, scales) with q a
+    [rows, stride] float8 tensor's first columns and uint8 scales of ``ecq_act8_scale_bytes``."""
+    shape = rows, cols = _like(x)
+    rc = (_lib or lib()).ecq_act8_store(rows, cols, _matrix(x, "x"), _matrix(out, "out", shape),
+                                        _matrix(out_t, "out_t", (cols, rows)), _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_act8_store")
+
+
+def ecq_act8_load(x8, out: torch.Tensor, stream=None) -> None:
+    """The values that the pair ``x8`` stands for."""
+    shape = rows, cols = _like(x8)
+    rc = (_lib or lib()).ecq_act8_load(rows, cols, _matrix(x8, "x8"), _matrix(out, "out", shape), _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_act8_load")
+
+
+def ecq_act8_gate(gate, up, out=None, out8=None, out8_t=None, gate8=None, up8=None, stream=None) -> None:
+    """gate * sigmoid(gate) * up, plain, in 8 bits and in 8 bits transposed, and gate and up in 8 bits,
+    each where it is given."""
+    shape = rows, cols = _like(gate)
+    rc = (_lib or lib()).ecq_act8_gate(
+        rows, cols, _matrix(gate, "gate"), _matrix(up, "up", shape), _matrix(out, "out", shape), _matrix(out8, "out8", shape),
+        _matrix(out8_t, "out8_t", (cols, rows)), _matrix(gate8, "gate8", shape), _matrix(up8, "up8", shape), _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_act8_gate")
+
+
+def ecq_act8_gate_grad(gate, up, d_out, d_gate=None, d_up=None, d_gate8=None, d_gate8_t=None, d_up8=None, d_up8_t=None,
+                       stream=None) -> None:
+    """Gradient of :func:`ecq_act8_gate`, from gate and up as they were given or kept."""
+    shape = rows, cols = _like(gate)
+    turned = (cols, rows)
+    rc = (_lib or lib()).ecq_act8_gate_grad(
+        rows, cols, _matrix(gate, "gate"), _matrix(up, "up", shape), _matrix(d_out, "d_out", shape),
+        _matrix(d_gate, "d_gate", shape), _matrix(d_up, "d_up", shape), _matrix(d_gate8, "d_gate8", shape),
+        _matrix(d_gate8_t, "d_gate8_t", turned), _matrix(d_up8, "d_up8", shape), _matrix(d_up8_t, "d_up8_t", turned),
+        _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_act8_gate_grad")
+
+
+def ecq_act8_norm(x, residual=None, weight=None, *, eps: float = 1e-6, sum=None, out=None, out8=None, sum8=None, rstd=None,
+                  stream=None) -> None:
+    """Root-mean-square norm of x + residual: the sum, the norm (plain and in 8 bits each) and the
+    rows' factors, each where it is given."""
+    shape = rows, cols = _like(x)
+    w, w_dtype = _weight(weight, cols)
+    rc = (_lib or lib()).ecq_act8_norm(
+        rows, cols, _matrix(x, "x"), _matrix(residual, "residual", shape), w, w_dtype, eps, _matrix(sum, "sum", shape),
+        _matrix(out, "out", shape), _matrix(out8, "out8", shape), _matrix(sum8, "sum8", shape),
+        _vector(rstd, torch.float32, rows, "rstd"), _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_act8_norm")
+
+
+def ecq_act8_norm_grad_workspace_bytes(rows: int, cols: int) -> int:
+    if not (0 <= rows < 1 << 64 and 0 <= cols < 1 << 64):
+        raise ValueError("rows and cols must not be negative, and below 2^64")
+    return int(lib().ecq_act8_norm_grad_workspace_bytes(rows, cols))
+
+
+def ecq_act8_norm_grad(sum, weight, rstd, d_out, d_x=None, d_weight=None, workspace=None, *, d_sum=None, stream=None) -> None:
+    """Gradient of :func:`ecq_act8_norm`, from the sum (a tensor, or the pair that ``sum8`` kept) and ``rstd``."""
+    shape = rows, cols = _like(sum)
+    w, w_dtype = _weight(weight, cols)
+    if workspace is not None and (not workspace.is_cuda or not workspace.is_contiguous() or
+                                  workspace.get_device() != _current_device()):
+        raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
+    rc = (_lib or lib()).ecq_act8_norm_grad(
+        rows, cols, _matrix(sum, "sum"), w, w_dtype, _vector(rstd, torch.float32, rows, "rstd"), _matrix(d_out, "d_out", shape),
+        _matrix(d_sum, "d_sum", shape), _matrix(d_x, "d_x", shape), _vector(d_weight, torch.float32, cols, "d_weight"),
+        None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_act8_norm_grad")
+
+
+def ecq_act8_product(a, b, out, add=None, status=None, stream=None) -> None:
+    """out = a b^T + add of pairs a [m, k] and b [n, k]; ``out`` is a tensor (``add`` may be the same), or a
+    pair where ``add`` is None.  ``status``: an int32 tensor of one entry, set to 2 if an in-kernel wait ran out."""
+    (m, k), (n, k2) = _like(a), _like(b)
+    if k != k2:
+        raise ValueError("a and b must have the same number of columns")
+    rc = (_lib or lib()).ecq_act8_product(
+        m, n, k, _matrix(a, "a"), _matrix(b, "b"), _matrix(add, "add", (m, n)), _matrix(out, "out", (m, n)),
+        _vector(status, torch.int32, 1, "status"), _stream(stream))
+    if rc != ECQ_OK:
+        raise EcqError(rc, "ecq_act8_product")
+
+
+def ecq_act8_set_wait_limit(polls: int = ECQ_WAIT_LIMIT_DEFAULT) -> None:
+    """Polls an in-kernel wait of this process's products makes before it gives up."""
+    if not 0 <= polls < 1 << 32:
+        raise ValueError("polls must be below 2^32")
+    lib().ecq_act8_set_wait_limit(polls)

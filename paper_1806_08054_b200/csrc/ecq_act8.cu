@@ -1,0 +1,267 @@
+// C ABI of the operators on matrices in 8 bits, the products apart: argument checks and launches.
+#include <cfloat>
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "../../include/ecq.h"
+#include "ecq_act8_host.h"
+#include "ecq_act8_kernels.cuh"
+
+using namespace ecq;
+
+namespace {
+
+int sm_count(int& sms) {
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess
+               ? ECQ_OK : ECQ_ERR_CUDA;
+}
+
+// ---- tiles
+template <int OP, typename S, typename T>
+int launch_tiles(const Act8Tiles& P, cudaStream_t st) {
+    return launch_act8(act8_tile_kernel<OP, S, T>, (P.rows + 127) / 128 * P.tiles_across, kActThreads, 0, 0, st, P);
+}
+template <int OP, typename T>
+int launch_tiles(const Act8Tiles& P, bool coded, cudaStream_t st) {
+    return coded ? launch_tiles<OP, uint8_t, T>(P, st) : launch_tiles<OP, T, T>(P, st);
+}
+template <int OP>
+int launch_tiles(Act8Tiles& P, uint64_t rows, uint64_t cols, int plain, bool coded, void* stream) {
+    P.rows = (uint32_t)rows;
+    P.cols = (uint32_t)cols;
+    P.tiles_across = (uint32_t)((cols + 127) / 128);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    switch (plain) {
+        case ECQ_F32: return launch_tiles<OP, float>(P, coded, st);
+        case ECQ_BF16: return launch_tiles<OP, __nv_bfloat16>(P, coded, st);
+        default: return launch_tiles<OP, __half>(P, coded, st);
+    }
+}
+
+// ---- norm: threads of a row, a power of two from 32 to 512, and columns of each
+struct RowShape { uint32_t per_row, per_cta; int vectors; };
+RowShape row_shape(uint64_t rows, uint64_t cols, int sms) {
+    RowShape s = {32, 256, 1};
+    const uint32_t eights = (uint32_t)((cols + 7) / 8);
+    // few rows: one vector a thread, and more threads; many: two
+    const uint32_t want = rows * eights <= (uint64_t)sms * 512 ? 1 : 2;
+    while (s.per_row < 512 && s.per_row * want < eights) s.per_row *= 2;
+    while (s.per_row * (uint32_t)s.vectors < eights) s.vectors *= 2;
+    s.per_cta = s.per_row > 256 || rows == 1 ? s.per_row : 256;
+    return s;
+}
+
+template <typename T, int NV>
+int launch_norm(const Act8Norm& P, const RowShape& s, int sms, cudaStream_t st) {
+    const uint64_t slots = s.per_cta / s.per_row, need = (P.rows + slots - 1) / slots, most = (uint64_t)sms * (1024 / s.per_cta);
+    return launch_act8(act8_norm_kernel<T, NV>, (uint32_t)(need < most ? need : most), s.per_cta, 0, 0, st, P);
+}
+template <typename T>
+int launch_norm(const Act8Norm& P, const RowShape& s, int sms, cudaStream_t st) {
+    return s.vectors == 1 ? launch_norm<T, 1>(P, s, sms, st) : s.vectors == 2 ? launch_norm<T, 2>(P, s, sms, st) : launch_norm<T, 4>(P, s, sms, st);
+}
+
+uint32_t grad_grid(uint64_t rows, const RowShape& s, int sms) {
+    const uint64_t slots = s.per_cta / s.per_row, need = (rows + slots - 1) / slots, most = (uint64_t)sms * (512 / s.per_cta);
+    return (uint32_t)(need < most ? need : most);
+}
+
+template <typename S, typename T, int NV>
+int launch_norm_grad(const Act8NormGrad& P, const RowShape& s, uint32_t grid, cudaStream_t st) {
+    return launch_act8(act8_norm_grad_kernel<S, T, NV>, grid, s.per_cta, 0, 0, st, P);
+}
+template <typename S, typename T>
+int launch_norm_grad(const Act8NormGrad& P, const RowShape& s, uint32_t grid, cudaStream_t st) {
+    return s.vectors == 1 ? launch_norm_grad<S, T, 1>(P, s, grid, st)
+         : s.vectors == 2 ? launch_norm_grad<S, T, 2>(P, s, grid, st) : launch_norm_grad<S, T, 4>(P, s, grid, st);
+}
+template <typename T>
+int launch_norm_grad(const Act8NormGrad& P, const RowShape& s, uint32_t grid, bool coded, cudaStream_t st) {
+    return coded ? launch_norm_grad<uint8_t, T>(P, s, grid, st) : launch_norm_grad<T, T>(P, s, grid, st);
+}
+
+// Plain matrices of a call have one type.
+bool same_type(int& type, const ecq_act8_matrix* m) {
+    if (!m || m->dtype >= 3) return true;
+    if (type >= 0 && type != m->dtype) return false;
+    type = m->dtype;
+    return true;
+}
+
+bool bad_weight(const void* w, int dtype) { return w && (!dtype_bytes(dtype) || !aligned_to(w, dtype_bytes(dtype))); }
+
+}  // namespace
+
+extern "C" {
+
+uint64_t ecq_act8_scale_bytes(uint64_t rows, uint64_t cols) {
+    if (rows > kActMaxSide || cols > kActMaxSide) return 0;
+    return (rows + 127) / 128 * ((cols + 511) / 512) * 512;
+}
+
+int ecq_act8_store(uint64_t rows, uint64_t cols, const ecq_act8_matrix* x, const ecq_act8_matrix* q, const ecq_act8_matrix* q_t,
+                   void* cuda_stream) {
+    if (bad_size(rows, cols) || (!q && !q_t) || bad_matrix(x, rows, cols, kAny) || (q && bad_matrix(q, rows, cols, kCoded)) ||
+        (q_t && bad_matrix(q_t, cols, rows, kCoded)))
+        return ECQ_ERR_ARG;
+    if (rows == 0) return ECQ_OK;
+    Act8Tiles P = {};
+    P.in[0] = act8_mat(x, cols);
+    P.q[0] = act8_mat(q, cols);
+    P.qt[0] = act8_mat(q_t, rows);
+    return launch_tiles<kActCopy>(P, rows, cols, x->dtype < 3 ? x->dtype : ECQ_F32, x->dtype >= 3, cuda_stream);
+}
+
+int ecq_act8_load(uint64_t rows, uint64_t cols, const ecq_act8_matrix* q, const ecq_act8_matrix* x, void* cuda_stream) {
+    if (bad_size(rows, cols) || bad_matrix(q, rows, cols, kCoded) || bad_matrix(x, rows, cols, kPlain)) return ECQ_ERR_ARG;
+    if (rows == 0) return ECQ_OK;
+    Act8Tiles P = {};
+    P.in[0] = act8_mat(q, cols);
+    P.plain[0] = act8_mat(x, cols);
+    return launch_tiles<kActCopy>(P, rows, cols, x->dtype, true, cuda_stream);
+}
+
+int ecq_act8_gate(uint64_t rows, uint64_t cols, const ecq_act8_matrix* gate, const ecq_act8_matrix* up, const ecq_act8_matrix* out,
+                  const ecq_act8_matrix* out8, const ecq_act8_matrix* out8_t, const ecq_act8_matrix* gate8,
+                  const ecq_act8_matrix* up8, void* cuda_stream) {
+    if (bad_size(rows, cols) || bad_matrix(gate, rows, cols, kAny) || bad_matrix(up, rows, cols, kAny) || gate->dtype != up->dtype)
+        return ECQ_ERR_ARG;
+    if ((out && bad_matrix(out, rows, cols, kPlain)) || (out8 && bad_matrix(out8, rows, cols, kCoded)) ||
+        (out8_t && bad_matrix(out8_t, cols, rows, kCoded)) || (gate8 && bad_matrix(gate8, rows, cols, kCoded)) ||
+        (up8 && bad_matrix(up8, rows, cols, kCoded)) || (!out && !out8 && !out8_t && !gate8 && !up8))
+        return ECQ_ERR_ARG;
+    int type = -1;
+    if (!same_type(type, gate) || !same_type(type, out)) return ECQ_ERR_ARG;
+    if (rows == 0) return ECQ_OK;
+    Act8Tiles P = {};
+    P.in[0] = act8_mat(gate, cols);
+    P.in[1] = act8_mat(up, cols);
+    P.plain[0] = act8_mat(out, cols);
+    P.q[0] = act8_mat(out8, cols);
+    P.qt[0] = act8_mat(out8_t, rows);
+    P.kept[0] = act8_mat(gate8, cols);
+    P.kept[1] = act8_mat(up8, cols);
+    return launch_tiles<kActGate>(P, rows, cols, type < 0 ? ECQ_F32 : type, gate->dtype >= 3, cuda_stream);
+}
+
+int ecq_act8_gate_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* gate, const ecq_act8_matrix* up,
+                       const ecq_act8_matrix* d_out, const ecq_act8_matrix* d_gate, const ecq_act8_matrix* d_up,
+                       const ecq_act8_matrix* d_gate8, const ecq_act8_matrix* d_gate8_t, const ecq_act8_matrix* d_up8,
+                       const ecq_act8_matrix* d_up8_t, void* cuda_stream) {
+    if (bad_size(rows, cols) || bad_matrix(gate, rows, cols, kAny) || bad_matrix(up, rows, cols, kAny) ||
+        gate->dtype != up->dtype || bad_matrix(d_out, rows, cols, kPlain))
+        return ECQ_ERR_ARG;
+    if ((d_gate && bad_matrix(d_gate, rows, cols, kPlain)) || (d_up && bad_matrix(d_up, rows, cols, kPlain)) ||
+        (d_gate8 && bad_matrix(d_gate8, rows, cols, kCoded)) || (d_gate8_t && bad_matrix(d_gate8_t, cols, rows, kCoded)) ||
+        (d_up8 && bad_matrix(d_up8, rows, cols, kCoded)) || (d_up8_t && bad_matrix(d_up8_t, cols, rows, kCoded)) ||
+        (!d_gate && !d_up && !d_gate8 && !d_gate8_t && !d_up8 && !d_up8_t))
+        return ECQ_ERR_ARG;
+    int type = d_out->dtype;
+    if (!same_type(type, gate) || !same_type(type, d_gate) || !same_type(type, d_up)) return ECQ_ERR_ARG;
+    if (rows == 0) return ECQ_OK;
+    Act8Tiles P = {};
+    P.in[0] = act8_mat(gate, cols);
+    P.in[1] = act8_mat(up, cols);
+    P.d = act8_mat(d_out, cols);
+    P.plain[0] = act8_mat(d_gate, cols);
+    P.plain[1] = act8_mat(d_up, cols);
+    P.q[0] = act8_mat(d_gate8, cols);
+    P.q[1] = act8_mat(d_up8, cols);
+    P.qt[0] = act8_mat(d_gate8_t, rows);
+    P.qt[1] = act8_mat(d_up8_t, rows);
+    return launch_tiles<kActGateGrad>(P, rows, cols, type, gate->dtype >= 3, cuda_stream);
+}
+
+int ecq_act8_norm(uint64_t rows, uint64_t cols, const ecq_act8_matrix* x, const ecq_act8_matrix* residual, const void* weight,
+                  int weight_dtype, float eps, const ecq_act8_matrix* sum, const ecq_act8_matrix* out, const ecq_act8_matrix* out8,
+                  const ecq_act8_matrix* sum8, float* rstd, void* cuda_stream) {
+    if (bad_size(rows, cols) || cols > ECQ_ACT8_NORM_MAX_COLS || bad_matrix(x, rows, cols, kPlain) ||
+        (residual && bad_matrix(residual, rows, cols, kPlain)) || bad_weight(weight, weight_dtype) || !(eps >= 0.f && eps <= FLT_MAX))
+        return ECQ_ERR_ARG;
+    if ((sum && bad_matrix(sum, rows, cols, kPlain)) || (out && bad_matrix(out, rows, cols, kPlain)) ||
+        (out8 && bad_matrix(out8, rows, cols, kCoded)) || (sum8 && bad_matrix(sum8, rows, cols, kCoded)) || !aligned_to(rstd, 4) ||
+        (!sum && !out && !out8 && !sum8 && !rstd))
+        return ECQ_ERR_ARG;
+    int type = x->dtype;
+    if (!same_type(type, residual) || !same_type(type, sum) || !same_type(type, out)) return ECQ_ERR_ARG;
+    if (rows == 0) return ECQ_OK;
+    int sms = 0;
+    if (sm_count(sms) != ECQ_OK) return ECQ_ERR_CUDA;
+    const RowShape s = row_shape(rows, cols, sms);
+    Act8Norm P = {};
+    P.x = act8_mat(x, cols);
+    P.residual = act8_mat(residual, cols);
+    P.sum = act8_mat(sum, cols);
+    P.y = act8_mat(out, cols);
+    P.y8 = act8_mat(out8, cols);
+    P.sum8 = act8_mat(sum8, cols);
+    P.weight = weight;
+    P.weight_dtype = weight_dtype;
+    P.rstd = rstd;
+    P.rows = (uint32_t)rows;
+    P.cols = (uint32_t)cols;
+    P.per_row = s.per_row;
+    P.eps = eps;
+    P.inv_cols = (float)(1.0 / (double)cols);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    switch (type) {
+        case ECQ_F32: return launch_norm<float>(P, s, sms, st);
+        case ECQ_BF16: return launch_norm<__nv_bfloat16>(P, s, sms, st);
+        default: return launch_norm<__half>(P, s, sms, st);
+    }
+}
+
+uint64_t ecq_act8_norm_grad_workspace_bytes(uint64_t rows, uint64_t cols) {
+    int sms = 0;
+    if (bad_size(rows, cols) || cols > ECQ_ACT8_NORM_MAX_COLS || sm_count(sms) != ECQ_OK) return 0;
+    const RowShape s = row_shape(rows, cols, sms);
+    return (uint64_t)grad_grid(rows, s, sms) * (s.per_cta / s.per_row) * cols * sizeof(float);
+}
+
+int ecq_act8_norm_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* sum, const void* weight, int weight_dtype,
+                       const float* rstd, const ecq_act8_matrix* d_out, const ecq_act8_matrix* d_sum, const ecq_act8_matrix* d_x,
+                       float* d_weight, void* workspace, uint64_t workspace_bytes, void* cuda_stream) {
+    if (bad_size(rows, cols) || cols > ECQ_ACT8_NORM_MAX_COLS || bad_matrix(sum, rows, cols, kAny) || bad_weight(weight, weight_dtype) ||
+        (rows && !rstd) || !aligned_to(rstd, 4) || bad_matrix(d_out, rows, cols, kPlain) || (d_sum && bad_matrix(d_sum, rows, cols, kPlain)) ||
+        (d_x && bad_matrix(d_x, rows, cols, kPlain)) || !aligned_to(d_weight, 4) || (!d_x && !d_weight) ||
+        (d_weight && rows && (!workspace || !aligned_to(workspace, 16))))
+        return ECQ_ERR_ARG;
+    int type = d_out->dtype;
+    if (!same_type(type, sum) || !same_type(type, d_sum) || !same_type(type, d_x)) return ECQ_ERR_ARG;
+    int sms = 0;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (rows == 0) {
+        if (!d_weight) return ECQ_OK;
+        return launch_act8(act8_add_kernel, (uint32_t)((cols + 31) / 32), 512, 0, 0, st, (const float*)nullptr, 0u, (uint32_t)cols, d_weight);
+    }
+    if (sm_count(sms) != ECQ_OK) return ECQ_ERR_CUDA;
+    const RowShape s = row_shape(rows, cols, sms);
+    const uint32_t grid = grad_grid(rows, s, sms), count = grid * (s.per_cta / s.per_row);
+    if (d_weight && workspace_bytes < (uint64_t)count * cols * sizeof(float)) return ECQ_ERR_ARG;
+    Act8NormGrad P = {};
+    P.s = act8_mat(sum, cols);
+    P.d_out = act8_mat(d_out, cols);
+    P.d_sum = act8_mat(d_sum, cols);
+    P.d_x = act8_mat(d_x, cols);
+    P.weight = weight;
+    P.weight_dtype = weight_dtype;
+    P.rstd = rstd;
+    P.sums = d_weight ? static_cast<float*>(workspace) : nullptr;
+    P.rows = (uint32_t)rows;
+    P.cols = (uint32_t)cols;
+    P.per_row = s.per_row;
+    P.inv_cols = (float)(1.0 / (double)cols);
+    const bool coded = sum->dtype >= 3;
+    int rc;
+    switch (type) {
+        case ECQ_F32: rc = launch_norm_grad<float>(P, s, grid, coded, st); break;
+        case ECQ_BF16: rc = launch_norm_grad<__nv_bfloat16>(P, s, grid, coded, st); break;
+        default: rc = launch_norm_grad<__half>(P, s, grid, coded, st); break;
+    }
+    if (rc != ECQ_OK || !d_weight) return rc;
+    return launch_act8(act8_add_kernel, (uint32_t)((cols + 31) / 32), 512, 0, 0, st, (const float*)P.sums, count, (uint32_t)cols, d_weight);
+}
+
+}  // extern "C"

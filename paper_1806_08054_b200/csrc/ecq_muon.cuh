@@ -8,6 +8,7 @@
 
 #include "ecq_common.cuh"
 #include "ecq_elem.cuh"
+#include "ecq_tensor.cuh"
 
 namespace ecq {
 
@@ -319,13 +320,6 @@ __global__ void __launch_bounds__(kMuonPrepThreads, 5) muon_prepare_kernel(const
 
 // ---- tensor-core products --------------------------------------------------------------------
 
-// Shared-memory descriptor of an operand without swizzle: units of eight rows of 16 bytes, 128 bytes
-// each.  `lead` is the byte distance from a unit to the next one along K, `step` to the next one
-// along M or N.
-__device__ __forceinline__ uint64_t umma_desc(uint32_t addr, uint32_t lead, uint32_t step) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(step >> 4) << 32) | (1ull << 46);
-}
-
 template <int CG>
 __device__ __forceinline__ void umma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     if (CG == 1)
@@ -338,83 +332,6 @@ __device__ __forceinline__ void umma_f16(uint32_t d, uint64_t a, uint64_t b, uin
                      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
                      "r"(idesc), "r"((uint32_t)add)
                      : "memory");
-}
-
-// Arrive on a barrier (of both CTAs of a pair) when every product issued so far has completed.
-template <int CG>
-__device__ __forceinline__ void umma_commit(uint32_t bar) {
-    if (CG == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                     ::"r"(bar), "h"((uint16_t)3)
-                     : "memory");
-}
-
-template <int CG>
-__device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t cols) {
-    if (CG == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    } else {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-    }
-}
-template <int CG>
-__device__ __forceinline__ void tmem_free(uint32_t base, uint32_t cols) {
-    if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols));
-    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols));
-}
-
-__device__ __forceinline__ void tmem_load32(uint32_t addr, float* v) {
-    uint32_t* r = reinterpret_cast<uint32_t*>(v);
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
-        "%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
-__device__ __forceinline__ void tmem_load16(uint32_t addr, float* v) {
-    uint32_t* r = reinterpret_cast<uint32_t*>(v);
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
-__device__ __forceinline__ void tcgen05_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tcgen05_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ uint32_t cta_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void pair_sync() {
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-// The same shared-memory location in another CTA of the cluster; in its first.
-__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t cta) {
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(cta));
-    return a;
-}
-__device__ __forceinline__ uint32_t leader_addr(uint32_t addr) {
-    uint32_t a;
-    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(addr));
-    return a;
-}
-__device__ __forceinline__ void leader_arrive(uint32_t leader_bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
 }
 
 // Eight pieces of a tile's 128 or 64 rows (from the unit-th eight on) into this CTA's shared memory; in a pair the bytes are counted on the first
@@ -506,28 +423,6 @@ struct MuonShape {
     static_assert(!KS || (CG == 1 && TN == 64), "");
 };
 
-// Waits that give up: the limit is per wait, and one that ran out ends all others soon.
-__device__ __forceinline__ bool muon_wait(uint32_t bar, uint32_t parity, uint32_t limit, volatile uint32_t* stop) {
-    for (uint32_t it = 0; it < limit; ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (*stop) return false;
-    }
-    *stop = 1;
-    return false;
-}
-// The same where the other CTA of a pair arrives and its writes are read.
-__device__ __forceinline__ bool muon_wait_pair(uint32_t bar, uint32_t parity, uint32_t limit, volatile uint32_t* stop) {
-    for (uint32_t it = 0; it < limit; ++it) {
-        uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\t"
-                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-                     "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return true;
-        if (*stop) return false;
-    }
-    *stop = 1;
-    return false;
-}
 // Until `need` parts of a matrix's tiles are finished; then their results may be loaded.
 __device__ __forceinline__ bool muon_wait_done(const unsigned long long* done, unsigned long long need, uint32_t limit,
                                                volatile uint32_t* stop, uint32_t pause) {
@@ -548,15 +443,6 @@ __device__ __forceinline__ bool muon_wait_done(const unsigned long long* done, u
 // Place of the 16 bytes with columns 8 c .. 8 c + 7 of row r in a block of 64-byte rows: neither
 // eight lanes with a row each nor eight with two whole rows meet in a bank.
 __device__ __forceinline__ uint32_t muon_swizzle(uint32_t r, uint32_t c) { return r * 64u + ((c ^ ((r >> 1) & 3u)) << 4); }
-
-__device__ __forceinline__ uint4 lds16(uint32_t addr) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
-    return v;
-}
-__device__ __forceinline__ void sts16(uint32_t addr, uint4 v) {
-    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
 
 // A row's 32 columns of a block: four pieces.  (Reads of what other SMs have written come behind an
 // acquire.)
@@ -659,15 +545,6 @@ __device__ __forceinline__ void muon_out_wide(const MuonIterate& P, const MuonMa
     }
 }
 
-// One lane of a converged warp, in a form from which the compiler can tell that it is one: TMA and
-// tcgen05 instructions take their operands from uniform registers, and behind a plain comparison of
-// the lane's number each of them costs about 0.1 us to issue.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
-}
-
 // Every step of every matrix in one launch.  Tiles are taken from a counter in a fixed order; each
 // waits until the tiles that its operands come from are finished.  Those are earlier in the order,
 // so they have been taken by CTAs that are running: some tile can always go on, whatever number
@@ -739,28 +616,28 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
     // n-th tile of this CTA (or pair); false when a wait ran out
     auto take = [&](uint32_t n, uint32_t& t) {
         const uint32_t q = n % kMuonQueue;
-        if (!muon_wait(q_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)) return false;
+        if (!wait_or_stop(q_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)) return false;
         t = *reinterpret_cast<volatile uint32_t*>(&queue[q]);
         return true;
     };
     auto taken = [&](uint32_t n) { mbar_arrive(q_empty + 8 * (n % kMuonQueue)); };
     auto give = [&](uint32_t n, uint32_t t) {
         const uint32_t q = n % kMuonQueue;
-        if (!muon_wait(q_empty + 8 * q, ((n / kMuonQueue) & 1) ^ 1, limit, &stop)) return false;
+        if (!wait_or_stop(q_empty + 8 * q, ((n / kMuonQueue) & 1) ^ 1, limit, &stop)) return false;
         *reinterpret_cast<volatile uint32_t*>(&queue[q]) = t;
         mbar_arrive(q_full + 8 * q);
         return true;
     };
     auto pass = [&](uint32_t n, uint32_t t) {                          // by the first CTA
         const uint32_t q = n % kMuonQueue;
-        if (!muon_wait_pair(pass_empty + 8 * q, ((n / kMuonQueue) & 1) ^ 1, limit, &stop)) return false;
+        if (!wait_pair_or_stop(pass_empty + 8 * q, ((n / kMuonQueue) & 1) ^ 1, limit, &stop)) return false;
         asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_addr(smem_u32(&passed[q]), 1)), "r"(t) : "memory");
         leader_arrive(peer_addr(pass_full + 8 * q, 1));
         return true;
     };
     auto receive = [&](uint32_t n, uint32_t& t) {                      // by the second
         const uint32_t q = n % kMuonQueue;
-        if (!muon_wait_pair(pass_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)) return false;
+        if (!wait_pair_or_stop(pass_full + 8 * q, (n / kMuonQueue) & 1, limit, &stop)) return false;
         t = *reinterpret_cast<volatile uint32_t*>(&passed[q]);
         leader_arrive(leader_addr(pass_empty + 8 * q));
         return true;
@@ -812,7 +689,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                 const uint32_t k1 = steps_to(kb);
                 for (uint32_t k = steps_from(kb); k < k1; ++k, ++it) {
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
-                    if (!muon_wait(empty + 8 * s, ph ^ 1, limit, &stop)) { ok = false; break; }
+                    if (!wait_or_stop(empty + 8 * s, ph ^ 1, limit, &stop)) { ok = false; break; }
                     const uint32_t bar = CG == 1 ? full + 8 * s : leader_addr(full + 8 * s);
                     const uint32_t da = ring + s * S::kStageBytes, db = da + S::kHalves * S::kBytesA;
                     if (first) {
@@ -872,13 +749,13 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                 const uint32_t k0 = steps_from(kb), k1 = steps_to(kb);
                 for (uint32_t k = k0; k < k1; ++k, ++it) {
                     if (in_chunk == 0) {
-                        ok = CG == 1 ? muon_wait(acc_empty + 8 * (acc & 1), ((acc >> 1) & 1) ^ 1, limit, &stop)
-                                     : muon_wait_pair(acc_empty + 8 * (acc & 1), ((acc >> 1) & 1) ^ 1, limit, &stop);
+                        ok = CG == 1 ? wait_or_stop(acc_empty + 8 * (acc & 1), ((acc >> 1) & 1) ^ 1, limit, &stop)
+                                     : wait_pair_or_stop(acc_empty + 8 * (acc & 1), ((acc >> 1) & 1) ^ 1, limit, &stop);
                         if (!ok) break;
                         d = tmem + (acc & 1) * S::kAccCols;
                     }
                     const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1;
-                    if (!muon_wait(full + 8 * s, ph, limit, &stop)) { ok = false; break; }
+                    if (!wait_or_stop(full + 8 * s, ph, limit, &stop)) { ok = false; break; }
                     tcgen05_after_sync();
                     const uint32_t a0 = ring + s * S::kStageBytes, b0 = a0 + S::kHalves * S::kBytesA;
                     const uint64_t da = umma_desc(a0, a_lead, 128), db = umma_desc(b0, b_lead, b_step);
@@ -913,7 +790,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                 taken(n);
                 if (t >= P.n_tasks) break;
                 const uint32_t mat = P.tasks[t].mat;
-                if (!muon_wait(stored + 8 * (n & 1), (n >> 1) & 1, limit, &stop)) break;
+                if (!wait_or_stop(stored + 8 * (n & 1), (n >> 1) & 1, limit, &stop)) break;
                 asm volatile("red.release.gpu.global.add.u64 [%0], %1;" ::"l"(P.done + mat), "l"(1ull) : "memory");
             }
         }
@@ -985,7 +862,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
 #pragma unroll
                 for (uint32_t i = 0; i < S::kCols; ++i) sum[SPLIT ? i : 0] = 0.f;
                 for (uint32_t chunk = 0; chunk < (steps + kMuonChunk - 1) / kMuonChunk; ++chunk, ++acc) {
-                    ok = __all_sync(~0u, muon_wait(acc_full + 8 * (acc & 1), (acc >> 1) & 1, limit, &stop));
+                    ok = __all_sync(~0u, wait_or_stop(acc_full + 8 * (acc & 1), (acc >> 1) & 1, limit, &stop));
                     if (!ok) break;
                     tcgen05_after_sync();
 #pragma unroll
@@ -1005,7 +882,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                     }
                 }
             } else if (steps) {
-                ok = __all_sync(~0u, muon_wait(acc_full + 8 * (acc & 1), (acc >> 1) & 1, limit, &stop));
+                ok = __all_sync(~0u, wait_or_stop(acc_full + 8 * (acc & 1), (acc >> 1) & 1, limit, &stop));
                 tcgen05_after_sync();
             }
             if (!ok) break;
@@ -1034,7 +911,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                         release();
                     }
                 }
-                ok = __all_sync(~0u, muon_wait_pair(share_empty + 8 * quad, (n & 1) ^ 1, limit, &stop));
+                ok = __all_sync(~0u, wait_pair_or_stop(share_empty + 8 * quad, (n & 1) ^ 1, limit, &stop));
                 if (!ok) break;
                 const uint32_t to = peer_addr(share, half);
                 const uint32_t bar = peer_addr(share_full + 8 * quad, half);
@@ -1048,7 +925,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
             }
 
             if (KS) {
-                ok = __all_sync(~0u, muon_wait_pair(share_full + 8 * quad, n & 1, limit, &stop));
+                ok = __all_sync(~0u, wait_pair_or_stop(share_full + 8 * quad, n & 1, limit, &stop));
                 if (!ok) break;
             }
 
@@ -1222,7 +1099,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
             if (!SPLIT && steps) release();
             __syncwarp();
             // the signal warp does the rest; the barrier's last use, two tiles ago, is over first
-            if (lane == 0 && muon_wait(stored + 8 * (n & 1), ((n >> 1) & 1) ^ 1, limit, &stop)) mbar_arrive(stored + 8 * (n & 1));
+            if (lane == 0 && wait_or_stop(stored + 8 * (n & 1), ((n >> 1) & 1) ^ 1, limit, &stop)) mbar_arrive(stored + 8 * (n & 1));
             // and the other may send the next tile's sums: last, as this release waits for the results
             // on their way to memory (before them: 1.2 us more a product)
             if (KS && lane == 0) leader_arrive(peer_addr(share_empty + 8 * quad, cta ^ 1));
