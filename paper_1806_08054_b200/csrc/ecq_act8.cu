@@ -32,6 +32,8 @@ int launch_tiles(Act8Tiles& P, uint64_t rows, uint64_t cols, int plain, bool cod
     P.rows = (uint32_t)rows;
     P.cols = (uint32_t)cols;
     P.tiles_across = (uint32_t)((cols + 127) / 128);
+    P.wide = 1;
+    for (const Act8Mat* m : {&P.in[0], &P.in[1], &P.d, &P.plain[0], &P.plain[1]}) P.wide &= !m->data || m->wide;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     switch (plain) {
         case ECQ_F32: return launch_tiles<OP, float>(P, coded, st);
@@ -205,6 +207,8 @@ int ecq_act8_norm(uint64_t rows, uint64_t cols, const ecq_act8_matrix* x, const 
     P.per_row = s.per_row;
     P.eps = eps;
     P.inv_cols = (float)(1.0 / (double)cols);
+    P.full = cols % 8 == 0;
+    for (const Act8Mat* m : {&P.x, &P.residual, &P.sum, &P.y}) P.full &= !m->data || m->wide;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     switch (type) {
         case ECQ_F32: return launch_norm<float>(P, s, sms, st);
@@ -253,6 +257,8 @@ int ecq_act8_norm_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* sum,
     P.cols = (uint32_t)cols;
     P.per_row = s.per_row;
     P.inv_cols = (float)(1.0 / (double)cols);
+    P.full = cols % 8 == 0;
+    for (const Act8Mat* m : {&P.s, &P.d_out, &P.d_sum, &P.d_x}) P.full &= !m->data || m->wide;
     const bool coded = sum->dtype >= 3;
     int rc;
     switch (type) {

@@ -31,61 +31,85 @@ struct Act8Mat {
     int wide;                            // rows begin on 16-byte boundaries
 };
 
-// Scale byte of a block by the bit pattern of its largest magnitude; what entries are multiplied by.
+// The scale byte is found from the bit pattern of a magnitude: adding 2^21 - 1 carries into the exponent
+// exactly where the mantissa is above 1.75, the limit of both types.  It grows with the magnitude, so the
+// largest byte of a block's parts is the block's.  NaN and Inf give 255.
 __device__ __forceinline__ uint32_t act8_byte(uint32_t amax, int dtype) {
-    if (amax >= 0x7F800000u) return 255u;
-    const int b = (int)(amax >> 23) - (dtype == 3 ? 8 : 15) + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    return b > 0 ? (uint32_t)b : 0u;
+    const int b = (int)((amax + 0x1FFFFFu) >> 23) - (dtype == 3 ? 8 : 15);
+    return amax >= 0x7F800000u ? 255u : (uint32_t)max(b, 0);
 }
+// What entries are multiplied by, to and from 8 bits.
 __device__ __forceinline__ float act8_down(uint32_t byte) {
-    return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((254u - byte) << 23);
+    return __uint_as_float(byte == 255u ? 0x7FC00000u : (254u - byte) << 23);
 }
 __device__ __forceinline__ float act8_up(uint32_t byte) {
     return __uint_as_float(byte == 255u ? 0x7FC00000u : byte ? byte << 23 : 0x00400000u);
 }
 
-__device__ __forceinline__ uint32_t act8_pair(float lo, float hi, int dtype) {
-    uint16_t r;
-    if (dtype == 3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+// Larger of magnitudes; NaN wins.
+__device__ __forceinline__ float top3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-__device__ __forceinline__ uint32_t act8_quad(const float* x, float by, int dtype) {
-    float a, b, c, d;
+__device__ __forceinline__ uint32_t act8_largest(const float* x) {
+    return __float_as_uint(top3(top3(top3(x[0], x[1], x[2]), x[3], x[4]), top3(x[5], x[6], x[7]), 0.f));
+}
+
+__device__ __forceinline__ uint16_t act8_e4m3(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint16_t act8_e5m2(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// N entries times `by` in 8 bits, four a word.  (Branches on the type lie around as much as possible: a
+// conversion that is predicated on it is issued all the same.)
+template <int N>
+__device__ __forceinline__ void act8_code(const float* x, float by, int dtype, uint32_t* w) {
+    float y[N];
     const uint64_t by2 = pack2(by, by);
-    unpack2(mul2(pack2(x[0], x[1]), by2), a, b);
-    unpack2(mul2(pack2(x[2], x[3]), by2), c, d);
-    return act8_pair(a, b, dtype) | act8_pair(c, d, dtype) << 16;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) unpack2(mul2(pack2(x[i], x[i + 1]), by2), y[i], y[i + 1]);
+    if (dtype == 3) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) w[i / 4] = act8_e4m3(y[i], y[i + 1]) | (uint32_t)act8_e4m3(y[i + 2], y[i + 3]) << 16;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) w[i / 4] = act8_e5m2(y[i], y[i + 1]) | (uint32_t)act8_e5m2(y[i + 2], y[i + 3]) << 16;
+    }
 }
-__device__ __forceinline__ void act8_unpair(uint32_t two, int dtype, float by, float* x) {
-    uint32_t h;
-    if (dtype == 3) asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-    else asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    unpack2(mul2(pack2(f.x, f.y), pack2(by, by)), x[0], x[1]);
+// And back.
+__device__ __forceinline__ void act8_decode8(uint2 q, int dtype, float by, float* x) {
+    const uint32_t two[4] = {q.x & 0xFFFFu, q.x >> 16, q.y & 0xFFFFu, q.y >> 16};
+    uint32_t h[4];
+    if (dtype == 3) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h[i]) : "h"((uint16_t)two[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h[i]) : "h"((uint16_t)two[i]));
+    }
+    const uint64_t by2 = pack2(by, by);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        unpack2(mul2(pack2(f.x, f.y), by2), x[2 * i], x[2 * i + 1]);
+    }
 }
 
-__device__ __forceinline__ uint32_t act8_largest(const float* x, uint32_t m) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-    return m;
-}
-// Of the 16 lanes that have a block.
-__device__ __forceinline__ uint32_t act8_block_max(uint32_t m) {
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(~0u, m, o));
-    return m;
-}
-
-// Eight consecutive entries of a row as they lie in memory.
+// Eight consecutive entries of a row as they lie in memory (of 8 bits with their block's scale byte).  FULL:
+// all eight are inside the matrix and its rows begin on 16-byte boundaries; otherwise `n` of them are
+// and the others are zeros.
 template <typename T> struct Raw8 { uint4 w[sizeof(T) / 2]; };
 template <> struct Raw8<uint8_t> { uint2 w; uint32_t byte; };
 
-// `n` of them are inside the matrix; the others are zeros.
-template <typename T>
-__device__ __forceinline__ void get8(const Act8Mat& m, uint32_t row, uint32_t col, uint32_t n, Raw8<T>& r) {
-    const unsigned char* p = m.data + row * m.stride + (uint64_t)col * sizeof(T);
-    if (n == 8 && m.wide) {
+template <bool FULL, typename T>
+__device__ __forceinline__ void get8(const unsigned char* p, const uint8_t*, uint32_t n, bool wide, Raw8<T>& r) {
+    if (FULL || (n == 8 && wide)) {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = *(reinterpret_cast<const uint4*>(p) + i);
         return;
@@ -96,15 +120,15 @@ __device__ __forceinline__ void get8(const Act8Mat& m, uint32_t row, uint32_t co
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = *(reinterpret_cast<const uint4*>(e) + i);
 }
-template <>
-__device__ __forceinline__ void get8<uint8_t>(const Act8Mat& m, uint32_t row, uint32_t col, uint32_t n, Raw8<uint8_t>& r) {
-    const unsigned char* p = m.data + row * m.stride + col;
-    r.byte = n ? m.scales[act8_scale_at(row, col >> 7, m.groups)] : 127u;
-    if (n == 8) {
+template <bool FULL>
+__device__ __forceinline__ void get8(const unsigned char* p, const uint8_t* scale, uint32_t n, bool, Raw8<uint8_t>& r) {
+    if (FULL || n == 8) {
         r.w = *reinterpret_cast<const uint2*>(p);
+        r.byte = *scale;
         return;
     }
     r.w = make_uint2(0, 0);
+    r.byte = n ? *scale : 127u;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i)
         if (i < n) (i < 4 ? r.w.x : r.w.y) |= (uint32_t)p[i] << (8 * (i & 3));
@@ -115,19 +139,11 @@ __device__ __forceinline__ void widen8(const Raw8<T>& r, int, float* x) {
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) Elem<T>::widen(r.w[i], x + i * Elem<T>::kPer16);
 }
-template <>
-__device__ __forceinline__ void widen8<uint8_t>(const Raw8<uint8_t>& r, int dtype, float* x) {
-    const float by = act8_up(r.byte);
-    act8_unpair(r.w.x, dtype, by, x);
-    act8_unpair(r.w.x >> 16, dtype, by, x + 2);
-    act8_unpair(r.w.y, dtype, by, x + 4);
-    act8_unpair(r.w.y >> 16, dtype, by, x + 6);
-}
+__device__ __forceinline__ void widen8(const Raw8<uint8_t>& r, int dtype, float* x) { act8_decode8(r.w, dtype, act8_up(r.byte), x); }
 
-template <typename T>
-__device__ __forceinline__ void put8(const Act8Mat& m, uint32_t row, uint32_t col, uint32_t n, const float* x) {
-    unsigned char* p = m.data + row * m.stride + (uint64_t)col * sizeof(T);
-    if (n == 8 && m.wide) {
+template <bool FULL, typename T>
+__device__ __forceinline__ void put8(unsigned char* p, uint32_t n, bool wide, const float* x) {
+    if (FULL || (n == 8 && wide)) {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i)
             *(reinterpret_cast<uint4*>(p) + i) = Elem<T>::narrow(x + i * Elem<T>::kPer16);
@@ -138,24 +154,29 @@ __device__ __forceinline__ void put8(const Act8Mat& m, uint32_t row, uint32_t co
         if (i < n) Elem<T>::store(reinterpret_cast<T*>(p) + i, x[i]);
 }
 
-// Eight entries and, from the first lane of a block, its scale, by the block's largest magnitude.
-__device__ __forceinline__ void put8_coded(const Act8Mat& m, uint32_t row, uint32_t col, uint32_t n, const float* x,
-                                           uint32_t block_max) {
-    if (!n) return;
-    const uint32_t byte = act8_byte(block_max, m.dtype);
-    const float by = act8_down(byte);
-    unsigned char* p = m.data + row * m.stride + col;
-    const uint2 w = make_uint2(act8_quad(x, by, m.dtype), act8_quad(x + 4, by, m.dtype));
-    if (n == 8) {
-        *reinterpret_cast<uint2*>(p) = w;
+// Eight entries in 8 bits by their block's scale byte, and from the first of the block's lanes the byte.
+template <bool FULL>
+__device__ __forceinline__ void put8_coded(unsigned char* p, uint8_t* scale, uint32_t n, bool first, int dtype, uint32_t byte,
+                                           const float* x) {
+    uint32_t w[2];
+    act8_code<8>(x, act8_down(byte), dtype, w);
+    if (FULL || n == 8) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     } else {
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i)
-            if (i < n) p[i] = (unsigned char)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+            if (i < n) p[i] = (unsigned char)(w[i >> 2] >> (8 * (i & 3)));
     }
-    if ((col & 127u) == 0) m.scales[act8_scale_at(row, col >> 7, m.groups)] = (uint8_t)byte;
+    if (first && (FULL || n)) *scale = (uint8_t)byte;
 }
 
 __device__ __forceinline__ uint32_t inside(uint32_t col, uint32_t cols) { return col >= cols ? 0u : min(8u, cols - col); }
+
+// The 16 lanes that have a block agree on its scale byte: two blocks' bytes in the halves of a word.
+__device__ __forceinline__ uint32_t act8_agree(uint32_t two) {
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) two = __vmaxu2(two, __shfl_xor_sync(~0u, two, o));
+    return two;
+}
 
 }  // namespace ecq

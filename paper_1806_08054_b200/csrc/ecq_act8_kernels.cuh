@@ -23,6 +23,7 @@ struct Act8Tiles {
     Act8Mat plain[2], q[2], qt[2];       // results (data NULL: not wanted): h, or d_gate and d_up
     Act8Mat kept[2];                     // gate and up in 8 bits
     uint32_t rows, cols, tiles_across;
+    int wide;                            // rows of all plain matrices begin on 16-byte boundaries
 };
 
 // 1 / (1 + exp(-x)); WIDE: the rounding of x log2(e) is added back, which shows in 32 bits alone.
@@ -40,115 +41,193 @@ __device__ __forceinline__ float act8_sigmoid(float x) {
     return y;
 }
 
-// Writes a thread's 4 x 8 results of a tile.
-template <typename T>
-__device__ __forceinline__ void act8_finish(const Act8Mat& plain, const Act8Mat& q, const Act8Mat& qt, uint32_t rows, uint32_t cols,
-                                            uint32_t row0, uint32_t col0, const float (&v)[4][8], unsigned char* turned,
-                                            uint32_t (*part)[128], uint32_t* top) {
-    const uint32_t tid = threadIdx.x, cg = tid & 15u, rg = tid >> 4, col = col0 + 8 * cg, n = inside(col, cols);
-    if (plain.data || q.data) {
+// A thread's place in a tile of a matrix: four rows, eight columns.
+struct Act8Place {
+    uint32_t rows, n;                    // rows and columns that are inside
+    uint32_t row, col;                   // the first
+};
+
+template <bool FULL, typename T>
+__device__ __forceinline__ void act8_put_plain(const Act8Mat& m, const Act8Place& at, const float (&v)[4][8]) {
+    unsigned char* p = m.data + at.row * m.stride + (uint64_t)at.col * sizeof(T);
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            const uint32_t row = row0 + 4 * rg + j, m = row < rows ? n : 0;
-            if (plain.data && m) put8<T>(plain, row, col, m, v[j]);
-            if (q.data) put8_coded(q, row, col, m, v[j], act8_block_max(act8_largest(v[j], 0)));
-        }
-    }
-    if (!qt.data) return;
+    for (uint32_t j = 0; j < 4; ++j, p += m.stride)
+        if (FULL || j < at.rows) put8<FULL, T>(p, at.n, m.wide, v[j]);
+}
+
+// Two of a thread's rows, the j-th and the next.
+template <bool FULL>
+__device__ __forceinline__ void act8_put_coded(const Act8Mat& m, const Act8Place& at, uint32_t j, const float* v, const float* w) {
+    const uint32_t bytes = act8_agree(act8_byte(act8_largest(v), m.dtype) | act8_byte(act8_largest(w), m.dtype) << 16);
+    unsigned char* p = m.data + (at.row + j) * m.stride + at.col;
+    uint8_t* s = m.scales + act8_scale_at(at.row, at.col >> 7, m.groups) + 16 * j;   // four rows never leave a group of 32
+    const bool first = (at.col & 127u) == 0;
+    if (FULL || j < at.rows) put8_coded<FULL>(p, s, at.n, first, m.dtype, bytes & 255u, v);
+    if (FULL || j + 1 < at.rows) put8_coded<FULL>(p + m.stride, s + 16, at.n, first, m.dtype, bytes >> 16, w);
+}
+
+template <bool FULL, typename T>
+__device__ __forceinline__ void act8_get(const Act8Mat& m, const Act8Place& at, Raw8<T> (&r)[4]) {
+    const unsigned char* p = m.data + at.row * m.stride + (uint64_t)at.col * sizeof(T);
+    const uint8_t* s = sizeof(T) == 1 ? m.scales + act8_scale_at(at.row, at.col >> 7, m.groups) : nullptr;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j, p += m.stride, s += 16) get8<FULL>(p, s, FULL || j < at.rows ? at.n : 0, m.wide, r[j]);
+}
+
+// A thread's 4 x 8 results in 8 bits transposed; the whole CTA.
+struct Act8Turn {
+    unsigned char turned[128 * 128];
+    uint32_t part[kActThreads / 32][128];
+    float down[128];
+};
+template <bool FULL>
+__device__ __forceinline__ void act8_put_turned(const Act8Mat& m, const Act8Place& at, uint32_t rows, uint32_t cols,
+                                                const float (&v)[4][8], Act8Turn& t) {
+    const uint32_t tid = threadIdx.x, cg = tid & 15u, rg = tid >> 4, row0 = at.row - 4 * rg, col0 = at.col - 8 * cg;
     // the columns' largest magnitudes: four rows in registers, two groups of rows a warp, 16 warps
+    uint32_t big[8];
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
-        uint32_t m = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) m = max(m, __float_as_uint(v[j][i]) & 0x7FFFFFFFu);
-        m = max(m, __shfl_xor_sync(~0u, m, 16));
-        if ((tid & 16u) == 0) part[tid >> 5][8 * cg + i] = m;
+        const float x = top3(top3(v[0][i], v[1][i], v[2][i]), v[3][i], 0.f);
+        big[i] = __float_as_uint(top3(x, __shfl_xor_sync(~0u, x, 16), 0.f));
+    }
+    if ((tid & 16u) == 0) {
+        uint4* to = reinterpret_cast<uint4*>(&t.part[tid >> 5][8 * cg]);
+        to[0] = make_uint4(big[0], big[1], big[2], big[3]);
+        to[1] = make_uint4(big[4], big[5], big[6], big[7]);
     }
     __syncthreads();
     if (tid < 128) {
-        uint32_t m = 0;
+        uint32_t top = 0;
 #pragma unroll
-        for (uint32_t w = 0; w < kActThreads / 32; ++w) m = max(m, part[w][tid]);
-        const uint32_t byte = act8_byte(m, qt.dtype);
-        top[tid] = byte;
-        if (col0 + tid < cols) qt.scales[act8_scale_at(col0 + tid, row0 >> 7, qt.groups)] = (uint8_t)byte;
+        for (uint32_t w = 0; w < kActThreads / 32; ++w) top = max(top, t.part[w][tid]);
+        const uint32_t byte = act8_byte(top, m.dtype);
+        t.down[tid] = act8_down(byte);
+        if (FULL || col0 + tid < cols) m.scales[act8_scale_at(col0 + tid, row0 >> 7, m.groups)] = (uint8_t)byte;
     }
     __syncthreads();
     // The tile turned in shared memory: column c has 128 bytes, its four-byte words exchanged by the
     // group of eight columns so that neither a warp's words nor its 16-byte reads meet in a bank.
+    float down[8];
+    Elem<float>::widen(*reinterpret_cast<const uint4*>(t.down + 8 * cg), down);
+    Elem<float>::widen(*reinterpret_cast<const uint4*>(t.down + 8 * cg + 4), down + 4);
+    uint32_t* to = reinterpret_cast<uint32_t*>(t.turned + 8 * cg * 128u + ((rg ^ (2 * cg)) << 2));
+    float y[8][4];
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
-        const uint32_t c = 8 * cg + i;
-        const float x[4] = {v[0][i], v[1][i], v[2][i], v[3][i]};
-        *reinterpret_cast<uint32_t*>(turned + c * 128u + ((rg ^ (2 * cg)) << 2)) = act8_quad(x, act8_down(top[c]), qt.dtype);
+        const uint64_t by2 = pack2(down[i], down[i]);
+        unpack2(mul2(pack2(v[0][i], v[1][i]), by2), y[i][0], y[i][1]);
+        unpack2(mul2(pack2(v[2][i], v[3][i]), by2), y[i][2], y[i][3]);
+    }
+    if (m.dtype == 3) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) to[32 * i] = act8_e4m3(y[i][0], y[i][1]) | (uint32_t)act8_e4m3(y[i][2], y[i][3]) << 16;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) to[32 * i] = act8_e5m2(y[i][0], y[i][1]) | (uint32_t)act8_e5m2(y[i][2], y[i][3]) << 16;
     }
     __syncthreads();
+    const uint32_t piece = tid & 7u, left = FULL ? 128u : row0 + 16 * piece < rows ? rows - (row0 + 16 * piece) : 0;
 #pragma unroll
     for (uint32_t p = 0; p < 2; ++p) {
-        const uint32_t c = (tid >> 3) + 64 * p, piece = tid & 7u, group = c >> 3;
-        if (col0 + c >= cols || row0 + 16 * piece >= rows) continue;
-        uint4 w = *reinterpret_cast<const uint4*>(turned + c * 128u + ((piece ^ (group >> 1)) << 4));
+        const uint32_t c = (tid >> 3) + 64 * p, group = c >> 3;
+        if (!FULL && (col0 + c >= cols || !left)) continue;
+        uint4 w = *reinterpret_cast<const uint4*>(t.turned + c * 128u + ((piece ^ (group >> 1)) << 4));
         if (group & 1u) w = make_uint4(w.z, w.w, w.x, w.y);
-        unsigned char* to = qt.data + (uint64_t)(col0 + c) * qt.stride + row0 + 16 * piece;
-        const uint32_t left = rows - (row0 + 16 * piece);
+        unsigned char* out = m.data + (uint64_t)(col0 + c) * m.stride + row0 + 16 * piece;
         if (left >= 16) {
-            *reinterpret_cast<uint4*>(to) = w;
+            *reinterpret_cast<uint4*>(out) = w;
         } else {
             const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i)
-                if (i < left) to[i] = (unsigned char)(u[i >> 2] >> (8 * (i & 3)));
+                if (i < left) out[i] = (unsigned char)(u[i >> 2] >> (8 * (i & 3)));
         }
     }
-    __syncthreads();                                                 // before the next results come here
 }
 
 // S: type of the inputs (uint8_t: either of 8 bits), T: of the plain results and of the gradient.
-template <int OP, typename S, typename T>
-__global__ void __launch_bounds__(kActThreads, OP == kActGateGrad ? 1 : 2) act8_tile_kernel(const __grid_constant__ Act8Tiles P) {
-    __shared__ __align__(16) unsigned char turned[128 * 128];
-    __shared__ uint32_t part[kActThreads / 32][128];
-    __shared__ uint32_t top[128];
-    const uint32_t tile_row = blockIdx.x / P.tiles_across, tile_col = blockIdx.x - tile_row * P.tiles_across;
-    const uint32_t row0 = tile_row * 128u, col0 = tile_col * 128u;
-    const uint32_t tid = threadIdx.x, cg = tid & 15u, rg = tid >> 4, col = col0 + 8 * cg, n = inside(col, P.cols);
+template <int OP, typename S, typename T, bool FULL>
+__device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& at, Act8Turn& turn) {
     constexpr bool wide = sizeof(T) == 4;
-    griddep_launch();
-    griddep_wait();
     Raw8<S> a[4], b[4];
     Raw8<T> d[4];
-#pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-        const uint32_t row = row0 + 4 * rg + j, m = row < P.rows ? n : 0;
-        get8<S>(P.in[0], row, col, m, a[j]);
-        if (OP != kActCopy) get8<S>(P.in[1], row, col, m, b[j]);
-        if (OP == kActGateGrad) get8<T>(P.d, row, col, m, d[j]);
-    }
+    act8_get<FULL>(P.in[0], at, a);
+    if (OP != kActCopy) act8_get<FULL>(P.in[1], at, b);
+    if (OP == kActGateGrad) act8_get<FULL>(P.d, at, d);
     float v[4][8], u[OP == kActGateGrad ? 4 : 1][8];
+    if constexpr (OP == kActCopy) {
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-        widen8<S>(a[j], P.in[0].dtype, v[j]);
-        if (OP == kActCopy) continue;
-        float x[8], y[8];
-        widen8<S>(b[j], P.in[1].dtype, x);
-        if (OP == kActGate) {
-            const uint32_t row = row0 + 4 * rg + j, m = row < P.rows ? n : 0;
-            if (P.kept[0].data) put8_coded(P.kept[0], row, col, m, v[j], act8_block_max(act8_largest(v[j], 0)));
-            if (P.kept[1].data) put8_coded(P.kept[1], row, col, m, x, act8_block_max(act8_largest(x, 0)));
+        for (uint32_t j = 0; j < 4; ++j) widen8(a[j], P.in[0].dtype, v[j]);
+    }
+    if constexpr (OP == kActGate) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[j][i] = __fmul_rn(__fmul_rn(v[j][i], act8_sigmoid<wide>(v[j][i])), x[i]);
-        } else {
-            widen8<T>(d[j], 0, y);
+        for (uint32_t j = 0; j < 4; j += 2) {
+            float x[2][8];
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+                widen8(a[j + h], P.in[0].dtype, v[j + h]);
+                widen8(b[j + h], P.in[1].dtype, x[h]);
+            }
+            if (P.kept[0].data) act8_put_coded<FULL>(P.kept[0], at, j, v[j], v[j + 1]);
+            if (P.kept[1].data) act8_put_coded<FULL>(P.kept[1], at, j, x[0], x[1]);
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float g = v[j + h][i];
+                    v[j + h][i] = __fmul_rn(__fmul_rn(g, act8_sigmoid<wide>(g)), x[h][i]);
+                }
+        }
+    }
+    if constexpr (OP == kActGateGrad) {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            float y[8];
+            widen8(a[j], P.in[0].dtype, v[j]);
+            widen8(b[j], P.in[1].dtype, u[j]);
+            widen8(d[j], 0, y);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float g = v[j][i], s = act8_sigmoid<wide>(g), ds = __fmul_rn(y[i], s);
-                u[OP == kActGateGrad ? j : 0][i] = __fmul_rn(ds, g);
-                v[j][i] = __fmul_rn(__fmul_rn(ds, x[i]), __fmaf_rn(g, __fsub_rn(1.f, s), 1.f));
+                v[j][i] = __fmul_rn(__fmul_rn(ds, u[j][i]), __fmaf_rn(g, __fsub_rn(1.f, s), 1.f));
+                u[j][i] = __fmul_rn(ds, g);
             }
         }
     }
-    act8_finish<T>(P.plain[0], P.q[0], P.qt[0], P.rows, P.cols, row0, col0, v, turned, part, top);
-    if constexpr (OP == kActGateGrad) act8_finish<T>(P.plain[1], P.q[1], P.qt[1], P.rows, P.cols, row0, col0, u, turned, part, top);
+    if (P.plain[0].data) act8_put_plain<FULL, T>(P.plain[0], at, v);
+    if (P.q[0].data) {
+        act8_put_coded<FULL>(P.q[0], at, 0, v[0], v[1]);
+        act8_put_coded<FULL>(P.q[0], at, 2, v[2], v[3]);
+    }
+    if (P.qt[0].data) act8_put_turned<FULL>(P.qt[0], at, P.rows, P.cols, v, turn);
+    if constexpr (OP == kActGateGrad) {
+        if (P.plain[1].data) act8_put_plain<FULL, T>(P.plain[1], at, u);
+        if (P.q[1].data) {
+        act8_put_coded<FULL>(P.q[1], at, 0, u[0], u[1]);
+        act8_put_coded<FULL>(P.q[1], at, 2, u[2], u[3]);
+    }
+        if (P.qt[1].data) {
+            __syncthreads();                                         // the first is out of shared memory
+            act8_put_turned<FULL>(P.qt[1], at, P.rows, P.cols, u, turn);
+        }
+    }
+}
+
+template <int OP, typename S, typename T>
+__global__ void __launch_bounds__(kActThreads, OP == kActGateGrad ? 1 : 2) act8_tile_kernel(const __grid_constant__ Act8Tiles P) {
+    __shared__ __align__(16) Act8Turn turn;
+    const uint32_t tile_row = blockIdx.x / P.tiles_across, tile_col = blockIdx.x - tile_row * P.tiles_across;
+    const uint32_t row0 = tile_row * 128u, col0 = tile_col * 128u;
+    Act8Place at;
+    at.row = row0 + 4 * (threadIdx.x >> 4);
+    at.col = col0 + 8 * (threadIdx.x & 15u);
+    at.n = inside(at.col, P.cols);
+    at.rows = at.row < P.rows ? min(4u, P.rows - at.row) : 0;
+    griddep_launch();
+    griddep_wait();
+    if (P.wide && row0 + 128 <= P.rows && col0 + 128 <= P.cols) act8_tile<OP, S, T, true>(P, at, turn);
+    else act8_tile<OP, S, T, false>(P, at, turn);
 }
 
 // ---- norm -----------------------------------------------------------------------------------------
@@ -162,9 +241,35 @@ struct Act8Norm {
     const void* weight;                  // NULL: ones
     float* rstd;
     int weight_dtype;
+    int full;                            // whole vectors: columns in eights, all rows on 16-byte boundaries
     uint32_t rows, cols, per_row;
     float eps, inv_cols;
 };
+
+// Where a row's vectors are.
+__device__ __forceinline__ unsigned char* act8_row(const Act8Mat& m, uint32_t row) { return m.data + row * m.stride; }
+// A row's scale bytes; block b's lies act8_scale_at(0, b, .) further.
+__device__ __forceinline__ uint8_t* act8_row_scales(const Act8Mat& m, uint32_t row) { return m.scales + act8_scale_at(row, 0, m.groups); }
+__device__ __forceinline__ uint32_t act8_block_at(uint32_t block) { return (block >> 2) * 512u + (block & 3u); }
+
+// Vectors of a row in 8 bits, two blocks' scales at a time.
+template <bool FULL, int NV>
+__device__ __forceinline__ void act8_put_row(const Act8Mat& m, uint32_t row, uint32_t t, uint32_t per_row, uint32_t cols, bool real,
+                                             const float (&v)[NV][8]) {
+    uint32_t bytes[(NV + 1) / 2];
+#pragma unroll
+    for (int k = 0; k < NV; k += 2) {
+        const uint32_t low = act8_byte(act8_largest(v[k]), m.dtype), high = k + 1 < NV ? act8_byte(act8_largest(v[k + 1 < NV ? k + 1 : k]), m.dtype) : 0;
+        bytes[k / 2] = act8_agree(low | high << 16);
+    }
+    unsigned char* p = act8_row(m, row) + 8 * t;
+    uint8_t* s = act8_row_scales(m, row);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const uint32_t col = (k * per_row + t) * 8, n = !real ? 0 : FULL ? (col < cols ? 8 : 0) : inside(col, cols);
+        if (n) put8_coded<FULL>(p + k * per_row * 8, s + act8_block_at(col >> 7), n, (t & 15u) == 0, m.dtype, (bytes[k / 2] >> (16 * (k & 1))) & 255u, v[k]);
+    }
+}
 
 __device__ __forceinline__ void act8_weight(const void* w, int dtype, uint32_t col, uint32_t n, float* x) {
 #pragma unroll
@@ -192,56 +297,81 @@ __device__ __forceinline__ float act8_row_sum(float v, uint32_t per_row, float* 
     return v;
 }
 
-template <typename T, int NV>
-__global__ void __launch_bounds__(512) act8_norm_kernel(const __grid_constant__ Act8Norm P) {
-    __shared__ float part[64];
+template <typename T, int NV, bool FULL>
+__device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part) {
     const uint32_t slot = threadIdx.x / P.per_row, t = threadIdx.x - slot * P.per_row, slots = blockDim.x / P.per_row;
-    griddep_launch();
-    griddep_wait();
     float w[NV][8];
+    uint32_t cols[NV];                                               // entries of each vector that are inside
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const uint32_t col = (k * P.per_row + t) * 8;
-        act8_weight(P.weight, P.weight_dtype, col, inside(col, P.cols), w[k]);
+        cols[k] = FULL ? (col < P.cols ? 8 : 0) : inside(col, P.cols);
+        act8_weight(P.weight, P.weight_dtype, col, cols[k], w[k]);
     }
+    const uint32_t step = P.per_row * 8 * (uint32_t)sizeof(T), at = 8 * t * (uint32_t)sizeof(T);
     uint32_t turn = 0;
     for (uint64_t first = (uint64_t)blockIdx.x * slots; first < P.rows; first += (uint64_t)gridDim.x * slots, ++turn) {
         const uint32_t row = (uint32_t)first + slot;
         const bool real = row < P.rows;
         Raw8<T> a[NV], b[NV];
+        const unsigned char *x = act8_row(P.x, row) + at, *r = act8_row(P.residual, row) + at;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const uint32_t col = (k * P.per_row + t) * 8, n = real ? inside(col, P.cols) : 0;
-            get8<T>(P.x, row, col, n, a[k]);
-            if (P.residual.data) get8<T>(P.residual, row, col, n, b[k]);
+            a[k] = {};
+            b[k] = {};
+            if (real && cols[k]) {
+                get8<FULL>(x + k * step, nullptr, cols[k], P.x.wide, a[k]);
+                if (P.residual.data) get8<FULL>(r + k * step, nullptr, cols[k], P.residual.wide, b[k]);
+            }
         }
         float s[NV][8], squares = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            widen8<T>(a[k], 0, s[k]);
-            if (P.residual.data) {
-                float r[8];
-                widen8<T>(b[k], 0, r);
+            float y[8];
+            widen8(a[k], 0, s[k]);
+            widen8(b[k], 0, y);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s[k][i] = __fadd_rn(s[k][i], r[i]);
+            for (int i = 0; i < 8; i += 2) {
+                if (P.residual.data) unpack2(add2(pack2(s[k][i], s[k][i + 1]), pack2(y[i], y[i + 1])), s[k][i], s[k][i + 1]);
+                squares = __fmaf_rn(s[k][i], s[k][i], squares);
+                squares = __fmaf_rn(s[k][i + 1], s[k][i + 1], squares);
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) squares = __fmaf_rn(s[k][i], s[k][i], squares);
         }
+        // what does not need the row's sum is written while the threads wait for each other
+        if (P.sum.data) {
+            unsigned char* to = act8_row(P.sum, row) + at;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (real && cols[k]) put8<FULL, T>(to + k * step, cols[k], P.sum.wide, s[k]);
+        }
+        if (P.sum8.data) act8_put_row<FULL, NV>(P.sum8, row, t, P.per_row, P.cols, real, s);
         squares = act8_row_sum(squares, P.per_row, part, turn);
         const float rstd = __fdiv_rn(1.f, __fsqrt_rn(__fmaf_rn(squares, P.inv_cols, P.eps)));
         if (real && t == 0 && P.rstd) P.rstd[row] = rstd;
+        if (!P.y.data && !P.y8.data) continue;
+        const uint64_t by = pack2(rstd, rstd);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const uint32_t col = (k * P.per_row + t) * 8, n = real ? inside(col, P.cols) : 0;
-            if (P.sum.data && n) put8<T>(P.sum, row, col, n, s[k]);
-            if (P.sum8.data) put8_coded(P.sum8, row, col, n, s[k], act8_block_max(act8_largest(s[k], 0)));
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[k][i] = __fmul_rn(__fmul_rn(s[k][i], rstd), w[k][i]);
-            if (P.y.data && n) put8<T>(P.y, row, col, n, s[k]);
-            if (P.y8.data) put8_coded(P.y8, row, col, n, s[k], act8_block_max(act8_largest(s[k], 0)));
+            for (int i = 0; i < 8; i += 2)
+                unpack2(mul2(mul2(pack2(s[k][i], s[k][i + 1]), by), pack2(w[k][i], w[k][i + 1])), s[k][i], s[k][i + 1]);
+        if (P.y.data) {
+            unsigned char* to = act8_row(P.y, row) + at;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (real && cols[k]) put8<FULL, T>(to + k * step, cols[k], P.y.wide, s[k]);
         }
+        if (P.y8.data) act8_put_row<FULL, NV>(P.y8, row, t, P.per_row, P.cols, real, s);
     }
+}
+
+template <typename T, int NV>
+__global__ void __launch_bounds__(512) act8_norm_kernel(const __grid_constant__ Act8Norm P) {
+    __shared__ float part[64];
+    griddep_launch();
+    griddep_wait();
+    if (P.full) act8_norm_rows<T, NV, true>(P, part);
+    else act8_norm_rows<T, NV, false>(P, part);
 }
 
 // Its gradient.  With n = s rstd and g = d_out w:  d_x = rstd (g - n mean(g n)) + d_sum, and the weight's
@@ -253,24 +383,25 @@ struct Act8NormGrad {
     const float* rstd;
     float* sums;                         // [grid x rows at a time][cols], or NULL
     int weight_dtype;
+    int full;
     uint32_t rows, cols, per_row;
     float inv_cols;
 };
 
-template <typename S, typename T, int NV>
-__global__ void __launch_bounds__(512) act8_norm_grad_kernel(const __grid_constant__ Act8NormGrad P) {
-    __shared__ float part[64];
+template <typename S, typename T, int NV, bool FULL>
+__device__ __forceinline__ void act8_norm_grad_rows(const Act8NormGrad& P, float* part) {
     const uint32_t slot = threadIdx.x / P.per_row, t = threadIdx.x - slot * P.per_row, slots = blockDim.x / P.per_row;
-    griddep_launch();
-    griddep_wait();
     float w[NV][8], dw[NV][8];
+    uint32_t cols[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const uint32_t col = (k * P.per_row + t) * 8;
-        act8_weight(P.weight, P.weight_dtype, col, inside(col, P.cols), w[k]);
+        cols[k] = FULL ? (col < P.cols ? 8 : 0) : inside(col, P.cols);
+        act8_weight(P.weight, P.weight_dtype, col, cols[k], w[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[k][i] = 0.f;
     }
+    const uint32_t step = P.per_row * 8 * (uint32_t)sizeof(T), at = 8 * t * (uint32_t)sizeof(T);
     uint32_t turn = 0;
     for (uint64_t first = (uint64_t)blockIdx.x * slots; first < P.rows; first += (uint64_t)gridDim.x * slots, ++turn) {
         const uint32_t row = (uint32_t)first + slot;
@@ -278,39 +409,51 @@ __global__ void __launch_bounds__(512) act8_norm_grad_kernel(const __grid_consta
         Raw8<S> a[NV];
         Raw8<T> b[NV], c[NV];
         const float rstd = real ? P.rstd[row] : 0.f;
+        const unsigned char* s = act8_row(P.s, row) + 8 * t * sizeof(S);
+        const uint8_t* scales = sizeof(S) == 1 ? act8_row_scales(P.s, row) : nullptr;
+        const unsigned char *d = act8_row(P.d_out, row) + at, *e = act8_row(P.d_sum, row) + at;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const uint32_t col = (k * P.per_row + t) * 8, n = real ? inside(col, P.cols) : 0;
-            get8<S>(P.s, row, col, n, a[k]);
-            get8<T>(P.d_out, row, col, n, b[k]);
-            if (P.d_sum.data) get8<T>(P.d_sum, row, col, n, c[k]);
+            a[k] = {};
+            b[k] = {};
+            c[k] = {};
+            if (real && cols[k]) {
+                const uint8_t* scale = sizeof(S) == 1 ? scales + act8_block_at((k * P.per_row + t) >> 4) : nullptr;
+                get8<FULL>(s + k * P.per_row * 8 * sizeof(S), scale, cols[k], P.s.wide, a[k]);
+                get8<FULL>(d + k * step, nullptr, cols[k], P.d_out.wide, b[k]);
+                if (P.d_sum.data) get8<FULL>(e + k * step, nullptr, cols[k], P.d_sum.wide, c[k]);
+            }
         }
         float normed[NV][8], g[NV][8], dot = 0.f;
+        const uint64_t by = pack2(rstd, rstd);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            widen8<S>(a[k], P.s.dtype, normed[k]);
-            widen8<T>(b[k], 0, g[k]);
+            widen8(a[k], P.s.dtype, normed[k]);
+            widen8(b[k], 0, g[k]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                normed[k][i] = __fmul_rn(normed[k][i], rstd);
-                dw[k][i] = __fmaf_rn(g[k][i], normed[k][i], dw[k][i]);
-                g[k][i] = __fmul_rn(g[k][i], w[k][i]);
+            for (int i = 0; i < 8; i += 2) {
+                const uint64_t n = mul2(pack2(normed[k][i], normed[k][i + 1]), by), o = pack2(g[k][i], g[k][i + 1]);
+                unpack2(n, normed[k][i], normed[k][i + 1]);
+                unpack2(fma2(o, n, pack2(dw[k][i], dw[k][i + 1])), dw[k][i], dw[k][i + 1]);
+                unpack2(mul2(o, pack2(w[k][i], w[k][i + 1])), g[k][i], g[k][i + 1]);
                 dot = __fmaf_rn(g[k][i], normed[k][i], dot);
+                dot = __fmaf_rn(g[k][i + 1], normed[k][i + 1], dot);
             }
         }
         const float mean = __fmul_rn(act8_row_sum(dot, P.per_row, part, turn), P.inv_cols);
         if (!P.d_x.data) continue;
+        unsigned char* to = act8_row(P.d_x, row) + at;
+        const uint64_t less = pack2(-mean, -mean);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const uint32_t col = (k * P.per_row + t) * 8, n = real ? inside(col, P.cols) : 0;
+            if (!real || !cols[k]) continue;
             float x[8];
-            if (P.d_sum.data) widen8<T>(c[k], 0, x);
+            widen8(c[k], 0, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = __fmaf_rn(-normed[k][i], mean, g[k][i]);
-                x[i] = P.d_sum.data ? __fmaf_rn(rstd, d, x[i]) : __fmul_rn(rstd, d);
-            }
-            if (n) put8<T>(P.d_x, row, col, n, x);
+            for (int i = 0; i < 8; i += 2)
+                unpack2(fma2(by, fma2(pack2(normed[k][i], normed[k][i + 1]), less, pack2(g[k][i], g[k][i + 1])), pack2(x[i], x[i + 1])),
+                        x[i], x[i + 1]);
+            put8<FULL, T>(to + k * step, cols[k], P.d_x.wide, x);
         }
     }
     if (!P.sums) return;
@@ -318,10 +461,24 @@ __global__ void __launch_bounds__(512) act8_norm_grad_kernel(const __grid_consta
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const uint32_t col = (k * P.per_row + t) * 8;
+        if (FULL && cols[k]) {
+            *reinterpret_cast<uint4*>(to + col) = Elem<float>::narrow(dw[k]);
+            *reinterpret_cast<uint4*>(to + col + 4) = Elem<float>::narrow(dw[k] + 4);
+            continue;
+        }
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i)
-            if (col + i < P.cols) to[col + i] = dw[k][i];
+            if (i < cols[k]) to[col + i] = dw[k][i];
     }
+}
+
+template <typename S, typename T, int NV>
+__global__ void __launch_bounds__(512) act8_norm_grad_kernel(const __grid_constant__ Act8NormGrad P) {
+    __shared__ float part[64];
+    griddep_launch();
+    griddep_wait();
+    if (P.full) act8_norm_grad_rows<S, T, NV, true>(P, part);
+    else act8_norm_grad_rows<S, T, NV, false>(P, part);
 }
 
 // Columns of `count` vectors added: 32 columns a CTA, 16 threads a column.

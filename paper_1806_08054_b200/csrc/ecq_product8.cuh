@@ -301,7 +301,9 @@ __global__ void __launch_bounds__(ProdPart<TN, SWAP>::kThreads, 1) act8_product_
             for (uint32_t i = 0; i < 4; ++i)
                 if (i < n) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
             top = __reduce_max_sync(~0u, top);
-            const uint32_t byte = act8_byte(top, P.out.dtype), w = act8_quad(y, act8_down(byte), P.out.dtype);
+            const uint32_t byte = act8_byte(top, P.out.dtype);
+            uint32_t w;
+            act8_code<4>(y, act8_down(byte), P.out.dtype, &w);
             unsigned char* to = P.out.data + row * P.out.stride + col;
             if (n == 4) {
                 *reinterpret_cast<uint32_t*>(to) = w;
@@ -475,10 +477,11 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
                     float y[32];
                     fetch(b, y);
 #pragma unroll
-                    for (uint32_t c = 0; c < 2; ++c)
-                        sts16(own + lane * 128u + (((2 * b + c) ^ (lane & 7u)) << 4),
-                              make_uint4(act8_quad(y + 16 * c, by, dtype), act8_quad(y + 16 * c + 4, by, dtype),
-                                         act8_quad(y + 16 * c + 8, by, dtype), act8_quad(y + 16 * c + 12, by, dtype)));
+                    for (uint32_t c = 0; c < 2; ++c) {
+                        uint32_t w[4];
+                        act8_code<16>(y + 16 * c, by, dtype, w);
+                        sts16(own + lane * 128u + (((2 * b + c) ^ (lane & 7u)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                    }
                 }
                 if (shares) release();
                 __syncwarp();
