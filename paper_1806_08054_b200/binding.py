@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Sequence
 
 import torch
@@ -34,11 +35,6 @@ class EcqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
         super().__init__("%s: %s (status %d)" % (where, strerror(status), status))
-
-
-class Act8Matrix(ctypes.Structure):
-    """A matrix of an ecq_act8_* call: ``ecq_act8_matrix`` of ecq.h."""
-    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_uint64), ("scales", ctypes.c_void_p), ("dtype", ctypes.c_int32)]
 
 
 def lib() -> ctypes.CDLL:
@@ -122,7 +118,7 @@ def lib() -> ctypes.CDLL:
         L.ecq_muon_step.restype = i32
         L.ecq_muon_status.argtypes = [vp, vp]
         L.ecq_muon_status.restype = i32
-        mat = ctypes.POINTER(Act8Matrix)
+        mat = vp                                            # the bytes of an ecq_act8_matrix
         L.ecq_act8_scale_bytes.argtypes = [u64, u64]
         L.ecq_act8_scale_bytes.restype = u64
         L.ecq_act8_store.argtypes = [u64, u64, mat, mat, mat, vp]
@@ -630,73 +626,82 @@ def ecq_act8_scale_bytes(rows: int, cols: int) -> int:
     return int(lib().ecq_act8_scale_bytes(rows, cols))
 
 
-def _matrix(m, name: str, shape=None):
-    """A plain tensor [rows, cols], or the pair (q, scales) of a matrix in 8 bits, as the library takes it."""
+_PACK = struct.Struct("@QQQi4x").pack           # ecq_act8_matrix of ecq.h
+
+
+def _matrix(m, name: str, rows: int, cols: int, device: int):
+    """A plain tensor [rows, cols], or the pair (q, scales) of a matrix in 8 bits, as the library takes it: the
+    bytes of an ``ecq_act8_matrix``."""
     if m is None:
         return None
-    scales = None
     if type(m) is tuple or type(m) is list:
         m, scales = m
-    have, stride = m.shape, m.stride()
-    if len(have) != 2 or not m.is_cuda:
-        raise ValueError("%s must be a CUDA tensor of two dimensions, or a pair (q, scales) (there is no CPU path)" % name)
-    if shape is not None and have != shape:
-        raise ValueError("%s must be %d x %d" % (name, *shape))
-    if have[1] > 1 and stride[1] != 1 or (have[0] > 1 and stride[0] < have[1]):
-        raise ValueError("%s must have contiguous rows that do not overlap" % name)
-    where = m.get_device()
-    if scales is None:
+        dtype = _DTYPES8.get(m.dtype)
+        if dtype is None or scales.dtype is not torch.uint8 or not scales.is_contiguous() or scales.get_device() != device or \
+                scales.numel() < ((rows + 127) >> 7) * ((cols + 511) >> 9) << 9:
+            raise ValueError("%s must be (float8_e4m3fn or float8_e5m2, uint8 scales of ecq_act8_scale_bytes), both on "
+                             "the current CUDA device" % name)
+        at = scales.data_ptr()
+    else:
         dtype = _DTYPES.get(m.dtype)
         if dtype is None:
             raise ValueError("%s must be float32, bfloat16 or float16, or a pair (q, scales)" % name)
-        at = None
-    else:
-        dtype = _DTYPES8.get(m.dtype)
-        if dtype is None or scales.dtype is not torch.uint8 or not scales.is_contiguous() or scales.get_device() != where or \
-                scales.numel() < -(-have[0] // 128) * -(-have[1] // 512) * 512:
-            raise ValueError("%s must be (float8_e4m3fn or float8_e5m2, uint8 scales of ecq_act8_scale_bytes on the same device)" % name)
-        at = scales.data_ptr()
-    if where != _current_device():
-        raise ValueError("%s must be on the current device" % name)
-    return Act8Matrix(m.data_ptr(), stride[0] if have[0] > 1 or scales is not None else max(stride[0], have[1]), at, dtype)
+        at = 0
+    if m.get_device() != device:
+        raise ValueError("%s must be on the current CUDA device (there is no CPU path)" % name)
+    if m.shape != (rows, cols):
+        raise ValueError("%s must be %d x %d" % (name, rows, cols))
+    stride, step = m.stride()
+    if (step != 1 and cols > 1) or (stride < cols and rows > 1):
+        raise ValueError("%s must have contiguous rows that do not overlap" % name)
+    return _PACK(m.data_ptr(), stride if rows > 1 else cols + 15 & ~15, at, dtype)
 
 
 def _current_device() -> int:
     return _device() if _device is not None else torch.cuda.current_device()
 
 
-def _like(t):
-    return (t[0] if type(t) is tuple or type(t) is list else t).shape
+def _size(m, name: str):
+    """Rows and columns of a call's first matrix, and the current device."""
+    if type(m) is tuple or type(m) is list:
+        m = m[0]
+    if not m.is_cuda:
+        raise ValueError("%s must be on the current CUDA device (there is no CPU path)" % name)
+    rows, cols = m.shape
+    return rows, cols, _current_device()
 
 
-def _vector(t, dtype, n: int, name: str):
-    if t is not None and t.is_cuda and t.get_device() != _current_device():
-        raise ValueError("%s must be on the current device" % name)
-    return _vec(t, dtype, n, name)
+def _vector(t, dtype, n: int, name: str, device: int):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous entries of %s on the current CUDA device" % (name, n, dtype))
+    return t.data_ptr()
 
 
-def _weight(w, n: int):
+def _weight(w, n: int, device: int):
     if w is None:
         return None, 0
-    if w.dtype not in _DTYPES:
+    dtype = _DTYPES.get(w.dtype)
+    if dtype is None:
         raise ValueError("weight must be float32, bfloat16 or float16")
-    return _vector(w, w.dtype, n, "weight"), _DTYPES[w.dtype]
+    return _vector(w, w.dtype, n, "weight", device), dtype
 
 
 def ecq_act8_store(x, out=None, out_t=None, stream=None) -> None:
     """``x`` (a tensor, or a pair) in 8 bits: ``out`` and, transposed, ``out_t`` are pairs (q, scales) with q a
     [rows, stride] float8 tensor's first columns and uint8 scales of ``ecq_act8_scale_bytes``."""
-    shape = rows, cols = _like(x)
-    rc = (_lib or lib()).ecq_act8_store(rows, cols, _matrix(x, "x"), _matrix(out, "out", shape),
-                                        _matrix(out_t, "out_t", (cols, rows)), _stream(stream))
+    r, c, dev = _size(x, "x")
+    rc = (_lib or lib()).ecq_act8_store(r, c, _matrix(x, "x", r, c, dev), _matrix(out, "out", r, c, dev),
+                                        _matrix(out_t, "out_t", c, r, dev), _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_act8_store")
 
 
 def ecq_act8_load(x8, out: torch.Tensor, stream=None) -> None:
     """The values that the pair ``x8`` stands for."""
-    shape = rows, cols = _like(x8)
-    rc = (_lib or lib()).ecq_act8_load(rows, cols, _matrix(x8, "x8"), _matrix(out, "out", shape), _stream(stream))
+    r, c, dev = _size(x8, "x8")
+    rc = (_lib or lib()).ecq_act8_load(r, c, _matrix(x8, "x8", r, c, dev), _matrix(out, "out", r, c, dev), _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_act8_load")
 
@@ -704,10 +709,11 @@ def ecq_act8_load(x8, out: torch.Tensor, stream=None) -> None:
 def ecq_act8_gate(gate, up, out=None, out8=None, out8_t=None, gate8=None, up8=None, stream=None) -> None:
     """gate * sigmoid(gate) * up, plain, in 8 bits and in 8 bits transposed, and gate and up in 8 bits,
     each where it is given."""
-    shape = rows, cols = _like(gate)
+    r, c, dev = _size(gate, "gate")
     rc = (_lib or lib()).ecq_act8_gate(
-        rows, cols, _matrix(gate, "gate"), _matrix(up, "up", shape), _matrix(out, "out", shape), _matrix(out8, "out8", shape),
-        _matrix(out8_t, "out8_t", (cols, rows)), _matrix(gate8, "gate8", shape), _matrix(up8, "up8", shape), _stream(stream))
+        r, c, _matrix(gate, "gate", r, c, dev), _matrix(up, "up", r, c, dev), _matrix(out, "out", r, c, dev),
+        _matrix(out8, "out8", r, c, dev), _matrix(out8_t, "out8_t", c, r, dev), _matrix(gate8, "gate8", r, c, dev),
+        _matrix(up8, "up8", r, c, dev), _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_act8_gate")
 
@@ -715,13 +721,12 @@ def ecq_act8_gate(gate, up, out=None, out8=None, out8_t=None, gate8=None, up8=No
 def ecq_act8_gate_grad(gate, up, d_out, d_gate=None, d_up=None, d_gate8=None, d_gate8_t=None, d_up8=None, d_up8_t=None,
                        stream=None) -> None:
     """Gradient of :func:`ecq_act8_gate`, from gate and up as they were given or kept."""
-    shape = rows, cols = _like(gate)
-    turned = (cols, rows)
+    r, c, dev = _size(gate, "gate")
     rc = (_lib or lib()).ecq_act8_gate_grad(
-        rows, cols, _matrix(gate, "gate"), _matrix(up, "up", shape), _matrix(d_out, "d_out", shape),
-        _matrix(d_gate, "d_gate", shape), _matrix(d_up, "d_up", shape), _matrix(d_gate8, "d_gate8", shape),
-        _matrix(d_gate8_t, "d_gate8_t", turned), _matrix(d_up8, "d_up8", shape), _matrix(d_up8_t, "d_up8_t", turned),
-        _stream(stream))
+        r, c, _matrix(gate, "gate", r, c, dev), _matrix(up, "up", r, c, dev), _matrix(d_out, "d_out", r, c, dev),
+        _matrix(d_gate, "d_gate", r, c, dev), _matrix(d_up, "d_up", r, c, dev), _matrix(d_gate8, "d_gate8", r, c, dev),
+        _matrix(d_gate8_t, "d_gate8_t", c, r, dev), _matrix(d_up8, "d_up8", r, c, dev),
+        _matrix(d_up8_t, "d_up8_t", c, r, dev), _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_act8_gate_grad")
 
@@ -730,12 +735,12 @@ def ecq_act8_norm(x, residual=None, weight=None, *, eps: float = 1e-6, sum=None,
                   stream=None) -> None:
     """Root-mean-square norm of x + residual: the sum, the norm (plain and in 8 bits each) and the
     rows' factors, each where it is given."""
-    shape = rows, cols = _like(x)
-    w, w_dtype = _weight(weight, cols)
+    r, c, dev = _size(x, "x")
+    w, w_dtype = _weight(weight, c, dev)
     rc = (_lib or lib()).ecq_act8_norm(
-        rows, cols, _matrix(x, "x"), _matrix(residual, "residual", shape), w, w_dtype, eps, _matrix(sum, "sum", shape),
-        _matrix(out, "out", shape), _matrix(out8, "out8", shape), _matrix(sum8, "sum8", shape),
-        _vector(rstd, torch.float32, rows, "rstd"), _stream(stream))
+        r, c, _matrix(x, "x", r, c, dev), _matrix(residual, "residual", r, c, dev), w, w_dtype, eps,
+        _matrix(sum, "sum", r, c, dev), _matrix(out, "out", r, c, dev), _matrix(out8, "out8", r, c, dev),
+        _matrix(sum8, "sum8", r, c, dev), _vector(rstd, torch.float32, r, "rstd", dev), _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_act8_norm")
 
@@ -748,15 +753,14 @@ def ecq_act8_norm_grad_workspace_bytes(rows: int, cols: int) -> int:
 
 def ecq_act8_norm_grad(sum, weight, rstd, d_out, d_x=None, d_weight=None, workspace=None, *, d_sum=None, stream=None) -> None:
     """Gradient of :func:`ecq_act8_norm`, from the sum (a tensor, or the pair that ``sum8`` kept) and ``rstd``."""
-    shape = rows, cols = _like(sum)
-    w, w_dtype = _weight(weight, cols)
-    if workspace is not None and (not workspace.is_cuda or not workspace.is_contiguous() or
-                                  workspace.get_device() != _current_device()):
-        raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
+    r, c, dev = _size(sum, "sum")
+    w, w_dtype = _weight(weight, c, dev)
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
     rc = (_lib or lib()).ecq_act8_norm_grad(
-        rows, cols, _matrix(sum, "sum"), w, w_dtype, _vector(rstd, torch.float32, rows, "rstd"), _matrix(d_out, "d_out", shape),
-        _matrix(d_sum, "d_sum", shape), _matrix(d_x, "d_x", shape), _vector(d_weight, torch.float32, cols, "d_weight"),
-        None if workspace is None else workspace.data_ptr(),
+        r, c, _matrix(sum, "sum", r, c, dev), w, w_dtype, _vector(rstd, torch.float32, r, "rstd", dev),
+        _matrix(d_out, "d_out", r, c, dev), _matrix(d_sum, "d_sum", r, c, dev), _matrix(d_x, "d_x", r, c, dev),
+        _vector(d_weight, torch.float32, c, "d_weight", dev), None if workspace is None else workspace.data_ptr(),
         0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_act8_norm_grad")
@@ -765,12 +769,11 @@ def ecq_act8_norm_grad(sum, weight, rstd, d_out, d_x=None, d_weight=None, worksp
 def ecq_act8_product(a, b, out, add=None, status=None, stream=None) -> None:
     """out = a b^T + add of pairs a [m, k] and b [n, k]; ``out`` is a tensor (``add`` may be the same), or a
     pair where ``add`` is None.  ``status``: an int32 tensor of one entry, set to 2 if an in-kernel wait ran out."""
-    (m, k), (n, k2) = _like(a), _like(b)
-    if k != k2:
-        raise ValueError("a and b must have the same number of columns")
+    m, k, dev = _size(a, "a")
+    n = (b[0] if type(b) is tuple or type(b) is list else b).shape[0]
     rc = (_lib or lib()).ecq_act8_product(
-        m, n, k, _matrix(a, "a"), _matrix(b, "b"), _matrix(add, "add", (m, n)), _matrix(out, "out", (m, n)),
-        _vector(status, torch.int32, 1, "status"), _stream(stream))
+        m, n, k, _matrix(a, "a", m, k, dev), _matrix(b, "b", n, k, dev), _matrix(add, "add", m, n, dev),
+        _matrix(out, "out", m, n, dev), _vector(status, torch.int32, 1, "status", dev), _stream(stream))
     if rc != ECQ_OK:
         raise EcqError(rc, "ecq_act8_product")
 

@@ -82,8 +82,8 @@ __device__ __forceinline__ void act8_code(const float* x, float by, int dtype, u
         for (int i = 0; i < N; i += 4) w[i / 4] = act8_e5m2(y[i], y[i + 1]) | (uint32_t)act8_e5m2(y[i + 2], y[i + 3]) << 16;
     }
 }
-// And back.
-__device__ __forceinline__ void act8_decode8(uint2 q, int dtype, float by, float* x) {
+// And back: unscaled, and times `by`.
+__device__ __forceinline__ void act8_decode8(uint2 q, int dtype, float* x) {
     const uint32_t two[4] = {q.x & 0xFFFFu, q.x >> 16, q.y & 0xFFFFu, q.y >> 16};
     uint32_t h[4];
     if (dtype == 3) {
@@ -93,12 +93,18 @@ __device__ __forceinline__ void act8_decode8(uint2 q, int dtype, float by, float
 #pragma unroll
         for (int i = 0; i < 4; ++i) asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h[i]) : "h"((uint16_t)two[i]));
     }
-    const uint64_t by2 = pack2(by, by);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-        unpack2(mul2(pack2(f.x, f.y), by2), x[2 * i], x[2 * i + 1]);
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
     }
+}
+__device__ __forceinline__ void act8_decode8(uint2 q, int dtype, float by, float* x) {
+    act8_decode8(q, dtype, x);
+    const uint64_t by2 = pack2(by, by);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) unpack2(mul2(pack2(x[i], x[i + 1]), by2), x[i], x[i + 1]);
 }
 
 // Eight consecutive entries of a row as they lie in memory (of 8 bits with their block's scale byte).  FULL:

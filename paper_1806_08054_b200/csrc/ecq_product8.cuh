@@ -20,7 +20,7 @@ namespace ecq {
 // memory for each four blocks.
 
 struct Product8 {
-    CUtensorMap left, right, left_scales, right_scales;
+    CUtensorMap left, right, left_scales, right_scales, result;
     const unsigned char* add;            // C, or NULL
     uint64_t add_stride;                 // bytes
     Act8Mat out;
@@ -32,7 +32,9 @@ struct Product8 {
     uint32_t left_groups, right_groups;  // of scales, along K
     uint32_t formats;                    // of the operands, as bits of the instruction descriptor
     uint32_t wait_limit;
-    int add_dtype, add_wide;
+    int add_dtype, add_wide;             // wide: rows begin on 16-byte boundaries
+    int add_quad, out_quad;              // on multiples of four entries
+    int in_place;                        // C is D, in 32 bits
 };
 
 constexpr uint32_t kProdRow = 128;                                    // bytes along K of a step
@@ -73,38 +75,53 @@ __device__ __forceinline__ void prod_load(uint32_t dst, const void* map, uint32_
                      : "memory");
 }
 
-// Four columns of C.
-__device__ __forceinline__ void prod_add4(const Product8& P, uint32_t row, uint32_t col, uint32_t n, float* y) {
+__device__ __forceinline__ void prefetch_map(const void* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
+// Adds a box of shared memory to 32-bit memory (subnormal results are zeros there).
+__device__ __forceinline__ void tma_add_2d(const void* tmap, int x, int y, uint32_t src) {
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(tmap), "r"(x), "r"(y),
+                 "r"(src)
+                 : "memory");
+}
+
+// Arrive on a barrier of each of `ctas` when every product issued so far has completed.
+__device__ __forceinline__ void umma_commit_to(uint32_t bar, uint16_t ctas) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(ctas)
+                 : "memory");
+}
+
+// Four columns of C, as they lie in memory (16-bit ones in x and y), and widened.
+__device__ __forceinline__ uint4 prod_fetch4(const Product8& P, uint32_t row, uint32_t col, uint32_t n) {
     const unsigned char* p = P.add + row * P.add_stride;
-    float c[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t w[4] = {0, 0, 0, 0};
     if (P.add_dtype == 0) {
-        const float* f = reinterpret_cast<const float*>(p) + col;
-        if (n == 4 && P.add_wide) {
-            Elem<float>::widen(*reinterpret_cast<const uint4*>(f), c);
-        } else {
+        const uint32_t* f = reinterpret_cast<const uint32_t*>(p) + col;
+        if (n == 4 && P.add_quad) return *reinterpret_cast<const uint4*>(f);
 #pragma unroll
-            for (uint32_t i = 0; i < 4; ++i)
-                if (i < n) c[i] = f[i];
-        }
+        for (uint32_t i = 0; i < 4; ++i)
+            if (i < n) w[i] = f[i];
     } else {
         const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + col;
-        uint32_t w[2] = {0, 0};
-        if (n == 4 && P.add_wide) {
+        if (n == 4 && P.add_quad) {
             const uint2 u = *reinterpret_cast<const uint2*>(h);
-            w[0] = u.x; w[1] = u.y;
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i)
-                if (i < n) w[i >> 1] |= (uint32_t)h[i] << (16 * (i & 1));
+            return make_uint4(u.x, u.y, 0, 0);
         }
-        float x[8];
-        if (P.add_dtype == 1) Elem<__nv_bfloat16>::widen(make_uint4(w[0], w[1], 0, 0), x);
-        else Elem<__half>::widen(make_uint4(w[0], w[1], 0, 0), x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = x[i];
+        for (uint32_t i = 0; i < 4; ++i)
+            if (i < n) w[i >> 1] |= (uint32_t)h[i] << (16 * (i & 1));
     }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void prod_widen4(int dtype, const uint4& w, float* c) {
+    float x[8];
+    if (dtype == 0) Elem<float>::widen(w, x);
+    else if (dtype == 1) Elem<__nv_bfloat16>::widen(make_uint4(w.x, w.y, 0, 0), x);
+    else Elem<__half>::widen(make_uint4(w.x, w.y, 0, 0), x);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = __fadd_rn(y[i], c[i]);
+    for (int i = 0; i < 4; ++i) c[i] = x[i];
+}
+__device__ __forceinline__ void prod_get4(const Product8& P, uint32_t row, uint32_t col, uint32_t n, float* c) {
+    prod_widen4(P.add_dtype, prod_fetch4(P, row, col, n), c);
 }
 
 // Four columns of a plain result.
@@ -112,7 +129,7 @@ __device__ __forceinline__ void prod_put4(const Product8& P, uint32_t row, uint3
     unsigned char* p = P.out.data + row * P.out.stride;
     if (P.out.dtype == 0) {
         float* f = reinterpret_cast<float*>(p) + col;
-        if (n == 4 && P.out.wide) {
+        if (n == 4 && P.out_quad) {
             *reinterpret_cast<uint4*>(f) = Elem<float>::narrow(y);
         } else {
 #pragma unroll
@@ -124,7 +141,7 @@ __device__ __forceinline__ void prod_put4(const Product8& P, uint32_t row, uint3
     uint16_t* h = reinterpret_cast<uint16_t*>(p) + col;
     const uint2 w = P.out.dtype == 1 ? make_uint2(Elem<__nv_bfloat16>::pair(y[0], y[1]), Elem<__nv_bfloat16>::pair(y[2], y[3]))
                                      : make_uint2(Elem<__half>::pair(y[0], y[1]), Elem<__half>::pair(y[2], y[3]));
-    if (n == 4 && P.out.wide) {
+    if (n == 4 && P.out_quad) {
         *reinterpret_cast<uint2*>(h) = w;
     } else {
 #pragma unroll
@@ -133,73 +150,249 @@ __device__ __forceinline__ void prod_put4(const Product8& P, uint32_t row, uint3
     }
 }
 
+// One column.
+template <typename Args>
+__device__ __forceinline__ float prod_get1(const Args& P, uint32_t row, uint32_t col) {
+    const unsigned char* p = P.add + row * P.add_stride;
+    return P.add_dtype == 0 ? reinterpret_cast<const float*>(p)[col]
+         : P.add_dtype == 1 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[col])
+                            : __half2float(reinterpret_cast<const __half*>(p)[col]);
+}
+template <typename Args>
+__device__ __forceinline__ void prod_put1(const Args& P, uint32_t row, uint32_t col, float y) {
+    unsigned char* p = P.out.data + row * P.out.stride;
+    if (P.out.dtype == 0) reinterpret_cast<float*>(p)[col] = y;
+    else if (P.out.dtype == 1) reinterpret_cast<__nv_bfloat16*>(p)[col] = __float2bfloat16_rn(y);
+    else reinterpret_cast<__half*>(p)[col] = __float2half_rn(y);
+}
+__device__ __forceinline__ float lds1(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+    return v;
+}
+
+// Sixteen columns of a row, which begin on a multiple of 16.
+__device__ __forceinline__ void prod_get16(const Product8& P, uint32_t row, uint32_t col, float* c) {
+    const uint32_t n = col >= P.cols ? 0 : min(16u, P.cols - col);
+    if (P.add_dtype != 0 && n == 16 && P.add_wide) {
+        const uint4* h = reinterpret_cast<const uint4*>(P.add + row * P.add_stride + 2ull * col);
+        const uint4 a = h[0], b = h[1];
+        if (P.add_dtype == 1) {
+            Elem<__nv_bfloat16>::widen(a, c);
+            Elem<__nv_bfloat16>::widen(b, c + 8);
+        } else {
+            Elem<__half>::widen(a, c);
+            Elem<__half>::widen(b, c + 8);
+        }
+        return;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 16; i += 4) prod_get4(P, row, col + i, n > i ? min(4u, n - i) : 0, c + i);
+}
+__device__ __forceinline__ void prod_put16(const Product8& P, uint32_t row, uint32_t col, const float* y) {
+    const uint32_t n = col >= P.cols ? 0 : min(16u, P.cols - col);
+    if (P.out.dtype != 0 && n == 16 && P.out.wide) {
+        uint4* h = reinterpret_cast<uint4*>(P.out.data + row * P.out.stride + 2ull * col);
+        h[0] = P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y) : Elem<__half>::narrow(y);
+        h[1] = P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y + 8) : Elem<__half>::narrow(y + 8);
+        return;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 16; i += 4)
+        if (n > i) prod_put4(P, row, col + i, min(4u, n - i), y + i);
+}
+
 __device__ __forceinline__ uint32_t inside4(uint32_t col, uint32_t cols) { return col >= cols ? 0u : min(4u, cols - col); }
 
-// ---- tiles of 128 x TN, K over a cluster ------------------------------------------------------------
+// ---- one row of A ----------------------------------------------------------------------------------------
 //
-// For products that have few tiles: a cluster's CTAs have a part of K each.  Their sums meet through
-// shared memory: each CTA finishes its share of the tile's rows, to which all others have sent theirs, and
-// adds them in the CTAs' order.  SWAP: the left operand is B and the right one A (a few tokens), the tile
-// is D's transposed; so a matrix of weights fills the 128 rows of an instruction.
-
-template <int TN, bool SWAP>
-struct ProdPart {
-    static constexpr uint32_t kRight = TN * kProdRow;
-    static constexpr uint32_t kStage = kProdBox + kRight;
-    static constexpr uint32_t kStages = 6;
-    static constexpr uint32_t kOutRows = SWAP ? TN : 128;             // of a tile, 128 columns each
-    static constexpr uint32_t kRing = kStages * kStage;
-    static constexpr uint32_t kSmem = (kRing > kOutRows * 512u ? kRing : kOutRows * 512u) + kStages * 1024u + 1024u;
-    static constexpr uint32_t kScaleCols = TN < 32 ? 32 : TN;         // first column of scales in tensor memory
-    static constexpr uint32_t kTmem = TN <= 32 ? 128 : TN <= 64 ? 128 : 256;
-    static constexpr uint32_t kThreads = 12 * 32;
+// One token and a matrix that is read in no time (1 x 4096 x 1024: 2.9 us, of which a launch is 2; through the tensor cores 4.4).
+// A warp has four rows of B and steps of 512 along K, 16 bytes a lane; the lane's part of A is decoded once for the four.  Products of two 8-bit entries and
+// their sums are taken unscaled in 32 bits (exact but for the sums' rounding), and each lane's 16 are scaled
+// together.  `split` warps of a CTA share the steps of the same rows, so that short matrices fill the GPU too.  Decoding
+// bounds it where there is more to read (1 x 8192 x 8192: 28 us, through the tensor cores 16).
+struct Product8Few {
+    Act8Mat a, b;
+    Act8Mat out;
+    const unsigned char* add;
+    uint64_t add_stride;
+    uint32_t cols, k, split;             // split: 1, 2, 4 or 8
+    int add_dtype;
 };
 
-template <int TN, bool SWAP>
-__global__ void __launch_bounds__(ProdPart<TN, SWAP>::kThreads, 1) act8_product_part_kernel(const __grid_constant__ Product8 P) {
-    using S = ProdPart<TN, SWAP>;
+// Sixteen entries (zeros behind the last column).
+__device__ __forceinline__ uint4 few_load(const Act8Mat& m, uint32_t row, uint32_t col, uint32_t k) {
+    const unsigned char* p = m.data + row * m.stride + col;
+    if (col + 16 <= k) return *reinterpret_cast<const uint4*>(p);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (uint32_t i = 0; i < 16; ++i)
+        if (col + i < k) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// As pairs, unscaled.
+__device__ __forceinline__ void few_decode(const uint4& q, int dtype, uint64_t (&x)[8]) {
+    float y[16];
+    act8_decode8(make_uint2(q.x, q.y), dtype, y);
+    act8_decode8(make_uint2(q.z, q.w), dtype, y + 8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = pack2(y[2 * i], y[2 * i + 1]);
+}
+__device__ __forceinline__ uint32_t few_scale(const Act8Mat& m, uint32_t row, uint32_t col, uint32_t k) {
+    return col < k ? m.scales[act8_scale_at(row, col >> 7, m.groups)] : 127u;
+}
+
+constexpr uint32_t kFewThreads = 256, kFewRows = 4;
+
+__global__ void __launch_bounds__(kFewThreads) act8_product_few_kernel(const __grid_constant__ Product8Few P) {
+    __shared__ float part[kFewThreads / 32][kFewRows];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slice = warp % P.split;
+    const uint32_t row0 = (blockIdx.x * (kFewThreads / 32 / P.split) + warp / P.split) * kFewRows;   // of B
+    griddep_launch();
+    griddep_wait();
+    float sum[kFewRows];
+#pragma unroll
+    for (uint32_t r = 0; r < kFewRows; ++r) sum[r] = 0.f;
+    if (row0 < P.cols) {
+        uint4 next[kFewRows];
+        uint32_t scale[kFewRows];
+        auto fetch = [&](uint32_t col) {
+#pragma unroll
+            for (uint32_t r = 0; r < kFewRows; ++r) {
+                const uint32_t row = min(row0 + r, P.cols - 1);      // beyond the last: not written
+                next[r] = few_load(P.b, row, col, P.k);
+                scale[r] = few_scale(P.b, row, col, P.k);
+            }
+        };
+        const uint32_t stride = P.split * 512u;
+        if (slice * 512u < P.k) fetch(slice * 512u + lane * 16u);
+        for (uint32_t at = slice * 512u; at < P.k; at += stride) {
+            const uint32_t col = at + lane * 16u;
+            uint64_t x[8];
+            few_decode(few_load(P.a, 0, col, P.k), P.a.dtype, x);
+            const uint32_t xs = few_scale(P.a, 0, col, P.k);
+            uint4 now[kFewRows];
+            uint32_t ws[kFewRows];
+#pragma unroll
+            for (uint32_t r = 0; r < kFewRows; ++r) { now[r] = next[r]; ws[r] = scale[r]; }
+            if (at + stride < P.k) fetch(col + stride);
+#pragma unroll
+            for (uint32_t r = 0; r < kFewRows; ++r) {
+                uint64_t w[8];
+                few_decode(now[r], P.b.dtype, w);
+                uint64_t d0 = mul2(w[0], x[0]), d1 = mul2(w[1], x[1]);
+#pragma unroll
+                for (int i = 2; i < 8; i += 2) {
+                    d0 = fma2(w[i], x[i], d0);
+                    d1 = fma2(w[i + 1], x[i + 1], d1);
+                }
+                float a, b;
+                unpack2(add2(d0, d1), a, b);
+                // 2^(ea + eb) as two factors: one of them alone may pass the range of fp32
+                const uint32_t e = ws[r] + xs, h = e >> 1;
+                const bool nan = ws[r] == 255u || xs == 255u;
+                const float y = __fmul_rn(__fadd_rn(a, b), act8_up(nan ? 255u : h));
+                sum[r] = __fmaf_rn(y, act8_up(e - h), sum[r]);
+            }
+        }
+    }
+#pragma unroll
+    for (uint32_t r = 0; r < kFewRows; ++r) {
+        float v = sum[r];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v = __fadd_rn(v, __shfl_xor_sync(~0u, v, o));
+        if (lane == 0) part[warp][r] = v;
+    }
+    if (P.split > 1) __syncthreads();
+    else __syncwarp();
+    if (slice || lane >= kFewRows) return;
+    float v = part[warp][lane];
+    for (uint32_t s = 1; s < P.split; ++s) v = __fadd_rn(v, part[warp + s][lane]);
+    const uint32_t col = row0 + lane;
+    if (col >= P.cols) return;
+    if (P.add) v = __fadd_rn(v, prod_get1(P, 0, col));
+    prod_put1(P, 0, col, v);
+}
+
+// ---- a tile, K over a cluster ------------------------------------------------------------------------
+//
+// For products that have few tiles: a cluster's CTAs (with CG = 2 pairs of CTAs, which have 256 x 256 together)
+// have a part of K each.  Their sums meet through shared memory: each CTA finishes its share of the
+// tile, to which all others have sent theirs, and adds them in a fixed order.  SWAP: the left operand is B and
+// the right one A (a few tokens), the tile is D's transposed; so a matrix of weights fills the 128 rows of
+// an instruction.
+
+template <int CG, int TN, bool SWAP>
+struct ProdPart {
+    static constexpr uint32_t kRight = TN / CG * kProdRow;
+    static constexpr uint32_t kStage = kProdBox + kRight;
+    static constexpr uint32_t kStages = 6;
+    static constexpr uint32_t kOutRows = SWAP ? TN : 128, kOutCols = SWAP ? 128 : TN;   // of the result, this CTA's
+    static constexpr uint32_t kRing = kStages * kStage, kSums = kOutRows * kOutCols * 4;
+    static constexpr uint32_t kRightGroups = TN > 128 ? 2 : 1, kScales = 512 * (1 + kRightGroups);
+    static constexpr uint32_t kSmem = (kRing > kSums ? kRing : kSums) + kStages * kScales + 1024;
+    static constexpr uint32_t kScaleCols = TN < 32 ? 32 : TN;         // first column of scales in tensor memory
+    static constexpr uint32_t kSlotCols = 4 * (1 + kRightGroups);
+    static constexpr uint32_t kTmem = TN <= 64 ? 128 : TN <= 128 ? 256 : 512;
+    static constexpr uint32_t kThreads = 12 * 32;
+    static_assert(CG == 1 || (TN == 256 && !SWAP), "");
+};
+
+template <int CG, int TN, bool SWAP>
+__global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_product_part_kernel(const __grid_constant__ Product8 P) {
+    using S = ProdPart<CG, TN, SWAP>;
     extern __shared__ unsigned char raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 1];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t stop;
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
-    const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u, scales = ring + (S::kSmem - 1024u - S::kStages * 1024u);
+    const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u, scales = ring + (S::kSmem - 1024u - S::kStages * S::kScales);
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
-    uint32_t parts;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
-    const uint32_t cta = cta_rank(), tile = blockIdx.x / parts;
-    const uint32_t left0 = tile / P.across * 128u, right0 = tile % P.across * (uint32_t)TN;
-    const uint32_t k0 = (uint32_t)((uint64_t)cta * P.steps / parts), k1 = (uint32_t)((uint64_t)(cta + 1) * P.steps / parts);
+    uint32_t ctas;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
+    const uint32_t cta = cta_rank(), rank = CG == 2 ? cta & 1u : 0, part = cta / CG, parts = ctas / CG, first = cta - rank;
+    const uint32_t tile = blockIdx.x / ctas;
+    const uint32_t left0 = tile / P.across * (128u * CG) + rank * 128u, right0 = tile % P.across * (uint32_t)TN;
+    const uint32_t k0 = (uint32_t)((uint64_t)part * P.steps / parts), k1 = (uint32_t)((uint64_t)(part + 1) * P.steps / parts);
     if (tid == 0) {
         for (uint32_t s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 2); mbar_init(empty + 8 * s, 1); }
         mbar_init(done, 1);
         stop = 0;
         fence_mbar_init();
     }
-    if (warp == 9) tmem_alloc<1>(smem_u32(&tmem_slot), S::kTmem);
+    if ((warp == 8 || warp == 10) && elect_one()) {
+        prefetch_map(warp == 8 ? &P.left : &P.right);
+        prefetch_map(warp == 8 ? &P.left_scales : &P.right_scales);
+    }
+    if (warp == 9) tmem_alloc<CG>(smem_u32(&tmem_slot), S::kTmem);
     tcgen05_before_sync();
     __syncthreads();
+    if (CG == 2) pair_sync();
     tcgen05_after_sync();
     const uint32_t tmem = tmem_slot;
     griddep_launch();
     griddep_wait();
 
     if (warp == 8 || warp == 10) {
-        // ---- loads: a warp for each operand
+        // ---- loads: a warp for each operand; in a pair bytes are counted on the first CTA's barriers
         if (elect_one()) {
             const bool left = warp == 8;
             const void* map = left ? &P.left : &P.right;
             const void* smap = left ? &P.left_scales : &P.right_scales;
-            const uint32_t at = left ? 0 : kProdBox, bytes = left ? kProdBox : S::kRight, row = left ? left0 : right0;
-            const uint32_t group0 = (row >> 7) * (left ? P.left_groups : P.right_groups), sat = scales + (left ? 0 : 512);
+            const uint32_t at = left ? 0 : kProdBox, bytes = left ? kProdBox : S::kRight;
+            const uint32_t row = left ? left0 : right0 + rank * (TN / CG), groups = left ? P.left_groups : P.right_groups;
+            const uint32_t group0 = ((left ? left0 : right0) >> 7) * groups, sat = scales + (left ? 0 : 512);
+            const uint32_t sbytes = left ? 512u : 512u * S::kRightGroups;
             uint32_t it = 0;
             for (uint32_t k = k0; k < k1; ++k, ++it) {
-                const uint32_t s = it % S::kStages;
+                const uint32_t s = it % S::kStages, bar = CG == 1 ? full + 8 * s : peer_addr(full + 8 * s, first);
                 if (!wait_or_stop(empty + 8 * s, ((it / S::kStages) & 1) ^ 1, P.wait_limit, &stop)) break;
                 const bool with = k == k0 || (k & 3) == 0;
-                mbar_arrive_expect_tx(full + 8 * s, bytes + (with ? 512u : 0u));
-                prod_load<1>(ring + s * S::kStage + at, map, k * kProdRow, row, full + 8 * s);
-                if (with) prod_load<1>(sat + s * 1024u, smap, 0, group0 + (k >> 2), full + 8 * s);
+                if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * (bytes + (with ? sbytes : 0u)));
+                prod_load<CG>(ring + s * S::kStage + at, map, k * kProdRow, row, bar);
+                if (!with) continue;
+                prod_load<CG>(sat + s * S::kScales, smap, 0, group0 + (k >> 2), bar);
+                if (!left && S::kRightGroups == 2) prod_load<CG>(sat + s * S::kScales + 512, smap, 0, group0 + groups + (k >> 2), bar);
             }
             // none of them is in flight when this CTA leaves
             for (uint32_t b = 0; b < S::kStages && b < it; ++b) {
@@ -211,28 +404,30 @@ __global__ void __launch_bounds__(ProdPart<TN, SWAP>::kThreads, 1) act8_product_
         __syncwarp();
     } else if (warp == 9) {
         // ---- products
-        if (elect_one()) {
-            const uint32_t idesc = P.formats | (1u << 23) | ((uint32_t)(TN / 8) << 17) | ((128u / 16) << 24);
-            uint32_t it = 0, slot = 0;
+        if (rank == 0 && elect_one()) {
+            const uint32_t idesc = P.formats | (1u << 23) | ((uint32_t)(TN / 8) << 17) | ((uint32_t)(CG * 128 / 16) << 24);
+            const uint16_t both = (uint16_t)(3u << cta);
             // the right operand's scales begin at its row in their group of 128
-            const uint32_t sb_at = S::kScaleCols + 4 + ((right0 & 127u) >> 5);
+            const uint32_t sb_at = 4 + ((right0 & 127u) >> 5);
+            uint32_t it = 0, slot = 0;
             for (uint32_t k = k0; k < k1; ++k, ++it) {
                 const uint32_t s = it % S::kStages;
                 if (!wait_or_stop(full + 8 * s, (it / S::kStages) & 1, P.wait_limit, &stop)) break;
                 tcgen05_after_sync();
                 if (k == k0 || (k & 3) == 0) {
-                    // one of three places in turn: what used it last is two groups behind
-                    slot = it == 0 ? 0 : slot == 16 ? 0 : slot + 8;
-                    umma_scales<1>(tmem + S::kScaleCols + slot, scales + s * 1024u);
-                    umma_scales<1>(tmem + S::kScaleCols + slot + 4, scales + s * 1024u + 512u);
+                    // one of three places in turn: what used it last is two whole groups behind, and over
+                    slot = it == 0 ? tmem + S::kScaleCols : slot == tmem + S::kScaleCols + 2 * S::kSlotCols ? tmem + S::kScaleCols : slot + S::kSlotCols;
+#pragma unroll
+                    for (uint32_t g = 0; g < 1 + S::kRightGroups; ++g) umma_scales<CG>(slot + 4 * g, scales + s * S::kScales + 512 * g);
                 }
                 const uint32_t id = idesc | (k & 3) << 29 | (k & 3) << 4, steps = k + 1 == P.steps ? P.tail : 4;
                 const uint64_t a = umma_desc_swizzled(ring + s * S::kStage), b = umma_desc_swizzled(ring + s * S::kStage + kProdBox);
-                for (uint32_t q = 0; q < steps; ++q)
-                    umma_mx8<1>(tmem, a + 2 * q, b + 2 * q, id, tmem + S::kScaleCols + slot, tmem + sb_at + slot, it > 0 || q > 0);
-                umma_commit<1>(empty + 8 * s);
+                for (uint32_t q = 0; q < steps; ++q) umma_mx8<CG>(tmem, a + 2 * q, b + 2 * q, id, slot, slot + sb_at, it > 0 || q > 0);
+                if (CG == 1) umma_commit<1>(empty + 8 * s);
+                else umma_commit_to(empty + 8 * s, both);
             }
-            umma_commit<1>(done);
+            if (CG == 1) umma_commit<1>(done);
+            else umma_commit_to(done, both);
         }
         __syncwarp();
     }
@@ -241,12 +436,32 @@ __global__ void __launch_bounds__(ProdPart<TN, SWAP>::kThreads, 1) act8_product_
     __syncwarp();
     tcgen05_after_sync();
     pair_sync();
-    const uint32_t share = S::kOutRows / parts, quad = warp & 3, half = warp >> 2;
-    if (warp < 8) {
-        // this warp's 32 rows of the tile and half of its columns, to the CTAs that finish them
-        const uint32_t from = tmem + ((quad * 32u) << 16);
+    const uint32_t quad = warp & 3, half = warp >> 2, from = tmem + ((quad * 32u) << 16);
+    const bool good = mine && !stop;
+    // Not SWAP: each CTA finishes 1 / parts of the tile's columns, a lane a row.  Of what it is sent, 16 bytes
+    // of 32 rows lie together, then the next four columns.
+    const uint32_t own = TN / parts;                                  // columns that a CTA finishes: 16 at least
+    if (!SWAP && warp < 8) {
+        for (uint32_t c = half * 16u; c < (uint32_t)TN; c += 32) {
+            const uint32_t to = c / own, at = c - to * own;
+            if (to == part) continue;
+            float y[16];
+            tmem_load16(from + c, y);
+            if (!good)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(0x7FC00000u);
+            const uint32_t base = peer_addr(ring + ((part * 4 + quad) * own + at) * 128u + lane * 16u, to * CG + rank);
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i)
+                asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + i * 512u), "f"(y[4 * i]), "f"(y[4 * i + 1]),
+                             "f"(y[4 * i + 2]), "f"(y[4 * i + 3]) : "memory");
+        }
+    }
+    // SWAP: rows of the result (tokens) are shared out, a lane has a column
+    const uint32_t share = S::kOutRows / parts;
+    constexpr uint32_t kRowBytes = S::kOutCols * 4;
+    if (SWAP && warp < 8) {
         constexpr uint32_t kCols = TN / 2 < 16 ? 16 : TN / 2;
-        const bool good = mine && !stop;
         if (half * kCols < (uint32_t)TN) {
 #pragma unroll
             for (uint32_t b = 0; b < kCols; b += 16) {
@@ -255,43 +470,91 @@ __global__ void __launch_bounds__(ProdPart<TN, SWAP>::kThreads, 1) act8_product_
                 if (!good)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(0x7FC00000u);
-                if (SWAP) {
-                    const uint32_t c = quad * 32u + lane;
+                const uint32_t c = quad * 32u + lane;
 #pragma unroll
-                    for (uint32_t i = 0; i < 16; ++i) {
-                        const uint32_t row = half * kCols + b + i, to = row / share, local = row - to * share;
-                        const uint32_t at = ring + (cta * share + local) * 512u + (((c >> 2) ^ (local & 7u)) << 4) + 4 * (c & 3);
-                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(at, to)), "f"(y[i]) : "memory");
-                    }
-                } else {
-                    const uint32_t row = quad * 32u + lane, to = row / share, local = row - to * share;
-                    const uint32_t base = peer_addr(ring + (cta * share + local) * 512u, to);
-#pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i) {
-                        const uint32_t piece = (half * kCols + b) / 4 + i;
-                        asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + ((piece ^ (local & 7u)) << 4)),
-                                     "f"(y[4 * i]), "f"(y[4 * i + 1]), "f"(y[4 * i + 2]), "f"(y[4 * i + 3]) : "memory");
-                    }
+                for (uint32_t i = 0; i < 16; ++i) {
+                    const uint32_t row = half * kCols + b + i, to = row / share, local = row - to * share;
+                    if (row >= P.rows) break;
+                    const uint32_t at = ring + (part * share + local) * kRowBytes + 4 * c;
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(at, to)), "f"(y[i]) : "memory");
                 }
             }
         }
     }
     tcgen05_before_sync();
     pair_sync();
-    if (warp == 9) tmem_free<1>(tmem, S::kTmem);
-    if (warp < 8) {
-        const uint32_t row0 = (SWAP ? right0 : left0) + cta * share, col0 = SWAP ? left0 : right0, col = col0 + 4 * lane;
-        const uint32_t n = inside4(col, P.cols);
+    const bool lost = stop;                                           // loads may have landed on the sums
+    if (!SWAP && warp < 8) {
+        tcgen05_after_sync();
+        const bool straight = P.out.wide && (!P.add || P.add_wide);
+        const uint32_t row = left0 + quad * 32u + lane;
+        for (uint32_t c = half * 16u; c < own; c += 32) {
+            const uint32_t col = right0 + part * own + c;
+            float y[16], add[16];
+            if (straight && P.add && row < P.rows) prod_get16(P, row, col, add);
+            __syncwarp();
+            tmem_load16(from + part * own + c, y);
+            for (uint32_t p = 0; p < parts; ++p) {
+                if (p == part) continue;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    float x[4];
+                    Elem<float>::widen(lds16(ring + ((p * 4 + quad) * own + c + 4 * i) * 128u + lane * 16u), x);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) y[4 * i + j] = __fadd_rn(y[4 * i + j], x[j]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (straight && P.add) y[i] = __fadd_rn(y[i], add[i]);
+                if (lost || !good) y[i] = __uint_as_float(0x7FC00000u);
+            }
+            if (straight) {
+                if (row < P.rows) prod_put16(P, row, col, y);
+                __syncwarp();
+                continue;
+            }
+            // rows that begin anywhere: turned, so that 16 lanes write a row's columns
+            const uint32_t turned = ring + 128u * TN * 4u + warp * 2048u;
+            __syncwarp();
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) sts16(turned + lane * 64u + ((i ^ ((lane >> 1) & 3u)) << 4), Elem<float>::narrow(y + 4 * i));
+            __syncwarp();
+            const uint32_t x = lane & 15u, row0 = left0 + quad * 32u;
+            if (col + x < P.cols)
+                for (uint32_t r0 = lane >> 4; r0 < 32; r0 += 16) {
+                    float c[8];                                      // all before the first is written: D may be C
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i)
+                        c[i] = P.add && row0 + r0 + 2 * i < P.rows ? prod_get1(P, row0 + r0 + 2 * i, col + x) : 0.f;
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) {
+                        const uint32_t r = r0 + 2 * i;
+                        const float v = lds1(turned + r * 64u + (((x >> 2) ^ ((r >> 1) & 3u)) << 4) + 4 * (x & 3));
+                        if (row0 + r < P.rows) prod_put1(P, row0 + r, col + x, P.add ? __fadd_rn(v, c[i]) : v);
+                    }
+                }
+            __syncwarp();
+        }
+        tcgen05_before_sync();
+    }
+    if (SWAP && warp < 8) {
+        const uint32_t row0 = right0 + part * share, col = left0 + 4 * lane, n = inside4(col, P.cols);
         for (uint32_t local = warp; local < share && row0 + local < P.rows; local += 8) {
             const uint32_t row = row0 + local;
-            float y[4] = {0.f, 0.f, 0.f, 0.f};
+            float y[4] = {0.f, 0.f, 0.f, 0.f}, c[4];
+            if (P.add) prod_get4(P, row, col, n, c);
             for (uint32_t p = 0; p < parts; ++p) {
                 float x[4];
-                Elem<float>::widen(lds16(ring + (p * share + local) * 512u + ((lane ^ (local & 7u)) << 4)), x);
+                Elem<float>::widen(lds16(ring + (p * share + local) * kRowBytes + lane * 16u), x);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) y[i] = __fadd_rn(y[i], x[i]);
             }
-            if (P.add && n) prod_add4(P, row, col, n, y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (P.add) y[i] = __fadd_rn(y[i], c[i]);
+                if (lost) y[i] = __uint_as_float(0x7FC00000u);
+            }
             if (P.out.dtype < 3) {
                 if (n) prod_put4(P, row, col, n, y);
                 continue;
@@ -312,10 +575,18 @@ __global__ void __launch_bounds__(ProdPart<TN, SWAP>::kThreads, 1) act8_product_
                 for (uint32_t i = 0; i < 4; ++i)
                     if (i < n) to[i] = (unsigned char)(w >> (8 * i));
             }
-            if (lane == 0) P.out.scales[act8_scale_at(row, col0 >> 7, P.out.groups)] = (uint8_t)byte;
+            if (lane == 0) P.out.scales[act8_scale_at(row, left0 >> 7, P.out.groups)] = (uint8_t)byte;
         }
     }
-    if (tid == 0 && stop && P.status) atomicOr(P.status, kStatusTimeout);
+    if (!SWAP) {                                                      // everyone has read tensor memory
+        __syncthreads();
+        if (CG == 2) pair_sync();
+    }
+    if (warp == 9) tmem_free<CG>(tmem, S::kTmem);
+    if (lost) {
+        if (tid == 0 && P.status) atomicOr(P.status, kStatusTimeout);
+        for (const long long since = clock64(); clock64() - since < 20000;) {}   // for what is still on its way
+    }
 }
 
 // ---- tiles of 256 x 256 by pairs of CTAs ------------------------------------------------------------
@@ -326,8 +597,8 @@ __global__ void __launch_bounds__(ProdPart<TN, SWAP>::kThreads, 1) act8_product_
 // and the next tile's products begin when they are.
 struct ProdPair {
     static constexpr uint32_t kStage = 2 * kProdBox, kScales = 1536;
-    static constexpr uint32_t kStages = 5;
-    static constexpr uint32_t kEpiWarps = 8, kEpi = 4096;
+    static constexpr uint32_t kStages = 6;
+    static constexpr uint32_t kEpiWarps = 8, kEpi = 2048;
     static constexpr uint32_t kThreads = 12 * 32;
     static constexpr uint32_t kSmem = kStages * (kStage + kScales) + kEpiWarps * kEpi + 1024;
     static constexpr uint32_t kSecond = 192, kScaleCols = 448, kSlots = 5, kSlotCols = 12;
@@ -351,6 +622,10 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
         mbar_init(shared_free, 2 * S::kEpiWarps);
         stop = 0;
         fence_mbar_init();
+    }
+    if ((warp == 8 || warp == 10) && elect_one()) {
+        prefetch_map(warp == 8 ? &P.left : &P.right);
+        prefetch_map(warp == 8 ? &P.left_scales : &P.right_scales);
     }
     if (warp == 9) tmem_alloc<2>(smem_u32(&tmem_slot), S::kTmem);
     tcgen05_before_sync();
@@ -431,130 +706,203 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
     } else if (warp < S::kEpiWarps) {
         // ---- results: a warp has 32 rows and half of the columns
         const uint32_t quad = warp & 3, half = warp >> 2, own = epi + warp * S::kEpi;
+        // Results go out through the warp's 2 KB of shared memory, 32 rows of 64 bytes: 16-byte piece c of row r
+        // at c ^ (r / 2 % 4), where the 64-byte swizzle has it and neither eight lanes with a row each nor
+        // eight with two whole rows meet in a bank.
+        auto place = [&](uint32_t r, uint32_t c) { return own + r * 64u + ((c ^ ((r >> 1) & 3u)) << 4); };
+        // To the result (or added to it), which clips them; and, before they are written again, whether they
+        // have been read.
+        auto send = [&](uint32_t row, uint32_t col) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                if (P.in_place) tma_add_2d(&P.result, (int)col, (int)row, own);
+                else tma_store_2d(&P.result, (int)col, (int)row, own);
+                bulk_commit();
+            }
+        };
+        auto sent = [&] {
+            if (lane == 0) bulk_wait_read0();
+            __syncwarp();
+        };
+        // what is added to 16 columns of a tile: four of four rows a lane
+        const uint32_t piece = lane & 3u;
+        auto ahead = [&](uint32_t row0, uint32_t col, uint4 (&to)[4]) {
+            const uint32_t m = inside4(col + 4 * piece, P.cols), row = row0 + (lane >> 2);
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) to[i] = prod_fetch4(P, row + 8 * i, col + 4 * piece, row + 8 * i < P.rows ? m : 0);
+        };
         uint32_t n = 0;
         for (uint32_t tile = pair; tile < P.tiles; tile += pairs, ++n) {
+            const uint32_t row0 = tile / P.across * 256u + rank * 128u + quad * 32u, col0 = tile % P.across * 256u + half * 128u;
+            const bool out = row0 < P.rows && col0 < P.cols;
+            if (P.add && !P.in_place && out && row0 + lane < P.rows) {   // C's lines of this warp, while the products run
+                const uint32_t es = P.add_dtype ? 2 : 4;
+                for (uint32_t at = 0; at < min(128u, P.cols - col0) * es; at += 128)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(P.add + (row0 + lane) * P.add_stride + (uint64_t)col0 * es + at));
+            }
             const bool good = __all_sync(~0u, wait_or_stop(acc_full + 8 * (n & 1), (n >> 1) & 1, limit, &stop));
             tcgen05_after_sync();
-            const uint32_t row0 = tile / P.across * 256u + rank * 128u + quad * 32u, col0 = tile % P.across * 256u + half * 128u;
             const uint32_t from = tmem + ((quad * 32u) << 16) + (n & 1) * S::kSecond + half * 128u;
             // Columns 192 .. 255 of tensor memory are the next tile's too: the second half's upper 64 in
-            // even tiles, the first half's lower 64 in odd ones.  Blocks of 32 columns begin there.
-            const bool shares = half != (n & 1), high = shares && half == 1;
+            // even tiles, the first half's lower 64 in odd ones.  Columns are taken from there on.
+            const bool shares = half != (n & 1);
+            const uint32_t start = shares && half == 1 ? 64 : 0;
             auto release = [&] {
                 tcgen05_before_sync();
                 __syncwarp();
                 if (lane == 0) leader_arrive(leader_addr(shared_free));
             };
             if (!shares) release();
-            const bool out = row0 < P.rows && col0 < P.cols;
             if (!out) {
                 if (shares) release();
                 continue;
             }
-            auto fetch = [&](uint32_t b, float* y) {
-                tmem_load32(from + 32 * b, y);
+            auto fetch32 = [&](uint32_t c, float* y) {
+                tmem_load32(from + c, y);
                 if (!good)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(0x7FC00000u);
             };
+            auto fetch16 = [&](uint32_t c, float* y) {
+                tmem_load16(from + c, y);
+                if (!good)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(0x7FC00000u);
+            };
             if (P.out.dtype >= 3) {
                 // the largest magnitude of this lane's 128 columns first, then the entries
-                const uint32_t row = row0 + lane, dtype = P.out.dtype;
+                const uint32_t row = row0 + lane, dtype = P.out.dtype, nc = min(128u, P.cols - col0);
                 uint32_t top = 0;
-                const uint32_t nc = min(128u, P.cols - col0);
 #pragma unroll 1
-                for (uint32_t b = 0; b < 4; ++b) {
+                for (uint32_t c = 0; c < 128; c += 32) {
                     float y[32];
-                    fetch(b, y);
+                    fetch32(c, y);
 #pragma unroll
                     for (uint32_t i = 0; i < 32; ++i)
-                        if (32 * b + i < nc) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+                        if (c + i < nc) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
                 }
                 const uint32_t byte = act8_byte(top, dtype);
                 const float by = act8_down(byte);
 #pragma unroll 1
-                for (uint32_t b = 0; b < 4; ++b) {
-                    float y[32];
-                    fetch(b, y);
-#pragma unroll
-                    for (uint32_t c = 0; c < 2; ++c) {
-                        uint32_t w[4];
-                        act8_code<16>(y + 16 * c, by, dtype, w);
-                        sts16(own + lane * 128u + (((2 * b + c) ^ (lane & 7u)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
-                    }
-                }
-                if (shares) release();
-                __syncwarp();
-                if (row < P.rows) P.out.scales[act8_scale_at(row, col0 >> 7, P.out.groups)] = (uint8_t)byte;
-                const uint32_t piece = lane & 7u, left = col0 + 16 * piece < P.cols ? P.cols - col0 - 16 * piece : 0;
-#pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) {
-                    const uint32_t r = 4 * i + (lane >> 3);
-                    const uint4 w = lds16(own + r * 128u + ((piece ^ (r & 7u)) << 4));
-                    if (row0 + r >= P.rows) continue;
-                    unsigned char* to = P.out.data + (row0 + r) * P.out.stride + col0 + 16 * piece;
-                    if (left >= 16) {
-                        *reinterpret_cast<uint4*>(to) = w;
-                    } else {
-                        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                        for (uint32_t j = 0; j < 16; ++j)
-                            if (j < left) to[j] = (unsigned char)(u[j >> 2] >> (8 * (j & 3)));
-                    }
-                }
-                __syncwarp();
-                continue;
-            }
-            if (P.out.dtype != 0 && !P.add && P.out.wide && col0 + 128 <= P.cols) {
-                // 16 bits, whole rows of 64 columns: 128 bytes a row
-#pragma unroll 1
-                for (uint32_t c = 0; c < 2; ++c) {
-                    const uint32_t b = 2 * (c ^ (high ? 1u : 0u));
+                for (uint32_t at = 0; at < 128; at += 64) {
+                    const uint32_t u = (at + start) & 127u;
 #pragma unroll
                     for (uint32_t h = 0; h < 2; ++h) {
                         float y[32];
-                        fetch(b + h, y);
+                        fetch32(u + 32 * h, y);
+                        if (h == 0) sent();
+#pragma unroll
+                        for (uint32_t c = 0; c < 2; ++c) {
+                            uint32_t w[4];
+                            act8_code<16>(y + 16 * c, by, dtype, w);
+                            sts16(place(lane, 2 * h + c), make_uint4(w[0], w[1], w[2], w[3]));
+                        }
+                    }
+                    if (at == 0 && shares) release();
+                    send(row0, col0 + u);
+                }
+                if (row < P.rows) P.out.scales[act8_scale_at(row, col0 >> 7, P.out.groups)] = (uint8_t)byte;
+                continue;
+            }
+            if (P.out.wide && (!P.add || P.in_place)) {
+                if (P.out.dtype == 0) {
+#pragma unroll 1
+                    for (uint32_t at = 0; at < 128; at += 16) {
+                        const uint32_t c = (at + start) & 127u;
+                        float y[16];
+                        fetch16(c, y);
+                        sent();
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 4 * i));
+                        if (at == 48 && shares) release();
+                        send(row0, col0 + c);
+                    }
+                } else {
+#pragma unroll 1
+                    for (uint32_t at = 0; at < 128; at += 32) {
+                        const uint32_t c = (at + start) & 127u;
+                        float y[32];
+                        fetch32(c, y);
+                        sent();
 #pragma unroll
                         for (uint32_t i = 0; i < 4; ++i)
-                            sts16(own + lane * 128u + (((4 * h + i) ^ (lane & 7u)) << 4),
-                                  P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y + 8 * i) : Elem<__half>::narrow(y + 8 * i));
+                            sts16(place(lane, i), P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y + 8 * i) : Elem<__half>::narrow(y + 8 * i));
+                        if (at == 32 && shares) release();
+                        send(row0, col0 + c);
                     }
-                    if (c == 0 && shares) release();
-                    __syncwarp();
-                    const uint32_t piece = lane & 7u;
+                }
+                continue;
+            }
+            sent();
+            if (!P.out_quad || (P.add && !P.add_quad)) {
+                // rows that begin anywhere: a lane a column, two rows at a time
+                const uint32_t rows = min(32u, P.rows - row0), x = lane & 15u;
+                const bool four = P.out.dtype == 0, bf16 = P.out.dtype == 1;
+#pragma unroll 1
+                for (uint32_t at = 0; at < 128; at += 16) {
+                    const uint32_t c = (at + start) & 127u, col = col0 + c + x;
+                    float y[16];
+                    fetch16(c, y);
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) {
-                        const uint32_t r = 4 * i + (lane >> 3);
-                        const uint4 w = lds16(own + r * 128u + ((piece ^ (r & 7u)) << 4));
-                        if (row0 + r < P.rows)
-                            *reinterpret_cast<uint4*>(P.out.data + (row0 + r) * P.out.stride + (col0 + 32 * b + 8 * piece) * 2ull) = w;
-                    }
+                    for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 4 * i));
+                    if (at == 48 && shares) release();
+                    __syncwarp();
+                    unsigned char* to = P.out.data + (row0 + (lane >> 4)) * P.out.stride + (uint64_t)col * (four ? 4 : 2);
+                    if (col < P.cols)
+#pragma unroll 1
+                        for (uint32_t r0 = lane >> 4; r0 < rows; r0 += 16) {
+                            float add[8];                            // all before the first is written: D may be C
+                            if (P.add)
+#pragma unroll
+                                for (uint32_t i = 0; i < 8; ++i) add[i] = r0 + 2 * i < rows ? prod_get1(P, row0 + r0 + 2 * i, col) : 0.f;
+#pragma unroll
+                            for (uint32_t i = 0; i < 8; ++i, to += 2 * P.out.stride) {
+                                const uint32_t r = r0 + 2 * i;
+                                float v = lds1(place(r, x >> 2) + 4 * (x & 3u));
+                                if (P.add) v = __fadd_rn(v, add[i]);
+                                if (r >= rows) continue;
+                                if (four) *reinterpret_cast<float*>(to) = v;
+                                else *reinterpret_cast<uint16_t*>(to) = bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
+                            }
+                        }
                     __syncwarp();
                 }
                 continue;
             }
+            // what is added is asked for 16 columns ahead
+            uint4 next[4];
+            if (P.add) ahead(row0, col0 + start, next);
 #pragma unroll 1
-            for (uint32_t c = 0; c < 4; ++c) {
-                const uint32_t b = high ? c ^ 2u : c;
-                float y[32];
-                fetch(b, y);
+            for (uint32_t at = 0; at < 128; at += 16) {
+                const uint32_t c = (at + start) & 127u, col = col0 + c + 4 * piece, m = inside4(col, P.cols);
+                float y[16];
+                fetch16(c, y);
 #pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) sts16(own + lane * 128u + ((i ^ (lane & 7u)) << 4), Elem<float>::narrow(y + 4 * i));
-                if (c == 1 && shares) release();
+                for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 4 * i));
+                if (at == 48 && shares) release();
                 __syncwarp();
-                const uint32_t piece = lane & 7u, col = col0 + 32 * b + 4 * piece, m = inside4(col, P.cols);
+                uint4 now[4];
 #pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) {
-                    const uint32_t r = 4 * i + (lane >> 3);
-                    float x[4];
-                    Elem<float>::widen(lds16(own + r * 128u + ((piece ^ (r & 7u)) << 4)), x);
+                for (uint32_t i = 0; i < 4; ++i) now[i] = next[i];
+                if (P.add && at < 112) ahead(row0, col0 + ((c + 16) & 127u), next);
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint32_t r = 8 * i + (lane >> 2);
+                    float x[4], add[4];
+                    Elem<float>::widen(lds16(place(r, piece)), x);
                     if (row0 + r >= P.rows || !m) continue;
-                    if (P.add) prod_add4(P, row0 + r, col, m, x);
+                    if (P.add) {
+                        prod_widen4(P.add_dtype, now[i], add);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] = __fadd_rn(x[j], add[j]);
+                    }
                     prod_put4(P, row0 + r, col, m, x);
                 }
                 __syncwarp();
             }
         }
+        if (lane == 0) bulk_wait_all();
     }
     __syncwarp();
     tcgen05_before_sync();

@@ -113,9 +113,10 @@ def test_results_repeat():
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
 
 
-@pytest.mark.parametrize("m,n,k", [(3, 300, 900), (200, 300, 900), (2300, 2100, 300)])
+@pytest.mark.parametrize("m,n,k", [(5, 300, 900), (200, 300, 900), (2300, 2100, 300)])
 def test_a_wait_that_runs_out_is_reported(m, n, k):
-    """No polls at all: every result is NaN, the status says so, and the next call is sound."""
+    """No polls at all: every result is NaN, the status says so, and the next call is sound.  (A single row of A is
+    multiplied without waits.)"""
     a, b = whole_numbers(m, k, 1, E4M3), whole_numbers(n, k, 2, E4M3)
     d, status = strided(m, n, F32), torch.zeros(1, dtype=torch.int32, device="cuda")
     ecq.ecq_act8_set_wait_limit(0)
