@@ -835,6 +835,63 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
                 continue;
             }
             sent();
+            if (!P.out_quad && !P.add) {
+                // Rows that begin anywhere, in words of four bytes, 16 to a row and two rows at a time; a row of 16-bit
+                // entries that begins between two words takes its words from both halves' neighbours, and its
+                // first and last entry go out alone.  Word i of row r lies at i ^ (r / 2), so that neither 32
+                // rows' same words nor two whole rows meet in a bank.
+                const bool four = P.out.dtype == 0;
+                const uint32_t rows = min(32u, P.rows - row0), x = lane & 15u, second = lane >> 4;
+                const uint32_t step = four ? 16 : 32;                 // columns
+#pragma unroll 1
+                for (uint32_t at = 0; at < 128; at += step) {
+                    const uint32_t c = (at + start) & 127u, left = col0 + c < P.cols ? min(step, P.cols - col0 - c) : 0;
+                    unsigned char* first = P.out.data + row0 * P.out.stride + (uint64_t)(col0 + c) * (four ? 4 : 2);
+                    uint32_t w[16];
+                    if (four) {
+                        fetch16(c, reinterpret_cast<float*>(w));
+                    } else {
+                        float y[32];
+                        fetch32(c, y);
+#pragma unroll
+                        for (uint32_t i = 0; i < 16; ++i)
+                            w[i] = P.out.dtype == 1 ? Elem<__nv_bfloat16>::pair(y[2 * i], y[2 * i + 1]) : Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
+                    }
+                    if (at + step == 64 && shares) release();
+                    __syncwarp();                                     // what was here has been read
+                    if (!left) continue;
+#pragma unroll
+                    for (uint32_t i = 0; i < 16; ++i)
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(own + lane * 64u + ((i ^ (lane >> 1)) << 2)), "r"(w[i]) : "memory");
+                    if (!four) {
+                        uint16_t* mine = reinterpret_cast<uint16_t*>(first + lane * P.out.stride);
+                        if (lane < rows && (reinterpret_cast<uintptr_t>(mine) & 2u)) {
+                            mine[0] = (uint16_t)w[0];
+                            if (left == 32) mine[31] = (uint16_t)(w[15] >> 16);
+                        }
+                    }
+                    __syncwarp();
+                    // this lane's word of rows `second`, `second` + 2, ...; rows alike in parity by the stride's
+                    unsigned char* to = first + second * P.out.stride + 4 * x;
+#pragma unroll
+                    for (uint32_t k = 0; k < 16; ++k, to += 2 * P.out.stride) {
+                        const uint32_t line = own + k * 128u + second * 64u;
+                        uint32_t v, next = 0;
+                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(line + ((x ^ k) << 2)));
+                        if (four) {
+                            if (2 * k + second < rows && x < left) *reinterpret_cast<uint32_t*>(to) = v;
+                            continue;
+                        }
+                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(next) : "r"(line + (((x + 1) & 15u) ^ k) * 4u));
+                        const uint32_t odd = (uint32_t)(reinterpret_cast<uintptr_t>(to) >> 1) & 1u, e = 2 * x + odd;   // first entry
+                        v = __funnelshift_r(v, next, 16 * odd);
+                        if (2 * k + second >= rows) continue;
+                        if (e + 1 < left) *reinterpret_cast<uint32_t*>(to + 2 * odd) = v;
+                        else if (e < left && !(odd && left == 32)) *reinterpret_cast<uint16_t*>(to + 2 * odd) = (uint16_t)v;
+                    }
+                }
+                continue;
+            }
             if (!P.out_quad || (P.add && !P.add_quad)) {
                 // rows that begin anywhere: a lane a column, two rows at a time
                 const uint32_t rows = min(32u, P.rows - row0), x = lane & 15u;
