@@ -1,7 +1,9 @@
 // C ABI of the operators on matrices in 8 bits, the products apart: argument checks and launches.
+#include <atomic>
 #include <cfloat>
 #include <cstdint>
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "../../include/ecq.h"
@@ -19,19 +21,47 @@ int sm_count(int& sms) {
 }
 
 // ---- tiles
+// Boxes of 128 x 128.
+bool tile_map(CUtensorMap* tm, const Act8Mat& m, uint64_t rows, uint64_t cols) {
+    static const CUtensorMapDataType types[] = {CU_TENSOR_MAP_DATA_TYPE_FLOAT32, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                                                CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_DATA_TYPE_UINT8};
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {m.stride};
+    const cuuint32_t boxes[2] = {128, 128}, unit[2] = {1, 1};
+    return tensor_map_encoder()(tm, types[m.dtype], 2, m.data, dims, strides, boxes, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int OP, typename S, typename T>
-int launch_tiles(const Act8Tiles& P, cudaStream_t st) {
-    return launch_act8(act8_tile_kernel<OP, S, T>, (P.rows + 127) / 128 * P.tiles_across, kActThreads, 0, 0, st, P);
+int launch_tiles(Act8Tiles& P, cudaStream_t st) {
+    static std::atomic<bool> done[kMaxDevices];
+    using R = Act8Ring<OP, S, T>;
+    auto kernel = act8_tile_kernel<OP, S, T>;
+    int sms = 0;
+    if (sm_count(sms) != ECQ_OK) return ECQ_ERR_CUDA;
+    // Tiles ahead where a CTA has several (8192 x 4096, in 8 bits transposed: 24.8 -> .. us)
+    const uint32_t ctas = (uint32_t)sms * R::kCtas;
+    P.ahead = R::kStages && P.wide && P.rows >= 128 && P.cols >= 128 && P.tiles >= 4 * ctas;
+    if (P.ahead) {
+        if (!tensor_map_encoder() || !tile_map(&P.maps[0], P.in[0], P.rows, P.cols) ||
+            (OP != kActCopy && !tile_map(&P.maps[1], P.in[1], P.rows, P.cols)) ||
+            (OP == kActGateGrad && !tile_map(&P.maps[2], P.d, P.rows, P.cols)) ||
+            !allow_smem(reinterpret_cast<const void*>(kernel), R::kSmem, done))
+            return ECQ_ERR_CUDA;
+        return launch_act8(kernel, ctas, kActThreads, R::kSmem, 0, st, P);
+    }
+    return launch_act8(kernel, P.tiles, kActThreads, 0, 0, st, P);
 }
 template <int OP, typename T>
-int launch_tiles(const Act8Tiles& P, bool coded, cudaStream_t st) {
+int launch_tiles(Act8Tiles& P, bool coded, cudaStream_t st) {
     return coded ? launch_tiles<OP, uint8_t, T>(P, st) : launch_tiles<OP, T, T>(P, st);
 }
+// `plain`: the type of the plain matrices (16 bits where there are none, as nothing needs 32 then).
 template <int OP>
 int launch_tiles(Act8Tiles& P, uint64_t rows, uint64_t cols, int plain, bool coded, void* stream) {
     P.rows = (uint32_t)rows;
     P.cols = (uint32_t)cols;
     P.tiles_across = (uint32_t)((cols + 127) / 128);
+    P.tiles = (P.rows + 127) / 128 * P.tiles_across;
     P.wide = 1;
     for (const Act8Mat* m : {&P.in[0], &P.in[1], &P.d, &P.plain[0], &P.plain[1]}) P.wide &= !m->data || m->wide;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -71,16 +101,23 @@ uint32_t grad_grid(uint64_t rows, const RowShape& s, int sms) {
 }
 
 template <typename S, typename T, int NV>
-int launch_norm_grad(const Act8NormGrad& P, const RowShape& s, uint32_t grid, cudaStream_t st) {
-    return launch_act8(act8_norm_grad_kernel<S, T, NV>, grid, s.per_cta, 0, 0, st, P);
+int launch_norm_grad(Act8NormGrad& P, const RowShape& s, uint32_t grid, cudaStream_t st) {
+    static std::atomic<bool> done[kMaxDevices];
+    auto kernel = act8_norm_grad_kernel<S, T, NV>;
+    constexpr uint32_t kRoom = 208u * 1024u;                          // an SM's, for 512 threads
+    const uint32_t ahead = 2 * s.per_cta * NormRead<S, T, NV>::kBytes, sums = s.per_cta > s.per_row ? s.per_cta * NV * 32 : 0;
+    P.full &= ahead * (512 / s.per_cta) <= kRoom;
+    const uint32_t smem = P.full && ahead > sums ? ahead : sums;
+    if (!allow_smem(reinterpret_cast<const void*>(kernel), kRoom, done)) return ECQ_ERR_CUDA;
+    return launch_act8(kernel, grid, s.per_cta, smem, 0, st, P);
 }
 template <typename S, typename T>
-int launch_norm_grad(const Act8NormGrad& P, const RowShape& s, uint32_t grid, cudaStream_t st) {
+int launch_norm_grad(Act8NormGrad& P, const RowShape& s, uint32_t grid, cudaStream_t st) {
     return s.vectors == 1 ? launch_norm_grad<S, T, 1>(P, s, grid, st)
          : s.vectors == 2 ? launch_norm_grad<S, T, 2>(P, s, grid, st) : launch_norm_grad<S, T, 4>(P, s, grid, st);
 }
 template <typename T>
-int launch_norm_grad(const Act8NormGrad& P, const RowShape& s, uint32_t grid, bool coded, cudaStream_t st) {
+int launch_norm_grad(Act8NormGrad& P, const RowShape& s, uint32_t grid, bool coded, cudaStream_t st) {
     return coded ? launch_norm_grad<uint8_t, T>(P, s, grid, st) : launch_norm_grad<T, T>(P, s, grid, st);
 }
 
@@ -110,18 +147,18 @@ int ecq_act8_store(uint64_t rows, uint64_t cols, const ecq_act8_matrix* x, const
         return ECQ_ERR_ARG;
     if (rows == 0) return ECQ_OK;
     Act8Tiles P = {};
-    P.in[0] = act8_mat(x, cols);
-    P.q[0] = act8_mat(q, cols);
-    P.qt[0] = act8_mat(q_t, rows);
-    return launch_tiles<kActCopy>(P, rows, cols, x->dtype < 3 ? x->dtype : ECQ_F32, x->dtype >= 3, cuda_stream);
+    P.in[0] = act8_mat(x, rows, cols);
+    P.q[0] = act8_mat(q, rows, cols);
+    P.qt[0] = act8_mat(q_t, cols, rows);
+    return launch_tiles<kActCopy>(P, rows, cols, x->dtype < 3 ? x->dtype : ECQ_BF16, x->dtype >= 3, cuda_stream);
 }
 
 int ecq_act8_load(uint64_t rows, uint64_t cols, const ecq_act8_matrix* q, const ecq_act8_matrix* x, void* cuda_stream) {
     if (bad_size(rows, cols) || bad_matrix(q, rows, cols, kCoded) || bad_matrix(x, rows, cols, kPlain)) return ECQ_ERR_ARG;
     if (rows == 0) return ECQ_OK;
     Act8Tiles P = {};
-    P.in[0] = act8_mat(q, cols);
-    P.plain[0] = act8_mat(x, cols);
+    P.in[0] = act8_mat(q, rows, cols);
+    P.plain[0] = act8_mat(x, rows, cols);
     return launch_tiles<kActCopy>(P, rows, cols, x->dtype, true, cuda_stream);
 }
 
@@ -138,14 +175,14 @@ int ecq_act8_gate(uint64_t rows, uint64_t cols, const ecq_act8_matrix* gate, con
     if (!same_type(type, gate) || !same_type(type, out)) return ECQ_ERR_ARG;
     if (rows == 0) return ECQ_OK;
     Act8Tiles P = {};
-    P.in[0] = act8_mat(gate, cols);
-    P.in[1] = act8_mat(up, cols);
-    P.plain[0] = act8_mat(out, cols);
-    P.q[0] = act8_mat(out8, cols);
-    P.qt[0] = act8_mat(out8_t, rows);
-    P.kept[0] = act8_mat(gate8, cols);
-    P.kept[1] = act8_mat(up8, cols);
-    return launch_tiles<kActGate>(P, rows, cols, type < 0 ? ECQ_F32 : type, gate->dtype >= 3, cuda_stream);
+    P.in[0] = act8_mat(gate, rows, cols);
+    P.in[1] = act8_mat(up, rows, cols);
+    P.plain[0] = act8_mat(out, rows, cols);
+    P.q[0] = act8_mat(out8, rows, cols);
+    P.qt[0] = act8_mat(out8_t, cols, rows);
+    P.kept[0] = act8_mat(gate8, rows, cols);
+    P.kept[1] = act8_mat(up8, rows, cols);
+    return launch_tiles<kActGate>(P, rows, cols, type < 0 ? ECQ_BF16 : type, gate->dtype >= 3, cuda_stream);
 }
 
 int ecq_act8_gate_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* gate, const ecq_act8_matrix* up,
@@ -164,15 +201,15 @@ int ecq_act8_gate_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* gate
     if (!same_type(type, gate) || !same_type(type, d_gate) || !same_type(type, d_up)) return ECQ_ERR_ARG;
     if (rows == 0) return ECQ_OK;
     Act8Tiles P = {};
-    P.in[0] = act8_mat(gate, cols);
-    P.in[1] = act8_mat(up, cols);
-    P.d = act8_mat(d_out, cols);
-    P.plain[0] = act8_mat(d_gate, cols);
-    P.plain[1] = act8_mat(d_up, cols);
-    P.q[0] = act8_mat(d_gate8, cols);
-    P.q[1] = act8_mat(d_up8, cols);
-    P.qt[0] = act8_mat(d_gate8_t, rows);
-    P.qt[1] = act8_mat(d_up8_t, rows);
+    P.in[0] = act8_mat(gate, rows, cols);
+    P.in[1] = act8_mat(up, rows, cols);
+    P.d = act8_mat(d_out, rows, cols);
+    P.plain[0] = act8_mat(d_gate, rows, cols);
+    P.plain[1] = act8_mat(d_up, rows, cols);
+    P.q[0] = act8_mat(d_gate8, rows, cols);
+    P.q[1] = act8_mat(d_up8, rows, cols);
+    P.qt[0] = act8_mat(d_gate8_t, cols, rows);
+    P.qt[1] = act8_mat(d_up8_t, cols, rows);
     return launch_tiles<kActGateGrad>(P, rows, cols, type, gate->dtype >= 3, cuda_stream);
 }
 
@@ -193,12 +230,12 @@ int ecq_act8_norm(uint64_t rows, uint64_t cols, const ecq_act8_matrix* x, const 
     if (sm_count(sms) != ECQ_OK) return ECQ_ERR_CUDA;
     const RowShape s = row_shape(rows, cols, sms);
     Act8Norm P = {};
-    P.x = act8_mat(x, cols);
-    P.residual = act8_mat(residual, cols);
-    P.sum = act8_mat(sum, cols);
-    P.y = act8_mat(out, cols);
-    P.y8 = act8_mat(out8, cols);
-    P.sum8 = act8_mat(sum8, cols);
+    P.x = act8_mat(x, rows, cols);
+    P.residual = act8_mat(residual, rows, cols);
+    P.sum = act8_mat(sum, rows, cols);
+    P.y = act8_mat(out, rows, cols);
+    P.y8 = act8_mat(out8, rows, cols);
+    P.sum8 = act8_mat(sum8, rows, cols);
     P.weight = weight;
     P.weight_dtype = weight_dtype;
     P.rstd = rstd;
@@ -221,7 +258,7 @@ uint64_t ecq_act8_norm_grad_workspace_bytes(uint64_t rows, uint64_t cols) {
     int sms = 0;
     if (bad_size(rows, cols) || cols > ECQ_ACT8_NORM_MAX_COLS || sm_count(sms) != ECQ_OK) return 0;
     const RowShape s = row_shape(rows, cols, sms);
-    return (uint64_t)grad_grid(rows, s, sms) * (s.per_cta / s.per_row) * cols * sizeof(float);
+    return (uint64_t)grad_grid(rows, s, sms) * ((cols + 7) / 8 * 8) * sizeof(float);
 }
 
 int ecq_act8_norm_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* sum, const void* weight, int weight_dtype,
@@ -238,17 +275,17 @@ int ecq_act8_norm_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* sum,
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (rows == 0) {
         if (!d_weight) return ECQ_OK;
-        return launch_act8(act8_add_kernel, (uint32_t)((cols + 31) / 32), 512, 0, 0, st, (const float*)nullptr, 0u, (uint32_t)cols, d_weight);
+        return launch_act8(act8_add_kernel, (uint32_t)((cols + 31) / 32), 1024, 0, 0, st, (const float*)nullptr, 0u, 0u, (uint32_t)cols, d_weight);
     }
     if (sm_count(sms) != ECQ_OK) return ECQ_ERR_CUDA;
     const RowShape s = row_shape(rows, cols, sms);
-    const uint32_t grid = grad_grid(rows, s, sms), count = grid * (s.per_cta / s.per_row);
-    if (d_weight && workspace_bytes < (uint64_t)count * cols * sizeof(float)) return ECQ_ERR_ARG;
+    const uint32_t grid = grad_grid(rows, s, sms), pitch = (uint32_t)((cols + 7) / 8 * 8);
+    if (d_weight && workspace_bytes < (uint64_t)grid * pitch * sizeof(float)) return ECQ_ERR_ARG;
     Act8NormGrad P = {};
-    P.s = act8_mat(sum, cols);
-    P.d_out = act8_mat(d_out, cols);
-    P.d_sum = act8_mat(d_sum, cols);
-    P.d_x = act8_mat(d_x, cols);
+    P.s = act8_mat(sum, rows, cols);
+    P.d_out = act8_mat(d_out, rows, cols);
+    P.d_sum = act8_mat(d_sum, rows, cols);
+    P.d_x = act8_mat(d_x, rows, cols);
     P.weight = weight;
     P.weight_dtype = weight_dtype;
     P.rstd = rstd;
@@ -256,6 +293,7 @@ int ecq_act8_norm_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* sum,
     P.rows = (uint32_t)rows;
     P.cols = (uint32_t)cols;
     P.per_row = s.per_row;
+    P.pitch = pitch;
     P.inv_cols = (float)(1.0 / (double)cols);
     P.full = cols % 8 == 0;
     for (const Act8Mat* m : {&P.s, &P.d_out, &P.d_sum, &P.d_x}) P.full &= !m->data || m->wide;
@@ -267,7 +305,7 @@ int ecq_act8_norm_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* sum,
         default: rc = launch_norm_grad<__half>(P, s, grid, coded, st); break;
     }
     if (rc != ECQ_OK || !d_weight) return rc;
-    return launch_act8(act8_add_kernel, (uint32_t)((cols + 31) / 32), 512, 0, 0, st, (const float*)P.sums, count, (uint32_t)cols, d_weight);
+    return launch_act8(act8_add_kernel, (uint32_t)((cols + 31) / 32), 1024, 0, 0, st, (const float*)P.sums, grid, pitch, (uint32_t)cols, d_weight);
 }
 
 }  // extern "C"

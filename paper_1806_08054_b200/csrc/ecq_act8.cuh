@@ -23,7 +23,7 @@ __host__ __device__ __forceinline__ uint64_t act8_scale_at(uint32_t row, uint32_
 
 // A matrix of a call: bytes from row to row, and for 8 bits its scales in groups of four blocks.
 struct Act8Mat {
-    unsigned char* data;
+    unsigned char *data, *end;           // first byte, and behind the last
     uint64_t stride;
     uint8_t* scales;
     uint32_t groups;
@@ -113,21 +113,60 @@ __device__ __forceinline__ void act8_decode8(uint2 q, int dtype, float by, float
 template <typename T> struct Raw8 { uint4 w[sizeof(T) / 2]; };
 template <> struct Raw8<uint8_t> { uint2 w; uint32_t byte; };
 
-template <bool FULL, typename T>
-__device__ __forceinline__ void get8(const unsigned char* p, const uint8_t*, uint32_t n, bool wide, Raw8<T>& r) {
-    if (FULL || (n == 8 && wide)) {
+// Words w[by] .. w[by + N - 1], by < 4, without indexing.
+template <int N, int M>
+__device__ __forceinline__ void from_word(const uint32_t (&w)[M], uint32_t by, uint32_t (&to)[N]) {
+    static_assert(M >= N + 3, "");
+    uint32_t x[N + 2];
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = *(reinterpret_cast<const uint4*>(p) + i);
+    for (int i = 0; i < N + 2; ++i) x[i] = by & 1u ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) to[i] = by & 2u ? x[i + 2] : x[i];
+}
+
+// Rows that begin anywhere: the 16-byte pieces that the eight lie in, moved by where they begin.  Pieces that are
+// not in the matrix's memory as a whole are not read; the entries are then read one by one.
+template <bool FULL, typename T>
+__device__ __forceinline__ void get8(const Act8Mat& m, const unsigned char* p, const uint8_t*, uint32_t n, Raw8<T>& r) {
+    constexpr int kVecs = (int)sizeof(T) / 2;                        // of 16 bytes
+    if (FULL || (n == 8 && m.wide)) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) r.w[i] = *(reinterpret_cast<const uint4*>(p) + i);
+        return;
+    }
+    const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15u;
+    const unsigned char* base = p - off;
+    if (n == 8 && base >= m.data && base + 16 * (kVecs + 1) <= m.end) {
+        uint32_t w[4 * kVecs + 4];
+#pragma unroll
+        for (int i = 0; i <= kVecs; ++i) {
+            const uint4 v = *(reinterpret_cast<const uint4*>(base) + i);
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+        if (sizeof(T) == 4) {
+            uint32_t x[4 * kVecs];
+            from_word(w, off >> 2, x);
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) r.w[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+        } else {
+            uint32_t x[5], z[4];
+            // the ninth word is needed for nothing but the shift's form
+            const uint32_t more[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
+            from_word(more, off >> 2, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = __funnelshift_r(x[i], x[i + 1], 8 * (off & 2u));
+            r.w[0] = make_uint4(z[0], z[1], z[2], z[3]);
+        }
         return;
     }
     T e[8];
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) e[i] = i < n ? reinterpret_cast<const T*>(p)[i] : T(0.f);
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = *(reinterpret_cast<const uint4*>(e) + i);
+    for (int i = 0; i < kVecs; ++i) r.w[i] = *(reinterpret_cast<const uint4*>(e) + i);
 }
 template <bool FULL>
-__device__ __forceinline__ void get8(const unsigned char* p, const uint8_t* scale, uint32_t n, bool, Raw8<uint8_t>& r) {
+__device__ __forceinline__ void get8(const Act8Mat&, const unsigned char* p, const uint8_t* scale, uint32_t n, Raw8<uint8_t>& r) {
     if (FULL || n == 8) {
         r.w = *reinterpret_cast<const uint2*>(p);
         r.byte = *scale;
@@ -147,17 +186,58 @@ __device__ __forceinline__ void widen8(const Raw8<T>& r, int, float* x) {
 }
 __device__ __forceinline__ void widen8(const Raw8<uint8_t>& r, int dtype, float* x) { act8_decode8(r.w, dtype, act8_up(r.byte), x); }
 
-template <bool FULL, typename T>
-__device__ __forceinline__ void put8(unsigned char* p, uint32_t n, bool wide, const float* x) {
-    if (FULL || (n == 8 && wide)) {
+// Writes them; LANES lanes (the whole warp takes part) have consecutive eights of a row.  Where rows begin anywhere a lane
+// writes the 16-byte pieces that begin in its eight, with the next lane's first entries; what is left at
+// both ends of the lanes' part goes out one by one.
+template <bool FULL, int LANES, typename T>
+__device__ __forceinline__ void put8(const Act8Mat& m, unsigned char* p, uint32_t n, const float* x) {
+    constexpr int kVecs = (int)sizeof(T) / 2;
+    if (FULL || m.wide) {
+        if (FULL || n == 8) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-            *(reinterpret_cast<uint4*>(p) + i) = Elem<T>::narrow(x + i * Elem<T>::kPer16);
+            for (int i = 0; i < kVecs; ++i)
+                *(reinterpret_cast<uint4*>(p) + i) = Elem<T>::narrow(x + i * Elem<T>::kPer16);
+            return;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i < n) Elem<T>::store(reinterpret_cast<T*>(p) + i, x[i]);
         return;
     }
+    uint32_t w[4 * kVecs + 4];
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i)
-        if (i < n) Elem<T>::store(reinterpret_cast<T*>(p) + i, x[i]);
+    for (int i = 0; i < kVecs; ++i) {
+        const uint4 v = Elem<T>::narrow(x + i * Elem<T>::kPer16);
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+    const uint32_t lane = threadIdx.x & (LANES - 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[4 * kVecs + i] = __shfl_down_sync(~0u, w[i], 1, LANES);
+    const uint32_t after = __shfl_down_sync(~0u, n, 1, LANES);
+    // bytes, and entries, to the first piece
+    const uint32_t off = (16u - ((uint32_t)reinterpret_cast<uintptr_t>(p) & 15u)) & 15u, h = off / (uint32_t)sizeof(T);
+    const bool whole = n == 8 && (h == 0 || (lane + 1 < LANES && after >= h));
+    const bool before = __shfl_up_sync(~0u, (int)whole, 1, LANES) && lane > 0;
+    if (whole) {
+        uint4* to = reinterpret_cast<uint4*>(p + off);
+        if (sizeof(T) == 4) {
+            uint32_t z[4 * kVecs];
+            from_word(w, off >> 2, z);
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) to[i] = make_uint4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]);
+        } else {
+            uint32_t y[5], z[4];
+            const uint32_t more[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
+            from_word(more, off >> 2, y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = __funnelshift_r(y[i], y[i + 1], 8 * (off & 2u));
+            to[0] = make_uint4(z[0], z[1], z[2], z[3]);
+        }
+    }
+    if ((h && !before && n) || (!whole && n))
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i < n && (i < h ? !before : !whole)) Elem<T>::store(reinterpret_cast<T*>(p) + i, x[i]);
 }
 
 // Eight entries in 8 bits by their block's scale byte, and from the first of the block's lanes the byte.

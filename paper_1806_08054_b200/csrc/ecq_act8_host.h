@@ -1,8 +1,11 @@
 // Checks and launches that the entry points on matrices in 8 bits share.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
+#include <mutex>
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "../../include/ecq.h"
@@ -34,17 +37,48 @@ inline bool bad_matrix(const ecq_act8_matrix* m, uint64_t rows, uint64_t cols, i
     return !m->scales || !aligned_to(m->data, 16) || !aligned_to(m->scales, 16) || m->stride < cols || (m->stride & 15);
 }
 
-inline Act8Mat act8_mat(const ecq_act8_matrix* m, uint64_t cols) {
+inline Act8Mat act8_mat(const ecq_act8_matrix* m, uint64_t rows, uint64_t cols) {
     Act8Mat r = {};
     if (!m) return r;
     const bool coded = m->dtype >= 3;
     r.data = static_cast<unsigned char*>(m->data);
     r.stride = m->stride * (coded ? 1u : dtype_bytes(m->dtype));
+    r.end = r.data + (rows - 1) * r.stride + cols * (coded ? 1u : dtype_bytes(m->dtype));
     r.scales = static_cast<uint8_t*>(m->scales);
     r.groups = (uint32_t)((cols + 511) / 512);
     r.dtype = m->dtype;
     r.wide = aligned_to(m->data, 16) && r.stride % 16 == 0;
     return r;
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline EncodeTiledFn tensor_map_encoder() {
+    static EncodeTiledFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    });
+    return fn;
+}
+
+// Kernels that take more shared memory than the default say so once a device.
+inline bool allow_smem(const void* kernel, size_t bytes, std::atomic<bool>* done) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= kMaxDevices) return false;
+    if (done[dev].load(std::memory_order_acquire)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    done[dev].store(true, std::memory_order_release);
+    return true;
 }
 
 // A launch whose CTAs may be placed while the work ahead of it in the stream is finishing (they touch

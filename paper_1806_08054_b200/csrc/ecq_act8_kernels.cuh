@@ -4,7 +4,10 @@
 
 #include <cstdint>
 
+#include <cuda.h>
+
 #include "ecq_act8.cuh"
+#include "ecq_tensor.cuh"
 
 namespace ecq {
 
@@ -18,12 +21,14 @@ enum { kActCopy = 0, kActGate = 1, kActGateGrad = 2 };
 constexpr uint32_t kActThreads = 512;
 
 struct Act8Tiles {
+    CUtensorMap maps[3];                 // in[0], in[1] and d in boxes of 128 x 128, with `ahead`
     Act8Mat in[2];                       // x; gate and up
     Act8Mat d;                           // gradient of the activation's output
     Act8Mat plain[2], q[2], qt[2];       // results (data NULL: not wanted): h, or d_gate and d_up
     Act8Mat kept[2];                     // gate and up in 8 bits
-    uint32_t rows, cols, tiles_across;
+    uint32_t rows, cols, tiles_across, tiles;
     int wide;                            // rows of all plain matrices begin on 16-byte boundaries
+    int ahead;                           // whole tiles are brought to shared memory ahead of their turn
 };
 
 // 1 / (1 + exp(-x)); WIDE: the rounding of x log2(e) is added back, which shows in 32 bits alone.
@@ -52,7 +57,7 @@ __device__ __forceinline__ void act8_put_plain(const Act8Mat& m, const Act8Place
     unsigned char* p = m.data + at.row * m.stride + (uint64_t)at.col * sizeof(T);
 #pragma unroll
     for (uint32_t j = 0; j < 4; ++j, p += m.stride)
-        if (FULL || j < at.rows) put8<FULL, T>(p, at.n, m.wide, v[j]);
+        put8<FULL, 16, T>(m, p, FULL || j < at.rows ? at.n : 0, v[j]);
 }
 
 // Two of a thread's rows, the j-th and the next.
@@ -71,10 +76,11 @@ __device__ __forceinline__ void act8_get(const Act8Mat& m, const Act8Place& at, 
     const unsigned char* p = m.data + at.row * m.stride + (uint64_t)at.col * sizeof(T);
     const uint8_t* s = sizeof(T) == 1 ? m.scales + act8_scale_at(at.row, at.col >> 7, m.groups) : nullptr;
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j, p += m.stride, s += 16) get8<FULL>(p, s, FULL || j < at.rows ? at.n : 0, m.wide, r[j]);
+    for (uint32_t j = 0; j < 4; ++j, p += m.stride, s += 16) get8<FULL>(m, p, s, FULL || j < at.rows ? at.n : 0, r[j]);
 }
 
-// A thread's 4 x 8 results in 8 bits transposed; the whole CTA.
+// A thread's 4 x 8 results in 8 bits transposed; the whole CTA.  Calls may follow each other: each part of shared
+// memory is written a barrier after its last reader.
 struct Act8Turn {
     unsigned char turned[128 * 128];
     uint32_t part[kActThreads / 32][128];
@@ -146,15 +152,59 @@ __device__ __forceinline__ void act8_put_turned(const Act8Mat& m, const Act8Plac
     }
 }
 
-// S: type of the inputs (uint8_t: either of 8 bits), T: of the plain results and of the gradient.
+// What a thread reads of a tile.  S: type of the inputs (uint8_t: either of 8 bits), T: of the plain results and of
+// the gradient.
+template <int OP, typename S, typename T>
+struct Act8Read {
+    Raw8<S> a[4], b[OP == kActCopy ? 1 : 4];
+    Raw8<T> d[OP == kActGateGrad ? 4 : 1];
+};
 template <int OP, typename S, typename T, bool FULL>
-__device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& at, Act8Turn& turn) {
+__device__ __forceinline__ void act8_read(const Act8Tiles& P, const Act8Place& at, Act8Read<OP, S, T>& r) {
+    act8_get<FULL>(P.in[0], at, r.a);
+    if constexpr (OP != kActCopy) act8_get<FULL>(P.in[1], at, r.b);
+    if constexpr (OP == kActGateGrad) act8_get<FULL>(P.d, at, r.d);
+}
+
+// Tiles on their way in shared memory: each matrix's 128 rows of 128 entries, and of one in 8 bits the
+// 512 scale bytes that its blocks are among.
+template <int OP, typename S, typename T>
+struct Act8Ring {
+    static constexpr uint32_t kIn = 128 * 128 * sizeof(S) + (sizeof(S) == 1 ? 512 : 0);
+    static constexpr uint32_t kBytes = kIn * (OP == kActCopy ? 1 : 2) + (OP == kActGateGrad ? 128 * 128 * sizeof(T) : 0);
+    // an SM; 64 registers a thread are too few for a gradient, and for two inputs in 32 bits
+    static constexpr uint32_t kCtas = OP == kActGateGrad || (OP == kActGate && sizeof(S) == 4) ? 1 : 2;
+    static constexpr uint32_t kRoom = 226u * 1024u / kCtas - 27u * 1024u;
+    static constexpr uint32_t kStages = kRoom / kBytes < 4 ? kRoom / kBytes : 4;
+    static constexpr uint32_t kSmem = kStages * kBytes + 128;
+};
+
+// A thread's entries of a matrix of a tile in shared memory.
+template <typename T>
+__device__ __forceinline__ void act8_take(uint32_t from, uint32_t block, Raw8<T> (&r)[4]) {
+    const uint32_t at = from + (threadIdx.x >> 4) * 4 * 128 * (uint32_t)sizeof(T) + (threadIdx.x & 15u) * 8 * (uint32_t)sizeof(T);
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r[j].w[i] = lds16(at + j * 128 * (uint32_t)sizeof(T) + 16 * i);
+}
+template <>
+__device__ __forceinline__ void act8_take<uint8_t>(uint32_t from, uint32_t block, Raw8<uint8_t> (&r)[4]) {
+    const uint32_t row = (threadIdx.x >> 4) * 4, at = from + row * 128 + (threadIdx.x & 15u) * 8;
+    const uint32_t scale = from + 128 * 128 + (uint32_t)act8_scale_at(row, block & 3u, 1);
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r[j].w.x), "=r"(r[j].w.y) : "r"(at + j * 128));
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(r[j].byte) : "r"(scale + 16 * j));
+    }
+}
+
+template <int OP, typename S, typename T, bool FULL>
+__device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& at, const Act8Read<OP, S, T>& in, Act8Turn& turn) {
     constexpr bool wide = sizeof(T) == 4;
-    Raw8<S> a[4], b[4];
-    Raw8<T> d[4];
-    act8_get<FULL>(P.in[0], at, a);
-    if (OP != kActCopy) act8_get<FULL>(P.in[1], at, b);
-    if (OP == kActGateGrad) act8_get<FULL>(P.d, at, d);
+    const auto& a = in.a;
+    const auto& b = in.b;
+    const auto& d = in.d;
     float v[4][8], u[OP == kActGateGrad ? 4 : 1][8];
     if constexpr (OP == kActCopy) {
 #pragma unroll
@@ -207,27 +257,84 @@ __device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& a
         act8_put_coded<FULL>(P.q[1], at, 0, u[0], u[1]);
         act8_put_coded<FULL>(P.q[1], at, 2, u[2], u[3]);
     }
-        if (P.qt[1].data) {
-            __syncthreads();                                         // the first is out of shared memory
-            act8_put_turned<FULL>(P.qt[1], at, P.rows, P.cols, u, turn);
-        }
+        if (P.qt[1].data) act8_put_turned<FULL>(P.qt[1], at, P.rows, P.cols, u, turn);
     }
 }
 
+// CTAs stay on the GPU and take every n-th tile.  Whole tiles come by TMA as many ahead as there is room for: a
+// thread's four rows alone are too little on their way to memory, in 8 bits above all, and registers have
+// no room for the next tile's.  (A wait that runs out reads the tile from memory instead.)
 template <int OP, typename S, typename T>
-__global__ void __launch_bounds__(kActThreads, OP == kActGateGrad ? 1 : 2) act8_tile_kernel(const __grid_constant__ Act8Tiles P) {
+__global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas) act8_tile_kernel(const __grid_constant__ Act8Tiles P) {
+    using R = Act8Ring<OP, S, T>;
+    constexpr uint32_t kStages = R::kStages ? R::kStages : 1;
+    extern __shared__ unsigned char raw[];
     __shared__ __align__(16) Act8Turn turn;
-    const uint32_t tile_row = blockIdx.x / P.tiles_across, tile_col = blockIdx.x - tile_row * P.tiles_across;
-    const uint32_t row0 = tile_row * 128u, col0 = tile_col * 128u;
-    Act8Place at;
-    at.row = row0 + 4 * (threadIdx.x >> 4);
-    at.col = col0 + 8 * (threadIdx.x & 15u);
-    at.n = inside(at.col, P.cols);
-    at.rows = at.row < P.rows ? min(4u, P.rows - at.row) : 0;
+    __shared__ __align__(8) uint64_t bars[kStages];
+    const uint32_t ring = (smem_u32(raw) + 127u) & ~127u, full = smem_u32(bars), tid = threadIdx.x;
+    const bool ahead = R::kStages && P.ahead;
+    auto whole = [&](uint32_t tile) {
+        return (tile / P.tiles_across + 1) * 128u <= P.rows && (tile % P.tiles_across + 1) * 128u <= P.cols && P.wide;
+    };
+    if (ahead && tid == 0) {
+        for (uint32_t s = 0; s < kStages; ++s) mbar_init(full + 8 * s, 1);
+        fence_mbar_init();
+    }
     griddep_launch();
+    if (ahead) __syncthreads();
     griddep_wait();
-    if (P.wide && row0 + 128 <= P.rows && col0 + 128 <= P.cols) act8_tile<OP, S, T, true>(P, at, turn);
-    else act8_tile<OP, S, T, false>(P, at, turn);
+    // by one thread: the next whole tile from `coming` on
+    uint32_t coming = blockIdx.x;
+    auto ask = [&](uint32_t s) {
+        while (coming < P.tiles && !whole(coming)) coming += gridDim.x;
+        if (coming >= P.tiles) return;
+        const uint32_t tr = coming / P.tiles_across, tc = coming % P.tiles_across, bar = full + 8 * s;
+        uint32_t to = ring + s * R::kBytes;
+        mbar_arrive_expect_tx(bar, R::kBytes);
+#pragma unroll
+        for (int m = 0; m < (OP == kActCopy ? 1 : 2); ++m, to += R::kIn) {
+            tma_load_2d(to, &P.maps[m], (int)(tc * 128), (int)(tr * 128), bar);
+            if (sizeof(S) == 1)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + 128 * 128),
+                             "l"(P.in[m].scales + ((uint64_t)tr * P.in[m].groups + (tc >> 2)) * 512), "r"(512u), "r"(bar)
+                             : "memory");
+        }
+        if (OP == kActGateGrad) tma_load_2d(to, &P.maps[2], (int)(tc * 128), (int)(tr * 128), bar);
+        coming += gridDim.x;
+    };
+    if (ahead && tid == 0)
+        for (uint32_t s = 0; s < kStages; ++s) ask(s);
+    uint32_t it = 0;                                                 // whole tiles so far
+    for (uint32_t tile = blockIdx.x; tile < P.tiles; tile += gridDim.x) {
+        const uint32_t row0 = tile / P.tiles_across * 128u, col0 = tile % P.tiles_across * 128u;
+        Act8Place at;
+        at.row = row0 + 4 * (tid >> 4);
+        at.col = col0 + 8 * (tid & 15u);
+        at.n = inside(at.col, P.cols);
+        at.rows = at.row < P.rows ? min(4u, P.rows - at.row) : 0;
+        Act8Read<OP, S, T> in;
+        if (!whole(tile)) {
+            act8_read<OP, S, T, false>(P, at, in);
+            act8_tile<OP, S, T, false>(P, at, in, turn);
+            continue;
+        }
+        if (ahead) {
+            const uint32_t s = it % kStages, from = ring + s * R::kBytes;
+            if (mbar_wait(full + 8 * s, (it / kStages) & 1)) {
+                act8_take(from, col0 >> 7, in.a);
+                if constexpr (OP != kActCopy) act8_take(from + R::kIn, col0 >> 7, in.b);
+                if constexpr (OP == kActGateGrad) act8_take(from + 2 * R::kIn, 0, in.d);
+            } else {
+                act8_read<OP, S, T, true>(P, at, in);
+            }
+            ++it;
+            __syncthreads();                                         // everyone has read the stage
+            if (tid == 0) ask(s);
+        } else {
+            act8_read<OP, S, T, true>(P, at, in);
+        }
+        act8_tile<OP, S, T, true>(P, at, in, turn);
+    }
 }
 
 // ---- norm -----------------------------------------------------------------------------------------
@@ -320,8 +427,8 @@ __device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part) {
             a[k] = {};
             b[k] = {};
             if (real && cols[k]) {
-                get8<FULL>(x + k * step, nullptr, cols[k], P.x.wide, a[k]);
-                if (P.residual.data) get8<FULL>(r + k * step, nullptr, cols[k], P.residual.wide, b[k]);
+                get8<FULL>(P.x, x + k * step, nullptr, cols[k], a[k]);
+                if (P.residual.data) get8<FULL>(P.residual, r + k * step, nullptr, cols[k], b[k]);
             }
         }
         float s[NV][8], squares = 0.f;
@@ -342,7 +449,7 @@ __device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part) {
             unsigned char* to = act8_row(P.sum, row) + at;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
-                if (real && cols[k]) put8<FULL, T>(to + k * step, cols[k], P.sum.wide, s[k]);
+                if (!FULL || (real && cols[k])) put8<FULL, 32, T>(P.sum, to + k * step, real ? cols[k] : 0, s[k]);
         }
         if (P.sum8.data) act8_put_row<FULL, NV>(P.sum8, row, t, P.per_row, P.cols, real, s);
         squares = act8_row_sum(squares, P.per_row, part, turn);
@@ -359,7 +466,7 @@ __device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part) {
             unsigned char* to = act8_row(P.y, row) + at;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
-                if (real && cols[k]) put8<FULL, T>(to + k * step, cols[k], P.y.wide, s[k]);
+                if (!FULL || (real && cols[k])) put8<FULL, 32, T>(P.y, to + k * step, real ? cols[k] : 0, s[k]);
         }
         if (P.y8.data) act8_put_row<FULL, NV>(P.y8, row, t, P.per_row, P.cols, real, s);
     }
@@ -376,20 +483,57 @@ __global__ void __launch_bounds__(512) act8_norm_kernel(const __grid_constant__ 
 
 // Its gradient.  With n = s rstd and g = d_out w:  d_x = rstd (g - n mean(g n)) + d_sum, and the weight's
 // gradient is the sum over the rows of d_out n: each thread adds its columns' in registers over the
-// rows that it has, and a second launch adds these sums in a fixed order.
+// rows that it has, a CTA its rows' at a time, and a second launch the CTAs' sums, all in a fixed order.
 struct Act8NormGrad {
     Act8Mat s, d_out, d_sum, d_x;
     const void* weight;
     const float* rstd;
-    float* sums;                         // [grid x rows at a time][cols], or NULL
+    float* sums;                         // [grid][pitch], or NULL
     int weight_dtype;
-    int full;
-    uint32_t rows, cols, per_row;
+    int full;                            // as Act8Norm's, and there is room for a row ahead
+    uint32_t rows, cols, per_row, pitch;
     float inv_cols;
 };
 
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, uint32_t bytes) {
+    if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
+
+// What a thread reads of a row.  FULL: the next row's part is on its way to shared memory meanwhile, in places of the
+// thread's own, so that nobody waits for anybody (registers have no room for it: 16 warps an SM then have
+// their one row each on the way, 59 us for 8192 x 4096 against ..).
+template <typename S, typename T, int NV>
+struct NormRead {
+    Raw8<S> a[NV];
+    Raw8<T> b[NV], c[NV];
+    float rstd;
+    static constexpr uint32_t kBytes = NV * (8 * sizeof(S) + 2 * 8 * sizeof(T));   // a thread
+    // 16 bytes (8 for a vector in 8 bits) of all threads lie together
+    template <typename F>
+    __device__ __forceinline__ static void places(uint32_t base, F f) {
+        const uint32_t threads = blockDim.x, tid = threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                f(0, k, i, base + tid * 16);
+                f(1, k, i, base + threads * 16 + tid * 16);
+                base += threads * 32;
+            }
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < (sizeof(S) == 1 ? 1 : (int)sizeof(S) / 2); ++i) {
+                f(2, k, i, base + tid * (sizeof(S) == 1 ? 8u : 16u));
+                base += threads * (sizeof(S) == 1 ? 8u : 16u);
+            }
+    }
+};
+
 template <typename S, typename T, int NV, bool FULL>
-__device__ __forceinline__ void act8_norm_grad_rows(const Act8NormGrad& P, float* part) {
+__device__ __forceinline__ void act8_norm_grad_rows(const Act8NormGrad& P, float* part, unsigned char* raw) {
+    using Read = NormRead<S, T, NV>;
     const uint32_t slot = threadIdx.x / P.per_row, t = threadIdx.x - slot * P.per_row, slots = blockDim.x / P.per_row;
     float w[NV][8], dw[NV][8];
     uint32_t cols[NV];
@@ -402,34 +546,88 @@ __device__ __forceinline__ void act8_norm_grad_rows(const Act8NormGrad& P, float
         for (int i = 0; i < 8; ++i) dw[k][i] = 0.f;
     }
     const uint32_t step = P.per_row * 8 * (uint32_t)sizeof(T), at = 8 * t * (uint32_t)sizeof(T);
+    const uint32_t ring = smem_u32(raw), stage = blockDim.x * Read::kBytes;
+    // scale byte of a vector in 8 bits
+    auto scale_of = [&](uint32_t row, int k) { return act8_row_scales(P.s, row) + act8_block_at((k * P.per_row + t) >> 4); };
+    auto ask = [&](uint32_t row, uint32_t from) {                    // FULL
+        const unsigned char* s = act8_row(P.s, row) + 8 * t * sizeof(S);
+        const unsigned char *d = act8_row(P.d_out, row) + at, *e = act8_row(P.d_sum, row) + at;
+        Read::places(from, [&](int m, int k, int i, uint32_t to) {
+            if (!cols[k]) return;
+            if (m == 2) copy_ahead(to, s + k * P.per_row * 8 * sizeof(S) + 16 * i, sizeof(S) == 1 ? 8 : 16);
+            else if (m == 0) copy_ahead(to, d + k * step + 16 * i, 16);
+            else if (P.d_sum.data) copy_ahead(to, e + k * step + 16 * i, 16);
+        });
+    };
+    const uint64_t stride = (uint64_t)gridDim.x * slots;
     uint32_t turn = 0;
-    for (uint64_t first = (uint64_t)blockIdx.x * slots; first < P.rows; first += (uint64_t)gridDim.x * slots, ++turn) {
+    float next_rstd = 0.f;
+    uint32_t next_scale[NV];
+    if (FULL) {
+        const uint64_t row = (uint64_t)blockIdx.x * slots + slot;
+        if (row < P.rows) {
+            ask((uint32_t)row, ring);
+            next_rstd = P.rstd[row];
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (sizeof(S) == 1 && cols[k]) next_scale[k] = *scale_of((uint32_t)row, k);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    for (uint64_t first = (uint64_t)blockIdx.x * slots; first < P.rows; first += stride, ++turn) {
         const uint32_t row = (uint32_t)first + slot;
         const bool real = row < P.rows;
-        Raw8<S> a[NV];
-        Raw8<T> b[NV], c[NV];
-        const float rstd = real ? P.rstd[row] : 0.f;
-        const unsigned char* s = act8_row(P.s, row) + 8 * t * sizeof(S);
-        const uint8_t* scales = sizeof(S) == 1 ? act8_row_scales(P.s, row) : nullptr;
-        const unsigned char *d = act8_row(P.d_out, row) + at, *e = act8_row(P.d_sum, row) + at;
+        Read in;
+        if (FULL) {
+            in.rstd = next_rstd;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            a[k] = {};
-            b[k] = {};
-            c[k] = {};
-            if (real && cols[k]) {
-                const uint8_t* scale = sizeof(S) == 1 ? scales + act8_block_at((k * P.per_row + t) >> 4) : nullptr;
-                get8<FULL>(s + k * P.per_row * 8 * sizeof(S), scale, cols[k], P.s.wide, a[k]);
-                get8<FULL>(d + k * step, nullptr, cols[k], P.d_out.wide, b[k]);
-                if (P.d_sum.data) get8<FULL>(e + k * step, nullptr, cols[k], P.d_sum.wide, c[k]);
+            for (int k = 0; k < NV; ++k) {
+                in.a[k] = {};
+                in.b[k] = {};
+                in.c[k] = {};
+                if constexpr (sizeof(S) == 1) in.a[k].byte = real && cols[k] ? next_scale[k] : 127u;
+            }
+            const uint64_t ahead = first + stride + slot;
+            if (ahead < P.rows) {
+                ask((uint32_t)ahead, ring + ((turn + 1) & 1u) * stage);
+                next_rstd = P.rstd[ahead];
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (sizeof(S) == 1 && cols[k]) next_scale[k] = *scale_of((uint32_t)ahead, k);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            if (real)
+                Read::places(ring + (turn & 1u) * stage, [&](int m, int k, int i, uint32_t from) {
+                    if (!cols[k] || (m == 1 && !P.d_sum.data)) return;
+                    if (m == 0) in.b[k].w[i] = lds16(from);
+                    else if (m == 1) in.c[k].w[i] = lds16(from);
+                    else if constexpr (sizeof(S) == 1) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(in.a[k].w.x), "=r"(in.a[k].w.y) : "r"(from));
+                    else in.a[k].w[i] = lds16(from);
+                });
+        } else {
+            in.rstd = real ? P.rstd[row] : 0.f;
+            const unsigned char* s = act8_row(P.s, row) + 8 * t * sizeof(S);
+            const unsigned char *d = act8_row(P.d_out, row) + at, *e = act8_row(P.d_sum, row) + at;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                in.a[k] = {};
+                in.b[k] = {};
+                in.c[k] = {};
+                if (real && cols[k]) {
+                    get8<false>(P.s, s + k * P.per_row * 8 * sizeof(S), sizeof(S) == 1 ? scale_of(row, k) : nullptr, cols[k], in.a[k]);
+                    get8<false>(P.d_out, d + k * step, nullptr, cols[k], in.b[k]);
+                    if (P.d_sum.data) get8<false>(P.d_sum, e + k * step, nullptr, cols[k], in.c[k]);
+                }
             }
         }
+        const float rstd = real ? in.rstd : 0.f;
         float normed[NV][8], g[NV][8], dot = 0.f;
         const uint64_t by = pack2(rstd, rstd);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            widen8(a[k], P.s.dtype, normed[k]);
-            widen8(b[k], 0, g[k]);
+            widen8(in.a[k], P.s.dtype, normed[k]);
+            widen8(in.b[k], 0, g[k]);
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
                 const uint64_t n = mul2(pack2(normed[k][i], normed[k][i + 1]), by), o = pack2(g[k][i], g[k][i + 1]);
@@ -446,55 +644,84 @@ __device__ __forceinline__ void act8_norm_grad_rows(const Act8NormGrad& P, float
         const uint64_t less = pack2(-mean, -mean);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (!real || !cols[k]) continue;
+            if (FULL && (!real || !cols[k])) continue;
             float x[8];
-            widen8(c[k], 0, x);
+            widen8(in.c[k], 0, x);
 #pragma unroll
             for (int i = 0; i < 8; i += 2)
                 unpack2(fma2(by, fma2(pack2(normed[k][i], normed[k][i + 1]), less, pack2(g[k][i], g[k][i + 1])), pack2(x[i], x[i + 1])),
                         x[i], x[i + 1]);
-            put8<FULL, T>(to + k * step, cols[k], P.d_x.wide, x);
+            put8<FULL, 32, T>(P.d_x, to + k * step, real ? cols[k] : 0, x);
         }
     }
     if (!P.sums) return;
-    float* to = P.sums + ((uint64_t)blockIdx.x * slots + slot) * P.cols;
+    float* to = P.sums + (uint64_t)blockIdx.x * P.pitch;
+    if (slots == 1) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const uint32_t col = (k * P.per_row + t) * 8;
-        if (FULL && cols[k]) {
+        for (int k = 0; k < NV; ++k) {
+            const uint32_t col = (k * P.per_row + t) * 8;
+            if (!cols[k]) continue;
             *reinterpret_cast<uint4*>(to + col) = Elem<float>::narrow(dw[k]);
             *reinterpret_cast<uint4*>(to + col + 4) = Elem<float>::narrow(dw[k] + 4);
-            continue;
         }
+        return;
+    }
+    // the rows at a time added up in shared memory
+    if (FULL) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+    }
+    float* all = reinterpret_cast<float*>(raw);
+    const uint32_t width = P.per_row * NV * 8;
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-            if (i < cols[k]) to[col + i] = dw[k][i];
+    for (int k = 0; k < NV; ++k) {
+        uint4* mine = reinterpret_cast<uint4*>(all + slot * width + (k * P.per_row + t) * 8);
+        mine[0] = Elem<float>::narrow(dw[k]);
+        mine[1] = Elem<float>::narrow(dw[k] + 4);
+    }
+    __syncthreads();
+    for (uint32_t col = threadIdx.x * 4; col < P.pitch; col += blockDim.x * 4) {
+        float v[4], x[4];
+        Elem<float>::widen(*reinterpret_cast<const uint4*>(all + col), v);
+        for (uint32_t s = 1; s < slots; ++s) {
+            Elem<float>::widen(*reinterpret_cast<const uint4*>(all + s * width + col), x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __fadd_rn(v[i], x[i]);
+        }
+        *reinterpret_cast<uint4*>(to + col) = Elem<float>::narrow(v);
     }
 }
 
 template <typename S, typename T, int NV>
 __global__ void __launch_bounds__(512) act8_norm_grad_kernel(const __grid_constant__ Act8NormGrad P) {
+    extern __shared__ __align__(16) unsigned char raw[];
     __shared__ float part[64];
     griddep_launch();
     griddep_wait();
-    if (P.full) act8_norm_grad_rows<S, T, NV, true>(P, part);
-    else act8_norm_grad_rows<S, T, NV, false>(P, part);
+    if (P.full) act8_norm_grad_rows<S, T, NV, true>(P, part, raw);
+    else act8_norm_grad_rows<S, T, NV, false>(P, part, raw);
 }
 
-// Columns of `count` vectors added: 32 columns a CTA, 16 threads a column.
-__global__ void __launch_bounds__(512) act8_add_kernel(const float* sums, uint32_t count, uint32_t cols, float* out) {
-    __shared__ float part[16][33];
+// Columns of `count` vectors added: 32 columns a CTA, 32 threads a column.
+__global__ void __launch_bounds__(1024) act8_add_kernel(const float* sums, uint32_t count, uint32_t pitch, uint32_t cols, float* out) {
+    __shared__ float part[32][33];
     const uint32_t col = blockIdx.x * 32u + (threadIdx.x & 31u), lane = threadIdx.x & 31u, row = threadIdx.x >> 5;
+    griddep_launch();
     griddep_wait();
     float v = 0.f;
     if (col < cols)
-#pragma unroll 4
-        for (uint32_t i = row; i < count; i += 16) v = __fadd_rn(v, sums[(uint64_t)i * cols + col]);
+        for (uint32_t i = row; i < count; i += 32 * 8) {
+            float x[8];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) x[j] = i + 32 * j < count ? sums[(uint64_t)(i + 32 * j) * pitch + col] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v = __fadd_rn(v, x[j]);
+        }
     part[row][lane] = v;
     __syncthreads();
     if (row || col >= cols) return;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) v = __fadd_rn(v, part[i][lane]);
+    for (int i = 1; i < 32; ++i) v = __fadd_rn(v, part[i][lane]);
     out[col] = v;
 }
 

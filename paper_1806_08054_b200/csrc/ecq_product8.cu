@@ -2,7 +2,6 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
-#include <mutex>
 
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -16,23 +15,6 @@ using namespace ecq;
 namespace {
 
 std::atomic<uint32_t> g_wait_limit{kWaitLimit};
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn tensor_map_encoder() {
-    static EncodeTiledFn fn = nullptr;
-    static std::once_flag once;
-    std::call_once(once, [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(p);
-    });
-    return fn;
-}
 
 // Boxes of 128 bytes along K and `box` rows; what is beyond the matrix arrives as zeros.
 bool entries_map(CUtensorMap* tm, const ecq_act8_matrix* m, uint64_t rows, uint64_t k, uint32_t box) {
@@ -61,19 +43,6 @@ bool scales_map(CUtensorMap* tm, const ecq_act8_matrix* m, uint64_t rows, uint64
     return tensor_map_encoder()(tm, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, m->scales, dims, strides, boxes, unit,
                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Kernels that take more shared memory than the default say so once a device.
-bool allow_smem(const void* kernel, size_t bytes, std::atomic<bool>* done) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev >= kMaxDevices) return false;
-    if (done[dev].load(std::memory_order_acquire)) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
-        cudaGetLastError();
-        return false;
-    }
-    done[dev].store(true, std::memory_order_release);
-    return true;
 }
 
 template <int CG, int TN, bool SWAP>
@@ -133,11 +102,11 @@ int ecq_act8_product(uint64_t m, uint64_t n, uint64_t k, const ecq_act8_matrix* 
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || !tensor_map_encoder())
         return ECQ_ERR_CUDA;
     Product8 P = {};
-    P.out = act8_mat(d, n);
+    P.out = act8_mat(d, m, n);
     const auto quad = [](const Act8Mat& x) { return aligned_to(x.data, x.dtype ? 8 : 16) && x.stride % (x.dtype ? 8 : 16) == 0; };
     P.out_quad = quad(P.out);
     if (c) {
-        const Act8Mat add = act8_mat(c, n);
+        const Act8Mat add = act8_mat(c, m, n);
         P.add = add.data;
         P.add_stride = add.stride;
         P.add_dtype = add.dtype;
@@ -154,7 +123,7 @@ int ecq_act8_product(uint64_t m, uint64_t n, uint64_t k, const ecq_act8_matrix* 
 
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (m == 1 && n * k <= 1u << 23 && d->dtype < 3) {
-        Product8Few F = {act8_mat(a, k), act8_mat(b, k), P.out, P.add, P.add_stride, P.cols, (uint32_t)k, 1, P.add_dtype};
+        Product8Few F = {act8_mat(a, m, k), act8_mat(b, n, k), P.out, P.add, P.add_stride, P.cols, (uint32_t)k, 1, P.add_dtype};
         const uint64_t warps = up(n, kFewRows);
         while (F.split < 8 && F.split * 512u < k && warps * F.split < (uint64_t)sms * 8) F.split *= 2;
         const uint32_t grid = up(warps * F.split, kFewThreads / 32);
