@@ -33,23 +33,26 @@ bool tile_map(CUtensorMap* tm, const Act8Mat& m, uint64_t rows, uint64_t cols) {
 
 template <int OP, typename S, typename T>
 int launch_tiles(Act8Tiles& P, cudaStream_t st) {
-    static std::atomic<bool> done[kMaxDevices];
     using R = Act8Ring<OP, S, T>;
-    auto kernel = act8_tile_kernel<OP, S, T>;
     int sms = 0;
     if (sm_count(sms) != ECQ_OK) return ECQ_ERR_CUDA;
-    // Tiles ahead where a CTA has several (8192 x 4096, in 8 bits transposed: 24.8 -> .. us)
+    // Tiles ahead of their turn where a CTA has several.  A tile a CTA, and that, in us: 8192 x 4096 from 8 to 8 bits transposed 24.8, 21.5;
+    // restored 19.7, 18.7; gate gradient 59, 46.5.  8192 x 1024: 7.0, 7.8; 6.3, 7.2; 18.2, 17.2.
     const uint32_t ctas = (uint32_t)sms * R::kCtas;
-    P.ahead = R::kStages && P.wide && P.rows >= 128 && P.cols >= 128 && P.tiles >= 4 * ctas;
-    if (P.ahead) {
-        if (!tensor_map_encoder() || !tile_map(&P.maps[0], P.in[0], P.rows, P.cols) ||
-            (OP != kActCopy && !tile_map(&P.maps[1], P.in[1], P.rows, P.cols)) ||
-            (OP == kActGateGrad && !tile_map(&P.maps[2], P.d, P.rows, P.cols)) ||
-            !allow_smem(reinterpret_cast<const void*>(kernel), R::kSmem, done))
-            return ECQ_ERR_CUDA;
-        return launch_act8(kernel, ctas, kActThreads, R::kSmem, 0, st, P);
+    if constexpr (R::kStages > 0) {
+        static std::atomic<bool> done[kMaxDevices];
+        auto kernel = act8_tiles_kernel<OP, S, T>;
+        Act8Maps maps = {};
+        if (P.wide && P.rows >= 128 && P.cols >= 128 && P.tiles >= (R::kCtas == 1 ? 2 : 4) * ctas) {
+            if (!tensor_map_encoder() || !tile_map(&maps.of[0], P.in[0], P.rows, P.cols) ||
+                (OP != kActCopy && !tile_map(&maps.of[1], P.in[1], P.rows, P.cols)) ||
+                (OP == kActGateGrad && !tile_map(&maps.of[2], P.d, P.rows, P.cols)) ||
+                !allow_smem(reinterpret_cast<const void*>(kernel), R::kSmem, done))
+                return ECQ_ERR_CUDA;
+            return launch_act8(kernel, ctas, kActThreads, R::kSmem, 0, st, P, maps);
+        }
     }
-    return launch_act8(kernel, P.tiles, kActThreads, 0, 0, st, P);
+    return launch_act8(act8_tile_kernel<OP, S, T>, P.tiles, kActThreads, 0, 0, st, P);
 }
 template <int OP, typename T>
 int launch_tiles(Act8Tiles& P, bool coded, cudaStream_t st) {

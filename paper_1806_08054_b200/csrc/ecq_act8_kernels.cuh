@@ -21,14 +21,12 @@ enum { kActCopy = 0, kActGate = 1, kActGateGrad = 2 };
 constexpr uint32_t kActThreads = 512;
 
 struct Act8Tiles {
-    CUtensorMap maps[3];                 // in[0], in[1] and d in boxes of 128 x 128, with `ahead`
     Act8Mat in[2];                       // x; gate and up
     Act8Mat d;                           // gradient of the activation's output
     Act8Mat plain[2], q[2], qt[2];       // results (data NULL: not wanted): h, or d_gate and d_up
     Act8Mat kept[2];                     // gate and up in 8 bits
     uint32_t rows, cols, tiles_across, tiles;
     int wide;                            // rows of all plain matrices begin on 16-byte boundaries
-    int ahead;                           // whole tiles are brought to shared memory ahead of their turn
 };
 
 // 1 / (1 + exp(-x)); WIDE: the rounding of x log2(e) is added back, which shows in 32 bits alone.
@@ -261,27 +259,56 @@ __device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& a
     }
 }
 
+__device__ __forceinline__ Act8Place act8_place(const Act8Tiles& P, uint32_t row0, uint32_t col0) {
+    Act8Place at;
+    at.row = row0 + 4 * (threadIdx.x >> 4);
+    at.col = col0 + 8 * (threadIdx.x & 15u);
+    at.n = inside(at.col, P.cols);
+    at.rows = at.row < P.rows ? min(4u, P.rows - at.row) : 0;
+    return at;
+}
+
+// A tile a CTA.
+template <int OP, typename S, typename T>
+__global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas) act8_tile_kernel(const __grid_constant__ Act8Tiles P) {
+    __shared__ __align__(16) Act8Turn turn;
+    const uint32_t row0 = blockIdx.x / P.tiles_across * 128u, col0 = blockIdx.x % P.tiles_across * 128u;
+    const Act8Place at = act8_place(P, row0, col0);
+    griddep_launch();
+    griddep_wait();
+    Act8Read<OP, S, T> in;
+    if (P.wide && row0 + 128 <= P.rows && col0 + 128 <= P.cols) {
+        act8_read<OP, S, T, true>(P, at, in);
+        act8_tile<OP, S, T, true>(P, at, in, turn);
+    } else {
+        act8_read<OP, S, T, false>(P, at, in);
+        act8_tile<OP, S, T, false>(P, at, in, turn);
+    }
+}
+
+struct Act8Maps { CUtensorMap of[3]; };  // in[0], in[1] and d in boxes of 128 x 128
+
 // CTAs stay on the GPU and take every n-th tile.  Whole tiles come by TMA as many ahead as there is room for: a
 // thread's four rows alone are too little on their way to memory, in 8 bits above all, and registers have
 // no room for the next tile's.  (A wait that runs out reads the tile from memory instead.)
 template <int OP, typename S, typename T>
-__global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas) act8_tile_kernel(const __grid_constant__ Act8Tiles P) {
+__global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas)
+    act8_tiles_kernel(const __grid_constant__ Act8Tiles P, const __grid_constant__ Act8Maps maps) {
     using R = Act8Ring<OP, S, T>;
-    constexpr uint32_t kStages = R::kStages ? R::kStages : 1;
+    constexpr uint32_t kStages = R::kStages;
     extern __shared__ unsigned char raw[];
     __shared__ __align__(16) Act8Turn turn;
     __shared__ __align__(8) uint64_t bars[kStages];
     const uint32_t ring = (smem_u32(raw) + 127u) & ~127u, full = smem_u32(bars), tid = threadIdx.x;
-    const bool ahead = R::kStages && P.ahead;
     auto whole = [&](uint32_t tile) {
         return (tile / P.tiles_across + 1) * 128u <= P.rows && (tile % P.tiles_across + 1) * 128u <= P.cols && P.wide;
     };
-    if (ahead && tid == 0) {
+    if (tid == 0) {
         for (uint32_t s = 0; s < kStages; ++s) mbar_init(full + 8 * s, 1);
         fence_mbar_init();
     }
     griddep_launch();
-    if (ahead) __syncthreads();
+    __syncthreads();
     griddep_wait();
     // by one thread: the next whole tile from `coming` on
     uint32_t coming = blockIdx.x;
@@ -293,46 +320,38 @@ __global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas) act8_t
         mbar_arrive_expect_tx(bar, R::kBytes);
 #pragma unroll
         for (int m = 0; m < (OP == kActCopy ? 1 : 2); ++m, to += R::kIn) {
-            tma_load_2d(to, &P.maps[m], (int)(tc * 128), (int)(tr * 128), bar);
+            tma_load_2d(to, &maps.of[m], (int)(tc * 128), (int)(tr * 128), bar);
             if (sizeof(S) == 1)
                 asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + 128 * 128),
                              "l"(P.in[m].scales + ((uint64_t)tr * P.in[m].groups + (tc >> 2)) * 512), "r"(512u), "r"(bar)
                              : "memory");
         }
-        if (OP == kActGateGrad) tma_load_2d(to, &P.maps[2], (int)(tc * 128), (int)(tr * 128), bar);
+        if (OP == kActGateGrad) tma_load_2d(to, &maps.of[2], (int)(tc * 128), (int)(tr * 128), bar);
         coming += gridDim.x;
     };
-    if (ahead && tid == 0)
+    if (tid == 0)
         for (uint32_t s = 0; s < kStages; ++s) ask(s);
     uint32_t it = 0;                                                 // whole tiles so far
     for (uint32_t tile = blockIdx.x; tile < P.tiles; tile += gridDim.x) {
         const uint32_t row0 = tile / P.tiles_across * 128u, col0 = tile % P.tiles_across * 128u;
-        Act8Place at;
-        at.row = row0 + 4 * (tid >> 4);
-        at.col = col0 + 8 * (tid & 15u);
-        at.n = inside(at.col, P.cols);
-        at.rows = at.row < P.rows ? min(4u, P.rows - at.row) : 0;
+        const Act8Place at = act8_place(P, row0, col0);
         Act8Read<OP, S, T> in;
         if (!whole(tile)) {
             act8_read<OP, S, T, false>(P, at, in);
             act8_tile<OP, S, T, false>(P, at, in, turn);
             continue;
         }
-        if (ahead) {
-            const uint32_t s = it % kStages, from = ring + s * R::kBytes;
-            if (mbar_wait(full + 8 * s, (it / kStages) & 1)) {
-                act8_take(from, col0 >> 7, in.a);
-                if constexpr (OP != kActCopy) act8_take(from + R::kIn, col0 >> 7, in.b);
-                if constexpr (OP == kActGateGrad) act8_take(from + 2 * R::kIn, 0, in.d);
-            } else {
-                act8_read<OP, S, T, true>(P, at, in);
-            }
-            ++it;
-            __syncthreads();                                         // everyone has read the stage
-            if (tid == 0) ask(s);
+        const uint32_t s = it % kStages, from = ring + s * R::kBytes;
+        if (mbar_wait(full + 8 * s, (it / kStages) & 1)) {
+            act8_take(from, col0 >> 7, in.a);
+            if constexpr (OP != kActCopy) act8_take(from + R::kIn, col0 >> 7, in.b);
+            if constexpr (OP == kActGateGrad) act8_take(from + 2 * R::kIn, 0, in.d);
         } else {
             act8_read<OP, S, T, true>(P, at, in);
         }
+        ++it;
+        __syncthreads();                                             // everyone has read the stage
+        if (tid == 0) ask(s);
         act8_tile<OP, S, T, true>(P, at, in, turn);
     }
 }
