@@ -119,9 +119,8 @@ __device__ __forceinline__ void act8_put_turned(const Act8Mat& m, const Act8Plac
     float y[8][4];
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
-        const uint64_t by2 = pack2(down[i], down[i]);
-        unpack2(mul2(pack2(v[0][i], v[1][i]), by2), y[i][0], y[i][1]);
-        unpack2(mul2(pack2(v[2][i], v[3][i]), by2), y[i][2], y[i][3]);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) y[i][j] = __fmul_rn(v[j][i], down[i]);   // not in pairs: rows are none
     }
     if (m.dtype == 3) {
 #pragma unroll
