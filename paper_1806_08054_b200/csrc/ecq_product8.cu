@@ -54,6 +54,38 @@ int launch_part(Product8& P, uint32_t parts, cudaStream_t st) {
     return launch_act8(kernel, P.tiles * parts * CG, S::kThreads, S::kSmem, parts * CG, st, P);
 }
 
+// Clusters of `parts` CTAs (pairs) that the current device holds at once: a cluster stays in a group of SMs, so
+// that there may be fewer than SMs would be enough for.
+template <int CG>
+uint32_t clusters_at_once(uint32_t parts, int dev, int sms) {
+    if (parts * CG == 1) return (uint32_t)sms;
+    static std::atomic<uint32_t> known[kMaxDevices][4];
+    const int at = parts == 1 ? 0 : parts == 2 ? 1 : parts == 4 ? 2 : 3;
+    uint32_t have = known[dev][at].load(std::memory_order_acquire);
+    if (have) return have;
+    using S = ProdPart<CG, 128, false>;
+    auto kernel = act8_product_part_kernel<CG, 128, false>;
+    static std::atomic<bool> done[kMaxDevices];
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute size;
+    size.id = cudaLaunchAttributeClusterDimension;
+    size.val.clusterDim.x = parts * CG;
+    size.val.clusterDim.y = size.val.clusterDim.z = 1;
+    cfg.gridDim = dim3(parts * CG);
+    cfg.blockDim = dim3(S::kThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.attrs = &size;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (!allow_smem(reinterpret_cast<const void*>(kernel), S::kSmem, done) || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;                                                     // not known: asked again
+    }
+    have = (uint32_t)std::max(0, n);
+    known[dev][at].store(have, std::memory_order_release);
+    return have;
+}
+
 int launch_pair(Product8& P, uint32_t pairs, cudaStream_t st) {
     static std::atomic<bool> done[kMaxDevices];
     if (!allow_smem(reinterpret_cast<const void*>(act8_product_pair_kernel), ProdPair::kSmem, done)) return ECQ_ERR_CUDA;
@@ -62,24 +94,30 @@ int launch_pair(Product8& P, uint32_t pairs, cudaStream_t st) {
 
 uint32_t up(uint64_t x, uint32_t by) { return (uint32_t)((x + by - 1) / by); }
 
-// Tiles of 256 x 256 by pairs of CTAs with all of K (cg 0), or K shared out over `parts` CTAs (cg 1, tiles of 128
-// x 128) or pairs (cg 2), by an estimate of the time in us.  A launch; steps of 128 along K, 32 KB a CTA: 0.28 us each
-// (the 64 bytes a clock that an SM takes), up to 0.48 where all SMs load; where K is shared the sums'
-// way through shared memory; and results that do not go out by TMA (`slow`), or that are added to what is there.  Measured (pairs, 128 x 128
-// in 2, 4, 8 parts, pairs in 2):
-//     1024 x 1024 x 8192     24.0   16.9   25.7   51.4   18.5       128 x 4096 x 1024    6.9    7.1    7.4   20.0    9.2
-//     300 x 500 x 1000, slow 10.3    9.4    7.9    8.4   13.6       128 x 4096 x 4096   15.2   11.9   11.4   26.4   14.2
-void choose(uint64_t tiles256, uint64_t tiles128, uint32_t steps, int sms, bool slow, bool in_place, int& cg, uint32_t& parts) {
-    const uint64_t pairs = (uint64_t)sms / 2;
-    double best = 3.9 + (slow ? 4.0 : in_place ? 2.0 : 0.0) +
+// Tiles of 256 x 256 by pairs of CTAs that stay (cg 0); or a tile of 128 x 128 a CTA (cg 1) or of 256 x 128 a pair (cg
+// 2), K shared out over `parts` of them.  By an estimate of the time in us: a launch, with its first loads and last results; steps of 128
+// along K, 0.28 us each where a CTA takes 32 KB (64 bytes a clock), 0.27 in tiles of 256 x 128, for pairs up to 0.48 when all
+// SMs load; the sums' way between CTAs; and results that do not go out by TMA (`slow`) or are added to what is there.
+// Measured, cg 0, then cg 1 in 1, 2, 4, 8 parts, then cg 2 in 1, 2, 4:
+//     1024 x 1024 x 8192   23.7   23.3  15.6  23.1  45.3   22.2  15.3  31.8      300 x 504 x 1000    8.4   7.0  6.3  6.3  7.2   6.6  5.9  6.3
+//     128 x 4096 x 4096    14.7   14.0  10.6   9.9  23.8   13.6  11.1  25.5      512 x 4096 x 1024   7.9   7.1 13.7 27.9 62.0   7.8 14.1 33.8
+//     the first, added     26.1   29.9  18.8  26.2  51.8   28.8  18.5  36.4      1000 x 2049 x 1537 15.7  13.4 19.8 38.1 74.2  13.3 25.0 40.3
+struct Way { uint32_t cg, parts; };
+
+Way choose(uint64_t m, uint64_t n, uint32_t steps, int dev, int sms, bool slow, bool in_place) {
+    const uint64_t pairs = (uint64_t)sms / 2, tiles256 = (uint64_t)up(m, 256) * up(n, 256);
+    double best = 4.8 + (slow ? 5.0 : in_place ? 2.4 : 0.0) +
                   (double)((tiles256 + pairs - 1) / pairs) * steps * (0.28 + 0.2 * std::min(1.0, (double)tiles256 / (double)pairs));
-    for (int way = 1; way <= 2; ++way)
-        for (uint32_t p = 2; p <= (way == 1 ? 8u : 2u) && 2 * p <= steps; p *= 2) {
-            const uint64_t ctas = way == 1 ? tiles128 * p : tiles256 * p * 2;
-            if (ctas > (uint64_t)sms) break;
-            const double t = (way == 1 ? 6.7 : 8.5) + (slow ? (way == 1 ? 10.0 / p : 14.0) : in_place ? 1.3 : 0.0) + (double)((steps + p - 1) / p) * (0.28 + 0.04 * (double)ctas / sms);
-            if (t < best) { best = t; cg = way; parts = p; }
+    Way way = {0, 1};
+    for (uint32_t cg = 1; cg <= 2; ++cg)
+        for (uint32_t p = 1; p <= (cg == 1 ? 8u : 4u) && p <= steps; p *= 2) {
+            const uint64_t clusters = (uint64_t)up(m, 128 * cg) * up(n, 128), ctas = clusters * p * cg;
+            if (ctas > (uint64_t)sms || clusters > (cg == 1 ? clusters_at_once<1>(p, dev, sms) : clusters_at_once<2>(p, dev, sms))) break;
+            const double t = (p == 1 ? 4.5 : 5.5 + 1.5 * (double)ctas / sms) + (slow ? 4.0 / p : in_place ? 5.0 / p : 0.0) +
+                             (double)((steps + p - 1) / p) * (cg == 1 ? 0.28 : 0.27);
+            if (t < best) { best = t; way = {cg, p}; }
         }
+    return way;
 }
 
 }  // namespace
@@ -98,7 +136,7 @@ int ecq_act8_product(uint64_t m, uint64_t n, uint64_t k, const ecq_act8_matrix* 
         return ECQ_ERR_ARG;
     if (m == 0) return ECQ_OK;
     int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= kMaxDevices ||
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || !tensor_map_encoder())
         return ECQ_ERR_CUDA;
     Product8 P = {};
@@ -147,17 +185,19 @@ int ecq_act8_product(uint64_t m, uint64_t n, uint64_t k, const ecq_act8_matrix* 
         return right_box == 16 ? launch_part<1, 16, true>(P, parts, st)
              : right_box == 32 ? launch_part<1, 32, true>(P, parts, st) : launch_part<1, 64, true>(P, parts, st);
     }
-    const uint64_t tiles256 = (uint64_t)up(m, 256) * up(n, 256), tiles128 = (uint64_t)up(m, 128) * up(n, 128);
-    int cg = 0;
-    uint32_t parts = 1;
     const bool in_place = P.add && P.out.wide && P.add == P.out.data && P.add_stride == P.out.stride && P.add_dtype == 0 && P.out.dtype == 0;
-    if (d->dtype < 3) choose(tiles256, tiles128, P.steps, sms, !P.out.wide || (P.add && !in_place), in_place, cg, parts);
-    P.in_place = in_place;
-    const uint32_t side = cg == 1 ? 128 : 256;
-    P.across = up(n, side);
-    P.tiles = (uint32_t)(cg == 1 ? tiles128 : tiles256);
-    if (cg == 0 && P.out.wide && !result_map(&P.result, P.out, m, n)) return ECQ_ERR_CUDA;
-    return cg == 0 ? launch_pair(P, (uint32_t)sms / 2, st) : cg == 1 ? launch_part<1, 128, false>(P, parts, st) : launch_part<2, 256, false>(P, parts, st);
+    Way way = {0, 1};
+    if (d->dtype < 3) way = choose(m, n, P.steps, dev, sms, !P.out.wide || (P.add && !in_place), in_place);
+    P.in_place = in_place && way.cg == 0;
+    P.across = up(n, way.cg ? 128 : 256);
+    P.tiles = up(m, way.cg == 1 ? 128 : 256) * P.across;
+    if (way.cg == 1) return launch_part<1, 128, false>(P, way.parts, st);
+    if (way.cg == 2) {
+        if (!entries_map(&P.right, b, n, k, 64)) return ECQ_ERR_CUDA;
+        return launch_part<2, 128, false>(P, way.parts, st);
+    }
+    if (P.out.wide && !result_map(&P.result, P.out, m, n)) return ECQ_ERR_CUDA;
+    return launch_pair(P, (uint32_t)sms / 2, st);
 }
 
 }  // extern "C"

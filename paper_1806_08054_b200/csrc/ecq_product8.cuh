@@ -84,6 +84,17 @@ __device__ __forceinline__ void tma_add_2d(const void* tmap, int x, int y, uint3
                  : "memory");
 }
 
+// Stores to a CTA of the cluster that count their bytes on a barrier of it.
+__device__ __forceinline__ void send4(uint32_t to, float v, uint32_t bar) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to), "r"(__float_as_uint(v)), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void send16(uint32_t to, const float* v, uint32_t bar) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1,%2,%3,%4}, [%5];" ::"r"(to), "f"(v[0]), "f"(v[1]),
+                 "f"(v[2]), "f"(v[3]), "r"(bar)
+                 : "memory");
+}
+
 // Arrive on a barrier of each of `ctas` when every product issued so far has completed.
 __device__ __forceinline__ void umma_commit_to(uint32_t bar, uint16_t ctas) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(ctas)
@@ -316,49 +327,53 @@ __global__ void __launch_bounds__(kFewThreads) act8_product_few_kernel(const __g
 
 // ---- a tile, K over a cluster ------------------------------------------------------------------------
 //
-// For products that have few tiles: a cluster's CTAs (with CG = 2 pairs of CTAs, which have 256 x 256 together)
-// have a part of K each.  Their sums meet through shared memory: each CTA finishes its share of the
-// tile, to which all others have sent theirs, and adds them in a fixed order.  SWAP: the left operand is B and
-// the right one A (a few tokens), the tile is D's transposed; so a matrix of weights fills the 128 rows of
-// an instruction.
+// For products that have few tiles: tiles of 128 x 128 by one CTA or 256 x 128 by a pair (CG = 2: 24 KB for what
+// two CTAs alone need 32 each), K shared out over the CTAs (pairs) of a cluster.  Each of them finishes its share of the
+// tile: the others send it theirs, by stores that count bytes on a barrier of its own, to a place that no
+// load uses, and it adds them in a fixed order.  (Both ways through the loads' ring, with a barrier of the cluster
+// before and behind: 1.. us more.)  SWAP: the left operand is B and the right one A (a few tokens), the tile is D's
+// transposed; so a matrix of weights fills the 128 rows of an instruction.
 
 template <int CG, int TN, bool SWAP>
 struct ProdPart {
     static constexpr uint32_t kRight = TN / CG * kProdRow;
-    static constexpr uint32_t kStage = kProdBox + kRight;
-    static constexpr uint32_t kStages = 6;
-    static constexpr uint32_t kOutRows = SWAP ? TN : 128, kOutCols = SWAP ? 128 : TN;   // of the result, this CTA's
-    static constexpr uint32_t kRing = kStages * kStage, kSums = kOutRows * kOutCols * 4;
-    static constexpr uint32_t kRightGroups = TN > 128 ? 2 : 1, kScales = 512 * (1 + kRightGroups);
-    static constexpr uint32_t kSmem = (kRing > kSums ? kRing : kSums) + kStages * kScales + 1024;
+    static constexpr uint32_t kStage = kProdBox + kRight, kScales = 1024;
+    static constexpr uint32_t kMostParts = CG == 2 ? 4 : 8;
+    // what the others send: columns of 128 rows, or rows (tokens) of 128 columns (and this CTA's own)
+    static constexpr uint32_t kSums = SWAP ? TN * 512u : 128u * TN * 4u / kMostParts * (kMostParts - 1);
+    static constexpr uint32_t kFit = (226u * 1024u - kSums) / (kStage + kScales), kStages = kFit < 7 ? kFit : 7;
+    static constexpr uint32_t kSmem = kStages * (kStage + kScales) + kSums + 1024;
     static constexpr uint32_t kScaleCols = TN < 32 ? 32 : TN;         // first column of scales in tensor memory
-    static constexpr uint32_t kSlotCols = 4 * (1 + kRightGroups);
-    static constexpr uint32_t kTmem = TN <= 64 ? 128 : TN <= 128 ? 256 : 512;
+    static constexpr uint32_t kTmem = TN <= 64 ? 128 : 256;
     static constexpr uint32_t kThreads = 12 * 32;
-    static_assert(CG == 1 || (TN == 256 && !SWAP), "");
+    static_assert(CG == 1 || (TN == 128 && !SWAP), "");
 };
 
 template <int CG, int TN, bool SWAP>
 __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_product_part_kernel(const __grid_constant__ Product8 P) {
     using S = ProdPart<CG, TN, SWAP>;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 1];
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t stop;
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
-    const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u, scales = ring + (S::kSmem - 1024u - S::kStages * S::kScales);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages;
+    const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u, scales = ring + S::kStages * S::kStage, sums = scales + S::kStages * S::kScales;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, come = done + 8;
     uint32_t ctas;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
     const uint32_t cta = cta_rank(), rank = CG == 2 ? cta & 1u : 0, part = cta / CG, parts = ctas / CG, first = cta - rank;
     const uint32_t tile = blockIdx.x / ctas;
     const uint32_t left0 = tile / P.across * (128u * CG) + rank * 128u, right0 = tile % P.across * (uint32_t)TN;
     const uint32_t k0 = (uint32_t)((uint64_t)part * P.steps / parts), k1 = (uint32_t)((uint64_t)(part + 1) * P.steps / parts);
+    const uint32_t own = TN / parts;                                  // columns that a CTA finishes (16 at least), or rows with SWAP
+    const uint32_t own_row0 = right0 + part * own, own_rows = own_row0 < P.rows ? min(own, P.rows - own_row0) : 0;   // SWAP
     if (tid == 0) {
         for (uint32_t s = 0; s < S::kStages; ++s) { mbar_init(full + 8 * s, 2); mbar_init(empty + 8 * s, 1); }
         mbar_init(done, 1);
+        mbar_init(come, 1);
         stop = 0;
         fence_mbar_init();
+        mbar_arrive_expect_tx(come, (parts - 1) * (SWAP ? own_rows : own) * 512u);
     }
     if ((warp == 8 || warp == 10) && elect_one()) {
         prefetch_map(warp == 8 ? &P.left : &P.right);
@@ -367,7 +382,7 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
     if (warp == 9) tmem_alloc<CG>(smem_u32(&tmem_slot), S::kTmem);
     tcgen05_before_sync();
     __syncthreads();
-    if (CG == 2) pair_sync();
+    pair_sync();                                                      // the others' barriers are there
     tcgen05_after_sync();
     const uint32_t tmem = tmem_slot;
     griddep_launch();
@@ -382,17 +397,14 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
             const uint32_t at = left ? 0 : kProdBox, bytes = left ? kProdBox : S::kRight;
             const uint32_t row = left ? left0 : right0 + rank * (TN / CG), groups = left ? P.left_groups : P.right_groups;
             const uint32_t group0 = ((left ? left0 : right0) >> 7) * groups, sat = scales + (left ? 0 : 512);
-            const uint32_t sbytes = left ? 512u : 512u * S::kRightGroups;
             uint32_t it = 0;
             for (uint32_t k = k0; k < k1; ++k, ++it) {
                 const uint32_t s = it % S::kStages, bar = CG == 1 ? full + 8 * s : peer_addr(full + 8 * s, first);
                 if (!wait_or_stop(empty + 8 * s, ((it / S::kStages) & 1) ^ 1, P.wait_limit, &stop)) break;
                 const bool with = k == k0 || (k & 3) == 0;
-                if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * (bytes + (with ? sbytes : 0u)));
+                if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, CG * (bytes + (with ? 512u : 0u)));
                 prod_load<CG>(ring + s * S::kStage + at, map, k * kProdRow, row, bar);
-                if (!with) continue;
-                prod_load<CG>(sat + s * S::kScales, smap, 0, group0 + (k >> 2), bar);
-                if (!left && S::kRightGroups == 2) prod_load<CG>(sat + s * S::kScales + 512, smap, 0, group0 + groups + (k >> 2), bar);
+                if (with) prod_load<CG>(sat + s * S::kScales, smap, 0, group0 + (k >> 2), bar);
             }
             // none of them is in flight when this CTA leaves
             for (uint32_t b = 0; b < S::kStages && b < it; ++b) {
@@ -416,9 +428,10 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
                 tcgen05_after_sync();
                 if (k == k0 || (k & 3) == 0) {
                     // one of three places in turn: what used it last is two whole groups behind, and over
-                    slot = it == 0 ? tmem + S::kScaleCols : slot == tmem + S::kScaleCols + 2 * S::kSlotCols ? tmem + S::kScaleCols : slot + S::kSlotCols;
-#pragma unroll
-                    for (uint32_t g = 0; g < 1 + S::kRightGroups; ++g) umma_scales<CG>(slot + 4 * g, scales + s * S::kScales + 512 * g);
+                    const uint32_t base = tmem + S::kScaleCols;
+                    slot = it == 0 || slot == base + 16 ? base : slot + 8;
+                    umma_scales<CG>(slot, scales + s * S::kScales);
+                    umma_scales<CG>(slot + 4, scales + s * S::kScales + 512);
                 }
                 const uint32_t id = idesc | (k & 3) << 29 | (k & 3) << 4, steps = k + 1 == P.steps ? P.tail : 4;
                 const uint64_t a = umma_desc_swizzled(ring + s * S::kStage), b = umma_desc_swizzled(ring + s * S::kStage + kProdBox);
@@ -431,161 +444,148 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
         }
         __syncwarp();
     }
-    // every product of this CTA is done, and with them its loads: the ring has room for sums
-    const bool mine = wait_or_stop(done, 0, P.wait_limit, &stop);
-    __syncwarp();
-    tcgen05_after_sync();
-    pair_sync();
+    // ---- results, by eight warps: 32 rows of the tile and every second 16 columns of it
     const uint32_t quad = warp & 3, half = warp >> 2, from = tmem + ((quad * 32u) << 16);
-    const bool good = mine && !stop;
-    // Not SWAP: each CTA finishes 1 / parts of the tile's columns, a lane a row.  Of what it is sent, 16 bytes
-    // of 32 rows lie together, then the next four columns.
-    const uint32_t own = TN / parts;                                  // columns that a CTA finishes: 16 at least
-    if (!SWAP && warp < 8) {
-        for (uint32_t c = half * 16u; c < (uint32_t)TN; c += 32) {
-            const uint32_t to = c / own, at = c - to * own;
-            if (to == part) continue;
-            float y[16];
+    if (warp < 8) {
+        const bool good = __all_sync(~0u, wait_or_stop(done, 0, P.wait_limit, &stop));
+        tcgen05_after_sync();
+        auto fetch = [&](uint32_t c, float* y) {
             tmem_load16(from + c, y);
             if (!good)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(0x7FC00000u);
-            const uint32_t base = peer_addr(ring + ((part * 4 + quad) * own + at) * 128u + lane * 16u, to * CG + rank);
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i)
-                asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(base + i * 512u), "f"(y[4 * i]), "f"(y[4 * i + 1]),
-                             "f"(y[4 * i + 2]), "f"(y[4 * i + 3]) : "memory");
-        }
-    }
-    // SWAP: rows of the result (tokens) are shared out, a lane has a column
-    const uint32_t share = S::kOutRows / parts;
-    constexpr uint32_t kRowBytes = S::kOutCols * 4;
-    if (SWAP && warp < 8) {
-        constexpr uint32_t kCols = TN / 2 < 16 ? 16 : TN / 2;
-        if (half * kCols < (uint32_t)TN) {
-#pragma unroll
-            for (uint32_t b = 0; b < kCols; b += 16) {
+        };
+        if (SWAP) {
+            // rows of the result (tokens) are shared out, a lane has a column
+            for (uint32_t c = half * 16u; c < (uint32_t)TN; c += 32) {
                 float y[16];
-                tmem_load16(from + half * kCols + b, y);
-                if (!good)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(0x7FC00000u);
-                const uint32_t c = quad * 32u + lane;
+                fetch(c, y);
 #pragma unroll
                 for (uint32_t i = 0; i < 16; ++i) {
-                    const uint32_t row = half * kCols + b + i, to = row / share, local = row - to * share;
-                    if (row >= P.rows) break;
-                    const uint32_t at = ring + (part * share + local) * kRowBytes + 4 * c;
-                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(at, to)), "f"(y[i]) : "memory");
+                    const uint32_t row = c + i, to = row / own, local = row - to * own;
+                    if (right0 + row >= P.rows) break;
+                    const uint32_t at = sums + (part * own + local) * 512u + 4 * (quad * 32u + lane);
+                    if (to == part) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(y[i]) : "memory");
+                    else send4(peer_addr(at, to), y[i], peer_addr(come, to));
                 }
+            }
+        } else {
+            // 16 bytes of 32 rows lie together, then the next four columns
+            for (uint32_t c = half * 16u; c < (uint32_t)TN; c += 32) {
+                const uint32_t to = c / own, at = c - to * own;
+                if (to == part) continue;
+                float y[16];
+                fetch(c, y);
+                const uint32_t from_part = part > to ? part - 1 : part;   // places of the others, without its own
+                const uint32_t base = peer_addr(sums + ((from_part * 4 + quad) * own + at) * 128u + lane * 16u, to * CG + rank);
+                const uint32_t bar = peer_addr(come, to * CG + rank);
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) send16(base + i * 512u, y + 4 * i, bar);
             }
         }
-    }
-    tcgen05_before_sync();
-    pair_sync();
-    const bool lost = stop;                                           // loads may have landed on the sums
-    if (!SWAP && warp < 8) {
-        tcgen05_after_sync();
-        const bool straight = P.out.wide && (!P.add || P.add_wide);
-        const uint32_t row = left0 + quad * 32u + lane;
-        for (uint32_t c = half * 16u; c < own; c += 32) {
-            const uint32_t col = right0 + part * own + c;
-            float y[16], add[16];
-            if (straight && P.add && row < P.rows) prod_get16(P, row, col, add);
-            __syncwarp();
-            tmem_load16(from + part * own + c, y);
-            for (uint32_t p = 0; p < parts; ++p) {
-                if (p == part) continue;
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    float x[4];
-                    Elem<float>::widen(lds16(ring + ((p * 4 + quad) * own + c + 4 * i) * 128u + lane * 16u), x);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) y[4 * i + j] = __fadd_rn(y[4 * i + j], x[j]);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if (straight && P.add) y[i] = __fadd_rn(y[i], add[i]);
-                if (lost || !good) y[i] = __uint_as_float(0x7FC00000u);
-            }
-            if (straight) {
-                if (row < P.rows) prod_put16(P, row, col, y);
+        if (SWAP) named_bar_sync(1, 256);                             // this CTA's own sums
+        const bool all = __all_sync(~0u, parts == 1 || wait_pair_or_stop(come, 0, P.wait_limit, &stop)) && good;
+        if (!SWAP) {
+            const bool straight = P.out.wide && (!P.add || P.add_wide);
+            const uint32_t row = left0 + quad * 32u + lane;
+            for (uint32_t c = half * 16u; c < own; c += 32) {
+                const uint32_t col = right0 + part * own + c;
+                float y[16], add[16];
+                if (straight && P.add && row < P.rows) prod_get16(P, row, col, add);
                 __syncwarp();
-                continue;
-            }
-            // rows that begin anywhere: turned, so that 16 lanes write a row's columns
-            const uint32_t turned = ring + 128u * TN * 4u + warp * 2048u;
-            __syncwarp();
+                fetch(part * own + c, y);
+                for (uint32_t p = 0; p + 1 < parts; ++p) {
 #pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) sts16(turned + lane * 64u + ((i ^ ((lane >> 1) & 3u)) << 4), Elem<float>::narrow(y + 4 * i));
-            __syncwarp();
-            const uint32_t x = lane & 15u, row0 = left0 + quad * 32u;
-            if (col + x < P.cols)
-                for (uint32_t r0 = lane >> 4; r0 < 32; r0 += 16) {
-                    float c[8];                                      // all before the first is written: D may be C
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        float x[4];
+                        Elem<float>::widen(lds16(sums + ((p * 4 + quad) * own + c + 4 * i) * 128u + lane * 16u), x);
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i)
-                        c[i] = P.add && row0 + r0 + 2 * i < P.rows ? prod_get1(P, row0 + r0 + 2 * i, col + x) : 0.f;
-#pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) {
-                        const uint32_t r = r0 + 2 * i;
-                        const float v = lds1(turned + r * 64u + (((x >> 2) ^ ((r >> 1) & 3u)) << 4) + 4 * (x & 3));
-                        if (row0 + r < P.rows) prod_put1(P, row0 + r, col + x, P.add ? __fadd_rn(v, c[i]) : v);
+                        for (int j = 0; j < 4; ++j) y[4 * i + j] = __fadd_rn(y[4 * i + j], x[j]);
                     }
                 }
-            __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (straight && P.add) y[i] = __fadd_rn(y[i], add[i]);
+                    if (!all) y[i] = __uint_as_float(0x7FC00000u);
+                }
+                if (straight) {
+                    if (row < P.rows) prod_put16(P, row, col, y);
+                    __syncwarp();
+                    continue;
+                }
+                // rows that begin anywhere: turned, so that 16 lanes write a row's columns.  (The loads' ring is free.)
+                const uint32_t turned = ring + warp * 2048u;
+                __syncwarp();
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) sts16(turned + lane * 64u + ((i ^ ((lane >> 1) & 3u)) << 4), Elem<float>::narrow(y + 4 * i));
+                __syncwarp();
+                const uint32_t x = lane & 15u, row0 = left0 + quad * 32u;
+                if (col + x < P.cols)
+                    for (uint32_t r0 = lane >> 4; r0 < 32; r0 += 16) {
+                        float add8[8];                               // all before the first is written: D may be C
+#pragma unroll
+                        for (uint32_t i = 0; i < 8; ++i)
+                            add8[i] = P.add && row0 + r0 + 2 * i < P.rows ? prod_get1(P, row0 + r0 + 2 * i, col + x) : 0.f;
+#pragma unroll
+                        for (uint32_t i = 0; i < 8; ++i) {
+                            const uint32_t r = r0 + 2 * i;
+                            const float v = lds1(turned + r * 64u + (((x >> 2) ^ ((r >> 1) & 3u)) << 4) + 4 * (x & 3));
+                            if (row0 + r < P.rows) prod_put1(P, row0 + r, col + x, P.add ? __fadd_rn(v, add8[i]) : v);
+                        }
+                    }
+                __syncwarp();
+            }
+        } else {
+            const uint32_t col = left0 + 4 * lane, n = inside4(col, P.cols);
+            for (uint32_t local = warp; local < own_rows; local += 8) {
+                const uint32_t row = own_row0 + local;
+                float y[4] = {0.f, 0.f, 0.f, 0.f}, c[4];
+                if (P.add) prod_get4(P, row, col, n, c);
+                for (uint32_t p = 0; p < parts; ++p) {
+                    float x[4];
+                    Elem<float>::widen(lds16(sums + (p * own + local) * 512u + lane * 16u), x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = __fadd_rn(y[i], x[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (P.add) y[i] = __fadd_rn(y[i], c[i]);
+                    if (!all) y[i] = __uint_as_float(0x7FC00000u);
+                }
+                if (P.out.dtype < 3) {
+                    if (n) prod_put4(P, row, col, n, y);
+                    continue;
+                }
+                uint32_t top = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    if (i < n) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+                top = __reduce_max_sync(~0u, top);
+                const uint32_t byte = act8_byte(top, P.out.dtype);
+                uint32_t w;
+                act8_code<4>(y, act8_down(byte), P.out.dtype, &w);
+                unsigned char* to = P.out.data + row * P.out.stride + col;
+                if (n == 4) {
+                    *reinterpret_cast<uint32_t*>(to) = w;
+                } else {
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
+                        if (i < n) to[i] = (unsigned char)(w >> (8 * i));
+                }
+                if (lane == 0) P.out.scales[act8_scale_at(row, left0 >> 7, P.out.groups)] = (uint8_t)byte;
+            }
         }
         tcgen05_before_sync();
     }
-    if (SWAP && warp < 8) {
-        const uint32_t row0 = right0 + part * share, col = left0 + 4 * lane, n = inside4(col, P.cols);
-        for (uint32_t local = warp; local < share && row0 + local < P.rows; local += 8) {
-            const uint32_t row = row0 + local;
-            float y[4] = {0.f, 0.f, 0.f, 0.f}, c[4];
-            if (P.add) prod_get4(P, row, col, n, c);
-            for (uint32_t p = 0; p < parts; ++p) {
-                float x[4];
-                Elem<float>::widen(lds16(ring + (p * share + local) * kRowBytes + lane * 16u), x);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = __fadd_rn(y[i], x[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (P.add) y[i] = __fadd_rn(y[i], c[i]);
-                if (lost) y[i] = __uint_as_float(0x7FC00000u);
-            }
-            if (P.out.dtype < 3) {
-                if (n) prod_put4(P, row, col, n, y);
-                continue;
-            }
-            uint32_t top = 0;
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i)
-                if (i < n) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
-            top = __reduce_max_sync(~0u, top);
-            const uint32_t byte = act8_byte(top, P.out.dtype);
-            uint32_t w;
-            act8_code<4>(y, act8_down(byte), P.out.dtype, &w);
-            unsigned char* to = P.out.data + row * P.out.stride + col;
-            if (n == 4) {
-                *reinterpret_cast<uint32_t*>(to) = w;
-            } else {
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i)
-                    if (i < n) to[i] = (unsigned char)(w >> (8 * i));
-            }
-            if (lane == 0) P.out.scales[act8_scale_at(row, left0 >> 7, P.out.groups)] = (uint8_t)byte;
-        }
-    }
-    if (!SWAP) {                                                      // everyone has read tensor memory
-        __syncthreads();
-        if (CG == 2) pair_sync();
-    }
+    __syncthreads();                                                  // tensor memory is read
+    pair_sync();                                                      // nobody sends any more
+    tcgen05_after_sync();
     if (warp == 9) tmem_free<CG>(tmem, S::kTmem);
-    if (lost) {
+    // After a wait that ran out, sums, loads and arrivals that this CTA did not wait for may still be on their way
+    // to it; the others have issued their last by now.
+    if (stop) {
         if (tid == 0 && P.status) atomicOr(P.status, kStatusTimeout);
-        for (const long long since = clock64(); clock64() - since < 20000;) {}   // for what is still on its way
+        for (const long long since = clock64(); clock64() - since < 20000;) {}
     }
 }
 
