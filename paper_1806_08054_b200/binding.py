@@ -679,6 +679,14 @@ def _vector(t, dtype, n: int, name: str, device: int):
     return t.data_ptr()
 
 
+# The three above as compiled code, where it was built (``csrc/ecq_marshal.cpp``).
+_in_python = (_matrix, _size, _vector)
+try:
+    from ._marshal import matrix as _matrix, size as _size, vector as _vector  # noqa: F811
+except ImportError:
+    pass
+
+
 def _weight(w, n: int, device: int):
     if w is None:
         return None, 0

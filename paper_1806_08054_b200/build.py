@@ -29,8 +29,38 @@ def _stale() -> bool:
     return any(os.path.getmtime(p) > t for p in deps)
 
 
+MARSHAL = os.path.join(_HERE, "_marshal.so")
+
+
+def build_marshal(force: bool = False) -> bool:
+    """Compile the binding's argument marshalling (``csrc/ecq_marshal.cpp``) next to this file.  Where that cannot
+    be done (no headers of Python or torch) the binding does the same in Python, a few microseconds a call slower."""
+    source = os.path.join(CSRC, "ecq_marshal.cpp")
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= os.path.getmtime(source):
+        return True
+    import sysconfig
+    import torch
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")      # loaded by torch before this is
+    base = os.path.join(os.path.dirname(torch.__file__), "include")
+    tmp = MARSHAL + ".tmp.%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-I" + sysconfig.get_paths()["include"], "-I" + base,
+           "-I" + os.path.join(base, "torch", "csrc", "api", "include"), source, "-o", tmp,
+           "-L" + libs, "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    try:
+        done = subprocess.run(cmd, capture_output=True, text=True)
+    except OSError as e:
+        print("ecq_marshal.cpp is not built: %s" % e)
+        return False
+    if done.returncode:
+        print("ecq_marshal.cpp is not built:\n" + done.stderr[-2000:])
+        return False
+    os.replace(tmp, MARSHAL)
+    return True
+
+
 def build_library(force: bool = False, verbose: bool = False) -> str:
     """Compile ``libecq.so`` next to this file if it is missing or out of date."""
+    build_marshal(force)
     if force or _stale():
         nvcc = os.environ.get("NVCC", "nvcc")
         tmp = LIB + ".tmp.%d" % os.getpid()

@@ -136,3 +136,42 @@ def test_the_struct_is_the_headers():
     assert len(packed) == ctypes.sizeof(Matrix)
     m = Matrix.from_buffer_copy(packed)
     assert (m.data, m.stride, m.scales, m.dtype) == (1 << 40, 7, 9, 3)
+
+
+def outcome(f, *args):
+    try:
+        return f(*args)
+    except (ValueError, AttributeError, TypeError) as e:
+        return type(e), str(e)
+
+
+def test_marshalling_is_the_same_compiled_and_in_python():
+    """On host tensors with their device's number, -1, in place of the current GPU's."""
+    from paper_1806_08054_b200.build import build_marshal
+    if not build_marshal():
+        pytest.skip("no headers of Python or torch")
+    from paper_1806_08054_b200 import _marshal
+    q8 = lambda r, c, stride, kind=torch.float8_e4m3fn: torch.zeros(r, stride, dtype=torch.uint8).view(kind)[:, :c]
+    scales = torch.zeros(512 * 2, dtype=torch.uint8)
+    matrices = [None, torch.zeros(4, 200), torch.zeros(4, 200, dtype=torch.bfloat16), torch.zeros(4, 300, dtype=torch.float16)[:, :200],
+                torch.zeros(4, 201), torch.zeros(5, 200), torch.zeros(200, 4).T, torch.zeros(1, 200).expand(4, 200), torch.zeros(4, 200).double(),
+                (q8(4, 200, 208), scales), [q8(4, 200, 256, torch.float8_e5m2), scales], (q8(4, 200, 208), scales[:511]),
+                (q8(4, 200, 208), scales[::2]), (q8(4, 200, 208), scales.float()), (torch.zeros(4, 200), scales),
+                (torch.zeros(4, 200, dtype=torch.uint8), scales), (q8(4, 201, 208), scales)]
+    for m in matrices:
+        for device in (-1, 0):
+            args = (m, "some", 4, 200, device)
+            assert outcome(_marshal.matrix, *args) == outcome(binding._in_python[0], *args)
+    one = torch.zeros(7, 33)[3:4, :17]
+    assert _marshal.matrix(one, "one", 1, 17, -1) == binding._in_python[0](one, "one", 1, 17, -1)
+    for m in (torch.zeros(4, 200), (q8(4, 200, 208), scales)):
+        assert outcome(_marshal.size, m, "some") == outcome(binding._in_python[1], m, "some")
+    for t, dtype, n in ((None, torch.float32, 5), (torch.zeros(5), torch.float32, 5), (torch.zeros(5), torch.float32, 6),
+                        (torch.zeros(5), torch.int32, 5), (torch.zeros(10)[::2], torch.float32, 5), (torch.zeros(5).half(), torch.float16, 5)):
+        for device in (-1, 0):
+            assert outcome(_marshal.vector, t, dtype, n, "some", device) == outcome(binding._in_python[2], t, dtype, n, "some", device)
+    for f in (_marshal.matrix, _marshal.size, _marshal.vector):
+        with pytest.raises(TypeError):
+            f(1)
+    with pytest.raises(ValueError):
+        _marshal.matrix(7, "some", 4, 200, -1)
