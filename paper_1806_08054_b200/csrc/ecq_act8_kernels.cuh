@@ -267,16 +267,16 @@ __device__ __forceinline__ Act8Place act8_place(const Act8Tiles& P, uint32_t row
     return at;
 }
 
-// A tile a CTA.
+// A tile a CTA; a part of one, of 32 rows, where nothing is written transposed.
 template <int OP, typename S, typename T>
 __global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas) act8_tile_kernel(const __grid_constant__ Act8Tiles P) {
     __shared__ __align__(16) Act8Turn turn;
-    const uint32_t row0 = blockIdx.x / P.tiles_across * 128u, col0 = blockIdx.x % P.tiles_across * 128u;
+    const uint32_t rows = blockDim.x / 4, row0 = blockIdx.x / P.tiles_across * rows, col0 = blockIdx.x % P.tiles_across * 128u;
     const Act8Place at = act8_place(P, row0, col0);
     griddep_launch();
     griddep_wait();
     Act8Read<OP, S, T> in;
-    if (P.wide && row0 + 128 <= P.rows && col0 + 128 <= P.cols) {
+    if (P.wide && row0 + rows <= P.rows && col0 + 128 <= P.cols) {
         act8_read<OP, S, T, true>(P, at, in);
         act8_tile<OP, S, T, true>(P, at, in, turn);
     } else {
