@@ -33,7 +33,7 @@ class Model:
     """Parameters as slices of one flat vector: embedding, two hidden matrices, output matrix."""
 
     shapes = [(VOCAB, WIDTH), (HIDDEN, WIDTH), (WIDTH, HIDDEN), (VOCAB, WIDTH)]
-    hidden, others = (1, 2), (0, 3)
+    hidden, others = (1, 2), {0: 20.0, 3: 20.0}          # stepped by the plan; the others' learning rates
 
     def __init__(self, seed: int):
         self.offsets, at = [], 0
@@ -90,7 +90,7 @@ class GatedModel(Model):
     """The same with a gated hidden layer behind a norm, in 8 bits: y = x + W_down (silu(W_gate n) * (W_up n))."""
 
     shapes = [(VOCAB, WIDTH), (1, WIDTH), (HIDDEN, WIDTH), (HIDDEN, WIDTH), (WIDTH, HIDDEN), (VOCAB, WIDTH)]
-    hidden, others = (2, 3, 4), (0, 1, 5)
+    hidden, others = (2, 3, 4), {0: 20.0, 1: 0.5, 5: 20.0}
 
     def __init__(self, seed: int):
         super().__init__(seed)
@@ -191,8 +191,8 @@ def train(steps: int, workers: int, batch: int = 2048, levels: int = 7, report=N
             ecq.ecq_encode_batch(codec, t, grads, errs, codes, scales)
             ecq.ecq_decode_mean(codec, codes, scales, mean)
             ecq.ecq_muon_step(plan, mean, momentum, model.params, mu=0.9, lr=0.02)
-            for i in model.others:
-                model.views(model.params)[i].sub_(model.views(mean)[i], alpha=20.0)
+            for i, rate in model.others.items():
+                model.views(model.params)[i].sub_(model.views(mean)[i], alpha=rate)
             losses.append(float(total) / workers)
             if report and (t % 10 == 0 or t == steps - 1):
                 report(t, losses[-1])
