@@ -29,19 +29,27 @@ struct Act8Tiles {
     int wide;                            // rows of all plain matrices begin on 16-byte boundaries
 };
 
-// 1 / (1 + exp(-x)); WIDE: the rounding of x log2(e) is added back, which shows in 32 bits alone.
+// 1 / (1 + exp(-x)) of two entries; WIDE: the rounding of x log2(e) is added back, which shows in 32 bits alone.
 template <bool WIDE>
-__device__ __forceinline__ float act8_sigmoid(float x) {
-    const float t = __fmul_rn(x, -1.44269504088896f);
-    float e = ex2(t);
+__device__ __forceinline__ uint64_t act8_sigmoid2(uint64_t x) {
+    const uint64_t by = pack2(-1.44269504088896f, -1.44269504088896f), t = mul2(x, by);
+    float t0, t1;
+    unpack2(t, t0, t1);
+    uint64_t e = pack2(ex2(t0), ex2(t1));
     if (WIDE) {
-        float lo = __fmaf_rn(x, -1.44269504088896f, -t);
-        lo = __fmaf_rn(x, -1.925963033e-8f, lo);               // log2(e) beyond 24 bits
-        e = t > -126.f && t < 126.f ? __fmaf_rn(e, __fmul_rn(lo, 0.693147181f), e) : e;
+        uint64_t lo = fma2(x, by, t ^ 0x8000000080000000ull);
+        lo = fma2(x, pack2(-1.925963033e-8f, -1.925963033e-8f), lo);   // log2(e) beyond 24 bits
+        lo = fma2(e, mul2(lo, pack2(0.693147181f, 0.693147181f)), e);
+        float e0, e1, l0, l1;
+        unpack2(e, e0, e1);
+        unpack2(lo, l0, l1);
+        e = pack2(t0 > -126.f && t0 < 126.f ? l0 : e0, t1 > -126.f && t1 < 126.f ? l1 : e1);
     }
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(__fadd_rn(1.f, e)));
-    return y;
+    float y0, y1;
+    unpack2(add2(e, pack2(1.f, 1.f)), y0, y1);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(y0));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(y1));
+    return pack2(y0, y1);
 }
 
 // A thread's place in a tile of a matrix: four rows, eight columns.
@@ -221,9 +229,9 @@ __device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& a
 #pragma unroll
             for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float g = v[j + h][i];
-                    v[j + h][i] = __fmul_rn(__fmul_rn(g, act8_sigmoid<wide>(g)), x[h][i]);
+                for (int i = 0; i < 8; i += 2) {
+                    const uint64_t g = pack2(v[j + h][i], v[j + h][i + 1]);
+                    unpack2(mul2(mul2(g, act8_sigmoid2<wide>(g)), pack2(x[h][i], x[h][i + 1])), v[j + h][i], v[j + h][i + 1]);
                 }
         }
     }
@@ -235,10 +243,11 @@ __device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& a
             widen8(b[j], P.in[1].dtype, u[j]);
             widen8(d[j], 0, y);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float g = v[j][i], s = act8_sigmoid<wide>(g), ds = __fmul_rn(y[i], s);
-                v[j][i] = __fmul_rn(__fmul_rn(ds, u[j][i]), __fmaf_rn(g, __fsub_rn(1.f, s), 1.f));
-                u[j][i] = __fmul_rn(ds, g);
+            for (int i = 0; i < 8; i += 2) {
+                const uint64_t one = pack2(1.f, 1.f), g = pack2(v[j][i], v[j][i + 1]), s = act8_sigmoid2<wide>(g);
+                const uint64_t ds = mul2(pack2(y[i], y[i + 1]), s), slope = fma2(g, sub2(one, s), one);
+                unpack2(mul2(mul2(ds, pack2(u[j][i], u[j][i + 1])), slope), v[j][i], v[j][i + 1]);
+                unpack2(mul2(ds, g), u[j][i], u[j][i + 1]);
             }
         }
     }
