@@ -85,74 +85,100 @@ __device__ __forceinline__ void act8_get(const Act8Mat& m, const Act8Place& at, 
     for (uint32_t j = 0; j < 4; ++j, p += m.stride, s += 16) get8<FULL>(m, p, s, FULL || j < at.rows ? at.n : 0, r[j]);
 }
 
-// A thread's 4 x 8 results in 8 bits transposed; the whole CTA.  Calls may follow each other: each part of shared
-// memory is written a barrier after its last reader.
-struct Act8Turn {
-    unsigned char turned[128 * 128];
-    uint32_t part[kActThreads / 32][128];
-    float down[128];
+// A thread's 4 x 8 entries of N results in 8 bits transposed, those that are wanted; the whole CTA.  Two together, as
+// each step ends in a barrier that they then share.  Calls may follow each other: each part of shared memory is written a
+// barrier after its last reader.
+template <int N> struct Act8Turn {
+    unsigned char turned[N][128 * 128];
+    uint32_t part[N][kActThreads / 32][128];
+    float down[N][128];
 };
-template <bool FULL>
-__device__ __forceinline__ void act8_put_turned(const Act8Mat& m, const Act8Place& at, uint32_t rows, uint32_t cols,
-                                                const float (&v)[4][8], Act8Turn& t) {
+template <> struct Act8Turn<2> {         // the second lies in the first, for want of room
+    union {
+        unsigned char turned[2][128 * 128];
+        uint32_t part[2][kActThreads / 32][128];
+    };
+    float down[2][128];
+};
+template <bool FULL, int N>
+__device__ __forceinline__ void act8_put_turned(const Act8Mat (&m)[2], const Act8Place& at, uint32_t rows, uint32_t cols,
+                                                const float (&v)[4][8], const float (&u)[4][8], Act8Turn<N>& t) {
     const uint32_t tid = threadIdx.x, cg = tid & 15u, rg = tid >> 4, row0 = at.row - 4 * rg, col0 = at.col - 8 * cg;
+    if (N == 2) __syncthreads();
     // the columns' largest magnitudes: four rows in registers, two groups of rows a warp, 16 warps
-    uint32_t big[8];
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-        const float x = top3(top3(v[0][i], v[1][i], v[2][i]), v[3][i], 0.f);
-        big[i] = __float_as_uint(top3(x, __shfl_xor_sync(~0u, x, 16), 0.f));
-    }
-    if ((tid & 16u) == 0) {
-        uint4* to = reinterpret_cast<uint4*>(&t.part[tid >> 5][8 * cg]);
-        to[0] = make_uint4(big[0], big[1], big[2], big[3]);
-        to[1] = make_uint4(big[4], big[5], big[6], big[7]);
+    for (int n = 0; n < N; ++n) {
+        if (!m[n].data) continue;
+        const float (&x)[4][8] = n ? u : v;
+        uint32_t big[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const float y = top3(top3(x[0][i], x[1][i], x[2][i]), x[3][i], 0.f);
+            big[i] = __float_as_uint(top3(y, __shfl_xor_sync(~0u, y, 16), 0.f));
+        }
+        if ((tid & 16u) == 0) {
+            uint4* to = reinterpret_cast<uint4*>(&t.part[n][tid >> 5][8 * cg]);
+            to[0] = make_uint4(big[0], big[1], big[2], big[3]);
+            to[1] = make_uint4(big[4], big[5], big[6], big[7]);
+        }
     }
     __syncthreads();
-    if (tid < 128) {
-        uint32_t top = 0;
+    if (tid < 128 * N) {
+        const uint32_t n = tid >> 7, c = tid & 127u;
+        const Act8Mat& to = N == 2 && n ? m[1] : m[0];
+        if (to.data) {
+            uint32_t top = 0;
 #pragma unroll
-        for (uint32_t w = 0; w < kActThreads / 32; ++w) top = max(top, t.part[w][tid]);
-        const uint32_t byte = act8_byte(top, m.dtype);
-        t.down[tid] = act8_down(byte);
-        if (FULL || col0 + tid < cols) m.scales[act8_scale_at(col0 + tid, row0 >> 7, m.groups)] = (uint8_t)byte;
+            for (uint32_t w = 0; w < kActThreads / 32; ++w) top = max(top, t.part[n][w][c]);
+            const uint32_t byte = act8_byte(top, to.dtype);
+            t.down[n][c] = act8_down(byte);
+            if (FULL || col0 + c < cols) to.scales[act8_scale_at(col0 + c, row0 >> 7, to.groups)] = (uint8_t)byte;
+        }
     }
     __syncthreads();
     // The tile turned in shared memory: column c has 128 bytes, its four-byte words exchanged by the
     // group of eight columns so that neither a warp's words nor its 16-byte reads meet in a bank.
-    float down[8];
-    Elem<float>::widen(*reinterpret_cast<const uint4*>(t.down + 8 * cg), down);
-    Elem<float>::widen(*reinterpret_cast<const uint4*>(t.down + 8 * cg + 4), down + 4);
-    uint32_t* to = reinterpret_cast<uint32_t*>(t.turned + 8 * cg * 128u + ((rg ^ (2 * cg)) << 2));
-    float y[8][4];
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
+    for (int n = 0; n < N; ++n) {
+        if (!m[n].data) continue;
+        const float (&x)[4][8] = n ? u : v;
+        float down[8];
+        Elem<float>::widen(*reinterpret_cast<const uint4*>(t.down[n] + 8 * cg), down);
+        Elem<float>::widen(*reinterpret_cast<const uint4*>(t.down[n] + 8 * cg + 4), down + 4);
+        uint32_t* to = reinterpret_cast<uint32_t*>(t.turned[n] + 8 * cg * 128u + ((rg ^ (2 * cg)) << 2));
+        float y[8][4];
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) y[i][j] = __fmul_rn(v[j][i], down[i]);   // not in pairs: rows are none
-    }
-    if (m.dtype == 3) {
+        for (uint32_t i = 0; i < 8; ++i)
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) to[32 * i] = act8_e4m3(y[i][0], y[i][1]) | (uint32_t)act8_e4m3(y[i][2], y[i][3]) << 16;
-    } else {
+            for (uint32_t j = 0; j < 4; ++j) y[i][j] = __fmul_rn(x[j][i], down[i]);   // not in pairs: rows are none
+        if (m[n].dtype == 3) {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) to[32 * i] = act8_e5m2(y[i][0], y[i][1]) | (uint32_t)act8_e5m2(y[i][2], y[i][3]) << 16;
+            for (uint32_t i = 0; i < 8; ++i) to[32 * i] = act8_e4m3(y[i][0], y[i][1]) | (uint32_t)act8_e4m3(y[i][2], y[i][3]) << 16;
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) to[32 * i] = act8_e5m2(y[i][0], y[i][1]) | (uint32_t)act8_e5m2(y[i][2], y[i][3]) << 16;
+        }
     }
     __syncthreads();
     const uint32_t piece = tid & 7u, left = FULL ? 128u : row0 + 16 * piece < rows ? rows - (row0 + 16 * piece) : 0;
 #pragma unroll
-    for (uint32_t p = 0; p < 2; ++p) {
-        const uint32_t c = (tid >> 3) + 64 * p, group = c >> 3;
-        if (!FULL && (col0 + c >= cols || !left)) continue;
-        uint4 w = *reinterpret_cast<const uint4*>(t.turned + c * 128u + ((piece ^ (group >> 1)) << 4));
-        if (group & 1u) w = make_uint4(w.z, w.w, w.x, w.y);
-        unsigned char* out = m.data + (uint64_t)(col0 + c) * m.stride + row0 + 16 * piece;
-        if (left >= 16) {
-            *reinterpret_cast<uint4*>(out) = w;
-        } else {
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    for (int n = 0; n < N; ++n) {
+        if (!m[n].data) continue;
 #pragma unroll
-            for (uint32_t i = 0; i < 16; ++i)
-                if (i < left) out[i] = (unsigned char)(u[i >> 2] >> (8 * (i & 3)));
+        for (uint32_t p = 0; p < 2; ++p) {
+            const uint32_t c = (tid >> 3) + 64 * p, group = c >> 3;
+            if (!FULL && (col0 + c >= cols || !left)) continue;
+            uint4 w = *reinterpret_cast<const uint4*>(t.turned[n] + c * 128u + ((piece ^ (group >> 1)) << 4));
+            if (group & 1u) w = make_uint4(w.z, w.w, w.x, w.y);
+            unsigned char* out = m[n].data + (uint64_t)(col0 + c) * m[n].stride + row0 + 16 * piece;
+            if (left >= 16) {
+                *reinterpret_cast<uint4*>(out) = w;
+            } else {
+                const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i)
+                    if (i < left) out[i] = (unsigned char)(q[i >> 2] >> (8 * (i & 3)));
+            }
         }
     }
 }
@@ -179,7 +205,7 @@ struct Act8Ring {
     static constexpr uint32_t kBytes = kIn * (OP == kActCopy ? 1 : 2) + (OP == kActGateGrad ? 128 * 128 * sizeof(T) : 0);
     // an SM; 64 registers a thread are too few for a gradient, and for two inputs in 32 bits
     static constexpr uint32_t kCtas = OP == kActGateGrad || (OP == kActGate && sizeof(S) == 4) ? 1 : 2;
-    static constexpr uint32_t kRoom = 226u * 1024u / kCtas - 27u * 1024u;
+    static constexpr uint32_t kRoom = 226u * 1024u / kCtas - (OP == kActGateGrad ? 35u : 27u) * 1024u;
     static constexpr uint32_t kStages = kRoom / kBytes < 4 ? kRoom / kBytes : 4;
     static constexpr uint32_t kSmem = kStages * kBytes + 128;
 };
@@ -205,7 +231,8 @@ __device__ __forceinline__ void act8_take<uint8_t>(uint32_t from, uint32_t block
 }
 
 template <int OP, typename S, typename T, bool FULL>
-__device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& at, const Act8Read<OP, S, T>& in, Act8Turn& turn) {
+__device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& at, const Act8Read<OP, S, T>& in,
+                                          Act8Turn<OP == kActGateGrad ? 2 : 1>& turn) {
     constexpr bool wide = sizeof(T) == 4;
     const auto& a = in.a;
     const auto& b = in.b;
@@ -256,14 +283,15 @@ __device__ __forceinline__ void act8_tile(const Act8Tiles& P, const Act8Place& a
         act8_put_coded<FULL>(P.q[0], at, 0, v[0], v[1]);
         act8_put_coded<FULL>(P.q[0], at, 2, v[2], v[3]);
     }
-    if (P.qt[0].data) act8_put_turned<FULL>(P.qt[0], at, P.rows, P.cols, v, turn);
     if constexpr (OP == kActGateGrad) {
         if (P.plain[1].data) act8_put_plain<FULL, T>(P.plain[1], at, u);
         if (P.q[1].data) {
-        act8_put_coded<FULL>(P.q[1], at, 0, u[0], u[1]);
-        act8_put_coded<FULL>(P.q[1], at, 2, u[2], u[3]);
-    }
-        if (P.qt[1].data) act8_put_turned<FULL>(P.qt[1], at, P.rows, P.cols, u, turn);
+            act8_put_coded<FULL>(P.q[1], at, 0, u[0], u[1]);
+            act8_put_coded<FULL>(P.q[1], at, 2, u[2], u[3]);
+        }
+        if (P.qt[0].data || P.qt[1].data) act8_put_turned<FULL, 2>(P.qt, at, P.rows, P.cols, v, u, turn);
+    } else {
+        if (P.qt[0].data) act8_put_turned<FULL, 1>(P.qt, at, P.rows, P.cols, v, v, turn);
     }
 }
 
@@ -279,7 +307,7 @@ __device__ __forceinline__ Act8Place act8_place(const Act8Tiles& P, uint32_t row
 // A tile a CTA; a part of one, of 32 rows, where nothing is written transposed.
 template <int OP, typename S, typename T>
 __global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas) act8_tile_kernel(const __grid_constant__ Act8Tiles P) {
-    __shared__ __align__(16) Act8Turn turn;
+    __shared__ __align__(16) Act8Turn<OP == kActGateGrad ? 2 : 1> turn;
     const uint32_t rows = blockDim.x / 4, row0 = blockIdx.x / P.tiles_across * rows, col0 = blockIdx.x % P.tiles_across * 128u;
     const Act8Place at = act8_place(P, row0, col0);
     griddep_launch();
@@ -305,7 +333,7 @@ __global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas)
     using R = Act8Ring<OP, S, T>;
     constexpr uint32_t kStages = R::kStages;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(16) Act8Turn turn;
+    __shared__ __align__(16) Act8Turn<OP == kActGateGrad ? 2 : 1> turn;
     __shared__ __align__(8) uint64_t bars[kStages];
     const uint32_t ring = (smem_u32(raw) + 127u) & ~127u, full = smem_u32(bars), tid = threadIdx.x;
     auto whole = [&](uint32_t tile) {
