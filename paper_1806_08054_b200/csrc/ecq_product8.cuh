@@ -806,30 +806,31 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
                 continue;
             }
             if (P.out.wide && (!P.add || P.in_place)) {
-                if (P.out.dtype == 0) {
+                // 64 columns to registers, and their place in tensor memory is free for the next tile
 #pragma unroll 1
-                    for (uint32_t at = 0; at < 128; at += 16) {
-                        const uint32_t c = (at + start) & 127u;
-                        float y[16];
-                        fetch16(c, y);
-                        sent();
+                for (uint32_t at = 0; at < 128; at += 64) {
+                    const uint32_t c = (at + start) & 127u;
+                    float y[64];
+                    fetch32(c, y);
+                    fetch32(c + 32, y + 32);
+                    if (at == 0 && shares) release();
+                    if (P.out.dtype == 0) {
 #pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 4 * i));
-                        if (at == 48 && shares) release();
-                        send(row0, col0 + c);
-                    }
-                } else {
-#pragma unroll 1
-                    for (uint32_t at = 0; at < 128; at += 32) {
-                        const uint32_t c = (at + start) & 127u;
-                        float y[32];
-                        fetch32(c, y);
-                        sent();
+                        for (uint32_t u = 0; u < 4; ++u) {
+                            sent();
 #pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i)
-                            sts16(place(lane, i), P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y + 8 * i) : Elem<__half>::narrow(y + 8 * i));
-                        if (at == 32 && shares) release();
-                        send(row0, col0 + c);
+                            for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 16 * u + 4 * i));
+                            send(row0, col0 + c + 16 * u);
+                        }
+                    } else {
+#pragma unroll
+                        for (uint32_t u = 0; u < 2; ++u) {
+                            sent();
+#pragma unroll
+                            for (uint32_t i = 0; i < 4; ++i)
+                                sts16(place(lane, i), P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y + 32 * u + 8 * i) : Elem<__half>::narrow(y + 32 * u + 8 * i));
+                            send(row0, col0 + c + 32 * u);
+                        }
                     }
                 }
                 continue;
