@@ -605,6 +605,46 @@ struct ProdPair {
     static constexpr uint32_t kTmem = 512;
 };
 
+// 16-byte piece c of row r in a warp's 2 KB of results, 32 rows of 64 bytes: where the 64-byte swizzle has it, and neither
+// eight lanes with a row each nor eight with two whole rows meet in a bank.
+__device__ __forceinline__ uint32_t prod_place(uint32_t own, uint32_t r, uint32_t c) { return own + r * 64u + ((c ^ ((r >> 1) & 3u)) << 4); }
+
+// These at the last columns of rows that do not end on a 16-byte boundary, a lane a row.  (Not inline: it would be at every
+// store, and cost 2 us in a product of 4096 x 4096 x 128.)
+__device__ __noinline__ void prod_edge(const Product8& P, uint32_t own, uint32_t row, uint32_t col, uint32_t es) {
+    const uint32_t lane = threadIdx.x & 31u;
+    __syncwarp();
+    if (row + lane < P.rows && col < P.cols) {
+        unsigned char* to = P.out.data + (row + lane) * P.out.stride + (uint64_t)col * es;
+        const uint32_t left = min(64u, (P.cols - col) * es);           // bytes
+        if (P.in_place) {
+            for (uint32_t i = 0; i < left; i += 4) {
+                float* f = reinterpret_cast<float*>(to + i);
+                *f = __fadd_rn(*f, lds1(prod_place(own, lane, i >> 4) + (i & 15u)));
+            }
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 64; i += 16) {
+                const uint4 w = lds16(prod_place(own, lane, i >> 4));
+                if (i + 16 <= left) {
+                    *reinterpret_cast<uint4*>(to + i) = w;
+                    continue;
+                }
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (uint32_t j = 0; j < 16; ++j) {
+                    if (i + j >= left || j % es) continue;
+                    const uint32_t v = u[j >> 2] >> (8 * (j & 3));
+                    if (es == 4) *reinterpret_cast<uint32_t*>(to + i + j) = v;
+                    else if (es == 2) *reinterpret_cast<uint16_t*>(to + i + j) = (uint16_t)v;
+                    else to[i + j] = (unsigned char)v;
+                }
+            }
+        }
+    }
+    __syncwarp();
+}
+
 __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kernel(const __grid_constant__ Product8 P) {
     using S = ProdPair;
     extern __shared__ unsigned char raw[];
@@ -706,13 +746,17 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
     } else if (warp < S::kEpiWarps) {
         // ---- results: a warp has 32 rows and half of the columns
         const uint32_t quad = warp & 3, half = warp >> 2, own = epi + warp * S::kEpi;
-        // Results go out through the warp's 2 KB of shared memory, 32 rows of 64 bytes: 16-byte piece c of row r
-        // at c ^ (r / 2 % 4), where the 64-byte swizzle has it and neither eight lanes with a row each nor
-        // eight with two whole rows meet in a bank.
-        auto place = [&](uint32_t r, uint32_t c) { return own + r * 64u + ((c ^ ((r >> 1) & 3u)) << 4); };
-        // To the result (or added to it), which clips them; and, before they are written again, whether they
-        // have been read.
+        // results go out through the warp's 2 KB of shared memory
+        auto place = [&](uint32_t r, uint32_t c) { return prod_place(own, r, c); };
+        // To the result (or added to it), which clips them, to 16 bytes: where its rows end between two such pieces, those that
+        // end go out one by one.  And, before they are written again, whether they have been read.
+        const uint32_t es = P.out.dtype == 0 ? 4 : P.out.dtype < 3 ? 2 : 1;
+        const bool ragged = P.cols * es % 16 != 0;
         auto send = [&](uint32_t row, uint32_t col) {
+            if (ragged && col + 64 / es > P.cols) {
+                prod_edge(P, own, row, col, es);
+                return;
+            }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
@@ -741,13 +785,61 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
                 for (uint32_t at = 0; at < min(128u, P.cols - col0) * es; at += 128)
                     asm volatile("prefetch.global.L2 [%0];" ::"l"(P.add + (row0 + lane) * P.add_stride + (uint64_t)col0 * es + at));
             }
-            const bool good = __all_sync(~0u, wait_or_stop(acc_full + 8 * (n & 1), (n >> 1) & 1, limit, &stop));
-            tcgen05_after_sync();
-            const uint32_t from = tmem + ((quad * 32u) << 16) + (n & 1) * S::kSecond + half * 128u;
             // Columns 192 .. 255 of tensor memory are the next tile's too: the second half's upper 64 in
             // even tiles, the first half's lower 64 in odd ones.  Columns are taken from there on.
             const bool shares = half != (n & 1);
             const uint32_t start = shares && half == 1 ? 64 : 0;
+            // where all rows begin on 16-byte boundaries a lane reads what is added to its row, 32 columns ahead
+            uint4 more[8];
+            auto ask = [&](uint32_t c) {
+                const uint32_t col = col0 + c, left = row0 + lane < P.rows && col < P.cols ? min(32u, P.cols - col) : 0;
+                const unsigned char* p = P.add + (row0 + lane) * P.add_stride;
+                if (left == 32) {
+                    const uint4* v = reinterpret_cast<const uint4*>(p + (uint64_t)col * (P.add_dtype ? 2 : 4));
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) more[i] = v[i];
+                    if (P.add_dtype == 0)
+#pragma unroll
+                        for (uint32_t i = 4; i < 8; ++i) more[i] = v[i];
+                    return;
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) {                    // the last columns of a row
+                    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) {
+                        if (P.add_dtype == 0 && j < 4 && 4 * i + j < left) w[j] = reinterpret_cast<const uint32_t*>(p)[col + 4 * i + j];
+                        if (P.add_dtype != 0 && i < 4 && 8 * i + j < left)
+                            w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[col + 8 * i + j] << (16 * (j & 1));
+                    }
+                    more[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            };
+            auto added = [&](float* y) {
+                if (P.add_dtype == 0) {
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) {
+                        float x[4];
+                        Elem<float>::widen(more[i], x);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) y[4 * i + j] = __fadd_rn(y[4 * i + j], x[j]);
+                    }
+                    return;
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    float x[8];
+                    if (P.add_dtype == 1) Elem<__nv_bfloat16>::widen(more[i], x);
+                    else Elem<__half>::widen(more[i], x);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[8 * i + j] = __fadd_rn(y[8 * i + j], x[j]);
+                }
+            };
+            const bool reads = P.add && !P.in_place && P.add_wide && P.out.wide && out;
+            if (reads) ask(start);
+            const bool good = __all_sync(~0u, wait_or_stop(acc_full + 8 * (n & 1), (n >> 1) & 1, limit, &stop));
+            tcgen05_after_sync();
+            const uint32_t from = tmem + ((quad * 32u) << 16) + (n & 1) * S::kSecond + half * 128u;
             auto release = [&] {
                 tcgen05_before_sync();
                 __syncwarp();
@@ -805,7 +897,7 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
                 if (row < P.rows) P.out.scales[act8_scale_at(row, col0 >> 7, P.out.groups)] = (uint8_t)byte;
                 continue;
             }
-            if (P.out.wide && (!P.add || P.in_place)) {
+            if (P.out.wide && (!P.add || P.in_place || reads)) {
                 // 64 columns to registers, and their place in tensor memory is free for the next tile
 #pragma unroll 1
                 for (uint32_t at = 0; at < 128; at += 64) {
@@ -814,22 +906,27 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
                     fetch32(c, y);
                     fetch32(c + 32, y + 32);
                     if (at == 0 && shares) release();
-                    if (P.out.dtype == 0) {
 #pragma unroll
-                        for (uint32_t u = 0; u < 4; ++u) {
-                            sent();
-#pragma unroll
-                            for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 16 * u + 4 * i));
-                            send(row0, col0 + c + 16 * u);
+                    for (uint32_t h = 0; h < 2; ++h) {
+                        if (reads) {
+                            added(y + 32 * h);
+                            if (h == 0) ask(c + 32);
+                            else if (at == 0) ask((c + 64) & 127u);
                         }
-                    } else {
+                        if (P.out.dtype == 0) {
 #pragma unroll
-                        for (uint32_t u = 0; u < 2; ++u) {
+                            for (uint32_t u = 0; u < 2; ++u) {
+                                sent();
+#pragma unroll
+                                for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 32 * h + 16 * u + 4 * i));
+                                send(row0, col0 + c + 32 * h + 16 * u);
+                            }
+                        } else {
                             sent();
 #pragma unroll
                             for (uint32_t i = 0; i < 4; ++i)
-                                sts16(place(lane, i), P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y + 32 * u + 8 * i) : Elem<__half>::narrow(y + 32 * u + 8 * i));
-                            send(row0, col0 + c + 32 * u);
+                                sts16(place(lane, i), P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y + 32 * h + 8 * i) : Elem<__half>::narrow(y + 32 * h + 8 * i));
+                            send(row0, col0 + c + 32 * h);
                         }
                     }
                 }

@@ -69,6 +69,50 @@ def test_random(m, n, k, out):
             check_plain(d, want, err)
 
 
+@pytest.mark.parametrize("m,n,k", [(5, 300, 400), (200, 300, 1300), (1000, 1500, 2000), (2300, 2100, 300), (2304, 2048, 700), (2500, 2333, 90)])
+@pytest.mark.parametrize("c_type,d_type", [(F32, F32), (BF16, BF16), (F16, F16), (F32, BF16), (BF16, F32), (F16, BF16)])
+def test_additions_of_aligned_rows(m, n, k, c_type, d_type):
+    """Rows on 16-byte boundaries, with columns that end anywhere; what lies behind them is left."""
+    a, b = stored(random(m, k, 3)), stored(random(n, k, 4, 1 / math.sqrt(k) / 8))
+    stride = -(-n // 16) * 16 + 16
+    want, err = values(a) @ values(b).T, bound(a, b, k)
+    c = strided(m, n, c_type, stride).copy_(random(m, n, 5))
+    d = strided(m, n, d_type, stride, fill=7.0)
+    total = want + c.double()
+    ecq.ecq_act8_product(a, b, d, add=c)
+    check_plain(d, total, err + total.abs() * 2.0 ** -24)
+    assert bool((torch.as_strided(d, (m, stride), (stride, 1))[:, n:] == 7.0).all())
+    if c_type == d_type:
+        ecq.ecq_act8_product(a, b, c, add=c)
+        assert torch.equal(c, d)
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 301, 400), (200, 333, 300), (2500, 2333, 90), (2304, 2056, 130)])
+@pytest.mark.parametrize("d_type", [F32, BF16, E4M3, E5M2])
+def test_what_lies_behind_the_last_column_is_left(m, n, k, d_type):
+    a, b = stored(random(m, k, 3)), stored(random(n, k, 4))
+    if d_type in (E4M3, E5M2):
+        d = pair(m, n, d_type, extra=1)
+        ecq.ecq_act8_product(a, b, d)
+        whole = torch.as_strided(d[0].view(torch.uint8), (m, d[0].stride(0)), (d[0].stride(0), 1))
+        assert bool((whole[:, n:] == 0xA5).all())
+        rest = torch.ones_like(d[1], dtype=torch.bool)
+        rest[scale_places(m, n)] = False
+        assert bool((d[1][rest] == 0xA5).all())
+    else:
+        stride = -(-n // 16) * 16 + 16
+        d = strided(m, n, d_type, stride, fill=7.0)
+        ecq.ecq_act8_product(a, b, d)
+        whole = torch.as_strided(d, (m, stride), (stride, 1))
+        assert bool((whole[:, n:] == 7.0).all())
+        check_plain(d, values(a) @ values(b).T, bound(a, b, k))
+        once = d.clone()
+        ecq.ecq_act8_product(a, b, d, add=d)
+        total = values(a) @ values(b).T + once.double()
+        check_plain(d, total, bound(a, b, k) + total.abs() * 2.0 ** -24)
+        assert bool((whole[:, n:] == 7.0).all())
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 300, 400), (200, 300, 1300), (2300, 2100, 300)])
 def test_in_place_addition(m, n, k):
     a, b = whole_numbers(m, k, 1, E4M3), whole_numbers(n, k, 2, E4M3)
