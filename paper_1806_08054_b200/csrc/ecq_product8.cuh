@@ -95,6 +95,12 @@ __device__ __forceinline__ void send16(uint32_t to, const float* v, uint32_t bar
                  : "memory");
 }
 
+// Arrive on the first CTA's barrier where no memory is handed over (tensor memory that has been read): a release at cluster
+// scope takes 1400 clocks (8192 x 4096 x 1024: 35.7 us against 30.2).
+__device__ __forceinline__ void leader_arrive_relaxed(uint32_t leader_bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
+}
+
 // Arrive on a barrier of each of `ctas` when every product issued so far has completed.
 __device__ __forceinline__ void umma_commit_to(uint32_t bar, uint16_t ctas) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(ctas)
@@ -645,6 +651,325 @@ __device__ __noinline__ void prod_edge(const Product8& P, uint32_t own, uint32_t
     __syncwarp();
 }
 
+// Results of tiles `begin`, `begin` + `step`, ..., by eight warps: each has 32 rows of its CTA's 128 and half of the columns.
+__device__ __forceinline__ void prod_pair_results(const Product8& P, uint32_t tmem, uint32_t own, uint32_t acc_full, uint32_t shared_free,
+                                                  uint32_t rank, uint32_t begin, uint32_t end, uint32_t step, volatile uint32_t* stop) {
+    using S = ProdPair;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = warp & 3, half = warp >> 2, limit = P.wait_limit;
+    // results go out through the warp's 2 KB of shared memory
+    auto place = [&](uint32_t r, uint32_t c) { return prod_place(own, r, c); };
+    // To the result (or added to it), which clips them, to 16 bytes: where its rows end between two such pieces, those that
+    // end go out one by one.  And, before they are written again, whether they have been read.
+    const uint32_t es = P.out.dtype == 0 ? 4 : P.out.dtype < 3 ? 2 : 1;
+    const bool ragged = P.cols * es % 16 != 0;
+    auto send = [&](uint32_t row, uint32_t col) {
+        if (ragged && col + 64 / es > P.cols) {
+            prod_edge(P, own, row, col, es);
+            return;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            if (P.in_place) tma_add_2d(&P.result, (int)col, (int)row, own);
+            else tma_store_2d(&P.result, (int)col, (int)row, own);
+            bulk_commit();
+        }
+    };
+    auto sent = [&] {
+        if (lane == 0) bulk_wait_read0();
+        __syncwarp();
+    };
+    // what is added to 16 columns of a tile: four of four rows a lane
+    const uint32_t piece = lane & 3u;
+    auto ahead = [&](uint32_t row0, uint32_t col, uint4 (&to)[4]) {
+        const uint32_t m = inside4(col + 4 * piece, P.cols), row = row0 + (lane >> 2);
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) to[i] = prod_fetch4(P, row + 8 * i, col + 4 * piece, row + 8 * i < P.rows ? m : 0);
+    };
+    uint32_t n = 0;
+    for (uint32_t tile = begin; tile < end; tile += step, ++n) {
+        const uint32_t row0 = tile / P.across * 256u + rank * 128u + quad * 32u, col0 = tile % P.across * 256u + half * 128u;
+        const bool out = row0 < P.rows && col0 < P.cols;
+        if (P.add && !P.in_place && out && row0 + lane < P.rows) {   // C's lines of this warp, while the products run
+            const uint32_t es = P.add_dtype ? 2 : 4;
+            for (uint32_t at = 0; at < min(128u, P.cols - col0) * es; at += 128)
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(P.add + (row0 + lane) * P.add_stride + (uint64_t)col0 * es + at));
+        }
+        // Columns 192 .. 255 of tensor memory are the next tile's too: the second half's upper 64 in
+        // even tiles, the first half's lower 64 in odd ones.  Columns are taken from there on.
+        const bool shares = half != (n & 1);
+        const uint32_t start = shares && half == 1 ? 64 : 0;
+        // where all rows begin on 16-byte boundaries a lane reads what is added to its row, 32 columns ahead
+        uint4 more[8];
+        auto ask = [&](uint32_t c) {
+            const uint32_t col = col0 + c, left = row0 + lane < P.rows && col < P.cols ? min(32u, P.cols - col) : 0;
+            const unsigned char* p = P.add + (row0 + lane) * P.add_stride;
+            if (left == 32) {
+                const uint4* v = reinterpret_cast<const uint4*>(p + (uint64_t)col * (P.add_dtype ? 2 : 4));
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) more[i] = v[i];
+                if (P.add_dtype == 0)
+#pragma unroll
+                    for (uint32_t i = 4; i < 8; ++i) more[i] = v[i];
+                return;
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {                    // the last columns of a row
+                uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) {
+                    if (P.add_dtype == 0 && j < 4 && 4 * i + j < left) w[j] = reinterpret_cast<const uint32_t*>(p)[col + 4 * i + j];
+                    if (P.add_dtype != 0 && i < 4 && 8 * i + j < left)
+                        w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[col + 8 * i + j] << (16 * (j & 1));
+                }
+                more[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        };
+        auto added = [&](float* y) {
+            if (P.add_dtype == 0) {
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) {
+                    float x[4];
+                    Elem<float>::widen(more[i], x);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) y[4 * i + j] = __fadd_rn(y[4 * i + j], x[j]);
+                }
+                return;
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                float x[8];
+                if (P.add_dtype == 1) Elem<__nv_bfloat16>::widen(more[i], x);
+                else Elem<__half>::widen(more[i], x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[8 * i + j] = __fadd_rn(y[8 * i + j], x[j]);
+            }
+        };
+        const bool reads = P.add && !P.in_place && P.add_wide && P.out.wide && out;
+        if (reads) ask(start);
+        const bool good = __all_sync(~0u, wait_or_stop(acc_full + 8 * (n & 1), (n >> 1) & 1, limit, stop));
+        tcgen05_after_sync();
+        const uint32_t from = tmem + ((quad * 32u) << 16) + (n & 1) * S::kSecond + half * 128u;
+        auto release = [&] {
+            tcgen05_before_sync();
+            __syncwarp();
+            if (lane == 0) leader_arrive_relaxed(leader_addr(shared_free));
+        };
+        if (!shares) release();
+        if (!out) {
+            if (shares) release();
+            continue;
+        }
+        auto fetch32 = [&](uint32_t c, float* y) {
+            tmem_load32(from + c, y);
+            if (!good)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(0x7FC00000u);
+        };
+        auto fetch16 = [&](uint32_t c, float* y) {
+            tmem_load16(from + c, y);
+            if (!good)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(0x7FC00000u);
+        };
+        if (P.out.dtype >= 3) {
+            // the largest magnitude of this lane's 128 columns first, then the entries
+            const uint32_t row = row0 + lane, dtype = P.out.dtype, nc = min(128u, P.cols - col0);
+            uint32_t top = 0;
+#pragma unroll 1
+            for (uint32_t c = 0; c < 128; c += 32) {
+                float y[32];
+                fetch32(c, y);
+#pragma unroll
+                for (uint32_t i = 0; i < 32; ++i)
+                    if (c + i < nc) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+            }
+            const uint32_t byte = act8_byte(top, dtype);
+            const float by = act8_down(byte);
+#pragma unroll 1
+            for (uint32_t at = 0; at < 128; at += 64) {
+                const uint32_t u = (at + start) & 127u;
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h) {
+                    float y[32];
+                    fetch32(u + 32 * h, y);
+                    if (h == 0) sent();
+#pragma unroll
+                    for (uint32_t c = 0; c < 2; ++c) {
+                        uint32_t w[4];
+                        act8_code<16>(y + 16 * c, by, dtype, w);
+                        sts16(place(lane, 2 * h + c), make_uint4(w[0], w[1], w[2], w[3]));
+                    }
+                }
+                if (at == 0 && shares) release();
+                send(row0, col0 + u);
+            }
+            if (row < P.rows) P.out.scales[act8_scale_at(row, col0 >> 7, P.out.groups)] = (uint8_t)byte;
+            continue;
+        }
+        if (P.out.wide && (!P.add || P.in_place || reads)) {
+            // 64 columns to registers, and their place in tensor memory is free for the next tile
+#pragma unroll 1
+            for (uint32_t at = 0; at < 128; at += 64) {
+                const uint32_t c = (at + start) & 127u;
+                float y[64];
+                fetch32(c, y);
+                fetch32(c + 32, y + 32);
+                if (at == 0 && shares) release();
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h) {
+                    if (reads) {
+                        added(y + 32 * h);
+                        if (h == 0) ask(c + 32);
+                        else if (at == 0) ask((c + 64) & 127u);
+                    }
+                    if (P.out.dtype == 0) {
+#pragma unroll
+                        for (uint32_t u = 0; u < 2; ++u) {
+                            sent();
+#pragma unroll
+                            for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 32 * h + 16 * u + 4 * i));
+                            send(row0, col0 + c + 32 * h + 16 * u);
+                        }
+                    } else {
+                        sent();
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i)
+                            sts16(place(lane, i), P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y + 32 * h + 8 * i) : Elem<__half>::narrow(y + 32 * h + 8 * i));
+                        send(row0, col0 + c + 32 * h);
+                    }
+                }
+            }
+            continue;
+        }
+        sent();
+        if (!P.out_quad && !P.add) {
+            // Rows that begin anywhere, in words of four bytes, 16 to a row and two rows at a time; a row of 16-bit
+            // entries that begins between two words takes its words from both halves' neighbours, and its
+            // first and last entry go out alone.  Word i of row r lies at i ^ (r / 2), so that neither 32
+            // rows' same words nor two whole rows meet in a bank.
+            const bool four = P.out.dtype == 0;
+            const uint32_t rows = min(32u, P.rows - row0), x = lane & 15u, second = lane >> 4;
+            const uint32_t step = four ? 16 : 32;                 // columns
+#pragma unroll 1
+            for (uint32_t at = 0; at < 128; at += step) {
+                const uint32_t c = (at + start) & 127u, left = col0 + c < P.cols ? min(step, P.cols - col0 - c) : 0;
+                unsigned char* first = P.out.data + row0 * P.out.stride + (uint64_t)(col0 + c) * (four ? 4 : 2);
+                uint32_t w[16];
+                if (four) {
+                    fetch16(c, reinterpret_cast<float*>(w));
+                } else {
+                    float y[32];
+                    fetch32(c, y);
+#pragma unroll
+                    for (uint32_t i = 0; i < 16; ++i)
+                        w[i] = P.out.dtype == 1 ? Elem<__nv_bfloat16>::pair(y[2 * i], y[2 * i + 1]) : Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
+                }
+                if (at + step == 64 && shares) release();
+                __syncwarp();                                     // what was here has been read
+                if (!left) continue;
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i)
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(own + lane * 64u + ((i ^ (lane >> 1)) << 2)), "r"(w[i]) : "memory");
+                if (!four) {
+                    uint16_t* mine = reinterpret_cast<uint16_t*>(first + lane * P.out.stride);
+                    if (lane < rows && (reinterpret_cast<uintptr_t>(mine) & 2u)) {
+                        mine[0] = (uint16_t)w[0];
+                        if (left == 32) mine[31] = (uint16_t)(w[15] >> 16);
+                    }
+                }
+                __syncwarp();
+                // this lane's word of rows `second`, `second` + 2, ...; rows alike in parity by the stride's
+                unsigned char* to = first + second * P.out.stride + 4 * x;
+#pragma unroll
+                for (uint32_t k = 0; k < 16; ++k, to += 2 * P.out.stride) {
+                    const uint32_t line = own + k * 128u + second * 64u;
+                    uint32_t v, next = 0;
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(line + ((x ^ k) << 2)));
+                    if (four) {
+                        if (2 * k + second < rows && x < left) *reinterpret_cast<uint32_t*>(to) = v;
+                        continue;
+                    }
+                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(next) : "r"(line + (((x + 1) & 15u) ^ k) * 4u));
+                    const uint32_t odd = (uint32_t)(reinterpret_cast<uintptr_t>(to) >> 1) & 1u, e = 2 * x + odd;   // first entry
+                    v = __funnelshift_r(v, next, 16 * odd);
+                    if (2 * k + second >= rows) continue;
+                    if (e + 1 < left) *reinterpret_cast<uint32_t*>(to + 2 * odd) = v;
+                    else if (e < left && !(odd && left == 32)) *reinterpret_cast<uint16_t*>(to + 2 * odd) = (uint16_t)v;
+                }
+            }
+            continue;
+        }
+        if (!P.out_quad || (P.add && !P.add_quad)) {
+            // rows that begin anywhere: a lane a column, two rows at a time
+            const uint32_t rows = min(32u, P.rows - row0), x = lane & 15u;
+            const bool four = P.out.dtype == 0, bf16 = P.out.dtype == 1;
+#pragma unroll 1
+            for (uint32_t at = 0; at < 128; at += 16) {
+                const uint32_t c = (at + start) & 127u, col = col0 + c + x;
+                float y[16];
+                fetch16(c, y);
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 4 * i));
+                if (at == 48 && shares) release();
+                __syncwarp();
+                unsigned char* to = P.out.data + (row0 + (lane >> 4)) * P.out.stride + (uint64_t)col * (four ? 4 : 2);
+                if (col < P.cols)
+#pragma unroll 1
+                    for (uint32_t r0 = lane >> 4; r0 < rows; r0 += 16) {
+                        float add[8];                            // all before the first is written: D may be C
+                        if (P.add)
+#pragma unroll
+                            for (uint32_t i = 0; i < 8; ++i) add[i] = r0 + 2 * i < rows ? prod_get1(P, row0 + r0 + 2 * i, col) : 0.f;
+#pragma unroll
+                        for (uint32_t i = 0; i < 8; ++i, to += 2 * P.out.stride) {
+                            const uint32_t r = r0 + 2 * i;
+                            float v = lds1(place(r, x >> 2) + 4 * (x & 3u));
+                            if (P.add) v = __fadd_rn(v, add[i]);
+                            if (r >= rows) continue;
+                            if (four) *reinterpret_cast<float*>(to) = v;
+                            else *reinterpret_cast<uint16_t*>(to) = bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
+                        }
+                    }
+                __syncwarp();
+            }
+            continue;
+        }
+        // what is added is asked for 16 columns ahead
+        uint4 next[4];
+        if (P.add) ahead(row0, col0 + start, next);
+#pragma unroll 1
+        for (uint32_t at = 0; at < 128; at += 16) {
+            const uint32_t c = (at + start) & 127u, col = col0 + c + 4 * piece, m = inside4(col, P.cols);
+            float y[16];
+            fetch16(c, y);
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 4 * i));
+            if (at == 48 && shares) release();
+            __syncwarp();
+            uint4 now[4];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) now[i] = next[i];
+            if (P.add && at < 112) ahead(row0, col0 + ((c + 16) & 127u), next);
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint32_t r = 8 * i + (lane >> 2);
+                float x[4], add[4];
+                Elem<float>::widen(lds16(place(r, piece)), x);
+                if (row0 + r >= P.rows || !m) continue;
+                if (P.add) {
+                    prod_widen4(P.add_dtype, now[i], add);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = __fadd_rn(x[j], add[j]);
+                }
+                prod_put4(P, row0 + r, col, m, x);
+            }
+            __syncwarp();
+        }
+    }
+    if (lane == 0) bulk_wait_all();
+}
+
 __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kernel(const __grid_constant__ Product8 P) {
     using S = ProdPair;
     extern __shared__ unsigned char raw[];
@@ -728,7 +1053,8 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
                     if (!wait_or_stop(full + 8 * s, (it / S::kStages) & 1, limit, &stop)) { ok = false; break; }
                     tcgen05_after_sync();
                     if ((k & 3) == 0) {
-                        // five places in turn: their last use is five steps behind, and over
+                        // places in turn, whose last use is over: in a tile 16 steps are between, and a tile begins when the
+                        // one before it is over
                         sc = tmem + S::kScaleCols + group * S::kSlotCols;
                         group = group + 1 == S::kSlots ? 0 : group + 1;
                         umma_scales<2>(sc, scales + s * S::kScales);
@@ -744,320 +1070,7 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
             }
         }
     } else if (warp < S::kEpiWarps) {
-        // ---- results: a warp has 32 rows and half of the columns
-        const uint32_t quad = warp & 3, half = warp >> 2, own = epi + warp * S::kEpi;
-        // results go out through the warp's 2 KB of shared memory
-        auto place = [&](uint32_t r, uint32_t c) { return prod_place(own, r, c); };
-        // To the result (or added to it), which clips them, to 16 bytes: where its rows end between two such pieces, those that
-        // end go out one by one.  And, before they are written again, whether they have been read.
-        const uint32_t es = P.out.dtype == 0 ? 4 : P.out.dtype < 3 ? 2 : 1;
-        const bool ragged = P.cols * es % 16 != 0;
-        auto send = [&](uint32_t row, uint32_t col) {
-            if (ragged && col + 64 / es > P.cols) {
-                prod_edge(P, own, row, col, es);
-                return;
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                if (P.in_place) tma_add_2d(&P.result, (int)col, (int)row, own);
-                else tma_store_2d(&P.result, (int)col, (int)row, own);
-                bulk_commit();
-            }
-        };
-        auto sent = [&] {
-            if (lane == 0) bulk_wait_read0();
-            __syncwarp();
-        };
-        // what is added to 16 columns of a tile: four of four rows a lane
-        const uint32_t piece = lane & 3u;
-        auto ahead = [&](uint32_t row0, uint32_t col, uint4 (&to)[4]) {
-            const uint32_t m = inside4(col + 4 * piece, P.cols), row = row0 + (lane >> 2);
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) to[i] = prod_fetch4(P, row + 8 * i, col + 4 * piece, row + 8 * i < P.rows ? m : 0);
-        };
-        uint32_t n = 0;
-        for (uint32_t tile = pair; tile < P.tiles; tile += pairs, ++n) {
-            const uint32_t row0 = tile / P.across * 256u + rank * 128u + quad * 32u, col0 = tile % P.across * 256u + half * 128u;
-            const bool out = row0 < P.rows && col0 < P.cols;
-            if (P.add && !P.in_place && out && row0 + lane < P.rows) {   // C's lines of this warp, while the products run
-                const uint32_t es = P.add_dtype ? 2 : 4;
-                for (uint32_t at = 0; at < min(128u, P.cols - col0) * es; at += 128)
-                    asm volatile("prefetch.global.L2 [%0];" ::"l"(P.add + (row0 + lane) * P.add_stride + (uint64_t)col0 * es + at));
-            }
-            // Columns 192 .. 255 of tensor memory are the next tile's too: the second half's upper 64 in
-            // even tiles, the first half's lower 64 in odd ones.  Columns are taken from there on.
-            const bool shares = half != (n & 1);
-            const uint32_t start = shares && half == 1 ? 64 : 0;
-            // where all rows begin on 16-byte boundaries a lane reads what is added to its row, 32 columns ahead
-            uint4 more[8];
-            auto ask = [&](uint32_t c) {
-                const uint32_t col = col0 + c, left = row0 + lane < P.rows && col < P.cols ? min(32u, P.cols - col) : 0;
-                const unsigned char* p = P.add + (row0 + lane) * P.add_stride;
-                if (left == 32) {
-                    const uint4* v = reinterpret_cast<const uint4*>(p + (uint64_t)col * (P.add_dtype ? 2 : 4));
-#pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i) more[i] = v[i];
-                    if (P.add_dtype == 0)
-#pragma unroll
-                        for (uint32_t i = 4; i < 8; ++i) more[i] = v[i];
-                    return;
-                }
-#pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) {                    // the last columns of a row
-                    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) {
-                        if (P.add_dtype == 0 && j < 4 && 4 * i + j < left) w[j] = reinterpret_cast<const uint32_t*>(p)[col + 4 * i + j];
-                        if (P.add_dtype != 0 && i < 4 && 8 * i + j < left)
-                            w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[col + 8 * i + j] << (16 * (j & 1));
-                    }
-                    more[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            };
-            auto added = [&](float* y) {
-                if (P.add_dtype == 0) {
-#pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) {
-                        float x[4];
-                        Elem<float>::widen(more[i], x);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) y[4 * i + j] = __fadd_rn(y[4 * i + j], x[j]);
-                    }
-                    return;
-                }
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    float x[8];
-                    if (P.add_dtype == 1) Elem<__nv_bfloat16>::widen(more[i], x);
-                    else Elem<__half>::widen(more[i], x);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y[8 * i + j] = __fadd_rn(y[8 * i + j], x[j]);
-                }
-            };
-            const bool reads = P.add && !P.in_place && P.add_wide && P.out.wide && out;
-            if (reads) ask(start);
-            const bool good = __all_sync(~0u, wait_or_stop(acc_full + 8 * (n & 1), (n >> 1) & 1, limit, &stop));
-            tcgen05_after_sync();
-            const uint32_t from = tmem + ((quad * 32u) << 16) + (n & 1) * S::kSecond + half * 128u;
-            auto release = [&] {
-                tcgen05_before_sync();
-                __syncwarp();
-                if (lane == 0) leader_arrive(leader_addr(shared_free));
-            };
-            if (!shares) release();
-            if (!out) {
-                if (shares) release();
-                continue;
-            }
-            auto fetch32 = [&](uint32_t c, float* y) {
-                tmem_load32(from + c, y);
-                if (!good)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(0x7FC00000u);
-            };
-            auto fetch16 = [&](uint32_t c, float* y) {
-                tmem_load16(from + c, y);
-                if (!good)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(0x7FC00000u);
-            };
-            if (P.out.dtype >= 3) {
-                // the largest magnitude of this lane's 128 columns first, then the entries
-                const uint32_t row = row0 + lane, dtype = P.out.dtype, nc = min(128u, P.cols - col0);
-                uint32_t top = 0;
-#pragma unroll 1
-                for (uint32_t c = 0; c < 128; c += 32) {
-                    float y[32];
-                    fetch32(c, y);
-#pragma unroll
-                    for (uint32_t i = 0; i < 32; ++i)
-                        if (c + i < nc) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
-                }
-                const uint32_t byte = act8_byte(top, dtype);
-                const float by = act8_down(byte);
-#pragma unroll 1
-                for (uint32_t at = 0; at < 128; at += 64) {
-                    const uint32_t u = (at + start) & 127u;
-#pragma unroll
-                    for (uint32_t h = 0; h < 2; ++h) {
-                        float y[32];
-                        fetch32(u + 32 * h, y);
-                        if (h == 0) sent();
-#pragma unroll
-                        for (uint32_t c = 0; c < 2; ++c) {
-                            uint32_t w[4];
-                            act8_code<16>(y + 16 * c, by, dtype, w);
-                            sts16(place(lane, 2 * h + c), make_uint4(w[0], w[1], w[2], w[3]));
-                        }
-                    }
-                    if (at == 0 && shares) release();
-                    send(row0, col0 + u);
-                }
-                if (row < P.rows) P.out.scales[act8_scale_at(row, col0 >> 7, P.out.groups)] = (uint8_t)byte;
-                continue;
-            }
-            if (P.out.wide && (!P.add || P.in_place || reads)) {
-                // 64 columns to registers, and their place in tensor memory is free for the next tile
-#pragma unroll 1
-                for (uint32_t at = 0; at < 128; at += 64) {
-                    const uint32_t c = (at + start) & 127u;
-                    float y[64];
-                    fetch32(c, y);
-                    fetch32(c + 32, y + 32);
-                    if (at == 0 && shares) release();
-#pragma unroll
-                    for (uint32_t h = 0; h < 2; ++h) {
-                        if (reads) {
-                            added(y + 32 * h);
-                            if (h == 0) ask(c + 32);
-                            else if (at == 0) ask((c + 64) & 127u);
-                        }
-                        if (P.out.dtype == 0) {
-#pragma unroll
-                            for (uint32_t u = 0; u < 2; ++u) {
-                                sent();
-#pragma unroll
-                                for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 32 * h + 16 * u + 4 * i));
-                                send(row0, col0 + c + 32 * h + 16 * u);
-                            }
-                        } else {
-                            sent();
-#pragma unroll
-                            for (uint32_t i = 0; i < 4; ++i)
-                                sts16(place(lane, i), P.out.dtype == 1 ? Elem<__nv_bfloat16>::narrow(y + 32 * h + 8 * i) : Elem<__half>::narrow(y + 32 * h + 8 * i));
-                            send(row0, col0 + c + 32 * h);
-                        }
-                    }
-                }
-                continue;
-            }
-            sent();
-            if (!P.out_quad && !P.add) {
-                // Rows that begin anywhere, in words of four bytes, 16 to a row and two rows at a time; a row of 16-bit
-                // entries that begins between two words takes its words from both halves' neighbours, and its
-                // first and last entry go out alone.  Word i of row r lies at i ^ (r / 2), so that neither 32
-                // rows' same words nor two whole rows meet in a bank.
-                const bool four = P.out.dtype == 0;
-                const uint32_t rows = min(32u, P.rows - row0), x = lane & 15u, second = lane >> 4;
-                const uint32_t step = four ? 16 : 32;                 // columns
-#pragma unroll 1
-                for (uint32_t at = 0; at < 128; at += step) {
-                    const uint32_t c = (at + start) & 127u, left = col0 + c < P.cols ? min(step, P.cols - col0 - c) : 0;
-                    unsigned char* first = P.out.data + row0 * P.out.stride + (uint64_t)(col0 + c) * (four ? 4 : 2);
-                    uint32_t w[16];
-                    if (four) {
-                        fetch16(c, reinterpret_cast<float*>(w));
-                    } else {
-                        float y[32];
-                        fetch32(c, y);
-#pragma unroll
-                        for (uint32_t i = 0; i < 16; ++i)
-                            w[i] = P.out.dtype == 1 ? Elem<__nv_bfloat16>::pair(y[2 * i], y[2 * i + 1]) : Elem<__half>::pair(y[2 * i], y[2 * i + 1]);
-                    }
-                    if (at + step == 64 && shares) release();
-                    __syncwarp();                                     // what was here has been read
-                    if (!left) continue;
-#pragma unroll
-                    for (uint32_t i = 0; i < 16; ++i)
-                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(own + lane * 64u + ((i ^ (lane >> 1)) << 2)), "r"(w[i]) : "memory");
-                    if (!four) {
-                        uint16_t* mine = reinterpret_cast<uint16_t*>(first + lane * P.out.stride);
-                        if (lane < rows && (reinterpret_cast<uintptr_t>(mine) & 2u)) {
-                            mine[0] = (uint16_t)w[0];
-                            if (left == 32) mine[31] = (uint16_t)(w[15] >> 16);
-                        }
-                    }
-                    __syncwarp();
-                    // this lane's word of rows `second`, `second` + 2, ...; rows alike in parity by the stride's
-                    unsigned char* to = first + second * P.out.stride + 4 * x;
-#pragma unroll
-                    for (uint32_t k = 0; k < 16; ++k, to += 2 * P.out.stride) {
-                        const uint32_t line = own + k * 128u + second * 64u;
-                        uint32_t v, next = 0;
-                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(line + ((x ^ k) << 2)));
-                        if (four) {
-                            if (2 * k + second < rows && x < left) *reinterpret_cast<uint32_t*>(to) = v;
-                            continue;
-                        }
-                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(next) : "r"(line + (((x + 1) & 15u) ^ k) * 4u));
-                        const uint32_t odd = (uint32_t)(reinterpret_cast<uintptr_t>(to) >> 1) & 1u, e = 2 * x + odd;   // first entry
-                        v = __funnelshift_r(v, next, 16 * odd);
-                        if (2 * k + second >= rows) continue;
-                        if (e + 1 < left) *reinterpret_cast<uint32_t*>(to + 2 * odd) = v;
-                        else if (e < left && !(odd && left == 32)) *reinterpret_cast<uint16_t*>(to + 2 * odd) = (uint16_t)v;
-                    }
-                }
-                continue;
-            }
-            if (!P.out_quad || (P.add && !P.add_quad)) {
-                // rows that begin anywhere: a lane a column, two rows at a time
-                const uint32_t rows = min(32u, P.rows - row0), x = lane & 15u;
-                const bool four = P.out.dtype == 0, bf16 = P.out.dtype == 1;
-#pragma unroll 1
-                for (uint32_t at = 0; at < 128; at += 16) {
-                    const uint32_t c = (at + start) & 127u, col = col0 + c + x;
-                    float y[16];
-                    fetch16(c, y);
-#pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 4 * i));
-                    if (at == 48 && shares) release();
-                    __syncwarp();
-                    unsigned char* to = P.out.data + (row0 + (lane >> 4)) * P.out.stride + (uint64_t)col * (four ? 4 : 2);
-                    if (col < P.cols)
-#pragma unroll 1
-                        for (uint32_t r0 = lane >> 4; r0 < rows; r0 += 16) {
-                            float add[8];                            // all before the first is written: D may be C
-                            if (P.add)
-#pragma unroll
-                                for (uint32_t i = 0; i < 8; ++i) add[i] = r0 + 2 * i < rows ? prod_get1(P, row0 + r0 + 2 * i, col) : 0.f;
-#pragma unroll
-                            for (uint32_t i = 0; i < 8; ++i, to += 2 * P.out.stride) {
-                                const uint32_t r = r0 + 2 * i;
-                                float v = lds1(place(r, x >> 2) + 4 * (x & 3u));
-                                if (P.add) v = __fadd_rn(v, add[i]);
-                                if (r >= rows) continue;
-                                if (four) *reinterpret_cast<float*>(to) = v;
-                                else *reinterpret_cast<uint16_t*>(to) = bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
-                            }
-                        }
-                    __syncwarp();
-                }
-                continue;
-            }
-            // what is added is asked for 16 columns ahead
-            uint4 next[4];
-            if (P.add) ahead(row0, col0 + start, next);
-#pragma unroll 1
-            for (uint32_t at = 0; at < 128; at += 16) {
-                const uint32_t c = (at + start) & 127u, col = col0 + c + 4 * piece, m = inside4(col, P.cols);
-                float y[16];
-                fetch16(c, y);
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) sts16(place(lane, i), Elem<float>::narrow(y + 4 * i));
-                if (at == 48 && shares) release();
-                __syncwarp();
-                uint4 now[4];
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) now[i] = next[i];
-                if (P.add && at < 112) ahead(row0, col0 + ((c + 16) & 127u), next);
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t r = 8 * i + (lane >> 2);
-                    float x[4], add[4];
-                    Elem<float>::widen(lds16(place(r, piece)), x);
-                    if (row0 + r >= P.rows || !m) continue;
-                    if (P.add) {
-                        prod_widen4(P.add_dtype, now[i], add);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) x[j] = __fadd_rn(x[j], add[j]);
-                    }
-                    prod_put4(P, row0 + r, col, m, x);
-                }
-                __syncwarp();
-            }
-        }
-        if (lane == 0) bulk_wait_all();
+        prod_pair_results(P, tmem, epi + warp * S::kEpi, acc_full, shared_free, rank, pair, P.tiles, pairs, &stop);
     }
     __syncwarp();
     tcgen05_before_sync();
