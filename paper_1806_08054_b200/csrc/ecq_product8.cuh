@@ -777,36 +777,42 @@ __device__ __forceinline__ void prod_pair_results(const Product8& P, uint32_t tm
                 for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(0x7FC00000u);
         };
         if (P.out.dtype >= 3) {
-            // the largest magnitude of this lane's 128 columns first, then the entries
-            const uint32_t row = row0 + lane, dtype = P.out.dtype, nc = min(128u, P.cols - col0);
+            // the largest magnitude of this lane's 128 columns first, then the entries; those that the next tile waits for
+            // stay in registers meanwhile
+            const uint32_t row = row0 + lane, dtype = P.out.dtype, nc = min(128u, P.cols - col0), other = start ^ 64u;
             uint32_t top = 0;
-#pragma unroll 1
-            for (uint32_t c = 0; c < 128; c += 32) {
-                float y[32];
-                fetch32(c, y);
+            auto largest = [&](uint32_t c, const float* y) {
 #pragma unroll
                 for (uint32_t i = 0; i < 32; ++i)
                     if (c + i < nc) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+            };
+            float y[64];
+            fetch32(start, y);
+            fetch32(start + 32, y + 32);
+            if (shares) release();
+            largest(start, y);
+            largest(start + 32, y + 32);
+#pragma unroll 1
+            for (uint32_t c = other; c < other + 64; c += 32) {
+                float z[32];
+                fetch32(c, z);
+                largest(c, z);
             }
             const uint32_t byte = act8_byte(top, dtype);
             const float by = act8_down(byte);
 #pragma unroll 1
-            for (uint32_t at = 0; at < 128; at += 64) {
-                const uint32_t u = (at + start) & 127u;
+            for (uint32_t c = start;; c = other) {
+                sent();
 #pragma unroll
-                for (uint32_t h = 0; h < 2; ++h) {
-                    float y[32];
-                    fetch32(u + 32 * h, y);
-                    if (h == 0) sent();
-#pragma unroll
-                    for (uint32_t c = 0; c < 2; ++c) {
-                        uint32_t w[4];
-                        act8_code<16>(y + 16 * c, by, dtype, w);
-                        sts16(place(lane, 2 * h + c), make_uint4(w[0], w[1], w[2], w[3]));
-                    }
+                for (uint32_t i = 0; i < 4; ++i) {
+                    uint32_t w[4];
+                    act8_code<16>(y + 16 * i, by, dtype, w);
+                    sts16(place(lane, i), make_uint4(w[0], w[1], w[2], w[3]));
                 }
-                if (at == 0 && shares) release();
-                send(row0, col0 + u);
+                send(row0, col0 + c);
+                if (c == other) break;
+                fetch32(other, y);
+                fetch32(other + 32, y + 32);
             }
             if (row < P.rows) P.out.scales[act8_scale_at(row, col0 >> 7, P.out.groups)] = (uint8_t)byte;
             continue;
