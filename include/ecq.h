@@ -524,7 +524,7 @@ int ecq_muon_status(ecq_muon* plan, void* cuda_stream);
  *
  * rows (m) == 0 does nothing (a weight's gradient is zero).  ECQ_ERR_ARG for rows or columns beyond 2^28, strides beyond 2^36, more than
  * 2^31 - 1 tiles of 128 x 128, no columns, or a violation of what is said above and below.  Results must not overlap each
- * other, or inputs; a plain result may be a plain input of the same place and strides.  Entries
+ * other, or inputs; a plain result may be a plain input of the same type, place and strides.  Entries
  * behind a row's last column are left as they are.  All on the current device; each call is one kernel
  * launch, ecq_act8_norm_grad with a weight's gradient two; no allocation; any of them may be captured into a CUDA graph.
  *
@@ -596,10 +596,12 @@ int ecq_act8_norm_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* sum,
  * Product of matrices in 8 bits, d = a b^T + c: a [m, k], b [n, k] with blocks along k (a weight or an activation
  * stored transposed serves the products of the backward pass), c [m, n] plain or NULL, d [m, n] plain, or in 8
  * bits where c is NULL.  Sums over k are in fp32, in an order that the sizes (and the GPU's number of SMs) fix; d is rounded once.  c may
- * be d, in place: adding a weight's gradient to what is there.
+ * be d, in place: adding a weight's gradient to what is there.  In place in 32 bits the memory may do the addition,
+ * which makes zeros of sums below 2^-126.
  *   status   device word or NULL: bit 1 (value 2) is set when an in-kernel wait ran out (ECQ_ERR_TIMEOUT's
  *            meaning); entries of d that it concerned are NaN.  Never cleared by the library.
- * ecq_act8_set_wait_limit  as ecq_set_wait_limit, for this process's products.
+ * ecq_act8_set_wait_limit  as ecq_set_wait_limit, for this process's calls on matrices in 8 bits (other than products they
+ *            read what did not come in time from memory: their results stay right).
  */
 int ecq_act8_product(uint64_t m, uint64_t n, uint64_t k, const ecq_act8_matrix* a, const ecq_act8_matrix* b,
                      const ecq_act8_matrix* c, const ecq_act8_matrix* d, uint32_t* status,

@@ -69,6 +69,7 @@ int launch_tiles(Act8Tiles& P, uint64_t rows, uint64_t cols, int plain, bool cod
     P.cols = (uint32_t)cols;
     P.tiles_across = (uint32_t)((cols + 127) / 128);
     P.tiles = (P.rows + 127) / 128 * P.tiles_across;
+    P.wait_limit = g_act8_wait_limit.load(std::memory_order_relaxed);
     P.wide = 1;
     for (const Act8Mat* m : {&P.in[0], &P.in[1], &P.d, &P.plain[0], &P.plain[1]}) P.wide &= !m->data || m->wide;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -14,6 +14,9 @@
 
 namespace ecq {
 
+// Polls of a wait inside a kernel (ecq_act8_set_wait_limit).
+inline std::atomic<uint32_t> g_act8_wait_limit{kWaitLimit};
+
 constexpr uint64_t kActMaxSide = 1ull << 28;
 constexpr uint64_t kActMaxStride = 1ull << 36;                        // entries
 

@@ -27,6 +27,7 @@ struct Act8Tiles {
     Act8Mat kept[2];                     // gate and up in 8 bits
     uint32_t rows, cols, tiles_across, tiles;
     int wide;                            // rows of all plain matrices begin on 16-byte boundaries
+    uint32_t wait_limit;
 };
 
 // 1 / (1 + exp(-x)) of two entries; WIDE: the rounding of x log2(e) is added back, which shows in 32 bits alone.
@@ -326,7 +327,7 @@ struct Act8Maps { CUtensorMap of[3]; };  // in[0], in[1] and d in boxes of 128 x
 
 // CTAs stay on the GPU and take every n-th tile.  Whole tiles come by TMA as many ahead as there is room for: a
 // thread's four rows alone are too little on their way to memory, in 8 bits above all, and registers have
-// no room for the next tile's.  (A wait that runs out reads the tile from memory instead.)
+// no room for the next tile's.  After a wait that ran out tiles are read from memory, and none is asked for any more.
 template <int OP, typename S, typename T>
 __global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas)
     act8_tiles_kernel(const __grid_constant__ Act8Tiles P, const __grid_constant__ Act8Maps maps) {
@@ -335,12 +336,14 @@ __global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas)
     extern __shared__ unsigned char raw[];
     __shared__ __align__(16) Act8Turn<OP == kActGateGrad ? 2 : 1> turn;
     __shared__ __align__(8) uint64_t bars[kStages];
+    __shared__ volatile uint32_t late, asked;
     const uint32_t ring = (smem_u32(raw) + 127u) & ~127u, full = smem_u32(bars), tid = threadIdx.x;
     auto whole = [&](uint32_t tile) {
         return (tile / P.tiles_across + 1) * 128u <= P.rows && (tile % P.tiles_across + 1) * 128u <= P.cols && P.wide;
     };
     if (tid == 0) {
         for (uint32_t s = 0; s < kStages; ++s) mbar_init(full + 8 * s, 1);
+        late = asked = 0;
         fence_mbar_init();
     }
     griddep_launch();
@@ -364,6 +367,7 @@ __global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas)
         }
         if (OP == kActGateGrad) tma_load_2d(to, &maps.of[2], (int)(tc * 128), (int)(tr * 128), bar);
         coming += gridDim.x;
+        asked = asked + 1;
     };
     if (tid == 0)
         for (uint32_t s = 0; s < kStages; ++s) ask(s);
@@ -378,18 +382,22 @@ __global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas)
             continue;
         }
         const uint32_t s = it % kStages, from = ring + s * R::kBytes;
-        if (mbar_wait(full + 8 * s, (it / kStages) & 1)) {
+        if (!late && mbar_wait_n(full + 8 * s, (it / kStages) & 1, P.wait_limit)) {
             act8_take(from, col0 >> 7, in.a);
             if constexpr (OP != kActCopy) act8_take(from + R::kIn, col0 >> 7, in.b);
             if constexpr (OP == kActGateGrad) act8_take(from + 2 * R::kIn, 0, in.d);
         } else {
+            late = 1;
             act8_read<OP, S, T, true>(P, at, in);
         }
         ++it;
         __syncthreads();                                             // everyone has read the stage
-        if (tid == 0) ask(s);
+        if (tid == 0 && !late) ask(s);
         act8_tile<OP, S, T, true>(P, at, in, turn);
     }
+    // nothing is in flight when this CTA leaves
+    if (tid == 0 && late)
+        for (uint32_t n = asked, j = n > kStages ? n - kStages : 0; j < n; ++j) mbar_wait(full + 8 * (j % kStages), (j / kStages) & 1);
 }
 
 // ---- norm -----------------------------------------------------------------------------------------
@@ -557,7 +565,7 @@ __device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, uint32
 
 // What a thread reads of a row.  FULL: the next row's part is on its way to shared memory meanwhile, in places of the
 // thread's own, so that nobody waits for anybody (registers have no room for it: 16 warps an SM then have
-// their one row each on the way, 59 us for 8192 x 4096 against ..).
+// their one row each on the way, 59 us for 8192 x 4096 against 42).
 template <typename S, typename T, int NV>
 struct NormRead {
     Raw8<S> a[NV];

@@ -14,8 +14,6 @@ using namespace ecq;
 
 namespace {
 
-std::atomic<uint32_t> g_wait_limit{kWaitLimit};
-
 // Boxes of 128 bytes along K and `box` rows; what is beyond the matrix arrives as zeros.
 bool entries_map(CUtensorMap* tm, const ecq_act8_matrix* m, uint64_t rows, uint64_t k, uint32_t box) {
     const cuuint64_t dims[2] = {k, rows}, strides[1] = {m->stride};
@@ -125,7 +123,7 @@ Way choose(uint64_t m, uint64_t n, uint32_t steps, int dev, int sms, bool slow, 
 extern "C" {
 
 int ecq_act8_set_wait_limit(uint32_t polls) {
-    g_wait_limit.store(polls, std::memory_order_relaxed);
+    g_act8_wait_limit.store(polls, std::memory_order_relaxed);
     return ECQ_OK;
 }
 
@@ -157,7 +155,7 @@ int ecq_act8_product(uint64_t m, uint64_t n, uint64_t k, const ecq_act8_matrix* 
     P.steps = up(k, 128);
     P.tail = up(k - (uint64_t)(P.steps - 1) * 128, 32);
     P.left_groups = P.right_groups = up(k, 512);
-    P.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
+    P.wait_limit = g_act8_wait_limit.load(std::memory_order_relaxed);
 
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (m == 1 && n * k <= 1u << 23 && d->dtype < 3) {

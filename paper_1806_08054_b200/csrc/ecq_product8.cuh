@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kFewThreads) act8_product_few_kernel(const __g
 // two CTAs alone need 32 each), K shared out over the CTAs (pairs) of a cluster.  Each of them finishes its share of the
 // tile: the others send it theirs, by stores that count bytes on a barrier of its own, to a place that no
 // load uses, and it adds them in a fixed order.  (Both ways through the loads' ring, with a barrier of the cluster
-// before and behind: 1.. us more.)  SWAP: the left operand is B and the right one A (a few tokens), the tile is D's
+// before and behind: 1.2 us more at 1024 x 1024 x 8192.)  SWAP: the left operand is B and the right one A (a few tokens), the tile is D's
 // transposed; so a matrix of weights fills the 128 rows of an instruction.
 
 template <int CG, int TN, bool SWAP>

@@ -242,6 +242,85 @@ def test_gate_in_place():
     assert torch.equal(g, want)
 
 
+def gate_parts(P, lo, hi, kept):
+    """Rows lo .. hi - 1 of a plain matrix, or of a pair as one of its own."""
+    if not kept:
+        return P[lo:hi]
+    p = pair(hi - lo, P[0].shape[1], P[0].dtype)
+    p[0].view(torch.uint8).copy_(P[0].view(torch.uint8)[lo:hi])
+    p[1][scale_places(*p[0].shape)] = scale_bytes(P)[lo:hi]
+    return p
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("kept", [False, True])
+def test_many_tiles_are_as_few(dtype, kept):
+    """Enough tiles that those ahead are on their way, whole ones and ones at both edges: bit for bit what calls on 512 rows
+    give (which the tests above hold to 64 bits)."""
+    rows, cols = 5000, 4008
+    x = strided(rows, cols, dtype).copy_(random(rows, cols, 51))
+    u = strided(rows, cols, dtype).copy_(random(rows, cols, 52))
+    d = strided(rows, cols, dtype).copy_(random(rows, cols, 53))
+    g8, u8 = pair(rows, cols, E5M2), pair(rows, cols, E5M2)
+    ecq.ecq_act8_store(x, g8)
+    ecq.ecq_act8_store(u, u8)
+    a, b = (g8, u8) if kept else (x, u)
+
+    def calls(a, b, d, rows):
+        plain = [strided(rows, cols, dtype) for _ in range(4)]
+        q = [pair(rows, cols, k) for k in (E4M3, E5M2, E4M3, E5M2, E4M3, E4M3)]
+        t = [pair(cols, rows, k) for k in (E4M3, E5M2, E4M3, E5M2)]
+        ecq.ecq_act8_store(a, q[0], t[0])
+        if kept:
+            ecq.ecq_act8_load(a, plain[0])
+        else:
+            plain[0].copy_(a)
+        ecq.ecq_act8_gate(a, b, plain[1], q[1], t[1], q[4], q[5])
+        ecq.ecq_act8_gate_grad(a, b, d, plain[2], plain[3], q[2], t[2], q[3], t[3])
+        return plain, q, t
+
+    plain, q, t = calls(a, b, d, rows)
+    for p in q + t:
+        behind_is_left(p)
+    for lo in range(0, rows, 512):
+        hi = min(rows, lo + 512)
+        few = calls(gate_parts(a, lo, hi, kept), gate_parts(b, lo, hi, kept), d[lo:hi], hi - lo)
+        for one, all_of in zip(few[0], plain):
+            assert torch.equal(one, all_of[lo:hi])
+        for one, all_of in zip(few[1], q):
+            assert torch.equal(bytes_of(one)[:, :cols], bytes_of(all_of)[lo:hi, :cols])
+            assert torch.equal(scale_bytes(one), scale_bytes(all_of)[lo:hi])
+        for one, all_of in zip(few[2], t):
+            assert torch.equal(bytes_of(one)[:, :hi - lo], bytes_of(all_of)[:, lo:hi])
+            assert torch.equal(scale_bytes(one), scale_bytes(all_of)[:, lo // 128:(hi + 127) // 128])
+
+
+def test_tiles_that_do_not_come_in_time_are_read_from_memory():
+    x = random(5000, 4000, 61).to(BF16)
+    q, t, late, late_t = pair(5000, 4000), pair(4000, 5000), pair(5000, 4000), pair(4000, 5000)
+    ecq.ecq_act8_store(x, q, t)
+    ecq.ecq_act8_set_wait_limit(0)
+    try:
+        ecq.ecq_act8_store(x, late, late_t)
+        torch.cuda.synchronize()
+    finally:
+        ecq.ecq_act8_set_wait_limit()
+    for a, b in ((q, late), (t, late_t)):
+        assert torch.equal(bytes_of(a), bytes_of(b)) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("rows,cols,stride", [(70, 200, 200), (70, 201, 203), (5000, 1024, 1024)])
+def test_gate_gradient_in_place(rows, cols, stride):
+    g, u, d = (strided(rows, cols, BF16, stride).copy_(random(rows, cols, k)) for k in (1, 2, 3))
+    dg, du = strided(rows, cols, BF16, stride), strided(rows, cols, BF16, stride)
+    ecq.ecq_act8_gate_grad(g, u, d, dg, du)
+    ecq.ecq_act8_gate_grad(g, u, d, g, u)
+    assert torch.equal(g, dg) and torch.equal(u, du)
+    ecq.ecq_act8_gate_grad(dg, du, d, g, u)
+    ecq.ecq_act8_gate_grad(dg, du, d, d)
+    assert torch.equal(d, g)
+
+
 # ---- norm ------------------------------------------------------------------------------------------
 
 NORM_SIZES = [(1, 1), (1, 7), (3, 8), (2, 200), (9, 256), (33, 513), (700, 1024), (1, 4096), (5, 4097), (3, 8192), (2, 12001),
@@ -334,6 +413,21 @@ def test_norm_grad(rows, cols, dtype, kept):
     again = torch.empty_like(d_w)
     ecq.ecq_act8_norm_grad(saved, w, rstd, d, None, again, work)
     assert torch.equal(d_w, again)
+
+
+@pytest.mark.parametrize("rows,cols,stride", [(300, 500, 500), (300, 1001, 1003), (3000, 1024, 1024), (2, 9000, 9001)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_norm_gradient_in_place(rows, cols, stride, dtype):
+    s, d, e = (strided(rows, cols, dtype, stride).copy_(random(rows, cols, k)) for k in (1, 2, 3))
+    w, rstd = random(1, cols, 4)[0].float(), torch.rand(rows, device="cuda") + 0.5
+    work = torch.empty(ecq.ecq_act8_norm_grad_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    want, dw = strided(rows, cols, dtype, stride), torch.empty(cols, device="cuda")
+    ecq.ecq_act8_norm_grad(s, w, rstd, d, want, dw, work, d_sum=e)
+    for place in (0, 1, 2):
+        x = [strided(rows, cols, dtype, stride).copy_(y) for y in (s, d, e)]
+        again = torch.empty_like(dw)
+        ecq.ecq_act8_norm_grad(x[0], w, rstd, x[1], x[place], again, work, d_sum=x[2])
+        assert torch.equal(x[place], want) and torch.equal(again, dw)
 
 
 def test_norm_grad_is_the_formulas_derivative():

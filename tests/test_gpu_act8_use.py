@@ -1,12 +1,15 @@
 """The operators on matrices in 8 bits as a program uses them: a gated layer's forward and backward pass run
 together, captured and replayed, on two streams, beside the codec, and beyond 2^32 bytes."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
 
 import paper_1806_08054_b200 as ecq
-from act8_util import E4M3, E5M2, check_plain, pair, random, scale_bytes, scale_places, stored, strided, values
+from act8_util import E5M2, check_plain, pair, random, scale_places, stored, strided, values
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -142,6 +145,47 @@ def test_captured_and_replayed(tokens, width, hidden):
     eager.step()
     for a, b in zip(L.results(), eager.results()):
         assert torch.equal(a, b)
+
+
+FIRST = """
+import torch
+import paper_1806_08054_b200 as ecq
+from act8_util import pair, random, stored
+x = random(300, 520, 1).bfloat16()
+q, t, out = pair(300, 520), pair(520, 300), torch.zeros_like(x)
+a, b, rstd = stored(random(2000, 700, 2)), stored(random(900, 700, 3)), torch.ones(300, device="cuda")
+d, one, dw = torch.zeros(2000, 900, device="cuda"), torch.zeros(200, 900, device="cuda"), torch.zeros(520, device="cuda")
+few = stored(random(200, 700, 4))
+work = torch.empty(ecq.ecq_act8_norm_grad_workspace_bytes(300, 520), dtype=torch.uint8, device="cuda")
+torch.cuda.synchronize()
+
+def calls():
+    ecq.ecq_act8_store(x, q, t)
+    ecq.ecq_act8_load(q, out)
+    ecq.ecq_act8_gate(x, x, out)
+    ecq.ecq_act8_norm(x, out, sum=out)
+    ecq.ecq_act8_norm_grad(x, None, rstd, x, out, dw, work)
+    ecq.ecq_act8_product(a, b, d)
+    ecq.ecq_act8_product(few, b, one)
+
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    calls()
+graph.replay()
+torch.cuda.synchronize()
+got = [y.clone() for y in (out, d, one, dw)]
+calls()
+for y, z in zip((out, d, one, dw), got):
+    assert torch.equal(y, z) and bool(z.any())
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    """Nothing that a first call sets up (kernels' limits, what the GPU holds at once) is refused while a stream is captured."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join([here, os.path.dirname(here)]))
+    run = subprocess.run([sys.executable, "-c", FIRST], env=env, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0, run.stderr[-2000:]
 
 
 def test_two_streams_at_once():

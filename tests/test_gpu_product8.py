@@ -122,6 +122,19 @@ def test_in_place_addition(m, n, k):
     assert torch.equal(d.double(), want)
 
 
+@pytest.mark.parametrize("m,n,k,stride", [(1, 300, 400, 300), (5, 301, 400, 303), (200, 304, 1300, 304), (200, 301, 300, 301), (2300, 2104, 300, 2104),
+                                          (2300, 2101, 300, 2101), (2300, 2102, 300, 2104)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_in_place_is_as_apart(m, n, k, stride, dtype):
+    a, b = stored(random(m, k, 1)), stored(random(n, k, 2))
+    c, d, e = (strided(m, n, dtype, stride) for _ in range(3))
+    c.copy_(random(m, n, 3))
+    e.copy_(c)
+    ecq.ecq_act8_product(a, b, d, add=c)
+    ecq.ecq_act8_product(a, b, e, add=e)
+    assert torch.equal(d, e)
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 300, 700), (200, 300, 1300), (2300, 2100, 300)])
 def test_nan_blocks_reach_their_rows_and_columns_alone(m, n, k):
     x, y = random(m, k, 1).float(), random(n, k, 2).float()
