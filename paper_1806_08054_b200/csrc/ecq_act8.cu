@@ -94,12 +94,29 @@ RowShape row_shape(uint64_t rows, uint64_t cols, int sms) {
 }
 
 template <typename T, int NV>
-int launch_norm(const Act8Norm& P, const RowShape& s, int sms, cudaStream_t st) {
-    const uint64_t slots = s.per_cta / s.per_row, need = (P.rows + slots - 1) / slots, most = (uint64_t)sms * (1024 / s.per_cta);
+int launch_norm(Act8Norm& P, const RowShape& s, int sms, cudaStream_t st) {
+    const uint64_t slots = s.per_cta / s.per_row, need = (P.rows + slots - 1) / slots;
+    uint64_t most = (uint64_t)sms * (1024 / s.per_cta);
+    // Two rows ahead where a CTA has several: of 16-bit entries, where rows are so long that
+    // few are worked on at a time, or where no time goes into 8 bits.  Without and with, in us, x and residual to sum and 8 bits:
+    // 2048 x 16384 50.7, 39.7, 4096 x 8192 43.2, 40.4, 8192 x 4096 41.2, 41.9; x alone to 16 bits: 2048 x 16384 40.6, 25.9,
+    // 8192 x 4096 30.5, 26.2, 8192 x 1024 10.6, 9.4, 8192 x 512 6.1, 6.4.  8192 x 4096 in 32 bits with a residual 73, 103 (half
+    // the threads have room).
+    if constexpr (sizeof(T) == 2 && NV > 1) {
+        if (P.full && need > most && (s.per_row == 512 || (s.per_row >= 64 && !P.y8.data && !P.sum8.data))) {
+            constexpr uint32_t kRoom = 192u * 1024u;                  // what an SM's CTAs take at most
+            static std::atomic<bool> done[kMaxDevices];
+            auto kernel = act8_norm_ahead_kernel<T, NV>;
+            const uint32_t ctas = (NV == 4 ? 512 : 1024) / s.per_cta, row = s.per_cta * NV * 16 * (P.residual.data ? 2 : 1);
+            most = (uint64_t)sms * ctas;
+            if (!allow_smem(reinterpret_cast<const void*>(kernel), kRoom, done)) return ECQ_ERR_CUDA;
+            return launch_act8(kernel, (uint32_t)(need < most ? need : most), s.per_cta, kNormStages * row, 0, st, P);
+        }
+    }
     return launch_act8(act8_norm_kernel<T, NV>, (uint32_t)(need < most ? need : most), s.per_cta, 0, 0, st, P);
 }
 template <typename T>
-int launch_norm(const Act8Norm& P, const RowShape& s, int sms, cudaStream_t st) {
+int launch_norm(Act8Norm& P, const RowShape& s, int sms, cudaStream_t st) {
     return s.vectors == 1 ? launch_norm<T, 1>(P, s, sms, st) : s.vectors == 2 ? launch_norm<T, 2>(P, s, sms, st) : launch_norm<T, 4>(P, s, sms, st);
 }
 

@@ -467,8 +467,17 @@ __device__ __forceinline__ float act8_row_sum(float v, uint32_t per_row, float* 
     return v;
 }
 
-template <typename T, int NV, bool FULL>
-__device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part) {
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, uint32_t bytes) {
+    if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
+
+constexpr uint32_t kNormStages = 3;
+
+// AHEAD: the parts of the next two rows are on their way to shared memory meanwhile, in places of the thread's own, so that
+// nobody waits for anybody.
+template <typename T, int NV, bool FULL, bool AHEAD>
+__device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part, unsigned char* raw) {
     const uint32_t slot = threadIdx.x / P.per_row, t = threadIdx.x - slot * P.per_row, slots = blockDim.x / P.per_row;
     float w[NV][8];
     uint32_t cols[NV];                                               // entries of each vector that are inside
@@ -479,21 +488,56 @@ __device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part) {
         act8_weight(P.weight, P.weight_dtype, col, cols[k], w[k]);
     }
     const uint32_t step = P.per_row * 8 * (uint32_t)sizeof(T), at = 8 * t * (uint32_t)sizeof(T);
+    const uint64_t stride = (uint64_t)gridDim.x * slots;
+    constexpr int kVecs = (int)sizeof(T) / 2;                        // 16 bytes of all threads lie together
+    const uint32_t piece = blockDim.x * 16u, stage = NV * kVecs * piece * (P.residual.data ? 2 : 1);
+    const uint32_t ring = smem_u32(raw) + threadIdx.x * 16u, rings = kNormStages * stage;
+    auto ask = [&](uint64_t row, uint32_t to) {
+        if (row < P.rows) {
+            const unsigned char *x = act8_row(P.x, (uint32_t)row) + at, *r = act8_row(P.residual, (uint32_t)row) + at;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < kVecs; ++i) {
+                    if (!cols[k]) continue;
+                    copy_ahead(to + (k * kVecs + i) * piece, x + k * step + 16 * i, 16);
+                    if (P.residual.data) copy_ahead(to + ((NV + k) * kVecs + i) * piece, r + k * step + 16 * i, 16);
+                }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    uint64_t coming = (uint64_t)blockIdx.x * slots + slot;           // the next row to ask for, and where to
+    uint32_t into = 0, from = 0;
+    if (AHEAD)
+        for (; into + stage < rings; into += stage, coming += stride) ask(coming, ring + into);
     uint32_t turn = 0;
-    for (uint64_t first = (uint64_t)blockIdx.x * slots; first < P.rows; first += (uint64_t)gridDim.x * slots, ++turn) {
+    for (uint64_t first = (uint64_t)blockIdx.x * slots; first < P.rows; first += stride, ++turn) {
         const uint32_t row = (uint32_t)first + slot;
         const bool real = row < P.rows;
         Raw8<T> a[NV], b[NV];
         const unsigned char *x = act8_row(P.x, row) + at, *r = act8_row(P.residual, row) + at;
+        if (AHEAD) {
+            ask(coming, ring + into);
+            coming += stride;
+            into = into + stage == rings ? 0 : into + stage;
+            asm volatile("cp.async.wait_group %0;" ::"n"(kNormStages - 1) : "memory");
+        }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             a[k] = {};
             b[k] = {};
-            if (real && cols[k]) {
+            if (AHEAD) {
+#pragma unroll
+                for (int i = 0; i < kVecs; ++i) {
+                    if (real && cols[k]) a[k].w[i] = lds16(ring + from + (k * kVecs + i) * piece);
+                    if (real && cols[k] && P.residual.data) b[k].w[i] = lds16(ring + from + ((NV + k) * kVecs + i) * piece);
+                }
+            } else if (real && cols[k]) {
                 get8<FULL>(P.x, x + k * step, nullptr, cols[k], a[k]);
                 if (P.residual.data) get8<FULL>(P.residual, r + k * step, nullptr, cols[k], b[k]);
             }
         }
+        if (AHEAD) from = from + stage == rings ? 0 : from + stage;
         float s[NV][8], squares = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -535,13 +579,23 @@ __device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part) {
     }
 }
 
+// (Two vectors of 32 bits: two CTAs of 512 have to fit, or the compiler takes 83 registers: 8192 x 4096 to 32 bits 63 -> 49 us,
+// 4096 x 5120 61 -> 39.)
 template <typename T, int NV>
-__global__ void __launch_bounds__(512) act8_norm_kernel(const __grid_constant__ Act8Norm P) {
+__global__ void __launch_bounds__(512, NV == 2 && sizeof(T) == 4 ? 2 : 0) act8_norm_kernel(const __grid_constant__ Act8Norm P) {
     __shared__ float part[64];
     griddep_launch();
     griddep_wait();
-    if (P.full) act8_norm_rows<T, NV, true>(P, part);
-    else act8_norm_rows<T, NV, false>(P, part);
+    if (P.full) act8_norm_rows<T, NV, true, false>(P, part, nullptr);
+    else act8_norm_rows<T, NV, false, false>(P, part, nullptr);
+}
+template <typename T, int NV>
+__global__ void __launch_bounds__(512, NV == 4 ? 1 : 2) act8_norm_ahead_kernel(const __grid_constant__ Act8Norm P) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    __shared__ float part[64];
+    griddep_launch();
+    griddep_wait();
+    act8_norm_rows<T, NV, true, true>(P, part, raw);
 }
 
 // Its gradient.  With n = s rstd and g = d_out w:  d_x = rstd (g - n mean(g n)) + d_sum, and the weight's
@@ -557,11 +611,6 @@ struct Act8NormGrad {
     uint32_t rows, cols, per_row, pitch;
     float inv_cols;
 };
-
-__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, uint32_t bytes) {
-    if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
-}
 
 // What a thread reads of a row.  FULL: the next row's part is on its way to shared memory meanwhile, in places of the
 // thread's own, so that nobody waits for anybody (registers have no room for it: 16 warps an SM then have

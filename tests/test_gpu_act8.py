@@ -352,6 +352,27 @@ def test_norm(rows, cols, dtype, residual):
     behind_is_left(s8)
 
 
+@pytest.mark.parametrize("rows,cols", [(2600, 1024), (1300, 4096), (700, 5128), (700, 8192), (500, 16384), (6000, 200)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("coded", [False, True])
+def test_norm_of_many_aligned_rows(rows, cols, dtype, residual, coded):
+    x = strided(rows, cols, dtype).copy_(random(rows, cols, 31, 0.2))
+    r = strided(rows, cols, dtype, cols + 8).copy_(random(rows, cols, 32, 0.2)) if residual else None
+    w = random(1, cols, 33)[0].float()
+    total, y, rstd = strided(rows, cols, dtype), strided(rows, cols, dtype, cols + 16), torch.full((rows,), 7.0, device="cuda")
+    y8 = pair(rows, cols) if coded else None
+    ecq.ecq_act8_norm(x, r, w, eps=1e-5, sum=total, out=y, out8=y8, rstd=rstd)
+    s = x.double() + (r.double() if residual else 0.0)
+    f = 1 / torch.sqrt(s.square().mean(1) + 1e-5)
+    want = s * f[:, None] * w.double()
+    assert bool(((rstd.double() - f).abs() <= f * NORM_REL).all())
+    check_plain(total, s, s.abs() * 2.0 ** -24, "sum")
+    check_plain(y, want, want.abs() * NORM_REL, "out")
+    if coded:
+        check_pair(y8, want, want.abs() * NORM_REL, "out8")
+
+
 def test_norm_without_a_weight_and_zero_rows():
     x = random(5, 300, 1).float()
     x[2] = 0.0
