@@ -467,8 +467,12 @@ __device__ __forceinline__ float act8_row_sum(float v, uint32_t per_row, float* 
     return v;
 }
 
-__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from, uint32_t bytes) {
-    if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+// 16 bytes of a row (8 of one in 8 bits), E an entry's.  A lane's eight entries of 32 bits are two of these, halves of what comes
+// from L2 as one, so it stays in L1 for the second.
+template <uint32_t E>
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from) {
+    if (E == 4) asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else if (E == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
 }
 
@@ -500,8 +504,8 @@ __device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part, u
 #pragma unroll
                 for (int i = 0; i < kVecs; ++i) {
                     if (!cols[k]) continue;
-                    copy_ahead(to + (k * kVecs + i) * piece, x + k * step + 16 * i, 16);
-                    if (P.residual.data) copy_ahead(to + ((NV + k) * kVecs + i) * piece, r + k * step + 16 * i, 16);
+                    copy_ahead<sizeof(T)>(to + (k * kVecs + i) * piece, x + k * step + 16 * i);
+                    if (P.residual.data) copy_ahead<sizeof(T)>(to + ((NV + k) * kVecs + i) * piece, r + k * step + 16 * i);
                 }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -666,9 +670,9 @@ __device__ __forceinline__ void act8_norm_grad_rows(const Act8NormGrad& P, float
         const unsigned char *d = act8_row(P.d_out, row) + at, *e = act8_row(P.d_sum, row) + at;
         Read::places(from, [&](int m, int k, int i, uint32_t to) {
             if (!cols[k]) return;
-            if (m == 2) copy_ahead(to, s + k * P.per_row * 8 * sizeof(S) + 16 * i, sizeof(S) == 1 ? 8 : 16);
-            else if (m == 0) copy_ahead(to, d + k * step + 16 * i, 16);
-            else if (P.d_sum.data) copy_ahead(to, e + k * step + 16 * i, 16);
+            if (m == 2) copy_ahead<sizeof(S)>(to, s + k * P.per_row * 8 * sizeof(S) + 16 * i);
+            else if (m == 0) copy_ahead<sizeof(T)>(to, d + k * step + 16 * i);
+            else if (P.d_sum.data) copy_ahead<sizeof(T)>(to, e + k * step + 16 * i);
         });
     };
     const uint64_t stride = (uint64_t)gridDim.x * slots;
