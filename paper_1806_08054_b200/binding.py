@@ -787,7 +787,7 @@ def ecq_act8_product(a, b, out, add=None, status=None, stream=None) -> None:
 
 
 def ecq_act8_set_wait_limit(polls: int = ECQ_WAIT_LIMIT_DEFAULT) -> None:
-    """Polls an in-kernel wait of this process's products makes before it gives up."""
+    """Polls an in-kernel wait of this process's calls on matrices in 8 bits makes before it gives up."""
     if not 0 <= polls < 1 << 32:
         raise ValueError("polls must be below 2^32")
     lib().ecq_act8_set_wait_limit(polls)

@@ -80,16 +80,15 @@ int launch_tiles(Act8Tiles& P, uint64_t rows, uint64_t cols, int plain, bool cod
     }
 }
 
-// ---- norm: threads of a row, a power of two from 32 to 512, and columns of each
+// ---- norm: threads of a row, whole warps up to 512, and vectors of eight columns of each
 struct RowShape { uint32_t per_row, per_cta; int vectors; };
 RowShape row_shape(uint64_t rows, uint64_t cols, int sms) {
-    RowShape s = {32, 256, 1};
     const uint32_t eights = (uint32_t)((cols + 7) / 8);
     // few rows: one vector a thread, and more threads; many: two
-    const uint32_t want = rows * eights <= (uint64_t)sms * 512 ? 1 : 2;
-    while (s.per_row < 512 && s.per_row * want < eights) s.per_row *= 2;
-    while (s.per_row * (uint32_t)s.vectors < eights) s.vectors *= 2;
-    s.per_cta = s.per_row > 256 || rows == 1 ? s.per_row : 256;
+    RowShape s = {0, 0, rows * eights <= (uint64_t)sms * 512 ? 1 : 2};
+    while (512 * (uint32_t)s.vectors < eights) s.vectors *= 2;
+    s.per_row = (eights + 32 * (uint32_t)s.vectors - 1) / (32 * (uint32_t)s.vectors) * 32;
+    s.per_cta = s.per_row > 128 || rows == 1 ? s.per_row : 256 / s.per_row * s.per_row;
     return s;
 }
 
@@ -103,7 +102,7 @@ int launch_norm(Act8Norm& P, const RowShape& s, int sms, cudaStream_t st) {
     // 8192 x 4096 30.5, 26.2, 8192 x 1024 10.6, 9.4, 8192 x 512 6.1, 6.4.  8192 x 4096 in 32 bits with a residual 73, 103 (half
     // the threads have room).
     if constexpr (sizeof(T) == 2 && NV > 1) {
-        if (P.full && need > most && (s.per_row == 512 || (s.per_row >= 64 && !P.y8.data && !P.sum8.data))) {
+        if (P.full && need > most && (s.per_row > 256 || (s.per_row >= 64 && !P.y8.data && !P.sum8.data))) {
             constexpr uint32_t kRoom = 192u * 1024u;                  // what an SM's CTAs take at most
             static std::atomic<bool> done[kMaxDevices];
             auto kernel = act8_norm_ahead_kernel<T, NV>;

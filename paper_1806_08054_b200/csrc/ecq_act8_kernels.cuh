@@ -14,8 +14,10 @@ namespace ecq {
 // ---- storing, restoring and the gated activation: tiles of 128 x 128 -----------------------------
 //
 // Whatever is written in 8 bits transposed has its blocks along the tile's columns, so a CTA has a
-// whole tile: a thread four rows of eight columns, 16 lanes a row's block.  All of it is bound by
-// memory: each input is read once and each output written once.
+// whole tile: a thread four rows of eight columns, 16 lanes a row's block.  Each input is read once and each output written
+// once.  Bound by memory where nothing is written transposed (8192 x 4096 bf16: stored 18.0 us, 5.6 TB/s, restored 18.4, the gate with
+// both inputs kept 46.5, 5.1, its gradient to bf16 44.6, 6.0), else by instructions: 130 for eight entries of a lane stored both ways (27.2
+// us), 314 for the gradient with both results both ways (71.6), at 0.5 to 0.6 a cycle and scheduler.
 
 enum { kActCopy = 0, kActGate = 1, kActGateGrad = 2 };
 constexpr uint32_t kActThreads = 512;
@@ -207,7 +209,10 @@ struct Act8Ring {
     // an SM; 64 registers a thread are too few for a gradient, and for two inputs in 32 bits
     static constexpr uint32_t kCtas = OP == kActGateGrad || (OP == kActGate && sizeof(S) == 4) ? 1 : 2;
     static constexpr uint32_t kRoom = 226u * 1024u / kCtas - (OP == kActGateGrad ? 35u : 27u) * 1024u;
-    static constexpr uint32_t kStages = kRoom / kBytes < 4 ? kRoom / kBytes : 4;
+    // Room for one alone is none ahead, and restoring to 32 bits is bound by its stores (8192 x 4096 with and without, us: gate in 32 bits
+    // 86.3, 61.4; stored from 32 bits 28.9, 25.8; restored to them 40.5, 36.5).
+    static constexpr uint32_t kFit = kRoom / kBytes;
+    static constexpr uint32_t kStages = kFit < 2 || (OP == kActCopy && sizeof(S) == 1 && sizeof(T) == 4) ? 0 : kFit < 4 ? kFit : 4;
     static constexpr uint32_t kSmem = kStages * kBytes + 128;
 };
 
@@ -402,9 +407,10 @@ __global__ void __launch_bounds__(kActThreads, Act8Ring<OP, S, T>::kCtas)
 
 // ---- norm -----------------------------------------------------------------------------------------
 //
-// A row belongs to `per_row` threads (whole warps, a power of two), NV times eight columns each, and
+// A row belongs to `per_row` threads (whole warps), NV times eight columns each, and
 // stays in their registers: every entry is read once.  CTAs go over the rows with the grid's step, so
-// that the weight is read once a CTA.
+// that the weight is read once a CTA.  Bound by memory (8192 x 4096 bf16 to bf16 25.3 us, 5.3 TB/s; with the residual to the sum
+// and 8 bits 41.2, 5.7), with few rows by latency (1 x 4096: 2.7, of which a launch is 2).
 
 struct Act8Norm {
     Act8Mat x, residual, sum, y, y8, sum8;
@@ -453,7 +459,7 @@ __device__ __forceinline__ void act8_weight(const void* w, int dtype, uint32_t c
 }
 
 // Sum over the threads of a row; `part` has room for a CTA's warps twice, taken in turn.
-__device__ __forceinline__ float act8_row_sum(float v, uint32_t per_row, float* part, uint32_t turn) {
+__device__ __forceinline__ float act8_row_sum(float v, uint32_t slot, uint32_t per_row, float* part, uint32_t turn) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = __fadd_rn(v, __shfl_xor_sync(~0u, v, o));
     if (per_row == 32) return v;
@@ -461,7 +467,7 @@ __device__ __forceinline__ float act8_row_sum(float v, uint32_t per_row, float* 
     float* mine = part + (turn & 1) * 32;
     if (lane == 0) mine[warp] = v;
     __syncthreads();
-    v = lane < warps ? mine[(warp & ~(warps - 1)) + lane] : 0.f;
+    v = lane < warps ? mine[slot * warps + lane] : 0.f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = __fadd_rn(v, __shfl_xor_sync(~0u, v, o));
     return v;
@@ -563,7 +569,7 @@ __device__ __forceinline__ void act8_norm_rows(const Act8Norm& P, float* part, u
                 if (!FULL || (real && cols[k])) put8<FULL, 32, T>(P.sum, to + k * step, real ? cols[k] : 0, s[k]);
         }
         if (P.sum8.data) act8_put_row<FULL, NV>(P.sum8, row, t, P.per_row, P.cols, real, s);
-        squares = act8_row_sum(squares, P.per_row, part, turn);
+        squares = act8_row_sum(squares, slot, P.per_row, part, turn);
         const float rstd = __fdiv_rn(1.f, __fsqrt_rn(__fmaf_rn(squares, P.inv_cols, P.eps)));
         if (real && t == 0 && P.rstd) P.rstd[row] = rstd;
         if (!P.y.data && !P.y8.data) continue;
@@ -604,7 +610,9 @@ __global__ void __launch_bounds__(512, NV == 4 ? 1 : 2) act8_norm_ahead_kernel(c
 
 // Its gradient.  With n = s rstd and g = d_out w:  d_x = rstd (g - n mean(g n)) + d_sum, and the weight's
 // gradient is the sum over the rows of d_out n: each thread adds its columns' in registers over the
-// rows that it has, a CTA its rows' at a time, and a second launch the CTAs' sums, all in a fixed order.
+// rows that it has, a CTA its rows' at a time, and a second launch the CTAs' sums, all in a fixed order.  Bound by memory up to 8192
+// columns (8192 x 4096 bf16 from 8 bits 42.3 us, 5.6 TB/s, without the weight's 37.7; 32 bits 71, 6.1); beyond, 32 entries a
+// thread pass its registers (2048 x 12288 74 us, 2.8).
 struct Act8NormGrad {
     Act8Mat s, d_out, d_sum, d_x;
     const void* weight;
@@ -754,7 +762,7 @@ __device__ __forceinline__ void act8_norm_grad_rows(const Act8NormGrad& P, float
                 dot = __fmaf_rn(g[k][i + 1], normed[k][i + 1], dot);
             }
         }
-        const float mean = __fmul_rn(act8_row_sum(dot, P.per_row, part, turn), P.inv_cols);
+        const float mean = __fmul_rn(act8_row_sum(dot, slot, P.per_row, part, turn), P.inv_cols);
         if (!P.d_x.data) continue;
         unsigned char* to = act8_row(P.d_x, row) + at;
         const uint64_t less = pack2(-mean, -mean);

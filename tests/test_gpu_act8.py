@@ -352,7 +352,7 @@ def test_norm(rows, cols, dtype, residual):
     behind_is_left(s8)
 
 
-@pytest.mark.parametrize("rows,cols", [(2600, 1024), (1300, 4096), (700, 5128), (700, 8192), (500, 16384), (6000, 200)])
+@pytest.mark.parametrize("rows,cols", [(2600, 1024), (1300, 4096), (700, 5128), (700, 8192), (500, 16384), (6000, 200), (4000, 520), (1500, 2560)])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("residual", [False, True])
 @pytest.mark.parametrize("coded", [False, True])
@@ -434,6 +434,28 @@ def test_norm_grad(rows, cols, dtype, kept):
     again = torch.empty_like(d_w)
     ecq.ecq_act8_norm_grad(saved, w, rstd, d, None, again, work)
     assert torch.equal(d_w, again)
+
+
+@pytest.mark.parametrize("rows,cols", [(2600, 1024), (700, 4096), (500, 5128), (300, 8192), (300, 16384), (6000, 200), (4000, 520), (1500, 2560)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("kept", [False, True])
+def test_norm_gradient_of_many_aligned_rows(rows, cols, dtype, kept):
+    x = random(rows, cols, 41, 0.3)
+    saved = stored(x) if kept else strided(rows, cols, dtype, cols + 8).copy_(x)
+    s = values(saved) if kept else saved.double()
+    w = random(1, cols, 42)[0].float()
+    d, d_sum = strided(rows, cols, dtype).copy_(random(rows, cols, 43, 0.1)), strided(rows, cols, dtype).copy_(random(rows, cols, 44, 0.1))
+    rstd = (1 / torch.sqrt(s.square().mean(1) + 1e-5)).float()
+    d_x, d_w = strided(rows, cols, dtype), torch.full((cols,), 7.0, device="cuda")
+    work = torch.full((ecq.ecq_act8_norm_grad_workspace_bytes(rows, cols),), 0xFF, dtype=torch.uint8, device="cuda")
+    ecq.ecq_act8_norm_grad(saved, w, rstd, d, d_x, d_w, work, d_sum=d_sum)
+    f = rstd.double()[:, None]
+    n, g = s * f, d.double() * w.double()
+    want = f * (g - n * (g * n).mean(1, keepdim=True)) + d_sum.double()
+    err = f * (g.abs() + n.abs() * (g * n).abs().mean(1, keepdim=True)) * NORM_REL
+    check_plain(d_x, want, err + want.abs() * 2.0 ** -23, "d_x")
+    terms = d.double() * n
+    assert bool(((d_w.double() - terms.sum(0)).abs() <= terms.abs().sum(0) * (rows + 64) * 2.0 ** -24 + 1e-37).all())
 
 
 @pytest.mark.parametrize("rows,cols,stride", [(300, 500, 500), (300, 1001, 1003), (3000, 1024, 1024), (2, 9000, 9001)])
