@@ -10,7 +10,8 @@ LIB = os.path.join(_HERE, "libecq.so")
 SOURCES = ["ecq_api.cu", "ecq_token.cu", "ecq_muon.cu", "ecq_act8.cu", "ecq_product8.cu"]
 HEADERS = ["ecq_common.cuh", "ecq_encode.cuh", "ecq_decode.cuh", "ecq_decode_ring.cuh", "ecq_stats.cuh", "ecq_entropy.cuh",
            "ecq_host.h", "ecq_elem.cuh", "ecq_token.cuh", "ecq_tensor.cuh", "ecq_muon.cuh",
-           "ecq_act8.cuh", "ecq_act8_kernels.cuh", "ecq_act8_host.h", "ecq_product8.cuh"]
+           "ecq_act8.cuh", "ecq_act8_kernels.cuh", "ecq_act8_host.h", "ecq_ring.h",
+           "ecq_product8.cuh"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -6,6 +6,7 @@
 #include <cuda.h>
 
 #include "ecq_act8.cuh"
+#include "ecq_ring.h"
 #include "ecq_tensor.cuh"
 
 namespace ecq {
@@ -103,6 +104,63 @@ __device__ __forceinline__ void cluster_sync_relaxed() { asm volatile("barrier.c
 // scope takes 1400 clocks (8192 x 4096 x 1024: 35.7 us against 30.2).
 __device__ __forceinline__ void leader_arrive_relaxed(uint32_t leader_bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
+}
+
+// What a CTA's warps leave for the case that a wait ran out.
+struct ProdEnd {
+    uint32_t asked[2];                   // loads issued: left, right
+    uint32_t multiplied, committed;      // of the first CTA: steps whose products were issued, commits of accumulators
+    uint32_t halted;                     // a wait ran out in a CTA of the cluster
+};
+__device__ __forceinline__ uint32_t peer_word(const volatile uint32_t& w, uint32_t cta) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer_addr(smem_u32(const_cast<const uint32_t*>(&w)), cta)) : "memory");
+    return v;
+}
+// All threads of the cluster meet at its end; what a CTA whose wait ran out says then is known to all.
+__device__ __forceinline__ bool prod_end(volatile ProdEnd& end, bool stop, uint32_t ctas) {
+    if (threadIdx.x == 0 && stop) {
+        for (uint32_t c = 0; c < ctas; ++c)
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_addr(smem_u32(const_cast<const uint32_t*>(&end.halted)), c)), "r"(1u) : "memory");
+        asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    }
+    cluster_sync_relaxed();
+    return end.halted != 0;
+}
+struct ProdBars {
+    uint32_t full;
+    __device__ void arrive(uint32_t s, uint32_t bytes) { mbar_arrive_expect_tx(full + 8 * s, bytes); }
+    __device__ void forgo(uint32_t s, uint32_t bytes) {
+        asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;" ::"r"(full + 8 * s), "r"(bytes) : "memory");
+    }
+    __device__ void wait(uint32_t s, uint32_t parity) { mbar_wait(full + 8 * s, parity); }
+};
+// After a wait that ran out: every thread of the cluster comes here, and leaves when all that was issued for its CTAs has
+// arrived, which these waits (with the built-in limit) see on the barriers where it is counted: loads,
+// products, sums from other CTAs (`come`, or 0).  Other arrivals from CTAs are over when the cluster has met.
+// Barriers lie as the kernels have them: full and empty ones of the stages, then those that accumulators are committed
+// to in turn.  begin, steps: of K in a tile.  (Inline: a call costs every launch 0.3 us, one token's among them.)
+template <int CG, uint32_t STAGES, uint32_t ACCS, uint32_t RIGHT, uint32_t RIGHT_SCALES>
+__device__ __forceinline__ void prod_settle(const volatile ProdEnd& end, uint32_t full, uint32_t come, uint32_t begin, uint32_t steps) {
+    pair_sync();
+    if (threadIdx.x == 0) {
+        const uint32_t stages = STAGES, empty = full + 8 * stages, acc = empty + 8 * stages, accs = ACCS;
+        const uint32_t rank = CG == 2 ? cta_rank() & 1u : 0, first = cta_rank() - rank;
+        if (rank == 0) {
+            const uint32_t l = end.asked[0], r = end.asked[1];
+            const RingLoads loads = {stages, CG, {kProdBox, RIGHT}, {512, RIGHT_SCALES}, begin, steps,
+                                     {{l, r}, {CG == 2 ? peer_word(end.asked[0], first + 1) : l, CG == 2 ? peer_word(end.asked[1], first + 1) : r}}};
+            ProdBars bars = {full};
+            ring_rest(loads, bars);
+        }
+        const uint32_t m = peer_word(end.multiplied, first), n = peer_word(end.committed, first);
+#pragma unroll 1
+        for (uint32_t j = m > stages ? m - stages : 0; j < m; ++j) mbar_wait(empty + 8 * (j % stages), (j / stages) & 1);
+#pragma unroll 1
+        for (uint32_t j = n > accs ? n - accs : 0; j < n; ++j) mbar_wait(acc + 8 * (j % accs), (j / accs) & 1);
+        if (come) mbar_wait(come, 0);
+    }
+    pair_sync();
 }
 
 // Arrive on a barrier of each of `ctas` when every product issued so far has completed.
@@ -366,6 +424,7 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t stop;
+    __shared__ volatile ProdEnd end;
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u, scales = ring + S::kStages * S::kStage, sums = scales + S::kStages * S::kScales;
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, come = done + 8;
@@ -382,6 +441,7 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
         mbar_init(done, 1);
         mbar_init(come, 1);
         stop = 0;
+        end.halted = 0;
         fence_mbar_init();
         mbar_arrive_expect_tx(come, (parts - 1) * (SWAP ? own_rows : own) * 512u);
     }
@@ -416,11 +476,11 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
                 prod_load<CG>(ring + s * S::kStage + at, map, k * kProdRow, row, bar);
                 if (with) prod_load<CG>(sat + s * S::kScales, smap, 0, group0 + (k >> 2), bar);
             }
+            end.asked[left ? 0 : 1] = it;
             // none of them is in flight when this CTA leaves
             for (uint32_t b = 0; b < S::kStages && b < it; ++b) {
-                const uint32_t last = it - 1 - b, most = stop ? 1u << 12 : kWaitLimit;
-                for (uint32_t n = 0; n < most; ++n)
-                    if (mbar_try_wait(empty + 8 * (last % S::kStages), (last / S::kStages) & 1)) break;
+                const uint32_t last = it - 1 - b;
+                if (!wait_or_stop(empty + 8 * (last % S::kStages), (last / S::kStages) & 1, P.wait_limit, &stop)) break;
             }
         }
         __syncwarp();
@@ -451,6 +511,8 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
             }
             if (CG == 1) umma_commit<1>(done);
             else umma_commit_to(done, both);
+            end.multiplied = it;
+            end.committed = 1;
         }
         __syncwarp();
     }
@@ -588,15 +650,12 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
         tcgen05_before_sync();
     }
     __syncthreads();                                                  // tensor memory is read
-    cluster_sync_relaxed();                                           // nobody sends any more
+    if (__builtin_expect(prod_end(end, stop, ctas), 0)) {             // nobody sends any more
+        prod_settle<CG, S::kStages, 1, S::kRight, 512>(end, full, parts > 1 ? come : 0, k0, k1 - k0);
+        if (tid == 0 && stop && P.status) atomicOr(P.status, kStatusTimeout);
+    }
     tcgen05_after_sync();
     if (warp == 9) tmem_free<CG>(tmem, S::kTmem);
-    // After a wait that ran out, sums, loads and arrivals that this CTA did not wait for may still be on their way
-    // to it; the others have issued their last by now.
-    if (stop) {
-        if (tid == 0 && P.status) atomicOr(P.status, kStatusTimeout);
-        for (const long long since = clock64(); clock64() - since < 20000;) {}
-    }
 }
 
 // ---- tiles of 256 x 256 by pairs of CTAs ------------------------------------------------------------
@@ -986,6 +1045,7 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 3];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t stop;
+    __shared__ volatile ProdEnd end;
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u, epi = ring + S::kStages * S::kStage, scales = epi + S::kEpiWarps * S::kEpi;
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, acc_full = empty + 8 * S::kStages, shared_free = acc_full + 16;
@@ -996,6 +1056,7 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
         mbar_init(acc_full + 8, 1);
         mbar_init(shared_free, 2 * S::kEpiWarps);
         stop = 0;
+        end.halted = 0;
         fence_mbar_init();
     }
     if ((warp == 8 || warp == 10) && elect_one()) {
@@ -1041,11 +1102,11 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
                     }
                 }
             }
+            end.asked[left ? 0 : 1] = it;
             // nothing of this CTA's is in flight when it leaves
             for (uint32_t b = 0; b < S::kStages && b < it; ++b) {
-                const uint32_t last = it - 1 - b, most = stop ? 1u << 12 : kWaitLimit;
-                for (uint32_t n = 0; n < most; ++n)
-                    if (mbar_try_wait(empty + 8 * (last % S::kStages), (last / S::kStages) & 1)) break;
+                const uint32_t last = it - 1 - b;
+                if (!wait_or_stop(empty + 8 * (last % S::kStages), (last / S::kStages) & 1, limit, &stop)) break;
             }
         }
     } else if (warp == 9) {
@@ -1054,7 +1115,7 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
             const uint32_t idesc = P.formats | (1u << 23) | ((256u / 8) << 17) | ((256u / 16) << 24);
             uint32_t it = 0, n = 0, group = 0, sc = 0;
             bool ok = true;
-            for (uint32_t tile = pair; ok && tile < P.tiles; tile += pairs, ++n) {
+            for (uint32_t tile = pair; tile < P.tiles; tile += pairs, ++n) {
                 if (n && !wait_pair_or_stop(shared_free, (n - 1) & 1, limit, &stop)) break;
                 tcgen05_after_sync();
                 const uint32_t d = tmem + (n & 1) * S::kSecond;
@@ -1076,8 +1137,11 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
                     for (uint32_t q = 0; q < steps; ++q) umma_mx8<2>(d, a + 2 * q, b + 2 * q, id, sc, sc + 4, k > 0 || q > 0);
                     umma_commit<2>(empty + 8 * s);
                 }
-                if (ok) umma_commit<2>(acc_full + 8 * (n & 1));
+                if (!ok) break;
+                umma_commit<2>(acc_full + 8 * (n & 1));
             }
+            end.multiplied = it;
+            end.committed = n;
         }
     } else if (warp < S::kEpiWarps) {
         prod_pair_results(P, tmem, epi + warp * S::kEpi, acc_full, shared_free, rank, pair, P.tiles, pairs, &stop);
@@ -1085,12 +1149,11 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
     __syncwarp();
     tcgen05_before_sync();
     __syncthreads();
-    cluster_sync_relaxed();
+    if (__builtin_expect(prod_end(end, stop, 2), 0)) {
+        prod_settle<2, S::kStages, 2, kProdBox, 1024>(end, full, 0, 0, P.steps);
+        if (tid == 0 && stop && P.status) atomicOr(P.status, kStatusTimeout);
+    }
     tcgen05_after_sync();
-    // after a wait that ran out, loads and arrivals for this CTA may still be on their way
-    if (stop)
-        for (const long long since = clock64(); clock64() - since < 20000;) {}
-    if (tid == 0 && stop && P.status) atomicOr(P.status, kStatusTimeout);
     if (warp == 9) tmem_free<2>(tmem, S::kTmem);
 }
 
