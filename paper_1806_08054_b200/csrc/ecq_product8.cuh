@@ -492,9 +492,10 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
             // the right operand's scales begin at its row in their group of 128
             const uint32_t sb_at = 4 + ((right0 & 127u) >> 5);
             uint32_t it = 0, slot = 0;
+            bool ok = true;
             for (uint32_t k = k0; k < k1; ++k, ++it) {
                 const uint32_t s = it % S::kStages;
-                if (!wait_or_stop(full + 8 * s, (it / S::kStages) & 1, P.wait_limit, &stop)) break;
+                if (!wait_or_stop(full + 8 * s, (it / S::kStages) & 1, P.wait_limit, &stop)) { ok = false; break; }
                 tcgen05_after_sync();
                 if (k == k0 || (k & 3) == 0) {
                     // one of three places in turn: what used it last is two whole groups behind, and over
@@ -509,10 +510,13 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
                 if (CG == 1) umma_commit<1>(empty + 8 * s);
                 else umma_commit_to(empty + 8 * s, both);
             }
-            if (CG == 1) umma_commit<1>(done);
-            else umma_commit_to(done, both);
+            // a sum of fewer products is nobody's result: those who wait for it give up too
+            if (ok) {
+                if (CG == 1) umma_commit<1>(done);
+                else umma_commit_to(done, both);
+            }
             end.multiplied = it;
-            end.committed = 1;
+            end.committed = ok;
         }
         __syncwarp();
     }

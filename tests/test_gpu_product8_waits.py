@@ -43,3 +43,25 @@ def test_the_next_call_is_right(m, n, k):
         status.zero_()
         ecq.ecq_act8_product(a, b, d, status=status)
         assert torch.equal(d.double(), want) and status.item() == 0
+
+
+def right_or_nan(m, n, k, dtype=F32, add=False, stride=None):
+    """Every entry is either the exact sum or NaN, and the status says whether there may be any of these."""
+    a, b = whole_numbers(m, k, 1, E4M3), whole_numbers(n, k, 2, E4M3)
+    d, status = strided(m, n, dtype, stride or n), torch.zeros(1, dtype=torch.int32, device="cuda")
+    c = strided(m, n, dtype, stride or n).copy_(torch.randint(-9, 10, (m, n), device="cuda")) if add else None
+    want = (values(a) @ values(b).T + (c.double() if add else 0)).to(dtype)     # one rounding of an exact sum
+    for polls in LIMITS:
+        d.fill_(7.0)
+        status.zero_()
+        with limit(polls):
+            ecq.ecq_act8_product(a, b, d, add=c, status=status)
+        bad = torch.isnan(d)
+        assert torch.equal(d[~bad], want[~bad]), polls
+        assert status.item() == 2 or (status.item() == 0 and not bool(bad.any()))
+
+
+@pytest.mark.parametrize("m,n,k", SIZES[:5] + [(33, 200, 5000), (300, 504, 1000), (512, 4096, 1024)])
+@pytest.mark.parametrize("add", [False, True])
+def test_what_did_not_come_is_nan_where_k_is_shared_out(m, n, k, add):
+    right_or_nan(m, n, k, add=add)
