@@ -753,6 +753,9 @@ __device__ __forceinline__ void prod_pair_results(const Product8& P, uint32_t tm
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) to[i] = prod_fetch4(P, row + 8 * i, col + 4 * piece, row + 8 * i < P.rows ? m : 0);
     };
+    // A warp whose wait ran out waits for no other tile, whose barrier's phase could pass for an older one's, and says of none
+    // any more that it has been read, as that would be taken for another warp's word.
+    bool good = true;
     uint32_t n = 0;
     for (uint32_t tile = begin; tile < end; tile += step, ++n) {
         const uint32_t row0 = tile / P.across * 256u + rank * 128u + quad * 32u, col0 = tile % P.across * 256u + half * 128u;
@@ -814,13 +817,13 @@ __device__ __forceinline__ void prod_pair_results(const Product8& P, uint32_t tm
         };
         const bool reads = P.add && !P.in_place && P.add_wide && P.out.wide && out;
         if (reads) ask(start);
-        const bool good = __all_sync(~0u, wait_or_stop(acc_full + 8 * (n & 1), (n >> 1) & 1, limit, stop));
+        good = good && __all_sync(~0u, wait_or_stop(acc_full + 8 * (n & 1), (n >> 1) & 1, limit, stop));
         tcgen05_after_sync();
         const uint32_t from = tmem + ((quad * 32u) << 16) + (n & 1) * S::kSecond + half * 128u;
         auto release = [&] {
             tcgen05_before_sync();
             __syncwarp();
-            if (lane == 0) leader_arrive_relaxed(leader_addr(shared_free));
+            if (lane == 0 && good) leader_arrive_relaxed(leader_addr(shared_free));
         };
         if (!shares) release();
         if (!out) {

@@ -65,3 +65,10 @@ def right_or_nan(m, n, k, dtype=F32, add=False, stride=None):
 @pytest.mark.parametrize("add", [False, True])
 def test_what_did_not_come_is_nan_where_k_is_shared_out(m, n, k, add):
     right_or_nan(m, n, k, add=add)
+
+
+@pytest.mark.parametrize("m,n,k", SIZES[5:] + [(8192, 4096, 256), (2304, 2048, 31)])
+@pytest.mark.parametrize("dtype,add", [(F32, False), (F32, True), (torch.bfloat16, False)])
+def test_what_did_not_come_is_nan_in_tiles_by_pairs(m, n, k, dtype, add):
+    for _ in range(3):
+        right_or_nan(m, n, k, dtype, add, stride=n + 16)
