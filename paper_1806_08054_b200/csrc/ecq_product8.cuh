@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
                     if (straight && P.add) y[i] = __fadd_rn(y[i], add[i]);
                     if (!all) y[i] = __uint_as_float(0x7FC00000u);
                 }
-                if (straight) {
+                if (straight || !all) {                              // (not turned after a wait that ran out: loads may land there)
                     if (row < P.rows) prod_put16(P, row, col, y);
                     __syncwarp();
                     continue;

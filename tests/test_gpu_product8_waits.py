@@ -72,3 +72,10 @@ def test_what_did_not_come_is_nan_where_k_is_shared_out(m, n, k, add):
 def test_what_did_not_come_is_nan_in_tiles_by_pairs(m, n, k, dtype, add):
     for _ in range(3):
         right_or_nan(m, n, k, dtype, add, stride=n + 16)
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 301, 900), (200, 301, 900), (1024, 1021, 8192), (128, 4095, 4096), (2300, 2101, 300)])
+@pytest.mark.parametrize("dtype,add", [(F32, False), (F32, True), (torch.float16, False), (torch.bfloat16, True)])
+def test_what_did_not_come_is_nan_in_rows_that_begin_anywhere(m, n, k, dtype, add):
+    for _ in range(3):
+        right_or_nan(m, n, k, dtype, add)
