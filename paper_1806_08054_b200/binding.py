@@ -14,7 +14,7 @@ from typing import Sequence
 
 import torch
 
-from .build import LIB
+from .build import LIB, load_marshal
 
 ECQ_OK, ECQ_ERR_ARG, ECQ_ERR_CUDA, ECQ_ERR_NONFINITE, ECQ_ERR_TIMEOUT, ECQ_ERR_ALLOC = range(6)
 ECQ_ERR_TOO_LARGE = 6
@@ -679,10 +679,11 @@ def _vector(t, dtype, n: int, name: str, device: int):
     return t.data_ptr()
 
 
-# The three above as compiled code, where it was built (``csrc/ecq_marshal.cpp``).
+# The three above as compiled code, where it was built for this torch and Python (``csrc/ecq_marshal.cpp``).
 _in_python = (_matrix, _size, _vector)
 try:
-    from ._marshal import matrix as _matrix, size as _size, vector as _vector  # noqa: F811
+    _compiled = load_marshal()
+    _matrix, _size, _vector = _compiled.matrix, _compiled.size, _compiled.vector
 except ImportError:
     pass
 

@@ -30,32 +30,58 @@ def _stale() -> bool:
     return any(os.path.getmtime(p) > t for p in deps)
 
 
-MARSHAL = os.path.join(_HERE, "_marshal.so")
+def marshal_path() -> str:
+    """The binding's compiled marshalling: it has torch's and Python's memory layouts in it, so its name says
+    which ones, and a file that was built for others is not looked at."""
+    import sysconfig
+    import torch
+    return os.path.join(_HERE, "_marshal-torch%s-%s%s" % (torch.__version__, (torch.version.git_version or "")[:8],
+                                                          sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
+
+
+def load_marshal():
+    """The module from that file; ImportError where there is none."""
+    import importlib.util
+    import sys
+    name = os.path.basename(_HERE) + "._marshal"
+    if name not in sys.modules:
+        path = marshal_path()
+        if not os.path.exists(path):
+            raise ImportError("not built: " + path)
+        spec = importlib.util.spec_from_file_location(name, path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        sys.modules[name] = module
+    return sys.modules[name]
 
 
 def build_marshal(force: bool = False) -> bool:
     """Compile the binding's argument marshalling (``csrc/ecq_marshal.cpp``) next to this file.  Where that cannot
     be done (no headers of Python or torch) the binding does the same in Python, a few microseconds a call slower."""
-    source = os.path.join(CSRC, "ecq_marshal.cpp")
-    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= os.path.getmtime(source):
-        return True
-    import sysconfig
-    import torch
-    libs = os.path.join(os.path.dirname(torch.__file__), "lib")      # loaded by torch before this is
-    base = os.path.join(os.path.dirname(torch.__file__), "include")
-    tmp = MARSHAL + ".tmp.%d" % os.getpid()
-    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-I" + sysconfig.get_paths()["include"], "-I" + base,
-           "-I" + os.path.join(base, "torch", "csrc", "api", "include"), source, "-o", tmp,
-           "-L" + libs, "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    source, target = os.path.join(CSRC, "ecq_marshal.cpp"), marshal_path()
+    if force or not os.path.exists(target) or os.path.getmtime(target) < os.path.getmtime(source):
+        import sysconfig
+        import torch
+        libs = os.path.join(os.path.dirname(torch.__file__), "lib")  # loaded by torch before this is
+        base = os.path.join(os.path.dirname(torch.__file__), "include")
+        tmp = target + ".tmp.%d" % os.getpid()
+        cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-I" + sysconfig.get_paths()["include"], "-I" + base,
+               "-I" + os.path.join(base, "torch", "csrc", "api", "include"), source, "-o", tmp,
+               "-L" + libs, "-ltorch_python", "-ltorch_cpu", "-lc10"]
+        try:
+            done = subprocess.run(cmd, capture_output=True, text=True)
+        except OSError as e:
+            print("ecq_marshal.cpp is not built: %s" % e)
+            return False
+        if done.returncode:
+            print("ecq_marshal.cpp is not built:\n" + done.stderr[-2000:])
+            return False
+        os.replace(tmp, target)
     try:
-        done = subprocess.run(cmd, capture_output=True, text=True)
-    except OSError as e:
-        print("ecq_marshal.cpp is not built: %s" % e)
+        load_marshal()
+    except ImportError as e:
+        print("ecq_marshal.cpp is built and not loaded: %s" % e)
         return False
-    if done.returncode:
-        print("ecq_marshal.cpp is not built:\n" + done.stderr[-2000:])
-        return False
-    os.replace(tmp, MARSHAL)
     return True
 
 
