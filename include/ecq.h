@@ -514,7 +514,8 @@ int ecq_muon_status(ecq_muon* plan, void* cuda_stream);
  *              ((r / 128) * ceil(cols / 512) + b / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4
  *            Bytes between those of real blocks are neither written nor used.
  * The scales being powers of two, restored values are exact in bf16 (between 2^-126 and its largest) and storing a matrix in 8 bits again,
- * along its other axis, changes only entries that are 2^-14 (e5m2: 2^-30) of their new block's largest or less.
+ * along its other axis in the same type, changes only entries that are 2^-14 of their new block's largest or less
+ * (e5m2: less than 2^-29, 1.75 2^-30 at most).
  *
  * A matrix of a call, in any type: its first entry, entries from row to row, and the scales (NULL where the
  * type has none).  Plain matrices (ECQ_F32, ECQ_BF16, ECQ_F16) are aligned to one entry only, any

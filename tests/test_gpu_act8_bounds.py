@@ -1,0 +1,36 @@
+"""Bounds that include/ecq.h states for matrices in 8 bits, at the entries that reach them."""
+import pytest
+import torch
+
+import paper_1806_08054_b200 as ecq
+from act8_util import E4M3, E5M2, expand, pair, random, stored, values
+from test_gpu_act8 import check_exactly
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+# The smallest largest entry of a block, unscaled, is the value above half the type's limit: 1.875 2^7 above 1.75 2^7, and 2^15
+# above 1.75 2^14.  The largest entry that may change is the one below the smallest normal number that the type's
+# subnormals (steps of 2^-9, 2^-16) do not have: 1.875 2^-7 and 1.75 2^-15.
+WORST = {E4M3: (1.875 * 2.0 ** 7, 1.875 * 2.0 ** -7, 2.0 ** -14), E5M2: (2.0 ** 15, 1.75 * 2.0 ** -15, 1.75 * 2.0 ** -30)}
+
+
+@pytest.mark.parametrize("kind", [E4M3, E5M2])
+@pytest.mark.parametrize("rows,cols", [(128, 128), (300, 700), (1, 40), (513, 129)])
+def test_storing_again_changes_only_small_entries_of_a_block(kind, rows, cols):
+    torch.manual_seed(rows)
+    sizes = torch.exp2(torch.randint(-40, 1, (rows, cols), device="cuda").double())
+    x = random(rows, cols, 4) * sizes
+    if rows > 1:                                             # both in one block of the transposed matrix, and apart in this one
+        x[:2] = x[:, :1] = 0
+        x[0, 0], x[1, 0] = WORST[kind][:2]
+    p, t = stored(x, kind), pair(cols, rows, kind)
+    ecq.ecq_act8_store(p, None, t)
+    check_exactly(t, values(p).T.contiguous())
+    v, again = values(p).T.contiguous(), values(t)
+    largest = torch.nn.functional.pad(v.abs(), (0, -rows % 128)).view(cols, -1, 128).amax(2)
+    share = v.abs() / expand(largest, rows)
+    changed = v != again
+    assert bool((share[changed] <= WORST[kind][2]).all())
+    if rows > 1:
+        assert bool(changed[0, 1]) and share[0, 1] == WORST[kind][2]
