@@ -3,8 +3,9 @@ import pytest
 import torch
 
 import paper_1806_08054_b200 as ecq
-from act8_util import E4M3, E5M2, expand, pair, random, stored, values
+from act8_util import E4M3, E5M2, check_plain, expand, pair, random, stored, strided, values
 from test_gpu_act8 import check_exactly
+from test_gpu_product8 import bound
 
 pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -34,3 +35,24 @@ def test_storing_again_changes_only_small_entries_of_a_block(kind, rows, cols):
     assert bool((share[changed] <= WORST[kind][2]).all())
     if rows > 1:
         assert bool(changed[0, 1]) and share[0, 1] == WORST[kind][2]
+
+
+@pytest.mark.parametrize("m,n,k", [(128, 128, 256), (128, 128, 384), (1024, 1024, 1280), (200, 300, 900), (1, 300, 700), (40, 300, 4096)])
+def test_a_products_bits_repeat_and_agree_between_calls_that_differ(m, n, k):
+    """K is shared out by how d and c lie too: alone, added from elsewhere, in place, and in rows that begin anywhere agree
+    to the sums' rounding (and the addition's and the result's), each repeats its own bits."""
+    a, b = stored(random(m, k, 1)), stored(random(n, k, 2))
+    c = random(m, n, 3).float()
+    want, err = values(a) @ values(b).T, bound(a, b, k)
+    total = want + c.double()
+    for stride in (n, n + 1):
+        for add in (None, "apart", "in place"):
+            got = []
+            for _ in range(3):
+                d = strided(m, n, F32, stride)
+                if add == "in place":
+                    d.copy_(c)
+                ecq.ecq_act8_product(a, b, d, add=None if add is None else d if add == "in place" else c)
+                got.append(d)
+            assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+            check_plain(got[0], want if add is None else total, err + (0 if add is None else total.abs() * 2.0 ** -24))
