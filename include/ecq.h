@@ -553,7 +553,11 @@ int ecq_act8_load(uint64_t rows, uint64_t cols, const ecq_act8_matrix* q, const 
  *   gate8, up8   gate and up in 8 bits, for the backward pass, or NULL
  * and its gradient, from gate and up as they were given or as they were kept:
  *   d_gate = d_out u sigmoid(g) (1 + g (1 - sigmoid(g)))      d_up = d_out g sigmoid(g)
- * each plain, in 8 bits or in 8 bits transposed, or several of these.  Arithmetic is fp32; entries of gate at -inf give NaN.
+ * each plain, in 8 bits or in 8 bits transposed, or several of these.  Arithmetic is fp32, with
+ *   - a sigmoid below 2^-126 taken as 0;
+ *   - where no plain matrix of the call is in 32 bits, a sigmoid whose argument is rounded once more: off by up to |g| 2^-23 of itself,
+ *     far below what 16 or 8 bits show.
+ * Entries of gate at -inf give NaN; at +inf d_gate is NaN, from 1 + inf 0, and out and d_up follow the formulas.
  */
 int ecq_act8_gate(uint64_t rows, uint64_t cols, const ecq_act8_matrix* gate, const ecq_act8_matrix* up,
                   const ecq_act8_matrix* out, const ecq_act8_matrix* out8, const ecq_act8_matrix* out8_t,
@@ -569,10 +573,11 @@ int ecq_act8_gate_grad(uint64_t rows, uint64_t cols, const ecq_act8_matrix* gate
  *   rstd = 1 / sqrt(mean_j s_j^2 + eps)               eps >= 0
  *   y_j = s_j rstd w_j                                weight [cols] of weight_dtype, or NULL: 1
  * in fp32 throughout (s is not rounded before it is normed; squares are added in fp32, so rows whose
- * sum of squares is beyond its range give zeros, as s rstd does there).
+ * sum of squares is beyond its range give zeros, as s rstd does there; squares of entries below 2^-63
+ * lose bits and below 2^-75 are zeros, which shows where eps is that small too).
  *   sum, out     s and y, plain, or NULL; sum8, out8: in 8 bits, or NULL; rstd [rows] or NULL
  *   cols         at most ECQ_ACT8_NORM_MAX_COLS
- * A row of zeros with eps == 0 gives NaN.
+ * A row of zeros, or of entries whose squares are, with eps == 0 has rstd = inf: zeros give NaN, the others infinities.
  *
  * Its gradient, from sum (plain, or in 8 bits as sum8 kept it) and rstd, with n = s rstd and g = d_out w:
  *   d_x = rstd (g - n mean_j(g_j n_j)) + d_sum        (d_sum, the gradient that reaches s by itself, or NULL)

@@ -56,3 +56,31 @@ def test_a_products_bits_repeat_and_agree_between_calls_that_differ(m, n, k):
                 got.append(d)
             assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
             check_plain(got[0], want if add is None else total, err + (0 if add is None else total.abs() * 2.0 ** -24))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [1, 300])
+def test_gate_at_the_ends_of_its_range(dtype, rows):
+    inf, nan, top = float("inf"), float("nan"), torch.finfo(dtype).max
+    g = torch.tensor([inf, -inf, top, -top, 200.0, -200.0, 0.0, inf], device="cuda").repeat(rows, 1).to(dtype)
+    u = torch.tensor([2.0, 2.0, 0.5, 2.0, 2.0, 2.0, 2.0, 0.0], device="cuda").repeat(rows, 1).to(dtype)
+    d = torch.full_like(g, 0.5)
+    out, d_gate, d_up = (torch.empty_like(g) for _ in range(3))
+    ecq.ecq_act8_gate(g, u, out)
+    ecq.ecq_act8_gate_grad(g, u, d, d_gate, d_up)
+    half = (torch.tensor(top, dtype=torch.float64) / 2).item()
+    for got, want in ((out, [inf, nan, half, 0, 400, 0, 0, nan]), (d_gate, [nan, nan, 0.25, 0, 1, 0, 0.5, nan]),
+                      (d_up, [inf, nan, half, 0, 100, 0, 0, inf])):
+        assert torch.equal(got.double().nan_to_num(nan=7.0, posinf=8.0), torch.tensor(want, device="cuda").double().nan_to_num(nan=7.0, posinf=8.0)
+                           .to(dtype).double().repeat(rows, 1))
+
+
+def test_norm_of_rows_whose_squares_underflow():
+    x = torch.zeros(3, 40, device="cuda")
+    x[1], x[2] = 1e-30, 1e-10
+    out, rstd = torch.empty_like(x), torch.empty(3, device="cuda")
+    ecq.ecq_act8_norm(x, eps=0.0, out=out, rstd=rstd)
+    assert bool(torch.isnan(out[0]).all()) and bool(torch.isinf(out[1]).all()) and bool((out[2] - 1).abs().max() < 1e-6)
+    assert bool(torch.isinf(rstd[:2]).all())
+    ecq.ecq_act8_norm(x, eps=1e-6, out=out)
+    check_plain(out, x.double() / torch.sqrt(x.double().square().mean(1, keepdim=True) + 1e-6), x.double().abs() * 1e3 * 2.0 ** -22)
