@@ -3,9 +3,9 @@ import pytest
 import torch
 
 import paper_1806_08054_b200 as ecq
-from act8_util import E4M3, E5M2, check_plain, expand, pair, random, stored, strided, values
+from act8_util import E4M3, E5M2, check_plain, expand, pair, random, scale_places, stored, strided, values
 from test_gpu_act8 import check_exactly
-from test_gpu_product8 import bound
+from test_gpu_product8 import bound, whole_numbers
 
 pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -84,3 +84,42 @@ def test_norm_of_rows_whose_squares_underflow():
     assert bool(torch.isinf(rstd[:2]).all())
     ecq.ecq_act8_norm(x, eps=1e-6, out=out)
     check_plain(out, x.double() / torch.sqrt(x.double().square().mean(1, keepdim=True) + 1e-6), x.double().abs() * 1e3 * 2.0 ** -22)
+
+
+ROWS = [(300, 400), (256, 4096), (5, 130)]                       # one row of A: K within a warp's step, shared out, and short
+
+
+@pytest.mark.parametrize("n,k", ROWS)
+@pytest.mark.parametrize("low,high", [(1, 253), (0, 254), (254, 0), (127, 127), (100, 1), (254, 254), (0, 0), (1, 0)])
+def test_far_scales_of_one_row(n, k, low, high):
+    """Scales at both ends of their range, which may cancel, overflow or underflow in the product.  Sums of whole numbers times
+    one power of two are exact in 32 bits as long as they are normal.  Below that, each sixteen products' sum is rounded once,
+    to a multiple of 2^-149 (by 2^-150 at most), and adding such multiples rounds nothing: ceil(k / 16) 2^-150 in all.  Where
+    the magnitudes together pass the range of 32 bits, sums of what is left of them may be anything."""
+    a, b = whole_numbers(1, k, 1, E4M3), whole_numbers(n, k, 2, E4M3)
+    a[1][scale_places(1, k)] = low
+    b[1][scale_places(n, k)] = high
+    d = strided(1, n, F32)
+    ecq.ecq_act8_product(a, b, d)
+    want, size = values(a) @ values(b).T, values(a).abs() @ values(b).abs().T
+    inside = size <= torch.finfo(F32).max
+    assert bool(((d.double() - want).abs() <= -(-k // 16) * 2.0 ** -150)[inside].all())
+    normal = inside & (size >= 2.0 ** -100)                       # units of these are far above 2^-149
+    assert torch.equal(d[normal].double(), want[normal])
+    assert not bool(torch.isfinite(d[want.abs() > torch.finfo(F32).max]).any())
+
+
+@pytest.mark.parametrize("n,k", ROWS)
+def test_nan_blocks_of_one_row(n, k):
+    x, y = random(1, k, 1).float(), random(n, k, 2).float()
+    y[n - 2, k - 1], y[1, 0] = float("nan"), float("inf")
+    a, b = stored(x.double()), stored(y.double())
+    c = random(1, n, 3).float()
+    for add in (None, c):
+        d = strided(1, n, F32)
+        ecq.ecq_act8_product(a, b, d, add=add)
+        bad = torch.isnan(d)
+        assert bool(bad[0, 1] and bad[0, n - 2]) and int(bad.sum()) == 2
+    x[0, k - 1] = float("nan")
+    ecq.ecq_act8_product(stored(x.double()), b, d)
+    assert bool(torch.isnan(d).all())
