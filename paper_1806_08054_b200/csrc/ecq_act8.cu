@@ -43,7 +43,16 @@ int launch_tiles(Act8Tiles& P, cudaStream_t st) {
         static std::atomic<bool> done[kMaxDevices];
         auto kernel = act8_tiles_kernel<OP, S, T>;
         Act8Maps maps = {};
-        if (P.wide && P.rows >= 128 && P.cols >= 128 && P.tiles >= (R::kCtas == 1 ? 2 : 4) * ctas) {
+        // With room for one alone: where results are in 8 bits, two or more, and work is long: transposed, or four tiles a CTA.  Without and
+        // with, in us, 8192 x 4096 and 8192 x 1024 (3.5 tiles a CTA): gradient from bf16, both results both ways 82.5, 66.7; 25.0, 22.8, in 8
+        // bits 55.0, 49.3; 17.6, 17.9, to bf16 54.5, 55.5; 16.6, 18.9, to bf16 and transposed 78.2, 75.2; 23.4, 23.6; gradient to 32 bits from
+        // 8, both ways 92.2, 79.6; 28.6, 26.1, plain 95.9, 95.4; 28.4, 31.6; gate in 32 bits, inputs kept 73.6, 67.6; 23.7, 23.8, and
+        // transposed 89.9, 75.5; 27.6, 26.0, to 8 bits alone 55.6, 65.9; 18.4, 21.2.
+        const int turned = (P.qt[0].data != nullptr) + (P.qt[1].data != nullptr);
+        const int coded = turned + (P.q[0].data != nullptr) + (P.q[1].data != nullptr) + (P.kept[0].data != nullptr) + (P.kept[1].data != nullptr);
+        const bool ahead = R::kStages > 1 || (coded >= 2 && !P.plain[0].data && !P.plain[1].data);
+        const uint32_t least = R::kCtas == 1 && (R::kStages > 1 || turned) ? 2 : 4;
+        if (ahead && P.wide && P.rows >= 128 && P.cols >= 128 && P.tiles >= least * ctas) {
             if (!tensor_map_encoder() || !tile_map(&maps.of[0], P.in[0], P.rows, P.cols) ||
                 (OP != kActCopy && !tile_map(&maps.of[1], P.in[1], P.rows, P.cols)) ||
                 (OP == kActGateGrad && !tile_map(&maps.of[2], P.d, P.rows, P.cols)) ||

@@ -209,10 +209,10 @@ struct Act8Ring {
     // an SM; 64 registers a thread are too few for a gradient, and for two inputs in 32 bits
     static constexpr uint32_t kCtas = OP == kActGateGrad || (OP == kActGate && sizeof(S) == 4) ? 1 : 2;
     static constexpr uint32_t kRoom = 226u * 1024u / kCtas - (OP == kActGateGrad ? 35u : 27u) * 1024u;
-    // Room for one alone is none ahead, and restoring to 32 bits is bound by its stores (8192 x 4096 with and without, us: gate in 32 bits
-    // 86.3, 61.4; stored from 32 bits 28.9, 25.8; restored to them 40.5, 36.5).
+    // Restoring to 32 bits is bound by its stores (8192 x 4096 with and without, us: 40.5, 36.5).  Room for one alone, which comes while
+    // the one before it is worked on, is used by launches whose work is long (`launch_tiles`); never of two CTAs an SM.
     static constexpr uint32_t kFit = kRoom / kBytes;
-    static constexpr uint32_t kStages = kFit < 2 || (OP == kActCopy && sizeof(S) == 1 && sizeof(T) == 4) ? 0 : kFit < 4 ? kFit : 4;
+    static constexpr uint32_t kStages = OP == kActCopy && sizeof(S) == 1 && sizeof(T) == 4 ? 0 : kFit >= 2 ? kFit < 4 ? kFit : 4 : kCtas == 1 ? kFit : 0;
     static constexpr uint32_t kSmem = kStages * kBytes + 128;
 };
 
