@@ -564,7 +564,8 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
     extern __shared__ unsigned char raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 6 + 4 * kMuonQueue + (KS ? 8 : 0)];
     __shared__ uint32_t tmem_slot, queue[kMuonQueue], passed[kMuonQueue];
-    __shared__ volatile uint32_t stop;
+    __shared__ volatile uint32_t stop, sent[4];                       // sent: sums, by a warp's rows
+    __shared__ volatile RingEnd end;
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages;
@@ -593,6 +594,9 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
         if (KS)
             for (uint32_t i = 0; i < 8; ++i) mbar_init(share_full + 8 * i, 1);
         stop = 0;
+        end.halted = 0;
+        if (KS)
+            for (uint32_t i = 0; i < 4; ++i) sent[i] = 0;
         fence_mbar_init();
     }
     if (warp == S::kEpiWarps + 1) tmem_alloc<CG>(smem_u32(&tmem_slot), S::kTmemCols);
@@ -716,12 +720,11 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                     }
                 }
             }
+            end.asked[first ? 0 : 1] = it;
             // nothing of this CTA's is in flight when it leaves: every stage's last load was consumed
-            // (or, where a wait ran out and nobody consumes them any more, has had time to land)
             for (uint32_t b = 0; b < S::kStages && b < it; ++b) {
-                const uint32_t last = it - 1 - b, most = stop ? 1u << 12 : kWaitLimit;
-                for (uint32_t n = 0; n < most; ++n)
-                    if (mbar_try_wait(empty + 8 * (last % S::kStages), (last / S::kStages) & 1)) break;
+                const uint32_t last = it - 1 - b;
+                if (!wait_or_stop(empty + 8 * (last % S::kStages), (last / S::kStages) & 1, limit, &stop)) break;
             }
         }
     } else if (warp == S::kEpiWarps + 1) {
@@ -778,6 +781,8 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                     }
                 }
             }
+            end.multiplied = it;
+            end.committed = acc;
         }
     } else if (warp == S::kEpiWarps + 2) {
         // ---- signals -----------------------------------------------------------------------------
@@ -921,6 +926,7 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
                 for (uint32_t c = 0; c < 8; ++c)
                     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1,%2,%3,%4}, [%5];"
                                  ::"r"(to + c * 512), "f"(y[4 * c]), "f"(y[4 * c + 1]), "f"(y[4 * c + 2]), "f"(y[4 * c + 3]), "r"(bar) : "memory");
+                if (lane == 0) sent[quad] = n + 1;
                 continue;
             }
 
@@ -1108,13 +1114,18 @@ __global__ void __launch_bounds__(MuonShape<CG, TN, SPLIT, KS>::kThreads, 1) muo
     __syncwarp();
     tcgen05_before_sync();
     __syncthreads();
-    if (kJoint) pair_sync();
+    if (__builtin_expect(kJoint ? ring_end<true>(end, stop, 2) : stop != 0, 0)) {
+        const RingLoads loads = {S::kStages, CG, {S::kHalves * S::kBytesA, S::kHalves * S::kBytesB}, {0, 0}, 0, 1, {}};
+        // and the other's sums: at most the last tile's are on their way
+        ring_settle<CG, 2>(end, loads, full, [&] {
+            for (uint32_t i = 0; KS && i < 4; ++i) {
+                const uint32_t n = peer_word(sent[i], cta ^ 1);
+                if (n) mbar_wait(share_full + 8 * i, (n - 1) & 1);
+            }
+        });
+        if (tid == 0 && stop) atomicOr(P.status, kStatusTimeout);
+    }
     tcgen05_after_sync();
-    // After a wait that ran out, partial sums and arrivals that this CTA did not wait for may still be on
-    // their way to it from the other one, which has issued its last by now: 20,000 clocks to land.
-    if (kJoint && stop)
-        for (const long long from = clock64(); clock64() - from < 20000;) {}
-    if (tid == 0 && stop) atomicOr(P.status, kStatusTimeout);
     if (warp == S::kEpiWarps + 1) tmem_free<CG>(tmem, S::kTmemCols);
 }
 

@@ -6,7 +6,6 @@
 #include <cuda.h>
 
 #include "ecq_act8.cuh"
-#include "ecq_ring.h"
 #include "ecq_tensor.cuh"
 
 namespace ecq {
@@ -96,71 +95,10 @@ __device__ __forceinline__ void send16(uint32_t to, const float* v, uint32_t bar
                  : "memory");
 }
 
-// All CTAs of a cluster, where no memory is handed over but barriers that were made visible by their own fence: a release would
-// wait for results on their way to memory.
-__device__ __forceinline__ void cluster_sync_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;\n\tbarrier.cluster.wait;" ::: "memory"); }
-
 // Arrive on the first CTA's barrier where no memory is handed over (tensor memory that has been read): a release at cluster
 // scope takes 1400 clocks (8192 x 4096 x 1024: 35.7 us against 30.2).
 __device__ __forceinline__ void leader_arrive_relaxed(uint32_t leader_bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
-}
-
-// What a CTA's warps leave for the case that a wait ran out.
-struct ProdEnd {
-    uint32_t asked[2];                   // loads issued: left, right
-    uint32_t multiplied, committed;      // of the first CTA: steps whose products were issued, commits of accumulators
-    uint32_t halted;                     // a wait ran out in a CTA of the cluster
-};
-__device__ __forceinline__ uint32_t peer_word(const volatile uint32_t& w, uint32_t cta) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer_addr(smem_u32(const_cast<const uint32_t*>(&w)), cta)) : "memory");
-    return v;
-}
-// All threads of the cluster meet at its end; what a CTA whose wait ran out says then is known to all.
-__device__ __forceinline__ bool prod_end(volatile ProdEnd& end, bool stop, uint32_t ctas) {
-    if (threadIdx.x == 0 && stop) {
-        for (uint32_t c = 0; c < ctas; ++c)
-            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_addr(smem_u32(const_cast<const uint32_t*>(&end.halted)), c)), "r"(1u) : "memory");
-        asm volatile("fence.acq_rel.cluster;" ::: "memory");
-    }
-    cluster_sync_relaxed();
-    return end.halted != 0;
-}
-struct ProdBars {
-    uint32_t full;
-    __device__ void arrive(uint32_t s, uint32_t bytes) { mbar_arrive_expect_tx(full + 8 * s, bytes); }
-    __device__ void forgo(uint32_t s, uint32_t bytes) {
-        asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;" ::"r"(full + 8 * s), "r"(bytes) : "memory");
-    }
-    __device__ void wait(uint32_t s, uint32_t parity) { mbar_wait(full + 8 * s, parity); }
-};
-// After a wait that ran out: every thread of the cluster comes here, and leaves when all that was issued for its CTAs has
-// arrived, which these waits (with the built-in limit) see on the barriers where it is counted: loads,
-// products, sums from other CTAs (`come`, or 0).  Other arrivals from CTAs are over when the cluster has met.
-// Barriers lie as the kernels have them: full and empty ones of the stages, then those that accumulators are committed
-// to in turn.  begin, steps: of K in a tile.  (Inline: a call costs every launch 0.3 us, one token's among them.)
-template <int CG, uint32_t STAGES, uint32_t ACCS, uint32_t RIGHT, uint32_t RIGHT_SCALES>
-__device__ __forceinline__ void prod_settle(const volatile ProdEnd& end, uint32_t full, uint32_t come, uint32_t begin, uint32_t steps) {
-    pair_sync();
-    if (threadIdx.x == 0) {
-        const uint32_t stages = STAGES, empty = full + 8 * stages, acc = empty + 8 * stages, accs = ACCS;
-        const uint32_t rank = CG == 2 ? cta_rank() & 1u : 0, first = cta_rank() - rank;
-        if (rank == 0) {
-            const uint32_t l = end.asked[0], r = end.asked[1];
-            const RingLoads loads = {stages, CG, {kProdBox, RIGHT}, {512, RIGHT_SCALES}, begin, steps,
-                                     {{l, r}, {CG == 2 ? peer_word(end.asked[0], first + 1) : l, CG == 2 ? peer_word(end.asked[1], first + 1) : r}}};
-            ProdBars bars = {full};
-            ring_rest(loads, bars);
-        }
-        const uint32_t m = peer_word(end.multiplied, first), n = peer_word(end.committed, first);
-#pragma unroll 1
-        for (uint32_t j = m > stages ? m - stages : 0; j < m; ++j) mbar_wait(empty + 8 * (j % stages), (j / stages) & 1);
-#pragma unroll 1
-        for (uint32_t j = n > accs ? n - accs : 0; j < n; ++j) mbar_wait(acc + 8 * (j % accs), (j / accs) & 1);
-        if (come) mbar_wait(come, 0);
-    }
-    pair_sync();
 }
 
 // Arrive on a barrier of each of `ctas` when every product issued so far has completed.
@@ -424,7 +362,7 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t stop;
-    __shared__ volatile ProdEnd end;
+    __shared__ volatile RingEnd end;
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u, scales = ring + S::kStages * S::kStage, sums = scales + S::kStages * S::kScales;
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, come = done + 8;
@@ -654,8 +592,9 @@ __global__ void __launch_bounds__(ProdPart<CG, TN, SWAP>::kThreads, 1) act8_prod
         tcgen05_before_sync();
     }
     __syncthreads();                                                  // tensor memory is read
-    if (__builtin_expect(prod_end(end, stop, ctas), 0)) {             // nobody sends any more
-        prod_settle<CG, S::kStages, 1, S::kRight, 512>(end, full, parts > 1 ? come : 0, k0, k1 - k0);
+    if (__builtin_expect(ring_end<false>(end, stop, ctas), 0)) {      // nobody sends any more
+        const RingLoads loads = {S::kStages, CG, {kProdBox, S::kRight}, {512, 512}, k0, k1 - k0, {}};
+        ring_settle<CG, 1>(end, loads, full, [&] { if (parts > 1) mbar_wait(come, 0); });   // and the sums that others sent
         if (tid == 0 && stop && P.status) atomicOr(P.status, kStatusTimeout);
     }
     tcgen05_after_sync();
@@ -1052,7 +991,7 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 3];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile uint32_t stop;
-    __shared__ volatile ProdEnd end;
+    __shared__ volatile RingEnd end;
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(raw) + 1023u) & ~1023u, epi = ring + S::kStages * S::kStage, scales = epi + S::kEpiWarps * S::kEpi;
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, acc_full = empty + 8 * S::kStages, shared_free = acc_full + 16;
@@ -1156,8 +1095,9 @@ __global__ void __launch_bounds__(ProdPair::kThreads, 1) act8_product_pair_kerne
     __syncwarp();
     tcgen05_before_sync();
     __syncthreads();
-    if (__builtin_expect(prod_end(end, stop, 2), 0)) {
-        prod_settle<2, S::kStages, 2, kProdBox, 1024>(end, full, 0, 0, P.steps);
+    if (__builtin_expect(ring_end<false>(end, stop, 2), 0)) {
+        const RingLoads loads = {S::kStages, 2, {kProdBox, kProdBox}, {512, 1024}, 0, P.steps, {}};
+        ring_settle<2, 2>(end, loads, full, [] {});
         if (tid == 0 && stop && P.status) atomicOr(P.status, kStatusTimeout);
     }
     tcgen05_after_sync();

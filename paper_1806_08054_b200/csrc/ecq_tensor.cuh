@@ -1,10 +1,11 @@
-// What kernels that use the tensor cores (tcgen05) share: descriptors, tensor memory, waits that give up,
-// pairs of CTAs.
+// What kernels that use the tensor cores (tcgen05) share: descriptors, tensor memory, pairs of CTAs, waits that give up,
+// and how a kernel leaves after one.
 #pragma once
 
 #include <cstdint>
 
 #include "ecq_common.cuh"
+#include "ecq_ring.h"
 
 namespace ecq {
 
@@ -92,6 +93,10 @@ __device__ __forceinline__ void leader_arrive(uint32_t leader_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_bar) : "memory");
 }
 
+// All CTAs of a cluster, where no memory is handed over but barriers that were made visible by their own fence: a release would
+// wait for results on their way to memory.
+__device__ __forceinline__ void cluster_sync_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;\n\tbarrier.cluster.wait;" ::: "memory"); }
+
 // Waits that give up: the limit is per wait, and one that ran out ends all others soon.
 __device__ __forceinline__ bool wait_or_stop(uint32_t bar, uint32_t parity, uint32_t limit, volatile uint32_t* stop) {
     for (uint32_t it = 0; it < limit; ++it) {
@@ -114,6 +119,66 @@ __device__ __forceinline__ bool wait_pair_or_stop(uint32_t bar, uint32_t parity,
     *stop = 1;
     return false;
 }
+// What a CTA's warps leave for the case that a wait ran out.
+struct RingEnd {
+    uint32_t asked[2];                   // loads issued: left, right
+    uint32_t multiplied, committed;      // of a pair's first CTA: steps whose products were issued, commits of accumulators
+    uint32_t halted;                     // a wait ran out in a CTA of the cluster
+};
+__device__ __forceinline__ uint32_t peer_word(const volatile uint32_t& w, uint32_t cta) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer_addr(smem_u32(const_cast<const uint32_t*>(&w)), cta)) : "memory");
+    return v;
+}
+// All threads of the cluster meet at its end; what a CTA whose wait ran out says then is known to all.  RELEASE: where
+// arrivals on other CTAs' barriers may be on their way that nobody waits for.
+template <bool RELEASE>
+__device__ __forceinline__ bool ring_end(volatile RingEnd& end, bool stop, uint32_t ctas) {
+    if (threadIdx.x == 0 && stop) {
+        for (uint32_t c = 0; c < ctas; ++c)
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_addr(smem_u32(const_cast<const uint32_t*>(&end.halted)), c)), "r"(1u) : "memory");
+        asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    }
+    if (RELEASE) pair_sync();
+    else cluster_sync_relaxed();
+    return end.halted != 0;
+}
+struct RingBars {
+    uint32_t full;
+    __device__ void arrive(uint32_t s, uint32_t bytes) { mbar_arrive_expect_tx(full + 8 * s, bytes); }
+    __device__ void forgo(uint32_t s, uint32_t bytes) {
+        asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;" ::"r"(full + 8 * s), "r"(bytes) : "memory");
+    }
+    __device__ void wait(uint32_t s, uint32_t parity) { mbar_wait(full + 8 * s, parity); }
+};
+// After a wait that ran out: every thread of the cluster comes here, and leaves when all that was issued for its CTAs has
+// arrived, which these waits (with the built-in limit) see on the barriers where it is counted: loads, products,
+// and what `others` waits for.  Other arrivals from CTAs are over when the cluster has met.  Barriers lie as the kernels
+// have them: full and empty ones of the stages, then ACCS that accumulators are committed to in turn.
+// CG CTAs share a ring.  (Inline: a call costs every launch 0.3 us, one token's product among them.)
+template <int CG, uint32_t ACCS, typename Others>
+__device__ __forceinline__ void ring_settle(const volatile RingEnd& end, const RingLoads& issued, uint32_t full, Others others) {
+    pair_sync();
+    if (threadIdx.x == 0) {
+        const uint32_t stages = issued.stages, empty = full + 8 * stages, acc = empty + 8 * stages;
+        const uint32_t rank = CG == 2 ? cta_rank() & 1u : 0, first = cta_rank() - rank;
+        if (rank == 0) {
+            const uint32_t l = end.asked[0], r = end.asked[1];
+            const RingLoads loads = {stages, CG, {issued.bytes[0], issued.bytes[1]}, {issued.more[0], issued.more[1]}, issued.begin, issued.steps,
+                                     {{l, r}, {CG == 2 ? peer_word(end.asked[0], first + 1) : l, CG == 2 ? peer_word(end.asked[1], first + 1) : r}}};
+            RingBars bars = {full};
+            ring_rest(loads, bars);
+        }
+        const uint32_t m = peer_word(end.multiplied, first), n = peer_word(end.committed, first);
+#pragma unroll 1
+        for (uint32_t j = m > stages ? m - stages : 0; j < m; ++j) mbar_wait(empty + 8 * (j % stages), (j / stages) & 1);
+#pragma unroll 1
+        for (uint32_t j = n > ACCS ? n - ACCS : 0; j < n; ++j) mbar_wait(acc + 8 * (j % ACCS), (j / ACCS) & 1);
+        others();
+    }
+    pair_sync();
+}
+
 __device__ __forceinline__ uint4 lds16(uint32_t addr) {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
