@@ -759,10 +759,12 @@ __device__ __forceinline__ void prod_pair_results(const Product8& P, uint32_t tm
         good = good && __all_sync(~0u, wait_or_stop(acc_full + 8 * (n & 1), (n >> 1) & 1, limit, stop));
         tcgen05_after_sync();
         const uint32_t from = tmem + ((quad * 32u) << 16) + (n & 1) * S::kSecond + half * 128u;
+        // nobody waits for the last tile's: the first CTA could be gone when the word comes
+        const bool tells = good && tile + step < end;
         auto release = [&] {
             tcgen05_before_sync();
             __syncwarp();
-            if (lane == 0 && good) leader_arrive_relaxed(leader_addr(shared_free));
+            if (lane == 0 && tells) leader_arrive_relaxed(leader_addr(shared_free));
         };
         if (!shares) release();
         if (!out) {

@@ -123,3 +123,15 @@ def test_nan_blocks_of_one_row(n, k):
     x[0, k - 1] = float("nan")
     ecq.ecq_act8_product(stored(x.double()), b, d)
     assert bool(torch.isnan(d).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(2600, 2304, 31), (4196, 4096, 128), (2304, 2148, 200)])
+@pytest.mark.parametrize("add", [False, True])
+def test_pairs_of_ctas_of_which_one_has_nothing_to_write(m, n, k, add):
+    """The last row or column of tiles is less than half inside; calls on top of each other."""
+    a, b = whole_numbers(m, k, 1, E4M3), whole_numbers(n, k, 2, E4M3)
+    want = values(a) @ values(b).T
+    d = torch.zeros(m, n, device="cuda")
+    for calls in range(1, 31):
+        ecq.ecq_act8_product(a, b, d, add=d if add else None)
+    assert torch.equal(d.double(), want * (calls if add else 1))
