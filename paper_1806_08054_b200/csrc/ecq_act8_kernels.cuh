@@ -16,8 +16,9 @@ namespace ecq {
 // Whatever is written in 8 bits transposed has its blocks along the tile's columns, so a CTA has a
 // whole tile: a thread four rows of eight columns, 16 lanes a row's block.  Each input is read once and each output written
 // once.  Bound by memory where nothing is written transposed (8192 x 4096 bf16: stored 18.0 us, 5.6 TB/s, restored 18.4, the gate with
-// both inputs kept 46.5, 5.1, its gradient to bf16 44.6, 6.0), else by instructions: 130 for eight entries of a lane stored both ways (27.2
-// us), 314 for the gradient with both results both ways (71.6), at 0.5 to 0.6 a cycle and scheduler.
+// both inputs kept 45.2, 5.2, its gradient to bf16 from 8 bits 44.6, 6.0, from bf16 54.5, 6.2), else by instructions: 130 for eight entries of
+// a lane stored both ways (27.2 us), 314 for the gradient with both results both ways from 8 bits (71.3), 271 from bf16 (66.7), at 0.4 to
+// 0.6 a cycle and scheduler.  The gate's 64 registers, for two CTAs an SM, keep 84 to 256 bytes a thread in local memory.
 
 enum { kActCopy = 0, kActGate = 1, kActGateGrad = 2 };
 constexpr uint32_t kActThreads = 512;
@@ -612,7 +613,7 @@ __global__ void __launch_bounds__(512, NV == 4 ? 1 : 2) act8_norm_ahead_kernel(c
 // gradient is the sum over the rows of d_out n: each thread adds its columns' in registers over the
 // rows that it has, a CTA its rows' at a time, and a second launch the CTAs' sums, all in a fixed order.  Bound by memory up to 8192
 // columns (8192 x 4096 bf16 from 8 bits 42.3 us, 5.6 TB/s, without the weight's 37.7; 32 bits 71, 6.1); beyond, 32 entries a
-// thread pass its registers (2048 x 12288 74 us, 2.8).
+// thread pass its 128 registers (844 to 1220 bytes in local memory; 2048 x 12288 74 us, 2.8).
 struct Act8NormGrad {
     Act8Mat s, d_out, d_sum, d_x;
     const void* weight;
